@@ -463,6 +463,121 @@ int mvla_masked_prefill_step(mvla_ctx* ctx, const mvla_layer_cfg* cfg,
                              int* rows_out, int32_t* lengths_out);
 
 /* ------------------------------------------------------------------------ */
+/* Answering: key/value cache, attention over it, eviction, token choice    */
+/* ------------------------------------------------------------------------ */
+
+/* A key/value cache of one layer, held in 4 bits.  Per sample and key head, slot t
+ * holds a key row and a value row of dh values in blocks of 32: one code of 4 bits a
+ * value and one power of two a block.
+ *   code  sign (bit 3) and magnitude 0, 1/2, 1, 3/2, 2, 3, 4, 6 (codes 0 .. 7); value
+ *         2i of a row in the low, value 2i+1 in the high half of byte i
+ *   power byte e: 2^(e - 127); 255: every value of the block is NaN
+ * A value is level * power, which bf16 holds exactly.  The rows are packed; the number
+ * of slots in use is not part of the cache but an argument (device int32 [B]) of the
+ * calls, so that layers can share it and a step can be captured into a graph.
+ * All pointers are device pointers, caller-owned; k, v, k_scale, v_scale 16-byte
+ * aligned, pos and weight 4-byte aligned.  Slots that are not in use may hold anything. */
+typedef struct {
+    int B, H_kv;       /* samples, key heads                                            */
+    int dh;            /* head dim: 64 or 128                                           */
+    int capacity;      /* slots per sample, a multiple of 32                            */
+    void* k;           /* uint8 [B, H_kv, capacity, dh/2]  codes                        */
+    void* v;           /* uint8 [B, H_kv, capacity, dh/2]                               */
+    void* k_scale;     /* uint8 [B, H_kv, capacity, dh/32] powers                       */
+    void* v_scale;     /* uint8 [B, H_kv, capacity, dh/32]                              */
+    int32_t* pos;      /* int32 [B, H_kv, capacity] position id of the row              */
+    float* weight;     /* fp32  [B, H_kv, capacity] accumulated attention weight        */
+} mvla_cache4;
+
+/* A bf16 tensor [sample, token, head, dh] by its strides, in elements (any sign). */
+typedef struct {
+    const void* data;
+    int64_t sample, token, head, channel;
+} mvla_rows;
+
+/* Bytes of a context's workspace that the calls below need for caches of B samples, H
+ * query and H_kv key heads of dh values, up to n_q queries a call and max_length slots
+ * (not less than mvla_create asks for).  A context that runs layers as well takes the
+ * larger of this and mvla_workspace_bytes.  0 for arguments that no call takes. */
+size_t mvla_cache_workspace_bytes(int B, int H, int H_kv, int dh, int n_q, int max_length);
+
+/* Write new key and value rows into a cache: row i < c_b of sample b goes to slot
+ * length[b] - c_b + i, with c_b = n_new[b] (n for n_new = NULL; clamped to [0, n]):
+ * `length` counts the new rows already.  Per block of 32 values, the power is the
+ * smallest 2^(e-127), e >= 0, under which the largest magnitude is below 7; each value
+ * is rounded to the nearest level, ties to the even code.  A block that holds an
+ * infinity or a NaN is written as NaN throughout.  The rows' pos is set and their
+ * weight cleared; rows that would fall outside [0, capacity) are not written.
+ * k, v  : bf16 [B, n, H_kv, dh] by their strides.  channel == 1 with 16-byte aligned
+ *         rows is the fast form, any other is taken as well.
+ * pos   : device int32 [B, n].  length: device int32 [B].  n_new: device int32 [B] or
+ *         NULL. */
+int mvla_cache_append(mvla_ctx* ctx, const mvla_cache4* cache, const mvla_rows* k, const mvla_rows* v,
+                      const int32_t* pos, int n, const int32_t* n_new, const int32_t* length);
+
+/* Read rows back: slots first[b] .. first[b] + n - 1 of every sample and key head as
+ * bf16 (exact).  Slots outside [0, capacity) read as zero.
+ * first: device int32 [B] or NULL (0).  k_out, v_out: device bf16 [B, H_kv, n, dh],
+ * 16-byte aligned. */
+int mvla_cache_read(mvla_ctx* ctx, const mvla_cache4* cache, const int32_t* first, int n, void* k_out,
+                    void* v_out);
+
+/* Attention of n_q queries a sample over its cache,
+ *     out = sum_t p_t v_t,   p = softmax_t(scale * q . k_t),
+ * query head h reading key head h / (H / H_kv).  Query i < c_b of sample b sees the
+ * slots t < length[b] - c_b + i + 1 (c_b as above: the new rows are the last ones and
+ * see each other causally; everything before them in any order).  Rows that see nothing
+ * (length 0, i >= c_b) are written as zeros.  A slot that a query does not see has no
+ * part in its result, whatever it holds.
+ * accumulate != 0: weight[b, g, t] += sum of p_t over the queries and the query heads of
+ * key head g, for t < length[b]; sums are formed in a fixed order.
+ * q, out: bf16 [B, n_q, H, dh] by their strides, channel == 1, 16-byte aligned rows;
+ *         must not overlap.  length: device int32 [B], clamped to [0, max_length].
+ * max_length: the largest length that the call has to expect, at most the capacity (it
+ *         sizes the launch).  scale: finite, > 0.
+ * Products of bf16 queries with the cache's exact values, 32-bit sums; probabilities are
+ * rounded to bf16 for the second product only. */
+int mvla_cache_attention(mvla_ctx* ctx, const mvla_cache4* cache, const mvla_rows* q, int H, int n_q,
+                         const int32_t* n_new, const int32_t* length, int max_length, float scale,
+                         int accumulate, const mvla_rows* out);
+
+/* Keep at most `budget` rows per sample and key head: the first in the order (position
+ * below first_pos or at least recent_from[b], then accumulated weight, then lower slot).
+ * Weights that are negative or NaN count as 0.  A sample of at most `budget` rows keeps
+ * all.  With n the new length min(length[b], budget), a kept row of a slot below n stays
+ * there; the others go, in ascending order, to the slots below n that are free, in
+ * ascending order.  (So a step that evicts one row moves at most one.)
+ * dst may be src itself (in place), or a cache of another capacity >= budget that shares
+ * no memory with it (all kept rows are copied; src is only read).
+ * length: device int32 [B]; recent_from: device int32 [B] or NULL (no recent rows).
+ * length_out: device int32 [B], new lengths; must not be `length`.
+ * kept: device int32 [B, H_kv, budget]: slot of src that each slot of dst holds, -1
+ *       beyond the new length. */
+int mvla_cache_evict(mvla_ctx* ctx, const mvla_cache4* src, const mvla_cache4* dst,
+                     const int32_t* length, int max_length, int budget, int first_pos,
+                     const int32_t* recent_from, int32_t* length_out, int32_t* kept);
+
+/* Choose the next token of each row of logits.  The tokens in descending order (equal
+ * logits: lower index first), weights w = exp((x - max) / temperature):
+ *   top_k > 0 : the first top_k stay;
+ *   top_p < 1 : of those a token stays while less than top_p of their total weight comes
+ *               before it (at least one stays);
+ *   min_p > 0 : of those the ones with w >= min(min_p, 1) stay.
+ * token = the first in ascending index at which the running sum of the weights that
+ * stay exceeds u times their total; prob = its share of that total.  temperature not
+ * above 0 (or NaN): the first token of the order, prob 1.  NaN logits are never chosen;
+ * +inf ones share everything; a row without any logit above -inf gives token -1, prob 0.
+ * Weights are summed in units of 2^-40 of the largest, exactly: results do not depend on
+ * any order of summation.
+ * logits : device, bf16 (half != 0) or fp32 [B, V], rows row_stride elements apart.
+ * temperature, top_p, min_p: device fp32 [B] or NULL (1; 1; 0); top_k: device int32 [B]
+ *          or NULL (0); u: device fp32 [B], uniform in [0, 1) (clamped).
+ * token: device int32 [B]; prob: device fp32 [B] or NULL.  V <= 2^22. */
+int mvla_sample(mvla_ctx* ctx, const void* logits, int half, int64_t row_stride, int B, int V,
+                const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
+                const float* u, int32_t* token, float* prob);
+
+/* ------------------------------------------------------------------------ */
 /* Measurement (the paper's overhead study, Table 4, reports the pruning    */
 /* method's own cost apart from the step latency; these calls give the same */
 /* split per kernel)                                                        */
@@ -480,11 +595,12 @@ int mvla_profile_enable(mvla_ctx* ctx, uint32_t kernel_mask, int max_records);
  * Clears the record list. */
 int mvla_profile_read(mvla_ctx* ctx, int capacity, int32_t* ids, int32_t* tags, float* ms,
                       int32_t* n_out);
-/* Name of kernel id 0..18 ("rmsnorm", "gemm_qkv", "score_probs",
+/* Name of kernel id 0..23 ("rmsnorm", "gemm_qkv", "score_probs",
  * "attention", "gemm_o", "rmsnorm_mlp", "gemm_gateup", "gemm_down", "salience",
  * "budget", "select", "compact", "rope_table", "prune_fused", "smooth",
- * "decompose", "feature_share", "candidate_masks", "mask_indices"), "?"
- * otherwise.  In mvla_prefill and mvla_masked_prefill_step a "compact" of up to
+ * "decompose", "feature_share", "candidate_masks", "mask_indices",
+ * "cache_append", "cache_read", "cache_attention", "cache_evict", "sample"; the last
+ * five may hold several launches), "?" otherwise.  In mvla_prefill and mvla_masked_prefill_step a "compact" of up to
  * 4 Mi kept values writes the next layer's first norm too; no "rmsnorm" follows.
  * Rows of up to 384 values may be normalised by the gate/up projection itself (as the
  * choice by size has it): no "rmsnorm_mlp" then, its time is in "gemm_gateup". */

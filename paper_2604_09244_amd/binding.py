@@ -27,6 +27,8 @@ EXPORTS = [
     "mvla_candidate_masks", "mvla_mask_indices", "mvla_prefill_layer_salience",
     "mvla_prefill_layer_prune", "mvla_tune_layers", "mvla_tuned_choice",
     "mvla_set_gemm_choice", "mvla_prefill", "mvla_peak_probe", "mvla_salience_noalloc", "mvla_masked_prefill_step",
+    "mvla_cache_workspace_bytes", "mvla_cache_append", "mvla_cache_read", "mvla_cache_attention",
+    "mvla_cache_evict", "mvla_sample",
 ]
 
 
@@ -95,6 +97,19 @@ class MaskedBuffers(C.Structure):
                 ("kept_len", C.c_void_p), ("kept_idx", C.c_void_p), ("pos_kept", C.c_void_p)]
 
 
+class Cache4C(C.Structure):
+    """mvla_cache4."""
+    _fields_ = [("B", C.c_int), ("H_kv", C.c_int), ("dh", C.c_int), ("capacity", C.c_int),
+                ("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p),
+                ("v_scale", C.c_void_p), ("pos", C.c_void_p), ("weight", C.c_void_p)]
+
+
+class Rows(C.Structure):
+    """mvla_rows: a bf16 tensor [sample, token, head, dh] by its strides."""
+    _fields_ = [("data", C.c_void_p), ("sample", C.c_int64), ("token", C.c_int64),
+                ("head", C.c_int64), ("channel", C.c_int64)]
+
+
 PROBE_READ, PROBE_COPY, PROBE_MFMA, PROBE_LAUNCH = 0, 1, 2, 3
 
 
@@ -152,6 +167,14 @@ def load() -> C.CDLL:
     lib.mvla_candidate_masks.argtypes = [vp, vp, vp, vp, i, i, i, C.POINTER(MaskRules), vp, vp, vp,
                                          vp]
     lib.mvla_mask_indices.argtypes = [vp, vp, vp, i, i, i, i, vp]
+    cache, rows = C.POINTER(Cache4C), C.POINTER(Rows)
+    lib.mvla_cache_workspace_bytes.restype = sz
+    lib.mvla_cache_workspace_bytes.argtypes = [i] * 6
+    lib.mvla_cache_append.argtypes = [vp, cache, rows, rows, vp, i, vp, vp]
+    lib.mvla_cache_read.argtypes = [vp, cache, vp, i, vp, vp]
+    lib.mvla_cache_attention.argtypes = [vp, cache, rows, i, i, vp, vp, i, f, i, rows]
+    lib.mvla_cache_evict.argtypes = [vp, cache, cache, vp, i, i, i, vp, vp, vp]
+    lib.mvla_sample.argtypes = [vp, vp, i, C.c_int64, i, i, vp, vp, vp, vp, vp, vp, vp]
     lib.mvla_profile_enable.argtypes = [vp, C.c_uint32, i]
     lib.mvla_profile_read.argtypes = [vp, i, vp, vp, vp, vp]
     lib.mvla_kernel_name.restype = C.c_char_p
@@ -197,11 +220,47 @@ def pack_layer(w: Dict[str, torch.Tensor]) -> Dict[str, torch.Tensor]:
                 g_mlp=w["g_mlp"].contiguous())
 
 
+def _rows(t: torch.Tensor) -> Rows:
+    """Description of a bf16 tensor [B, tokens, heads, dh] of any strides."""
+    assert t.is_cuda and t.dtype == torch.bfloat16 and t.dim() == 4, (t.device, t.dtype, t.shape)
+    return Rows(t.data_ptr(), *t.stride())
+
+
+class Cache4:
+    """A layer's key/value cache held in 4 bits (mvla_cache4) and the tensors that it lies in.
+    ``Cache4.empty`` allocates them."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor,
+                 v_scale: torch.Tensor, pos: torch.Tensor, weight: torch.Tensor):
+        B, H, cap, half = _dev(k, torch.uint8).shape
+        dh = 2 * half
+        assert _dev(v, torch.uint8).shape == k.shape
+        for s in (k_scale, v_scale):
+            assert _dev(s, torch.uint8).shape == (B, H, cap, dh // 32), s.shape
+        assert _dev(pos, torch.int32).shape == _dev(weight, torch.float32).shape == (B, H, cap)
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.pos, self.weight = pos, weight
+        self.B, self.H_kv, self.dh, self.capacity = B, H, dh, cap
+        self._c = Cache4C(B, H, dh, cap, k.data_ptr(), v.data_ptr(), k_scale.data_ptr(),
+                          v_scale.data_ptr(), pos.data_ptr(), weight.data_ptr())
+        self._ref = C.byref(self._c)
+
+    @classmethod
+    def empty(cls, B: int, H_kv: int, dh: int, capacity: int, device=None) -> "Cache4":
+        """Room for ``capacity`` rows (rounded up to a multiple of 32) per sample and key head."""
+        cap = (capacity + 31) // 32 * 32
+        new = lambda n, dt: torch.empty(B, H_kv, cap, *n, dtype=dt, device=device or "cuda")
+        u8 = torch.uint8
+        return cls(new((dh // 2,), u8), new((dh // 2,), u8), new((dh // 32,), u8),
+                   new((dh // 32,), u8), new((), torch.int32), new((), torch.float32))
+
+
 class Context:
-    """Owns a device workspace and a library context bound to the current stream."""
+    """Owns a device workspace and a library context bound to the current stream.
+    ``min_bytes``: at least so much workspace (the cache's calls: see ``cache_bytes``)."""
 
     def __init__(self, B: int, S: int, D: int, H: int, F: int, n_query_tail: int = 0,
-                 device: Optional[torch.device] = None):
+                 device: Optional[torch.device] = None, min_bytes: int = 0):
         lib = load()
         if not torch.cuda.is_available():
             raise RuntimeError("no GPU visible: the HIP path has no CPU fallback")
@@ -209,6 +268,30 @@ class Context:
         nbytes = lib.mvla_workspace_bytes(B, S, D, H, F, n_query_tail)
         if nbytes == 0:
             raise MvlaError(-1, "mvla_workspace_bytes")
+        self._create(max(nbytes, min_bytes))
+
+    @staticmethod
+    def cache_bytes(B: int, H: int, H_kv: int, n_q: int, max_length: int, dh: int) -> int:
+        """mvla_cache_workspace_bytes."""
+        nbytes = load().mvla_cache_workspace_bytes(B, H, H_kv, dh, n_q, max_length)
+        if nbytes == 0:
+            raise MvlaError(-1, "mvla_cache_workspace_bytes")
+        return nbytes
+
+    @classmethod
+    def for_cache(cls, B: int, H: int, H_kv: int, n_q: int, max_length: int, dh: int,
+                  device: Optional[torch.device] = None) -> "Context":
+        """A context for the calls on caches (and the token choice) alone: no layer runs in it."""
+        self = cls.__new__(cls)
+        nbytes = cls.cache_bytes(B, H, H_kv, n_q, max_length, dh)
+        if not torch.cuda.is_available():
+            raise RuntimeError("no GPU visible: the HIP path has no CPU fallback")
+        self.device = torch.device("cuda", torch.cuda.current_device()) if device is None else device
+        self._create(nbytes)
+        return self
+
+    def _create(self, nbytes: int):
+        lib = load()
         self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
         self._h = C.c_void_p()
         stream = torch.cuda.current_stream(self.device).cuda_stream
@@ -476,6 +559,93 @@ class Context:
         _check(load().mvla_tuned_choice(self._h, M, N, K, epilogue, C.byref(c), C.byref(p)),
                "mvla_tuned_choice")
         return c.value, p.value
+
+    # ---- answering -----------------------------------------------------------
+    def cache_append(self, cache: Cache4, k: torch.Tensor, v: torch.Tensor, pos: torch.Tensor,
+                     length: torch.Tensor, n_new: Optional[torch.Tensor] = None):
+        """Write rows k, v [B, n, H_kv, dh] (bf16, any strides) as the last of each sample's
+        ``length`` (which counts them already), n_new[b] of them where given."""
+        B, n, H, dh = k.shape
+        assert k.shape == v.shape and (B, H, dh) == (cache.B, cache.H_kv, cache.dh), k.shape
+        assert _dev(pos, torch.int32).shape == (B, n) and _dev(length, torch.int32).shape == (B,)
+        assert n_new is None or _dev(n_new, torch.int32).shape == (B,)
+        _check(load().mvla_cache_append(self._h, cache._ref, C.byref(_rows(k)), C.byref(_rows(v)),
+                                        pos.data_ptr(), n, _ptr(n_new), length.data_ptr()),
+               "mvla_cache_append")
+
+    def cache_read(self, cache: Cache4, first: Optional[torch.Tensor], n: int, out=None):
+        """Rows first[b] .. first[b] + n - 1 (first None: from 0) as bf16 (k, v) [B, H_kv, n, dh]."""
+        assert first is None or _dev(first, torch.int32).shape == (cache.B,)
+        shape = (cache.B, cache.H_kv, n, cache.dh)
+        k, v = out if out is not None else (
+            torch.empty(shape, dtype=torch.bfloat16, device=cache.k.device) for _ in range(2))
+        assert _dev(k, torch.bfloat16).shape == _dev(v, torch.bfloat16).shape == shape
+        _check(load().mvla_cache_read(self._h, cache._ref, _ptr(first), n, k.data_ptr(),
+                                      v.data_ptr()), "mvla_cache_read")
+        return k, v
+
+    def cache_attention(self, cache: Cache4, q: torch.Tensor, length: torch.Tensor,
+                        n_new: Optional[torch.Tensor] = None, max_length: Optional[int] = None,
+                        scale: Optional[float] = None, accumulate: bool = False,
+                        out: Optional[torch.Tensor] = None):
+        """Attention of q [B, n_q, H, dh] (bf16) over the cache; ``accumulate`` adds the
+        probabilities to the rows' weights.  ``max_length``: a bound on ``length`` (default: the
+        capacity).  Returns out [B, n_q, H, dh]."""
+        B, n_q, H, dh = q.shape
+        assert (B, dh) == (cache.B, cache.dh) and _dev(length, torch.int32).shape == (B,)
+        assert n_new is None or _dev(n_new, torch.int32).shape == (B,)
+        if out is None:
+            out = torch.empty(B, n_q, H, dh, dtype=torch.bfloat16, device=q.device)
+        assert out.shape == q.shape
+        _check(load().mvla_cache_attention(self._h, cache._ref, C.byref(_rows(q)), H, n_q,
+                                           _ptr(n_new), length.data_ptr(),
+                                           cache.capacity if max_length is None else max_length,
+                                           dh ** -0.5 if scale is None else scale,
+                                           int(accumulate), C.byref(_rows(out))),
+               "mvla_cache_attention")
+        return out
+
+    def cache_evict(self, src: Cache4, dst: Cache4, length: torch.Tensor, budget: int,
+                    first_pos: int = 0, recent_from: Optional[torch.Tensor] = None,
+                    max_length: Optional[int] = None, out=None):
+        """Keep the ``budget`` rows of highest accumulated weight (those of positions below
+        first_pos or from recent_from[b] on before all others), in dst: src itself or a cache
+        that shares no memory with it.  Returns (kept [B, H_kv, budget], new lengths [B])."""
+        B = src.B
+        assert _dev(length, torch.int32).shape == (B,)
+        assert recent_from is None or _dev(recent_from, torch.int32).shape == (B,)
+        kept, new = out if out is not None else (
+            torch.empty(B, src.H_kv, budget, dtype=torch.int32, device=length.device),
+            torch.empty(B, dtype=torch.int32, device=length.device))
+        assert _dev(kept, torch.int32).shape == (B, src.H_kv, budget)
+        assert _dev(new, torch.int32).shape == (B,)
+        _check(load().mvla_cache_evict(self._h, src._ref, dst._ref, length.data_ptr(),
+                                       src.capacity if max_length is None else max_length, budget,
+                                       first_pos, _ptr(recent_from), new.data_ptr(),
+                                       kept.data_ptr()), "mvla_cache_evict")
+        return kept, new
+
+    def sample(self, logits: torch.Tensor, u: torch.Tensor,
+               temperature: Optional[torch.Tensor] = None, top_k: Optional[torch.Tensor] = None,
+               top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None,
+               out=None):
+        """Next token of each row of logits [B, V] (bf16 or fp32, rows of any stride) from one
+        uniform number a row; the settings are per row, None leaves a filter out.  Returns
+        (token int32 [B], its probability among those that could be chosen fp32 [B])."""
+        B, V = logits.shape
+        half = logits.dtype == torch.bfloat16
+        assert logits.is_cuda and (half or logits.dtype == torch.float32), logits.dtype
+        assert logits.stride(1) == 1 or V == 1, logits.stride()
+        for t, dt in ((u, torch.float32), (temperature, torch.float32), (top_k, torch.int32),
+                      (top_p, torch.float32), (min_p, torch.float32)):
+            assert t is None or _dev(t, dt).shape == (B,)
+        token, prob = out if out is not None else (
+            torch.empty(B, dtype=torch.int32, device=logits.device),
+            torch.empty(B, dtype=torch.float32, device=logits.device))
+        _check(load().mvla_sample(self._h, logits.data_ptr(), int(half), logits.stride(0), B, V,
+                                  _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p),
+                                  u.data_ptr(), token.data_ptr(), _ptr(prob)), "mvla_sample")
+        return token, prob
 
     def peak_probe(self, kind: int, buf: Optional[torch.Tensor], reps: int = 10) -> float:
         """Measured rate of a probe kernel (synchronises): GB/s for PROBE_READ / PROBE_COPY,

@@ -108,7 +108,8 @@ struct Timed {
 const char* const kKernelNames[KID_COUNT] = {
     "rmsnorm", "gemm_qkv", "score_probs", "attention", "gemm_o", "rmsnorm_mlp",
     "gemm_gateup", "gemm_down", "salience", "budget", "select", "compact", "rope_table",
-    "prune_fused", "smooth", "decompose", "feature_share", "candidate_masks", "mask_indices"};
+    "prune_fused", "smooth", "decompose", "feature_share", "candidate_masks", "mask_indices",
+    "cache_append", "cache_read", "cache_attention", "cache_evict", "sample"};
 
 }  // namespace
 
@@ -1007,6 +1008,153 @@ int mvla_score_only(mvla_ctx* ctx, const mvla_layer_cfg* cfg, const mvla_layer_w
     TIMED(ctx, KID_SCORE_PROBS, M,
           launch_score_probs(q_buf, D, true, k_buf, D, key_bias, B, S, H, dh, n_query_tail,
                              probs_out, 0, score_tile_queries(B, H, S, n_query_tail, false), st));
+    return MVLA_OK;
+}
+
+// ---------------------------------------------------------------------------
+// Answering: the 4-bit cache, attention over it, eviction, token choice
+namespace {
+
+constexpr int kMaxGrid = 65535;   // of the second and third launch axes
+
+int check_cache(const mvla_cache4* c) {
+    if (!c || !c->k || !c->v || !c->k_scale || !c->v_scale || !c->pos || !c->weight) return MVLA_EINVAL;
+    if (c->B <= 0 || c->H_kv <= 0 || c->capacity <= 0 || c->capacity % 32 != 0) return MVLA_EINVAL;
+    if (c->dh != 64 && c->dh != 128) return MVLA_EUNSUPPORTED;
+    if (c->B > kMaxGrid || c->H_kv > kMaxGrid / 2) return MVLA_EUNSUPPORTED;
+    if (!aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->k_scale, 16) || !aligned(c->v_scale, 16) ||
+        !aligned(c->pos, 4) || !aligned(c->weight, 4))
+        return MVLA_EINVAL;
+    return MVLA_OK;
+}
+
+CacheView cache_view(const mvla_cache4& c) {
+    auto u8 = [](void* p) { return static_cast<uint8_t*>(p); };
+    return {u8(c.k), u8(c.v), u8(c.k_scale), u8(c.v_scale), c.pos, c.weight, c.B, c.H_kv, c.dh, c.capacity};
+}
+
+CacheRows cache_rows(const mvla_rows& r) {
+    return {static_cast<const bf16_t*>(r.data), r.sample, r.token, r.head, r.channel};
+}
+
+// whether two memory ranges touch
+bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+    const char *x = static_cast<const char*>(a), *y = static_cast<const char*>(b);
+    return x < y + nb && y < x + na;
+}
+
+bool caches_overlap(const mvla_cache4& a, const mvla_cache4& b) {
+    auto parts = [](const mvla_cache4& c, const void** p, size_t* n) {
+        const size_t rows = (size_t)c.B * c.H_kv * c.capacity;
+        const void* at[6] = {c.k, c.v, c.k_scale, c.v_scale, c.pos, c.weight};
+        const size_t bytes[6] = {(size_t)c.dh / 2, (size_t)c.dh / 2, (size_t)c.dh / 32, (size_t)c.dh / 32, 4, 4};
+        for (int i = 0; i < 6; ++i) p[i] = at[i], n[i] = rows * bytes[i];
+    };
+    const void *p[6], *q[6];
+    size_t n[6], m[6];
+    parts(a, p, n);
+    parts(b, q, m);
+    for (int i = 0; i < 6; ++i)
+        for (int j = 0; j < 6; ++j)
+            if (overlap(p[i], n[i], q[j], m[j])) return true;
+    return false;
+}
+
+bool same_cache(const mvla_cache4& a, const mvla_cache4& b) {
+    return a.k == b.k && a.v == b.v && a.k_scale == b.k_scale && a.v_scale == b.v_scale && a.pos == b.pos &&
+           a.weight == b.weight && a.B == b.B && a.H_kv == b.H_kv && a.dh == b.dh && a.capacity == b.capacity;
+}
+
+}  // namespace
+
+size_t mvla_cache_workspace_bytes(int B, int H, int H_kv, int dh, int n_q, int max_length) {
+    if (B <= 0 || H <= 0 || H_kv <= 0 || H % H_kv != 0 || n_q <= 0 || max_length <= 0) return 0;
+    if (dh != 64 && dh != 128) return 0;
+    const size_t attention = cache_attention_bytes(B, H, H_kv, dh, n_q, max_length, true);
+    const size_t evict = (size_t)B * H_kv * max_length * 4;
+    return kCounterBytes + gemm_partial_bytes() + align_up(attention > evict ? attention : evict, 256) + 256;
+}
+
+int mvla_cache_append(mvla_ctx* ctx, const mvla_cache4* cache, const mvla_rows* k, const mvla_rows* v,
+                      const int32_t* pos, int n, const int32_t* n_new, const int32_t* length) {
+    if (!ctx || n < 0) return MVLA_EINVAL;
+    if (int rc = check_cache(cache)) return rc;
+    if (n == 0) return MVLA_OK;   // (an empty tensor has no address)
+    if (!k || !v || !k->data || !v->data || !pos || !length) return MVLA_EINVAL;
+    if (!aligned(k->data, 2) || !aligned(v->data, 2)) return MVLA_EINVAL;
+    if ((uint64_t)n * cache->H_kv * (cache->dh / 8) >= (uint64_t)1 << 31) return MVLA_EUNSUPPORTED;
+    int rc;
+    TIMED(ctx, KID_CACHE_APPEND, cache->B * n,
+          launch_cache_append(cache_view(*cache), cache_rows(*k), cache_rows(*v), pos, n, n_new, length, ctx->stream));
+    return MVLA_OK;
+}
+
+int mvla_cache_read(mvla_ctx* ctx, const mvla_cache4* cache, const int32_t* first, int n, void* k_out,
+                    void* v_out) {
+    if (!ctx || n < 0) return MVLA_EINVAL;
+    if (int rc = check_cache(cache)) return rc;
+    if (n == 0) return MVLA_OK;
+    if (!k_out || !v_out) return MVLA_EINVAL;
+    if (!aligned(k_out, 16) || !aligned(v_out, 16)) return MVLA_EINVAL;
+    if ((uint64_t)n * (cache->dh / 8) >= (uint64_t)1 << 31) return MVLA_EUNSUPPORTED;
+    int rc;
+    TIMED(ctx, KID_CACHE_READ, cache->B * n,
+          launch_cache_read(cache_view(*cache), first, n, static_cast<bf16_t*>(k_out), static_cast<bf16_t*>(v_out),
+                            ctx->stream));
+    return MVLA_OK;
+}
+
+static int check_attention(const mvla_ctx* ctx, const mvla_cache4* cache, const mvla_rows* q, int H, int n_q,
+                           const int32_t* length, int max_length, float scale, const mvla_rows* out) {
+    if (!ctx || !q || !out || !q->data || !out->data || !length) return MVLA_EINVAL;
+    if (int rc = check_cache(cache)) return rc;
+    if (H <= 0 || H % cache->H_kv != 0 || n_q <= 0 || max_length <= 0 || max_length > cache->capacity) return MVLA_EINVAL;
+    if (!(scale > 0.f) || !(scale <= 3.0e38f)) return MVLA_EINVAL;
+    if (!cache_rows_wide(cache_rows(*q)) || !cache_rows_wide(cache_rows(*out))) return MVLA_EINVAL;
+    // (rows of a key head, as the kernels count them)
+    if ((int64_t)n_q * (H / cache->H_kv) > 128 * (int64_t)kMaxGrid) return MVLA_EUNSUPPORTED;
+    return MVLA_OK;
+}
+
+int mvla_cache_attention(mvla_ctx* ctx, const mvla_cache4* cache, const mvla_rows* q, int H, int n_q,
+                         const int32_t* n_new, const int32_t* length, int max_length, float scale,
+                         int accumulate, const mvla_rows* out) {
+    if (int rc = check_attention(ctx, cache, q, H, n_q, length, max_length, scale, out)) return rc;
+    if (cache_attention_bytes(cache->B, H, cache->H_kv, cache->dh, n_q, max_length, accumulate != 0) > ctx->scratch_bytes)
+        return MVLA_ENOMEM;
+    int rc;
+    const CacheAttention a = {cache_rows(*q), cache_rows(*out), length, n_new, H, n_q, max_length, accumulate, scale};
+    TIMED(ctx, KID_CACHE_ATTENTION, cache->B * n_q, launch_cache_attention(cache_view(*cache), a, ctx->scratch, ctx->stream));
+    return MVLA_OK;
+}
+
+int mvla_cache_evict(mvla_ctx* ctx, const mvla_cache4* src, const mvla_cache4* dst,
+                     const int32_t* length, int max_length, int budget, int first_pos,
+                     const int32_t* recent_from, int32_t* length_out, int32_t* kept) {
+    if (!ctx || !length || !length_out || length == length_out || !kept) return MVLA_EINVAL;
+    if (int rc = check_cache(src)) return rc;
+    if (int rc = check_cache(dst)) return rc;
+    if (src->B != dst->B || src->H_kv != dst->H_kv || src->dh != dst->dh) return MVLA_EINVAL;
+    if (budget <= 0 || budget > dst->capacity || max_length <= 0 || max_length > src->capacity) return MVLA_EINVAL;
+    if (!same_cache(*src, *dst) && caches_overlap(*src, *dst)) return MVLA_EINVAL;
+    if ((size_t)src->B * src->H_kv * (budget < max_length ? budget : max_length) * 4 > ctx->scratch_bytes) return MVLA_ENOMEM;
+    if ((uint64_t)budget * (src->dh / 16) >= (uint64_t)1 << 31) return MVLA_EUNSUPPORTED;
+    int rc;
+    TIMED(ctx, KID_CACHE_EVICT, src->B,
+          launch_cache_evict(cache_view(*src), cache_view(*dst), length, max_length, budget, first_pos, recent_from,
+                             length_out, kept, reinterpret_cast<int32_t*>(ctx->scratch), ctx->stream));
+    return MVLA_OK;
+}
+
+int mvla_sample(mvla_ctx* ctx, const void* logits, int half, int64_t row_stride, int B, int V,
+                const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
+                const float* u, int32_t* token, float* prob) {
+    if (!ctx || !logits || !u || !token) return MVLA_EINVAL;
+    if (B <= 0 || V <= 0 || !aligned(logits, half ? 2 : 4)) return MVLA_EINVAL;
+    if (V > (1 << 22)) return MVLA_EUNSUPPORTED;   // (sums of weights in 64 bits)
+    int rc;
+    TIMED(ctx, KID_SAMPLE, B, launch_sample(logits, half != 0, row_stride, B, V, temperature, top_k, top_p, min_p, u, token,
+                                            prob, ctx->stream));
     return MVLA_OK;
 }
 

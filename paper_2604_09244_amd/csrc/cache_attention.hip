@@ -1,0 +1,754 @@
+// Attention over the key/value cache held in 4 bits.
+//
+// o[r] = sum_t p[r][t] v[t],  p[r] = softmax over the slots t that row r sees of scale * q[r].k[t].  A row is a query
+// and one of the query heads that share a key head (r = query * group + head of the group); it sees the slots below
+// its limit.  Both products are computed transposed (S^T = K Q^T, O^T = V^T P^T), so that a lane's column is a row r
+// and the logits that a lane holds are the operand that the second product takes from it.
+#include "common.h"
+#include "fp4.h"
+#include "wave.h"
+
+#include <type_traits>
+
+namespace mvla {
+
+// What a sample's rows see.
+struct Span {
+    int len, count;   // slots in use, new rows (the last ones)
+};
+__device__ __forceinline__ Span sample_span(const CacheAttention& a, int capacity, int b) {
+    Span s;
+    s.len = min(min(max(a.len[b], 0), capacity), a.max_len);
+    s.count = a.n_new ? min(max(a.n_new[b], 0), a.n_q) : a.n_q;
+    return s;
+}
+// slots that query i sees
+__device__ __forceinline__ int seen_by(const Span& s, int i) {
+    return i < s.count ? min(max(s.len - s.count + i + 1, 0), s.len) : 0;
+}
+
+// largest of the four lanes that share a column (lane distances 16 and 32), in all of them
+__device__ __forceinline__ float column_max(float x) {
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float column_sum(float x) {
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+__device__ __forceinline__ uint32_t column_or(uint32_t x) {
+    const auto a = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    x = a[0] | a[1];
+    const auto b = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    return b[0] | b[1];
+}
+
+// ---- few rows ----------------------------------------------------------------------------------------------------
+// Up to 16 rows a key head: a wave takes 32 slots at a time straight from memory to registers, nothing passes through
+// LDS.  The slots of a step are dealt to the operand rows so that no lane needs another's data:
+//   K: row r of tile j (of two) is slot 8 (r / 4) + 4 j + r % 4, a lane's k-range the block (or half block) of its
+//      16-lane group: 16 (8) bytes of codes a lane, whole key rows per wave
+//   S^T: a lane of group g then holds the logits of slots 8 g .. 8 g + 7 of its column, in order: its P^T operand
+//   V: lane c of a group takes dims c CH .. c CH + CH - 1 of the group's eight slots; the codes become pairs of dims of
+//      one slot, two permutes turn two slots' pairs into pairs of slots of one dim
+//   O^T: tile d holds dims c CH + d, so a lane ends with CH consecutive dims per register index: whole 16-byte stores
+constexpr int FEW_WAVES = 4, FEW_STEP = 32;
+
+template <int DH>
+struct FewRaw {
+    static constexpr int KW = DH / 32;                       // words of codes a lane and K tile
+    uint32_t k[2][KW], v[8], ks[2], vs[8];
+};
+
+template <int DH>
+__device__ __forceinline__ void few_load(FewRaw<DH>& x, const uint8_t* k, const uint8_t* ks, const uint8_t* v,
+                                         const uint8_t* vs, int slot0, int c, int g) {
+    constexpr int NB = DH / 32;
+    const int kr = slot0 + 8 * (c >> 2) + (c & 3), vr = slot0 + 8 * g;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const size_t at = (size_t)(kr + 4 * j);
+        if constexpr (DH == 128) {
+            const uint4 w = *reinterpret_cast<const uint4*>(k + at * (DH / 2) + g * 16);
+            x.k[j][0] = w.x, x.k[j][1] = w.y, x.k[j][2] = w.z, x.k[j][3] = w.w;
+            x.ks[j] = *reinterpret_cast<const uint32_t*>(ks + at * NB);
+        } else {
+            const uint2 w = *reinterpret_cast<const uint2*>(k + at * (DH / 2) + g * 8);
+            x.k[j][0] = w.x, x.k[j][1] = w.y;
+            x.ks[j] = *reinterpret_cast<const uint16_t*>(ks + at * NB);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint8_t* p = v + (size_t)(vr + i) * (DH / 2) + c * (DH / 32);
+        if constexpr (DH == 128) x.v[i] = *reinterpret_cast<const uint32_t*>(p);
+        else x.v[i] = *reinterpret_cast<const uint16_t*>(p);
+    }
+    const uint4* s = reinterpret_cast<const uint4*>(vs + (size_t)vr * NB);
+    if constexpr (DH == 128) {
+        const uint4 a = s[0], b = s[1];
+        x.vs[0] = a.x, x.vs[1] = a.y, x.vs[2] = a.z, x.vs[3] = a.w;
+        x.vs[4] = b.x, x.vs[5] = b.y, x.vs[6] = b.z, x.vs[7] = b.w;
+    } else {
+        const uint4 a = s[0];
+        x.vs[0] = a.x & 0xffffu, x.vs[1] = a.x >> 16, x.vs[2] = a.y & 0xffffu, x.vs[3] = a.y >> 16;
+        x.vs[4] = a.z & 0xffffu, x.vs[5] = a.z >> 16, x.vs[6] = a.w & 0xffffu, x.vs[7] = a.w >> 16;
+    }
+}
+
+template <int DH>
+__global__ __launch_bounds__(FEW_WAVES * 64) void few_rows_kernel(CacheView cache, CacheAttention a, int group, int splits,
+                                                                  float* __restrict__ part_o, float2* __restrict__ part_ml,
+                                                                  float* __restrict__ logits, int logit_pitch) {
+    constexpr int NB = DH / 32, CH = DH / 16, STEPS = DH / 32;
+    __shared__ alignas(16) float sh_o[FEW_WAVES][16 * DH];
+    __shared__ float sh_m[FEW_WAVES][16], sh_l[FEW_WAVES][16];
+
+    const int split = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c = lane & 15, g = lane >> 4;
+    const Span span = sample_span(a, cache.capacity, b);
+    const int rows = a.n_q * group;
+    const int n_steps = (span.len + FEW_STEP - 1) / FEW_STEP;
+    const int step0 = (int)((int64_t)n_steps * split / splits), step1 = (int)((int64_t)n_steps * (split + 1) / splits);
+
+    const size_t head = (size_t)b * cache.H_kv + h;
+    const uint8_t* k = cache.k + head * cache.capacity * (DH / 2);
+    const uint8_t* v = cache.v + head * cache.capacity * (DH / 2);
+    const uint8_t* ks = cache.k_scale + head * cache.capacity * NB;
+    const uint8_t* vs = cache.v_scale + head * cache.capacity * NB;
+
+    FewRaw<DH> next;
+    if (step0 + wave < step1) few_load<DH>(next, k, ks, v, vs, (step0 + wave) * FEW_STEP, c, g);
+
+    // this lane's column: row c (columns beyond the rows hold zeros and see everything; nobody reads them)
+    const int qi = c / group;
+    const bool real = c < rows;
+    const int limit = real && qi < span.count ? seen_by(span, qi) : span.len;
+    const int least = seen_by(span, 0);       // no row of the sample sees fewer slots
+    uint4 qf[STEPS];
+#pragma unroll
+    for (int st = 0; st < STEPS; ++st) qf[st] = make_uint4(0u, 0u, 0u, 0u);
+    if (real) {
+        const bf16_t* src = a.q.p + b * a.q.sample + qi * a.q.token + (h * group + c % group) * a.q.head +
+                            g * (DH / 4);
+#pragma unroll
+        for (int st = 0; st < STEPS; ++st) qf[st] = *reinterpret_cast<const uint4*>(src + st * 8);
+    }
+    const float scale_log2e = a.scale * 1.4426950408889634f;
+    const int k_blk = DH == 128 ? g : g >> 1, v_blk = DH == 128 ? c >> 2 : c >> 3;
+    float* row_logits = logits ? logits + (head * rows + c) * (size_t)logit_pitch : nullptr;
+
+    f32x4_t o[CH];
+#pragma unroll
+    for (int d = 0; d < CH; ++d) o[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    float run_m = -INFINITY, run_l = 0.f;     // run_l: this lane's share
+    uint32_t not_a_number = 0;                // blocks of a value row that this lane's row sees and that hold none
+
+    for (int step = step0 + wave; step < step1; step += FEW_WAVES) {
+        FewRaw<DH> x = next;
+        if (step + FEW_WAVES < step1) few_load<DH>(next, k, ks, v, vs, (step + FEW_WAVES) * FEW_STEP, c, g);
+        const int slot0 = step * FEW_STEP;
+        // ---- S^T
+        f32x4_t s[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            s[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            const float scale = fp4_scale(x.ks[j], k_blk);
+#pragma unroll
+            for (int st = 0; st < STEPS; ++st) s[j] = mfma16(fp4_values(x.k[j][st], scale), qf[st], s[j]);
+        }
+        const int my0 = slot0 + 8 * g;        // slot of s[0][0]
+        if (row_logits && real) {             // (raw: scaled where they are read)
+            *reinterpret_cast<float4*>(row_logits + my0) = make_float4(s[0][0], s[0][1], s[0][2], s[0][3]);
+            *reinterpret_cast<float4*>(row_logits + my0 + 4) = make_float4(s[1][0], s[1][1], s[1][2], s[1][3]);
+        }
+        // ---- slots that not every row sees, or that hold nothing yet
+        if (slot0 + FEW_STEP > least) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (my0 + i >= limit) s[i >> 2][i & 3] = -INFINITY;
+                if (my0 + i >= span.len) {    // (whatever lies there must not meet a weight of zero: it may be no number)
+                    x.v[i] = 0;
+                    x.vs[i] = 0x7f7f7f7fu;
+                }
+            }
+            // a new row whose values are no numbers reaches the rows that see it, not those before it
+            bool any = false;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int blk = 0; blk < NB; ++blk) any |= ((x.vs[i] >> (8 * blk)) & 0xffu) == 0xffu;
+            if (__any(any)) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+#pragma unroll
+                    for (int blk = 0; blk < NB; ++blk)
+                        if (((x.vs[i] >> (8 * blk)) & 0xffu) == 0xffu) {
+                            if (my0 + i < limit) not_a_number |= 1u << blk;
+                            if (blk == v_blk) {
+                                x.v[i] = 0;
+                                x.vs[i] &= ~(0x80u << (8 * blk));
+                            }
+                        }
+            }
+        }
+        // ---- softmax against the running maximum
+        float top = s[0][0];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) top = fmaxf(top, s[i >> 2][i & 3]);
+        if (__any(top > run_m)) {
+            const float m = fmaxf(run_m, column_max(top));
+            const float f = m == run_m ? 1.f : __builtin_amdgcn_exp2f((run_m - m) * scale_log2e);
+            run_l *= f;
+#pragma unroll
+            for (int d = 0; d < CH; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[d][i] *= f;
+            run_m = m;
+        }
+        const float neg_m = run_m == -INFINITY ? 0.f : -run_m * scale_log2e;   // (a row that has seen nothing yet)
+        float e[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            e[i] = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][i & 3], scale_log2e, neg_m));
+            run_l += e[i];
+        }
+        const uint4 pf = make_uint4(pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3]), pack_bf16x2(e[4], e[5]),
+                                    pack_bf16x2(e[6], e[7]));
+        // ---- O^T: pairs of dims of one slot to pairs of slots of one dim
+        float sc[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sc[i] = fp4_scale(x.vs[i], v_blk);
+        auto pairs = [&](auto sel) __attribute__((always_inline)) {
+            constexpr int E = decltype(sel)::value;
+            uint32_t w[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = fp4_pair<E>(x.v[i], sc[i]);
+            uint4 even, odd;
+            even.x = __builtin_amdgcn_perm(w[1], w[0], 0x05040100u), odd.x = __builtin_amdgcn_perm(w[1], w[0], 0x07060302u);
+            even.y = __builtin_amdgcn_perm(w[3], w[2], 0x05040100u), odd.y = __builtin_amdgcn_perm(w[3], w[2], 0x07060302u);
+            even.z = __builtin_amdgcn_perm(w[5], w[4], 0x05040100u), odd.z = __builtin_amdgcn_perm(w[5], w[4], 0x07060302u);
+            even.w = __builtin_amdgcn_perm(w[7], w[6], 0x05040100u), odd.w = __builtin_amdgcn_perm(w[7], w[6], 0x07060302u);
+            o[2 * E] = mfma16(even, pf, o[2 * E]);
+            o[2 * E + 1] = mfma16(odd, pf, o[2 * E + 1]);
+        };
+        pairs(std::integral_constant<int, 0>{});
+        pairs(std::integral_constant<int, 1>{});
+        if constexpr (CH == 8) {
+            pairs(std::integral_constant<int, 2>{});
+            pairs(std::integral_constant<int, 3>{});
+        }
+    }
+
+    // ---- the waves' parts of a row, joined
+    run_l = column_sum(run_l);
+    not_a_number = column_or(not_a_number);
+    if (not_a_number >> k_blk & 1u)           // (this lane's dims, (4 g + i) CH + d, lie in block k_blk)
+#pragma unroll
+        for (int d = 0; d < CH; ++d) o[d] = f32x4_t{NAN, NAN, NAN, NAN};
+    if (g == 0) {
+        sh_m[wave][c] = run_m;
+        sh_l[wave][c] = run_l;
+    }
+    if (real)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int q = 0; q < CH / 4; ++q)
+                *reinterpret_cast<float4*>(&sh_o[wave][c * DH + (4 * g + i) * CH + 4 * q]) =
+                    make_float4(o[4 * q][i], o[4 * q + 1][i], o[4 * q + 2][i], o[4 * q + 3][i]);
+    __syncthreads();
+    for (int id = tid; id < rows * DH; id += FEW_WAVES * 64) {
+        const int r = id / DH;
+        float m = sh_m[0][r], l = 0.f, acc = 0.f;
+#pragma unroll
+        for (int w = 1; w < FEW_WAVES; ++w) m = fmaxf(m, sh_m[w][r]);
+#pragma unroll
+        for (int w = 0; w < FEW_WAVES; ++w) {
+            const float f = sh_m[w][r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((sh_m[w][r] - m) * scale_log2e);
+            l = fmaf(sh_l[w][r], f, l);
+            acc = fmaf(sh_o[w][id], sh_m[w][r] == -INFINITY ? 1.f : f, acc);
+        }
+        const size_t row = ((size_t)split * cache.B * cache.H_kv + head) * rows + r;
+        part_o[row * DH + id % DH] = acc;
+        if (id % DH == 0) part_ml[row] = make_float2(m, l);
+    }
+}
+
+// ---- the parts of all splits of a row, and the weights ------------------------------------------------------------
+// Workgroup (x, key head, sample): the first x write the rows' outputs, 256 values each; all add the weights of 1024
+// slots to the rows' own, from the logits that the pass over the cache left behind.
+constexpr int JOIN_THREADS = 256, JOIN_SLOTS = 1024;
+
+__global__ __launch_bounds__(JOIN_THREADS) void join_kernel(CacheView cache, CacheAttention a, int group, int splits,
+                                                            const float* __restrict__ part_o, const float2* __restrict__ part_ml,
+                                                            const float* __restrict__ logits, int logit_pitch,
+                                                            float2* __restrict__ row_ml) {
+    const int h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, DH = cache.dh;
+    const Span span = sample_span(a, cache.capacity, b);
+    const int rows = a.n_q * group;
+    const size_t head = (size_t)b * cache.H_kv + h, pitch = (size_t)cache.B * cache.H_kv * rows;
+    const float scale_log2e = a.scale * 1.4426950408889634f;
+    const float2* ml = part_ml + head * rows;
+    auto joined = [&](int r) {
+        float m = -INFINITY, l = 0.f;
+        for (int s = 0; s < splits; ++s) m = fmaxf(m, ml[s * pitch + r].x);
+        for (int s = 0; s < splits; ++s) {
+            const float2 t = ml[s * pitch + r];
+            if (t.x != -INFINITY) l = fmaf(t.y, __builtin_amdgcn_exp2f((t.x - m) * scale_log2e), l);
+            else l += t.y;
+        }
+        return make_float2(m, l);
+    };
+    for (int id = blockIdx.x * JOIN_THREADS + tid; id < rows * DH; id += gridDim.x * JOIN_THREADS) {
+        const int r = id / DH, ch = id % DH, i = r / group;
+        const float2 t = joined(r);
+        float acc = 0.f;
+        for (int s = 0; s < splits; ++s) {
+            const float m = ml[s * pitch + r].x;
+            acc = fmaf(part_o[(s * pitch + head * rows + r) * DH + ch],
+                       m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - t.x) * scale_log2e), acc);
+        }
+        // (a row that sees nothing is zero; one whose logits are all -inf is 0 / 0)
+        const bf16_t o = seen_by(span, i) > 0 ? f32_to_bf16(acc / t.y) : (bf16_t)0;
+        const_cast<bf16_t*>(a.out.p)[b * a.out.sample + i * a.out.token + (h * group + r % group) * a.out.head + ch] = o;
+        if (row_ml && ch == 0) row_ml[head * rows + r] = t;
+    }
+    if (!logits) return;
+    float sum[JOIN_SLOTS / JOIN_THREADS] = {};
+    const int slot0 = blockIdx.x * JOIN_SLOTS + tid;
+    if (blockIdx.x * JOIN_SLOTS >= span.len) return;
+    for (int r = 0; r < rows; ++r) {
+        const int limit = seen_by(span, r / group);
+        const float2 t = joined(r);
+        const float inv = 1.f / t.y, neg_m = -t.x * scale_log2e;
+        const float* x = logits + (head * rows + r) * (size_t)logit_pitch;
+#pragma unroll
+        for (int j = 0; j < JOIN_SLOTS / JOIN_THREADS; ++j) {
+            const int slot = slot0 + j * JOIN_THREADS;
+            if (slot < limit) sum[j] += __builtin_amdgcn_exp2f(fmaf(x[slot], scale_log2e, neg_m)) * inv;
+        }
+    }
+    float* w = cache.weight + head * cache.capacity;
+#pragma unroll
+    for (int j = 0; j < JOIN_SLOTS / JOIN_THREADS; ++j) {
+        const int slot = slot0 + j * JOIN_THREADS;
+        if (slot < span.len) w[slot] += sum[j];
+    }
+}
+
+// ---- many rows -----------------------------------------------------------------------------------------------------
+// 128 rows a workgroup, 32 a wave, 64 slots at a time: the codes become bf16 once per workgroup on their way into LDS
+// (keys row by row, values transposed), two stages deep, the next tile's codes on their way meanwhile.
+constexpr int MANY_THREADS = 256, MANY_ROWS = 128, MANY_KT = 64;
+
+// LDS row r holds slot many_key(r) of a tile (bits 2 and 3 swapped: a lane's eight probabilities of a 16-slot step are
+// then eight consecutive slots); its own inverse
+__device__ __forceinline__ int many_key(int r) { return (r & ~12) | ((r & 4) << 1) | ((r & 8) >> 1); }
+template <int CPR>
+__device__ __forceinline__ int many_swz(int row) {
+    return CPR == 16 ? (row & 15) : ((row >> 1) & 7);
+}
+
+template <int DH>
+struct ManyRaw {
+    uint32_t k[DH / 32], ks, v[8], vs[8];
+};
+
+template <int DH>
+__global__ __launch_bounds__(MANY_THREADS, 2) void many_rows_kernel(CacheView cache, CacheAttention a, int group, int splits,
+                                                                    float* __restrict__ part_o,
+                                                                    float2* __restrict__ part_ml) {
+    constexpr int NB = DH / 32, CPR = DH / 8, STEPS = DH / 16, DB = DH / 32;
+    constexpr int K_SLOTS = MANY_KT * CPR, V_SLOTS = DH * 8, STAGE = K_SLOTS + V_SLOTS;
+    constexpr int KE = DH / 4, VE = DH / 32;   // values of a key row a thread stages; dims of eight value rows
+    extern __shared__ uint4 lds[];
+    __shared__ uint32_t sh_bad[2][8];          // per stage and eight slots: blocks that hold no numbers, a byte a block
+
+    const int h = blockIdx.x, row0 = blockIdx.y * MANY_ROWS, split = blockIdx.z % splits, b = blockIdx.z / splits;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int fr = lane & 31, fg = lane >> 5;
+    const Span span = sample_span(a, cache.capacity, b);
+    const int rows = a.n_q * group;
+    const int my_row = row0 + wave * 32 + fr, my_i = my_row / group;
+    const bool real = my_row < rows;
+    const int seen = real ? seen_by(span, my_i) : 0;
+    // (a row that is none, or that is not among its sample's new ones, takes part as if it saw everything and is not
+    // stored, or stored as zeros)
+    const int limit = real && my_i < span.count ? seen : span.len;
+    // slots that the workgroup's last real row sees, and the fewest that any of its rows does
+    const int last_i = min((min(row0 + MANY_ROWS, rows) - 1) / group, span.count - 1);
+    const int most = last_i * group + group - 1 < row0 ? 0 : seen_by(span, last_i);
+    const int wave_row0 = row0 + wave * 32, wave_last = min((min(wave_row0 + 32, rows) - 1) / group, span.count - 1);
+    const int wave_most = wave_row0 < rows && wave_last * group + group - 1 >= wave_row0 ? seen_by(span, wave_last) : 0;
+    const int least = row0 / group < span.count ? seen_by(span, row0 / group) : span.len;
+    const int n_kt = (most + MANY_KT - 1) / MANY_KT;
+    const int kt0 = (int)((int64_t)n_kt * split / splits), kt1 = (int)((int64_t)n_kt * (split + 1) / splits);
+
+    const size_t head = (size_t)b * cache.H_kv + h;
+    const uint8_t* kp = cache.k + head * cache.capacity * (DH / 2);
+    const uint8_t* vp = cache.v + head * cache.capacity * (DH / 2);
+    const uint8_t* ksp = cache.k_scale + head * cache.capacity * NB;
+    const uint8_t* vsp = cache.v_scale + head * cache.capacity * NB;
+
+    const int k_key = tid >> 2, k_part = tid & 3, k_blk = k_part * KE / 32;
+    const int v_oct = tid >> 5, v_dim = (tid & 31) * VE, v_blk = v_dim / 32;
+    auto load = [&](ManyRaw<DH>& x, int kt) __attribute__((always_inline)) {
+        const int slot0 = kt * MANY_KT;
+        // (a tile ends within the capacity, which is a multiple of 32, or its last half is read from the first)
+        const int ks_ = min(slot0 + k_key, cache.capacity - 1);
+        if constexpr (DH == 128) {
+            const uint4 w = *reinterpret_cast<const uint4*>(kp + (size_t)ks_ * 64 + k_part * 16);
+            x.k[0] = w.x, x.k[1] = w.y, x.k[2] = w.z, x.k[3] = w.w;
+        } else {
+            const uint2 w = *reinterpret_cast<const uint2*>(kp + (size_t)ks_ * 32 + k_part * 8);
+            x.k[0] = w.x, x.k[1] = w.y;
+        }
+        x.ks = ksp[(size_t)ks_ * NB + k_blk];
+        int v0 = slot0 + v_oct * 8;
+        if (v0 >= cache.capacity) v0 -= 32;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint8_t* p = vp + (size_t)(v0 + i) * (DH / 2) + v_dim / 2;
+            if constexpr (DH == 128) x.v[i] = *reinterpret_cast<const uint16_t*>(p);
+            else x.v[i] = *p;
+            x.vs[i] = vsp[(size_t)(v0 + i) * NB + v_blk];
+        }
+    };
+    auto stage_tile = [&](ManyRaw<DH>& x, int kt, int stg) __attribute__((always_inline)) {
+        uint4* Kc = lds + stg * STAGE;
+        uint4* Vc = Kc + K_SLOTS;
+        const float ks = __uint_as_float(x.ks << 23);
+        const int row = many_key(k_key);
+#pragma unroll
+        for (int j = 0; j < KE / 8; ++j)
+            Kc[row * CPR + ((k_part * (KE / 8) + j) ^ many_swz<CPR>(row))] = fp4_values(x.k[j], ks);
+        if (kt * MANY_KT + MANY_KT > least) {       // (wave-uniform) see few_rows_kernel
+            uint32_t bad = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const bool none = kt * MANY_KT + v_oct * 8 + i >= span.len, nan = x.vs[i] == 0xffu;
+                if (nan && !none) bad |= 1u << i;
+                if (none || nan) {
+                    x.v[i] = 0;
+                    x.vs[i] = 0x7fu;
+                }
+            }
+            if (v_dim % 32 == 0) reinterpret_cast<uint8_t*>(&sh_bad[stg][v_oct])[v_blk] = (uint8_t)bad;
+        }
+        uint32_t w[VE / 2][8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float vs = __uint_as_float(x.vs[i] << 23);
+            w[0][i] = fp4_pair<0>(x.v[i], vs);
+            if constexpr (VE == 4) w[1][i] = fp4_pair<1>(x.v[i], vs);
+        }
+#pragma unroll
+        for (int e = 0; e < VE / 2; ++e)
+#pragma unroll
+            for (int o = 0; o < 2; ++o) {
+                const uint32_t sel = o ? 0x07060302u : 0x05040100u;
+                const int dim = v_dim + 2 * e + o;
+                Vc[dim * 8 + (v_oct ^ many_swz<8>(dim))] =
+                    make_uint4(__builtin_amdgcn_perm(w[e][1], w[e][0], sel), __builtin_amdgcn_perm(w[e][3], w[e][2], sel),
+                               __builtin_amdgcn_perm(w[e][5], w[e][4], sel), __builtin_amdgcn_perm(w[e][7], w[e][6], sel));
+            }
+    };
+
+    ManyRaw<DH> raw;
+    if (tid < 16) sh_bad[tid >> 3][tid & 7] = 0;
+    if (kt0 < kt1) load(raw, kt0);
+    uint4 qf[STEPS];
+#pragma unroll
+    for (int st = 0; st < STEPS; ++st) qf[st] = make_uint4(0u, 0u, 0u, 0u);
+    if (real) {
+        const bf16_t* src = a.q.p + b * a.q.sample + my_i * a.q.token + (h * group + my_row % group) * a.q.head + fg * 8;
+#pragma unroll
+        for (int st = 0; st < STEPS; ++st) qf[st] = *reinterpret_cast<const uint4*>(src + st * 16);
+    }
+    const float scale_log2e = a.scale * 1.4426950408889634f;
+    f32x16_t o_acc[DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) o_acc[d][v] = 0.f;
+    float run_m = -INFINITY, run_l = 0.f;
+    uint32_t not_a_number = 0;
+    __syncthreads();
+    if (kt0 < kt1) {
+        stage_tile(raw, kt0, 0);
+        if (kt0 + 1 < kt1) load(raw, kt0 + 1);
+    }
+    int stage = 0;
+    for (int kt = kt0; kt < kt1; ++kt, stage ^= 1) {
+        __syncthreads();      // tile kt is in LDS for every wave; the other stage has been read by all
+        if (kt + 1 < kt1) {
+            stage_tile(raw, kt + 1, stage ^ 1);
+            if (kt + 2 < kt1) load(raw, kt + 2);
+        }
+        const int key0 = kt * MANY_KT;
+        if (key0 >= wave_most) continue;
+        const uint4* Kc = lds + stage * STAGE;
+        const uint4* Vc = Kc + K_SLOTS;
+        f32x16_t s_acc[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) s_acc[t][v] = 0.f;
+#pragma unroll
+        for (int st = 0; st < STEPS; ++st)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const int row = t * 32 + fr;
+                s_acc[t] = mfma32(Kc[row * CPR + ((st * 2 + fg) ^ many_swz<CPR>(row))], qf[st], s_acc[t]);
+            }
+        if (key0 + MANY_KT > least) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int v = 0; v < 16; ++v)
+                    if (key0 + t * 32 + 16 * (v >> 3) + 8 * fg + (v & 7) >= limit) s_acc[t][v] = -INFINITY;
+            uint32_t any = 0;
+#pragma unroll
+            for (int o = 0; o < 8; ++o) any |= sh_bad[stage][o];
+            if (any)
+                for (int i = 0; i < MANY_KT; ++i)
+#pragma unroll
+                    for (int blk = 0; blk < NB; ++blk)
+                        if ((sh_bad[stage][i >> 3] >> (8 * blk + (i & 7)) & 1u) && key0 + i < limit) not_a_number |= 1u << blk;
+        }
+        float tile_m = -INFINITY;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) tile_m = fmaxf(tile_m, s_acc[t][v]);
+        tile_m = fmaxf(tile_m, __shfl_xor(tile_m, 32));
+        const float new_m = fmaxf(run_m, tile_m);
+        const float neg_m = new_m == -INFINITY ? 0.f : -new_m * scale_log2e;
+        float psum = 0.f;
+        uint4 pf[4];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int hh = 0; hh < 2; ++hh) {
+                float e[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    e[i] = __builtin_amdgcn_exp2f(fmaf(s_acc[t][hh * 8 + i], scale_log2e, neg_m));
+                    psum += e[i];
+                }
+                pf[t * 2 + hh] = make_uint4(pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3]), pack_bf16x2(e[4], e[5]),
+                                            pack_bf16x2(e[6], e[7]));
+            }
+        if (__any(new_m != run_m)) {
+            const float corr = new_m == run_m ? 1.f : __builtin_amdgcn_exp2f((run_m - new_m) * scale_log2e);
+            run_l *= corr;
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) o_acc[d][v] *= corr;
+            run_m = new_m;
+        }
+        run_l += psum;
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+            const int row = d * 32 + fr, sw = many_swz<8>(row);
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks) o_acc[d] = mfma32(Vc[row * 8 + ((ks * 2 + fg) ^ sw)], pf[ks], o_acc[d]);
+        }
+    }
+    // ---- this lane: row my_row, dims d 32 + 8 (v / 4) + 4 fg + v % 4
+    const float tot = run_l + __shfl_xor(run_l, 32);
+    if (!real) return;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+        if (not_a_number >> d & 1u)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) o_acc[d][v] = NAN;
+    const size_t row = ((size_t)split * cache.B * cache.H_kv + head) * rows + my_row;
+    if (fg == 0) part_ml[row] = make_float2(run_m, tot);
+    if (splits > 1) {
+        float* orow = part_o + row * DH;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int v4 = 0; v4 < 4; ++v4)
+                *reinterpret_cast<float4*>(orow + d * 32 + 8 * v4 + 4 * fg) =
+                    make_float4(o_acc[d][v4 * 4], o_acc[d][v4 * 4 + 1], o_acc[d][v4 * 4 + 2], o_acc[d][v4 * 4 + 3]);
+        return;
+    }
+    const float inv = 1.0f / tot;
+    bf16_t* orow = const_cast<bf16_t*>(a.out.p) + b * a.out.sample + my_i * a.out.token +
+                   (h * group + my_row % group) * a.out.head;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int v4 = 0; v4 < 4; ++v4) {
+            uint2 w;
+            w.x = pack_bf16x2(o_acc[d][v4 * 4 + 0] * inv, o_acc[d][v4 * 4 + 1] * inv);
+            w.y = pack_bf16x2(o_acc[d][v4 * 4 + 2] * inv, o_acc[d][v4 * 4 + 3] * inv);
+            if (seen == 0) w = make_uint2(0u, 0u);
+            *reinterpret_cast<uint2*>(orow + d * 32 + 8 * v4 + 4 * fg) = w;
+        }
+}
+
+// ---- weights of many rows ----------------------------------------------------------------------------------------
+// The logits once more (keys only), against the rows' final maxima and sums: a wave holds 32 slots' keys in registers
+// and walks the rows, 16 at a time; the columns' sums go over the lanes of a group at the end.  No value is added twice
+// or in another order from run to run.
+constexpr int WEIGH_WAVES = 4;
+
+template <int DH>
+__global__ __launch_bounds__(WEIGH_WAVES * 64) void weigh_kernel(CacheView cache, CacheAttention a, int group,
+                                                                 const float2* __restrict__ row_ml) {
+    constexpr int NB = DH / 32, STEPS = DH / 32;
+    const int h = blockIdx.y, b = blockIdx.z, lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
+    const Span span = sample_span(a, cache.capacity, b);
+    const int slot0 = (blockIdx.x * WEIGH_WAVES + wave) * FEW_STEP;
+    if (slot0 >= span.len) return;
+    const int rows = a.n_q * group;
+    const size_t head = (size_t)b * cache.H_kv + h;
+    uint4 kf[2][STEPS];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const size_t at = head * cache.capacity + slot0 + 8 * (c >> 2) + 4 * j + (c & 3);
+        const float scale = __uint_as_float((uint32_t)cache.k_scale[at * NB + (DH == 128 ? g : g >> 1)] << 23);
+        const uint32_t* p = reinterpret_cast<const uint32_t*>(cache.k + at * (DH / 2) + g * (DH / 8));
+#pragma unroll
+        for (int st = 0; st < STEPS; ++st) kf[j][st] = fp4_values(p[st], scale);
+    }
+    const float scale_log2e = a.scale * 1.4426950408889634f;
+    const int my0 = slot0 + 8 * g;
+    // the first query that sees any of these slots
+    const int first_i = max(0, slot0 - (span.len - span.count)), last_row = min(rows, span.count * group);
+    float sum[8] = {};
+    for (int r0 = first_i * group; r0 < last_row; r0 += 16) {
+        const int r = min(r0 + c, last_row - 1), i = r / group;
+        const bf16_t* src = a.q.p + b * a.q.sample + i * a.q.token + (h * group + r % group) * a.q.head + g * (DH / 4);
+        uint4 qf[STEPS];
+#pragma unroll
+        for (int st = 0; st < STEPS; ++st) qf[st] = *reinterpret_cast<const uint4*>(src + st * 8);
+        const float2 t = row_ml[head * rows + r];
+        const float inv = 1.f / t.y, neg_m = -t.x * scale_log2e;
+        const int limit = r0 + c < last_row ? seen_by(span, i) : 0;
+        f32x4_t s[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            s[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int st = 0; st < STEPS; ++st) s[j] = mfma16(kf[j][st], qf[st], s[j]);
+        }
+#pragma unroll
+        for (int n = 0; n < 8; ++n)
+            if (my0 + n < limit)
+                sum[n] += __builtin_amdgcn_exp2f(fmaf(s[n >> 2][n & 3], scale_log2e, neg_m)) * inv;
+    }
+    // over the 16 columns of a group
+#pragma unroll
+    for (int n = 0; n < 8; ++n) {
+        float x = sum[n];
+        x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x128, 0xf, 0xf, false));   // row_ror:8
+        x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x124, 0xf, 0xf, false));
+        x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x122, 0xf, 0xf, false));
+        x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x121, 0xf, 0xf, false));
+        if (c == n && my0 + n < span.len) cache.weight[head * cache.capacity + my0 + n] += x;
+    }
+}
+
+// ---- host --------------------------------------------------------------------------------------------------------
+namespace {
+
+struct AttentionPlan {
+    bool many;
+    int group, rows, splits, pitch;
+    size_t o_bytes, ml_bytes, row_bytes, logit_bytes;
+    size_t bytes() const { return o_bytes + ml_bytes + row_bytes + logit_bytes; }
+};
+
+AttentionPlan attention_plan(int B, int H, int H_kv, int dh, int n_q, int max_len, bool accumulate) {
+    AttentionPlan p{};
+    p.group = H / H_kv;
+    p.rows = n_q * p.group;
+    p.many = p.rows > 16;
+    const int tile = p.many ? MANY_KT : FEW_STEP * FEW_WAVES;
+    const int64_t tiles = ((int64_t)max_len + tile - 1) / tile;
+    const int64_t wgs = (int64_t)B * H_kv * (p.many ? (p.rows + MANY_ROWS - 1) / MANY_ROWS : 1);
+    const int64_t want = 4 * (int64_t)device_cu_count();
+    int64_t s = p.many ? (2 * (int64_t)device_cu_count() + wgs - 1) / wgs : (want + wgs - 1) / wgs;
+    const int64_t most = p.many ? (tiles + 3) / 4 : tiles;   // (few tiles each are not worth a part of their own)
+    if (s > most) s = most;
+    if (s > 64) s = 64;
+    p.splits = s < 1 ? 1 : (int)s;
+    p.pitch = (max_len + FEW_STEP - 1) / FEW_STEP * FEW_STEP;
+    const size_t all = (size_t)B * H_kv * p.rows;
+    p.o_bytes = p.many && p.splits == 1 ? 0 : align_up(all * p.splits * dh * 4, 256);
+    p.ml_bytes = align_up(all * p.splits * 8, 256);
+    p.row_bytes = align_up(all * 8, 256);
+    p.logit_bytes = accumulate && !p.many ? align_up(all * p.pitch * 4, 256) : 0;
+    return p;
+}
+
+template <int DH>
+int run_attention(const CacheView& c, const CacheAttention& a, const AttentionPlan& p, char* scratch, hipStream_t st) {
+    float* o = reinterpret_cast<float*>(scratch);
+    float2* ml = reinterpret_cast<float2*>(scratch + p.o_bytes);
+    float2* row_ml = reinterpret_cast<float2*>(scratch + p.o_bytes + p.ml_bytes);
+    float* logits = reinterpret_cast<float*>(scratch + p.o_bytes + p.ml_bytes + p.row_bytes);
+    if (!p.many) {
+        float* lg = a.accumulate ? logits : nullptr;
+        hipLaunchKernelGGL((few_rows_kernel<DH>), dim3(p.splits, c.H_kv, c.B), dim3(FEW_WAVES * 64), 0, st, c, a, p.group,
+                           p.splits, o, ml, lg, p.pitch);
+        MVLA_HIP_CHECK(hipGetLastError());
+        const int wide = (p.rows * DH + JOIN_THREADS - 1) / JOIN_THREADS;
+        const int chunks = a.accumulate ? (a.max_len + JOIN_SLOTS - 1) / JOIN_SLOTS : 1;
+        hipLaunchKernelGGL(join_kernel, dim3(wide > chunks ? wide : chunks, c.H_kv, c.B), dim3(JOIN_THREADS), 0, st, c, a,
+                           p.group, p.splits, o, ml, lg, p.pitch, nullptr);
+        MVLA_HIP_CHECK(hipGetLastError());
+        return MVLA_OK;
+    }
+    static bool lds_set[kMaxDevices] = {};
+    const size_t lds = 2 * (MANY_KT * (DH / 8) + DH * 8) * sizeof(uint4);
+    int dev = 0;   // (the dynamic-LDS limit is raised once per device)
+    MVLA_HIP_CHECK(hipGetDevice(&dev));
+    if (dev < 0 || dev >= kMaxDevices || !lds_set[dev]) {
+        MVLA_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void*>(&many_rows_kernel<DH>),
+                                           hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+        if (dev >= 0 && dev < kMaxDevices) lds_set[dev] = true;
+    }
+    hipLaunchKernelGGL((many_rows_kernel<DH>), dim3(c.H_kv, (p.rows + MANY_ROWS - 1) / MANY_ROWS, c.B * p.splits),
+                       dim3(MANY_THREADS), lds, st, c, a, p.group, p.splits, o, ml);
+    MVLA_HIP_CHECK(hipGetLastError());
+    const float2* joined = ml;
+    if (p.splits > 1) {
+        hipLaunchKernelGGL(join_kernel, dim3((p.rows * DH + JOIN_THREADS - 1) / JOIN_THREADS, c.H_kv, c.B),
+                           dim3(JOIN_THREADS), 0, st, c, a, p.group, p.splits, o, ml, nullptr, 0, row_ml);
+        MVLA_HIP_CHECK(hipGetLastError());
+        joined = row_ml;
+    }
+    if (a.accumulate) {
+        const int per = FEW_STEP * WEIGH_WAVES;
+        hipLaunchKernelGGL((weigh_kernel<DH>), dim3((a.max_len + per - 1) / per, c.H_kv, c.B), dim3(WEIGH_WAVES * 64), 0, st,
+                           c, a, p.group, joined);
+        MVLA_HIP_CHECK(hipGetLastError());
+    }
+    return MVLA_OK;
+}
+
+}  // namespace
+
+size_t cache_attention_bytes(int B, int H, int H_kv, int dh, int n_q, int max_len, bool accumulate) {
+    return attention_plan(B, H, H_kv, dh, n_q, max_len, accumulate).bytes();
+}
+
+int launch_cache_attention(const CacheView& c, const CacheAttention& a, char* scratch, hipStream_t st) {
+    const AttentionPlan p = attention_plan(c.B, a.H, c.H_kv, c.dh, a.n_q, a.max_len, a.accumulate != 0);
+    return c.dh == 128 ? run_attention<128>(c, a, p, scratch, st) : run_attention<64>(c, a, p, scratch, st);
+}
+
+}  // namespace mvla

@@ -15,7 +15,8 @@ enum KernelId {
     KID_RMSNORM = 0, KID_GEMM_QKV, KID_SCORE_PROBS, KID_ATTENTION, KID_GEMM_O,
     KID_RMSNORM_MLP, KID_GEMM_GATEUP, KID_GEMM_DOWN, KID_SALIENCE, KID_BUDGET, KID_SELECT,
     KID_COMPACT, KID_ROPE_TABLE, KID_PRUNE_FUSED, KID_SMOOTH, KID_DECOMPOSE, KID_FEATURE_SHARE,
-    KID_CANDIDATE, KID_MASK_INDEX, KID_COUNT
+    KID_CANDIDATE, KID_MASK_INDEX, KID_CACHE_APPEND, KID_CACHE_READ, KID_CACHE_ATTENTION, KID_CACHE_EVICT,
+    KID_SAMPLE, KID_COUNT
 };
 
 struct ProfRecord {
@@ -168,5 +169,42 @@ int launch_probe_empty(hipStream_t st);
 // attention.hip: causal flash attention; q,k rows inside qkv (row stride ldqkv), vt [B,H,dh,S_pad]
 int launch_attention(const bf16_t* q, const bf16_t* k, int ldqkv, const bf16_t* vt, int S_pad,
                      int B, int S, int H, int dh, bf16_t* out, int ldo, hipStream_t st);
+
+// cache_kernels.hip, cache_attention.hip: the key/value cache held in 4 bits (mvla_cache4, device pointers by type)
+struct CacheView {
+    uint8_t *k, *v, *k_scale, *v_scale;
+    int32_t* pos;
+    float* weight;
+    int B, H_kv, dh, capacity;
+};
+// rows [B, tokens, heads, dh] by their strides, in elements
+struct CacheRows {
+    const bf16_t* p;
+    int64_t sample, token, head, channel;
+};
+// whether a row is whole 16-byte pieces
+inline bool cache_rows_wide(const CacheRows& r) {
+    return r.channel == 1 && reinterpret_cast<uintptr_t>(r.p) % 16 == 0 && r.sample % 8 == 0 && r.token % 8 == 0 &&
+           r.head % 8 == 0;
+}
+int launch_cache_append(const CacheView& c, const CacheRows& k, const CacheRows& v, const int32_t* pos, int n,
+                        const int32_t* n_new, const int32_t* len, hipStream_t st);
+int launch_cache_read(const CacheView& c, const int32_t* first, int n, bf16_t* k_out, bf16_t* v_out, hipStream_t st);
+// c into d (the same cache: in place); holes: int32 scratch [B, H_kv, min(budget, max_len)]
+int launch_cache_evict(const CacheView& c, const CacheView& d, const int32_t* len, int max_len, int budget, int first_pos,
+                       const int32_t* recent_from, int32_t* len_out, int32_t* kept, int32_t* holes, hipStream_t st);
+struct CacheAttention {
+    CacheRows q, out;
+    const int32_t *len, *n_new;
+    int H, n_q, max_len, accumulate;
+    float scale;
+};
+size_t cache_attention_bytes(int B, int H, int H_kv, int dh, int n_q, int max_len, bool accumulate);
+int launch_cache_attention(const CacheView& c, const CacheAttention& a, char* scratch, hipStream_t st);
+
+// sample_kernels.hip
+int launch_sample(const void* logits, bool half, int64_t row_stride, int B, int V, const float* temperature,
+                  const int32_t* top_k, const float* top_p, const float* min_p, const float* u, int32_t* token, float* prob,
+                  hipStream_t st);
 
 }  // namespace mvla
