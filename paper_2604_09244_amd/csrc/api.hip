@@ -1154,7 +1154,8 @@ int mvla_sample(mvla_ctx* ctx, const void* logits, int half, int64_t row_stride,
     if (V > (1 << 22)) return MVLA_EUNSUPPORTED;   // (sums of weights in 64 bits)
     int rc;
     TIMED(ctx, KID_SAMPLE, B, launch_sample(logits, half != 0, row_stride, B, V, temperature, top_k, top_p, min_p, u, token,
-                                            prob, ctx->stream));
+                                            prob, reinterpret_cast<char*>(ctx->gemm_partial), ctx->gemm_partial_bytes,
+                                            ctx->stream));
     return MVLA_OK;
 }
 

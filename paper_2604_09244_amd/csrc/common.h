@@ -205,6 +205,6 @@ int launch_cache_attention(const CacheView& c, const CacheAttention& a, char* sc
 // sample_kernels.hip
 int launch_sample(const void* logits, bool half, int64_t row_stride, int B, int V, const float* temperature,
                   const int32_t* top_k, const float* top_p, const float* min_p, const float* u, int32_t* token, float* prob,
-                  hipStream_t st);
+                  char* scratch, size_t scratch_bytes, hipStream_t st);
 
 }  // namespace mvla

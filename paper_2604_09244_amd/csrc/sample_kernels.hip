@@ -5,23 +5,36 @@
 // w >= min_p.  The chosen token is the first, in ascending index, at which the running sum of what stays passes u times
 // its total.
 //
-// Nothing is sorted: every filter keeps a beginning of the order, so it is one smallest place in it, a logit and an
-// index.  One workgroup a row; the row is read as few times as the settings allow:
-//   the maximum, and every thread's own (1 pass);
-//   top_k up to 1024: at least top_k tokens are no smaller than the top_k-th largest of the 1024 threads' maxima, and
-//     hardly more are: they are gathered (1 pass) and all that follows happens on that short list in LDS;
-//   otherwise: the total (1 pass), a histogram over (max - x) / T of the tokens that can still lie before the border
-//     (1 pass), the border's bin gathered into the list (1 pass), the running sum (1 pass).
-// Passes after the first find the row in the L2.  Weights are summed over neighbours that one lane reads together in 32
-// bits, in that order, and as whole numbers of 2^-40 beyond: no sum depends on the order in which it was formed.
+// Nothing is sorted: every filter keeps a beginning of the order, so it is one last place in it, a logit and an index.
+// A row is read once for its maximum (and those of groups of its tokens) and once more to bring what can stay into a
+// list, or to sum tiles of neighbouring tokens; what follows looks at the list, at one tile, or at one bin's tokens:
+//   top_k: at least top_k tokens are no smaller than the top_k-th largest of the groups' maxima, and hardly more are:
+//     these are the list, and everything else happens there;
+//   min_p: the tokens above that share of the largest are the list;
+//   top_p alone: how many tokens lie in each bin of 1/25.6 octaves shows the border to a bin or so; another pass sums the
+//     tiles up to the bins around it and brings their tokens into a list, whose exact order shows the border.
+// What no list can take (a list that overflows because thousands of tokens are alike) is found digit by digit from
+// histograms over the row, place().
+// Weights are summed over neighbours that one lane reads together in 32 bits, in that order, and as whole numbers of
+// 2^-40 beyond, so that no sum depends on the order in which it was formed.
+//
+// Bound: arithmetic of some 10 to 30 operations a token (131072 of them keep one compute unit busy for 8 to 30 us a
+// pass).  Long rows are therefore dealt out over the chip, SLICE tokens a workgroup, in up to four launches; short ones
+// take one workgroup and one launch.
 #include "common.h"
 #include "mfma.h"
+#include "wave.h"
 
 namespace mvla {
 
-constexpr int SAMPLE_THREADS = 1024, SAMPLE_WAVES = SAMPLE_THREADS / 64, SAMPLE_BINS = 1024;
-constexpr int SAMPLE_TILES = 64;          // tiles of a wave's run whose sums are kept
+typedef unsigned long long u64;    // (as atomics take it)
+
+constexpr int SAMPLE_THREADS = 1024, SAMPLE_WAVES = SAMPLE_THREADS / 64;
+constexpr int SAMPLE_BINS = 1024;         // of octaves below the largest weight, and at most so many tiles
+constexpr int SAMPLE_LIST = 14336;        // tokens on the list: 112 of the 160 KiB of LDS
+constexpr int SLICE_THREADS = 256;
 constexpr float SAMPLE_OCTAVES = 40.f;    // weights below 2^-40 of the largest count as none
+constexpr float LOWEST = -3.4028235e38f;  // (-inf never stays)
 
 // order-preserving bits of a logit that is a number
 __device__ __forceinline__ uint32_t logit_key(float x) {
@@ -32,13 +45,13 @@ __device__ __forceinline__ float key_logit(uint32_t k) {
     return __uint_as_float(k ^ ((k >> 31) ? 0x80000000u : 0xffffffffu));
 }
 // place of a token in the order, larger is earlier
-__device__ __forceinline__ uint64_t place_of(float x, uint32_t i) { return ((uint64_t)logit_key(x) << 32) | (0xffffffffu - i); }
-__device__ __forceinline__ float place_logit(uint64_t p) { return key_logit((uint32_t)(p >> 32)); }
-__device__ __forceinline__ uint32_t place_index(uint64_t p) { return 0xffffffffu - (uint32_t)p; }
+__device__ __forceinline__ u64 place_of(float x, uint32_t i) { return ((u64)logit_key(x) << 32) | (0xffffffffu - i); }
+__device__ __forceinline__ float place_logit(u64 p) { return key_logit((uint32_t)(p >> 32)); }
+__device__ __forceinline__ uint32_t place_index(u64 p) { return 0xffffffffu - (uint32_t)p; }
 
-__device__ __forceinline__ uint64_t whole(float w) {            // w in [0, 16] as a whole number of 2^-40
+__device__ __forceinline__ u64 whole(float w) {                 // w in [0, 16] as a whole number of 2^-40
     const float h = __builtin_truncf(w * 0x1p16f);
-    return ((uint64_t)(uint32_t)h << 24) + (uint32_t)fmaf(fmaf(w, 0x1p16f, -h), 0x1p24f, 0.5f);
+    return ((u64)(uint32_t)h << 24) + (uint32_t)fmaf(fmaf(w, 0x1p16f, -h), 0x1p24f, 0.5f);
 }
 
 template <typename T>
@@ -46,11 +59,15 @@ struct Row {                             // a row in pieces of 16 bytes from the
     static constexpr int VEC = 16 / (int)sizeof(T);
     const T* p;
     int V, off, pieces;
+    int steps, tiles;                    // a tile: `steps` times 64 pieces; at most SAMPLE_BINS of them
+    bool endless = false;                // the largest logit is infinite: those are 0 then, all others no numbers
     __device__ __forceinline__ Row(const T* row, int v) {
         off = (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
         p = row - off;
         V = v;
-        pieces = (int)(((int64_t)v + off + VEC - 1) / VEC);
+        pieces = (v + off + VEC - 1) / VEC;
+        steps = (pieces + 64 * SAMPLE_BINS - 1) / (64 * SAMPLE_BINS);
+        tiles = (pieces + 64 * steps - 1) / (64 * steps);
     }
     __device__ __forceinline__ int first(int j) const { return j * VEC - off; }
     // piece j; what lies outside the row is no number
@@ -65,58 +82,438 @@ struct Row {                             // a row in pieces of 16 bytes from the
             } else {
                 x[0] = __uint_as_float(w.x), x[1] = __uint_as_float(w.y), x[2] = __uint_as_float(w.z), x[3] = __uint_as_float(w.w);
             }
-            return;
-        }
+        } else {
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            x[e] = NAN;
-            if (i0 + e >= 0 && i0 + e < V) {
-                if constexpr (VEC == 8) x[e] = bf16_to_f32(p[j * VEC + e]);
-                else x[e] = p[j * VEC + e];
+            for (int e = 0; e < VEC; ++e) {
+                x[e] = NAN;
+                if (i0 + e >= 0 && i0 + e < V) {
+                    if constexpr (VEC == 8) x[e] = bf16_to_f32(p[j * VEC + e]);
+                    else x[e] = p[j * VEC + e];
+                }
             }
         }
+        if (endless)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) x[e] = x[e] == INFINITY ? 0.f : NAN;
     }
 };
 
-__device__ __forceinline__ uint64_t wave_total(uint64_t x) {
+// sum over the lanes, in parts whose sums fit 32 bits
+__device__ __forceinline__ u64 wave_total(u64 x) {
+    return wave_sum_u32((uint32_t)x & 0x3fffffu) + ((u64)wave_sum_u32((uint32_t)(x >> 22) & 0x3fffffu) << 22) +
+           ((u64)wave_sum_u32((uint32_t)(x >> 44)) << 44);
+}
+__device__ __forceinline__ float wave_max(float x) {
 #pragma unroll
-    for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
+    for (int o = 32; o; o >>= 1) x = fmaxf(x, __shfl_xor(x, o));
     return x;
 }
-__device__ __forceinline__ uint64_t wave_running(uint64_t x, int lane) {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const uint64_t t = __shfl_up(x, o);
-        if (lane >= o) x += t;
-    }
+template <int CTRL, int ROWS>
+__device__ __forceinline__ u64 lane_from(u64 x) {     // another lane's value (0 where there is none), on the vector unit
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)x, CTRL, ROWS, 0xf, false);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(x >> 32), CTRL, ROWS, 0xf, false);
+    return ((u64)hi << 32) | lo;
+}
+// running sum over the lanes (all 64 active)
+__device__ __forceinline__ u64 wave_running(u64 x) {
+    x += lane_from<0x111, 0xf>(x);    // row_shr:1
+    x += lane_from<0x112, 0xf>(x);
+    x += lane_from<0x114, 0xf>(x);
+    x += lane_from<0x118, 0xf>(x);
+    x += lane_from<0x142, 0xa>(x);    // row_bcast:15 to rows 1 and 3
+    x += lane_from<0x143, 0xc>(x);    // row_bcast:31 to rows 2 and 3
     return x;
 }
 
+// A row's settings, and how its weights are measured once its maximum is known.
+struct Settings {
+    float t, p, least;
+    int k, V;
+    bool by_k, by_p, by_least;
+    float per_t, ref;
+    __device__ __forceinline__ Settings(int b, int v, const float* temperature, const int32_t* top_k, const float* top_p,
+                                        const float* min_p) {
+        V = v;
+        t = temperature ? temperature[b] : 1.f;
+        k = top_k ? top_k[b] : 0;
+        p = top_p ? top_p[b] : 1.f;
+        least = min_p ? fminf(min_p[b], 1.f) : 0.f;
+        by_k = k > 0 && k < V;
+        by_p = p < 1.f;
+        by_least = min_p && min_p[b] > 0.f;
+    }
+    __device__ __forceinline__ bool greedy() const { return !(t > 0.f); }
+    __device__ __forceinline__ void measure(float most) {
+        per_t = 1.4426950408889634f / t;
+        ref = most == INFINITY ? 0.f : most;
+    }
+    // octaves below the largest weight (NaN where that is no number)
+    __device__ __forceinline__ float octaves(float x) const { return (ref - x) * per_t; }
+    static __device__ __forceinline__ float weight(float oct) { return __builtin_amdgcn_exp2f(-oct); }
+    static __device__ __forceinline__ bool counts(float oct) { return oct < SAMPLE_OCTAVES; }
+    static __device__ __forceinline__ int bin_of(float oct) {
+        return min((int)(oct * (SAMPLE_BINS / SAMPLE_OCTAVES)), SAMPLE_BINS - 1);
+    }
+    // Tally of a bin: its tokens, and how far into it they lie, in 64ths; and what these weigh, to 3e-5 (tokens of one bin
+    // differ by 2.7 % at most, what is left out is the second order of that).
+    static __device__ __forceinline__ u64 tallied(float oct) {
+        return ((u64)1 << 32) + (uint32_t)(__builtin_amdgcn_fractf(oct * (SAMPLE_BINS / SAMPLE_OCTAVES)) * 64.f);
+    }
+    static __device__ __forceinline__ u64 about(u64 tally, int bin) {
+        const uint32_t c = (uint32_t)(tally >> 32);
+        if (!c) return 0;
+        const float in = ((float)(uint32_t)tally / (float)c + 0.5f) * (1.f / 64.f);
+        return c * whole(weight(((float)bin + in) * (SAMPLE_OCTAVES / SAMPLE_BINS)));
+    }
+    // where a running sum that is known so well has to be looked at for what reaches `want`
+    static __device__ __forceinline__ u64 early(u64 want) { return want - (want >> 12); }
+    static __device__ __forceinline__ u64 late(u64 want) { return want + (want >> 12); }
+    __device__ __forceinline__ u64 mass_of(u64 place) const { return whole(weight(octaves(place_logit(place)))); }
+    // less than this comes before a token that top_p lets stay
+    __device__ __forceinline__ u64 part_of(u64 total) const {
+        const u64 a = (u64)ceil((double)fmaxf(p, 0.f) * (double)total);
+        return a < 1 ? 1 : a < total ? a : total;
+    }
+    // from which logit on tokens can have min_p of the largest weight (a hair below: the weight itself is asked again)
+    __device__ __forceinline__ float least_logit() const {
+        return fminf(fmaxf(LOWEST, ref + (__builtin_amdgcn_logf(least) - 0x1p-10f) / per_t), ref);
+    }
+};
+
+// What the launches on slices of a row hand on.
+struct RowState {
+    float most, low;
+    uint32_t n_list, first_at;
+    float window0, window1;       // octaves of the bins around the border of top_p
+};
+struct SampleScratch {
+    RowState* state;              // [rows]
+    float* maxima;                // [rows][slices * SLICE_THREADS]
+    u64* tally;                   // [rows][SAMPLE_BINS]
+    u64* tile_sum;                // [rows][SAMPLE_BINS]
+    u64* total;                   // [rows][slices]
+    u64* list;                    // [rows][SAMPLE_LIST]
+    int slices;
+};
+
+// Appends a wave's tokens for which `in` holds to a list of `room` entries; *n counts all of them.
+template <int VEC>
+__device__ __forceinline__ void append_places(const float (&x)[VEC], const bool (&in)[VEC], int i0, uint32_t* n, u64* list,
+                                              uint32_t room, int lane) {
+    u64 mask[VEC];
+    uint32_t c = 0;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+        mask[e] = __ballot(in[e]);
+        c += (uint32_t)__popcll(mask[e]);
+    }
+    if (!c) return;
+    const int head = __ffsll((u64)__ballot(true)) - 1;
+    uint32_t at = 0;
+    if (lane == head) at = atomicAdd(n, c);
+    at = __shfl(at, head);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+        const uint32_t to = at + __builtin_amdgcn_mbcnt_hi((uint32_t)(mask[e] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask[e], 0));
+        if (in[e] && to < room) list[to] = place_of(x[e], (uint32_t)(i0 + e));
+        at += (uint32_t)__popcll(mask[e]);
+    }
+}
+
+// ---- launches on slices of a row --------------------------------------------------------------------------------------
+// calls f(tile, values, piece, whether the piece exists) for the wave's pieces of a slice; done(tile) behind each tile
+template <typename T, typename F, typename G>
+__device__ __forceinline__ void slice_tiles(const Row<T>& row, int slice, int slices, F f, G done) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int per = (row.tiles + slices - 1) / slices, t1 = min((slice + 1) * per, row.tiles);
+    for (int t = slice * per + wave; t < t1; t += SLICE_THREADS / 64) {
+        for (int q = 0; q < row.steps; ++q) {
+            const int j = (t * row.steps + q) * 64 + lane;
+            float x[Row<T>::VEC];
+            const bool there = j < row.pieces;
+#pragma unroll
+            for (int e = 0; e < Row<T>::VEC; ++e) x[e] = NAN;
+            if (there) row.load(j, x);
+            f(t, x, j, there);
+        }
+        done(t);
+    }
+}
+
 template <typename T>
+__global__ __launch_bounds__(SLICE_THREADS) void sample_max_kernel(const T* __restrict__ logits, int64_t stride, int V,
+                                                                   SampleScratch sc) {
+    constexpr int VEC = Row<T>::VEC;
+    const int slice = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
+    const Row<T> row(logits + b * stride, V);
+    if (slice == 0) {
+        for (int i = tid; i < SAMPLE_BINS; i += SLICE_THREADS) sc.tally[(size_t)b * SAMPLE_BINS + i] = 0;
+        if (tid == 0) {
+            sc.state[b].n_list = 0;
+            sc.state[b].first_at = 0xffffffffu;
+        }
+    }
+    float m = -INFINITY;
+    // (pieces of a slice side by side over the threads: the order within it is nobody's business here)
+    const int per = (row.tiles + sc.slices - 1) / sc.slices * row.steps * 64, j1 = min((slice + 1) * per, row.pieces);
+    int j = slice * per + tid;
+    for (; j + 3 * SLICE_THREADS < j1; j += 4 * SLICE_THREADS) {
+        float x[4][VEC];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) row.load(j + q * SLICE_THREADS, x[q]);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) m = fmaxf(m, x[q][e]);
+    }
+    for (; j < j1; j += SLICE_THREADS) {
+        float x[VEC];
+        row.load(j, x);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) m = fmaxf(m, x[e]);
+    }
+    sc.maxima[((size_t)b * sc.slices + slice) * SLICE_THREADS + tid] = m;
+}
+
+// The second look at a row: the list, the tiles' sums, or the bins' tallies, as its settings ask.
+template <typename T>
+__global__ __launch_bounds__(SLICE_THREADS) void sample_collect_kernel(const T* __restrict__ logits, int64_t stride, int V,
+                                                                       const float* __restrict__ temperature,
+                                                                       const int32_t* __restrict__ top_k,
+                                                                       const float* __restrict__ top_p,
+                                                                       const float* __restrict__ min_p, SampleScratch sc) {
+    constexpr int VEC = Row<T>::VEC, WAVES = SLICE_THREADS / 64, PER = SAMPLE_BINS / SLICE_THREADS;
+    __shared__ u64 tally[SAMPLE_BINS];
+    __shared__ uint32_t counts[WAVES];
+    __shared__ float tops[WAVES];
+    __shared__ u64 sums[WAVES];
+    __shared__ int found;
+    const int slice = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    Row<T> row(logits + b * stride, V);
+    Settings s(b, V, temperature, top_k, top_p, min_p);
+    const int n_max = sc.slices * SLICE_THREADS;
+    const float* maxima = sc.maxima + (size_t)b * n_max;
+    float most = -INFINITY;
+    for (int i = tid; i < n_max; i += SLICE_THREADS) most = fmaxf(most, maxima[i]);
+    most = wave_max(most);
+    if (lane == 0) tops[wave] = most;
+    for (int i = tid; i < SAMPLE_BINS; i += SLICE_THREADS) tally[i] = 0;
+    if (tid == 0) found = -1;
+    __syncthreads();
+    for (int w = 0; w < WAVES; ++w) most = fmaxf(most, tops[w]);
+    if (slice == 0 && tid == 0) sc.state[b].most = most;
+    if (most == -INFINITY) return;
+    auto nothing = [](int) {};
+    if (s.greedy()) {
+        slice_tiles<T>(row, slice, sc.slices, [&](int, float (&x)[VEC], int j, bool) {
+            uint32_t at = 0xffffffffu;
+#pragma unroll
+            for (int e = VEC - 1; e >= 0; --e)
+                if (x[e] == most) at = (uint32_t)(row.first(j) + e);
+            if (at != 0xffffffffu) atomicMin(&sc.state[b].first_at, at);
+        }, nothing);
+        return;
+    }
+    s.measure(most);
+    row.endless = most == INFINITY;
+    auto of_max = [&](float m) { return row.endless ? (m == most ? 0.f : -INFINITY) : m; };
+    if (s.by_k && s.k > n_max) return;                     // (for place())
+    const bool list = s.by_k || s.by_least, sum = !s.by_k && (s.by_p ? s.by_least : !s.by_least);
+    float low = s.by_least ? s.least_logit() : LOWEST;
+    if (s.by_k) {
+        low = LOWEST;
+        for (int i = tid; i < n_max; i += SLICE_THREADS) {
+            const float oct = s.octaves(of_max(maxima[i]));
+            if (s.counts(oct)) atomicAdd(&tally[s.bin_of(oct)], (u64)1);
+        }
+        __syncthreads();
+        uint32_t c[PER], mine = 0;
+#pragma unroll
+        for (int q = 0; q < PER; ++q) mine += c[q] = (uint32_t)tally[tid * PER + q];
+        uint32_t inc = mine;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const uint32_t t = __shfl_up(inc, o);
+            if (lane >= o) inc += t;
+        }
+        if (lane == 63) counts[wave] = inc;
+        __syncthreads();
+        uint32_t before = inc - mine;
+        for (int w = 0; w < wave; ++w) before += counts[w];
+#pragma unroll
+        for (int q = 0; q < PER; ++q) {
+            if (before < (uint32_t)s.k && before + c[q] >= (uint32_t)s.k) found = tid * PER + q;
+            before += c[q];
+        }
+        __syncthreads();
+        if (found >= 0) {                                  // the smallest maximum of the bins up to it
+            float m = INFINITY;
+            for (int i = tid; i < n_max; i += SLICE_THREADS) {
+                const float x = of_max(maxima[i]), oct = s.octaves(x);
+                if (s.counts(oct) && s.bin_of(oct) <= found) m = fminf(m, x);
+            }
+            m = -wave_max(-m);
+            if (lane == 0) tops[wave] = m;
+            __syncthreads();
+            low = tops[0];
+            for (int w = 1; w < WAVES; ++w) low = fminf(low, tops[w]);
+        }
+    }
+    if (list || sum) {
+        uint32_t* n = &sc.state[b].n_list;
+        u64* places = sc.list + (size_t)b * SAMPLE_LIST;
+        u64 total = 0, tile = 0;
+        slice_tiles<T>(row, slice, sc.slices, [&](int, float (&x)[VEC], int j, bool) {
+            if (list) {
+                bool in[VEC];
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) in[e] = x[e] >= low;
+                append_places<VEC>(x, in, row.first(j), n, places, SAMPLE_LIST, lane);
+            }
+            if (sum) {
+                float w = 0.f;
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) w += fmaxf(s.weight(s.octaves(x[e])), 0.f);    // (no number: 0)
+                tile += whole(w);
+            }
+        }, [&](int t) {
+            if (sum) {
+                tile = wave_total(tile);
+                if (lane == 0) sc.tile_sum[(size_t)b * SAMPLE_BINS + t] = tile;
+                total += tile;
+                tile = 0;
+            }
+        });
+        if (sum) {
+            if (lane == 0) sums[wave] = total;
+            __syncthreads();
+            if (tid == 0) {
+                u64 all = 0;
+                for (int w = 0; w < WAVES; ++w) all += sums[w];
+                sc.total[(size_t)b * sc.slices + slice] = all;
+            }
+        }
+        return;
+    }
+    // top_p alone
+    slice_tiles<T>(row, slice, sc.slices, [&](int, float (&x)[VEC], int, bool) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            const float oct = s.octaves(x[e]);
+            if (s.counts(oct)) atomicAdd(&tally[s.bin_of(oct)], s.tallied(oct));
+        }
+    }, nothing);
+    __syncthreads();
+    for (int i = tid; i < SAMPLE_BINS; i += SLICE_THREADS)
+        if (tally[i]) atomicAdd(&sc.tally[(size_t)b * SAMPLE_BINS + i], tally[i]);
+}
+
+// top_p alone: the bins around its border, and behind that the total, the tiles' sums up to them, and their tokens.
+template <typename T>
+__global__ __launch_bounds__(SLICE_THREADS) void sample_window_kernel(const T* __restrict__ logits, int64_t stride, int V,
+                                                                      const float* __restrict__ temperature,
+                                                                      const int32_t* __restrict__ top_k,
+                                                                      const float* __restrict__ top_p,
+                                                                      const float* __restrict__ min_p, SampleScratch sc) {
+    constexpr int VEC = Row<T>::VEC, WAVES = SLICE_THREADS / 64, PER = SAMPLE_BINS / SLICE_THREADS;
+    constexpr float WIDTH = SAMPLE_OCTAVES / SAMPLE_BINS;
+    __shared__ u64 sums[WAVES];
+    __shared__ int found[2];
+    const int slice = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    Settings s(b, V, temperature, top_k, top_p, min_p);
+    const float most = sc.state[b].most;
+    if (!s.by_p || s.by_k || s.by_least || s.greedy() || most == -INFINITY) return;
+    s.measure(most);
+    Row<T> row(logits + b * stride, V);
+    row.endless = most == INFINITY;
+    u64 mass[PER], mine = 0;
+#pragma unroll
+    for (int q = 0; q < PER; ++q) {
+        const int bin = tid * PER + q;
+        mine += mass[q] = s.about(sc.tally[(size_t)b * SAMPLE_BINS + bin], bin);
+    }
+    const u64 inc = wave_running(mine);
+    if (lane == 63) sums[wave] = inc;
+    if (tid == 0) found[0] = 0, found[1] = SAMPLE_BINS;
+    __syncthreads();
+    u64 before = inc - mine, total = 0;
+    for (int w = 0; w < WAVES; ++w) {
+        if (w < wave) before += sums[w];
+        total += sums[w];
+    }
+    const u64 want = s.part_of(total), early = s.early(want), late = s.late(want);
+#pragma unroll
+    for (int q = 0; q < PER; ++q) {
+        const u64 v = before + mass[q];
+        if (before < early && v >= early) found[0] = tid * PER + q;
+        if (before < late && v >= late) found[1] = tid * PER + q;
+        before = v;
+    }
+    __syncthreads();
+    const float first = (float)(found[0] - 1) * WIDTH, last = (float)(found[1] + 2) * WIDTH;
+    if (slice == 0 && tid == 0) {
+        sc.state[b].window0 = first;
+        sc.state[b].window1 = last;
+    }
+    u64 all = 0, tile = 0;
+    slice_tiles<T>(row, slice, sc.slices, [&](int, float (&x)[VEC], int j, bool) {
+        float sure = 0.f, any = 0.f;
+        bool in[VEC];
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            const float oct = s.octaves(x[e]), w = fmaxf(s.weight(oct), 0.f);
+            any += w;
+            sure += oct < first ? w : 0.f;
+            in[e] = oct >= first && oct < last;
+        }
+        append_places<VEC>(x, in, row.first(j), &sc.state[b].n_list, sc.list + (size_t)b * SAMPLE_LIST, SAMPLE_LIST, lane);
+        all += whole(any);
+        tile += whole(sure);
+    }, [&](int t) {
+        tile = wave_total(tile);
+        if (lane == 0) sc.tile_sum[(size_t)b * SAMPLE_BINS + t] = tile;
+        tile = 0;
+    });
+    all = wave_total(all);
+    __syncthreads();
+    if (lane == 0) sums[wave] = all;
+    __syncthreads();
+    if (tid == 0) {
+        all = 0;
+        for (int w = 0; w < WAVES; ++w) all += sums[w];
+        sc.total[(size_t)b * sc.slices + slice] = all;
+    }
+}
+
+// ---- a row's choice ----------------------------------------------------------------------------------------------------
+// SPLIT: behind the launches above, from what they left; otherwise a whole row by itself.
+template <typename T, bool SPLIT>
 __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(const T* __restrict__ logits, int64_t stride, int V,
                                                                 const float* __restrict__ temperature,
                                                                 const int32_t* __restrict__ top_k,
                                                                 const float* __restrict__ top_p,
                                                                 const float* __restrict__ min_p,
                                                                 const float* __restrict__ u, int32_t* __restrict__ token,
-                                                                float* __restrict__ prob) {
+                                                                float* __restrict__ prob, SampleScratch sc) {
     constexpr int VEC = Row<T>::VEC;
-    __shared__ uint64_t bins[SAMPLE_BINS];
-    __shared__ uint64_t list[SAMPLE_THREADS], sorted[SAMPLE_THREADS];
-    __shared__ uint64_t sums[SAMPLE_WAVES], tile_sum[SAMPLE_WAVES][SAMPLE_TILES];
-    __shared__ uint64_t found[3];
-    __shared__ float maxima[SAMPLE_WAVES];
+    constexpr float WIDTH = SAMPLE_OCTAVES / SAMPLE_BINS;
+    extern __shared__ u64 list[];
+    __shared__ u64 bins[SAMPLE_BINS], tile_sum[SAMPLE_BINS], few[SAMPLE_THREADS];
+    __shared__ u64 sums[SAMPLE_WAVES], found[3];
     __shared__ uint32_t n_list, first_at;
+    __shared__ float maxima[SAMPLE_WAVES];
 
     const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const Row<T> row(logits + b * stride, V);
-    const float t = temperature ? temperature[b] : 1.f;
-    const int k = top_k ? top_k[b] : 0;
-    const float p = top_p ? top_p[b] : 1.f;
-    const float least = min_p ? fminf(min_p[b], 1.f) : 0.f;
-    const bool by_least = min_p && min_p[b] > 0.f;
+    Row<T> row(logits + b * stride, V);
+    Settings s(b, V, temperature, top_k, top_p, min_p);
     const float r = u[b];
     if (tid == 0) n_list = 0, first_at = 0xffffffffu;
+    bins[tid] = 0;
+    tile_sum[tid] = 0;
+    auto choose = [&](int at, double share) {
+        token[b] = at;
+        if (prob) prob[b] = (float)share;
+    };
 
     // calls f(piece, values) for this thread's pieces, four loads on their way at a time
     auto each = [&](auto f) __attribute__((always_inline)) {
@@ -134,329 +531,598 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(const T* __restr
             f(j, x);
         }
     };
+    // calls f(piece, values) for the wave's tiles (a lane without a piece gets no numbers), done(tile) behind each
+    auto each_tile = [&](auto f, auto done) __attribute__((always_inline)) {
+        for (int t = wave; t < row.tiles; t += SAMPLE_WAVES) {
+            for (int q = 0; q < row.steps; ++q) {
+                const int j = (t * row.steps + q) * 64 + lane;
+                float x[VEC];
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) x[e] = NAN;
+                if (j < row.pieces) row.load(j, x);
+                f(j, x);
+            }
+            done(t);
+        }
+    };
+    // sum of one number a wave over the workgroup
+    auto all_waves = [&](u64 x) {
+        if (lane == 0) sums[wave] = x;
+        __syncthreads();
+        u64 t = 0;
+        for (int w = 0; w < SAMPLE_WAVES; ++w) t += sums[w];
+        __syncthreads();
+        return t;
+    };
 
     // ---- the largest logit, and each thread's
-    float mine = -INFINITY;
-    each([&](int, float (&x)[VEC]) __attribute__((always_inline)) {
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) mine = fmaxf(mine, x[e]);
-    });
-    float most = mine;
-#pragma unroll
-    for (int o = 32; o; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
-    if (lane == 0) maxima[wave] = most;
-    bins[tid] = 0;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < SAMPLE_WAVES; ++w) most = fmaxf(most, maxima[w]);
-    if (most == -INFINITY) {    // nothing but -inf and what is no number
-        if (tid == 0) {
-            token[b] = -1;
-            if (prob) prob[b] = 0.f;
-        }
-        return;
-    }
-    if (!(t > 0.f)) {           // greedy: where it is first
-        if (mine == most)
-            each([&](int j, float (&x)[VEC]) __attribute__((always_inline)) {
-#pragma unroll
-                for (int e = VEC - 1; e >= 0; --e)
-                    if (x[e] == most) atomicMin(&first_at, (uint32_t)(row.first(j) + e));
-            });
+    float mine = -INFINITY, most;
+    if constexpr (SPLIT) {
+        most = sc.state[b].most;
         __syncthreads();
-        if (tid == 0) {
-            token[b] = (int32_t)first_at;
-            if (prob) prob[b] = 1.f;
+    } else {
+        each([&](int, float (&x)[VEC]) __attribute__((always_inline)) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) mine = fmaxf(mine, x[e]);
+        });
+        most = wave_max(mine);
+        if (lane == 0) maxima[wave] = most;
+        __syncthreads();
+        for (int w = 0; w < SAMPLE_WAVES; ++w) most = fmaxf(most, maxima[w]);
+    }
+    if (most == -INFINITY) {    // nothing but -inf and what is no number
+        if (tid == 0) choose(-1, 0.0);
+        return;
+    }
+    if (s.greedy()) {           // where it is first
+        if constexpr (SPLIT) {
+            if (tid == 0) choose((int)sc.state[b].first_at, 1.0);
+        } else {
+            if (mine == most)
+                each([&](int j, float (&x)[VEC]) __attribute__((always_inline)) {
+#pragma unroll
+                    for (int e = VEC - 1; e >= 0; --e)
+                        if (x[e] == most) atomicMin(&first_at, (uint32_t)(row.first(j) + e));
+                });
+            __syncthreads();
+            if (tid == 0) choose((int)first_at, 1.0);
         }
         return;
     }
-    const float per_t = 1.4426950408889634f / t;
-    // weight of x as a number of octaves below the largest
-    auto octaves = [&](float x) __attribute__((always_inline)) { return x == most ? 0.f : (most - x) * per_t; };
-    auto weight = [](float oct) __attribute__((always_inline)) { return __builtin_amdgcn_exp2f(-oct); };
-    auto bin_of = [](float oct) __attribute__((always_inline)) {
-        return min((int)(oct * (SAMPLE_BINS / SAMPLE_OCTAVES)), SAMPLE_BINS - 1);
-    };
-    auto counts = [](float oct) __attribute__((always_inline)) { return oct < SAMPLE_OCTAVES; };   // (not: far, or no number)
+    s.measure(most);
+    row.endless = most == INFINITY;
+    if (row.endless) mine = mine == most ? 0.f : -INFINITY;
+    const bool by_k = s.by_k, by_p = s.by_p, by_least = s.by_least;
 
-    // the bin, from bin 0 on (from the last on for `down`), in which the running sum of the bins reaches `want`, and what
-    // came before it; bin -1 where it never does.  All threads call it behind a barrier; bins are clear afterwards.
+    // the bin, thread tid having bin `at` of size v, in which the running sum in ascending bin reaches `want`, and what came
+    // before it; bin -1 where it never does.  bins[at] is clear afterwards.
     struct Border {
         int bin;
-        uint64_t before;
+        u64 before;
     };
-    auto border = [&](uint64_t want, bool down) {
-        const int at = down ? SAMPLE_BINS - 1 - tid : tid;
-        const uint64_t v = bins[at], inc = wave_running(v, lane);
+    auto border_of = [&](u64 v, int at, u64 want) {
+        const u64 inc = wave_running(v);
         if (lane == 63) sums[wave] = inc;
-        if (tid == 0) found[0] = ~0ull;
+        if (tid == 0) found[0] = ~(u64)0;
         __syncthreads();
-        uint64_t before = inc - v;
-        for (int w = 0; w < wave; ++w) before += sums[w];
-        if (before < want && before + v >= want) found[0] = (uint64_t)at, found[1] = before;
+        u64 before = inc - v;
+#pragma unroll
+        for (int w = 0; w < SAMPLE_WAVES; ++w) before += w < wave ? sums[w] : 0;
+        if (before < want && before + v >= want) found[0] = (u64)at, found[1] = before;
         bins[at] = 0;
         __syncthreads();
         const Border x = {(int)found[0], found[1]};
         __syncthreads();
         return x;
     };
-    // tokens for which f holds into the list (as many as it takes); n_list counts all of them
-    auto gather = [&](auto f) __attribute__((always_inline)) {
-        each([&](int j, float (&x)[VEC]) __attribute__((always_inline)) {
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                const uint32_t i = (uint32_t)(row.first(j) + e);
-                if (f(x[e], i)) {
-                    const uint32_t at = atomicAdd(&n_list, 1u);
-                    if (at < SAMPLE_THREADS) list[at] = place_of(x[e], i);
-                }
-            }
-        });
-        __syncthreads();
+    auto border = [&](u64 want, bool down) {
+        const int at = down ? SAMPLE_BINS - 1 - tid : tid;
+        return border_of(bins[at], at, want);
     };
-
     const double share = (double)(r > 0.f ? fminf(r, 1.f) : 0.f);
-    auto aim_of = [&](uint64_t total) {       // the running sum that the token passes
-        const uint64_t a = (uint64_t)(share * (double)total);
+    auto aim_of = [&](u64 total) {            // the running sum that the token passes
+        const u64 a = (u64)(share * (double)total);
         return a < total ? a : total - 1;
     };
-    auto part_of = [&](uint64_t total) {      // less than this comes before a token that top_p lets stay
-        const uint64_t a = (uint64_t)ceil((double)fmaxf(p, 0.f) * (double)total);
-        return a < 1 ? 1ull : a < total ? a : total;
+
+    // Of the list's n entries, by descending key: the one that brings the sum of their sizes to `want`, and its size; 0
+    // where they never do.  bin_of_entry: 0 .. SAMPLE_BINS - 1, not descending as the key ascends; finer bins, between the
+    // smallest and the largest key that are left, follow until few enough are in one to be compared with each other.
+    auto locate = [&](int n, auto bin_of_entry, auto key_of, auto size_of, u64 want, u64& size) __attribute__((always_inline)) {
+        constexpr int MOST = 64;              // entries that are compared with each other, sixteen threads each
+        for (int q = tid; q < n; q += SAMPLE_THREADS) {
+            const u64 e = list[q], m = size_of(e);
+            if (m) atomicAdd(&bins[bin_of_entry(e)], m);
+        }
+        __syncthreads();
+        Border x = border(want, false);
+        const int bin = x.bin;
+        u64 lo = 0, hi = ~(u64)0;
+        size = 0;
+        while (x.bin >= 0) {
+            want -= x.before;
+            if (tid == 0) n_list = 0, found[0] = found[2] = 0, found[1] = ~(u64)0;
+            __syncthreads();
+            auto left = [&](u64 e) { return bin_of_entry(e) == bin && key_of(e) >= lo && key_of(e) <= hi && size_of(e); };
+            for (int q = tid; q < n; q += SAMPLE_THREADS)
+                if (left(list[q])) {
+                    const uint32_t to = atomicAdd(&n_list, 1u);
+                    if (to < MOST) few[to] = list[q];
+                }
+            __syncthreads();
+            const int c = (int)n_list;
+            if (c <= MOST) {
+                const int i = tid >> 4, part = tid & 15;      // thread `part` of entry i
+                u64 before = 0, me = 0, mine_size = 0;
+                if (i < c) {
+                    me = few[i], mine_size = size_of(me);
+                    for (int q = part; q < c; q += 16)
+                        if (key_of(few[q]) > key_of(me)) before += size_of(few[q]);
+                }
+#pragma unroll
+                for (int o = 8; o; o >>= 1) before += __shfl_xor(before, o);
+                if (i < c && part == 0 && before < want && before + mine_size >= want) found[0] = me, found[1] = mine_size;
+                __syncthreads();
+                const u64 at = found[0];
+                size = found[1];
+                __syncthreads();
+                return at;
+            }
+            for (int q = tid; q < n; q += SAMPLE_THREADS)
+                if (left(list[q])) {
+                    atomicMin(&found[1], key_of(list[q]));
+                    atomicMax(&found[2], key_of(list[q]));
+                }
+            __syncthreads();
+            lo = found[1], hi = found[2];
+            const int bits = 64 - __clzll((long long)(hi - lo)), shift = bits > 10 ? bits - 10 : 0;
+            for (int q = tid; q < n; q += SAMPLE_THREADS)
+                if (left(list[q])) atomicAdd(&bins[(key_of(list[q]) - lo) >> shift], size_of(list[q]));
+            __syncthreads();
+            x = border(want, true);
+            lo += (u64)max(x.bin, 0) << shift;
+            hi = min(hi, lo + (((u64)1 << shift) - 1));
+        }
+        return (u64)0;
     };
 
-    uint64_t cut = 0;                         // last place that stays
-    if (k > 0 && k < V) {
-        bool listed = false;
-        if (k <= SAMPLE_THREADS) {
-            const float oct = octaves(mine);
-            if (mine > -INFINITY && counts(oct)) atomicAdd((unsigned long long*)&bins[bin_of(oct)], 1ull);
+    // ---- what can stay, as a list
+    const bool can = by_k ? SPLIT ? s.k <= sc.slices * SLICE_THREADS : s.k <= SAMPLE_THREADS
+                          : by_least || (!SPLIT && by_p && V <= SAMPLE_LIST);
+    if (can) {
+        u64 total = 0;
+        if constexpr (SPLIT) {
+            n_list = sc.state[b].n_list;      // (all threads the same)
+            const int n = min((int)n_list, SAMPLE_LIST);
+            for (int i = tid; i < n; i += SAMPLE_THREADS) list[i] = sc.list[(size_t)b * SAMPLE_LIST + i];
+            if (by_p && !by_k)
+                for (int i = 0; i < sc.slices; ++i) total += sc.total[(size_t)b * sc.slices + i];
             __syncthreads();
-            const Border x = border((uint64_t)k, false);
-            const int last = x.bin < 0 ? SAMPLE_BINS - 1 : x.bin;
-            gather([&](float v, uint32_t) __attribute__((always_inline)) {
-                const float oct_v = octaves(v);
-                return counts(oct_v) && bin_of(oct_v) <= last;
+        } else {
+            float low = LOWEST;
+            const float oct = s.octaves(mine);
+            if (by_k) {
+                if (s.counts(oct)) atomicAdd(&bins[s.bin_of(oct)], (u64)1);
+                __syncthreads();
+                const Border x = border((u64)s.k, false);
+                if (x.bin >= 0) {             // the smallest maximum of the bins up to it
+                    const float m = -wave_max(s.counts(oct) && s.bin_of(oct) <= x.bin ? -mine : -INFINITY);
+                    if (lane == 0) maxima[wave] = m;
+                    __syncthreads();
+                    low = maxima[0];
+                    for (int w = 1; w < SAMPLE_WAVES; ++w) low = fminf(low, maxima[w]);
+                }
+            } else if (by_least) {
+                low = s.least_logit();
+            }
+            const bool sum = by_p && !by_k;
+            each([&](int j, float (&x)[VEC]) __attribute__((always_inline)) {
+                bool in[VEC];
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) in[e] = x[e] >= low;
+                append_places<VEC>(x, in, row.first(j), &n_list, list, SAMPLE_LIST, lane);
+                if (sum) {
+                    float w = 0.f;
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) w += fmaxf(s.weight(s.octaves(x[e])), 0.f);    // (no number: 0)
+                    total += whole(w);
+                }
             });
-            listed = n_list <= SAMPLE_THREADS;
+            if (sum) total = all_waves(wave_total(total));
+            else __syncthreads();
         }
-        if (listed) {
-            // ---- everything on the list: in order by counting who is earlier
-            const int n = (int)n_list;
-            if (tid < n) {
-                const uint64_t me = list[tid];
+        const int n = (int)n_list;
+        if (n <= SAMPLE_LIST) {
+            if (n <= SAMPLE_THREADS / 4) {
+                // ---- a short list: in order by counting who is earlier, four threads an entry
+                const int i = tid >> 2, part = tid & 3;
+                const u64 entry = i < n ? list[i] : 0;
                 int rank = 0;
-                for (int s = 0; s < n; ++s) rank += list[s] > me ? 1 : 0;
-                sorted[rank] = me;
+#pragma unroll 4
+                for (int q = part; q < n; q += 4) rank += list[q] > entry ? 1 : 0;
+                rank += __shfl_xor(rank, 1);
+                rank += __shfl_xor(rank, 2);
+                if (i < n && part == 0) few[rank] = entry;
+                __syncthreads();
+                const u64 me = tid < n ? few[tid] : 0;
+                const float w = tid < n ? s.weight(s.octaves(place_logit(me))) : 0.f;
+                const bool in_k = tid < n && (!by_k || tid < s.k);
+                const u64 m = in_k ? whole(w) : 0, inc = wave_running(m);
+                if (lane == 63) sums[wave] = inc;
+                __syncthreads();
+                u64 before = inc - m, sum = 0;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    before += q < wave ? sums[q] : 0;
+                    sum += sums[q];
+                }
+                const bool stays = in_k && (!by_p || before < s.part_of(by_k ? sum : total)) && (!by_least || w >= s.least);
+                list[tid] = stays ? m : 0;
+                __syncthreads();
+                const u64 kept = all_waves(wave_total(stays ? m : 0)), aim = aim_of(kept);
+                // the running sum in ascending index, four threads an entry again
+                const u64 again = i < n ? few[i] : 0, size = i < n ? list[i] : 0;
+                before = 0;
+#pragma unroll 4
+                for (int q = part; q < n; q += 4) before += place_index(few[q]) < place_index(again) ? list[q] : 0;
+                before += __shfl_xor(before, 1);
+                before += __shfl_xor(before, 2);
+                if (part == 0 && before <= aim && aim < before + size) choose((int)place_index(again), (double)size / (double)kept);
+                return;
             }
-            __syncthreads();
-            const uint64_t me = tid < n ? sorted[tid] : 0;
-            const float w = tid < n ? weight(octaves(place_logit(me))) : 0.f;
-            const uint64_t m = tid < min(n, k) ? whole(w) : 0;
-            const uint64_t inc = wave_running(m, lane);
-            if (lane == 63) sums[wave] = inc;
-            __syncthreads();
-            uint64_t before = inc - m, total = 0;
-            for (int s = 0; s < SAMPLE_WAVES; ++s) {
-                if (s < wave) before += sums[s];
-                total += sums[s];
+            auto place_itself = [](u64 q) __attribute__((always_inline)) { return q; };
+            auto by_index = [](u64 q) __attribute__((always_inline)) { return q & 0xffffffffu; };    // (descending: ascending indices)
+            auto octave_bin = [&](u64 q) __attribute__((always_inline)) { return s.bin_of(s.octaves(place_logit(q))); };
+            const uint32_t per_bin = ((uint32_t)V + SAMPLE_BINS - 1) / SAMPLE_BINS;
+            u64 cut = 0, m;
+            if (by_k && n > s.k) cut = locate(n, octave_bin, place_itself, [](u64) { return (u64)1; }, (u64)s.k, m);
+            auto mass_from = [&](u64 q) __attribute__((always_inline)) { return q >= cut ? s.mass_of(q) : 0; };
+            auto sum_of = [&](auto f) __attribute__((always_inline)) {
+                u64 t = 0;
+                for (int q = tid; q < n; q += SAMPLE_THREADS) t += f(list[q]);
+                return all_waves(wave_total(t));
+            };
+            if (by_p) {
+                const u64 here = sum_of(mass_from), want = s.part_of(by_k ? here : total);
+                // (less on the list than that: all of it stays)
+                if (here >= want) cut = locate(n, octave_bin, place_itself, mass_from, want, m);
             }
-            const bool stays = tid < min(n, k) && (!(p < 1.f) || before < part_of(total)) && (!by_least || w >= least);
-            __syncthreads();
-            const uint64_t kept = wave_total(stays ? m : 0);
-            if (lane == 0) sums[wave] = kept;
-            list[tid] = stays ? m : 0;
-            const int n_kept = __syncthreads_count(stays);
-            total = 0;
-            for (int s = 0; s < SAMPLE_WAVES; ++s) total += sums[s];
-            if (!stays) return;
-            const uint64_t aim = aim_of(total);
-            const uint32_t i = place_index(me);
-            before = 0;
-            for (int s = 0; s < n_kept; ++s) before += place_index(sorted[s]) < i ? list[s] : 0;
-            if (before <= aim && aim < before + m) {
-                token[b] = (int32_t)i;
-                if (prob) prob[b] = (float)((double)m / (double)total);
-            }
+            auto mass_kept = [&](u64 q) __attribute__((always_inline)) {
+                const float w = s.weight(s.octaves(place_logit(q)));
+                return q >= cut && (!by_least || w >= s.least) ? whole(w) : 0;
+            };
+            const u64 kept = sum_of(mass_kept);
+            const u64 at = locate(n, [&](u64 q) { return (int)(place_index(q) / per_bin); }, by_index, mass_kept, aim_of(kept) + 1, m);
+            if (tid == 0) choose((int)place_index(at), (double)m / (double)kept);
             return;
         }
     }
 
-    // last place, of those before `from`, at which the running sum in descending order of ones or of weights reaches `want`;
-    // `small`: weights below it need not be looked at
-    auto place = [&](bool by_mass, uint64_t from, uint64_t want, float small) {
+    // ---- borders from the whole row: the last place of those before `from` at which the running sum in descending order,
+    // of ones or of weights, reaches `want`
+    auto place = [&](bool by_mass, u64 from, u64 want) {
+        auto size = [&](float oct) __attribute__((always_inline)) { return by_mass ? whole(s.weight(oct)) : (u64)1; };
         auto look = [&](auto f) __attribute__((always_inline)) {
             each([&](int j, float (&x)[VEC]) __attribute__((always_inline)) {
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
-                    const float oct = octaves(x[e]);
-                    if (counts(oct)) {
-                        const float w = weight(oct);
-                        const uint64_t at = place_of(x[e], (uint32_t)(row.first(j) + e));
-                        if (w >= small && at >= from) f(oct, at, by_mass ? whole(w) : 1ull);
+                    const float oct = s.octaves(x[e]);
+                    if (s.counts(oct)) {
+                        const u64 at = place_of(x[e], (uint32_t)(row.first(j) + e));
+                        if (at >= from) f(oct, at);
                     }
                 }
             });
             __syncthreads();
         };
-        auto histogram = [&]() __attribute__((always_inline)) {
-            look([&](float oct, uint64_t, uint64_t m) __attribute__((always_inline)) {
-                atomicAdd((unsigned long long*)&bins[bin_of(oct)], (unsigned long long)m);
-            });
-            return border(want, false);
-        };
-        Border x = histogram();
-        if (x.bin < 0 && small > 0.f) {       // (a share so near 1 that the roundings of the sums are more than the rest)
-            small = 0.f;
-            x = histogram();
-        }
+        look([&](float oct, u64) __attribute__((always_inline)) { atomicAdd(&bins[s.bin_of(oct)], size(oct)); });
+        Border x = border(want, false);
         if (x.bin < 0) return from;
         want -= x.before;
         const int bin = x.bin;
-        uint64_t lo = 0, hi = ~0ull;          // places that are left of that bin's
+        u64 lo = 0, hi = ~(u64)0;             // places that are left of that bin's
         for (;;) {
-            if (tid == 0) n_list = 0, found[1] = ~0ull, found[2] = 0;
+            if (tid == 0) n_list = 0, found[1] = ~(u64)0, found[2] = 0;
             __syncthreads();
-            look([&](float oct, uint64_t at, uint64_t) __attribute__((always_inline)) {
-                if (bin_of(oct) != bin || at < lo || at > hi) return;
+            look([&](float oct, u64 at) __attribute__((always_inline)) {
+                if (s.bin_of(oct) != bin || at < lo || at > hi) return;
                 const uint32_t q = atomicAdd(&n_list, 1u);
-                if (q < SAMPLE_THREADS) list[q] = at;
+                if (q < SAMPLE_THREADS) few[q] = at;
                 else {                        // too many: what a finer histogram has to cover
-                    atomicMin((unsigned long long*)&found[1], (unsigned long long)at);
-                    atomicMax((unsigned long long*)&found[2], (unsigned long long)at);
+                    atomicMin(&found[1], at);
+                    atomicMax(&found[2], at);
                 }
             });
             const int n = (int)min(n_list, (uint32_t)SAMPLE_THREADS);
+            const u64 me = tid < n ? few[tid] : 0;
             if (n_list <= SAMPLE_THREADS) {
                 if (tid < n) {
-                    const uint64_t me = list[tid];
-                    uint64_t before = 0;
-                    for (int s = 0; s < n; ++s)
-                        if (list[s] > me) before += by_mass ? whole(weight(octaves(place_logit(list[s])))) : 1ull;
-                    if (before < want && before + (by_mass ? whole(weight(octaves(place_logit(me)))) : 1ull) >= want) found[0] = me;
+                    u64 before = 0;
+                    for (int q = 0; q < n; ++q)
+                        if (few[q] > me) before += size(s.octaves(place_logit(few[q])));
+                    if (before < want && before + size(s.octaves(place_logit(me))) >= want) found[0] = me;
                 }
                 __syncthreads();
-                const uint64_t at = found[0];
+                const u64 at = found[0];
                 __syncthreads();
                 return at;
             }
             // (those on the list take part in the range too)
             if (tid < n) {
-                atomicMin((unsigned long long*)&found[1], (unsigned long long)list[tid]);
-                atomicMax((unsigned long long*)&found[2], (unsigned long long)list[tid]);
+                atomicMin(&found[1], me);
+                atomicMax(&found[2], me);
             }
             __syncthreads();
             lo = found[1], hi = found[2];
             const int bits = 64 - __clzll((long long)(hi - lo)), shift = bits > 10 ? bits - 10 : 0;
             __syncthreads();
-            look([&](float oct, uint64_t at, uint64_t m) __attribute__((always_inline)) {
-                if (bin_of(oct) == bin && at >= lo && at <= hi)
-                    atomicAdd((unsigned long long*)&bins[(at - lo) >> shift], (unsigned long long)m);
+            look([&](float oct, u64 at) __attribute__((always_inline)) {
+                if (s.bin_of(oct) == bin && at >= lo && at <= hi) atomicAdd(&bins[(at - lo) >> shift], size(oct));
             });
             x = border(want, true);
             want -= x.before;
-            lo += (uint64_t)x.bin << shift;
-            hi = min(hi, lo + (((uint64_t)1 << shift) - 1));
+            lo += (u64)x.bin << shift;
+            hi = min(hi, lo + (((u64)1 << shift) - 1));
         }
     };
-    if (k > 0 && k < V) cut = place(false, 0, (uint64_t)k, 0.f);
-    // sum of the weights of f's tokens over a piece: 32 bits, in order
-    if (p < 1.f) {
-        uint64_t total = 0;
-        each([&](int j, float (&x)[VEC]) __attribute__((always_inline)) {
-            float s = 0.f;
+    const u64 cut = by_k ? place(false, 0, (u64)s.k) : 0;
+    float border_x = LOWEST;
+    int border_i = V;
+    auto set_border = [&](u64 at) {
+        if (at) border_x = place_logit(at), border_i = (int)place_index(at);
+    };
+    set_border(cut);
+    auto before_border = [&](int e, float x, int left) __attribute__((always_inline)) {   // left: border_i - index of e = 0
+        return x > border_x || (x == border_x && e <= left);
+    };
+    auto mass_at = [&](int e, float x, int left) __attribute__((always_inline)) {
+        const float w = s.weight(s.octaves(x));
+        return before_border(e, x, left) && (!by_least || w >= s.least) ? w : 0.f;
+    };
+
+    bool summed = false, bordered = !by_p;
+    if (by_p) {
+        // how many tokens lie in each bin, and from that the bins around the border
+        float first, last;
+        if constexpr (SPLIT) {
+            first = sc.state[b].window0, last = sc.state[b].window1;
+        }
+        const bool left_over = SPLIT && !by_k && !by_least;      // (the launches before this one did it)
+        if (!left_over) {
+            each([&](int j, float (&x)[VEC]) __attribute__((always_inline)) {
+                const int left = border_i - row.first(j);
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                const float oct = octaves(x[e]);
-                s += counts(oct) && place_of(x[e], (uint32_t)(row.first(j) + e)) >= cut ? weight(oct) : 0.f;
+                for (int e = 0; e < VEC; ++e) {
+                    const float oct = s.octaves(x[e]);
+                    if (s.counts(oct) && before_border(e, x[e], left)) atomicAdd(&bins[s.bin_of(oct)], s.tallied(oct));
+                }
+            });
+            __syncthreads();
+            const u64 about = s.about(bins[tid], tid), want = s.part_of(all_waves(wave_total(about)));
+            const Border x = border_of(about, tid, s.early(want)), y = border_of(about, tid, s.late(want));
+            first = (float)(x.bin - 1) * WIDTH, last = (float)((y.bin < 0 ? SAMPLE_BINS : y.bin) + 2) * WIDTH;
+        }
+        if (by_least && -__builtin_amdgcn_logf(s.least) < first) bordered = true;    // (min_p alone says what stays)
+        else {
+            u64 total = 0;
+            if (left_over) {
+                tile_sum[tid] = tid < row.tiles ? sc.tile_sum[(size_t)b * SAMPLE_BINS + tid] : 0;
+                for (int i = 0; i < sc.slices; ++i) total += sc.total[(size_t)b * sc.slices + i];
+                n_list = sc.state[b].n_list;  // (all threads the same)
+                const int n = min((int)n_list, SAMPLE_LIST);
+                for (int i = tid; i < n; i += SAMPLE_THREADS) list[i] = sc.list[(size_t)b * SAMPLE_LIST + i];
+                __syncthreads();
+            } else {
+                if (tid == 0) n_list = 0;
+                __syncthreads();
+                u64 tile = 0;
+                each_tile([&](int j, float (&x)[VEC]) __attribute__((always_inline)) {
+                    float sure = 0.f, any = 0.f;
+                    const int left = border_i - row.first(j);
+                    bool in[VEC];
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) {
+                        const float oct = s.octaves(x[e]);
+                        const bool ok = before_border(e, x[e], left);
+                        const float w = ok ? s.weight(oct) : 0.f;
+                        any += w;
+                        sure += oct < first ? w : 0.f;
+                        in[e] = ok && oct >= first && oct < last;
+                    }
+                    append_places<VEC>(x, in, row.first(j), &n_list, list, SAMPLE_LIST, lane);
+                    total += whole(any);
+                    tile += whole(sure);
+                }, [&](int t) __attribute__((always_inline)) {
+                    tile = wave_total(tile);
+                    if (lane == 0) tile_sum[t] = tile;
+                    tile = 0;
+                });
+                total = all_waves(wave_total(total));
             }
-            total += whole(s);
+            const int n = (int)n_list;
+            const u64 sure = all_waves(wave_total(tile_sum[tid])), want = s.part_of(total);
+            u64 at = 0, size;
+            if (n <= SAMPLE_LIST && sure < want)
+                at = locate(n, [&](u64 q) {
+                    const float f = (s.octaves(place_logit(q)) - first) * (SAMPLE_BINS / (last - first));
+                    return min(max((int)f, 0), SAMPLE_BINS - 1);
+                }, [](u64 q) { return q; }, [&](u64 q) { return s.mass_of(q); }, want - sure, size);
+            if (at) {
+                set_border(at);
+                for (int q = tid; q < n; q += SAMPLE_THREADS) {
+                    const u64 me = list[q];
+                    if (me >= at && (!by_least || s.weight(s.octaves(place_logit(me))) >= s.least))
+                        atomicAdd(&tile_sum[((int)place_index(me) + row.off) / (VEC * 64 * row.steps)], s.mass_of(me));
+                }
+                __syncthreads();
+                summed = bordered = true;
+            }
+        }
+    }
+    if (!bordered) {                          // (many tokens that are alike at the border)
+        u64 total = 0;
+        each([&](int j, float (&x)[VEC]) __attribute__((always_inline)) {
+            const int left = border_i - row.first(j);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e)
+                total += before_border(e, x[e], left) ? whole(s.weight(s.octaves(x[e]))) : 0;
         });
-        total = wave_total(total);
-        if (lane == 0) sums[wave] = total;
-        __syncthreads();
-        total = 0;
-        for (int s = 0; s < SAMPLE_WAVES; ++s) total += sums[s];
-        __syncthreads();
-        // all tokens of less than (1 - p) total / V together hold less than what top_p leaves out: the border is above
-        // them (a quarter of that, for the roundings of the sums)
-        const float small = (float)(0.25 * (1.0 - (double)fmaxf(p, 0.f)) * ((double)total * 0x1p-40) / V);
-        cut = place(true, cut, part_of(total), small);
+        total = all_waves(wave_total(total));
+        set_border(place(true, cut, s.part_of(total)));
     }
 
-    // ---- the running sum in ascending index: a wave owns a contiguous run of pieces, 64 at a time a tile
-    const int run = (row.pieces + SAMPLE_WAVES * 64 - 1) / (SAMPLE_WAVES * 64) * 64;
-    const int lo = wave * run, hi = min(lo + run, row.pieces);
-    auto mass_at = [&](int e, float x, int i0) __attribute__((always_inline)) {
-        const float oct = octaves(x), w = weight(oct);
-        return counts(oct) && place_of(x, (uint32_t)(i0 + e)) >= cut && (!by_least || w >= least) ? w : 0.f;
-    };
-    auto piece_mass = [&](int j) __attribute__((always_inline)) {
-        float s = 0.f;
-        if (j < hi) {
-            float x[VEC];
-            row.load(j, x);
+    // ---- the tile in which the running sum in ascending index passes the aim, and the token in it
+    if (!summed) {
+        if (SPLIT && !by_k && !by_p && !by_least) {
+            tile_sum[tid] = tid < row.tiles ? sc.tile_sum[(size_t)b * SAMPLE_BINS + tid] : 0;
+        } else {
+            u64 tile = 0;
+            each_tile([&](int j, float (&x)[VEC]) __attribute__((always_inline)) {
+                const int left = border_i - row.first(j);
+                float sum = 0.f;
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) s += mass_at(e, x[e], row.first(j));
+                for (int e = 0; e < VEC; ++e) sum += mass_at(e, x[e], left);
+                tile += whole(sum);
+            }, [&](int t) __attribute__((always_inline)) {
+                tile = wave_total(tile);
+                if (lane == 0) tile_sum[t] = tile;
+                tile = 0;
+            });
         }
-        return whole(s);
-    };
-    uint64_t own = 0;
-    {
-        int q = 0;
-        for (int j0 = lo; j0 < hi; j0 += 64, ++q) {
-            const uint64_t m = wave_total(piece_mass(j0 + lane));
-            if (q < SAMPLE_TILES && lane == 0) tile_sum[wave][q] = m;
-            own += m;
+        __syncthreads();
+    }
+    const u64 total = all_waves(wave_total(tile_sum[tid])), aim = aim_of(total);
+    const Border in = border_of(tile_sum[tid], tid, aim + 1);
+    if (wave != 0) return;
+    // (a tile's sum and that of its pieces may differ in the last 2^-40 where the border's tokens were added: the last
+    // token that stays then)
+    u64 before = in.before;
+    int last = -1;
+    float last_w = 0.f;
+    for (int q = 0; q < row.steps; ++q) {
+        const int j = (in.bin * row.steps + q) * 64 + lane, i0 = row.first(j);
+        float x[VEC], v[VEC], sum = 0.f;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) x[e] = NAN;
+        if (j < row.pieces) row.load(j, x);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            v[e] = mass_at(e, x[e], border_i - i0);
+            sum += v[e];
+            if (v[e] > 0.f) last = i0 + e, last_w = v[e];
         }
-    }
-    if (lane == 0) sums[wave] = own;
-    __syncthreads();
-    uint64_t total = 0, before = 0;
-    for (int s = 0; s < SAMPLE_WAVES; ++s) {
-        if (s < wave) before += sums[s];
-        total += sums[s];
-    }
-    const uint64_t aim = aim_of(total);
-    if (aim < before || aim >= before + own) return;     // (another wave's)
-    int j0 = lo;
-    for (int q = 0; q < SAMPLE_TILES && before + tile_sum[wave][q] <= aim; ++q, j0 += 64) before += tile_sum[wave][q];
-    for (; j0 < hi; j0 += 64) {
-        const uint64_t m = piece_mass(j0 + lane), inc = wave_running(m, lane);
-        const uint64_t past = __ballot(before + inc > aim);
+        const u64 m = whole(sum), inc = wave_running(m);
+        const u64 past = __ballot(before + inc > aim);
         if (past) {
-            if (lane == __ffsll((unsigned long long)past) - 1) {
-                const uint64_t left = aim - (before + inc - m);
-                const int j = j0 + lane, i0 = row.first(j);
-                float x[VEC], s = 0.f, w = 0.f;
-                row.load(j, x);
+            if (lane == __ffsll(past) - 1) {
+                const u64 left = aim - (before + inc - m);
+                float run = 0.f, w = 0.f;
                 int at = -1;
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
-                    const float v = mass_at(e, x[e], i0);
-                    s += v;
-                    if (at < 0 && whole(s) > left) at = e, w = v;
+                    run += v[e];
+                    if (at < 0 && whole(run) > left) at = e, w = v[e];
                 }
-                token[b] = i0 + at;
-                if (prob) prob[b] = (float)((double)w * 0x1p40 / (double)total);
+                choose(i0 + at, (double)w * 0x1p40 / (double)total);
             }
             return;
         }
         before += __shfl(inc, 63);
     }
+    int end = last;
+#pragma unroll
+    for (int o = 32; o; o >>= 1) end = max(end, __shfl_xor(end, o));
+    if (last == end && last >= 0) choose(last, (double)last_w * 0x1p40 / (double)total);
 }
+
+// ---- host ------------------------------------------------------------------------------------------------------------
+namespace {
+
+constexpr int SLICE_TOKENS = 16384;       // a slice at least; a row has at most 32
+constexpr int ONE_WORKGROUP = 32768;      // tokens of a row that one workgroup takes by itself
+
+// bytes of scratch a row, and where its parts lie for `rows` rows
+size_t sample_scratch(char* base, int rows, int slices, SampleScratch* sc) {
+    size_t off = 0;
+    auto take = [&](size_t bytes) {
+        char* p = base ? base + off : nullptr;
+        off += align_up(bytes * rows, 256);
+        return p;
+    };
+    SampleScratch s{};
+    s.state = reinterpret_cast<RowState*>(take(sizeof(RowState)));
+    s.maxima = reinterpret_cast<float*>(take((size_t)slices * SLICE_THREADS * 4));
+    s.tally = reinterpret_cast<u64*>(take(SAMPLE_BINS * 8));
+    s.tile_sum = reinterpret_cast<u64*>(take(SAMPLE_BINS * 8));
+    s.total = reinterpret_cast<u64*>(take((size_t)slices * 8));
+    s.list = reinterpret_cast<u64*>(take((size_t)SAMPLE_LIST * 8));
+    s.slices = slices;
+    if (sc) *sc = s;
+    return off;
+}
+
+template <typename T, bool SPLIT>
+int choose_rows(const T* logits, int64_t stride, int B, int V, const float* temperature, const int32_t* top_k,
+                const float* top_p, const float* min_p, const float* u, int32_t* token, float* prob, const SampleScratch& sc,
+                hipStream_t st) {
+    static bool lds_set[kMaxDevices] = {};
+    const size_t lds = (size_t)SAMPLE_LIST * sizeof(u64);
+    int dev = 0;   // (the dynamic-LDS limit is raised once per device)
+    MVLA_HIP_CHECK(hipGetDevice(&dev));
+    if (dev < 0 || dev >= kMaxDevices || !lds_set[dev]) {
+        MVLA_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void*>(&sample_kernel<T, SPLIT>),
+                                           hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+        if (dev >= 0 && dev < kMaxDevices) lds_set[dev] = true;
+    }
+    hipLaunchKernelGGL((sample_kernel<T, SPLIT>), dim3(B), dim3(SAMPLE_THREADS), lds, st, logits, stride, V, temperature,
+                       top_k, top_p, min_p, u, token, prob, sc);
+    MVLA_HIP_CHECK(hipGetLastError());
+    return MVLA_OK;
+}
+
+template <typename T>
+int sample_rows(const T* logits, int64_t stride, int B, int V, const float* temperature, const int32_t* top_k,
+                const float* top_p, const float* min_p, const float* u, int32_t* token, float* prob, char* scratch,
+                size_t scratch_bytes, hipStream_t st) {
+    if (V <= ONE_WORKGROUP)
+        return choose_rows<T, false>(logits, stride, B, V, temperature, top_k, top_p, min_p, u, token, prob, SampleScratch{}, st);
+    int slices = (V + SLICE_TOKENS - 1) / SLICE_TOKENS;
+    if (slices > 32) slices = 32;
+    int rows = B;
+    while (rows > 1 && sample_scratch(nullptr, rows, slices, nullptr) > scratch_bytes) rows = (rows + 1) / 2;
+    for (int b0 = 0; b0 < B; b0 += rows) {
+        const int n = B - b0 < rows ? B - b0 : rows;
+        auto at = [&](auto* p) { return p ? p + b0 : nullptr; };
+        SampleScratch sc;
+        sample_scratch(scratch, rows, slices, &sc);
+        const T* x = logits + b0 * stride;
+        const dim3 grid(slices, n);
+        hipLaunchKernelGGL((sample_max_kernel<T>), grid, dim3(SLICE_THREADS), 0, st, x, stride, V, sc);
+        MVLA_HIP_CHECK(hipGetLastError());
+        hipLaunchKernelGGL((sample_collect_kernel<T>), grid, dim3(SLICE_THREADS), 0, st, x, stride, V, at(temperature),
+                           at(top_k), at(top_p), at(min_p), sc);
+        MVLA_HIP_CHECK(hipGetLastError());
+        if (top_p) {
+            hipLaunchKernelGGL((sample_window_kernel<T>), grid, dim3(SLICE_THREADS), 0, st, x, stride, V, at(temperature),
+                               at(top_k), at(top_p), at(min_p), sc);
+            MVLA_HIP_CHECK(hipGetLastError());
+        }
+        if (int rc = choose_rows<T, true>(x, stride, n, V, at(temperature), at(top_k), at(top_p), at(min_p), at(u), at(token),
+                                          at(prob), sc, st))
+            return rc;
+    }
+    return MVLA_OK;
+}
+
+}  // namespace
 
 int launch_sample(const void* logits, bool half, int64_t row_stride, int B, int V, const float* temperature,
                   const int32_t* top_k, const float* top_p, const float* min_p, const float* u, int32_t* token, float* prob,
-                  hipStream_t st) {
-    if (half)
-        hipLaunchKernelGGL((sample_kernel<bf16_t>), dim3(B), dim3(SAMPLE_THREADS), 0, st,
-                           static_cast<const bf16_t*>(logits), row_stride, V, temperature, top_k, top_p, min_p, u, token, prob);
-    else
-        hipLaunchKernelGGL((sample_kernel<float>), dim3(B), dim3(SAMPLE_THREADS), 0, st, static_cast<const float*>(logits),
-                           row_stride, V, temperature, top_k, top_p, min_p, u, token, prob);
-    MVLA_HIP_CHECK(hipGetLastError());
-    return MVLA_OK;
+                  char* scratch, size_t scratch_bytes, hipStream_t st) {
+    return half ? sample_rows(static_cast<const bf16_t*>(logits), row_stride, B, V, temperature, top_k, top_p, min_p, u, token,
+                              prob, scratch, scratch_bytes, st)
+                : sample_rows(static_cast<const float*>(logits), row_stride, B, V, temperature, top_k, top_p, min_p, u, token,
+                              prob, scratch, scratch_bytes, st);
 }
 
 }  // namespace mvla
