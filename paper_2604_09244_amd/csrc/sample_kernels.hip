@@ -32,7 +32,7 @@ typedef unsigned long long u64;    // (as atomics take it)
 constexpr int SAMPLE_THREADS = 1024, SAMPLE_WAVES = SAMPLE_THREADS / 64;
 constexpr int SAMPLE_BINS = 1024;         // of octaves below the largest weight, and at most so many tiles
 constexpr int SAMPLE_LIST = 14336;        // tokens on the list: 112 of the 160 KiB of LDS
-constexpr int SLICE_THREADS = 256;
+constexpr int SLICE_THREADS = 256, SLICE_MAXIMA = 128;
 constexpr float SAMPLE_OCTAVES = 40.f;    // weights below 2^-40 of the largest count as none
 constexpr float LOWEST = -3.4028235e38f;  // (-inf never stays)
 
@@ -188,7 +188,7 @@ struct RowState {
 };
 struct SampleScratch {
     RowState* state;              // [rows]
-    float* maxima;                // [rows][slices * SLICE_THREADS]
+    float* maxima;                // [rows][slices * SLICE_MAXIMA]
     u64* tally;                   // [rows][SAMPLE_BINS]
     u64* tile_sum;                // [rows][SAMPLE_BINS]
     u64* total;                   // [rows][slices]
@@ -221,23 +221,41 @@ __device__ __forceinline__ void append_places(const float (&x)[VEC], const bool 
 }
 
 // ---- launches on slices of a row --------------------------------------------------------------------------------------
-// calls f(tile, values, piece, whether the piece exists) for the wave's pieces of a slice; done(tile) behind each tile
+// calls f(values, piece) for a wave's 64 pieces at a time of the tiles t0, t0 + stride, .. below t1 (no numbers where a piece
+// does not exist), done(tile) behind each tile; four loads on their way at a time
+template <typename T, typename F, typename G>
+__device__ __forceinline__ void walk_tiles(const Row<T>& row, int t0, int t1, int stride, F f, G done) {
+    constexpr int VEC = Row<T>::VEC, AHEAD = 4;
+    const int lane = threadIdx.x & 63;
+    int t = t0, q = 0;                       // the next to load
+    int t_done = t0, q_done = 0;             // the next to hand on
+    while (t_done < t1) {
+        float x[AHEAD][VEC];
+        int piece[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            piece[i] = t < t1 ? (t * row.steps + q) * 64 + lane : row.pieces;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) x[i][e] = NAN;
+            if (piece[i] < row.pieces) row.load(piece[i], x[i]);
+            if (++q == row.steps) q = 0, t += stride;
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            if (t_done >= t1) break;
+            f(x[i], piece[i]);
+            if (++q_done == row.steps) {
+                done(t_done);
+                q_done = 0, t_done += stride;
+            }
+        }
+    }
+}
+// the same for a slice's waves
 template <typename T, typename F, typename G>
 __device__ __forceinline__ void slice_tiles(const Row<T>& row, int slice, int slices, F f, G done) {
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int per = (row.tiles + slices - 1) / slices, t1 = min((slice + 1) * per, row.tiles);
-    for (int t = slice * per + wave; t < t1; t += SLICE_THREADS / 64) {
-        for (int q = 0; q < row.steps; ++q) {
-            const int j = (t * row.steps + q) * 64 + lane;
-            float x[Row<T>::VEC];
-            const bool there = j < row.pieces;
-#pragma unroll
-            for (int e = 0; e < Row<T>::VEC; ++e) x[e] = NAN;
-            if (there) row.load(j, x);
-            f(t, x, j, there);
-        }
-        done(t);
-    }
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), per = (row.tiles + slices - 1) / slices;
+    walk_tiles<T>(row, slice * per + wave, min((slice + 1) * per, row.tiles), SLICE_THREADS / 64, f, done);
 }
 
 template <typename T>
@@ -272,7 +290,8 @@ __global__ __launch_bounds__(SLICE_THREADS) void sample_max_kernel(const T* __re
 #pragma unroll
         for (int e = 0; e < VEC; ++e) m = fmaxf(m, x[e]);
     }
-    sc.maxima[((size_t)b * sc.slices + slice) * SLICE_THREADS + tid] = m;
+    m = fmaxf(m, __shfl_xor(m, 1));
+    if ((tid & 1) == 0) sc.maxima[((size_t)b * sc.slices + slice) * SLICE_MAXIMA + (tid >> 1)] = m;
 }
 
 // The second look at a row: the list, the tiles' sums, or the bins' tallies, as its settings ask.
@@ -291,7 +310,7 @@ __global__ __launch_bounds__(SLICE_THREADS) void sample_collect_kernel(const T* 
     const int slice = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     Row<T> row(logits + b * stride, V);
     Settings s(b, V, temperature, top_k, top_p, min_p);
-    const int n_max = sc.slices * SLICE_THREADS;
+    const int n_max = sc.slices * SLICE_MAXIMA;
     const float* maxima = sc.maxima + (size_t)b * n_max;
     float most = -INFINITY;
     for (int i = tid; i < n_max; i += SLICE_THREADS) most = fmaxf(most, maxima[i]);
@@ -305,7 +324,7 @@ __global__ __launch_bounds__(SLICE_THREADS) void sample_collect_kernel(const T* 
     if (most == -INFINITY) return;
     auto nothing = [](int) {};
     if (s.greedy()) {
-        slice_tiles<T>(row, slice, sc.slices, [&](int, float (&x)[VEC], int j, bool) {
+        slice_tiles<T>(row, slice, sc.slices, [&](float (&x)[VEC], int j) {
             uint32_t at = 0xffffffffu;
 #pragma unroll
             for (int e = VEC - 1; e >= 0; --e)
@@ -363,7 +382,7 @@ __global__ __launch_bounds__(SLICE_THREADS) void sample_collect_kernel(const T* 
         uint32_t* n = &sc.state[b].n_list;
         u64* places = sc.list + (size_t)b * SAMPLE_LIST;
         u64 total = 0, tile = 0;
-        slice_tiles<T>(row, slice, sc.slices, [&](int, float (&x)[VEC], int j, bool) {
+        slice_tiles<T>(row, slice, sc.slices, [&](float (&x)[VEC], int j) {
             if (list) {
                 bool in[VEC];
 #pragma unroll
@@ -396,7 +415,7 @@ __global__ __launch_bounds__(SLICE_THREADS) void sample_collect_kernel(const T* 
         return;
     }
     // top_p alone
-    slice_tiles<T>(row, slice, sc.slices, [&](int, float (&x)[VEC], int, bool) {
+    slice_tiles<T>(row, slice, sc.slices, [&](float (&x)[VEC], int) {
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
             const float oct = s.octaves(x[e]);
@@ -456,7 +475,7 @@ __global__ __launch_bounds__(SLICE_THREADS) void sample_window_kernel(const T* _
         sc.state[b].window1 = last;
     }
     u64 all = 0, tile = 0;
-    slice_tiles<T>(row, slice, sc.slices, [&](int, float (&x)[VEC], int j, bool) {
+    slice_tiles<T>(row, slice, sc.slices, [&](float (&x)[VEC], int j) {
         float sure = 0.f, any = 0.f;
         bool in[VEC];
 #pragma unroll
@@ -531,19 +550,8 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(const T* __restr
             f(j, x);
         }
     };
-    // calls f(piece, values) for the wave's tiles (a lane without a piece gets no numbers), done(tile) behind each
     auto each_tile = [&](auto f, auto done) __attribute__((always_inline)) {
-        for (int t = wave; t < row.tiles; t += SAMPLE_WAVES) {
-            for (int q = 0; q < row.steps; ++q) {
-                const int j = (t * row.steps + q) * 64 + lane;
-                float x[VEC];
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) x[e] = NAN;
-                if (j < row.pieces) row.load(j, x);
-                f(j, x);
-            }
-            done(t);
-        }
+        walk_tiles<T>(row, wave, row.tiles, SAMPLE_WAVES, f, done);
     };
     // sum of one number a wave over the workgroup
     auto all_waves = [&](u64 x) {
@@ -687,7 +695,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(const T* __restr
     };
 
     // ---- what can stay, as a list
-    const bool can = by_k ? SPLIT ? s.k <= sc.slices * SLICE_THREADS : s.k <= SAMPLE_THREADS
+    const bool can = by_k ? SPLIT ? s.k <= sc.slices * SLICE_MAXIMA : s.k <= SAMPLE_THREADS
                           : by_least || (!SPLIT && by_p && V <= SAMPLE_LIST);
     if (can) {
         u64 total = 0;
@@ -916,7 +924,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(const T* __restr
                 if (tid == 0) n_list = 0;
                 __syncthreads();
                 u64 tile = 0;
-                each_tile([&](int j, float (&x)[VEC]) __attribute__((always_inline)) {
+                each_tile([&](float (&x)[VEC], int j) __attribute__((always_inline)) {
                     float sure = 0.f, any = 0.f;
                     const int left = border_i - row.first(j);
                     bool in[VEC];
@@ -977,7 +985,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(const T* __restr
             tile_sum[tid] = tid < row.tiles ? sc.tile_sum[(size_t)b * SAMPLE_BINS + tid] : 0;
         } else {
             u64 tile = 0;
-            each_tile([&](int j, float (&x)[VEC]) __attribute__((always_inline)) {
+            each_tile([&](float (&x)[VEC], int j) __attribute__((always_inline)) {
                 const int left = border_i - row.first(j);
                 float sum = 0.f;
 #pragma unroll
@@ -1051,7 +1059,7 @@ size_t sample_scratch(char* base, int rows, int slices, SampleScratch* sc) {
     };
     SampleScratch s{};
     s.state = reinterpret_cast<RowState*>(take(sizeof(RowState)));
-    s.maxima = reinterpret_cast<float*>(take((size_t)slices * SLICE_THREADS * 4));
+    s.maxima = reinterpret_cast<float*>(take((size_t)slices * SLICE_MAXIMA * 4));
     s.tally = reinterpret_cast<u64*>(take(SAMPLE_BINS * 8));
     s.tile_sum = reinterpret_cast<u64*>(take(SAMPLE_BINS * 8));
     s.total = reinterpret_cast<u64*>(take((size_t)slices * 8));
