@@ -56,7 +56,8 @@ __device__ __forceinline__ uint32_t column_or(uint32_t x) {
 //   V: lane c of a group takes dims c CH .. c CH + CH - 1 of the group's eight slots; the codes become pairs of dims of
 //      one slot, two permutes turn two slots' pairs into pairs of slots of one dim
 //   O^T: tile d holds dims c CH + d, so a lane ends with CH consecutive dims per register index: whole 16-byte stores
-constexpr int FEW_WAVES = 4, FEW_STEP = 32;
+// Bound by memory: 2 (dh / 2 + dh / 32) bytes a slot; three steps of codes are on their way per wave.
+constexpr int FEW_STEP = 32, FEW_ROWS = 16;
 
 template <int DH>
 struct FewRaw {
@@ -100,21 +101,25 @@ __device__ __forceinline__ void few_load(FewRaw<DH>& x, const uint8_t* k, const 
     }
 }
 
-template <int DH>
-__global__ __launch_bounds__(FEW_WAVES * 64) void few_rows_kernel(CacheView cache, CacheAttention a, int group, int splits,
-                                                                  float* __restrict__ part_o, float2* __restrict__ part_ml,
-                                                                  float* __restrict__ logits, int logit_pitch) {
+// WHOLE: the workgroup has all of its sample's slots; it keeps the logits in LDS and finishes outputs and weights itself.
+// Otherwise it leaves its part (maximum, sum, O) and the raw logits for join_kernel.
+template <int DH, int WAVES, bool WHOLE>
+__global__ __launch_bounds__(WAVES * 64) void few_rows_kernel(CacheView cache, CacheAttention a, int group, int splits,
+                                                              float* __restrict__ part_o, float2* __restrict__ part_ml,
+                                                              float* __restrict__ logits, int logit_pitch) {
     constexpr int NB = DH / 32, CH = DH / 16, STEPS = DH / 32;
-    __shared__ alignas(16) float sh_o[FEW_WAVES][16 * DH];
-    __shared__ float sh_m[FEW_WAVES][16], sh_l[FEW_WAVES][16];
+    extern __shared__ float4 parts[];         // [WAVES][rows * DH / 4] parts of O, then (WHOLE) [rows][logit_pitch] logits
+    __shared__ float sh_m[WAVES][FEW_ROWS], sh_l[WAVES][FEW_ROWS];
+    __shared__ float2 sh_row[FEW_ROWS];
 
-    const int split = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
+    const int split = WHOLE ? 0 : blockIdx.x % splits, h = WHOLE ? blockIdx.x : blockIdx.x / splits, b = blockIdx.y;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 15, g = lane >> 4;
     const Span span = sample_span(a, cache.capacity, b);
     const int rows = a.n_q * group;
     const int n_steps = (span.len + FEW_STEP - 1) / FEW_STEP;
-    const int step0 = (int)((int64_t)n_steps * split / splits), step1 = (int)((int64_t)n_steps * (split + 1) / splits);
+    const int step0 = WHOLE ? 0 : (int)((int64_t)n_steps * split / splits);
+    const int step1 = WHOLE ? n_steps : (int)((int64_t)n_steps * (split + 1) / splits);
 
     const size_t head = (size_t)b * cache.H_kv + h;
     const uint8_t* k = cache.k + head * cache.capacity * (DH / 2);
@@ -122,8 +127,12 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void few_rows_kernel(CacheView cach
     const uint8_t* ks = cache.k_scale + head * cache.capacity * NB;
     const uint8_t* vs = cache.v_scale + head * cache.capacity * NB;
 
-    FewRaw<DH> next;
-    if (step0 + wave < step1) few_load<DH>(next, k, ks, v, vs, (step0 + wave) * FEW_STEP, c, g);
+    FewRaw<DH> raw[3];
+    auto load = [&](FewRaw<DH>& x, int step) __attribute__((always_inline)) {
+        if (step < step1) few_load<DH>(x, k, ks, v, vs, step * FEW_STEP, c, g);
+    };
+#pragma unroll
+    for (int i = 0; i < 3; ++i) load(raw[i], step0 + wave + i * WAVES);
 
     // this lane's column: row c (columns beyond the rows hold zeros and see everything; nobody reads them)
     const int qi = c / group;
@@ -141,7 +150,10 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void few_rows_kernel(CacheView cach
     }
     const float scale_log2e = a.scale * 1.4426950408889634f;
     const int k_blk = DH == 128 ? g : g >> 1, v_blk = DH == 128 ? c >> 2 : c >> 3;
-    float* row_logits = logits ? logits + (head * rows + c) * (size_t)logit_pitch : nullptr;
+    float* sh_o = reinterpret_cast<float*>(parts);
+    float* sh_x = sh_o + WAVES * rows * DH;   // (WHOLE)
+    const bool keep = WHOLE ? a.accumulate != 0 : logits != nullptr;
+    float* row_logits = WHOLE ? sh_x + c * logit_pitch : keep ? logits + (head * rows + c) * (size_t)logit_pitch : nullptr;
 
     f32x4_t o[CH];
 #pragma unroll
@@ -149,9 +161,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void few_rows_kernel(CacheView cach
     float run_m = -INFINITY, run_l = 0.f;     // run_l: this lane's share
     uint32_t not_a_number = 0;                // blocks of a value row that this lane's row sees and that hold none
 
-    for (int step = step0 + wave; step < step1; step += FEW_WAVES) {
-        FewRaw<DH> x = next;
-        if (step + FEW_WAVES < step1) few_load<DH>(next, k, ks, v, vs, (step + FEW_WAVES) * FEW_STEP, c, g);
+    auto take = [&](FewRaw<DH>& x, int step) __attribute__((always_inline)) {
         const int slot0 = step * FEW_STEP;
         // ---- S^T
         f32x4_t s[2];
@@ -163,7 +173,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void few_rows_kernel(CacheView cach
             for (int st = 0; st < STEPS; ++st) s[j] = mfma16(fp4_values(x.k[j][st], scale), qf[st], s[j]);
         }
         const int my0 = slot0 + 8 * g;        // slot of s[0][0]
-        if (row_logits && real) {             // (raw: scaled where they are read)
+        if (keep && real) {                   // (raw: scaled where they are read)
             *reinterpret_cast<float4*>(row_logits + my0) = make_float4(s[0][0], s[0][1], s[0][2], s[0][3]);
             *reinterpret_cast<float4*>(row_logits + my0 + 4) = make_float4(s[1][0], s[1][1], s[1][2], s[1][3]);
         }
@@ -243,6 +253,14 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void few_rows_kernel(CacheView cach
             pairs(std::integral_constant<int, 2>{});
             pairs(std::integral_constant<int, 3>{});
         }
+    };
+    for (int step = step0 + wave; step < step1; step += 3 * WAVES) {
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+            if (step + i * WAVES < step1) {
+                take(raw[i], step + i * WAVES);
+                load(raw[i], step + (i + 3) * WAVES);
+            }
     }
 
     // ---- the waves' parts of a row, joined
@@ -260,86 +278,144 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void few_rows_kernel(CacheView cach
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int q = 0; q < CH / 4; ++q)
-                *reinterpret_cast<float4*>(&sh_o[wave][c * DH + (4 * g + i) * CH + 4 * q]) =
+                *reinterpret_cast<float4*>(&sh_o[(wave * rows + c) * DH + (4 * g + i) * CH + 4 * q]) =
                     make_float4(o[4 * q][i], o[4 * q + 1][i], o[4 * q + 2][i], o[4 * q + 3][i]);
     __syncthreads();
-    for (int id = tid; id < rows * DH; id += FEW_WAVES * 64) {
-        const int r = id / DH;
-        float m = sh_m[0][r], l = 0.f, acc = 0.f;
+    // a row's maximum and sum over the waves
+    auto joined = [&](int r, float (&f)[WAVES]) __attribute__((always_inline)) {
+        float m = sh_m[0][r], l = 0.f;
 #pragma unroll
-        for (int w = 1; w < FEW_WAVES; ++w) m = fmaxf(m, sh_m[w][r]);
+        for (int w = 1; w < WAVES; ++w) m = fmaxf(m, sh_m[w][r]);
 #pragma unroll
-        for (int w = 0; w < FEW_WAVES; ++w) {
-            const float f = sh_m[w][r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((sh_m[w][r] - m) * scale_log2e);
-            l = fmaf(sh_l[w][r], f, l);
-            acc = fmaf(sh_o[w][id], sh_m[w][r] == -INFINITY ? 1.f : f, acc);
+        for (int w = 0; w < WAVES; ++w) {
+            f[w] = sh_m[w][r] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((sh_m[w][r] - m) * scale_log2e);
+            l = fmaf(sh_l[w][r], f[w], l);
         }
-        const size_t row = ((size_t)split * cache.B * cache.H_kv + head) * rows + r;
-        part_o[row * DH + id % DH] = acc;
-        if (id % DH == 0) part_ml[row] = make_float2(m, l);
+        return make_float2(m, l);
+    };
+    for (int id = tid; id < rows * (DH / 4); id += WAVES * 64) {
+        const int r = id / (DH / 4), ch = id % (DH / 4) * 4;
+        float f[WAVES];
+        const float2 ml = joined(r, f);
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            const float4 t = parts[(w * rows + r) * (DH / 4) + ch / 4];
+            acc.x = fmaf(t.x, f[w], acc.x), acc.y = fmaf(t.y, f[w], acc.y);
+            acc.z = fmaf(t.z, f[w], acc.z), acc.w = fmaf(t.w, f[w], acc.w);
+        }
+        if constexpr (WHOLE) {
+            const int i = r / group;
+            uint2 w = make_uint2(pack_bf16x2(acc.x / ml.y, acc.y / ml.y), pack_bf16x2(acc.z / ml.y, acc.w / ml.y));
+            if (seen_by(span, i) == 0) w = make_uint2(0u, 0u);   // (one whose logits are all -inf is 0 / 0)
+            *reinterpret_cast<uint2*>(const_cast<bf16_t*>(a.out.p) + b * a.out.sample + i * a.out.token +
+                                      (h * group + r % group) * a.out.head + ch) = w;
+        } else {
+            const size_t row = ((size_t)split * cache.B * cache.H_kv + head) * rows + r;
+            *reinterpret_cast<float4*>(part_o + row * DH + ch) = acc;
+            if (ch == 0) part_ml[row] = ml;
+        }
+    }
+    if constexpr (WHOLE) {
+        if (!keep) return;
+        if (tid < rows) {
+            float f[WAVES];
+            const float2 ml = joined(tid, f);
+            sh_row[tid] = make_float2(-ml.x * scale_log2e, 1.f / ml.y);
+        }
+        __syncthreads();
+        float* weight = cache.weight + head * cache.capacity;
+        for (int slot = tid * 4; slot < span.len; slot += WAVES * 256) {
+            float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int r = 0; r < rows; ++r) {
+                const float neg_m = sh_row[r].x, inv = sh_row[r].y;
+                const int sees = seen_by(span, r / group);
+                const float4 x = *reinterpret_cast<const float4*>(sh_x + r * logit_pitch + slot);
+                if (slot < sees) sum.x += __builtin_amdgcn_exp2f(fmaf(x.x, scale_log2e, neg_m)) * inv;
+                if (slot + 1 < sees) sum.y += __builtin_amdgcn_exp2f(fmaf(x.y, scale_log2e, neg_m)) * inv;
+                if (slot + 2 < sees) sum.z += __builtin_amdgcn_exp2f(fmaf(x.z, scale_log2e, neg_m)) * inv;
+                if (slot + 3 < sees) sum.w += __builtin_amdgcn_exp2f(fmaf(x.w, scale_log2e, neg_m)) * inv;
+            }
+            weight[slot] += sum.x;
+            if (slot + 1 < span.len) weight[slot + 1] += sum.y;
+            if (slot + 2 < span.len) weight[slot + 2] += sum.z;
+            if (slot + 3 < span.len) weight[slot + 3] += sum.w;
+        }
     }
 }
 
 // ---- the parts of all splits of a row, and the weights ------------------------------------------------------------
-// Workgroup (x, key head, sample): the first x write the rows' outputs, 256 values each; all add the weights of 1024
+// Workgroup (x, key head, sample): the workgroups of a head share out its rows' outputs; each adds the weights of 1024
 // slots to the rows' own, from the logits that the pass over the cache left behind.
-constexpr int JOIN_THREADS = 256, JOIN_SLOTS = 1024;
+constexpr int JOIN_THREADS = 256, JOIN_SLOTS = 1024, JOIN_ROWS = 16, MAX_SPLITS = 64;
 
 __global__ __launch_bounds__(JOIN_THREADS) void join_kernel(CacheView cache, CacheAttention a, int group, int splits,
                                                             const float* __restrict__ part_o, const float2* __restrict__ part_ml,
                                                             const float* __restrict__ logits, int logit_pitch,
                                                             float2* __restrict__ row_ml) {
-    const int h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, DH = cache.dh;
+    __shared__ float factor[JOIN_ROWS][MAX_SPLITS];
+    __shared__ float2 row[JOIN_ROWS];
+    const int h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, QUADS = cache.dh / 4;
     const Span span = sample_span(a, cache.capacity, b);
     const int rows = a.n_q * group;
     const size_t head = (size_t)b * cache.H_kv + h, pitch = (size_t)cache.B * cache.H_kv * rows;
     const float scale_log2e = a.scale * 1.4426950408889634f;
-    const float2* ml = part_ml + head * rows;
-    auto joined = [&](int r) {
-        float m = -INFINITY, l = 0.f;
-        for (int s = 0; s < splits; ++s) m = fmaxf(m, ml[s * pitch + r].x);
-        for (int s = 0; s < splits; ++s) {
-            const float2 t = ml[s * pitch + r];
-            if (t.x != -INFINITY) l = fmaf(t.y, __builtin_amdgcn_exp2f((t.x - m) * scale_log2e), l);
-            else l += t.y;
+    // (rows in runs of 16: with logits there is one run, without a workgroup takes every gridDim.x-th)
+    const int runs = (rows + JOIN_ROWS - 1) / JOIN_ROWS;
+    for (int run = logits ? 0 : blockIdx.x; run < runs; run += logits ? 1 : gridDim.x) {
+        const int r0 = run * JOIN_ROWS, n = min(JOIN_ROWS, rows - r0);
+        __syncthreads();
+        for (int r = wave; r < n; r += JOIN_THREADS / 64) {      // lane: split
+            const float2 ml = lane < splits ? part_ml[lane * pitch + head * rows + r0 + r] : make_float2(-INFINITY, 0.f);
+            float m = ml.x;
+#pragma unroll
+            for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+            const float f = ml.x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((ml.x - m) * scale_log2e);
+            const float l = wave_sum_f32(ml.y * f);
+            factor[r][lane] = f;
+            if (lane == 0) row[r] = make_float2(m, l);
         }
-        return make_float2(m, l);
-    };
-    for (int id = blockIdx.x * JOIN_THREADS + tid; id < rows * DH; id += gridDim.x * JOIN_THREADS) {
-        const int r = id / DH, ch = id % DH, i = r / group;
-        const float2 t = joined(r);
-        float acc = 0.f;
-        for (int s = 0; s < splits; ++s) {
-            const float m = ml[s * pitch + r].x;
-            acc = fmaf(part_o[(s * pitch + head * rows + r) * DH + ch],
-                       m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - t.x) * scale_log2e), acc);
+        __syncthreads();
+        const int first = logits ? blockIdx.x * JOIN_THREADS : 0, stride = logits ? gridDim.x * JOIN_THREADS : JOIN_THREADS;
+        for (int id = first + tid; id < n * QUADS; id += stride) {
+            const int r = id / QUADS, ch = id % QUADS * 4, i = (r0 + r) / group;
+            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+            const float* p = part_o + (head * rows + r0 + r) * cache.dh + ch;
+#pragma unroll 4
+            for (int s = 0; s < splits; ++s) {
+                const float4 t = *reinterpret_cast<const float4*>(p + s * pitch * cache.dh);
+                const float f = factor[r][s];
+                acc.x = fmaf(t.x, f, acc.x), acc.y = fmaf(t.y, f, acc.y), acc.z = fmaf(t.z, f, acc.z), acc.w = fmaf(t.w, f, acc.w);
+            }
+            const float l = row[r].y;
+            uint2 w = make_uint2(pack_bf16x2(acc.x / l, acc.y / l), pack_bf16x2(acc.z / l, acc.w / l));
+            if (seen_by(span, i) == 0) w = make_uint2(0u, 0u);   // (one whose logits are all -inf is 0 / 0)
+            *reinterpret_cast<uint2*>(const_cast<bf16_t*>(a.out.p) + b * a.out.sample + i * a.out.token +
+                                      (h * group + (r0 + r) % group) * a.out.head + ch) = w;
+            if (row_ml && ch == 0) row_ml[head * rows + r0 + r] = row[r];
         }
-        // (a row that sees nothing is zero; one whose logits are all -inf is 0 / 0)
-        const bf16_t o = seen_by(span, i) > 0 ? f32_to_bf16(acc / t.y) : (bf16_t)0;
-        const_cast<bf16_t*>(a.out.p)[b * a.out.sample + i * a.out.token + (h * group + r % group) * a.out.head + ch] = o;
-        if (row_ml && ch == 0) row_ml[head * rows + r] = t;
     }
-    if (!logits) return;
-    float sum[JOIN_SLOTS / JOIN_THREADS] = {};
-    const int slot0 = blockIdx.x * JOIN_SLOTS + tid;
-    if (blockIdx.x * JOIN_SLOTS >= span.len) return;
+    const int slot = blockIdx.x * JOIN_SLOTS + tid * 4;
+    if (!logits || slot >= span.len) return;
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
     for (int r = 0; r < rows; ++r) {
-        const int limit = seen_by(span, r / group);
-        const float2 t = joined(r);
-        const float inv = 1.f / t.y, neg_m = -t.x * scale_log2e;
-        const float* x = logits + (head * rows + r) * (size_t)logit_pitch;
-#pragma unroll
-        for (int j = 0; j < JOIN_SLOTS / JOIN_THREADS; ++j) {
-            const int slot = slot0 + j * JOIN_THREADS;
-            if (slot < limit) sum[j] += __builtin_amdgcn_exp2f(fmaf(x[slot], scale_log2e, neg_m)) * inv;
-        }
+        const int sees = seen_by(span, r / group);
+        const float inv = 1.f / row[r].y, neg_m = -row[r].x * scale_log2e;
+        const float4 x = *reinterpret_cast<const float4*>(logits + (head * rows + r) * (size_t)logit_pitch + slot);
+        if (slot < sees) sum.x += __builtin_amdgcn_exp2f(fmaf(x.x, scale_log2e, neg_m)) * inv;
+        if (slot + 1 < sees) sum.y += __builtin_amdgcn_exp2f(fmaf(x.y, scale_log2e, neg_m)) * inv;
+        if (slot + 2 < sees) sum.z += __builtin_amdgcn_exp2f(fmaf(x.z, scale_log2e, neg_m)) * inv;
+        if (slot + 3 < sees) sum.w += __builtin_amdgcn_exp2f(fmaf(x.w, scale_log2e, neg_m)) * inv;
     }
-    float* w = cache.weight + head * cache.capacity;
-#pragma unroll
-    for (int j = 0; j < JOIN_SLOTS / JOIN_THREADS; ++j) {
-        const int slot = slot0 + j * JOIN_THREADS;
-        if (slot < span.len) w[slot] += sum[j];
-    }
+    // (beyond the length a weight stays what it is, whatever that is)
+    float4* w = reinterpret_cast<float4*>(cache.weight + head * cache.capacity + slot);
+    float4 old = *w;
+    old.x += sum.x;
+    if (slot + 1 < span.len) old.y += sum.y;
+    if (slot + 2 < span.len) old.z += sum.z;
+    if (slot + 3 < span.len) old.w += sum.w;
+    *w = old;
 }
 
 // ---- many rows -----------------------------------------------------------------------------------------------------
@@ -666,32 +742,68 @@ namespace {
 
 struct AttentionPlan {
     bool many;
-    int group, rows, splits, pitch;
+    int group, rows, splits, waves, pitch;    // waves: of few_rows_kernel; splits 0: whole samples, no second launch
     size_t o_bytes, ml_bytes, row_bytes, logit_bytes;
     size_t bytes() const { return o_bytes + ml_bytes + row_bytes + logit_bytes; }
 };
+
+// bytes of LDS of few_rows_kernel
+size_t few_lds(int dh, int waves, int rows, int logits) { return ((size_t)waves * rows * dh + (size_t)rows * logits) * 4; }
 
 AttentionPlan attention_plan(int B, int H, int H_kv, int dh, int n_q, int max_len, bool accumulate) {
     AttentionPlan p{};
     p.group = H / H_kv;
     p.rows = n_q * p.group;
-    p.many = p.rows > 16;
-    const int tile = p.many ? MANY_KT : FEW_STEP * FEW_WAVES;
-    const int64_t tiles = ((int64_t)max_len + tile - 1) / tile;
-    const int64_t wgs = (int64_t)B * H_kv * (p.many ? (p.rows + MANY_ROWS - 1) / MANY_ROWS : 1);
-    const int64_t want = 4 * (int64_t)device_cu_count();
-    int64_t s = p.many ? (2 * (int64_t)device_cu_count() + wgs - 1) / wgs : (want + wgs - 1) / wgs;
-    const int64_t most = p.many ? (tiles + 3) / 4 : tiles;   // (few tiles each are not worth a part of their own)
-    if (s > most) s = most;
-    if (s > 64) s = 64;
-    p.splits = s < 1 ? 1 : (int)s;
+    p.many = p.rows > FEW_ROWS;
     p.pitch = (max_len + FEW_STEP - 1) / FEW_STEP * FEW_STEP;
-    const size_t all = (size_t)B * H_kv * p.rows;
-    p.o_bytes = p.many && p.splits == 1 ? 0 : align_up(all * p.splits * dh * 4, 256);
+    const int cus = device_cu_count();
+    const int64_t heads = (int64_t)B * H_kv, steps = p.pitch / FEW_STEP;
+    if (!p.many) {
+        // Whole samples a workgroup where that fills the chip, or where there is little to split; eight waves where a
+        // launch leaves compute units idle.
+        p.waves = heads <= cus ? 8 : 4;
+        const size_t lds = few_lds(dh, p.waves, p.rows, accumulate ? p.pitch : 0);
+        const bool whole = lds <= 72 * 1024 && (heads >= cus + cus / 2 || steps <= 4 * p.waves);
+        if (!whole) {
+            p.waves = 4;
+            const int64_t tiles = (steps + 3) / 4, want = (4 * (int64_t)cus + heads - 1) / heads;
+            p.splits = (int)(want > tiles ? tiles : want);
+        }
+    } else {
+        const int64_t wgs = heads * ((p.rows + MANY_ROWS - 1) / MANY_ROWS), tiles = ((int64_t)max_len + MANY_KT - 1) / MANY_KT;
+        const int64_t want = (2 * (int64_t)cus + wgs - 1) / wgs, most = (tiles + 3) / 4;   // (few tiles are not worth a part)
+        p.splits = (int)(want > most ? most : want);
+    }
+    if (p.splits > MAX_SPLITS) p.splits = MAX_SPLITS;
+    const size_t all = (size_t)heads * p.rows;
+    p.o_bytes = p.splits < (p.many ? 2 : 1) ? 0 : align_up(all * p.splits * dh * 4, 256);
     p.ml_bytes = align_up(all * p.splits * 8, 256);
-    p.row_bytes = align_up(all * 8, 256);
-    p.logit_bytes = accumulate && !p.many ? align_up(all * p.pitch * 4, 256) : 0;
+    p.row_bytes = p.many ? align_up(all * 8, 256) : 0;
+    p.logit_bytes = accumulate && !p.many && p.splits ? align_up(all * p.pitch * 4, 256) : 0;
     return p;
+}
+
+// raises a kernel's dynamic-LDS limit once per device
+int allow_lds(const void* kernel, bool* set, size_t lds) {
+    int dev = 0;
+    MVLA_HIP_CHECK(hipGetDevice(&dev));
+    if (dev < 0 || dev >= kMaxDevices || !set[dev]) {
+        MVLA_HIP_CHECK(hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+        if (dev >= 0 && dev < kMaxDevices) set[dev] = true;
+    }
+    return MVLA_OK;
+}
+
+template <int DH, int WAVES, bool WHOLE>
+int launch_few(const CacheView& c, const CacheAttention& a, const AttentionPlan& p, float* o, float2* ml, float* logits,
+               hipStream_t st) {
+    static bool lds_set[kMaxDevices] = {};
+    if (int rc = allow_lds(reinterpret_cast<const void*>(&few_rows_kernel<DH, WAVES, WHOLE>), lds_set, 80 * 1024)) return rc;
+    const size_t lds = few_lds(DH, WAVES, p.rows, WHOLE && a.accumulate ? p.pitch : 0);
+    hipLaunchKernelGGL((few_rows_kernel<DH, WAVES, WHOLE>), dim3(WHOLE ? c.H_kv : c.H_kv * p.splits, c.B), dim3(WAVES * 64), lds,
+                       st, c, a, p.group, p.splits, o, ml, logits, p.pitch);
+    MVLA_HIP_CHECK(hipGetLastError());
+    return MVLA_OK;
 }
 
 template <int DH>
@@ -701,33 +813,27 @@ int run_attention(const CacheView& c, const CacheAttention& a, const AttentionPl
     float2* row_ml = reinterpret_cast<float2*>(scratch + p.o_bytes + p.ml_bytes);
     float* logits = reinterpret_cast<float*>(scratch + p.o_bytes + p.ml_bytes + p.row_bytes);
     if (!p.many) {
+        if (!p.splits)
+            return p.waves == 8 ? launch_few<DH, 8, true>(c, a, p, nullptr, nullptr, nullptr, st)
+                                : launch_few<DH, 4, true>(c, a, p, nullptr, nullptr, nullptr, st);
         float* lg = a.accumulate ? logits : nullptr;
-        hipLaunchKernelGGL((few_rows_kernel<DH>), dim3(p.splits, c.H_kv, c.B), dim3(FEW_WAVES * 64), 0, st, c, a, p.group,
-                           p.splits, o, ml, lg, p.pitch);
-        MVLA_HIP_CHECK(hipGetLastError());
-        const int wide = (p.rows * DH + JOIN_THREADS - 1) / JOIN_THREADS;
+        if (int rc = launch_few<DH, 4, false>(c, a, p, o, ml, lg, st)) return rc;
         const int chunks = a.accumulate ? (a.max_len + JOIN_SLOTS - 1) / JOIN_SLOTS : 1;
-        hipLaunchKernelGGL(join_kernel, dim3(wide > chunks ? wide : chunks, c.H_kv, c.B), dim3(JOIN_THREADS), 0, st, c, a,
-                           p.group, p.splits, o, ml, lg, p.pitch, nullptr);
+        hipLaunchKernelGGL(join_kernel, dim3(chunks, c.H_kv, c.B), dim3(JOIN_THREADS), 0, st, c, a, p.group, p.splits, o, ml,
+                           lg, p.pitch, nullptr);
         MVLA_HIP_CHECK(hipGetLastError());
         return MVLA_OK;
     }
     static bool lds_set[kMaxDevices] = {};
     const size_t lds = 2 * (MANY_KT * (DH / 8) + DH * 8) * sizeof(uint4);
-    int dev = 0;   // (the dynamic-LDS limit is raised once per device)
-    MVLA_HIP_CHECK(hipGetDevice(&dev));
-    if (dev < 0 || dev >= kMaxDevices || !lds_set[dev]) {
-        MVLA_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void*>(&many_rows_kernel<DH>),
-                                           hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-        if (dev >= 0 && dev < kMaxDevices) lds_set[dev] = true;
-    }
+    if (int rc = allow_lds(reinterpret_cast<const void*>(&many_rows_kernel<DH>), lds_set, lds)) return rc;
     hipLaunchKernelGGL((many_rows_kernel<DH>), dim3(c.H_kv, (p.rows + MANY_ROWS - 1) / MANY_ROWS, c.B * p.splits),
                        dim3(MANY_THREADS), lds, st, c, a, p.group, p.splits, o, ml);
     MVLA_HIP_CHECK(hipGetLastError());
     const float2* joined = ml;
     if (p.splits > 1) {
-        hipLaunchKernelGGL(join_kernel, dim3((p.rows * DH + JOIN_THREADS - 1) / JOIN_THREADS, c.H_kv, c.B),
-                           dim3(JOIN_THREADS), 0, st, c, a, p.group, p.splits, o, ml, nullptr, 0, row_ml);
+        hipLaunchKernelGGL(join_kernel, dim3((p.rows + JOIN_ROWS - 1) / JOIN_ROWS, c.H_kv, c.B), dim3(JOIN_THREADS), 0, st,
+                           c, a, p.group, p.splits, o, ml, nullptr, 0, row_ml);
         MVLA_HIP_CHECK(hipGetLastError());
         joined = row_ml;
     }
