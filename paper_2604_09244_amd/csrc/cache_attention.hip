@@ -8,6 +8,7 @@
 #include "fp4.h"
 #include "wave.h"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace mvla {
@@ -345,8 +346,8 @@ __global__ __launch_bounds__(WAVES * 64) void few_rows_kernel(CacheView cache, C
 }
 
 // ---- the parts of all splits of a row, and the weights ------------------------------------------------------------
-// Workgroup (x, key head, sample): the workgroups of a head share out its rows' outputs; each adds the weights of 1024
-// slots to the rows' own, from the logits that the pass over the cache left behind.
+// Workgroup (x, key head, sample): the workgroups of a head share out its rows' outputs, and runs of 1024 slots whose
+// weights they add to the rows' own, from the logits that the pass over the cache left behind.
 constexpr int JOIN_THREADS = 256, JOIN_SLOTS = 1024, JOIN_ROWS = 16, MAX_SPLITS = 64;
 
 __global__ __launch_bounds__(JOIN_THREADS) void join_kernel(CacheView cache, CacheAttention a, int group, int splits,
@@ -395,27 +396,28 @@ __global__ __launch_bounds__(JOIN_THREADS) void join_kernel(CacheView cache, Cac
             if (row_ml && ch == 0) row_ml[head * rows + r0 + r] = row[r];
         }
     }
-    const int slot = blockIdx.x * JOIN_SLOTS + tid * 4;
-    if (!logits || slot >= span.len) return;
-    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (!logits) return;
+    for (int slot = (blockIdx.x * JOIN_THREADS + tid) * 4; slot < span.len; slot += gridDim.x * JOIN_SLOTS) {
+        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+        float4* w = reinterpret_cast<float4*>(cache.weight + head * cache.capacity + slot);
+        float4 old = *w;
 #pragma unroll 4
-    for (int r = 0; r < rows; ++r) {
-        const int sees = seen_by(span, r / group);
-        const float inv = 1.f / row[r].y, neg_m = -row[r].x * scale_log2e;
-        const float4 x = *reinterpret_cast<const float4*>(logits + (head * rows + r) * (size_t)logit_pitch + slot);
-        if (slot < sees) sum.x += __builtin_amdgcn_exp2f(fmaf(x.x, scale_log2e, neg_m)) * inv;
-        if (slot + 1 < sees) sum.y += __builtin_amdgcn_exp2f(fmaf(x.y, scale_log2e, neg_m)) * inv;
-        if (slot + 2 < sees) sum.z += __builtin_amdgcn_exp2f(fmaf(x.z, scale_log2e, neg_m)) * inv;
-        if (slot + 3 < sees) sum.w += __builtin_amdgcn_exp2f(fmaf(x.w, scale_log2e, neg_m)) * inv;
+        for (int r = 0; r < rows; ++r) {
+            const int sees = seen_by(span, r / group);
+            const float inv = 1.f / row[r].y, neg_m = -row[r].x * scale_log2e;
+            const float4 x = *reinterpret_cast<const float4*>(logits + (head * rows + r) * (size_t)logit_pitch + slot);
+            if (slot < sees) sum.x += __builtin_amdgcn_exp2f(fmaf(x.x, scale_log2e, neg_m)) * inv;
+            if (slot + 1 < sees) sum.y += __builtin_amdgcn_exp2f(fmaf(x.y, scale_log2e, neg_m)) * inv;
+            if (slot + 2 < sees) sum.z += __builtin_amdgcn_exp2f(fmaf(x.z, scale_log2e, neg_m)) * inv;
+            if (slot + 3 < sees) sum.w += __builtin_amdgcn_exp2f(fmaf(x.w, scale_log2e, neg_m)) * inv;
+        }
+        // (beyond the length a weight stays what it is, whatever that is)
+        old.x += sum.x;
+        if (slot + 1 < span.len) old.y += sum.y;
+        if (slot + 2 < span.len) old.z += sum.z;
+        if (slot + 3 < span.len) old.w += sum.w;
+        *w = old;
     }
-    // (beyond the length a weight stays what it is, whatever that is)
-    float4* w = reinterpret_cast<float4*>(cache.weight + head * cache.capacity + slot);
-    float4 old = *w;
-    old.x += sum.x;
-    if (slot + 1 < span.len) old.y += sum.y;
-    if (slot + 2 < span.len) old.z += sum.z;
-    if (slot + 3 < span.len) old.w += sum.w;
-    *w = old;
 }
 
 // ---- many rows -----------------------------------------------------------------------------------------------------
@@ -766,8 +768,12 @@ AttentionPlan attention_plan(int B, int H, int H_kv, int dh, int n_q, int max_le
         const bool whole = lds <= 72 * 1024 && (heads >= cus + cus / 2 || steps <= 4 * p.waves);
         if (!whole) {
             p.waves = 4;
-            const int64_t tiles = (steps + 3) / 4, want = (4 * (int64_t)cus + heads - 1) / heads;
-            p.splits = (int)(want > tiles ? tiles : want);
+            // enough workgroups to fill the chip, and where they would still be long (eight steps a wave) so many that
+            // samples of different lengths even out
+            const int64_t tiles = (steps + 3) / 4;
+            const int64_t fill = std::min(tiles, (4 * (int64_t)cus + heads - 1) / heads);
+            const int64_t even = std::min(tiles / 8, (16 * (int64_t)cus + heads - 1) / heads);
+            p.splits = (int)std::max(fill, even);
         }
     } else {
         const int64_t wgs = heads * ((p.rows + MANY_ROWS - 1) / MANY_ROWS), tiles = ((int64_t)max_len + MANY_KT - 1) / MANY_KT;
@@ -818,7 +824,9 @@ int run_attention(const CacheView& c, const CacheAttention& a, const AttentionPl
                                 : launch_few<DH, 4, true>(c, a, p, nullptr, nullptr, nullptr, st);
         float* lg = a.accumulate ? logits : nullptr;
         if (int rc = launch_few<DH, 4, false>(c, a, p, o, ml, lg, st)) return rc;
-        const int chunks = a.accumulate ? (a.max_len + JOIN_SLOTS - 1) / JOIN_SLOTS : 1;
+        // (a workgroup's start, the rows' maxima and sums, costs as much as a run: several runs where there are many)
+        const int runs = a.accumulate ? (a.max_len + JOIN_SLOTS - 1) / JOIN_SLOTS : 1;
+        const int chunks = std::max(1, std::min(runs, 8 * device_cu_count() / (c.H_kv * c.B)));
         hipLaunchKernelGGL(join_kernel, dim3(chunks, c.H_kv, c.B), dim3(JOIN_THREADS), 0, st, c, a, p.group, p.splits, o, ml,
                            lg, p.pitch, nullptr);
         MVLA_HIP_CHECK(hipGetLastError());
