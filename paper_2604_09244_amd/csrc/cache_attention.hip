@@ -66,46 +66,85 @@ struct FewRaw {
     uint32_t k[2][KW], v[8], ks[2], vs[8];
 };
 
+// A key head's rows, and where in a step of them lane (c, g) finds its own (bytes): the step's start is the wave's, the
+// lane's part the same for all steps.
 template <int DH>
-__device__ __forceinline__ void few_load(FewRaw<DH>& x, const uint8_t* k, const uint8_t* ks, const uint8_t* v,
-                                         const uint8_t* vs, int slot0, int c, int g) {
-    constexpr int NB = DH / 32;
-    const int kr = slot0 + 8 * (c >> 2) + (c & 3), vr = slot0 + 8 * g;
+struct FewRows {
+    static constexpr int NB = DH / 32;
+    const uint8_t *k, *v, *ks, *vs;
+    uint32_t k_off, v_off, ks_off, vs_off;
+    __device__ __forceinline__ FewRows(const CacheView& cache, size_t head, int c, int g) {
+        const size_t row = head * cache.capacity;
+        k = cache.k + row * (DH / 2), v = cache.v + row * (DH / 2);
+        ks = cache.k_scale + row * NB, vs = cache.v_scale + row * NB;
+        const int kr = 8 * (c >> 2) + (c & 3);
+        k_off = (uint32_t)(kr * (DH / 2) + g * (DH / 8)), ks_off = (uint32_t)(kr * NB);
+        v_off = (uint32_t)(8 * g * (DH / 2) + c * (DH / 32)), vs_off = (uint32_t)(8 * g * NB);
+    }
+    __device__ __forceinline__ void load(FewRaw<DH>& x, int slot0) const {
+        const uint8_t *kp = k + (size_t)slot0 * (DH / 2), *vp = v + (size_t)slot0 * (DH / 2);
+        const uint8_t *ksp = ks + (size_t)slot0 * NB, *vsp = vs + (size_t)slot0 * NB;
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const size_t at = (size_t)(kr + 4 * j);
+        for (int j = 0; j < 2; ++j) {
+            const uint8_t* p = kp + k_off + 4 * j * (DH / 2);
+            const uint8_t* e = ksp + ks_off + 4 * j * NB;
+            if constexpr (DH == 128) {
+                const uint4 w = *reinterpret_cast<const uint4*>(p);
+                x.k[j][0] = w.x, x.k[j][1] = w.y, x.k[j][2] = w.z, x.k[j][3] = w.w;
+                x.ks[j] = *reinterpret_cast<const uint32_t*>(e);
+            } else {
+                const uint2 w = *reinterpret_cast<const uint2*>(p);
+                x.k[j][0] = w.x, x.k[j][1] = w.y;
+                x.ks[j] = *reinterpret_cast<const uint16_t*>(e);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint8_t* p = vp + v_off + i * (DH / 2);
+            if constexpr (DH == 128) x.v[i] = *reinterpret_cast<const uint32_t*>(p);
+            else x.v[i] = *reinterpret_cast<const uint16_t*>(p);
+        }
+        const uint8_t* e = vsp + vs_off;
+        const uint4 a = *reinterpret_cast<const uint4*>(e);
         if constexpr (DH == 128) {
-            const uint4 w = *reinterpret_cast<const uint4*>(k + at * (DH / 2) + g * 16);
-            x.k[j][0] = w.x, x.k[j][1] = w.y, x.k[j][2] = w.z, x.k[j][3] = w.w;
-            x.ks[j] = *reinterpret_cast<const uint32_t*>(ks + at * NB);
+            const uint4 b = *reinterpret_cast<const uint4*>(e + 16);
+            x.vs[0] = a.x, x.vs[1] = a.y, x.vs[2] = a.z, x.vs[3] = a.w;
+            x.vs[4] = b.x, x.vs[5] = b.y, x.vs[6] = b.z, x.vs[7] = b.w;
         } else {
-            const uint2 w = *reinterpret_cast<const uint2*>(k + at * (DH / 2) + g * 8);
-            x.k[j][0] = w.x, x.k[j][1] = w.y;
-            x.ks[j] = *reinterpret_cast<const uint16_t*>(ks + at * NB);
+            x.vs[0] = a.x & 0xffffu, x.vs[1] = a.x >> 16, x.vs[2] = a.y & 0xffffu, x.vs[3] = a.y >> 16;
+            x.vs[4] = a.z & 0xffffu, x.vs[5] = a.z >> 16, x.vs[6] = a.w & 0xffffu, x.vs[7] = a.w >> 16;
         }
     }
+};
+
+// whether one of a word's bytes is 255 (the test for a byte of zeros, of the complement)
+__device__ __forceinline__ bool some_byte_ff(uint32_t w) {
+    const uint32_t n = ~w;
+    return ((n - 0x01010101u) & ~n & 0x80808080u) != 0;
+}
+
+// Values of dims 2 E and 2 E + 1 (of a lane's CH) of its eight slots, as operands: codes become pairs of dims of one slot,
+// two permutes turn two slots' pairs into pairs of slots of one dim.
+struct FewPairs {
+    uint4 even, odd;
+};
+template <int DH, int E>
+__device__ __forceinline__ FewPairs few_pairs(const FewRaw<DH>& x, const float (&sc)[8]) {
+    uint32_t w[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const uint8_t* p = v + (size_t)(vr + i) * (DH / 2) + c * (DH / 32);
-        if constexpr (DH == 128) x.v[i] = *reinterpret_cast<const uint32_t*>(p);
-        else x.v[i] = *reinterpret_cast<const uint16_t*>(p);
-    }
-    const uint4* s = reinterpret_cast<const uint4*>(vs + (size_t)vr * NB);
-    if constexpr (DH == 128) {
-        const uint4 a = s[0], b = s[1];
-        x.vs[0] = a.x, x.vs[1] = a.y, x.vs[2] = a.z, x.vs[3] = a.w;
-        x.vs[4] = b.x, x.vs[5] = b.y, x.vs[6] = b.z, x.vs[7] = b.w;
-    } else {
-        const uint4 a = s[0];
-        x.vs[0] = a.x & 0xffffu, x.vs[1] = a.x >> 16, x.vs[2] = a.y & 0xffffu, x.vs[3] = a.y >> 16;
-        x.vs[4] = a.z & 0xffffu, x.vs[5] = a.z >> 16, x.vs[6] = a.w & 0xffffu, x.vs[7] = a.w >> 16;
-    }
+    for (int i = 0; i < 8; ++i) w[i] = fp4_pair<E>(x.v[i], sc[i]);
+    FewPairs p;
+    p.even.x = __builtin_amdgcn_perm(w[1], w[0], 0x05040100u), p.odd.x = __builtin_amdgcn_perm(w[1], w[0], 0x07060302u);
+    p.even.y = __builtin_amdgcn_perm(w[3], w[2], 0x05040100u), p.odd.y = __builtin_amdgcn_perm(w[3], w[2], 0x07060302u);
+    p.even.z = __builtin_amdgcn_perm(w[5], w[4], 0x05040100u), p.odd.z = __builtin_amdgcn_perm(w[5], w[4], 0x07060302u);
+    p.even.w = __builtin_amdgcn_perm(w[7], w[6], 0x05040100u), p.odd.w = __builtin_amdgcn_perm(w[7], w[6], 0x07060302u);
+    return p;
 }
 
 // WHOLE: the workgroup has all of its sample's slots; it keeps the logits in LDS and finishes outputs and weights itself.
 // Otherwise it leaves its part (maximum, sum, O) and the raw logits for join_kernel.
 template <int DH, int WAVES, bool WHOLE>
-__global__ __launch_bounds__(WAVES * 64) void few_rows_kernel(CacheView cache, CacheAttention a, int group, int splits,
+__global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void few_rows_kernel(CacheView cache, CacheAttention a, int group, int splits,
                                                               float* __restrict__ part_o, float2* __restrict__ part_ml,
                                                               float* __restrict__ logits, int logit_pitch) {
     constexpr int NB = DH / 32, CH = DH / 16, STEPS = DH / 32;
@@ -123,14 +162,11 @@ __global__ __launch_bounds__(WAVES * 64) void few_rows_kernel(CacheView cache, C
     const int step1 = WHOLE ? n_steps : (int)((int64_t)n_steps * (split + 1) / splits);
 
     const size_t head = (size_t)b * cache.H_kv + h;
-    const uint8_t* k = cache.k + head * cache.capacity * (DH / 2);
-    const uint8_t* v = cache.v + head * cache.capacity * (DH / 2);
-    const uint8_t* ks = cache.k_scale + head * cache.capacity * NB;
-    const uint8_t* vs = cache.v_scale + head * cache.capacity * NB;
+    const FewRows<DH> from(cache, head, c, g);
 
     FewRaw<DH> raw[3];
     auto load = [&](FewRaw<DH>& x, int step) __attribute__((always_inline)) {
-        if (step < step1) few_load<DH>(x, k, ks, v, vs, step * FEW_STEP, c, g);
+        if (step < step1) from.load(x, step * FEW_STEP);
     };
 #pragma unroll
     for (int i = 0; i < 3; ++i) load(raw[i], step0 + wave + i * WAVES);
@@ -191,9 +227,7 @@ __global__ __launch_bounds__(WAVES * 64) void few_rows_kernel(CacheView cache, C
             // a new row whose values are no numbers reaches the rows that see it, not those before it
             bool any = false;
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-#pragma unroll
-                for (int blk = 0; blk < NB; ++blk) any |= ((x.vs[i] >> (8 * blk)) & 0xffu) == 0xffu;
+            for (int i = 0; i < 8; ++i) any |= some_byte_ff(x.vs[i]);
             if (__any(any)) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
@@ -237,16 +271,9 @@ __global__ __launch_bounds__(WAVES * 64) void few_rows_kernel(CacheView cache, C
         for (int i = 0; i < 8; ++i) sc[i] = fp4_scale(x.vs[i], v_blk);
         auto pairs = [&](auto sel) __attribute__((always_inline)) {
             constexpr int E = decltype(sel)::value;
-            uint32_t w[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) w[i] = fp4_pair<E>(x.v[i], sc[i]);
-            uint4 even, odd;
-            even.x = __builtin_amdgcn_perm(w[1], w[0], 0x05040100u), odd.x = __builtin_amdgcn_perm(w[1], w[0], 0x07060302u);
-            even.y = __builtin_amdgcn_perm(w[3], w[2], 0x05040100u), odd.y = __builtin_amdgcn_perm(w[3], w[2], 0x07060302u);
-            even.z = __builtin_amdgcn_perm(w[5], w[4], 0x05040100u), odd.z = __builtin_amdgcn_perm(w[5], w[4], 0x07060302u);
-            even.w = __builtin_amdgcn_perm(w[7], w[6], 0x05040100u), odd.w = __builtin_amdgcn_perm(w[7], w[6], 0x07060302u);
-            o[2 * E] = mfma16(even, pf, o[2 * E]);
-            o[2 * E + 1] = mfma16(odd, pf, o[2 * E + 1]);
+            const FewPairs w = few_pairs<DH, E>(x, sc);
+            o[2 * E] = mfma16(w.even, pf, o[2 * E]);
+            o[2 * E + 1] = mfma16(w.odd, pf, o[2 * E + 1]);
         };
         pairs(std::integral_constant<int, 0>{});
         pairs(std::integral_constant<int, 1>{});
@@ -341,6 +368,231 @@ __global__ __launch_bounds__(WAVES * 64) void few_rows_kernel(CacheView cache, C
             if (slot + 1 < span.len) weight[slot + 1] += sum.y;
             if (slot + 2 < span.len) weight[slot + 2] += sum.z;
             if (slot + 3 < span.len) weight[slot + 3] += sum.w;
+        }
+    }
+}
+
+// ---- some rows -----------------------------------------------------------------------------------------------------
+// 16 CT rows a workgroup: the same step with CT column tiles a wave, so that a slot's codes become values once for all of
+// them.  Eight waves a workgroup; queries wait in LDS (their registers go to the accumulators), and the waves' parts are joined
+// there in three rounds, half of the waves handing theirs to the others each time.
+constexpr int SOME_WAVES = 8;
+
+template <int DH, int CT>
+__global__ __launch_bounds__(SOME_WAVES * 64) void some_rows_kernel(CacheView cache, CacheAttention a, int group, int splits,
+                                                                    float* __restrict__ part_o, float2* __restrict__ part_ml) {
+    constexpr int NB = DH / 32, CH = DH / 16, STEPS = DH / 32;
+    extern __shared__ float4 parts[];         // [4][CT * CH][64] parts of O; before that the queries [CT * STEPS][64]
+    __shared__ float sh_m[SOME_WAVES / 2][CT][64], sh_l[SOME_WAVES / 2][CT][64];
+
+    const int split = blockIdx.x % splits, h = blockIdx.x / splits, b = blockIdx.y, r0 = blockIdx.z * 16 * CT;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c = lane & 15, g = lane >> 4;
+    const Span span = sample_span(a, cache.capacity, b);
+    const int rows = a.n_q * group;
+    // (steps beyond what the block's last row sees are nobody's)
+    const int last_i = min((min(r0 + 16 * CT, rows) - 1) / group, span.count - 1);
+    const int n_steps = last_i < r0 / group ? 0 : (seen_by(span, last_i) + FEW_STEP - 1) / FEW_STEP;
+    const int step0 = (int)((int64_t)n_steps * split / splits), step1 = (int)((int64_t)n_steps * (split + 1) / splits);
+
+    const size_t head = (size_t)b * cache.H_kv + h;
+    const FewRows<DH> from(cache, head, c, g);
+    FewRaw<DH> x, next;
+    if (step0 + wave < step1) from.load(next, (step0 + wave) * FEW_STEP);
+
+    uint4* sh_q = reinterpret_cast<uint4*>(parts);
+    for (int id = tid; id < CT * STEPS * 64; id += SOME_WAVES * 64) {
+        const int ct = id / (STEPS * 64), st = id / 64 % STEPS, r = r0 + ct * 16 + (id & 15), i = r / group;
+        uint4 q = make_uint4(0u, 0u, 0u, 0u);
+        if (r < rows)
+            q = *reinterpret_cast<const uint4*>(a.q.p + b * a.q.sample + i * a.q.token + (h * group + r % group) * a.q.head +
+                                                (id >> 4 & 3) * (DH / 4) + st * 8);
+        sh_q[id] = q;
+    }
+    // slots that row r0 + ct * 16 + c sees, this lane's column of tile ct (see few_rows_kernel); only masked steps ask
+    auto limit_of = [&](int ct) __attribute__((always_inline)) {
+        const int r = r0 + ct * 16 + c, i = r / group;
+        return r < rows && i < span.count ? seen_by(span, i) : span.len;
+    };
+    const int least = r0 / group < span.count ? seen_by(span, r0 / group) : span.len;
+    const float scale_log2e = a.scale * 1.4426950408889634f;
+    const int k_blk = DH == 128 ? g : g >> 1, v_blk = DH == 128 ? c >> 2 : c >> 3;
+    f32x4_t o[CT][CH];
+    float run_m[CT], run_l[CT];
+    uint32_t not_a_number = 0;                // NB bits a column tile
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+        run_m[ct] = -INFINITY, run_l[ct] = 0.f;
+#pragma unroll
+        for (int d = 0; d < CH; ++d) o[ct][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
+    __syncthreads();
+    for (int step = step0 + wave; step < step1; step += SOME_WAVES) {
+        x = next;
+        if (step + SOME_WAVES < step1) from.load(next, (step + SOME_WAVES) * FEW_STEP);
+        const int my0 = step * FEW_STEP + 8 * g;
+        const bool masked = step * FEW_STEP + FEW_STEP > least;
+        // ---- S^T of all tiles
+        f32x4_t s[CT][2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const float scale = fp4_scale(x.ks[j], k_blk);
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) s[ct][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int st = 0; st < STEPS; ++st) {
+                const uint4 kf = fp4_values(x.k[j][st], scale);
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) s[ct][j] = mfma16(kf, sh_q[(ct * STEPS + st) * 64 + lane], s[ct][j]);
+            }
+        }
+        if (masked) {
+            bool any = false;
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) {
+                const int limit = limit_of(ct);
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (my0 + i >= limit) s[ct][i >> 2][i & 3] = -INFINITY;
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (my0 + i >= span.len) {
+                    x.v[i] = 0;
+                    x.vs[i] = 0x7f7f7f7fu;
+                }
+                any |= some_byte_ff(x.vs[i]);
+            }
+            if (__any(any)) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+#pragma unroll
+                    for (int blk = 0; blk < NB; ++blk)
+                        if (((x.vs[i] >> (8 * blk)) & 0xffu) == 0xffu) {
+#pragma unroll
+                            for (int ct = 0; ct < CT; ++ct)
+                                if (my0 + i < limit_of(ct)) not_a_number |= 1u << (ct * NB + blk);
+                            if (blk == v_blk) {
+                                x.v[i] = 0;
+                                x.vs[i] &= ~(0x80u << (8 * blk));
+                            }
+                        }
+            }
+        }
+        // ---- softmax against the running maxima
+        uint4 pf[CT];
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+            float top = s[ct][0][0];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) top = fmaxf(top, s[ct][i >> 2][i & 3]);
+            if (__any(top > run_m[ct])) {
+                const float m = fmaxf(run_m[ct], column_max(top));
+                const float f = m == run_m[ct] ? 1.f : __builtin_amdgcn_exp2f((run_m[ct] - m) * scale_log2e);
+                run_l[ct] *= f;
+#pragma unroll
+                for (int d = 0; d < CH; ++d)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[ct][d][i] *= f;
+                run_m[ct] = m;
+            }
+            const float neg_m = run_m[ct] == -INFINITY ? 0.f : -run_m[ct] * scale_log2e;
+            float e[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                e[i] = __builtin_amdgcn_exp2f(fmaf(s[ct][i >> 2][i & 3], scale_log2e, neg_m));
+                run_l[ct] += e[i];
+            }
+            pf[ct] = make_uint4(pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3]), pack_bf16x2(e[4], e[5]),
+                                pack_bf16x2(e[6], e[7]));
+        }
+        // ---- O^T
+        float sc[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sc[i] = fp4_scale(x.vs[i], v_blk);
+        auto pairs = [&](auto sel) __attribute__((always_inline)) {
+            constexpr int E = decltype(sel)::value;
+            const FewPairs w = few_pairs<DH, E>(x, sc);
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) {
+                o[ct][2 * E] = mfma16(w.even, pf[ct], o[ct][2 * E]);
+                o[ct][2 * E + 1] = mfma16(w.odd, pf[ct], o[ct][2 * E + 1]);
+            }
+        };
+        pairs(std::integral_constant<int, 0>{});
+        pairs(std::integral_constant<int, 1>{});
+        if constexpr (CH == 8) {
+            pairs(std::integral_constant<int, 2>{});
+            pairs(std::integral_constant<int, 3>{});
+        }
+    }
+
+    // ---- the waves' parts, joined
+    not_a_number = column_or(not_a_number);
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+        run_l[ct] = column_sum(run_l[ct]);
+        if (not_a_number >> (ct * NB + k_blk) & 1u)       // (this lane's dims lie in block k_blk)
+#pragma unroll
+            for (int d = 0; d < CH; ++d) o[ct][d] = f32x4_t{NAN, NAN, NAN, NAN};
+    }
+#pragma unroll
+    for (int half = SOME_WAVES / 2; half; half >>= 1) {
+        __syncthreads();                      // (the queries, and the round before, have been read)
+        if (wave >= half && wave < 2 * half) {
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) {
+                sh_m[wave - half][ct][lane] = run_m[ct];
+                sh_l[wave - half][ct][lane] = run_l[ct];
+#pragma unroll
+                for (int d = 0; d < CH; ++d)
+                    parts[((wave - half) * CT * CH + ct * CH + d) * 64 + lane] = make_float4(o[ct][d][0], o[ct][d][1], o[ct][d][2], o[ct][d][3]);
+            }
+        }
+        __syncthreads();
+        if (wave < half) {
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) {
+                const float m1 = sh_m[wave][ct][lane], m = fmaxf(run_m[ct], m1);
+                const float f0 = run_m[ct] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((run_m[ct] - m) * scale_log2e);
+                const float f1 = m1 == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m1 - m) * scale_log2e);
+                run_m[ct] = m;
+                run_l[ct] = fmaf(run_l[ct], f0, sh_l[wave][ct][lane] * f1);
+#pragma unroll
+                for (int d = 0; d < CH; ++d) {
+                    const float4 t = parts[(wave * CT * CH + ct * CH + d) * 64 + lane];
+                    o[ct][d][0] = fmaf(t.x, f1, o[ct][d][0] * f0), o[ct][d][1] = fmaf(t.y, f1, o[ct][d][1] * f0);
+                    o[ct][d][2] = fmaf(t.z, f1, o[ct][d][2] * f0), o[ct][d][3] = fmaf(t.w, f1, o[ct][d][3] * f0);
+                }
+            }
+        }
+    }
+    if (wave != 0) return;
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+        const int r = r0 + ct * 16 + c, i = r / group;
+        if (r >= rows) continue;
+        const size_t row = ((size_t)split * cache.B * cache.H_kv + head) * rows + r;
+        if (g == 0) part_ml[row] = make_float2(run_m[ct], run_l[ct]);
+        const bool none = seen_by(span, i) == 0;
+        const float inv = 1.f / run_l[ct];
+        bf16_t* out = const_cast<bf16_t*>(a.out.p) + b * a.out.sample + i * a.out.token + (h * group + r % group) * a.out.head;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {         // dims (4 g + e) CH ..
+            if (splits > 1) {
+#pragma unroll
+                for (int q = 0; q < CH / 4; ++q)
+                    *reinterpret_cast<float4*>(part_o + row * DH + (4 * g + e) * CH + 4 * q) =
+                        make_float4(o[ct][4 * q][e], o[ct][4 * q + 1][e], o[ct][4 * q + 2][e], o[ct][4 * q + 3][e]);
+            } else {
+#pragma unroll
+                for (int q = 0; q < CH / 4; ++q) {
+                    uint2 w = make_uint2(pack_bf16x2(o[ct][4 * q][e] * inv, o[ct][4 * q + 1][e] * inv),
+                                         pack_bf16x2(o[ct][4 * q + 2][e] * inv, o[ct][4 * q + 3][e] * inv));
+                    if (none) w = make_uint2(0u, 0u);
+                    *reinterpret_cast<uint2*>(out + (4 * g + e) * CH + 4 * q) = w;
+                }
+            }
         }
     }
 }
@@ -692,6 +944,25 @@ __global__ __launch_bounds__(WEIGH_WAVES * 64) void weigh_kernel(CacheView cache
     if (slot0 >= span.len) return;
     const int rows = a.n_q * group;
     const size_t head = (size_t)b * cache.H_kv + h;
+    // the first query that sees any of these slots
+    const int first_i = max(0, slot0 - (span.len - span.count)), last_row = min(rows, span.count * group);
+    struct Column {                           // a row's queries, this lane's part, and its maximum and sum
+        uint4 q[STEPS];
+        float2 ml;
+        int i;
+    };
+    const bf16_t* q0 = a.q.p + b * a.q.sample + g * (DH / 4);
+    auto load = [&](Column& x, int r0) __attribute__((always_inline)) {
+        if (r0 >= last_row) return;
+        const int r = min(r0 + c, last_row - 1);
+        x.i = r / group;
+        const bf16_t* src = q0 + x.i * a.q.token + (h * group + r - x.i * group) * a.q.head;
+#pragma unroll
+        for (int st = 0; st < STEPS; ++st) x.q[st] = *reinterpret_cast<const uint4*>(src + st * 8);
+        x.ml = row_ml[head * rows + r];
+    };
+    Column next;
+    load(next, first_i * group);
     uint4 kf[2][STEPS];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
@@ -703,29 +974,24 @@ __global__ __launch_bounds__(WEIGH_WAVES * 64) void weigh_kernel(CacheView cache
     }
     const float scale_log2e = a.scale * 1.4426950408889634f;
     const int my0 = slot0 + 8 * g;
-    // the first query that sees any of these slots
-    const int first_i = max(0, slot0 - (span.len - span.count)), last_row = min(rows, span.count * group);
     float sum[8] = {};
     for (int r0 = first_i * group; r0 < last_row; r0 += 16) {
-        const int r = min(r0 + c, last_row - 1), i = r / group;
-        const bf16_t* src = a.q.p + b * a.q.sample + i * a.q.token + (h * group + r % group) * a.q.head + g * (DH / 4);
-        uint4 qf[STEPS];
-#pragma unroll
-        for (int st = 0; st < STEPS; ++st) qf[st] = *reinterpret_cast<const uint4*>(src + st * 8);
-        const float2 t = row_ml[head * rows + r];
-        const float inv = 1.f / t.y, neg_m = -t.x * scale_log2e;
-        const int limit = r0 + c < last_row ? seen_by(span, i) : 0;
+        const Column x = next;
+        load(next, r0 + 16);
+        const float inv = 1.f / x.ml.y, neg_m = -x.ml.x * scale_log2e;
         f32x4_t s[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             s[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int st = 0; st < STEPS; ++st) s[j] = mfma16(kf[j][st], qf[st], s[j]);
+            for (int st = 0; st < STEPS; ++st) s[j] = mfma16(kf[j][st], x.q[st], s[j]);
         }
+        const int limit = r0 + c < last_row ? seen_by(span, x.i) : 0;
 #pragma unroll
-        for (int n = 0; n < 8; ++n)
-            if (my0 + n < limit)
-                sum[n] += __builtin_amdgcn_exp2f(fmaf(s[n >> 2][n & 3], scale_log2e, neg_m)) * inv;
+        for (int n = 0; n < 8; ++n) {
+            const float p = __builtin_amdgcn_exp2f(fmaf(s[n >> 2][n & 3], scale_log2e, neg_m)) * inv;
+            sum[n] += my0 + n < limit ? p : 0.f;
+        }
     }
     // over the 16 columns of a group
 #pragma unroll
@@ -742,9 +1008,11 @@ __global__ __launch_bounds__(WEIGH_WAVES * 64) void weigh_kernel(CacheView cache
 // ---- host --------------------------------------------------------------------------------------------------------
 namespace {
 
+enum AttentionKind { FEW, SOME, MANY };
+constexpr int SOME_MOST = 96;
 struct AttentionPlan {
-    bool many;
-    int group, rows, splits, waves, pitch;    // waves: of few_rows_kernel; splits 0: whole samples, no second launch
+    AttentionKind kind;
+    int group, rows, tiles, splits, waves, pitch;    // tiles: of some_rows_kernel, waves: of few_rows_kernel; splits 0: whole samples, no second launch
     size_t o_bytes, ml_bytes, row_bytes, logit_bytes;
     size_t bytes() const { return o_bytes + ml_bytes + row_bytes + logit_bytes; }
 };
@@ -756,11 +1024,12 @@ AttentionPlan attention_plan(int B, int H, int H_kv, int dh, int n_q, int max_le
     AttentionPlan p{};
     p.group = H / H_kv;
     p.rows = n_q * p.group;
-    p.many = p.rows > FEW_ROWS;
+    p.kind = p.rows <= FEW_ROWS ? FEW : p.rows <= SOME_MOST ? SOME : MANY;
+    p.tiles = p.rows <= 32 || (p.rows > 48 && p.rows <= 64) ? 2 : 3;
     p.pitch = (max_len + FEW_STEP - 1) / FEW_STEP * FEW_STEP;
     const int cus = device_cu_count();
     const int64_t heads = (int64_t)B * H_kv, steps = p.pitch / FEW_STEP;
-    if (!p.many) {
+    if (p.kind == FEW) {
         // Whole samples a workgroup where that fills the chip, or where there is little to split; eight waves where a
         // launch leaves compute units idle.
         p.waves = heads <= cus ? 8 : 4;
@@ -775,6 +1044,10 @@ AttentionPlan attention_plan(int B, int H, int H_kv, int dh, int n_q, int max_le
             const int64_t even = std::min(tiles / 8, (16 * (int64_t)cus + heads - 1) / heads);
             p.splits = (int)std::max(fill, even);
         }
+    } else if (p.kind == SOME) {
+        const int64_t most = (steps + SOME_WAVES - 1) / SOME_WAVES, blocks = (p.rows + 16 * p.tiles - 1) / (16 * p.tiles);
+        const int64_t want = cus / (heads * blocks);   // (one workgroup a compute unit)
+        p.splits = (int)std::max((int64_t)1, std::min(most, want));
     } else {
         const int64_t wgs = heads * ((p.rows + MANY_ROWS - 1) / MANY_ROWS), tiles = ((int64_t)max_len + MANY_KT - 1) / MANY_KT;
         const int64_t want = (2 * (int64_t)cus + wgs - 1) / wgs, most = (tiles + 3) / 4;   // (few tiles are not worth a part)
@@ -782,10 +1055,10 @@ AttentionPlan attention_plan(int B, int H, int H_kv, int dh, int n_q, int max_le
     }
     if (p.splits > MAX_SPLITS) p.splits = MAX_SPLITS;
     const size_t all = (size_t)heads * p.rows;
-    p.o_bytes = p.splits < (p.many ? 2 : 1) ? 0 : align_up(all * p.splits * dh * 4, 256);
+    p.o_bytes = p.splits < (p.kind == FEW ? 1 : 2) ? 0 : align_up(all * p.splits * dh * 4, 256);
     p.ml_bytes = align_up(all * p.splits * 8, 256);
-    p.row_bytes = p.many ? align_up(all * 8, 256) : 0;
-    p.logit_bytes = accumulate && !p.many && p.splits ? align_up(all * p.pitch * 4, 256) : 0;
+    p.row_bytes = p.kind != FEW ? align_up(all * 8, 256) : 0;
+    p.logit_bytes = accumulate && p.kind == FEW && p.splits ? align_up(all * p.pitch * 4, 256) : 0;
     return p;
 }
 
@@ -812,13 +1085,36 @@ int launch_few(const CacheView& c, const CacheAttention& a, const AttentionPlan&
     return MVLA_OK;
 }
 
+template <int DH, int CT>
+int launch_some(const CacheView& c, const CacheAttention& a, const AttentionPlan& p, float* o, float2* ml, hipStream_t st) {
+    static bool lds_set[kMaxDevices] = {};
+    const size_t lds = (size_t)(SOME_WAVES / 2) * CT * (DH / 16) * 64 * sizeof(float4);
+    if (int rc = allow_lds(reinterpret_cast<const void*>(&some_rows_kernel<DH, CT>), lds_set, lds)) return rc;
+    hipLaunchKernelGGL((some_rows_kernel<DH, CT>), dim3(c.H_kv * p.splits, c.B, (p.rows + 16 * CT - 1) / (16 * CT)),
+                       dim3(SOME_WAVES * 64), lds, st, c, a, p.group,
+                       p.splits, o, ml);
+    MVLA_HIP_CHECK(hipGetLastError());
+    return MVLA_OK;
+}
+
+template <int DH>
+int launch_many(const CacheView& c, const CacheAttention& a, const AttentionPlan& p, float* o, float2* ml, hipStream_t st) {
+    static bool lds_set[kMaxDevices] = {};
+    const size_t lds = 2 * (MANY_KT * (DH / 8) + DH * 8) * sizeof(uint4);
+    if (int rc = allow_lds(reinterpret_cast<const void*>(&many_rows_kernel<DH>), lds_set, lds)) return rc;
+    hipLaunchKernelGGL((many_rows_kernel<DH>), dim3(c.H_kv, (p.rows + MANY_ROWS - 1) / MANY_ROWS, c.B * p.splits),
+                       dim3(MANY_THREADS), lds, st, c, a, p.group, p.splits, o, ml);
+    MVLA_HIP_CHECK(hipGetLastError());
+    return MVLA_OK;
+}
+
 template <int DH>
 int run_attention(const CacheView& c, const CacheAttention& a, const AttentionPlan& p, char* scratch, hipStream_t st) {
     float* o = reinterpret_cast<float*>(scratch);
     float2* ml = reinterpret_cast<float2*>(scratch + p.o_bytes);
     float2* row_ml = reinterpret_cast<float2*>(scratch + p.o_bytes + p.ml_bytes);
     float* logits = reinterpret_cast<float*>(scratch + p.o_bytes + p.ml_bytes + p.row_bytes);
-    if (!p.many) {
+    if (p.kind == FEW) {
         if (!p.splits)
             return p.waves == 8 ? launch_few<DH, 8, true>(c, a, p, nullptr, nullptr, nullptr, st)
                                 : launch_few<DH, 4, true>(c, a, p, nullptr, nullptr, nullptr, st);
@@ -832,12 +1128,9 @@ int run_attention(const CacheView& c, const CacheAttention& a, const AttentionPl
         MVLA_HIP_CHECK(hipGetLastError());
         return MVLA_OK;
     }
-    static bool lds_set[kMaxDevices] = {};
-    const size_t lds = 2 * (MANY_KT * (DH / 8) + DH * 8) * sizeof(uint4);
-    if (int rc = allow_lds(reinterpret_cast<const void*>(&many_rows_kernel<DH>), lds_set, lds)) return rc;
-    hipLaunchKernelGGL((many_rows_kernel<DH>), dim3(c.H_kv, (p.rows + MANY_ROWS - 1) / MANY_ROWS, c.B * p.splits),
-                       dim3(MANY_THREADS), lds, st, c, a, p.group, p.splits, o, ml);
-    MVLA_HIP_CHECK(hipGetLastError());
+    const int rc = p.kind == MANY ? launch_many<DH>(c, a, p, o, ml, st)
+                   : p.tiles == 2 ? launch_some<DH, 2>(c, a, p, o, ml, st) : launch_some<DH, 3>(c, a, p, o, ml, st);
+    if (rc) return rc;
     const float2* joined = ml;
     if (p.splits > 1) {
         hipLaunchKernelGGL(join_kernel, dim3((p.rows + JOIN_ROWS - 1) / JOIN_ROWS, c.H_kv, c.B), dim3(JOIN_THREADS), 0, st,
