@@ -931,77 +931,131 @@ __global__ __launch_bounds__(MANY_THREADS, 2) void many_rows_kernel(CacheView ca
 // The logits once more (keys only), against the rows' final maxima and sums: a wave holds 32 slots' keys in registers
 // and walks the rows, 16 at a time; the columns' sums go over the lanes of a group at the end.  No value is added twice
 // or in another order from run to run.
-constexpr int WEIGH_WAVES = 4;
+constexpr int WEIGH_WAVES = 4, SOME_MOST = 96;
 
-template <int DH>
-__global__ __launch_bounds__(WEIGH_WAVES * 64) void weigh_kernel(CacheView cache, CacheAttention a, int group,
+// LDS_ROWS: up to so many rows' queries, maxima and sums come to LDS once per workgroup, and a wave goes on to `groups`
+// runs of 32 slots, the next run's keys on their way; 0: more rows, straight from memory, one run a wave.
+template <int DH, int LDS_ROWS>
+__global__ __launch_bounds__(WEIGH_WAVES * 64) void weigh_kernel(CacheView cache, CacheAttention a, int group, int groups,
                                                                  const float2* __restrict__ row_ml) {
-    constexpr int NB = DH / 32, STEPS = DH / 32;
+    constexpr int NB = DH / 32, STEPS = DH / 32, TILES = LDS_ROWS / 16;
+    __shared__ uint4 sh_q[TILES ? TILES * STEPS * 64 : 1];
+    __shared__ float2 sh_ml[TILES ? LDS_ROWS : 1];
+    __shared__ int sh_sees[TILES ? LDS_ROWS : 1];
     const int h = blockIdx.y, b = blockIdx.z, lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
     const Span span = sample_span(a, cache.capacity, b);
-    const int slot0 = (blockIdx.x * WEIGH_WAVES + wave) * FEW_STEP;
-    if (slot0 >= span.len) return;
-    const int rows = a.n_q * group;
+    const int rows = a.n_q * group, stride = gridDim.x * WEIGH_WAVES * FEW_STEP;
+    int slot0 = (blockIdx.x * WEIGH_WAVES + wave) * FEW_STEP;
+    if (blockIdx.x * WEIGH_WAVES * FEW_STEP >= span.len) return;
     const size_t head = (size_t)b * cache.H_kv + h;
-    // the first query that sees any of these slots
-    const int first_i = max(0, slot0 - (span.len - span.count)), last_row = min(rows, span.count * group);
-    struct Column {                           // a row's queries, this lane's part, and its maximum and sum
+    const float scale_log2e = a.scale * 1.4426950408889634f;
+    const int last_row = min(rows, span.count * group);
+    struct Keys {                             // this lane's codes of a run's two tiles
+        uint32_t k[2][STEPS], e[2];
+    };
+    auto load_keys = [&](Keys& x, int at_slot) __attribute__((always_inline)) {
+        if (at_slot >= span.len) return;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const size_t at = head * cache.capacity + at_slot + 8 * (c >> 2) + 4 * j + (c & 3);
+            x.e[j] = cache.k_scale[at * NB + (DH == 128 ? g : g >> 1)];
+            const uint8_t* p = cache.k + at * (DH / 2) + g * (DH / 8);
+            if constexpr (DH == 128) {
+                const uint4 w = *reinterpret_cast<const uint4*>(p);
+                x.k[j][0] = w.x, x.k[j][1] = w.y, x.k[j][2] = w.z, x.k[j][3] = w.w;
+            } else {
+                const uint2 w = *reinterpret_cast<const uint2*>(p);
+                x.k[j][0] = w.x, x.k[j][1] = w.y;
+            }
+        }
+    };
+    Keys next;
+    load_keys(next, slot0);
+    // a row's queries, this lane's part, with -maximum * scale and 1 / sum, and what the row sees
+    struct Column {
         uint4 q[STEPS];
         float2 ml;
-        int i;
+        int sees;
     };
-    const bf16_t* q0 = a.q.p + b * a.q.sample + g * (DH / 4);
-    auto load = [&](Column& x, int r0) __attribute__((always_inline)) {
+    auto from_memory = [&](Column& x, int r0) __attribute__((always_inline)) {
         if (r0 >= last_row) return;
-        const int r = min(r0 + c, last_row - 1);
-        x.i = r / group;
-        const bf16_t* src = q0 + x.i * a.q.token + (h * group + r - x.i * group) * a.q.head;
+        const int r = min(r0 + c, last_row - 1), i = r / group;
+        const bf16_t* src = a.q.p + b * a.q.sample + i * a.q.token + (h * group + r - i * group) * a.q.head + g * (DH / 4);
 #pragma unroll
         for (int st = 0; st < STEPS; ++st) x.q[st] = *reinterpret_cast<const uint4*>(src + st * 8);
         x.ml = row_ml[head * rows + r];
+        x.sees = r0 + c < last_row ? seen_by(span, i) : 0;
     };
-    Column next;
-    load(next, first_i * group);
-    uint4 kf[2][STEPS];
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const size_t at = head * cache.capacity + slot0 + 8 * (c >> 2) + 4 * j + (c & 3);
-        const float scale = __uint_as_float((uint32_t)cache.k_scale[at * NB + (DH == 128 ? g : g >> 1)] << 23);
-        const uint32_t* p = reinterpret_cast<const uint32_t*>(cache.k + at * (DH / 2) + g * (DH / 8));
-#pragma unroll
-        for (int st = 0; st < STEPS; ++st) kf[j][st] = fp4_values(p[st], scale);
-    }
-    const float scale_log2e = a.scale * 1.4426950408889634f;
-    const int my0 = slot0 + 8 * g;
-    float sum[8] = {};
-    for (int r0 = first_i * group; r0 < last_row; r0 += 16) {
-        const Column x = next;
-        load(next, r0 + 16);
-        const float inv = 1.f / x.ml.y, neg_m = -x.ml.x * scale_log2e;
-        f32x4_t s[2];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            s[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int st = 0; st < STEPS; ++st) s[j] = mfma16(kf[j][st], x.q[st], s[j]);
+    if constexpr (TILES > 0) {
+        for (int id = threadIdx.x; id < (rows + 15) / 16 * STEPS * 64; id += WEIGH_WAVES * 64) {
+            const int tile = id / (STEPS * 64), st = id / 64 % STEPS, r = min(tile * 16 + (id & 15), rows - 1), i = r / group;
+            sh_q[id] = *reinterpret_cast<const uint4*>(a.q.p + b * a.q.sample + i * a.q.token + (h * group + r % group) * a.q.head +
+                                                       (id >> 4 & 3) * (DH / 4) + st * 8);
         }
-        const int limit = r0 + c < last_row ? seen_by(span, x.i) : 0;
+        for (int r = threadIdx.x; r < LDS_ROWS; r += WEIGH_WAVES * 64) {
+            const float2 ml = row_ml[head * rows + min(r, rows - 1)];
+            sh_ml[r] = make_float2(-ml.x * scale_log2e, 1.f / ml.y);
+            sh_sees[r] = r < last_row ? seen_by(span, r / group) : 0;
+        }
+        __syncthreads();
+    }
+    for (int run = 0; run < (TILES ? groups : 1) && slot0 < span.len; ++run, slot0 += stride) {
+        uint4 kf[2][STEPS];
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int st = 0; st < STEPS; ++st) kf[j][st] = fp4_values(next.k[j][st], __uint_as_float(next.e[j] << 23));
+        if (TILES && run + 1 < groups) load_keys(next, slot0 + stride);
+        const int my0 = slot0 + 8 * g;
+        // the first query that sees any of these slots
+        const int first_row = max(0, slot0 - (span.len - span.count)) * group;
+        float sum[8] = {};
+        auto add = [&](const uint4 (&q)[STEPS], float2 ml, int sees) __attribute__((always_inline)) {
+            f32x4_t s[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                s[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int st = 0; st < STEPS; ++st) s[j] = mfma16(kf[j][st], q[st], s[j]);
+            }
+#pragma unroll
+            for (int n = 0; n < 8; ++n) {
+                const float p = __builtin_amdgcn_exp2f(fmaf(s[n >> 2][n & 3], scale_log2e, ml.x)) * ml.y;
+                sum[n] += my0 + n < sees ? p : 0.f;
+            }
+        };
+        if constexpr (TILES > 0) {
+            for (int tile = first_row / 16; tile * 16 < last_row; ++tile) {
+                uint4 q[STEPS];
+#pragma unroll
+                for (int st = 0; st < STEPS; ++st) q[st] = sh_q[(tile * STEPS + st) * 64 + lane];
+                add(q, sh_ml[tile * 16 + c], sh_sees[tile * 16 + c]);
+            }
+        } else {
+            Column ahead;
+            from_memory(ahead, first_row);
+            for (int r0 = first_row; r0 < last_row; r0 += 16) {
+                const Column x = ahead;
+                from_memory(ahead, r0 + 16);
+                add(x.q, make_float2(-x.ml.x * scale_log2e, 1.f / x.ml.y), x.sees);
+            }
+        }
+        // over the 16 columns of a group
+        float* w = cache.weight + head * cache.capacity + my0;
 #pragma unroll
         for (int n = 0; n < 8; ++n) {
-            const float p = __builtin_amdgcn_exp2f(fmaf(s[n >> 2][n & 3], scale_log2e, neg_m)) * inv;
-            sum[n] += my0 + n < limit ? p : 0.f;
+            float x = sum[n];
+            x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x128, 0xf, 0xf, false));   // row_ror:8
+            x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x124, 0xf, 0xf, false));
+            x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x122, 0xf, 0xf, false));
+            x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x121, 0xf, 0xf, false));
+            sum[n] = x;
         }
-    }
-    // over the 16 columns of a group
+        float mine = sum[0];
 #pragma unroll
-    for (int n = 0; n < 8; ++n) {
-        float x = sum[n];
-        x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x128, 0xf, 0xf, false));   // row_ror:8
-        x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x124, 0xf, 0xf, false));
-        x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x122, 0xf, 0xf, false));
-        x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x121, 0xf, 0xf, false));
-        if (c == n && my0 + n < span.len) cache.weight[head * cache.capacity + my0 + n] += x;
+        for (int n = 1; n < 8; ++n) mine = c == n ? sum[n] : mine;
+        if (c < 8 && my0 + c < span.len) w[c] += mine;
     }
 }
 
@@ -1009,7 +1063,6 @@ __global__ __launch_bounds__(WEIGH_WAVES * 64) void weigh_kernel(CacheView cache
 namespace {
 
 enum AttentionKind { FEW, SOME, MANY };
-constexpr int SOME_MOST = 96;
 struct AttentionPlan {
     AttentionKind kind;
     int group, rows, tiles, splits, waves, pitch;    // tiles: of some_rows_kernel, waves: of few_rows_kernel; splits 0: whole samples, no second launch
@@ -1139,9 +1192,15 @@ int run_attention(const CacheView& c, const CacheAttention& a, const AttentionPl
         joined = row_ml;
     }
     if (a.accumulate) {
-        const int per = FEW_STEP * WEIGH_WAVES;
-        hipLaunchKernelGGL((weigh_kernel<DH>), dim3((a.max_len + per - 1) / per, c.H_kv, c.B), dim3(WEIGH_WAVES * 64), 0, st,
-                           c, a, p.group, joined);
+        const int per = FEW_STEP * WEIGH_WAVES, runs = (a.max_len + per - 1) / per;
+        // (runs of 32 slots a wave: as many as leave four waves a SIMD)
+        const int64_t all = (int64_t)runs * c.H_kv * c.B;
+        const int groups = p.kind == SOME ? (int)std::max((int64_t)1, std::min((int64_t)8, all / (4 * device_cu_count()))) : 1;
+        const dim3 grid((runs + groups - 1) / groups, c.H_kv, c.B);
+        if (p.kind == SOME)
+            hipLaunchKernelGGL((weigh_kernel<DH, SOME_MOST>), grid, dim3(WEIGH_WAVES * 64), 0, st, c, a, p.group, groups, joined);
+        else
+            hipLaunchKernelGGL((weigh_kernel<DH, 0>), grid, dim3(WEIGH_WAVES * 64), 0, st, c, a, p.group, 1, joined);
         MVLA_HIP_CHECK(hipGetLastError());
     }
     return MVLA_OK;
