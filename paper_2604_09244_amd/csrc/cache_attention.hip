@@ -927,21 +927,90 @@ __global__ __launch_bounds__(MANY_THREADS, 2) void many_rows_kernel(CacheView ca
         }
 }
 
-// ---- weights of many rows ----------------------------------------------------------------------------------------
-// The logits once more (keys only), against the rows' final maxima and sums: a wave holds 32 slots' keys in registers
-// and walks the rows, 16 at a time; the columns' sums go over the lanes of a group at the end.  No value is added twice
-// or in another order from run to run.
+// ---- weights of some and of many rows --------------------------------------------------------------------------------
+// The logits once more (keys only), against the rows' final maxima and sums: a wave holds its slots' keys in registers and
+// walks the rows, 16 at a time; the columns' sums go over the lanes of a group at the end.  No value is added twice or in
+// another order from run to run.
 constexpr int WEIGH_WAVES = 4, SOME_MOST = 96;
 
-// LDS_ROWS: up to so many rows' queries, maxima and sums come to LDS once per workgroup, and a wave goes on to `groups`
-// runs of 32 slots, the next run's keys on their way; 0: more rows, straight from memory, one run a wave.
-template <int DH, int LDS_ROWS>
-__global__ __launch_bounds__(WEIGH_WAVES * 64) void weigh_kernel(CacheView cache, CacheAttention a, int group, int groups,
-                                                                 const float2* __restrict__ row_ml) {
-    constexpr int NB = DH / 32, STEPS = DH / 32, TILES = LDS_ROWS / 16;
-    __shared__ uint4 sh_q[TILES ? TILES * STEPS * 64 : 1];
-    __shared__ float2 sh_ml[TILES ? LDS_ROWS : 1];
-    __shared__ int sh_sees[TILES ? LDS_ROWS : 1];
+// this lane's codes of the two K tiles of 32 slots
+template <int DH>
+struct WeighKeys {
+    uint32_t k[2][DH / 32], e[2];
+};
+template <int DH>
+__device__ __forceinline__ void weigh_load(WeighKeys<DH>& x, const CacheView& cache, size_t head, int slot0, int len, int c, int g) {
+    constexpr int NB = DH / 32;
+    if (slot0 >= len) return;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const size_t at = head * cache.capacity + slot0 + 8 * (c >> 2) + 4 * j + (c & 3);
+        x.e[j] = cache.k_scale[at * NB + (DH == 128 ? g : g >> 1)];
+        const uint8_t* p = cache.k + at * (DH / 2) + g * (DH / 8);
+        if constexpr (DH == 128) {
+            const uint4 w = *reinterpret_cast<const uint4*>(p);
+            x.k[j][0] = w.x, x.k[j][1] = w.y, x.k[j][2] = w.z, x.k[j][3] = w.w;
+        } else {
+            const uint2 w = *reinterpret_cast<const uint2*>(p);
+            x.k[j][0] = w.x, x.k[j][1] = w.y;
+        }
+    }
+}
+template <int DH>
+__device__ __forceinline__ void weigh_values(uint4 (&kf)[2][DH / 32], const WeighKeys<DH>& x) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int st = 0; st < DH / 32; ++st) kf[j][st] = fp4_values(x.k[j][st], __uint_as_float(x.e[j] << 23));
+}
+// adds a column's probabilities of N runs of 32 slots to this lane's sums; ml: -maximum * scale, 1 / sum.  MASK: only of slots
+// below `sees`.  (The products' chains alternate: one alone waits for its own results.)
+template <int DH, int N, bool MASK>
+__device__ __forceinline__ void weigh_add(float (&sum)[N][8], const uint4 (&kf)[N][2][DH / 32], const uint4 (&q)[DH / 32],
+                                          float2 ml, int sees, int my0, float scale_log2e) {
+    f32x4_t s[N][2];
+#pragma unroll
+    for (int st = 0; st < DH / 32; ++st)
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                s[n][j] = mfma16(kf[n][j][st], q[st], st ? s[n][j] : f32x4_t{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float e = __builtin_amdgcn_exp2f(fmaf(s[n][i >> 2][i & 3], scale_log2e, ml.x));
+            if constexpr (MASK) sum[n][i] += my0 + 32 * n + i < sees ? e * ml.y : 0.f;
+            else sum[n][i] = fmaf(e, ml.y, sum[n][i]);
+        }
+}
+// the sums over the 16 columns of a group, added to the slots' weights
+__device__ __forceinline__ void weigh_store(float (&sum)[8], float* weight, int my0, int len, int c) {
+#pragma unroll
+    for (int n = 0; n < 8; ++n) {
+        float x = sum[n];
+        x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x128, 0xf, 0xf, false));   // row_ror:8
+        x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x124, 0xf, 0xf, false));
+        x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x122, 0xf, 0xf, false));
+        x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x121, 0xf, 0xf, false));
+        sum[n] = x;
+    }
+    float mine = sum[0];
+#pragma unroll
+    for (int n = 1; n < 8; ++n) mine = c == n ? sum[n] : mine;
+    if (c < 8 && my0 + c < len) weight[my0 + c] += mine;
+}
+
+// Up to SOME_MOST rows: all queries, maxima and sums come to LDS once per workgroup, and a wave goes on to `groups` runs of
+// 32 slots, the next run's keys on their way.
+template <int DH>
+__global__ __launch_bounds__(WEIGH_WAVES * 64, 2) void weigh_some_kernel(CacheView cache, CacheAttention a, int group, int groups,
+                                                                      const float2* __restrict__ row_ml) {
+    constexpr int STEPS = DH / 32;
+    __shared__ uint4 sh_q[SOME_MOST / 16 * STEPS * 64];
+    __shared__ float2 sh_ml[SOME_MOST];
+    __shared__ int sh_sees[SOME_MOST];
     const int h = blockIdx.y, b = blockIdx.z, lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
     const Span span = sample_span(a, cache.capacity, b);
@@ -950,113 +1019,115 @@ __global__ __launch_bounds__(WEIGH_WAVES * 64) void weigh_kernel(CacheView cache
     if (blockIdx.x * WEIGH_WAVES * FEW_STEP >= span.len) return;
     const size_t head = (size_t)b * cache.H_kv + h;
     const float scale_log2e = a.scale * 1.4426950408889634f;
-    const int last_row = min(rows, span.count * group);
-    struct Keys {                             // this lane's codes of a run's two tiles
-        uint32_t k[2][STEPS], e[2];
-    };
-    auto load_keys = [&](Keys& x, int at_slot) __attribute__((always_inline)) {
-        if (at_slot >= span.len) return;
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const size_t at = head * cache.capacity + at_slot + 8 * (c >> 2) + 4 * j + (c & 3);
-            x.e[j] = cache.k_scale[at * NB + (DH == 128 ? g : g >> 1)];
-            const uint8_t* p = cache.k + at * (DH / 2) + g * (DH / 8);
-            if constexpr (DH == 128) {
-                const uint4 w = *reinterpret_cast<const uint4*>(p);
-                x.k[j][0] = w.x, x.k[j][1] = w.y, x.k[j][2] = w.z, x.k[j][3] = w.w;
-            } else {
-                const uint2 w = *reinterpret_cast<const uint2*>(p);
-                x.k[j][0] = w.x, x.k[j][1] = w.y;
-            }
-        }
-    };
-    Keys next;
-    load_keys(next, slot0);
-    // a row's queries, this lane's part, with -maximum * scale and 1 / sum, and what the row sees
-    struct Column {
-        uint4 q[STEPS];
-        float2 ml;
-        int sees;
-    };
-    auto from_memory = [&](Column& x, int r0) __attribute__((always_inline)) {
-        if (r0 >= last_row) return;
-        const int r = min(r0 + c, last_row - 1), i = r / group;
-        const bf16_t* src = a.q.p + b * a.q.sample + i * a.q.token + (h * group + r - i * group) * a.q.head + g * (DH / 4);
-#pragma unroll
-        for (int st = 0; st < STEPS; ++st) x.q[st] = *reinterpret_cast<const uint4*>(src + st * 8);
-        x.ml = row_ml[head * rows + r];
-        x.sees = r0 + c < last_row ? seen_by(span, i) : 0;
-    };
-    if constexpr (TILES > 0) {
-        for (int id = threadIdx.x; id < (rows + 15) / 16 * STEPS * 64; id += WEIGH_WAVES * 64) {
-            const int tile = id / (STEPS * 64), st = id / 64 % STEPS, r = min(tile * 16 + (id & 15), rows - 1), i = r / group;
-            sh_q[id] = *reinterpret_cast<const uint4*>(a.q.p + b * a.q.sample + i * a.q.token + (h * group + r % group) * a.q.head +
-                                                       (id >> 4 & 3) * (DH / 4) + st * 8);
-        }
-        for (int r = threadIdx.x; r < LDS_ROWS; r += WEIGH_WAVES * 64) {
-            const float2 ml = row_ml[head * rows + min(r, rows - 1)];
-            sh_ml[r] = make_float2(-ml.x * scale_log2e, 1.f / ml.y);
-            sh_sees[r] = r < last_row ? seen_by(span, r / group) : 0;
-        }
-        __syncthreads();
+    const int last_row = min(rows, span.count * group), tiles = (rows + 15) / 16;
+    WeighKeys<DH> next;
+    weigh_load<DH>(next, cache, head, slot0, span.len, c, g);
+    for (int id = threadIdx.x; id < tiles * STEPS * 64; id += WEIGH_WAVES * 64) {
+        const int tile = id / (STEPS * 64), st = id / 64 % STEPS, r = min(tile * 16 + (id & 15), rows - 1), i = r / group;
+        sh_q[id] = *reinterpret_cast<const uint4*>(a.q.p + b * a.q.sample + i * a.q.token + (h * group + r % group) * a.q.head +
+                                                   (id >> 4 & 3) * (DH / 4) + st * 8);
     }
-    for (int run = 0; run < (TILES ? groups : 1) && slot0 < span.len; ++run, slot0 += stride) {
-        uint4 kf[2][STEPS];
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int st = 0; st < STEPS; ++st) kf[j][st] = fp4_values(next.k[j][st], __uint_as_float(next.e[j] << 23));
-        if (TILES && run + 1 < groups) load_keys(next, slot0 + stride);
+    for (int r = threadIdx.x; r < tiles * 16; r += WEIGH_WAVES * 64) {
+        const float2 ml = row_ml[head * rows + min(r, rows - 1)];
+        sh_ml[r] = make_float2(-ml.x * scale_log2e, 1.f / ml.y);
+        sh_sees[r] = r < last_row ? seen_by(span, r / group) : 0;
+    }
+    __syncthreads();
+    for (int run = 0; run < groups && slot0 < span.len; ++run, slot0 += stride) {
+        uint4 kf[1][2][STEPS];
+        weigh_values<DH>(kf[0], next);
+        if (run + 1 < groups) weigh_load<DH>(next, cache, head, slot0 + stride, span.len, c, g);
         const int my0 = slot0 + 8 * g;
-        // the first query that sees any of these slots
-        const int first_row = max(0, slot0 - (span.len - span.count)) * group;
-        float sum[8] = {};
-        auto add = [&](const uint4 (&q)[STEPS], float2 ml, int sees) __attribute__((always_inline)) {
-            f32x4_t s[2];
+        float sum[1][8] = {};
+        // (from the first query that sees any of these slots on)
+        for (int tile = max(0, slot0 - (span.len - span.count)) * group / 16; tile * 16 < last_row; ++tile) {
+            uint4 q[STEPS];
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                s[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            for (int st = 0; st < STEPS; ++st) q[st] = sh_q[(tile * STEPS + st) * 64 + lane];
+            weigh_add<DH, 1, true>(sum, kf, q, sh_ml[tile * 16 + c], sh_sees[tile * 16 + c], my0, scale_log2e);
+        }
+        weigh_store(sum[0], cache.weight + head * cache.capacity, my0, span.len, c);
+    }
+}
+
+// More rows: a wave keeps 64 slots' keys, and the workgroup brings the queries to LDS 32 rows at a time, the next ones on
+// their way meanwhile (from memory every wave would read all of them: 512 rows of 4 x 32 heads over 2624 slots 171 us).
+constexpr int WEIGH_CHUNK = 32;
+
+template <int DH>
+__global__ __launch_bounds__(WEIGH_WAVES * 64, 2) void weigh_many_kernel(CacheView cache, CacheAttention a, int group,
+                                                                      const float2* __restrict__ row_ml) {
+    constexpr int STEPS = DH / 32, UNITS = DH / 8, LD = WEIGH_CHUNK * UNITS / (WEIGH_WAVES * 64);   // 16-byte pieces
+    __shared__ uint4 sh_q[2][WEIGH_CHUNK / 16 * STEPS * 64];
+    __shared__ float2 sh_ml[2][WEIGH_CHUNK];
+    __shared__ int sh_sees[2][WEIGH_CHUNK];
+    const int h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, g = lane >> 4;
+    const Span span = sample_span(a, cache.capacity, b);
+    const int rows = a.n_q * group, wg0 = blockIdx.x * WEIGH_WAVES * 64, slot0 = wg0 + wave * 64;
+    if (wg0 >= span.len) return;
+    const size_t head = (size_t)b * cache.H_kv + h;
+    const float scale_log2e = a.scale * 1.4426950408889634f;
+    const int last_row = min(rows, span.count * group);
+    WeighKeys<DH> raw[2];
 #pragma unroll
-                for (int st = 0; st < STEPS; ++st) s[j] = mfma16(kf[j][st], q[st], s[j]);
-            }
+    for (int n = 0; n < 2; ++n) weigh_load<DH>(raw[n], cache, head, slot0 + 32 * n, span.len, c, g);
+    uint4 q_next[LD] = {};
+    float2 ml_next = make_float2(0.f, 0.f);
+    int sees_next = 0;
+    auto fetch = [&](int r0) __attribute__((always_inline)) {   // (behind the last row: that row again)
 #pragma unroll
-            for (int n = 0; n < 8; ++n) {
-                const float p = __builtin_amdgcn_exp2f(fmaf(s[n >> 2][n & 3], scale_log2e, ml.x)) * ml.y;
-                sum[n] += my0 + n < sees ? p : 0.f;
-            }
-        };
-        if constexpr (TILES > 0) {
-            for (int tile = first_row / 16; tile * 16 < last_row; ++tile) {
+        for (int i = 0; i < LD; ++i) {
+            const int id = i * WEIGH_WAVES * 64 + tid, r = min(r0 + id / UNITS, rows - 1), n = r / group;
+            q_next[i] = *reinterpret_cast<const uint4*>(a.q.p + b * a.q.sample + n * a.q.token +
+                                                        (h * group + r - n * group) * a.q.head + id % UNITS * 8);
+        }
+        if (tid < WEIGH_CHUNK) {
+            const int r = r0 + tid;
+            const float2 ml = row_ml[head * rows + min(r, rows - 1)];
+            ml_next = make_float2(-ml.x * scale_log2e, 1.f / ml.y);
+            sees_next = r < last_row ? seen_by(span, r / group) : 0;
+        }
+    };
+    auto put = [&](int stage) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < LD; ++i) {
+            // piece u of a row: the values of lane group u / STEPS in product step u % STEPS
+            const int id = i * WEIGH_WAVES * 64 + tid, r = id / UNITS, u = id % UNITS;
+            sh_q[stage][((r >> 4) * STEPS + u % STEPS) * 64 + u / STEPS * 16 + (r & 15)] = q_next[i];
+        }
+        if (tid < WEIGH_CHUNK) sh_ml[stage][tid] = ml_next, sh_sees[stage][tid] = sees_next;
+    };
+    // (from the first query that sees any of the workgroup's slots on)
+    const int first = max(0, wg0 - (span.len - span.count)) * group / 16 * 16;
+    fetch(first);
+    uint4 kf[2][2][STEPS];
+    float sum[2][8] = {};
+#pragma unroll
+    for (int n = 0; n < 2; ++n) weigh_values<DH>(kf[n], raw[n]);
+    int stage = 0;
+    for (int r0 = first; r0 < last_row; r0 += WEIGH_CHUNK, stage ^= 1) {
+        put(stage);
+        __syncthreads();                      // (the other stage has been read by all)
+        fetch(r0 + WEIGH_CHUNK);
+        const bool all = r0 + WEIGH_CHUNK <= last_row && slot0 + 64 <= seen_by(span, r0 / group);
+        auto tiles = [&](auto mask) __attribute__((always_inline)) {
+#pragma unroll
+            for (int tile = 0; tile < WEIGH_CHUNK / 16; ++tile) {
                 uint4 q[STEPS];
 #pragma unroll
-                for (int st = 0; st < STEPS; ++st) q[st] = sh_q[(tile * STEPS + st) * 64 + lane];
-                add(q, sh_ml[tile * 16 + c], sh_sees[tile * 16 + c]);
+                for (int st = 0; st < STEPS; ++st) q[st] = sh_q[stage][(tile * STEPS + st) * 64 + lane];
+                weigh_add<DH, 2, decltype(mask)::value>(sum, kf, q, sh_ml[stage][tile * 16 + c], sh_sees[stage][tile * 16 + c],
+                                                        slot0 + 8 * g, scale_log2e);
             }
-        } else {
-            Column ahead;
-            from_memory(ahead, first_row);
-            for (int r0 = first_row; r0 < last_row; r0 += 16) {
-                const Column x = ahead;
-                from_memory(ahead, r0 + 16);
-                add(x.q, make_float2(-x.ml.x * scale_log2e, 1.f / x.ml.y), x.sees);
-            }
-        }
-        // over the 16 columns of a group
-        float* w = cache.weight + head * cache.capacity + my0;
-#pragma unroll
-        for (int n = 0; n < 8; ++n) {
-            float x = sum[n];
-            x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x128, 0xf, 0xf, false));   // row_ror:8
-            x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x124, 0xf, 0xf, false));
-            x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x122, 0xf, 0xf, false));
-            x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x121, 0xf, 0xf, false));
-            sum[n] = x;
-        }
-        float mine = sum[0];
-#pragma unroll
-        for (int n = 1; n < 8; ++n) mine = c == n ? sum[n] : mine;
-        if (c < 8 && my0 + c < span.len) w[c] += mine;
+        };
+        if (all) tiles(std::false_type{});
+        else if (slot0 < span.len) tiles(std::true_type{});
     }
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+        if (slot0 + 32 * n < span.len)
+            weigh_store(sum[n], cache.weight + head * cache.capacity, slot0 + 32 * n + 8 * g, span.len, c);
 }
 
 // ---- host --------------------------------------------------------------------------------------------------------
@@ -1192,15 +1263,18 @@ int run_attention(const CacheView& c, const CacheAttention& a, const AttentionPl
         joined = row_ml;
     }
     if (a.accumulate) {
-        const int per = FEW_STEP * WEIGH_WAVES, runs = (a.max_len + per - 1) / per;
-        // (runs of 32 slots a wave: as many as leave four waves a SIMD)
-        const int64_t all = (int64_t)runs * c.H_kv * c.B;
-        const int groups = p.kind == SOME ? (int)std::max((int64_t)1, std::min((int64_t)8, all / (4 * device_cu_count()))) : 1;
-        const dim3 grid((runs + groups - 1) / groups, c.H_kv, c.B);
-        if (p.kind == SOME)
-            hipLaunchKernelGGL((weigh_kernel<DH, SOME_MOST>), grid, dim3(WEIGH_WAVES * 64), 0, st, c, a, p.group, groups, joined);
-        else
-            hipLaunchKernelGGL((weigh_kernel<DH, 0>), grid, dim3(WEIGH_WAVES * 64), 0, st, c, a, p.group, 1, joined);
+        if (p.kind == SOME) {
+            // (runs of 32 slots a wave: as many as leave four waves a SIMD)
+            const int per = FEW_STEP * WEIGH_WAVES, runs = (a.max_len + per - 1) / per;
+            const int64_t share = (int64_t)runs * c.H_kv * c.B / (4 * device_cu_count());
+            const int groups = (int)std::max((int64_t)1, std::min((int64_t)8, share));
+            hipLaunchKernelGGL((weigh_some_kernel<DH>), dim3((runs + groups - 1) / groups, c.H_kv, c.B), dim3(WEIGH_WAVES * 64), 0,
+                               st, c, a, p.group, groups, joined);
+        } else {
+            const int per = 64 * WEIGH_WAVES;
+            hipLaunchKernelGGL((weigh_many_kernel<DH>), dim3((a.max_len + per - 1) / per, c.H_kv, c.B), dim3(WEIGH_WAVES * 64), 0,
+                               st, c, a, p.group, joined);
+        }
         MVLA_HIP_CHECK(hipGetLastError());
     }
     return MVLA_OK;
