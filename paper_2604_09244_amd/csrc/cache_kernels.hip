@@ -164,58 +164,139 @@ int launch_cache_read(const CacheView& c, const int32_t* first, int n, bf16_t* k
 // ---- eviction ------------------------------------------------------------------------------------------------------
 // One workgroup per (key head, sample) finds which rows stay and where each slot of the budget takes its row from.
 // Rows are ordered by (stays whatever its weight, weight, lower slot): a 32-bit key with the flag on top, since the bits
-// of a float that is not negative are in its order.  The key of the last row that stays is found digit by digit (11, 11
-// and 10 bits) with a histogram in LDS; rows above it stay, of those equal to it the first ones.  A wave then owns a
-// contiguous run of slots and numbers free slots and late rows by ballots behind the counts of the waves before it.
-constexpr int EVICT_THREADS = 512, EVICT_WAVES = EVICT_THREADS / 64, EVICT_BINS = 2048;
+// of a float that is not negative are in its order.  The key of the last row that stays lies in one bin of a histogram
+// between the smallest and the largest key, which narrows down to the keys in that bin until they are few enough to be
+// compared, or all alike; rows above that key stay, of those equal to it the first ones.  A wave then owns a contiguous
+// run of slots and numbers free slots and late rows by ballots behind the counts of the waves before it.
+// Keys (and the free slots) are in LDS up to EVICT_LDS rows, else formed from memory again each time.  MOVE: the workgroup
+// copies its rows as well; where workgroups are few and rows many, evict_move_kernel does that with the whole chip.
+// Bound: a dozen rounds of the workgroup over LDS and barriers, then the rows' copy.
+constexpr int EVICT_THREADS = 512, EVICT_WAVES = EVICT_THREADS / 64, EVICT_BINS = 2048, EVICT_FEW = 128;
+constexpr int EVICT_LDS = 16384;
 
 __device__ __forceinline__ uint32_t evict_key(float w, int pos, int first_pos, int recent_from) {
     const uint32_t bits = w > 0.f ? __float_as_uint(w) : 0u;   // (negative, NaN: as if nothing had looked at the row)
     return bits | (pos < first_pos || pos >= recent_from ? 0x80000000u : 0u);
 }
 
-__global__ __launch_bounds__(EVICT_THREADS) void evict_select_kernel(CacheView c, const int32_t* __restrict__ len, int max_len,
-                                                                     int budget, int first_pos, const int32_t* __restrict__ recent_from,
-                                                                     int32_t* __restrict__ len_out,
-                                                                     int32_t* __restrict__ kept, int32_t* __restrict__ holes) {
+// 16 bytes of codes of a row, their scale byte, and its position or weight.  part: piece of the key row, then of the value
+// row (their first ones bring the position and the weight)
+struct EvictPiece {
+    uint4 codes;
+    uint8_t scale;
+    uint32_t more;
+};
+template <int DH>
+__device__ __forceinline__ EvictPiece evict_load(const CacheView& c, size_t row, uint32_t part) {
+    constexpr uint32_t CODES = DH / 32;                        // 16-byte pieces, and scale bytes, of a row
+    const bool keys = part < CODES;
+    const uint32_t piece = keys ? part : part - CODES;
+    EvictPiece x;
+    x.codes = reinterpret_cast<const uint4*>(keys ? c.k : c.v)[row * CODES + piece];
+    x.scale = (keys ? c.k_scale : c.v_scale)[row * CODES + piece];
+    x.more = 0;
+    if (piece == 0) x.more = keys ? (uint32_t)c.pos[row] : __float_as_uint(c.weight[row]);
+    return x;
+}
+template <int DH>
+__device__ __forceinline__ void evict_store(const CacheView& d, size_t row, uint32_t part, const EvictPiece& x) {
+    constexpr uint32_t CODES = DH / 32;
+    const bool keys = part < CODES;
+    const uint32_t piece = keys ? part : part - CODES;
+    reinterpret_cast<uint4*>(keys ? d.k : d.v)[row * CODES + piece] = x.codes;
+    (keys ? d.k_scale : d.v_scale)[row * CODES + piece] = x.scale;
+    if (piece == 0) {
+        if (keys) d.pos[row] = (int32_t)x.more;
+        else d.weight[row] = __uint_as_float(x.more);
+    }
+}
+
+template <bool IN_LDS, int MOVE_DH>
+__global__ __launch_bounds__(EVICT_THREADS) void evict_select_kernel(CacheView c, CacheView d, const int32_t* __restrict__ len,
+                                                                     int max_len, int budget, int first_pos,
+                                                                     const int32_t* __restrict__ recent_from,
+                                                                     int32_t* __restrict__ len_out, int32_t* __restrict__ kept,
+                                                                     int32_t* __restrict__ holes, int in_place) {
+    extern __shared__ uint32_t lds_rows[];                     // (IN_LDS) keys [max_len], free slots [min(budget, max_len)]
     __shared__ uint32_t hist[EVICT_BINS];
-    __shared__ uint32_t wave_sum[EVICT_WAVES];
-    __shared__ uint32_t found[2];
+    __shared__ uint32_t wave_sum[EVICT_WAVES], few[EVICT_FEW];
+    __shared__ uint32_t found[2], range[2], n_few;
     const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int n = min(max(len[b], 0), max_len), nb = min(n, budget);
-    const size_t row0 = ((size_t)b * c.H_kv + h) * c.capacity;
+    const size_t head = (size_t)b * c.H_kv + h, row0 = head * c.capacity;
     const float* w = c.weight + row0;
     const int32_t* p = c.pos + row0;
-    int32_t* out = kept + ((size_t)b * c.H_kv + h) * budget;
-    int32_t* hole = holes + ((size_t)b * c.H_kv + h) * min(budget, max_len);
+    int32_t* out = kept + head * budget;
+    int32_t* hole_mem = holes + head * min(budget, max_len);
     const int recent = recent_from ? recent_from[b] : 0x7fffffff;
     if (h == 0 && tid == 0) len_out[b] = nb;
+    auto move_rows = [&]() {
+        if constexpr (MOVE_DH > 0) {
+            constexpr uint32_t LANES = 2 * MOVE_DH / 32, AHEAD = 4;
+            const uint32_t all = (uint32_t)nb * LANES;
+            for (uint32_t id0 = tid; id0 < all; id0 += AHEAD * EVICT_THREADS) {
+                int src[AHEAD];
+                EvictPiece x[AHEAD];
+#pragma unroll
+                for (uint32_t q = 0; q < AHEAD; ++q) {
+                    const uint32_t id = id0 + q * EVICT_THREADS, i = id / LANES;
+                    src[q] = id < all ? n <= budget ? (int)i : out[i] : -1;
+                    if (in_place && src[q] == (int)i) src[q] = -1;
+                }
+#pragma unroll
+                for (uint32_t q = 0; q < AHEAD; ++q)
+                    if (src[q] >= 0) x[q] = evict_load<MOVE_DH>(c, row0 + src[q], (id0 + q * EVICT_THREADS) % LANES);
+#pragma unroll
+                for (uint32_t q = 0; q < AHEAD; ++q) {
+                    const uint32_t id = id0 + q * EVICT_THREADS;
+                    if (src[q] >= 0) evict_store<MOVE_DH>(d, head * d.capacity + id / LANES, id % LANES, x[q]);
+                }
+            }
+        }
+    };
     if (n <= budget) {
         for (int i = tid; i < budget; i += EVICT_THREADS) out[i] = i < n ? i : -1;
+        if (!in_place) move_rows();
         return;
     }
+    auto key_of = [&](int i) __attribute__((always_inline)) {
+        if constexpr (IN_LDS) return lds_rows[i];
+        else return evict_key(w[i], p[i], first_pos, recent);
+    };
     // ---- key of the nb-th row
-    uint32_t prefix = 0, mask = 0, want = (uint32_t)nb;
-    const int shifts[3] = {21, 10, 0};
-#pragma unroll
-    for (int d = 0; d < 3; ++d) {
-        const int shift = shifts[d];
-        const uint32_t bins = d == 2 ? 1024u : 2048u;
+    uint32_t lo = 0xffffffffu, hi = 0;
+    for (int i = tid; i < n; i += EVICT_THREADS) {
+        const uint32_t key = evict_key(w[i], p[i], first_pos, recent);
+        if constexpr (IN_LDS) lds_rows[i] = key;
+        lo = min(lo, key), hi = max(hi, key);
+    }
+    uint32_t want = (uint32_t)nb, last;
+    for (;;) {
+        // smallest and largest of what is left, and their bins
+        if (tid == 0) range[0] = 0xffffffffu, range[1] = 0, n_few = 0;
         for (int i = tid; i < EVICT_BINS; i += EVICT_THREADS) hist[i] = 0;
+#pragma unroll
+        for (int o = 32; o; o >>= 1) lo = min(lo, (uint32_t)__shfl_xor((int)lo, o)), hi = max(hi, (uint32_t)__shfl_xor((int)hi, o));
         __syncthreads();
+        if (lane == 0) {
+            atomicMin(&range[0], lo);
+            atomicMax(&range[1], hi);
+        }
+        __syncthreads();
+        lo = range[0], hi = range[1];
+        last = lo;
+        if (lo == hi) break;                                   // (all alike: the first `want` of them stay)
+        const int bits = 32 - __clz((int)(hi - lo)), shift = bits > 11 ? bits - 11 : 0;
         for (int i = tid; i < n; i += EVICT_THREADS) {
-            const uint32_t key = evict_key(w[i], p[i], first_pos, recent);
-            if ((key & mask) == prefix) atomicAdd(&hist[(key >> shift) & (bins - 1)], 1u);
+            const uint32_t key = key_of(i);
+            if (key >= lo && key <= hi) atomicAdd(&hist[(key - lo) >> shift], 1u);
         }
         __syncthreads();
         // bins from the top, four a thread; the thread whose bins hold the want-th row says which
         uint32_t v[4], s = 0;
-        const int top = (int)bins - 1 - tid * 4;
+        const int top = EVICT_BINS - 1 - tid * 4;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            v[j] = top - j >= 0 ? hist[top - j] : 0u;
-            s += v[j];
-        }
+        for (int j = 0; j < 4; ++j) s += v[j] = hist[top - j];
         uint32_t inc = s;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
@@ -225,7 +306,8 @@ __global__ __launch_bounds__(EVICT_THREADS) void evict_select_kernel(CacheView c
         if (lane == 63) wave_sum[wave] = inc;
         __syncthreads();
         uint32_t before = inc - s;
-        for (int k = 0; k < wave; ++k) before += wave_sum[k];
+#pragma unroll
+        for (int k = 0; k < EVICT_WAVES; ++k) before += k < wave ? wave_sum[k] : 0;
         if (before < want && before + s >= want) {
             uint32_t left = want - before;
             int j = 0;
@@ -234,92 +316,148 @@ __global__ __launch_bounds__(EVICT_THREADS) void evict_select_kernel(CacheView c
             found[1] = left;
         }
         __syncthreads();
-        prefix |= found[0] << shift;
-        mask |= (bins - 1) << shift;
+        lo += found[0] << shift;
+        hi = shift ? min(hi, lo + ((1u << shift) - 1)) : lo;
         want = found[1];
+        last = lo;
+        if (shift == 0) break;
+        // few enough: the want-th largest of them by counting
+        uint32_t in_lo = 0xffffffffu, in_hi = 0;
+        for (int i = tid; i < n; i += EVICT_THREADS) {
+            const uint32_t key = key_of(i);
+            if (key >= lo && key <= hi) {
+                const uint32_t at = atomicAdd(&n_few, 1u);
+                if (at < EVICT_FEW) few[at] = key;
+                in_lo = min(in_lo, key), in_hi = max(in_hi, key);
+            }
+        }
+        __syncthreads();
+        const uint32_t m = n_few;
+        if (m <= EVICT_FEW) {
+            if (tid < (int)m) {
+                const uint32_t key = few[tid];
+                uint32_t above = 0, alike = 0;
+                for (uint32_t q = 0; q < m; ++q) above += few[q] > key ? 1 : 0, alike += few[q] == key ? 1 : 0;
+                if (above < want && above + alike >= want) found[0] = key, found[1] = want - above;   // (all of them the same)
+            }
+            __syncthreads();
+            last = found[0], want = found[1];
+            break;
+        }
+        lo = in_lo, hi = in_hi;
         __syncthreads();
     }
     // ---- of the rows with that key the first `want` stay
-    const int run = ((n + EVICT_WAVES - 1) / EVICT_WAVES + 63) / 64 * 64, lo = wave * run, hi = min(lo + run, n);
-    auto key_at = [&](int i) { return i < hi ? evict_key(w[i], p[i], first_pos, recent) : 0u; };
+    const int run = ((n + EVICT_WAVES - 1) / EVICT_WAVES + 63) / 64 * 64, run0 = wave * run, run1 = min(run0 + run, n);
     const uint64_t below = ((uint64_t)1 << lane) - 1;
     auto sum_before = [&](uint32_t mine) {
         __syncthreads();
         if (lane == 0) wave_sum[wave] = mine;
         __syncthreads();
         uint32_t s = 0;
-        for (int k = 0; k < wave; ++k) s += wave_sum[k];
+#pragma unroll
+        for (int k = 0; k < EVICT_WAVES; ++k) s += k < wave ? wave_sum[k] : 0;
         return s;
     };
     uint32_t eq = 0;
-    for (int i0 = lo; i0 < hi; i0 += 64) eq += (uint32_t)__popcll(__ballot(i0 + lane < hi && key_at(i0 + lane) == prefix));
+    for (int i0 = run0; i0 < run1; i0 += 64)
+        eq += (uint32_t)__popcll(__ballot(i0 + lane < run1 && key_of(min(i0 + lane, n - 1)) == last));
     const uint32_t eq0 = sum_before(eq);
-    // free slots within the budget, late rows beyond it
-    uint32_t n_hole = 0, n_late = 0, rank = eq0;
-    for (int i0 = lo; i0 < hi; i0 += 64) {
-        const int i = i0 + lane;
-        const uint32_t key = key_at(i);
-        const uint64_t ties = __ballot(i < hi && key == prefix);
-        const bool stays = i < hi && (key > prefix || (key == prefix && rank + (uint32_t)__popcll(ties & below) < want));
-        rank += (uint32_t)__popcll(ties);
-        n_hole += (uint32_t)__popcll(__ballot(i < nb && i < hi && !stays));
-        n_late += (uint32_t)__popcll(__ballot(i >= nb && stays));
-    }
-    uint32_t hole0 = sum_before(n_hole), late0 = sum_before(n_late);
-#pragma unroll
-    for (int phase = 0; phase < 2; ++phase) {
-        uint32_t at_hole = hole0, at_late = late0;
-        rank = eq0;
-        for (int i0 = lo; i0 < hi; i0 += 64) {
+    // calls f(slot, whether it is one, whether its row stays) for the wave's slots
+    auto each = [&](auto f) __attribute__((always_inline)) {
+        uint32_t rank = eq0;
+        for (int i0 = run0; i0 < run1; i0 += 64) {
             const int i = i0 + lane;
-            const uint32_t key = key_at(i);
-            const uint64_t ties = __ballot(i < hi && key == prefix);
-            const bool stays = i < hi && (key > prefix || (key == prefix && rank + (uint32_t)__popcll(ties & below) < want));
+            const bool there = i < run1;
+            const uint32_t key = key_of(min(i, n - 1));
+            const uint64_t ties = __ballot(there && key == last);
+            f(i, there, there && (key > last || (key == last && rank + (uint32_t)__popcll(ties & below) < want)));
             rank += (uint32_t)__popcll(ties);
-            if (phase == 0) {
-                const bool free_slot = i < nb && i < hi && !stays;
-                const uint64_t f = __ballot(free_slot);
-                if (free_slot) hole[at_hole + (uint32_t)__popcll(f & below)] = i;
-                if (i < nb && stays) out[i] = i;
-                at_hole += (uint32_t)__popcll(f);
-            } else {
-                const bool late = i >= nb && stays;
-                const uint64_t f = __ballot(late);
-                if (late) out[hole[at_late + (uint32_t)__popcll(f & below)]] = i;
-                at_late += (uint32_t)__popcll(f);
-            }
         }
+    };
+    // free slots within the budget, late rows beyond it
+    uint32_t n_hole = 0, n_late = 0;
+    each([&](int i, bool there, bool stays) {
+        n_hole += (uint32_t)__popcll(__ballot(there && i < nb && !stays));
+        n_late += (uint32_t)__popcll(__ballot(stays && i >= nb));
+    });
+    uint32_t hole_at = sum_before(n_hole), late_at = sum_before(n_late);
+    uint32_t* hole_lds = lds_rows + max_len;
+    each([&](int i, bool there, bool stays) {
+        const bool free_slot = there && i < nb && !stays;
+        const uint64_t f = __ballot(free_slot);
+        if (free_slot) {
+            const uint32_t at = hole_at + (uint32_t)__popcll(f & below);
+            if constexpr (IN_LDS) hole_lds[at] = (uint32_t)i;
+            else hole_mem[at] = i;
+        }
+        if (stays && i < nb) out[i] = i;
+        hole_at += (uint32_t)__popcll(f);
+    });
+    __syncthreads();
+    each([&](int i, bool, bool stays) {
+        const bool late = stays && i >= nb;
+        const uint64_t f = __ballot(late);
+        if (late) {
+            const uint32_t at = late_at + (uint32_t)__popcll(f & below);
+            if constexpr (IN_LDS) out[hole_lds[at]] = i;
+            else out[hole_mem[at]] = i;
+        }
+        late_at += (uint32_t)__popcll(f);
+    });
+    if constexpr (MOVE_DH > 0) {
         __syncthreads();
+        move_rows();
     }
 }
 
-// Rows to their slots: 16 bytes of codes a lane.  In place only rows from beyond the budget move, into slots within it:
-// no row that is read is written.
+// Rows to their slots, over the whole chip.  In place only rows from beyond the budget move, into slots within it: no row
+// that is read is written.
 template <int DH>
 __global__ __launch_bounds__(256) void evict_move_kernel(CacheView c, CacheView d, const int32_t* __restrict__ kept, int budget,
                                                          int in_place) {
-    constexpr int CODES = DH / 32, LANES = 2 * CODES;     // 16-byte pieces of a key (or value) row; lanes a row
+    constexpr uint32_t LANES = 2 * DH / 32;
     const int h = blockIdx.y, b = blockIdx.z;
-    const uint32_t id = blockIdx.x * 256 + threadIdx.x, part = id % LANES, i = id / LANES;
+    const uint32_t id = blockIdx.x * 256 + threadIdx.x, i = id / LANES;
     if (i >= (uint32_t)budget) return;
     const size_t head = (size_t)b * c.H_kv + h;
     const int src = kept[head * budget + i];
     if (src < 0 || (in_place && src == (int)i)) return;
-    const size_t from = head * c.capacity + src, to = head * d.capacity + i;
-    const bool keys = part < CODES;
-    const uint32_t piece = keys ? part : part - CODES;
-    reinterpret_cast<uint4*>(keys ? d.k : d.v)[to * CODES + piece] =
-        reinterpret_cast<const uint4*>(keys ? c.k : c.v)[from * CODES + piece];
-    (keys ? d.k_scale : d.v_scale)[to * CODES + piece] = (keys ? c.k_scale : c.v_scale)[from * CODES + piece];
-    if (part == 0) d.pos[to] = c.pos[from];
-    if (part == CODES) d.weight[to] = c.weight[from];
+    evict_store<DH>(d, head * d.capacity + i, id % LANES, evict_load<DH>(c, head * c.capacity + src, id % LANES));
+}
+
+template <bool IN_LDS, int MOVE_DH>
+static int evict_select(const CacheView& c, const CacheView& d, const int32_t* len, int max_len, int budget, int first_pos,
+                        const int32_t* recent_from, int32_t* len_out, int32_t* kept, int32_t* holes, hipStream_t st) {
+    static bool lds_set[kMaxDevices] = {};
+    int dev = 0;   // (the dynamic-LDS limit is raised once per device)
+    MVLA_HIP_CHECK(hipGetDevice(&dev));
+    if (IN_LDS && (dev < 0 || dev >= kMaxDevices || !lds_set[dev])) {
+        MVLA_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void*>(&evict_select_kernel<IN_LDS, MOVE_DH>),
+                                           hipFuncAttributeMaxDynamicSharedMemorySize, 2 * EVICT_LDS * 4));
+        if (dev >= 0 && dev < kMaxDevices) lds_set[dev] = true;
+    }
+    const size_t lds = IN_LDS ? (size_t)(max_len + (budget < max_len ? budget : max_len)) * 4 : 0;
+    hipLaunchKernelGGL((evict_select_kernel<IN_LDS, MOVE_DH>), dim3(c.H_kv, c.B), dim3(EVICT_THREADS), lds, st, c, d, len, max_len,
+                       budget, first_pos, recent_from, len_out, kept, holes, c.k == d.k);
+    MVLA_HIP_CHECK(hipGetLastError());
+    return MVLA_OK;
+}
+
+// Rows of a workgroup that it copies itself: all while there are workgroups for the chip, a few hundred otherwise.
+static bool evict_moves(const CacheView& c, int budget, int max_len) {
+    const int rows = budget < max_len ? budget : max_len;
+    return c.B * c.H_kv >= device_cu_count() || rows <= 512;
 }
 
 int launch_cache_evict(const CacheView& c, const CacheView& d, const int32_t* len, int max_len, int budget, int first_pos,
                        const int32_t* recent_from, int32_t* len_out, int32_t* kept, int32_t* holes, hipStream_t st) {
-    hipLaunchKernelGGL(evict_select_kernel, dim3(c.H_kv, c.B), dim3(EVICT_THREADS), 0, st, c, len, max_len, budget, first_pos,
-                       recent_from, len_out, kept, holes);
-    MVLA_HIP_CHECK(hipGetLastError());
+    const bool move = evict_moves(c, budget, max_len);
+#define MVLA_EVICT(LDS, DH) evict_select<LDS, DH>(c, d, len, max_len, budget, first_pos, recent_from, len_out, kept, holes, st)
+    const int rc = max_len <= EVICT_LDS ? (!move ? MVLA_EVICT(true, 0) : c.dh == 128 ? MVLA_EVICT(true, 128) : MVLA_EVICT(true, 64))
+                                        : (!move ? MVLA_EVICT(false, 0) : c.dh == 128 ? MVLA_EVICT(false, 128) : MVLA_EVICT(false, 64));
+#undef MVLA_EVICT
+    if (rc || move) return rc;
     const unsigned blocks = (unsigned)(((uint64_t)budget * (c.dh / 16) + 255) / 256);
     const dim3 grid(blocks, c.H_kv, c.B);
     if (c.dh == 128)
