@@ -497,8 +497,8 @@ typedef struct {
 
 /* Bytes of a context's workspace that the calls below need for caches of B samples, H
  * query and H_kv key heads of dh values, up to n_q queries a call and max_length slots
- * (not less than mvla_create asks for).  A context that runs layers as well takes the
- * larger of this and mvla_workspace_bytes.  0 for arguments that no call takes. */
+ * (not less than mvla_create asks for).  A context that runs other calls as well takes
+ * the largest of their needs.  0 for arguments that no call takes. */
 size_t mvla_cache_workspace_bytes(int B, int H, int H_kv, int dh, int n_q, int max_length);
 
 /* Write new key and value rows into a cache: row i < c_b of sample b goes to slot
@@ -556,6 +556,35 @@ int mvla_cache_attention(mvla_ctx* ctx, const mvla_cache4* cache, const mvla_row
 int mvla_cache_evict(mvla_ctx* ctx, const mvla_cache4* src, const mvla_cache4* dst,
                      const int32_t* length, int max_length, int budget, int first_pos,
                      const int32_t* recent_from, int32_t* length_out, int32_t* kept);
+
+/* mvla_prefill with the keys and values of every layer left in caches: layer l's go to
+ * the first slots of caches[l] (HOST array of n_layers descriptors, each with H_kv = H,
+ * the layer's dh and B, and room for the rows that the layer runs on: S up to layer p - 1
+ * and at a cold start, k_total + n_text behind the pruning step), with the rows'
+ * positions and weight 0.  Same results as mvla_prefill. */
+int mvla_prefill_cached(mvla_ctx* ctx, const mvla_layer_cfg* cfg, const mvla_layer_weights* layers,
+                        const mvla_prefill_desc* desc, const void* x, const int32_t* pos,
+                        const float* key_bias, const mvla_prefill_buffers* buffers,
+                        const mvla_cache4* caches, void** y_out, int* rows_out);
+
+/* Bytes of workspace for mvla_decode_step on n tokens of B samples over caches of up to
+ * max_length slots, and for mvla_cache_evict on them.  0 for arguments that it refuses. */
+size_t mvla_decode_workspace_bytes(int B, int n, int D, int H, int F, int max_length);
+
+/* The layers on n new tokens a sample, in order: norm, q/k/v projection with rotation by
+ * pos, mvla_cache_append, mvla_cache_attention over the cache (the new rows included, as
+ * the cache holds them; scale 1/sqrt(dh)), output projection, MLP.
+ * caches: HOST array of n_layers descriptors (H_kv = H).  x: device bf16 [B, n, D]; pos:
+ * device int32 [B, n], below rope_len; n_new: device int32 [B] or NULL (n).
+ * length: device int32 [n_layers, B], the layers' lengths, new rows counted.
+ * max_length, accumulate: as mvla_cache_attention; a layer whose cache has fewer slots
+ * takes its capacity.
+ * h: HOST array of two device buffers bf16 [B, n, D], disjoint from x; *y_out (host): the
+ * one that holds the last layer's output.  Rows i >= n_new[b] of it mean nothing. */
+int mvla_decode_step(mvla_ctx* ctx, const mvla_layer_cfg* cfg, const mvla_layer_weights* layers,
+                     const mvla_cache4* caches, int n_layers, const void* x, const int32_t* pos, int B,
+                     int n, const int32_t* n_new, const int32_t* length, int max_length,
+                     int accumulate, void* const* h, void** y_out);
 
 /* Choose the next token of each row of logits.  The tokens in descending order (equal
  * logits: lower index first), weights w = exp((x - max) / temperature):

@@ -28,7 +28,7 @@ EXPORTS = [
     "mvla_prefill_layer_prune", "mvla_tune_layers", "mvla_tuned_choice",
     "mvla_set_gemm_choice", "mvla_prefill", "mvla_peak_probe", "mvla_salience_noalloc", "mvla_masked_prefill_step",
     "mvla_cache_workspace_bytes", "mvla_cache_append", "mvla_cache_read", "mvla_cache_attention",
-    "mvla_cache_evict", "mvla_sample",
+    "mvla_cache_evict", "mvla_sample", "mvla_prefill_cached", "mvla_decode_workspace_bytes", "mvla_decode_step",
 ]
 
 
@@ -174,6 +174,13 @@ def load() -> C.CDLL:
     lib.mvla_cache_read.argtypes = [vp, cache, vp, i, vp, vp]
     lib.mvla_cache_attention.argtypes = [vp, cache, rows, i, i, vp, vp, i, f, i, rows]
     lib.mvla_cache_evict.argtypes = [vp, cache, cache, vp, i, i, i, vp, vp, vp]
+    lib.mvla_prefill_cached.argtypes = [vp, C.POINTER(LayerCfg), C.POINTER(LayerWeightsC),
+                                        C.POINTER(PrefillDesc), vp, vp, vp, C.POINTER(PrefillBuffers),
+                                        cache, C.POINTER(vp), C.POINTER(i)]
+    lib.mvla_decode_workspace_bytes.restype = C.c_size_t
+    lib.mvla_decode_workspace_bytes.argtypes = [i] * 6
+    lib.mvla_decode_step.argtypes = [vp, C.POINTER(LayerCfg), C.POINTER(LayerWeightsC), cache, i, vp,
+                                     vp, i, i, vp, vp, i, i, C.POINTER(vp), C.POINTER(vp)]
     lib.mvla_sample.argtypes = [vp, vp, i, C.c_int64, i, i, vp, vp, vp, vp, vp, vp, vp]
     lib.mvla_profile_enable.argtypes = [vp, C.c_uint32, i]
     lib.mvla_profile_read.argtypes = [vp, i, vp, vp, vp, vp]
@@ -240,7 +247,7 @@ class Cache4:
         assert _dev(pos, torch.int32).shape == _dev(weight, torch.float32).shape == (B, H, cap)
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.pos, self.weight = pos, weight
-        self.B, self.H_kv, self.dh, self.capacity = B, H, dh, cap
+        self.B, self.H_kv, self.dh, self.capacity, self.device = B, H, dh, cap, k.device
         self._c = Cache4C(B, H, dh, cap, k.data_ptr(), v.data_ptr(), k_scale.data_ptr(),
                           v_scale.data_ptr(), pos.data_ptr(), weight.data_ptr())
         self._ref = C.byref(self._c)
@@ -577,9 +584,12 @@ class Context:
         """Rows first[b] .. first[b] + n - 1 (first None: from 0) as bf16 (k, v) [B, H_kv, n, dh]."""
         assert first is None or _dev(first, torch.int32).shape == (cache.B,)
         shape = (cache.B, cache.H_kv, n, cache.dh)
-        k, v = out if out is not None else (
-            torch.empty(shape, dtype=torch.bfloat16, device=cache.k.device) for _ in range(2))
-        assert _dev(k, torch.bfloat16).shape == _dev(v, torch.bfloat16).shape == shape
+        if out is None:
+            k = torch.empty(shape, dtype=torch.bfloat16, device=cache.device)
+            v = torch.empty(shape, dtype=torch.bfloat16, device=cache.device)
+        else:
+            k, v = out
+            assert _dev(k, torch.bfloat16).shape == _dev(v, torch.bfloat16).shape == shape
         _check(load().mvla_cache_read(self._h, cache._ref, _ptr(first), n, k.data_ptr(),
                                       v.data_ptr()), "mvla_cache_read")
         return k, v
@@ -595,8 +605,9 @@ class Context:
         assert (B, dh) == (cache.B, cache.dh) and _dev(length, torch.int32).shape == (B,)
         assert n_new is None or _dev(n_new, torch.int32).shape == (B,)
         if out is None:
-            out = torch.empty(B, n_q, H, dh, dtype=torch.bfloat16, device=q.device)
-        assert out.shape == q.shape
+            out = torch.empty(B, n_q, H, dh, dtype=torch.bfloat16, device=cache.device)
+        else:
+            assert out.shape == q.shape
         _check(load().mvla_cache_attention(self._h, cache._ref, C.byref(_rows(q)), H, n_q,
                                            _ptr(n_new), length.data_ptr(),
                                            cache.capacity if max_length is None else max_length,
@@ -614,11 +625,13 @@ class Context:
         B = src.B
         assert _dev(length, torch.int32).shape == (B,)
         assert recent_from is None or _dev(recent_from, torch.int32).shape == (B,)
-        kept, new = out if out is not None else (
-            torch.empty(B, src.H_kv, budget, dtype=torch.int32, device=length.device),
-            torch.empty(B, dtype=torch.int32, device=length.device))
-        assert _dev(kept, torch.int32).shape == (B, src.H_kv, budget)
-        assert _dev(new, torch.int32).shape == (B,)
+        if out is None:
+            kept = torch.empty(B, src.H_kv, budget, dtype=torch.int32, device=src.device)
+            new = torch.empty(B, dtype=torch.int32, device=src.device)
+        else:
+            kept, new = out
+            assert _dev(kept, torch.int32).shape == (B, src.H_kv, budget)
+            assert _dev(new, torch.int32).shape == (B,)
         _check(load().mvla_cache_evict(self._h, src._ref, dst._ref, length.data_ptr(),
                                        src.capacity if max_length is None else max_length, budget,
                                        first_pos, _ptr(recent_from), new.data_ptr(),
@@ -639,9 +652,13 @@ class Context:
         for t, dt in ((u, torch.float32), (temperature, torch.float32), (top_k, torch.int32),
                       (top_p, torch.float32), (min_p, torch.float32)):
             assert t is None or _dev(t, dt).shape == (B,)
-        token, prob = out if out is not None else (
-            torch.empty(B, dtype=torch.int32, device=logits.device),
-            torch.empty(B, dtype=torch.float32, device=logits.device))
+        if out is None:
+            token = torch.empty(B, dtype=torch.int32, device=logits.device)
+            prob = torch.empty(B, dtype=torch.float32, device=logits.device)
+        else:
+            token, prob = out
+            assert _dev(token, torch.int32).shape == (B,)
+            assert prob is None or _dev(prob, torch.float32).shape == (B,)
         _check(load().mvla_sample(self._h, logits.data_ptr(), int(half), logits.stride(0), B, V,
                                   _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p),
                                   u.data_ptr(), token.data_ptr(), _ptr(prob)), "mvla_sample")
@@ -707,14 +724,15 @@ class PrefillPlan:
 
     def run(self, x: torch.Tensor, pos: torch.Tensor, key_bias: Optional[torch.Tensor] = None,
             fused_prune: bool = True, smooth_step: int = 0, smooth_k: int = 7,
-            smooth_beta: float = 0.85, on_the_fly: bool = False):
+            smooth_beta: float = 0.85, on_the_fly: bool = False, caches=None):
         """Pruned prefill: p full layers, pruning step, L-p layers on kept tokens -- one call
         of mvla_prefill, which does the sequencing.
 
         smooth_step > 0 turns on the action-iteration smoothing of the salience: the call is
         timestep ``smooth_step`` (1-based) of an episode; step 1 is the cold start and returns
         the unpruned prefill, later steps select on the smoothed salience.  ``on_the_fly``
-        reduces the scoring rows inside the scoring kernel (no probability tensor)."""
+        reduces the scoring rows inside the scoring kernel (no probability tensor).  ``caches``
+        (an array of Cache4C, one a layer) takes every layer's keys and values."""
         _dev(x, torch.bfloat16)
         _dev(pos, torch.int32)
         if key_bias is not None:
@@ -723,10 +741,14 @@ class PrefillPlan:
                         smooth_step, smooth_k, smooth_beta, 0 if on_the_fly else 1,
                         0 if fused_prune else 1)
         y_ptr, rows = C.c_void_p(), C.c_int()
-        _check(load().mvla_prefill(self.ctx.handle, C.byref(self.cfg), self._layer_array,
-                                   C.byref(d), x.data_ptr(), pos.data_ptr(), _ptr(key_bias),
-                                   C.byref(self._buffers), C.byref(y_ptr), C.byref(rows)),
-               "mvla_prefill")
+        args = (self.ctx.handle, C.byref(self.cfg), self._layer_array, C.byref(d), x.data_ptr(),
+                pos.data_ptr(), _ptr(key_bias), C.byref(self._buffers))
+        if caches is None:
+            _check(load().mvla_prefill(*args, C.byref(y_ptr), C.byref(rows)), "mvla_prefill")
+        else:
+            assert len(caches) == self.L
+            _check(load().mvla_prefill_cached(*args, caches, C.byref(y_ptr), C.byref(rows)),
+                   "mvla_prefill_cached")
         for t in self.h_kept + self.h_full:          # which of the plan's tensors holds the result
             if t.data_ptr() == y_ptr.value:
                 assert t.shape[1] == rows.value

@@ -1,5 +1,6 @@
 // C ABI of the pruned-prefill library: argument validation, workspace carving
 // and launch sequencing.  No computation happens on the host.
+#include <math.h>
 #include <new>
 
 #include "common.h"
@@ -413,6 +414,69 @@ int mvla_rope_table(mvla_ctx* ctx, double base, int rope_len, int dh, float* cos
     return MVLA_OK;
 }
 
+namespace {
+
+constexpr int kMaxGrid = 65535;   // of the second and third launch axes
+
+int check_cache(const mvla_cache4* c) {
+    if (!c || !c->k || !c->v || !c->k_scale || !c->v_scale || !c->pos || !c->weight) return MVLA_EINVAL;
+    if (c->B <= 0 || c->H_kv <= 0 || c->capacity <= 0 || c->capacity % 32 != 0) return MVLA_EINVAL;
+    if (c->dh != 64 && c->dh != 128) return MVLA_EUNSUPPORTED;
+    if (c->B > kMaxGrid || c->H_kv > kMaxGrid / 2) return MVLA_EUNSUPPORTED;
+    if (!aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->k_scale, 16) || !aligned(c->v_scale, 16) ||
+        !aligned(c->pos, 4) || !aligned(c->weight, 4))
+        return MVLA_EINVAL;
+    return MVLA_OK;
+}
+
+CacheView cache_view(const mvla_cache4& c) {
+    auto u8 = [](void* p) { return static_cast<uint8_t*>(p); };
+    return {u8(c.k), u8(c.v), u8(c.k_scale), u8(c.v_scale), c.pos, c.weight, c.B, c.H_kv, c.dh, c.capacity};
+}
+
+CacheRows cache_rows(const mvla_rows& r) {
+    return {static_cast<const bf16_t*>(r.data), r.sample, r.token, r.head, r.channel};
+}
+
+// whether two memory ranges touch
+bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+    const char *x = static_cast<const char*>(a), *y = static_cast<const char*>(b);
+    return x < y + nb && y < x + na;
+}
+
+bool caches_overlap(const mvla_cache4& a, const mvla_cache4& b) {
+    auto parts = [](const mvla_cache4& c, const void** p, size_t* n) {
+        const size_t rows = (size_t)c.B * c.H_kv * c.capacity;
+        const void* at[6] = {c.k, c.v, c.k_scale, c.v_scale, c.pos, c.weight};
+        const size_t bytes[6] = {(size_t)c.dh / 2, (size_t)c.dh / 2, (size_t)c.dh / 32, (size_t)c.dh / 32, 4, 4};
+        for (int i = 0; i < 6; ++i) p[i] = at[i], n[i] = rows * bytes[i];
+    };
+    const void *p[6], *q[6];
+    size_t n[6], m[6];
+    parts(a, p, n);
+    parts(b, q, m);
+    for (int i = 0; i < 6; ++i)
+        for (int j = 0; j < 6; ++j)
+            if (overlap(p[i], n[i], q[j], m[j])) return true;
+    return false;
+}
+
+bool same_cache(const mvla_cache4& a, const mvla_cache4& b) {
+    return a.k == b.k && a.v == b.v && a.k_scale == b.k_scale && a.v_scale == b.v_scale && a.pos == b.pos &&
+           a.weight == b.weight && a.B == b.B && a.H_kv == b.H_kv && a.dh == b.dh && a.capacity == b.capacity;
+}
+
+}  // namespace
+
+// The cache that a layer's new keys and values go to; over: and that its attention runs over (else over the rows of the
+// call itself).
+struct LayerCache {
+    const mvla_cache4* cache;
+    const int32_t *n_new, *length;   // length null: the cache is empty, the rows start it
+    int max_length, accumulate;
+    bool over;
+};
+
 // What the scoring rows of a layer are reduced to when the probabilities are not wanted:
 // the salience alone, or salience + budget + selection (kept_idx != null).
 struct ScoreReduce {
@@ -422,9 +486,22 @@ struct ScoreReduce {
     int32_t* kept_idx;
 };
 
+// (layer_bytes: what the layer itself takes of the scratch)
+static int check_layer_cache(const LayerCache& lc, int B, int n, int H, int dh, size_t layer_bytes, size_t scratch_bytes) {
+    if (int rc = check_cache(lc.cache)) return rc;
+    if (lc.cache->B != B || lc.cache->H_kv != H || lc.cache->dh != dh) return MVLA_EINVAL;
+    if ((uint64_t)n * H * (dh / 8) >= (uint64_t)1 << 31) return MVLA_EUNSUPPORTED;
+    if (!lc.over) return n <= lc.cache->capacity ? MVLA_OK : MVLA_EINVAL;
+    if (!lc.length || lc.max_length <= 0 || lc.max_length > lc.cache->capacity) return MVLA_EINVAL;
+    if (n > 128 * kMaxGrid) return MVLA_EUNSUPPORTED;
+    const size_t need = cache_attention_bytes(B, H, H, dh, n, lc.max_length, lc.accumulate != 0);
+    return align_up(layer_bytes, 256) + need <= scratch_bytes ? MVLA_OK : MVLA_ENOMEM;
+}
+
 static int run_layer(mvla_ctx* ctx, const mvla_layer_cfg* cfg, const mvla_layer_weights* w,
                      const void* x, const int32_t* pos, int B, int S, void* y, int n_query_tail,
-                     const float* key_bias, float* probs_out, const ScoreReduce* red, bool normed = false) {
+                     const float* key_bias, float* probs_out, const ScoreReduce* red, bool normed = false,
+                     const LayerCache* lc = nullptr) {
     int rc = check_layer_args(ctx, cfg, w, x, pos, B, S, n_query_tail,
                               red ? red->sal : probs_out, true);
     if (rc) return rc;
@@ -433,6 +510,7 @@ static int run_layer(mvla_ctx* ctx, const mvla_layer_cfg* cfg, const mvla_layer_
     if ((size_t)B * S > (size_t)INT32_MAX / 4) return MVLA_EUNSUPPORTED;
     const LayerBuffers lb = layer_buffers(ctx->scratch, B, S, D, F);
     if (lb.bytes > ctx->scratch_bytes) return MVLA_ENOMEM;
+    if (lc && (rc = check_layer_cache(*lc, B, S, H, dh, lb.bytes, ctx->scratch_bytes))) return rc;
     const int M = B * S;
     hipStream_t st = ctx->stream;
     const bf16_t* xin = static_cast<const bf16_t*>(x);
@@ -447,6 +525,12 @@ static int run_layer(mvla_ctx* ctx, const mvla_layer_cfg* cfg, const mvla_layer_
     TIMED(ctx, KID_GEMM_QKV, M,
           launch_gemm(lb.u, D, wqkv, M, 3 * D, D, lb.qkv, 3 * D, nullptr, 0, EPI_QKV_ROPE,
                       GEMM_WS(ctx), GEMM_PICK(ctx, M, 3 * D, D, EPI_QKV_ROPE), &rope, st));
+    if (lc) {
+        const int64_t row = 3 * (int64_t)D;
+        const CacheRows k = {lb.qkv + D, S * row, row, dh, 1}, v = {lb.vt, (int64_t)D * lb.S_pad, 1, (int64_t)dh * lb.S_pad, lb.S_pad};
+        TIMED(ctx, KID_CACHE_APPEND, M,
+              launch_cache_append(cache_view(*lc->cache), k, v, pos, S, lc->n_new, lc->length, st));
+    }
     if (n_query_tail > 0 && !red) {
         TIMED(ctx, KID_SCORE_PROBS, M,
               launch_score_probs(lb.qkv, 3 * D, false, lb.qkv + D, 3 * D, key_bias, B, S, H, dh,
@@ -480,8 +564,15 @@ static int run_layer(mvla_ctx* ctx, const mvla_layer_cfg* cfg, const mvla_layer_
                                   H * n_query_tail, st));
         }
     }
-    TIMED(ctx, KID_ATTENTION, M,
-          launch_attention(lb.qkv, lb.qkv + D, 3 * D, lb.vt, lb.S_pad, B, S, H, dh, lb.attn, D, st));
+    if (lc && lc->over) {
+        const CacheAttention a = {{lb.qkv, S * 3 * (int64_t)D, 3 * (int64_t)D, dh, 1}, {lb.attn, S * (int64_t)D, D, dh, 1},
+                                  lc->length, lc->n_new, H, S, lc->max_length, lc->accumulate, 1.0f / sqrtf((float)dh)};
+        TIMED(ctx, KID_CACHE_ATTENTION, M,
+              launch_cache_attention(cache_view(*lc->cache), a, ctx->scratch + align_up(lb.bytes, 256), st));
+    } else {
+        TIMED(ctx, KID_ATTENTION, M,
+              launch_attention(lb.qkv, lb.qkv + D, 3 * D, lb.vt, lb.S_pad, B, S, H, dh, lb.attn, D, st));
+    }
     TIMED(ctx, KID_GEMM_O, M,
           launch_gemm(lb.attn, D, static_cast<const bf16_t*>(w->wo), M, D, D, lb.x1, D, xin, D,
                       EPI_RES_BF16_TO_F32, GEMM_WS(ctx), GEMM_PICK(ctx, M, D, D, EPI_RES_BF16_TO_F32),
@@ -523,7 +614,7 @@ static int layer_prune(mvla_ctx* ctx, const mvla_layer_cfg* cfg, const mvla_laye
                        const void* x, const int32_t* pos, int B, int S, void* y, int n2, int n3,
                        int n_text, int k_total, int min2, int min3, const float* key_bias,
                        float* sal, int32_t* k2k3, int32_t* kept_idx, void* h_out,
-                       int32_t* pos_out, NextNorm* next) {
+                       int32_t* pos_out, NextNorm* next, const LayerCache* lc = nullptr) {
     if (!sal || !k2k3 || !kept_idx || !h_out || !pos_out || !y) return MVLA_EINVAL;
     if (n2 < 0 || n3 < 0 || n2 + n3 <= 0 || n_text <= 0 || (long)n2 + n3 + n_text != S)
         return MVLA_EINVAL;
@@ -539,7 +630,7 @@ static int layer_prune(mvla_ctx* ctx, const mvla_layer_cfg* cfg, const mvla_laye
         if (a < bb + nb && bb < a + na) return MVLA_EINVAL;
     }
     const ScoreReduce red{n2, n3, n_text, k_total, min2, min3, sal, k2k3, kept_idx};
-    int rc = run_layer(ctx, cfg, w, x, pos, B, S, y, n_text, key_bias, nullptr, &red);
+    int rc = run_layer(ctx, cfg, w, x, pos, B, S, y, n_text, key_bias, nullptr, &red, false, lc);
     if (rc) return rc;
     return compact_rows(ctx, y, pos, kept_idx, B, S, k_total + n_text, cfg->D, h_out, pos_out, next);
 }
@@ -553,11 +644,11 @@ int mvla_prefill_layer_prune(mvla_ctx* ctx, const mvla_layer_cfg* cfg, const mvl
                        h_out, pos_out, nullptr);
 }
 
-// The whole pruned prefill: sequencing only, every step is one of the calls above.
-int mvla_prefill(mvla_ctx* ctx, const mvla_layer_cfg* cfg, const mvla_layer_weights* layers,
-                 const mvla_prefill_desc* d, const void* x, const int32_t* pos,
-                 const float* key_bias, const mvla_prefill_buffers* buf, void** y_out,
-                 int* rows_out) {
+// The whole pruned prefill: sequencing only, every step is one of the calls above.  caches: one a layer, or null.
+static int prefill(mvla_ctx* ctx, const mvla_layer_cfg* cfg, const mvla_layer_weights* layers,
+                   const mvla_prefill_desc* d, const void* x, const int32_t* pos,
+                   const float* key_bias, const mvla_prefill_buffers* buf, const mvla_cache4* caches, void** y_out,
+                   int* rows_out) {
     if (!ctx || !cfg || !layers || !d || !x || !pos || !buf || !y_out || !rows_out)
         return MVLA_EINVAL;
     const int B = d->B, n2 = d->n2, n3 = d->n3, nt = d->n_text, L = d->n_layers, p = d->p;
@@ -591,6 +682,14 @@ int mvla_prefill(mvla_ctx* ctx, const mvla_layer_cfg* cfg, const mvla_layer_weig
     if (layer_buffers(nullptr, B, S, cfg->D, cfg->F).bytes > ctx->scratch_bytes ||
         salience_scratch_bytes(B, cfg->H, nt, n_vis) > ctx->scratch_bytes)
         return MVLA_ENOMEM;
+    LayerCache lc = {nullptr, nullptr, nullptr, 0, 0, false};
+    auto cache_of = [&](int l) -> const LayerCache* {
+        lc.cache = caches ? &caches[l] : nullptr;
+        return caches ? &lc : nullptr;
+    };
+    if (caches)
+        for (int l = 0; l < L; ++l)
+            if (int rc = check_layer_cache(*cache_of(l), B, cold || l < p ? S : S_kept, cfg->H, cfg->dh, 0, 0)) return rc;
 
     int rc;
     const void* h = x;
@@ -610,15 +709,15 @@ int mvla_prefill(mvla_ctx* ctx, const mvla_layer_cfg* cfg, const mvla_layer_weig
     for (int l = 0; l < p; ++l) {
         void* y = buf->h_full[l & 1];
         if (l < p - 1) {
-            rc = mvla_prefill_layer(ctx, cfg, &layers[l], h, pos, B, S, y, 0, nullptr, nullptr);
+            rc = run_layer(ctx, cfg, &layers[l], h, pos, B, S, y, 0, nullptr, nullptr, nullptr, false, cache_of(l));
         } else if (need_probs) {
-            rc = mvla_prefill_layer(ctx, cfg, &layers[l], h, pos, B, S, y, nt, key_bias, buf->probs);
+            rc = run_layer(ctx, cfg, &layers[l], h, pos, B, S, y, nt, key_bias, buf->probs, nullptr, false, cache_of(l));
         } else if (fused_layer && !cold) {
             rc = layer_prune(ctx, cfg, &layers[l], h, pos, B, S, y, n2, n3, nt, K, d->min2, d->min3, key_bias, buf->sal,
-                             buf->k2k3, buf->kept_idx, buf->h_kept[0], buf->pos_kept, norm);
+                             buf->k2k3, buf->kept_idx, buf->h_kept[0], buf->pos_kept, norm, cache_of(l));
         } else {
-            rc = mvla_prefill_layer_salience(ctx, cfg, &layers[l], h, pos, B, S, y, nt, key_bias,
-                                             n_vis, buf->sal);
+            const ScoreReduce red{n_vis, 0, 0, 0, 0, 0, buf->sal, nullptr, nullptr};
+            rc = run_layer(ctx, cfg, &layers[l], h, pos, B, S, y, nt, key_bias, nullptr, &red, false, cache_of(l));
         }
         if (rc) return rc;
         h = y;
@@ -658,7 +757,7 @@ int mvla_prefill(mvla_ctx* ctx, const mvla_layer_cfg* cfg, const mvla_layer_weig
     if (cold) {
         for (int l = p; l < L; ++l) {
             void* y = buf->h_full[l & 1];
-            rc = mvla_prefill_layer(ctx, cfg, &layers[l], h, pos, B, S, y, 0, nullptr, nullptr);
+            rc = run_layer(ctx, cfg, &layers[l], h, pos, B, S, y, 0, nullptr, nullptr, nullptr, false, cache_of(l));
             if (rc) return rc;
             h = y;
         }
@@ -670,13 +769,28 @@ int mvla_prefill(mvla_ctx* ctx, const mvla_layer_cfg* cfg, const mvla_layer_weig
     for (int l = p; l < L; ++l) {
         void* y = buf->h_kept[(l - p + 1) & 1];
         rc = run_layer(ctx, cfg, &layers[l], h, buf->pos_kept, B, S_kept, y, 0, nullptr, nullptr, nullptr,
-                       l == p && next.done);
+                       l == p && next.done, cache_of(l));
         if (rc) return rc;
         h = y;
     }
     *y_out = const_cast<void*>(h);
     *rows_out = S_kept;
     return MVLA_OK;
+}
+
+int mvla_prefill(mvla_ctx* ctx, const mvla_layer_cfg* cfg, const mvla_layer_weights* layers,
+                 const mvla_prefill_desc* d, const void* x, const int32_t* pos,
+                 const float* key_bias, const mvla_prefill_buffers* buf, void** y_out,
+                 int* rows_out) {
+    return prefill(ctx, cfg, layers, d, x, pos, key_bias, buf, nullptr, y_out, rows_out);
+}
+
+int mvla_prefill_cached(mvla_ctx* ctx, const mvla_layer_cfg* cfg, const mvla_layer_weights* layers,
+                        const mvla_prefill_desc* d, const void* x, const int32_t* pos,
+                        const float* key_bias, const mvla_prefill_buffers* buf, const mvla_cache4* caches, void** y_out,
+                        int* rows_out) {
+    if (!caches) return MVLA_EINVAL;
+    return prefill(ctx, cfg, layers, d, x, pos, key_bias, buf, caches, y_out, rows_out);
 }
 
 // One action-iteration step with the masks of Algorithm 1: sequencing only.
@@ -1013,60 +1127,6 @@ int mvla_score_only(mvla_ctx* ctx, const mvla_layer_cfg* cfg, const mvla_layer_w
 
 // ---------------------------------------------------------------------------
 // Answering: the 4-bit cache, attention over it, eviction, token choice
-namespace {
-
-constexpr int kMaxGrid = 65535;   // of the second and third launch axes
-
-int check_cache(const mvla_cache4* c) {
-    if (!c || !c->k || !c->v || !c->k_scale || !c->v_scale || !c->pos || !c->weight) return MVLA_EINVAL;
-    if (c->B <= 0 || c->H_kv <= 0 || c->capacity <= 0 || c->capacity % 32 != 0) return MVLA_EINVAL;
-    if (c->dh != 64 && c->dh != 128) return MVLA_EUNSUPPORTED;
-    if (c->B > kMaxGrid || c->H_kv > kMaxGrid / 2) return MVLA_EUNSUPPORTED;
-    if (!aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->k_scale, 16) || !aligned(c->v_scale, 16) ||
-        !aligned(c->pos, 4) || !aligned(c->weight, 4))
-        return MVLA_EINVAL;
-    return MVLA_OK;
-}
-
-CacheView cache_view(const mvla_cache4& c) {
-    auto u8 = [](void* p) { return static_cast<uint8_t*>(p); };
-    return {u8(c.k), u8(c.v), u8(c.k_scale), u8(c.v_scale), c.pos, c.weight, c.B, c.H_kv, c.dh, c.capacity};
-}
-
-CacheRows cache_rows(const mvla_rows& r) {
-    return {static_cast<const bf16_t*>(r.data), r.sample, r.token, r.head, r.channel};
-}
-
-// whether two memory ranges touch
-bool overlap(const void* a, size_t na, const void* b, size_t nb) {
-    const char *x = static_cast<const char*>(a), *y = static_cast<const char*>(b);
-    return x < y + nb && y < x + na;
-}
-
-bool caches_overlap(const mvla_cache4& a, const mvla_cache4& b) {
-    auto parts = [](const mvla_cache4& c, const void** p, size_t* n) {
-        const size_t rows = (size_t)c.B * c.H_kv * c.capacity;
-        const void* at[6] = {c.k, c.v, c.k_scale, c.v_scale, c.pos, c.weight};
-        const size_t bytes[6] = {(size_t)c.dh / 2, (size_t)c.dh / 2, (size_t)c.dh / 32, (size_t)c.dh / 32, 4, 4};
-        for (int i = 0; i < 6; ++i) p[i] = at[i], n[i] = rows * bytes[i];
-    };
-    const void *p[6], *q[6];
-    size_t n[6], m[6];
-    parts(a, p, n);
-    parts(b, q, m);
-    for (int i = 0; i < 6; ++i)
-        for (int j = 0; j < 6; ++j)
-            if (overlap(p[i], n[i], q[j], m[j])) return true;
-    return false;
-}
-
-bool same_cache(const mvla_cache4& a, const mvla_cache4& b) {
-    return a.k == b.k && a.v == b.v && a.k_scale == b.k_scale && a.v_scale == b.v_scale && a.pos == b.pos &&
-           a.weight == b.weight && a.B == b.B && a.H_kv == b.H_kv && a.dh == b.dh && a.capacity == b.capacity;
-}
-
-}  // namespace
-
 size_t mvla_cache_workspace_bytes(int B, int H, int H_kv, int dh, int n_q, int max_length) {
     if (B <= 0 || H <= 0 || H_kv <= 0 || H % H_kv != 0 || n_q <= 0 || max_length <= 0) return 0;
     if (dh != 64 && dh != 128) return 0;
@@ -1125,6 +1185,45 @@ int mvla_cache_attention(mvla_ctx* ctx, const mvla_cache4* cache, const mvla_row
     int rc;
     const CacheAttention a = {cache_rows(*q), cache_rows(*out), length, n_new, H, n_q, max_length, accumulate, scale};
     TIMED(ctx, KID_CACHE_ATTENTION, cache->B * n_q, launch_cache_attention(cache_view(*cache), a, ctx->scratch, ctx->stream));
+    return MVLA_OK;
+}
+
+size_t mvla_decode_workspace_bytes(int B, int n, int D, int H, int F, int max_length) {
+    if (B <= 0 || n <= 0 || D <= 0 || H <= 0 || F <= 0 || D % H != 0 || max_length <= 0) return 0;
+    if (D / H != 64 && D / H != 128) return 0;
+    const size_t over = align_up(layer_buffers(nullptr, B, n, D, F).bytes, 256) +
+                        cache_attention_bytes(B, H, H, D / H, n, max_length, true);
+    const size_t evict = (size_t)B * H * max_length * 4;
+    return kCounterBytes + gemm_partial_bytes() + align_up(over > evict ? over : evict, 256) + 256;
+}
+
+int mvla_decode_step(mvla_ctx* ctx, const mvla_layer_cfg* cfg, const mvla_layer_weights* layers,
+                     const mvla_cache4* caches, int n_layers, const void* x, const int32_t* pos, int B, int n,
+                     const int32_t* n_new, const int32_t* length, int max_length, int accumulate, void* const* h,
+                     void** y_out) {
+    if (!ctx || !cfg || !layers || !caches || !x || !pos || !length || !h || !h[0] || !h[1] || !y_out) return MVLA_EINVAL;
+    if (n_layers <= 0 || B <= 0 || n <= 0 || max_length <= 0) return MVLA_EINVAL;
+    auto layer_cache = [&](int l) -> LayerCache {
+        const int bound = max_length < caches[l].capacity ? max_length : caches[l].capacity;
+        return {&caches[l], n_new, length + (size_t)l * B, bound, accumulate, true};
+    };
+    for (int l = 0; l < n_layers; ++l) {      // everything is checked before the first launch
+        if (int rc = check_layer_args(ctx, cfg, &layers[l], x, pos, B, n, 0, nullptr, true)) return rc;
+        if ((size_t)B * n > (size_t)INT32_MAX / 4) return MVLA_EUNSUPPORTED;
+        const size_t layer = layer_buffers(nullptr, B, n, cfg->D, cfg->F).bytes;
+        if (int rc = check_layer_cache(layer_cache(l), B, n, cfg->H, cfg->dh, layer, ctx->scratch_bytes)) return rc;
+    }
+    const size_t bytes = (size_t)B * n * cfg->D * 2;
+    if (!aligned(h[0], 16) || !aligned(h[1], 16) || overlap(x, bytes, h[0], bytes) || overlap(x, bytes, h[1], bytes) ||
+        overlap(h[0], bytes, h[1], bytes))
+        return MVLA_EINVAL;
+    const void* in = x;
+    for (int l = 0; l < n_layers; ++l) {
+        const LayerCache lc = layer_cache(l);
+        if (int rc = run_layer(ctx, cfg, &layers[l], in, pos, B, n, h[l & 1], 0, nullptr, nullptr, nullptr, false, &lc)) return rc;
+        in = h[l & 1];
+    }
+    *y_out = const_cast<void*>(in);
     return MVLA_OK;
 }
 

@@ -13,13 +13,13 @@ __device__ __forceinline__ uint32_t max_magnitude(uint32_t m, uint32_t pair) {
     return __builtin_bit_cast(uint32_t, r);
 }
 
-// rows of one sample that an append writes: `count` of them from slot `first` on
+// rows of one sample that an append writes: `count` of them from slot `first` on (no lengths: the cache is empty)
 struct NewRows {
     int first, count;
 };
 __device__ __forceinline__ NewRows new_rows(const int32_t* len, const int32_t* n_new, int b, int n) {
     const int c = n_new ? min(max(n_new[b], 0), n) : n;
-    return {len[b] - c, c};
+    return {len ? len[b] - c : 0, c};
 }
 
 // ---- rows into the cache -----------------------------------------------------------------------------------------
