@@ -32,6 +32,7 @@ typedef unsigned long long u64;    // (as atomics take it)
 constexpr int SAMPLE_THREADS = 1024, SAMPLE_WAVES = SAMPLE_THREADS / 64;
 constexpr int SAMPLE_BINS = 1024;         // of octaves below the largest weight, and at most so many tiles
 constexpr int SAMPLE_LIST = 14336;        // tokens on the list: 112 of the 160 KiB of LDS
+constexpr int ONE_WORKGROUP = 32768;      // tokens of a row that one workgroup takes by itself
 constexpr int SLICE_THREADS = 256, SLICE_MAXIMA = 128;
 constexpr float SAMPLE_OCTAVES = 40.f;    // weights below 2^-40 of the largest count as none
 constexpr float LOWEST = -3.4028235e38f;  // (-inf never stays)
@@ -70,32 +71,37 @@ struct Row {                             // a row in pieces of 16 bytes from the
         tiles = (pieces + 64 * steps - 1) / (64 * steps);
     }
     __device__ __forceinline__ int first(int j) const { return j * VEC - off; }
-    // piece j; what lies outside the row is no number
-    __device__ __forceinline__ void load(int j, float (&x)[VEC]) const {
+    static __device__ __forceinline__ uint4 nothing() {
+        const uint32_t w = VEC == 8 ? 0x7fc07fc0u : 0x7fc00000u;
+        return make_uint4(w, w, w, w);
+    }
+    // piece j as it lies in memory; what lies outside the row is no number
+    __device__ __forceinline__ uint4 raw(int j) const {
         const int i0 = first(j);
-        if (i0 >= 0 && i0 + VEC <= V) {
-            const uint4 w = *reinterpret_cast<const uint4*>(p + (size_t)j * VEC);
-            if constexpr (VEC == 8) {
-                const uint32_t a[4] = {w.x, w.y, w.z, w.w};
+        if (i0 >= 0 && i0 + VEC <= V) return *reinterpret_cast<const uint4*>(p + (size_t)j * VEC);
+        uint4 w = nothing();
+        uint32_t a[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[2 * e] = __uint_as_float(a[e] << 16), x[2 * e + 1] = __uint_as_float(a[e] & 0xffff0000u);
-            } else {
-                x[0] = __uint_as_float(w.x), x[1] = __uint_as_float(w.y), x[2] = __uint_as_float(w.z), x[3] = __uint_as_float(w.w);
+        for (int e = 0; e < VEC; ++e)
+            if (i0 + e >= 0 && i0 + e < V) {
+                if constexpr (VEC == 8) a[e / 2] = (e & 1) ? (a[e / 2] & 0xffffu) | (uint32_t)p[j * VEC + e] << 16
+                                                           : (a[e / 2] & 0xffff0000u) | p[j * VEC + e];
+                else a[e] = __float_as_uint(p[j * VEC + e]);
             }
-        } else {
+        return make_uint4(a[0], a[1], a[2], a[3]);
+    }
+    __device__ __forceinline__ void values(const uint4& w, float (&x)[VEC]) const {
+        const uint32_t a[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                x[e] = NAN;
-                if (i0 + e >= 0 && i0 + e < V) {
-                    if constexpr (VEC == 8) x[e] = bf16_to_f32(p[j * VEC + e]);
-                    else x[e] = p[j * VEC + e];
-                }
-            }
+        for (int e = 0; e < 4; ++e) {
+            if constexpr (VEC == 8) x[2 * e] = __uint_as_float(a[e] << 16), x[2 * e + 1] = __uint_as_float(a[e] & 0xffff0000u);
+            else x[e] = __uint_as_float(a[e]);
         }
         if (endless)
 #pragma unroll
             for (int e = 0; e < VEC; ++e) x[e] = x[e] == INFINITY ? 0.f : NAN;
     }
+    __device__ __forceinline__ void load(int j, float (&x)[VEC]) const { values(raw(j), x); }
 };
 
 // sum over the lanes, in parts whose sums fit 32 bits
@@ -221,42 +227,49 @@ __device__ __forceinline__ void append_places(const float (&x)[VEC], const bool 
 }
 
 // ---- launches on slices of a row --------------------------------------------------------------------------------------
-// calls f(values, piece) for a wave's 64 pieces at a time of the tiles t0, t0 + stride, .. below t1 (no numbers where a piece
-// does not exist), done(tile) behind each tile; four loads on their way at a time
-template <typename T, typename F, typename G>
-__device__ __forceinline__ void walk_tiles(const Row<T>& row, int t0, int t1, int stride, F f, G done) {
-    constexpr int VEC = Row<T>::VEC, AHEAD = 4;
-    const int lane = threadIdx.x & 63;
-    int t = t0, q = 0;                       // the next to load
-    int t_done = t0, q_done = 0;             // the next to hand on
-    while (t_done < t1) {
-        float x[AHEAD][VEC];
-        int piece[AHEAD];
+// A wave's tiles t0, t0 + stride, .. below t1, 64 pieces at a time (no numbers where a piece does not exist): fetch() sends
+// AHEAD loads on their way, run() calls f(values, piece) for all pieces and done(tile) behind each tile.
+template <typename T, int AHEAD>
+struct TileWalk {
+    static constexpr int VEC = Row<T>::VEC;
+    int t1, stride, t, q = 0, t_done, q_done = 0;    // the next to load, and to hand on
+    uint4 held[AHEAD];
+    int piece[AHEAD];
+    __device__ __forceinline__ TileWalk(int t0, int t1_, int stride_) : t1(t1_), stride(stride_), t(t0), t_done(t0) {}
+    __device__ __forceinline__ void fetch(const Row<T>& row) {
+        const int lane = threadIdx.x & 63;
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
             piece[i] = t < t1 ? (t * row.steps + q) * 64 + lane : row.pieces;
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) x[i][e] = NAN;
-            if (piece[i] < row.pieces) row.load(piece[i], x[i]);
+            held[i] = piece[i] < row.pieces ? row.raw(piece[i]) : Row<T>::nothing();
             if (++q == row.steps) q = 0, t += stride;
         }
+    }
+    template <typename F, typename G>
+    __device__ __forceinline__ void run(const Row<T>& row, F f, G done) {      // (behind a fetch)
+        while (t_done < t1) {
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) {
-            if (t_done >= t1) break;
-            f(x[i], piece[i]);
-            if (++q_done == row.steps) {
-                done(t_done);
-                q_done = 0, t_done += stride;
+            for (int i = 0; i < AHEAD; ++i) {
+                if (t_done >= t1) break;
+                float x[VEC];
+                row.values(held[i], x);
+                f(x, piece[i]);
+                if (++q_done == row.steps) {
+                    done(t_done);
+                    q_done = 0, t_done += stride;
+                }
             }
+            if (t_done < t1) fetch(row);
         }
     }
-}
-// the same for a slice's waves
-template <typename T, typename F, typename G>
-__device__ __forceinline__ void slice_tiles(const Row<T>& row, int slice, int slices, F f, G done) {
-    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), per = (row.tiles + slices - 1) / slices;
-    walk_tiles<T>(row, slice * per + wave, min((slice + 1) * per, row.tiles), SLICE_THREADS / 64, f, done);
-}
+};
+// the same for a slice's waves; most slices are one fetch
+template <typename T>
+struct SliceWalk : TileWalk<T, 8> {
+    __device__ __forceinline__ SliceWalk(const Row<T>& row, int slice, int per)
+        : TileWalk<T, 8>(slice * per + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), min((slice + 1) * per, row.tiles),
+                         SLICE_THREADS / 64) {}
+};
 
 template <typename T>
 __global__ __launch_bounds__(SLICE_THREADS) void sample_max_kernel(const T* __restrict__ logits, int64_t stride, int V,
@@ -275,20 +288,17 @@ __global__ __launch_bounds__(SLICE_THREADS) void sample_max_kernel(const T* __re
     // (pieces of a slice side by side over the threads: the order within it is nobody's business here)
     const int per = (row.tiles + sc.slices - 1) / sc.slices * row.steps * 64, j1 = min((slice + 1) * per, row.pieces);
     int j = slice * per + tid;
-    for (; j + 3 * SLICE_THREADS < j1; j += 4 * SLICE_THREADS) {
-        float x[4][VEC];
+    for (; j < j1; j += 8 * SLICE_THREADS) {
+        uint4 w[8];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) row.load(j + q * SLICE_THREADS, x[q]);
+        for (int q = 0; q < 8; ++q) w[q] = j + q * SLICE_THREADS < j1 ? row.raw(j + q * SLICE_THREADS) : Row<T>::nothing();
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
+        for (int q = 0; q < 8; ++q) {
+            float x[VEC];
+            row.values(w[q], x);
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) m = fmaxf(m, x[q][e]);
-    }
-    for (; j < j1; j += SLICE_THREADS) {
-        float x[VEC];
-        row.load(j, x);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) m = fmaxf(m, x[e]);
+            for (int e = 0; e < VEC; ++e) m = fmaxf(m, x[e]);
+        }
     }
     m = fmaxf(m, __shfl_xor(m, 1));
     if ((tid & 1) == 0) sc.maxima[((size_t)b * sc.slices + slice) * SLICE_MAXIMA + (tid >> 1)] = m;
@@ -312,6 +322,8 @@ __global__ __launch_bounds__(SLICE_THREADS) void sample_collect_kernel(const T* 
     Settings s(b, V, temperature, top_k, top_p, min_p);
     const int n_max = sc.slices * SLICE_MAXIMA;
     const float* maxima = sc.maxima + (size_t)b * n_max;
+    SliceWalk<T> walk(row, slice, (row.tiles + sc.slices - 1) / sc.slices);
+    walk.fetch(row);
     float most = -INFINITY;
     for (int i = tid; i < n_max; i += SLICE_THREADS) most = fmaxf(most, maxima[i]);
     most = wave_max(most);
@@ -324,7 +336,7 @@ __global__ __launch_bounds__(SLICE_THREADS) void sample_collect_kernel(const T* 
     if (most == -INFINITY) return;
     auto nothing = [](int) {};
     if (s.greedy()) {
-        slice_tiles<T>(row, slice, sc.slices, [&](float (&x)[VEC], int j) {
+        walk.run(row, [&](float (&x)[VEC], int j) {
             uint32_t at = 0xffffffffu;
 #pragma unroll
             for (int e = VEC - 1; e >= 0; --e)
@@ -382,7 +394,7 @@ __global__ __launch_bounds__(SLICE_THREADS) void sample_collect_kernel(const T* 
         uint32_t* n = &sc.state[b].n_list;
         u64* places = sc.list + (size_t)b * SAMPLE_LIST;
         u64 total = 0, tile = 0;
-        slice_tiles<T>(row, slice, sc.slices, [&](float (&x)[VEC], int j) {
+        walk.run(row, [&](float (&x)[VEC], int j) {
             if (list) {
                 bool in[VEC];
 #pragma unroll
@@ -415,7 +427,7 @@ __global__ __launch_bounds__(SLICE_THREADS) void sample_collect_kernel(const T* 
         return;
     }
     // top_p alone
-    slice_tiles<T>(row, slice, sc.slices, [&](float (&x)[VEC], int) {
+    walk.run(row, [&](float (&x)[VEC], int) {
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
             const float oct = s.octaves(x[e]);
@@ -444,6 +456,8 @@ __global__ __launch_bounds__(SLICE_THREADS) void sample_window_kernel(const T* _
     if (!s.by_p || s.by_k || s.by_least || s.greedy() || most == -INFINITY) return;
     s.measure(most);
     Row<T> row(logits + b * stride, V);
+    SliceWalk<T> walk(row, slice, (row.tiles + sc.slices - 1) / sc.slices);
+    walk.fetch(row);
     row.endless = most == INFINITY;
     u64 mass[PER], mine = 0;
 #pragma unroll
@@ -475,7 +489,7 @@ __global__ __launch_bounds__(SLICE_THREADS) void sample_window_kernel(const T* _
         sc.state[b].window1 = last;
     }
     u64 all = 0, tile = 0;
-    slice_tiles<T>(row, slice, sc.slices, [&](float (&x)[VEC], int j) {
+    walk.run(row, [&](float (&x)[VEC], int j) {
         float sure = 0.f, any = 0.f;
         bool in[VEC];
 #pragma unroll
@@ -525,6 +539,12 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(const T* __restr
     const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     Row<T> row(logits + b * stride, V);
     Settings s(b, V, temperature, top_k, top_p, min_p);
+    // a row by itself: each thread's pieces stay in registers
+    constexpr int HELD = SPLIT ? 1 : ONE_WORKGROUP / (SAMPLE_THREADS * VEC);
+    uint4 held[HELD];
+    if constexpr (!SPLIT)
+#pragma unroll
+        for (int q = 0; q < HELD; ++q) held[q] = tid + q * SAMPLE_THREADS < row.pieces ? row.raw(tid + q * SAMPLE_THREADS) : Row<T>::nothing();
     const float r = u[b];
     if (tid == 0) n_list = 0, first_at = 0xffffffffu;
     bins[tid] = 0;
@@ -550,8 +570,25 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(const T* __restr
             f(j, x);
         }
     };
+    // the same where the registers hold the most of them
+    auto each_held = [&](auto f) __attribute__((always_inline)) {
+#pragma unroll
+        for (int q = 0; q < HELD; ++q) {
+            if (q * SAMPLE_THREADS >= row.pieces) break;
+            float x[VEC];
+            row.values(held[q], x);
+            f(tid + q * SAMPLE_THREADS, x);
+        }
+        for (int j = tid + HELD * SAMPLE_THREADS; j < row.pieces; j += SAMPLE_THREADS) {
+            float x[VEC];
+            row.load(j, x);
+            f(j, x);
+        }
+    };
     auto each_tile = [&](auto f, auto done) __attribute__((always_inline)) {
-        walk_tiles<T>(row, wave, row.tiles, SAMPLE_WAVES, f, done);
+        TileWalk<T, 4> walk(wave, row.tiles, SAMPLE_WAVES);
+        walk.fetch(row);
+        walk.run(row, f, done);
     };
     // sum of one number a wave over the workgroup
     auto all_waves = [&](u64 x) {
@@ -569,7 +606,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(const T* __restr
         most = sc.state[b].most;
         __syncthreads();
     } else {
-        each([&](int, float (&x)[VEC]) __attribute__((always_inline)) {
+        each_held([&](int, float (&x)[VEC]) __attribute__((always_inline)) {
 #pragma unroll
             for (int e = 0; e < VEC; ++e) mine = fmaxf(mine, x[e]);
         });
@@ -587,7 +624,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(const T* __restr
             if (tid == 0) choose((int)sc.state[b].first_at, 1.0);
         } else {
             if (mine == most)
-                each([&](int j, float (&x)[VEC]) __attribute__((always_inline)) {
+                each_held([&](int j, float (&x)[VEC]) __attribute__((always_inline)) {
 #pragma unroll
                     for (int e = VEC - 1; e >= 0; --e)
                         if (x[e] == most) atomicMin(&first_at, (uint32_t)(row.first(j) + e));
@@ -724,7 +761,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(const T* __restr
                 low = s.least_logit();
             }
             const bool sum = by_p && !by_k;
-            each([&](int j, float (&x)[VEC]) __attribute__((always_inline)) {
+            each_held([&](int j, float (&x)[VEC]) __attribute__((always_inline)) {
                 bool in[VEC];
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) in[e] = x[e] >= low;
@@ -1047,7 +1084,6 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(const T* __restr
 namespace {
 
 constexpr int SLICE_TOKENS = 16384;       // a slice at least; a row has at most 32
-constexpr int ONE_WORKGROUP = 32768;      // tokens of a row that one workgroup takes by itself
 
 // bytes of scratch a row, and where its parts lie for `rows` rows
 size_t sample_scratch(char* base, int rows, int slices, SampleScratch* sc) {
