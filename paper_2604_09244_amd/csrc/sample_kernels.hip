@@ -19,7 +19,7 @@
 // 2^-40 beyond, so that no sum depends on the order in which it was formed.
 //
 // Bound: arithmetic of some 10 to 30 operations a token (131072 of them keep one compute unit busy for 8 to 30 us a
-// pass).  Long rows are therefore dealt out over the chip, SLICE tokens a workgroup, in up to four launches; short ones
+// pass).  Long rows are therefore dealt out over the chip, SLICE tokens a workgroup, in three launches; short ones
 // take one workgroup and one launch.
 #include "common.h"
 #include "mfma.h"
@@ -34,6 +34,7 @@ constexpr int SAMPLE_BINS = 1024;         // of octaves below the largest weight
 constexpr int SAMPLE_LIST = 14336;        // tokens on the list: 112 of the 160 KiB of LDS
 constexpr int ONE_WORKGROUP = 32768;      // tokens of a row that one workgroup takes by itself
 constexpr int SLICE_THREADS = 256, SLICE_MAXIMA = 128;
+constexpr int SLICE_EACH = 12;            // tokens of a thread that come to its row's list together (24 KiB of LDS)
 constexpr float SAMPLE_OCTAVES = 40.f;    // weights below 2^-40 of the largest count as none
 constexpr float LOWEST = -3.4028235e38f;  // (-inf never stays)
 
@@ -149,6 +150,7 @@ struct Settings {
         by_least = min_p && min_p[b] > 0.f;
     }
     __device__ __forceinline__ bool greedy() const { return !(t > 0.f); }
+    __device__ __forceinline__ bool p_alone() const { return by_p && !by_k && !by_least && !greedy(); }
     __device__ __forceinline__ void measure(float most) {
         per_t = 1.4426950408889634f / t;
         ref = most == INFINITY ? 0.f : most;
@@ -165,11 +167,13 @@ struct Settings {
     static __device__ __forceinline__ u64 tallied(float oct) {
         return ((u64)1 << 32) + (uint32_t)(__builtin_amdgcn_fractf(oct * (SAMPLE_BINS / SAMPLE_OCTAVES)) * 64.f);
     }
+    static __device__ __forceinline__ float mean_weight(u64 tally, int bin) {
+        const float in = ((float)(uint32_t)tally / (float)(uint32_t)(tally >> 32) + 0.5f) * (1.f / 64.f);
+        return weight(((float)bin + in) * (SAMPLE_OCTAVES / SAMPLE_BINS));
+    }
     static __device__ __forceinline__ u64 about(u64 tally, int bin) {
         const uint32_t c = (uint32_t)(tally >> 32);
-        if (!c) return 0;
-        const float in = ((float)(uint32_t)tally / (float)c + 0.5f) * (1.f / 64.f);
-        return c * whole(weight(((float)bin + in) * (SAMPLE_OCTAVES / SAMPLE_BINS)));
+        return c ? c * whole(mean_weight(tally, bin)) : 0;
     }
     // where a running sum that is known so well has to be looked at for what reaches `want`
     static __device__ __forceinline__ u64 early(u64 want) { return want - (want >> 12); }
@@ -195,7 +199,8 @@ struct RowState {
 struct SampleScratch {
     RowState* state;              // [rows]
     float* maxima;                // [rows][slices * SLICE_MAXIMA]
-    u64* tally;                   // [rows][SAMPLE_BINS]
+    float* top;                   // [rows][slices] largest logit
+    float* mass;                  // [rows][slices][SAMPLE_BINS] weight up to bins below that, in units of its own (top_p alone)
     u64* tile_sum;                // [rows][SAMPLE_BINS]
     u64* total;                   // [rows][slices]
     u64* list;                    // [rows][SAMPLE_LIST]
@@ -225,86 +230,147 @@ __device__ __forceinline__ void append_places(const float (&x)[VEC], const bool 
         at += (uint32_t)__popcll(mask[e]);
     }
 }
+// Calls f(raw piece, its number) for held[0 .. N - 1], `COPIES` of them in one turn of a loop whose turns move the rest up:
+// code that runs once comes from memory, and eight copies of it cost more than the moves.
+template <int COPIES, int N, typename F>
+__device__ __forceinline__ void each_of(uint4 (&held)[N], F f) {
+#pragma unroll 1
+    for (int i = 0; i < N; i += COPIES) {
+#pragma unroll
+        for (int c = 0; c < COPIES; ++c) f(held[c], i + c);
+#pragma unroll
+        for (int c = 0; c + COPIES < N; ++c) held[c] = held[c + COPIES];
+    }
+}
 
 // ---- launches on slices of a row --------------------------------------------------------------------------------------
 // A wave's tiles t0, t0 + stride, .. below t1, 64 pieces at a time (no numbers where a piece does not exist): fetch() sends
 // AHEAD loads on their way, run() calls f(values, piece) for all pieces and done(tile) behind each tile.
-template <typename T, int AHEAD>
+template <typename T, int AHEAD, int COPIES>
 struct TileWalk {
     static constexpr int VEC = Row<T>::VEC;
     int t1, stride, t, q = 0, t_done, q_done = 0;    // the next to load, and to hand on
     uint4 held[AHEAD];
-    int piece[AHEAD];
     __device__ __forceinline__ TileWalk(int t0, int t1_, int stride_) : t1(t1_), stride(stride_), t(t0), t_done(t0) {}
     __device__ __forceinline__ void fetch(const Row<T>& row) {
-        const int lane = threadIdx.x & 63;
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
-            piece[i] = t < t1 ? (t * row.steps + q) * 64 + lane : row.pieces;
-            held[i] = piece[i] < row.pieces ? row.raw(piece[i]) : Row<T>::nothing();
+            const int piece = t < t1 ? (t * row.steps + q) * 64 + (int)(threadIdx.x & 63) : row.pieces;
+            held[i] = piece < row.pieces ? row.raw(piece) : Row<T>::nothing();
             if (++q == row.steps) q = 0, t += stride;
         }
     }
     template <typename F, typename G>
     __device__ __forceinline__ void run(const Row<T>& row, F f, G done) {      // (behind a fetch)
         while (t_done < t1) {
-#pragma unroll
-            for (int i = 0; i < AHEAD; ++i) {
-                if (t_done >= t1) break;
+            each_of<COPIES>(held, [&](const uint4& w, int) __attribute__((always_inline)) {
+                if (t_done >= t1) return;
                 float x[VEC];
-                row.values(held[i], x);
-                f(x, piece[i]);
+                row.values(w, x);
+                f(x, (t_done * row.steps + q_done) * 64 + (int)(threadIdx.x & 63));
                 if (++q_done == row.steps) {
                     done(t_done);
                     q_done = 0, t_done += stride;
                 }
-            }
+            });
             if (t_done < t1) fetch(row);
         }
     }
 };
 // the same for a slice's waves; most slices are one fetch
 template <typename T>
-struct SliceWalk : TileWalk<T, 8> {
+struct SliceWalk : TileWalk<T, 8, 2> {
     __device__ __forceinline__ SliceWalk(const Row<T>& row, int slice, int per)
-        : TileWalk<T, 8>(slice * per + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), min((slice + 1) * per, row.tiles),
+        : TileWalk<T, 8, 2>(slice * per + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), min((slice + 1) * per, row.tiles),
                          SLICE_THREADS / 64) {}
 };
 
+// The first look at a row: its largest logits; for top_p alone also what weighs how much in each slice, by bins below the
+// slice's own largest logit.
 template <typename T>
 __global__ __launch_bounds__(SLICE_THREADS) void sample_max_kernel(const T* __restrict__ logits, int64_t stride, int V,
-                                                                   SampleScratch sc) {
-    constexpr int VEC = Row<T>::VEC;
-    const int slice = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
-    const Row<T> row(logits + b * stride, V);
-    if (slice == 0) {
-        for (int i = tid; i < SAMPLE_BINS; i += SLICE_THREADS) sc.tally[(size_t)b * SAMPLE_BINS + i] = 0;
-        if (tid == 0) {
-            sc.state[b].n_list = 0;
-            sc.state[b].first_at = 0xffffffffu;
-        }
+                                                                   const float* __restrict__ temperature,
+                                                                   const int32_t* __restrict__ top_k,
+                                                                   const float* __restrict__ top_p,
+                                                                   const float* __restrict__ min_p, SampleScratch sc) {
+    constexpr int VEC = Row<T>::VEC, WAVES = SLICE_THREADS / 64, AHEAD = 8, PER = SAMPLE_BINS / SLICE_THREADS;
+    static_assert(PER == 4);
+    __shared__ u64 tally[SAMPLE_BINS], sums[WAVES];
+    __shared__ float tops[WAVES];
+    const int slice = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    Row<T> row(logits + b * stride, V);
+    if (slice == 0 && tid == 0) {
+        sc.state[b].n_list = 0;
+        sc.state[b].first_at = 0xffffffffu;
     }
-    float m = -INFINITY;
     // (pieces of a slice side by side over the threads: the order within it is nobody's business here)
     const int per = (row.tiles + sc.slices - 1) / sc.slices * row.steps * 64, j1 = min((slice + 1) * per, row.pieces);
-    int j = slice * per + tid;
-    for (; j < j1; j += 8 * SLICE_THREADS) {
-        uint4 w[8];
+    const int j0 = slice * per + tid;
+    uint4 held[AHEAD];
+    auto fetch = [&](int j) {
 #pragma unroll
-        for (int q = 0; q < 8; ++q) w[q] = j + q * SLICE_THREADS < j1 ? row.raw(j + q * SLICE_THREADS) : Row<T>::nothing();
+        for (int q = 0; q < AHEAD; ++q) held[q] = j + q * SLICE_THREADS < j1 ? row.raw(j + q * SLICE_THREADS) : Row<T>::nothing();
+    };
+    fetch(j0);
+    Settings s(b, V, temperature, top_k, top_p, min_p);
+    const bool weigh = s.p_alone();
+    if (weigh)
+        for (int i = tid; i < SAMPLE_BINS; i += SLICE_THREADS) tally[i] = 0;
+    float m = -INFINITY;
+    for (int j = j0;;) {
 #pragma unroll
-        for (int q = 0; q < 8; ++q) {
+        for (int q = 0; q < AHEAD; ++q) {
             float x[VEC];
-            row.values(w[q], x);
+            row.values(held[q], x);
 #pragma unroll
             for (int e = 0; e < VEC; ++e) m = fmaxf(m, x[e]);
         }
+        j += AHEAD * SLICE_THREADS;
+        if (j - tid >= j1) break;                          // (the same for all threads)
+        fetch(j);
     }
     m = fmaxf(m, __shfl_xor(m, 1));
-    if ((tid & 1) == 0) sc.maxima[((size_t)b * sc.slices + slice) * SLICE_MAXIMA + (tid >> 1)] = m;
+    if (s.by_k && (tid & 1) == 0) sc.maxima[((size_t)b * sc.slices + slice) * SLICE_MAXIMA + (tid >> 1)] = m;
+    m = wave_max(m);
+    if (lane == 0) tops[wave] = m;
+    __syncthreads();
+    for (int w = 0; w < WAVES; ++w) m = fmaxf(m, tops[w]);
+    if (tid == 0) sc.top[(size_t)b * sc.slices + slice] = m;
+    if (!weigh) return;
+    s.measure(m);
+    row.endless = m == INFINITY;
+    if (m > -INFINITY) {
+        if (j0 - tid + AHEAD * SLICE_THREADS < j1) fetch(j0);      // (else all of them are there still)
+        for (int j = j0;;) {
+            each_of<2>(held, [&](const uint4& w, int) __attribute__((always_inline)) {
+                float x[VEC];
+                row.values(w, x);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    const float oct = s.octaves(x[e]);
+                    if (s.counts(oct)) atomicAdd(&tally[s.bin_of(oct)], s.tallied(oct));
+                }
+            });
+            j += AHEAD * SLICE_THREADS;
+            if (j - tid >= j1) break;
+            fetch(j);
+        }
+    }
+    __syncthreads();
+    u64 sum[PER], mine = 0;
+#pragma unroll
+    for (int q = 0; q < PER; ++q) sum[q] = mine += s.about(tally[tid * PER + q], tid * PER + q);
+    const u64 inc = wave_running(mine);
+    if (lane == 63) sums[wave] = inc;
+    __syncthreads();
+    u64 before = inc - mine;
+    for (int w = 0; w < wave; ++w) before += sums[w];
+    float4 out = make_float4((float)(before + sum[0]), (float)(before + sum[1]), (float)(before + sum[2]), (float)(before + sum[3]));
+    *reinterpret_cast<float4*>(sc.mass + ((size_t)b * sc.slices + slice) * SAMPLE_BINS + tid * PER) = out;
 }
 
-// The second look at a row: the list, the tiles' sums, or the bins' tallies, as its settings ask.
+// The second look at a row: the list or the tiles' sums, as its settings ask; for top_p alone the bins around its border, the
+// tiles' sums up to them, and their tokens.
 template <typename T>
 __global__ __launch_bounds__(SLICE_THREADS) void sample_collect_kernel(const T* __restrict__ logits, int64_t stride, int V,
                                                                        const float* __restrict__ temperature,
@@ -317,6 +383,9 @@ __global__ __launch_bounds__(SLICE_THREADS) void sample_collect_kernel(const T* 
     __shared__ float tops[WAVES];
     __shared__ u64 sums[WAVES];
     __shared__ int found;
+    __shared__ u64 here[SLICE_EACH][SLICE_THREADS];
+    __shared__ uint32_t to_row;
+    constexpr float WIDTH = SAMPLE_OCTAVES / SAMPLE_BINS;
     const int slice = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     Row<T> row(logits + b * stride, V);
     Settings s(b, V, temperature, top_k, top_p, min_p);
@@ -324,14 +393,11 @@ __global__ __launch_bounds__(SLICE_THREADS) void sample_collect_kernel(const T* 
     const float* maxima = sc.maxima + (size_t)b * n_max;
     SliceWalk<T> walk(row, slice, (row.tiles + sc.slices - 1) / sc.slices);
     walk.fetch(row);
-    float most = -INFINITY;
-    for (int i = tid; i < n_max; i += SLICE_THREADS) most = fmaxf(most, maxima[i]);
-    most = wave_max(most);
-    if (lane == 0) tops[wave] = most;
+    const float my_top = lane < sc.slices ? sc.top[(size_t)b * sc.slices + lane] : -INFINITY;    // (lane i has slice i's)
     for (int i = tid; i < SAMPLE_BINS; i += SLICE_THREADS) tally[i] = 0;
     if (tid == 0) found = -1;
     __syncthreads();
-    for (int w = 0; w < WAVES; ++w) most = fmaxf(most, tops[w]);
+    const float most = wave_max(my_top);
     if (slice == 0 && tid == 0) sc.state[b].most = most;
     if (most == -INFINITY) return;
     auto nothing = [](int) {};
@@ -390,16 +456,52 @@ __global__ __launch_bounds__(SLICE_THREADS) void sample_collect_kernel(const T* 
             for (int w = 1; w < WAVES; ++w) low = fminf(low, tops[w]);
         }
     }
+    // Tokens for the list gather in LDS first, each thread's by itself: hardly any of its 64 is meant, and a place in a list
+    // that threads share costs a count of all of them for each piece.
+    uint32_t* n = &sc.state[b].n_list;
+    u64* places = sc.list + (size_t)b * SAMPLE_LIST;
+    int n_here = 0;
+    auto gather = [&](const float (&x)[VEC], const bool (&in)[VEC], int j) __attribute__((always_inline)) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+            if (in[e]) {
+                const u64 place = place_of(x[e], (uint32_t)(row.first(j) + e));
+                if (n_here < SLICE_EACH) {
+                    here[n_here++][tid] = place;
+                } else {
+                    const uint32_t to = atomicAdd(n, 1u);
+                    if (to < SAMPLE_LIST) places[to] = place;
+                }
+            }
+    };
+    auto hand_over = [&]() {
+        uint32_t inc = (uint32_t)n_here;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const uint32_t t = __shfl_up(inc, o);
+            if (lane >= o) inc += t;
+        }
+        if (lane == 63) counts[wave] = inc;
+        __syncthreads();
+        uint32_t to = inc - (uint32_t)n_here, all = 0;
+        for (int w = 0; w < WAVES; ++w) {
+            if (w < wave) to += counts[w];
+            all += counts[w];
+        }
+        if (tid == 0 && all) to_row = atomicAdd(n, all);
+        __syncthreads();
+        if (all) to += to_row;
+        for (int i = 0; i < n_here; ++i)
+            if (to + i < SAMPLE_LIST) places[to + i] = here[i][tid];
+    };
     if (list || sum) {
-        uint32_t* n = &sc.state[b].n_list;
-        u64* places = sc.list + (size_t)b * SAMPLE_LIST;
         u64 total = 0, tile = 0;
         walk.run(row, [&](float (&x)[VEC], int j) {
             if (list) {
                 bool in[VEC];
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) in[e] = x[e] >= low;
-                append_places<VEC>(x, in, row.first(j), n, places, SAMPLE_LIST, lane);
+                gather(x, in, j);
             }
             if (sum) {
                 float w = 0.f;
@@ -415,6 +517,7 @@ __global__ __launch_bounds__(SLICE_THREADS) void sample_collect_kernel(const T* 
                 tile = 0;
             }
         });
+        if (list) hand_over();
         if (sum) {
             if (lane == 0) sums[wave] = total;
             __syncthreads();
@@ -426,64 +529,36 @@ __global__ __launch_bounds__(SLICE_THREADS) void sample_collect_kernel(const T* 
         }
         return;
     }
-    // top_p alone
-    walk.run(row, [&](float (&x)[VEC], int) {
+    // top_p alone: where the weight up to a bin, summed over the slices, reaches p of all of it, by every wave for itself:
+    // among every sixteenth bin, then among sixteen.  A slice's bin lies across two of the row's and counts in one of them,
+    // so a sum up to a bin here is one up to at most a bin earlier or later.
+    const float down = s.octaves(of_max(my_top)), share = down < SAMPLE_OCTAVES ? s.weight(down) : 0.f;
+    const int shift = min((int)fmaxf(fmaf(down, SAMPLE_BINS / SAMPLE_OCTAVES, 0.5f), 0.f), SAMPLE_BINS);
+    auto weight_to = [&](int bin) {
+        constexpr int AT_ONCE = 8;
+        float w = 0.f;
+        for (int i0 = 0; i0 < sc.slices; i0 += AT_ONCE) {
+            float v[AT_ONCE];
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            const float oct = s.octaves(x[e]);
-            if (s.counts(oct)) atomicAdd(&tally[s.bin_of(oct)], s.tallied(oct));
+            for (int i = 0; i < AT_ONCE; ++i) {
+                const int from = min(i0 + i, sc.slices - 1), at = bin - __builtin_amdgcn_readlane(shift, from);
+                v[i] = sc.mass[((size_t)b * sc.slices + from) * SAMPLE_BINS + max(at, 0)];
+                if (at < 0 || i0 + i >= sc.slices) v[i] = 0.f;
+            }
+#pragma unroll
+            for (int i = 0; i < AT_ONCE; ++i)
+                w += v[i] * __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(share), min(i0 + i, sc.slices - 1)));
         }
-    }, nothing);
-    __syncthreads();
-    for (int i = tid; i < SAMPLE_BINS; i += SLICE_THREADS)
-        if (tally[i]) atomicAdd(&sc.tally[(size_t)b * SAMPLE_BINS + i], tally[i]);
-}
-
-// top_p alone: the bins around its border, and behind that the total, the tiles' sums up to them, and their tokens.
-template <typename T>
-__global__ __launch_bounds__(SLICE_THREADS) void sample_window_kernel(const T* __restrict__ logits, int64_t stride, int V,
-                                                                      const float* __restrict__ temperature,
-                                                                      const int32_t* __restrict__ top_k,
-                                                                      const float* __restrict__ top_p,
-                                                                      const float* __restrict__ min_p, SampleScratch sc) {
-    constexpr int VEC = Row<T>::VEC, WAVES = SLICE_THREADS / 64, PER = SAMPLE_BINS / SLICE_THREADS;
-    constexpr float WIDTH = SAMPLE_OCTAVES / SAMPLE_BINS;
-    __shared__ u64 sums[WAVES];
-    __shared__ int found[2];
-    const int slice = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    Settings s(b, V, temperature, top_k, top_p, min_p);
-    const float most = sc.state[b].most;
-    if (!s.by_p || s.by_k || s.by_least || s.greedy() || most == -INFINITY) return;
-    s.measure(most);
-    Row<T> row(logits + b * stride, V);
-    SliceWalk<T> walk(row, slice, (row.tiles + sc.slices - 1) / sc.slices);
-    walk.fetch(row);
-    row.endless = most == INFINITY;
-    u64 mass[PER], mine = 0;
-#pragma unroll
-    for (int q = 0; q < PER; ++q) {
-        const int bin = tid * PER + q;
-        mine += mass[q] = s.about(sc.tally[(size_t)b * SAMPLE_BINS + bin], bin);
-    }
-    const u64 inc = wave_running(mine);
-    if (lane == 63) sums[wave] = inc;
-    if (tid == 0) found[0] = 0, found[1] = SAMPLE_BINS;
-    __syncthreads();
-    u64 before = inc - mine, total = 0;
-    for (int w = 0; w < WAVES; ++w) {
-        if (w < wave) before += sums[w];
-        total += sums[w];
-    }
-    const u64 want = s.part_of(total), early = s.early(want), late = s.late(want);
-#pragma unroll
-    for (int q = 0; q < PER; ++q) {
-        const u64 v = before + mass[q];
-        if (before < early && v >= early) found[0] = tid * PER + q;
-        if (before < late && v >= late) found[1] = tid * PER + q;
-        before = v;
-    }
-    __syncthreads();
-    const float first = (float)(found[0] - 1) * WIDTH, last = (float)(found[1] + 2) * WIDTH;
+        return w;
+    };
+    const float coarse = weight_to(16 * lane + 15);
+    const float want = fmaxf(s.p, 0.f) * __shfl(coarse, 63), early = want - want * 0x1p-12f, late = want + want * 0x1p-12f;
+    const u64 c0 = __ballot(coarse >= early), c1 = __ballot(coarse >= late);
+    const int from0 = 16 * (c0 ? __ffsll(c0) - 1 : 63), from1 = 16 * (c1 ? __ffsll(c1) - 1 : 63);
+    const float fine = weight_to((lane < 32 ? from0 : from1) + (lane & 15));
+    const u64 f0 = __ballot(fine >= early) & 0xffff, f1 = (__ballot(fine >= late) >> 32) & 0xffff;
+    const int border0 = from0 + (f0 ? __ffsll(f0) - 1 : 15), border1 = f1 ? from1 + __ffsll(f1) - 1 : SAMPLE_BINS;
+    const float first = (float)(border0 - 2) * WIDTH, last = (float)(border1 + 3) * WIDTH;
     if (slice == 0 && tid == 0) {
         sc.state[b].window0 = first;
         sc.state[b].window1 = last;
@@ -499,7 +574,7 @@ __global__ __launch_bounds__(SLICE_THREADS) void sample_window_kernel(const T* _
             sure += oct < first ? w : 0.f;
             in[e] = oct >= first && oct < last;
         }
-        append_places<VEC>(x, in, row.first(j), &sc.state[b].n_list, sc.list + (size_t)b * SAMPLE_LIST, SAMPLE_LIST, lane);
+        gather(x, in, j);
         all += whole(any);
         tile += whole(sure);
     }, [&](int t) {
@@ -508,7 +583,7 @@ __global__ __launch_bounds__(SLICE_THREADS) void sample_window_kernel(const T* _
         tile = 0;
     });
     all = wave_total(all);
-    __syncthreads();
+    hand_over();
     if (lane == 0) sums[wave] = all;
     __syncthreads();
     if (tid == 0) {
@@ -586,7 +661,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(const T* __restr
         }
     };
     auto each_tile = [&](auto f, auto done) __attribute__((always_inline)) {
-        TileWalk<T, 4> walk(wave, row.tiles, SAMPLE_WAVES);
+        TileWalk<T, 4, 4> walk(wave, row.tiles, SAMPLE_WAVES);
         walk.fetch(row);
         walk.run(row, f, done);
     };
@@ -741,7 +816,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(const T* __restr
             const int n = min((int)n_list, SAMPLE_LIST);
             for (int i = tid; i < n; i += SAMPLE_THREADS) list[i] = sc.list[(size_t)b * SAMPLE_LIST + i];
             if (by_p && !by_k)
-                for (int i = 0; i < sc.slices; ++i) total += sc.total[(size_t)b * sc.slices + i];
+                total = wave_total(lane < sc.slices ? sc.total[(size_t)b * sc.slices + lane] : 0);
             __syncthreads();
         } else {
             float low = LOWEST;
@@ -952,7 +1027,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(const T* __restr
             u64 total = 0;
             if (left_over) {
                 tile_sum[tid] = tid < row.tiles ? sc.tile_sum[(size_t)b * SAMPLE_BINS + tid] : 0;
-                for (int i = 0; i < sc.slices; ++i) total += sc.total[(size_t)b * sc.slices + i];
+                total = wave_total(lane < sc.slices ? sc.total[(size_t)b * sc.slices + lane] : 0);
                 n_list = sc.state[b].n_list;  // (all threads the same)
                 const int n = min((int)n_list, SAMPLE_LIST);
                 for (int i = tid; i < n; i += SAMPLE_THREADS) list[i] = sc.list[(size_t)b * SAMPLE_LIST + i];
@@ -1096,7 +1171,8 @@ size_t sample_scratch(char* base, int rows, int slices, SampleScratch* sc) {
     SampleScratch s{};
     s.state = reinterpret_cast<RowState*>(take(sizeof(RowState)));
     s.maxima = reinterpret_cast<float*>(take((size_t)slices * SLICE_MAXIMA * 4));
-    s.tally = reinterpret_cast<u64*>(take(SAMPLE_BINS * 8));
+    s.top = reinterpret_cast<float*>(take((size_t)slices * 4));
+    s.mass = reinterpret_cast<float*>(take((size_t)slices * SAMPLE_BINS * 4));
     s.tile_sum = reinterpret_cast<u64*>(take(SAMPLE_BINS * 8));
     s.total = reinterpret_cast<u64*>(take((size_t)slices * 8));
     s.list = reinterpret_cast<u64*>(take((size_t)SAMPLE_LIST * 8));
@@ -1141,16 +1217,12 @@ int sample_rows(const T* logits, int64_t stride, int B, int V, const float* temp
         sample_scratch(scratch, rows, slices, &sc);
         const T* x = logits + b0 * stride;
         const dim3 grid(slices, n);
-        hipLaunchKernelGGL((sample_max_kernel<T>), grid, dim3(SLICE_THREADS), 0, st, x, stride, V, sc);
+        hipLaunchKernelGGL((sample_max_kernel<T>), grid, dim3(SLICE_THREADS), 0, st, x, stride, V, at(temperature),
+                           at(top_k), at(top_p), at(min_p), sc);
         MVLA_HIP_CHECK(hipGetLastError());
         hipLaunchKernelGGL((sample_collect_kernel<T>), grid, dim3(SLICE_THREADS), 0, st, x, stride, V, at(temperature),
                            at(top_k), at(top_p), at(min_p), sc);
         MVLA_HIP_CHECK(hipGetLastError());
-        if (top_p) {
-            hipLaunchKernelGGL((sample_window_kernel<T>), grid, dim3(SLICE_THREADS), 0, st, x, stride, V, at(temperature),
-                               at(top_k), at(top_p), at(min_p), sc);
-            MVLA_HIP_CHECK(hipGetLastError());
-        }
         if (int rc = choose_rows<T, true>(x, stride, n, V, at(temperature), at(top_k), at(top_p), at(min_p), at(u), at(token),
                                           at(prob), sc, st))
             return rc;
