@@ -586,7 +586,7 @@ class Context:
         shape = (cache.B, cache.H_kv, n, cache.dh)
         if out is None:
             k = torch.empty(shape, dtype=torch.bfloat16, device=cache.device)
-            v = torch.empty(shape, dtype=torch.bfloat16, device=cache.device)
+            v = torch.empty_like(k)
         else:
             k, v = out
             assert _dev(k, torch.bfloat16).shape == _dev(v, torch.bfloat16).shape == shape
@@ -605,7 +605,7 @@ class Context:
         assert (B, dh) == (cache.B, cache.dh) and _dev(length, torch.int32).shape == (B,)
         assert n_new is None or _dev(n_new, torch.int32).shape == (B,)
         if out is None:
-            out = torch.empty(B, n_q, H, dh, dtype=torch.bfloat16, device=cache.device)
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
         else:
             assert out.shape == q.shape
         _check(load().mvla_cache_attention(self._h, cache._ref, C.byref(_rows(q)), H, n_q,
@@ -627,7 +627,7 @@ class Context:
         assert recent_from is None or _dev(recent_from, torch.int32).shape == (B,)
         if out is None:
             kept = torch.empty(B, src.H_kv, budget, dtype=torch.int32, device=src.device)
-            new = torch.empty(B, dtype=torch.int32, device=src.device)
+            new = torch.empty_like(length)
         else:
             kept, new = out
             assert _dev(kept, torch.int32).shape == (B, src.H_kv, budget)
@@ -654,7 +654,7 @@ class Context:
             assert t is None or _dev(t, dt).shape == (B,)
         if out is None:
             token = torch.empty(B, dtype=torch.int32, device=logits.device)
-            prob = torch.empty(B, dtype=torch.float32, device=logits.device)
+            prob = torch.empty_like(u)
         else:
             token, prob = out
             assert _dev(token, torch.int32).shape == (B,)
