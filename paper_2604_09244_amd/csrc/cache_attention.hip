@@ -1148,17 +1148,23 @@ AttentionPlan attention_plan(int B, int H, int H_kv, int dh, int n_q, int max_le
     AttentionPlan p{};
     p.group = H / H_kv;
     p.rows = n_q * p.group;
+    // Some rows against many, us: 8 x 32 heads of 128 over 1840 slots, 17 rows 19 / 41, 48 26 / 51, 96 47 / 57, 112 66 / 60,
+    // 128 68 / 62; 16 samples over 2624 slots 48 rows 61 / 105, 96 116 / 111, 112 166 / 118.  Two column tiles against three
+    // there: 32 rows 20 / 24, 48 37 / 26, 64 38 / 46, 96 54 / 47: as few blocks of rows as there can be, then the smaller ones.
     p.kind = p.rows <= FEW_ROWS ? FEW : p.rows <= SOME_MOST ? SOME : MANY;
     p.tiles = p.rows <= 32 || (p.rows > 48 && p.rows <= 64) ? 2 : 3;
     p.pitch = (max_len + FEW_STEP - 1) / FEW_STEP * FEW_STEP;
     const int cus = device_cu_count();
     const int64_t heads = (int64_t)B * H_kv, steps = p.pitch / FEW_STEP;
     if (p.kind == FEW) {
-        // Whole samples a workgroup where that fills the chip, or where there is little to split; eight waves where a
-        // launch leaves compute units idle.
+        // Whole samples a workgroup (one launch, logits in LDS) where there is one for every compute unit or little to
+        // split for those that there are; eight waves where a launch leaves compute units idle.  One row of 128, with
+        // weights, whole against split, us: 32 heads of 237 slots 6.3 / 9.2, 1024 9.2 / 10.3, 1500 10.9 / 10.2; 64 heads of
+        // 1500 11.0 / 11.8, 2624 15.5 / 14.8; 128 of 2624 17.0 / 19.2, 8192 38.6 / 31.9; 256 of 1840 15.5 / 21.3, 16384
+        // 118 / 130; 512 of 2624 34.2 / 37.8.  Four rows: 64 heads of 512 7.6 / 10.9, 512 of 4096 54.3 / 73.1.
         p.waves = heads <= cus ? 8 : 4;
         const size_t lds = few_lds(dh, p.waves, p.rows, accumulate ? p.pitch : 0);
-        const bool whole = lds <= 72 * 1024 && (heads >= cus + cus / 2 || steps <= 4 * p.waves);
+        const bool whole = lds <= 72 * 1024 && (heads >= cus || steps <= std::max<int64_t>(32, heads));
         if (!whole) {
             p.waves = 4;
             // enough workgroups to fill the chip, and where they would still be long (eight steps a wave) so many that

@@ -444,15 +444,19 @@ static int evict_select(const CacheView& c, const CacheView& d, const int32_t* l
     return MVLA_OK;
 }
 
-// Rows of a workgroup that it copies itself: all while there are workgroups for the chip, a few hundred otherwise.
-static bool evict_moves(const CacheView& c, int budget, int max_len) {
-    const int rows = budget < max_len ? budget : max_len;
-    return c.B * c.H_kv >= device_cu_count() || rows <= 512;
+// Whether the workgroups copy the rows themselves.  Into another cache that pays with workgroups for the chip, and with few
+// rows, where a second launch costs the caller 3 us more than it saves the chip: 32 heads, 512 of 1024 rows 12.8 us against
+// 10.8 with the second launch, 1344 of 2624 23.0 / 15.4; 128 heads 27.4 / 24.3, 224 30.0 / 31.3, 512 53.5 / 57.2.  In place
+// fewer rows move: 32 heads, 512 of 1024 11.2 / 11.4, 1344 of 2624 18.7 / 17.9, 8192 of 16384 68 / 58; 1344 of 2624, 128 heads
+// 18.7 / 19.3, 512 23.2 / 29.9.
+static bool evict_moves(const CacheView& c, bool in_place, int budget, int max_len) {
+    const int rows = budget < max_len ? budget : max_len, heads = c.B * c.H_kv, cus = device_cu_count();
+    return in_place ? heads >= cus / 4 || rows <= 1024 : heads >= cus * 3 / 4 || rows <= 512;
 }
 
 int launch_cache_evict(const CacheView& c, const CacheView& d, const int32_t* len, int max_len, int budget, int first_pos,
                        const int32_t* recent_from, int32_t* len_out, int32_t* kept, int32_t* holes, hipStream_t st) {
-    const bool move = evict_moves(c, budget, max_len);
+    const bool move = evict_moves(c, c.k == d.k, budget, max_len);
 #define MVLA_EVICT(LDS, DH) evict_select<LDS, DH>(c, d, len, max_len, budget, first_pos, recent_from, len_out, kept, holes, st)
     const int rc = max_len <= EVICT_LDS ? (!move ? MVLA_EVICT(true, 0) : c.dh == 128 ? MVLA_EVICT(true, 128) : MVLA_EVICT(true, 64))
                                         : (!move ? MVLA_EVICT(false, 0) : c.dh == 128 ? MVLA_EVICT(false, 128) : MVLA_EVICT(false, 64));

@@ -32,7 +32,10 @@ typedef unsigned long long u64;    // (as atomics take it)
 constexpr int SAMPLE_THREADS = 1024, SAMPLE_WAVES = SAMPLE_THREADS / 64;
 constexpr int SAMPLE_BINS = 1024;         // of octaves below the largest weight, and at most so many tiles
 constexpr int SAMPLE_LIST = 14336;        // tokens on the list: 112 of the 160 KiB of LDS
-constexpr int ONE_WORKGROUP = 32768;      // tokens of a row that one workgroup takes by itself
+// Tokens of a row that one workgroup takes by itself.  96 rows of fp32, one workgroup a row against slices, us: 32768 tokens
+// no filter 14 / 20, top-k and top-p 15 / 24, top-p 30 / 38; 65536 22 / 25, 19 / 27, 47 / 49; one row of 65536 22 / 19, 18 / 22,
+// 45 / 36.
+constexpr int ONE_WORKGROUP = 32768;
 constexpr int SLICE_THREADS = 256, SLICE_MAXIMA = 128;
 constexpr int SLICE_EACH = 12;            // tokens of a thread that come to its row's list together (24 KiB of LDS)
 constexpr float SAMPLE_OCTAVES = 40.f;    // weights below 2^-40 of the largest count as none
@@ -1158,7 +1161,9 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(const T* __restr
 // ---- host ------------------------------------------------------------------------------------------------------------
 namespace {
 
-constexpr int SLICE_TOKENS = 16384;       // a slice at least; a row has at most 32
+// Tokens of a slice: 16384, and down to 8192 while two workgroups a compute unit are not there; a row has at most 32 slices.
+// (One row of 131072 fp32 tokens, 8 slices against 16: no filter 19.5 / 15.0 us, top-p 37.2 / 29.5, top-k 22.7 / 21.0.)
+constexpr int SLICE_TOKENS = 16384, SLICE_LEAST = 8192;
 
 // bytes of scratch a row, and where its parts lie for `rows` rows
 size_t sample_scratch(char* base, int rows, int slices, SampleScratch* sc) {
@@ -1206,7 +1211,9 @@ int sample_rows(const T* logits, int64_t stride, int B, int V, const float* temp
                 size_t scratch_bytes, hipStream_t st) {
     if (V <= ONE_WORKGROUP)
         return choose_rows<T, false>(logits, stride, B, V, temperature, top_k, top_p, min_p, u, token, prob, SampleScratch{}, st);
-    int slices = (V + SLICE_TOKENS - 1) / SLICE_TOKENS;
+    const int fill = (2 * device_cu_count() + B - 1) / B, most = (V - 1) / SLICE_LEAST + 1;
+    int slices = (V - 1) / SLICE_TOKENS + 1;
+    if (slices < fill) slices = fill < most ? fill : most;
     if (slices > 32) slices = 32;
     int rows = B;
     while (rows > 1 && sample_scratch(nullptr, rows, slices, nullptr) > scratch_bytes) rows = (rows + 1) / 2;
