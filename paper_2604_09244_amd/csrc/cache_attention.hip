@@ -57,7 +57,12 @@ __device__ __forceinline__ uint32_t column_or(uint32_t x) {
 //   V: lane c of a group takes dims c CH .. c CH + CH - 1 of the group's eight slots; the codes become pairs of dims of
 //      one slot, two permutes turn two slots' pairs into pairs of slots of one dim
 //   O^T: tile d holds dims c CH + d, so a lane ends with CH consecutive dims per register index: whole 16-byte stores
-// Bound by memory: 2 (dh / 2 + dh / 32) bytes a slot; three steps of codes are on their way per wave.
+// Bound by memory: 2 (dh / 2 + dh / 32) bytes a slot, 8 more for its weight, and where the logits of a split sample pass
+// through memory 8 for each row; three steps of codes are on their way per wave.  One query, 32 heads of 128, with weights:
+// 16 samples of 2624 slots 42 us, 4.6 TB/s; one sample of 237 6.3 us, the latency of its loads and of the join.  64 x 8
+// heads of four rows, up to 16384 slots of ragged samples: 168 us here and 34 in join_kernel, 3.9 TB/s of the codes and
+// weights alone, 4.7 with the logits.  (Turns of a few samples, so that their logits stay in the last-level cache, were
+// never faster and up to twice as slow.)
 constexpr int FEW_STEP = 32, FEW_ROWS = 16;
 
 template <int DH>
@@ -376,6 +381,8 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void few_rows_kerne
 // 16 CT rows a workgroup: the same step with CT column tiles a wave, so that a slot's codes become values once for all of
 // them.  Eight waves a workgroup; queries wait in LDS (their registers go to the accumulators), and the waves' parts are joined
 // there in three rounds, half of the waves handing theirs to the others each time.
+// Bound by the latency of a few steps a wave (a workgroup's start, seven steps and the join for 1840 slots), then by the
+// steps' arithmetic: 8 x 32 heads of 128, 48 rows over up to 1840 slots 26 us, 4.9 of them matrix products at a library's rate.
 constexpr int SOME_WAVES = 8;
 
 template <int DH, int CT>
@@ -675,6 +682,8 @@ __global__ __launch_bounds__(JOIN_THREADS) void join_kernel(CacheView cache, Cac
 // ---- many rows -----------------------------------------------------------------------------------------------------
 // 128 rows a workgroup, 32 a wave, 64 slots at a time: the codes become bf16 once per workgroup on their way into LDS
 // (keys row by row, values transposed), two stages deep, the next tile's codes on their way meanwhile.
+// Bound by the issue of vector operations (softmax, codes to bf16) beside the matrix products: 4 x 32 heads of 128, 512 rows
+// over 2624 slots 114 us, 0.70 PFLOP/s, the rate of the attention over bf16 keys at these lengths.
 constexpr int MANY_THREADS = 256, MANY_ROWS = 128, MANY_KT = 64;
 
 // LDS row r holds slot many_key(r) of a tile (bits 2 and 3 swapped: a lane's eight probabilities of a 16-slot step are
@@ -931,6 +940,8 @@ __global__ __launch_bounds__(MANY_THREADS, 2) void many_rows_kernel(CacheView ca
 // The logits once more (keys only), against the rows' final maxima and sums: a wave holds its slots' keys in registers and
 // walks the rows, 16 at a time; the columns' sums go over the lanes of a group at the end.  No value is added twice or in
 // another order from run to run.
+// 8 x 32 heads of 128, 48 rows over up to 1840 slots 14.5 us, 22 MB of keys at 1.5 TB/s: latency of one run of slots a wave.
+// (512 rows of 4 x 32 heads over 2624 slots: 100 us.)
 constexpr int WEIGH_WAVES = 4, SOME_MOST = 96;
 
 // this lane's codes of the two K tiles of 32 slots
