@@ -1170,9 +1170,9 @@ AttentionPlan attention_plan(int B, int H, int H_kv, int dh, int n_q, int max_le
     if (p.kind == FEW) {
         // Whole samples a workgroup (one launch, logits in LDS) where there is one for every compute unit or little to
         // split for those that there are; eight waves where a launch leaves compute units idle.  One row of 128, with
-        // weights, whole against split, us: 32 heads of 237 slots 6.3 / 9.2, 1024 9.2 / 10.3, 1500 10.9 / 10.2; 64 heads of
-        // 1500 11.0 / 11.8, 2624 15.5 / 14.8; 128 of 2624 17.0 / 19.2, 8192 38.6 / 31.9; 256 of 1840 15.5 / 21.3, 16384
-        // 118 / 130; 512 of 2624 34.2 / 37.8.  Four rows: 64 heads of 512 7.6 / 10.9, 512 of 4096 54.3 / 73.1.
+        // weights, whole against split, us: 32 heads of 237 slots 6.6 / 8.8, 1024 8.9 / 9.4, 1500 10.7 / 9.7; 64 heads of
+        // 1500 10.8 / 11.6, 2624 15.4 / 14.5; 128 of 2624 16.7 / 18.6, 8192 39 / 32; 256 of 1840 15.0 / 20.9, 8192 55 / 60;
+        // 512 of 2624 33.6 / 37.3.  Four rows: 64 heads of 512 7.4 / 9.6, 512 of 4096 53 / 72.
         p.waves = heads <= cus ? 8 : 4;
         const size_t lds = few_lds(dh, p.waves, p.rows, accumulate ? p.pitch : 0);
         const bool whole = lds <= 72 * 1024 && (heads >= cus || steps <= std::max<int64_t>(32, heads));

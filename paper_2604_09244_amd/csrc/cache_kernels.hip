@@ -272,9 +272,22 @@ __global__ __launch_bounds__(EVICT_THREADS) void evict_select_kernel(CacheView c
     };
     // ---- key of the nb-th row
     uint32_t lo = 0xffffffffu, hi = 0;
-    for (int i = tid; i < n; i += EVICT_THREADS) {
-        const uint32_t key = evict_key(w[i], p[i], first_pos, recent);
-        if constexpr (IN_LDS) lds_rows[i] = key;
+    int i1 = tid;                                              // (four loads of each on their way where there are as many)
+    for (; i1 - tid + 4 * EVICT_THREADS <= n; i1 += 4 * EVICT_THREADS) {
+        float weight[4];
+        int pos[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) weight[q] = w[i1 + q * EVICT_THREADS], pos[q] = p[i1 + q * EVICT_THREADS];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const uint32_t key = evict_key(weight[q], pos[q], first_pos, recent);
+            if constexpr (IN_LDS) lds_rows[i1 + q * EVICT_THREADS] = key;
+            lo = min(lo, key), hi = max(hi, key);
+        }
+    }
+    for (; i1 < n; i1 += EVICT_THREADS) {
+        const uint32_t key = evict_key(w[i1], p[i1], first_pos, recent);
+        if constexpr (IN_LDS) lds_rows[i1] = key;
         lo = min(lo, key), hi = max(hi, key);
     }
     uint32_t want = (uint32_t)nb, last;
@@ -452,10 +465,10 @@ static int evict_select(const CacheView& c, const CacheView& d, const int32_t* l
 }
 
 // Whether the workgroups copy the rows themselves.  Into another cache that pays with workgroups for the chip, and with few
-// rows, where a second launch costs the caller 3 us more than it saves the chip: 32 heads, 512 of 1024 rows 12.8 us against
-// 10.8 with the second launch, 1344 of 2624 23.0 / 15.4; 128 heads 27.4 / 24.3, 224 30.0 / 31.3, 512 53.5 / 57.2.  In place
-// fewer rows move: 32 heads, 512 of 1024 11.2 / 11.4, 1344 of 2624 18.7 / 17.9, 8192 of 16384 68 / 58; 1344 of 2624, 128 heads
-// 18.7 / 19.3, 512 23.2 / 29.9.
+// rows, where a second launch costs the caller 3 us as well: 32 heads, 64 of 128 rows 6.9 us against 8.8 with the second
+// launch, 1344 of 2624 20.0 / 17.8, 8192 of 16384 102 / 61; 1344 of 2624, 128 heads 24.5 / 24.7, 256 31.0 / 32.0.  In place fewer
+// rows move: 32 heads, 512 of 1024 10.2 / 12.4, 1344 of 2624 17.7 / 17.7, 8192 of 16384 64 / 52; 1344 of 2624, 128 heads 17.8 /
+// 18.9, 512 22.3 / 26.5.
 static bool evict_moves(const CacheView& c, bool in_place, int budget, int max_len) {
     const int rows = budget < max_len ? budget : max_len, heads = c.B * c.H_kv, cus = device_cu_count();
     return in_place ? heads >= cus / 4 || rows <= 1024 : heads >= cus * 3 / 4 || rows <= 512;

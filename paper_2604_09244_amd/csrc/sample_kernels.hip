@@ -35,9 +35,9 @@ typedef unsigned long long u64;    // (as atomics take it)
 constexpr int SAMPLE_THREADS = 1024, SAMPLE_WAVES = SAMPLE_THREADS / 64;
 constexpr int SAMPLE_BINS = 1024;         // of octaves below the largest weight, and at most so many tiles
 constexpr int SAMPLE_LIST = 14336;        // tokens on the list: 112 of the 160 KiB of LDS
-// Tokens of a row that one workgroup takes by itself.  96 rows of fp32, one workgroup a row against slices, us: 32768 tokens
-// no filter 14 / 20, top-k and top-p 15 / 24, top-p 30 / 38; 65536 22 / 25, 19 / 27, 47 / 49; one row of 65536 22 / 19, 18 / 22,
-// 45 / 36.
+// Tokens of a row that one workgroup takes by itself.  Rows of fp32, one workgroup a row against slices, us, without a filter /
+// with top-k and top-p / top-p alone: 96 of 32768 tokens 14 14 30 / 17 20 31, of 65536 22 19 47 / 23 25 46; one of 32768
+// 13 13 29 / 15 19 27, of 49152 18 16 37 / 15 19 27.
 constexpr int ONE_WORKGROUP = 32768;
 constexpr int SLICE_THREADS = 256, SLICE_MAXIMA = 128;
 constexpr int SLICE_EACH = 12;            // tokens of a thread that come to its row's list together (24 KiB of LDS)
