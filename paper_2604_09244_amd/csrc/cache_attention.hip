@@ -940,7 +940,7 @@ __global__ __launch_bounds__(MANY_THREADS, 2) void many_rows_kernel(CacheView ca
 // The logits once more (keys only), against the rows' final maxima and sums: a wave holds its slots' keys in registers and
 // walks the rows, 16 at a time; the columns' sums go over the lanes of a group at the end.  No value is added twice or in
 // another order from run to run.
-// 8 x 32 heads of 128, 48 rows over up to 1840 slots 14.5 us, 22 MB of keys at 1.5 TB/s: latency of one run of slots a wave.
+// 8 x 32 heads of 128, 48 rows over up to 1840 slots 13 us, 22 MB of keys at 1.7 TB/s: latency of a few runs of slots a wave.
 // (512 rows of 4 x 32 heads over 2624 slots: 100 us.)
 constexpr int WEIGH_WAVES = 4, SOME_MOST = 96;
 
@@ -1033,16 +1033,26 @@ __global__ __launch_bounds__(WEIGH_WAVES * 64, 2) void weigh_some_kernel(CacheVi
     const int last_row = min(rows, span.count * group), tiles = (rows + 15) / 16;
     WeighKeys<DH> next;
     weigh_load<DH>(next, cache, head, slot0, span.len, c, g);
-    for (int id = threadIdx.x; id < tiles * STEPS * 64; id += WEIGH_WAVES * 64) {
-        const int tile = id / (STEPS * 64), st = id / 64 % STEPS, r = min(tile * 16 + (id & 15), rows - 1), i = r / group;
-        sh_q[id] = *reinterpret_cast<const uint4*>(a.q.p + b * a.q.sample + i * a.q.token + (h * group + r % group) * a.q.head +
-                                                   (id >> 4 & 3) * (DH / 4) + st * 8);
+    // (rows that are not there: zero queries, whose probabilities are zero)
+    constexpr int QUERIES = SOME_MOST / 16 * STEPS * 64 / (WEIGH_WAVES * 64);
+    uint4 wait[QUERIES];
+#pragma unroll
+    for (int n = 0; n < QUERIES; ++n) {
+        const int id = n * WEIGH_WAVES * 64 + (int)threadIdx.x, tile = id / (STEPS * 64), st = id / 64 % STEPS;
+        const int r = tile * 16 + (id & 15), i = group == 1 ? r : r / group;
+        wait[n] = make_uint4(0u, 0u, 0u, 0u);
+        if (r < last_row)
+            wait[n] = *reinterpret_cast<const uint4*>(a.q.p + b * a.q.sample + i * a.q.token + (h * group + r - i * group) * a.q.head +
+                                                      (id >> 4 & 3) * (DH / 4) + st * 8);
     }
     for (int r = threadIdx.x; r < tiles * 16; r += WEIGH_WAVES * 64) {
         const float2 ml = row_ml[head * rows + min(r, rows - 1)];
-        sh_ml[r] = make_float2(-ml.x * scale_log2e, 1.f / ml.y);
+        sh_ml[r] = r < last_row ? make_float2(-ml.x * scale_log2e, 1.f / ml.y) : make_float2(-INFINITY, 0.f);
         sh_sees[r] = r < last_row ? seen_by(span, r / group) : 0;
     }
+#pragma unroll
+    for (int n = 0; n < QUERIES; ++n) sh_q[n * WEIGH_WAVES * 64 + threadIdx.x] = wait[n];
+    const int least = seen_by(span, 0);       // (or nobody sees anything, and last_row is 0)
     __syncthreads();
     for (int run = 0; run < groups && slot0 < span.len; ++run, slot0 += stride) {
         uint4 kf[1][2][STEPS];
@@ -1051,12 +1061,17 @@ __global__ __launch_bounds__(WEIGH_WAVES * 64, 2) void weigh_some_kernel(CacheVi
         const int my0 = slot0 + 8 * g;
         float sum[1][8] = {};
         // (from the first query that sees any of these slots on)
-        for (int tile = max(0, slot0 - (span.len - span.count)) * group / 16; tile * 16 < last_row; ++tile) {
-            uint4 q[STEPS];
+        auto walk = [&](auto mask, int tile) __attribute__((always_inline)) {
+            for (; tile * 16 < last_row; ++tile) {
+                uint4 q[STEPS];
 #pragma unroll
-            for (int st = 0; st < STEPS; ++st) q[st] = sh_q[(tile * STEPS + st) * 64 + lane];
-            weigh_add<DH, 1, true>(sum, kf, q, sh_ml[tile * 16 + c], sh_sees[tile * 16 + c], my0, scale_log2e);
-        }
+                for (int st = 0; st < STEPS; ++st) q[st] = sh_q[(tile * STEPS + st) * 64 + lane];
+                weigh_add<DH, 1, decltype(mask)::value>(sum, kf, q, sh_ml[tile * 16 + c], decltype(mask)::value ? sh_sees[tile * 16 + c] : 0, my0,
+                                                        scale_log2e);
+            }
+        };
+        if (slot0 + FEW_STEP <= least) walk(std::false_type{}, 0);
+        else walk(std::true_type{}, max(0, slot0 - (span.len - span.count)) * group / 16);
         weigh_store(sum[0], cache.weight + head * cache.capacity, my0, span.len, c);
     }
 }
