@@ -143,7 +143,7 @@ struct Settings {
     float t, p, least;
     int k, V;
     bool by_k, by_p, by_least;
-    float per_t, ref;
+    float twice_per_t, ref, half_ref;
     __device__ __forceinline__ Settings(int b, int v, const float* temperature, const int32_t* top_k, const float* top_p,
                                         const float* min_p) {
         V = v;
@@ -158,11 +158,12 @@ struct Settings {
     __device__ __forceinline__ bool greedy() const { return !(t > 0.f); }
     __device__ __forceinline__ bool p_alone() const { return by_p && !by_k && !by_least && !greedy(); }
     __device__ __forceinline__ void measure(float most) {
-        per_t = 1.4426950408889634f / t;
+        twice_per_t = fminf(2.8853900817779268f / t, -LOWEST);
         ref = most == INFINITY ? 0.f : most;
+        half_ref = 0.5f * ref;
     }
-    // octaves below the largest weight (NaN where that is no number)
-    __device__ __forceinline__ float octaves(float x) const { return (ref - x) * per_t; }
+    // octaves below the largest weight (NaN where that is no number); by halves, which no two logits are too far apart for
+    __device__ __forceinline__ float octaves(float x) const { return fmaf(x, -0.5f, half_ref) * twice_per_t; }
     static __device__ __forceinline__ float weight(float oct) { return __builtin_amdgcn_exp2f(-oct); }
     static __device__ __forceinline__ bool counts(float oct) { return oct < SAMPLE_OCTAVES; }
     static __device__ __forceinline__ int bin_of(float oct) {
@@ -192,7 +193,7 @@ struct Settings {
     }
     // from which logit on tokens can have min_p of the largest weight (a hair below: the weight itself is asked again)
     __device__ __forceinline__ float least_logit() const {
-        return fminf(fmaxf(LOWEST, ref + (__builtin_amdgcn_logf(least) - 0x1p-10f) / per_t), ref);
+        return fminf(fmaxf(LOWEST, ref + 2.f * (__builtin_amdgcn_logf(least) - 0x1p-10f) / twice_per_t), ref);
     }
 };
 
