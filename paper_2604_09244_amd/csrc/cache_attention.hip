@@ -683,7 +683,9 @@ __global__ __launch_bounds__(JOIN_THREADS) void join_kernel(CacheView cache, Cac
 // 128 rows a workgroup, 32 a wave, 64 slots at a time: the codes become bf16 once per workgroup on their way into LDS
 // (keys row by row, values transposed), two stages deep, the next tile's codes on their way meanwhile.
 // Bound by the issue of vector operations (softmax, codes to bf16) beside the matrix products: 4 x 32 heads of 128, 512 rows
-// over 2624 slots 114 us, 0.70 PFLOP/s, the rate of the attention over bf16 keys at these lengths.
+// over 2624 slots 106 us, 0.75 PFLOP/s, a little above the attention over bf16 keys at these lengths.  (The second product's
+// accumulators in turn rather than one after the other 109 / 105; two waves' priorities by phase, or exponentials
+// between the products by the scheduler's groups, no faster.)
 constexpr int MANY_THREADS = 256, MANY_ROWS = 128, MANY_KT = 64;
 
 // LDS row r holds slot many_key(r) of a tile (bits 2 and 3 swapped: a lane's eight probabilities of a 16-slot step are
@@ -823,6 +825,12 @@ __global__ __launch_bounds__(MANY_THREADS, 2) void many_rows_kernel(CacheView ca
         stage_tile(raw, kt0, 0);
         if (kt0 + 1 < kt1) load(raw, kt0 + 1);
     }
+    // fragments' places in a stage; 32 rows on, the swizzle is the same
+    int k_at[STEPS], v_at[4];
+#pragma unroll
+    for (int st = 0; st < STEPS; ++st) k_at[st] = fr * CPR + ((st * 2 + fg) ^ many_swz<CPR>(fr));
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) v_at[ks] = K_SLOTS + fr * 8 + ((ks * 2 + fg) ^ many_swz<8>(fr));
     int stage = 0;
     for (int kt = kt0; kt < kt1; ++kt, stage ^= 1) {
         __syncthreads();      // tile kt is in LDS for every wave; the other stage has been read by all
@@ -832,8 +840,7 @@ __global__ __launch_bounds__(MANY_THREADS, 2) void many_rows_kernel(CacheView ca
         }
         const int key0 = kt * MANY_KT;
         if (key0 >= wave_most) continue;
-        const uint4* Kc = lds + stage * STAGE;
-        const uint4* Vc = Kc + K_SLOTS;
+        const uint4* tile = lds + stage * STAGE;
         f32x16_t s_acc[2];
 #pragma unroll
         for (int t = 0; t < 2; ++t)
@@ -842,10 +849,7 @@ __global__ __launch_bounds__(MANY_THREADS, 2) void many_rows_kernel(CacheView ca
 #pragma unroll
         for (int st = 0; st < STEPS; ++st)
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const int row = t * 32 + fr;
-                s_acc[t] = mfma32(Kc[row * CPR + ((st * 2 + fg) ^ many_swz<CPR>(row))], qf[st], s_acc[t]);
-            }
+            for (int t = 0; t < 2; ++t) s_acc[t] = mfma32(tile[k_at[st] + t * 32 * CPR], qf[st], s_acc[t]);
         if (key0 + MANY_KT > least) {
 #pragma unroll
             for (int t = 0; t < 2; ++t)
@@ -866,10 +870,10 @@ __global__ __launch_bounds__(MANY_THREADS, 2) void many_rows_kernel(CacheView ca
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int v = 0; v < 16; ++v) tile_m = fmaxf(tile_m, s_acc[t][v]);
-        tile_m = fmaxf(tile_m, __shfl_xor(tile_m, 32));
-        const float new_m = fmaxf(run_m, tile_m);
+        const auto other = __builtin_amdgcn_permlane32_swap(__float_as_uint(tile_m), __float_as_uint(tile_m), false, false);
+        const float new_m = fmaxf(run_m, fmaxf(__uint_as_float(other[0]), __uint_as_float(other[1])));
         const float neg_m = new_m == -INFINITY ? 0.f : -new_m * scale_log2e;
-        float psum = 0.f;
+        float psum[4] = {};                   // (one chain of 32 sums would wait for itself)
         uint4 pf[4];
 #pragma unroll
         for (int t = 0; t < 2; ++t)
@@ -879,7 +883,7 @@ __global__ __launch_bounds__(MANY_THREADS, 2) void many_rows_kernel(CacheView ca
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     e[i] = __builtin_amdgcn_exp2f(fmaf(s_acc[t][hh * 8 + i], scale_log2e, neg_m));
-                    psum += e[i];
+                    psum[i & 3] += e[i];
                 }
                 pf[t * 2 + hh] = make_uint4(pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3]), pack_bf16x2(e[4], e[5]),
                                             pack_bf16x2(e[6], e[7]));
@@ -893,13 +897,11 @@ __global__ __launch_bounds__(MANY_THREADS, 2) void many_rows_kernel(CacheView ca
                 for (int v = 0; v < 16; ++v) o_acc[d][v] *= corr;
             run_m = new_m;
         }
-        run_l += psum;
+        run_l += (psum[0] + psum[1]) + (psum[2] + psum[3]);
 #pragma unroll
-        for (int d = 0; d < DB; ++d) {
-            const int row = d * 32 + fr, sw = many_swz<8>(row);
+        for (int ks = 0; ks < 4; ++ks)
 #pragma unroll
-            for (int ks = 0; ks < 4; ++ks) o_acc[d] = mfma32(Vc[row * 8 + ((ks * 2 + fg) ^ sw)], pf[ks], o_acc[d]);
-        }
+            for (int d = 0; d < DB; ++d) o_acc[d] = mfma32(tile[v_at[ks] + d * 32 * 8], pf[ks], o_acc[d]);
     }
     // ---- this lane: row my_row, dims d 32 + 8 (v / 4) + 4 fg + v % 4
     const float tot = run_l + __shfl_xor(run_l, 32);
