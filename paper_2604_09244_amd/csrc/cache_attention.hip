@@ -943,7 +943,7 @@ __global__ __launch_bounds__(MANY_THREADS, 2) void many_rows_kernel(CacheView ca
 // walks the rows, 16 at a time; the columns' sums go over the lanes of a group at the end.  No value is added twice or in
 // another order from run to run.
 // 8 x 32 heads of 128, 48 rows over up to 1840 slots 13 us, 22 MB of keys at 1.7 TB/s: latency of a few runs of slots a wave.
-// (512 rows of 4 x 32 heads over 2624 slots: 100 us.)
+// (512 rows of 4 x 32 heads over 2624 slots: 65 us; with two waves a SIMD instead of three 79.)
 constexpr int WEIGH_WAVES = 4, SOME_MOST = 96;
 
 // this lane's codes of the two K tiles of 32 slots
@@ -1083,7 +1083,7 @@ __global__ __launch_bounds__(WEIGH_WAVES * 64, 2) void weigh_some_kernel(CacheVi
 constexpr int WEIGH_CHUNK = 32;
 
 template <int DH>
-__global__ __launch_bounds__(WEIGH_WAVES * 64, 2) void weigh_many_kernel(CacheView cache, CacheAttention a, int group,
+__global__ __launch_bounds__(WEIGH_WAVES * 64, 3) void weigh_many_kernel(CacheView cache, CacheAttention a, int group,
                                                                       const float2* __restrict__ row_ml) {
     constexpr int STEPS = DH / 32, UNITS = DH / 8, LD = WEIGH_CHUNK * UNITS / (WEIGH_WAVES * 64);   // 16-byte pieces
     __shared__ uint4 sh_q[2][WEIGH_CHUNK / 16 * STEPS * 64];
@@ -1100,16 +1100,18 @@ __global__ __launch_bounds__(WEIGH_WAVES * 64, 2) void weigh_many_kernel(CacheVi
     WeighKeys<DH> raw[2];
 #pragma unroll
     for (int n = 0; n < 2; ++n) weigh_load<DH>(raw[n], cache, head, slot0 + 32 * n, span.len, c, g);
-    uint4 q_next[LD] = {};
+    static_assert(LD <= 2);
+    uint4 q0, q1;
     float2 ml_next = make_float2(0.f, 0.f);
     int sees_next = 0;
     auto fetch = [&](int r0) __attribute__((always_inline)) {   // (behind the last row: that row again)
-#pragma unroll
-        for (int i = 0; i < LD; ++i) {
-            const int id = i * WEIGH_WAVES * 64 + tid, r = min(r0 + id / UNITS, rows - 1), n = r / group;
-            q_next[i] = *reinterpret_cast<const uint4*>(a.q.p + b * a.q.sample + n * a.q.token +
-                                                        (h * group + r - n * group) * a.q.head + id % UNITS * 8);
-        }
+        auto piece = [&](int id) __attribute__((always_inline)) {
+            const int r = min(r0 + id / UNITS, rows - 1), n = group == 1 ? r : r / group;
+            return *reinterpret_cast<const uint4*>(a.q.p + b * a.q.sample + n * a.q.token + (h * group + r - n * group) * a.q.head +
+                                                   id % UNITS * 8);
+        };
+        q0 = piece(tid);
+        if constexpr (LD == 2) q1 = piece(WEIGH_WAVES * 64 + tid);
         if (tid < WEIGH_CHUNK) {
             const int r = r0 + tid;
             const float2 ml = row_ml[head * rows + min(r, rows - 1)];
@@ -1118,12 +1120,13 @@ __global__ __launch_bounds__(WEIGH_WAVES * 64, 2) void weigh_many_kernel(CacheVi
         }
     };
     auto put = [&](int stage) __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < LD; ++i) {
+        auto piece = [&](int id, const uint4& q) __attribute__((always_inline)) {
             // piece u of a row: the values of lane group u / STEPS in product step u % STEPS
-            const int id = i * WEIGH_WAVES * 64 + tid, r = id / UNITS, u = id % UNITS;
-            sh_q[stage][((r >> 4) * STEPS + u % STEPS) * 64 + u / STEPS * 16 + (r & 15)] = q_next[i];
-        }
+            const int r = id / UNITS, u = id % UNITS;
+            sh_q[stage][((r >> 4) * STEPS + u % STEPS) * 64 + u / STEPS * 16 + (r & 15)] = q;
+        };
+        piece(tid, q0);
+        if constexpr (LD == 2) piece(WEIGH_WAVES * 64 + tid, q1);
         if (tid < WEIGH_CHUNK) sh_ml[stage][tid] = ml_next, sh_sees[stage][tid] = sees_next;
     };
     // (from the first query that sees any of the workgroup's slots on)
