@@ -96,6 +96,24 @@ def test_a_cold_start_leaves_all_rows_in_every_cache():
     plan.ctx.close()
 
 
+def test_pruning_before_any_layer_leaves_kept_rows_everywhere():
+    wl, L = TINY, 2
+    plan, w = _plan(wl, L, 0)
+    x, pos = W.hidden_states(wl, device="cuda")
+    want = plan.run(x, pos, None, on_the_fly=True).clone()
+    n = wl.k_total + wl.nt
+    caches = [garbage_cache(wl.B, wl.H, wl.dh, n + 32) for _ in range(L)]
+    got = plan.run(x, pos, None, on_the_fly=True, caches=(mv.Cache4C * L)(*[c._c for c in caches]))
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
+    at, kept = plan.prune["pos"], plan.prune["kept_idx"].cpu()
+    for c in caches:
+        assert (c.pos[:, :, :n] == at[:, None]).all() and (c.pos[:, :, n:] == -77).all()
+    for b in range(wl.B):
+        _check_rows(caches[0], b, to64(x[b])[kept[b].numpy()], at[b].cpu().numpy(), oracle_weights(w[0]), wl, f"sample {b}")
+    plan.ctx.close()
+
+
 def _decode(plan, caches, x, pos, length, n_new=None, max_length=None, accumulate=1, h=None):
     B, n, D = x.shape
     h = h or [torch.empty_like(x) for _ in range(2)]
