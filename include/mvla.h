@@ -496,8 +496,8 @@ typedef struct {
 } mvla_rows;
 
 /* Bytes of a context's workspace that the calls below need for caches of B samples, H
- * query and H_kv key heads of dh values, up to n_q queries a call and max_length slots
- * (not less than mvla_create asks for).  A context that runs other calls as well takes
+ * query and H_kv key heads of dh values, up to n_q queries a call and max_length slots:
+ * any call of 1 .. n_q queries (not less than mvla_create asks for).  A context that runs other calls as well takes
  * the largest of their needs.  0 for arguments that no call takes. */
 size_t mvla_cache_workspace_bytes(int B, int H, int H_kv, int dh, int n_q, int max_length);
 
@@ -567,8 +567,8 @@ int mvla_prefill_cached(mvla_ctx* ctx, const mvla_layer_cfg* cfg, const mvla_lay
                         const float* key_bias, const mvla_prefill_buffers* buffers,
                         const mvla_cache4* caches, void** y_out, int* rows_out);
 
-/* Bytes of workspace for mvla_decode_step on n tokens of B samples over caches of up to
- * max_length slots, and for mvla_cache_evict on them.  0 for arguments that it refuses. */
+/* Bytes of workspace for mvla_decode_step on up to n tokens of B samples over caches of up
+ * to max_length slots, and for mvla_cache_evict on them.  0 for arguments that it refuses. */
 size_t mvla_decode_workspace_bytes(int B, int n, int D, int H, int F, int max_length);
 
 /* The layers on n new tokens a sample, in order: norm, q/k/v projection with rotation by

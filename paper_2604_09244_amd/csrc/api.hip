@@ -1130,7 +1130,7 @@ int mvla_score_only(mvla_ctx* ctx, const mvla_layer_cfg* cfg, const mvla_layer_w
 size_t mvla_cache_workspace_bytes(int B, int H, int H_kv, int dh, int n_q, int max_length) {
     if (B <= 0 || H <= 0 || H_kv <= 0 || H % H_kv != 0 || n_q <= 0 || max_length <= 0) return 0;
     if (dh != 64 && dh != 128) return 0;
-    const size_t attention = cache_attention_bytes(B, H, H_kv, dh, n_q, max_length, true);
+    const size_t attention = cache_attention_most_bytes(B, H, H_kv, dh, n_q, max_length);
     const size_t evict = (size_t)B * H_kv * max_length * 4;
     return kCounterBytes + gemm_partial_bytes() + align_up(attention > evict ? attention : evict, 256) + 256;
 }
@@ -1192,7 +1192,7 @@ size_t mvla_decode_workspace_bytes(int B, int n, int D, int H, int F, int max_le
     if (B <= 0 || n <= 0 || D <= 0 || H <= 0 || F <= 0 || D % H != 0 || max_length <= 0) return 0;
     if (D / H != 64 && D / H != 128) return 0;
     const size_t over = align_up(layer_buffers(nullptr, B, n, D, F).bytes, 256) +
-                        cache_attention_bytes(B, H, H, D / H, n, max_length, true);
+                        cache_attention_most_bytes(B, H, H, D / H, n, max_length);
     const size_t evict = (size_t)B * H * max_length * 4;
     return kCounterBytes + gemm_partial_bytes() + align_up(over > evict ? over : evict, 256) + 256;
 }

@@ -1183,7 +1183,7 @@ AttentionPlan attention_plan(int B, int H, int H_kv, int dh, int n_q, int max_le
     // 128 68 / 62; 16 samples over 2624 slots 48 rows 61 / 105, 96 116 / 111, 112 166 / 118.  Two column tiles against three
     // there: 32 rows 20 / 24, 48 37 / 26, 64 38 / 46, 96 54 / 47: as few blocks of rows as there can be, then the smaller ones.
     p.kind = p.rows <= FEW_ROWS ? FEW : p.rows <= SOME_MOST ? SOME : MANY;
-    p.tiles = p.rows <= 32 || (p.rows > 48 && p.rows <= 64) ? 2 : 3;
+    p.tiles = p.rows <= 32 || (p.rows > 48 && p.rows <= 64) ? 2 : 3;   // (cache_attention_most_bytes knows these ends)
     p.pitch = (max_len + FEW_STEP - 1) / FEW_STEP * FEW_STEP;
     const int cus = device_cu_count();
     const int64_t heads = (int64_t)B * H_kv, steps = p.pitch / FEW_STEP;
@@ -1321,6 +1321,23 @@ int run_attention(const CacheView& c, const CacheAttention& a, const AttentionPl
 
 size_t cache_attention_bytes(int B, int H, int H_kv, int dh, int n_q, int max_len, bool accumulate) {
     return attention_plan(B, H, H_kv, dh, n_q, max_len, accumulate).bytes();
+}
+
+// The largest of that for 1 .. n_q queries.  It is not n_q's own: fewer rows take another path, or have fewer blocks of them and
+// so more splits.  Between two numbers of rows that end a path or a block it grows with the rows, and from where blocks alone
+// fill the chip (no splits) on it does so too; with the length it always does.
+size_t cache_attention_most_bytes(int B, int H, int H_kv, int dh, int n_q, int max_len) {
+    const int64_t group = H / H_kv, rows = (int64_t)n_q * group, heads = (int64_t)B * H_kv, fill = 2 * (int64_t)device_cu_count();
+    size_t most = cache_attention_bytes(B, H, H_kv, dh, n_q, max_len, true);
+    auto up_to = [&](int64_t end) {
+        if (end < rows && end >= group) most = std::max(most, cache_attention_bytes(B, H, H_kv, dh, (int)(end / group), max_len, true));
+    };
+    for (int end : {FEW_ROWS, 32, 48, 64, SOME_MOST}) up_to(end);
+    for (int64_t block = 1; block * MANY_ROWS < rows; ++block) {
+        up_to(block * MANY_ROWS);
+        if (block * heads >= fill && block * MANY_ROWS >= group) break;
+    }
+    return most;
 }
 
 int launch_cache_attention(const CacheView& c, const CacheAttention& a, char* scratch, hipStream_t st) {

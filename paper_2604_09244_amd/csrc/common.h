@@ -200,6 +200,7 @@ struct CacheAttention {
     float scale;
 };
 size_t cache_attention_bytes(int B, int H, int H_kv, int dh, int n_q, int max_len, bool accumulate);
+size_t cache_attention_most_bytes(int B, int H, int H_kv, int dh, int n_q, int max_len);   // of up to n_q queries
 int launch_cache_attention(const CacheView& c, const CacheAttention& a, char* scratch, hipStream_t st);
 
 // sample_kernels.hip
