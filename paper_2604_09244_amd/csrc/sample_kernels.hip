@@ -15,9 +15,9 @@
 //     to those and brings their tokens into a list, whose exact order shows the border.
 // What no list can take (a list that overflows because thousands of tokens are alike) is found digit by digit from
 // histograms over the row, place().
-// Weights are summed over neighbours that one lane reads together in 32 bits, in that order, and as whole numbers of
-// 2^-40 beyond, so that no sum depends on the order in which it was formed.  Bins' weights (32 bits, good to 3e-5) only say
-// where to look.
+// Each weight counts as a whole number of 2^-40, and sums are sums of these: none depends on the order in which it was
+// formed, on where the row lies or on how many workgroups it has.  Bins' weights (32 bits, good to 3e-5) only say where to
+// look.
 //
 // Long rows are dealt out over the chip, a slice a workgroup, in three launches: largest logits (and weights by bins),
 // list and tiles, choice.  Short ones take one workgroup and one launch, their tokens in registers.
@@ -41,7 +41,7 @@ constexpr int SAMPLE_LIST = 14336;        // tokens on the list: 112 of the 160 
 constexpr int ONE_WORKGROUP = 32768;
 constexpr int SLICE_THREADS = 256, SLICE_MAXIMA = 128;
 constexpr int SLICE_EACH = 12;            // tokens of a thread that come to its row's list together (24 KiB of LDS)
-constexpr float SAMPLE_OCTAVES = 40.f;    // weights below 2^-40 of the largest count as none
+constexpr float SAMPLE_OCTAVES = 40.f;    // what the bins cover; weights below 2^-41 of the largest are no unit of 2^-40
 constexpr float LOWEST = -3.4028235e38f;  // (-inf never stays)
 
 // order-preserving bits of a logit that is a number
@@ -57,10 +57,20 @@ __device__ __forceinline__ u64 place_of(float x, uint32_t i) { return ((u64)logi
 __device__ __forceinline__ float place_logit(u64 p) { return key_logit((uint32_t)(p >> 32)); }
 __device__ __forceinline__ uint32_t place_index(u64 p) { return 0xffffffffu - (uint32_t)p; }
 
-__device__ __forceinline__ u64 whole(float w) {                 // w in [0, 16] as a whole number of 2^-40
-    const float h = __builtin_truncf(w * 0x1p16f);
-    return ((u64)(uint32_t)h << 24) + (uint32_t)fmaf(fmaf(w, 0x1p16f, -h), 0x1p24f, 0.5f);
-}
+// Weights as whole numbers of 2^-40.  Few of them at a time (up to 128, none above 2): high and low parts summed apart, each
+// exactly in 32 bits.
+struct Wholes {
+    float high = 0.f;                    // of 2^-16
+    uint32_t low = 0;                    // of 2^-40
+    static __device__ __forceinline__ Wholes of(float w) {      // (rounded to nearest)
+        const float h = __builtin_truncf(w * 0x1p16f);
+        return {h, (uint32_t)fmaf(fmaf(w, 0x1p16f, -h), 0x1p24f, 0.5f)};
+    }
+    __device__ __forceinline__ void add(const Wholes& w) { high += w.high, low += w.low; }
+    __device__ __forceinline__ void add(const Wholes& w, bool if_) { high += if_ ? w.high : 0.f, low += if_ ? w.low : 0u; }
+    __device__ __forceinline__ u64 sum() const { return ((u64)(uint32_t)high << 24) + low; }
+};
+__device__ __forceinline__ u64 whole(float w) { return Wholes::of(w).sum(); }
 
 template <typename T>
 struct Row {                             // a row in pieces of 16 bytes from the aligned address at or before its start
@@ -165,7 +175,7 @@ struct Settings {
     // octaves below the largest weight (NaN where that is no number); by halves, which no two logits are too far apart for
     __device__ __forceinline__ float octaves(float x) const { return fmaf(x, -0.5f, half_ref) * twice_per_t; }
     static __device__ __forceinline__ float weight(float oct) { return __builtin_amdgcn_exp2f(-oct); }
-    static __device__ __forceinline__ bool counts(float oct) { return oct < SAMPLE_OCTAVES; }
+    static __device__ __forceinline__ bool counts(float oct) { return oct <= SAMPLE_OCTAVES + 1.f; }   // (one unit at least)
     static __device__ __forceinline__ int bin_of(float oct) {
         return min((int)(oct * (SAMPLE_BINS / SAMPLE_OCTAVES)), SAMPLE_BINS - 1);
     }
@@ -511,10 +521,10 @@ __global__ __launch_bounds__(SLICE_THREADS) void sample_collect_kernel(const T* 
                 gather(x, in, j);
             }
             if (sum) {
-                float w = 0.f;
+                Wholes w;
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) w += fmaxf(s.weight(s.octaves(x[e])), 0.f);    // (no number: 0)
-                tile += whole(w);
+                for (int e = 0; e < VEC; ++e) w.add(Wholes::of(fmaxf(s.weight(s.octaves(x[e])), 0.f)));    // (no number: 0)
+                tile += w.sum();
             }
         }, [&](int t) {
             if (sum) {
@@ -572,18 +582,19 @@ __global__ __launch_bounds__(SLICE_THREADS) void sample_collect_kernel(const T* 
     }
     u64 all = 0, tile = 0;
     walk.run(row, [&](float (&x)[VEC], int j) {
-        float sure = 0.f, any = 0.f;
+        Wholes sure, any;
         bool in[VEC];
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
-            const float oct = s.octaves(x[e]), w = fmaxf(s.weight(oct), 0.f);
-            any += w;
-            sure += oct < first ? w : 0.f;
+            const float oct = s.octaves(x[e]);
+            const Wholes w = Wholes::of(fmaxf(s.weight(oct), 0.f));
+            any.add(w);
+            sure.add(w, oct < first);
             in[e] = oct >= first && oct < last;
         }
         gather(x, in, j);
-        all += whole(any);
-        tile += whole(sure);
+        all += any.sum();
+        tile += sure.sum();
     }, [&](int t) {
         tile = wave_total(tile);
         if (lane == 0) sc.tile_sum[(size_t)b * SAMPLE_BINS + t] = tile;
@@ -849,10 +860,10 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(const T* __restr
                 for (int e = 0; e < VEC; ++e) in[e] = x[e] >= low;
                 append_places<VEC>(x, in, row.first(j), &n_list, list, SAMPLE_LIST, lane);
                 if (sum) {
-                    float w = 0.f;
+                    Wholes w;
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) w += fmaxf(s.weight(s.octaves(x[e])), 0.f);    // (no number: 0)
-                    total += whole(w);
+                    for (int e = 0; e < VEC; ++e) w.add(Wholes::of(fmaxf(s.weight(s.octaves(x[e])), 0.f)));    // (no number: 0)
+                    total += w.sum();
                 }
             });
             if (sum) total = all_waves(wave_total(total));
@@ -1029,7 +1040,8 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(const T* __restr
             const Border x = border_of(about, tid, s.early(want)), y = border_of(about, tid, s.late(want));
             first = (float)(x.bin - 1) * WIDTH, last = (float)((y.bin < 0 ? SAMPLE_BINS : y.bin) + 2) * WIDTH;
         }
-        if (by_least && -__builtin_amdgcn_logf(s.least) < first) bordered = true;    // (min_p alone says what stays)
+        // (min_p alone says what stays; the hair is for the logarithm, and far less than the bin before the border)
+        if (by_least && -__builtin_amdgcn_logf(s.least) < first + 0x1p-10f) bordered = true;
         else {
             u64 total = 0;
             if (left_over) {
@@ -1044,21 +1056,21 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(const T* __restr
                 __syncthreads();
                 u64 tile = 0;
                 each_tile([&](float (&x)[VEC], int j) __attribute__((always_inline)) {
-                    float sure = 0.f, any = 0.f;
+                    Wholes sure, any;
                     const int left = border_i - row.first(j);
                     bool in[VEC];
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) {
                         const float oct = s.octaves(x[e]);
                         const bool ok = before_border(e, x[e], left);
-                        const float w = ok ? s.weight(oct) : 0.f;
-                        any += w;
-                        sure += oct < first ? w : 0.f;
+                        const Wholes w = Wholes::of(ok ? s.weight(oct) : 0.f);
+                        any.add(w);
+                        sure.add(w, oct < first);
                         in[e] = ok && oct >= first && oct < last;
                     }
                     append_places<VEC>(x, in, row.first(j), &n_list, list, SAMPLE_LIST, lane);
-                    total += whole(any);
-                    tile += whole(sure);
+                    total += any.sum();
+                    tile += sure.sum();
                 }, [&](int t) __attribute__((always_inline)) {
                     tile = wave_total(tile);
                     if (lane == 0) tile_sum[t] = tile;
@@ -1106,10 +1118,10 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(const T* __restr
             u64 tile = 0;
             each_tile([&](float (&x)[VEC], int j) __attribute__((always_inline)) {
                 const int left = border_i - row.first(j);
-                float sum = 0.f;
+                Wholes sum;
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) sum += mass_at(e, x[e], left);
-                tile += whole(sum);
+                for (int e = 0; e < VEC; ++e) sum.add(Wholes::of(mass_at(e, x[e], left)));
+                tile += sum.sum();
             }, [&](int t) __attribute__((always_inline)) {
                 tile = wave_total(tile);
                 if (lane == 0) tile_sum[t] = tile;
@@ -1121,45 +1133,40 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(const T* __restr
     const u64 total = all_waves(wave_total(tile_sum[tid])), aim = aim_of(total);
     const Border in = border_of(tile_sum[tid], tid, aim + 1);
     if (wave != 0) return;
-    // (a tile's sum and that of its pieces may differ in the last 2^-40 where the border's tokens were added: the last
-    // token that stays then)
+    // (some piece passes the aim: the pieces' sums are the tile's)
     u64 before = in.before;
-    int last = -1;
-    float last_w = 0.f;
     for (int q = 0; q < row.steps; ++q) {
         const int j = (in.bin * row.steps + q) * 64 + lane, i0 = row.first(j);
-        float x[VEC], v[VEC], sum = 0.f;
+        float x[VEC];
+        Wholes v[VEC];
+        Wholes sum;
 #pragma unroll
         for (int e = 0; e < VEC; ++e) x[e] = NAN;
         if (j < row.pieces) row.load(j, x);
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
-            v[e] = mass_at(e, x[e], border_i - i0);
-            sum += v[e];
-            if (v[e] > 0.f) last = i0 + e, last_w = v[e];
+            v[e] = Wholes::of(mass_at(e, x[e], border_i - i0));
+            sum.add(v[e]);
         }
-        const u64 m = whole(sum), inc = wave_running(m);
+        const u64 m = sum.sum(), inc = wave_running(m);
         const u64 past = __ballot(before + inc > aim);
         if (past) {
             if (lane == __ffsll(past) - 1) {
                 const u64 left = aim - (before + inc - m);
-                float run = 0.f, w = 0.f;
+                Wholes run;
+                u64 w = 0;
                 int at = -1;
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
-                    run += v[e];
-                    if (at < 0 && whole(run) > left) at = e, w = v[e];
+                    run.add(v[e]);
+                    if (at < 0 && run.sum() > left) at = e, w = v[e].sum();
                 }
-                choose(i0 + at, (double)w * 0x1p40 / (double)total);
+                choose(i0 + at, (double)w / (double)total);
             }
             return;
         }
         before += __shfl(inc, 63);
     }
-    int end = last;
-#pragma unroll
-    for (int o = 32; o; o >>= 1) end = max(end, __shfl_xor(end, o));
-    if (last == end && last >= 0) choose(last, (double)last_w * 0x1p40 / (double)total);
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------
