@@ -471,8 +471,10 @@ int mvla_masked_prefill_step(mvla_ctx* ctx, const mvla_layer_cfg* cfg,
  * value and one power of two a block.
  *   code  sign (bit 3) and magnitude 0, 1/2, 1, 3/2, 2, 3, 4, 6 (codes 0 .. 7); value
  *         2i of a row in the low, value 2i+1 in the high half of byte i
- *   power byte e: 2^(e - 127); 255: every value of the block is NaN
- * A value is level * power, which bf16 holds exactly.  The rows are packed; the number
+ *   power byte e <= 252: 2^(e - 127); 255: every value of the block is NaN
+ * A value is level * power, which bf16 holds exactly.  (No call writes 253 or 254, whose
+ * larger levels bf16 does not hold: they read as infinities there, and attention may take
+ * all of such a block as NaN.)  The rows are packed; the number
  * of slots in use is not part of the cache but an argument (device int32 [B]) of the
  * calls, so that layers can share it and a step can be captured into a graph.
  * All pointers are device pointers, caller-owned; k, v, k_scale, v_scale 16-byte
@@ -504,8 +506,9 @@ size_t mvla_cache_workspace_bytes(int B, int H, int H_kv, int dh, int n_q, int m
 /* Write new key and value rows into a cache: row i < c_b of sample b goes to slot
  * length[b] - c_b + i, with c_b = n_new[b] (n for n_new = NULL; clamped to [0, n]):
  * `length` counts the new rows already.  Per block of 32 values, the power is the
- * smallest 2^(e-127), e >= 0, under which the largest magnitude is below 7; each value
- * is rounded to the nearest level, ties to the even code.  A block that holds an
+ * smallest 2^(e-127), 0 <= e <= 252, under which the largest magnitude is below 7 (252
+ * where none is); each value is rounded to the nearest level, ties to the even code:
+ * finite values stay finite.  A block that holds an
  * infinity or a NaN is written as NaN throughout.  The rows' pos is set and their
  * weight cleared; rows that would fall outside [0, capacity) are not written.
  * k, v  : bf16 [B, n, H_kv, dh] by their strides.  channel == 1 with 16-byte aligned

@@ -17,7 +17,7 @@ def fp4_encode(x):
             powers[at] = 255
             continue
         e = 0
-        while np.max(np.abs(y)) >= 7.0 * 2.0 ** (e - 127):
+        while e < 252 and np.max(np.abs(y)) >= 7.0 * 2.0 ** (e - 127):    # (a level of 252 is below 2^128)
             e += 1
         powers[at] = e
         a = np.abs(y) / 2.0 ** (e - 127)

@@ -122,12 +122,6 @@ struct FewRows {
     }
 };
 
-// whether one of a word's bytes is 255 (the test for a byte of zeros, of the complement)
-__device__ __forceinline__ bool some_byte_ff(uint32_t w) {
-    const uint32_t n = ~w;
-    return ((n - 0x01010101u) & ~n & 0x80808080u) != 0;
-}
-
 // Values of dims 2 E and 2 E + 1 (of a lane's CH) of its eight slots, as operands: codes become pairs of dims of one slot,
 // two permutes turn two slots' pairs into pairs of slots of one dim.
 struct FewPairs {
@@ -229,16 +223,17 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void few_rows_kerne
                     x.vs[i] = 0x7f7f7f7fu;
                 }
             }
-            // a new row whose values are no numbers reaches the rows that see it, not those before it
+            // a new row whose values are no numbers (or may be infinite: powers that append never writes, taken alike)
+            // reaches the rows that see it, not those before it
             bool any = false;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) any |= some_byte_ff(x.vs[i]);
+            for (int i = 0; i < 8; ++i) any |= fp4_some_unbounded(x.vs[i]);
             if (__any(any)) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
 #pragma unroll
                     for (int blk = 0; blk < NB; ++blk)
-                        if (((x.vs[i] >> (8 * blk)) & 0xffu) == 0xffu) {
+                        if (fp4_unbounded((x.vs[i] >> (8 * blk)) & 0xffu)) {
                             if (my0 + i < limit) not_a_number |= 1u << blk;
                             if (blk == v_blk) {
                                 x.v[i] = 0;
@@ -468,14 +463,14 @@ __global__ __launch_bounds__(SOME_WAVES * 64) void some_rows_kernel(CacheView ca
                     x.v[i] = 0;
                     x.vs[i] = 0x7f7f7f7fu;
                 }
-                any |= some_byte_ff(x.vs[i]);
+                any |= fp4_some_unbounded(x.vs[i]);
             }
             if (__any(any)) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
 #pragma unroll
                     for (int blk = 0; blk < NB; ++blk)
-                        if (((x.vs[i] >> (8 * blk)) & 0xffu) == 0xffu) {
+                        if (fp4_unbounded((x.vs[i] >> (8 * blk)) & 0xffu)) {
 #pragma unroll
                             for (int ct = 0; ct < CT; ++ct)
                                 if (my0 + i < limit_of(ct)) not_a_number |= 1u << (ct * NB + blk);
@@ -773,7 +768,7 @@ __global__ __launch_bounds__(MANY_THREADS, 2) void many_rows_kernel(CacheView ca
             uint32_t bad = 0;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const bool none = kt * MANY_KT + v_oct * 8 + i >= span.len, nan = x.vs[i] == 0xffu;
+                const bool none = kt * MANY_KT + v_oct * 8 + i >= span.len, nan = fp4_unbounded(x.vs[i]);
                 if (nan && !none) bad |= 1u << i;
                 if (none || nan) {
                     x.v[i] = 0;

@@ -25,7 +25,8 @@ __device__ __forceinline__ uint4 fp4_values(uint32_t codes, float scale) {
                       fp4_pair<3>(codes, scale));
 }
 
-// eight bf16 values (finite, below 7 * scale in magnitude) as a word of codes, rounded to nearest, ties to the even code
+// eight bf16 values (finite) as a word of codes, rounded to nearest, ties to the even code; from 7 * scale on in magnitude,
+// which only the largest power meets, the largest level
 __device__ __forceinline__ uint32_t fp4_codes(const uint4& x, float scale) {
     uint32_t c = 0;
     c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2_t, x.x), scale, 0);
@@ -36,11 +37,20 @@ __device__ __forceinline__ uint32_t fp4_codes(const uint4& x, float scale) {
 }
 
 // Exponent byte of a block whose largest magnitude has the bf16 bits `top` (sign off): the smallest power under which
-// it stays below 7 (from 7 on, 6 would no longer be the nearest level); 255 where it is no finite number.
+// it stays below 7 (from 7 on, 6 would no longer be the nearest level), but none above FP4_LARGEST, whose levels are the
+// last that all stay below 2^128; 255 where it is no finite number.
+constexpr uint32_t FP4_LARGEST = 252;
 __device__ __forceinline__ uint32_t fp4_exponent(uint32_t top) {
     if (top >= 0x7f80u) return 255u;
     const int e = (int)(top >> 7) - 2 + ((top & 0x7fu) >= 0x60u ? 1 : 0);
-    return e < 0 ? 0u : (uint32_t)e;
+    return e < 0 ? 0u : min((uint32_t)e, FP4_LARGEST);
+}
+
+// whether a block of this power may hold what is no finite number
+__device__ __forceinline__ bool fp4_unbounded(uint32_t power) { return power > FP4_LARGEST; }
+// ... one of the four of a word of powers (low seven bits from 125 on carry into the top one, which has to be set already)
+__device__ __forceinline__ bool fp4_some_unbounded(uint32_t powers) {
+    return (((powers & 0x7f7f7f7fu) + 0x03030303u) & powers & 0x80808080u) != 0;
 }
 
 }  // namespace mvla
