@@ -21,9 +21,9 @@ class Answer:
     evicts every layer down to that many rows a head (positions below ``first_pos`` and the last
     ``n_recent`` ones stay).  Nothing is allocated and nothing waits on the device in a step.
 
-    The plan's rotary table has to cover the answer's positions (``rope_len``) and its context the
-    workspace (``Context(..., min_bytes=Answer.workspace_bytes(...))``).  ``room``: the longest
-    answer."""
+    The plan's rotary table has to cover the prompt's and the answer's positions (``rope_len`` of
+    S + room at least) and its context the workspace (``Context(...,
+    min_bytes=Answer.workspace_bytes(...))``).  ``room``: the longest answer."""
 
     @staticmethod
     def workspace_bytes(B: int, S: int, D: int, H: int, F: int, room: int) -> int:
@@ -35,6 +35,9 @@ class Answer:
     def __init__(self, plan: mv.PrefillPlan, room: int, budget: Optional[int] = None,
                  first_pos: int = 0, n_recent: int = 0):
         assert room >= 1 and (budget is None or budget >= 1) and n_recent >= 0
+        if plan.rope[0].shape[0] < plan.S + room:    # (later positions would be rotated as the last one of the table)
+            raise ValueError(f"the plan's rotary table (rope_len) has {plan.rope[0].shape[0]} positions, an answer of "
+                             f"{room} tokens needs {plan.S + room}")
         self.plan, self.room, self.budget = plan, room, budget
         self.first_pos, self.n_recent = first_pos, n_recent
         B, L, cfg, dev = plan.B, plan.L, plan.cfg, plan.ctx.device

@@ -1,0 +1,27 @@
+"""What an answer's loop refuses, and what a refusal leaves."""
+import pytest
+import torch
+
+from paper_2604_09244_amd import binding as mv
+from paper_2604_09244_amd import workloads as W
+from paper_2604_09244_amd.answer import Answer
+from helpers import layer_cfg
+from test_gpu_answer import TINY
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("rope_len", [None, TINY.S + 7])
+def test_a_rotary_table_that_ends_before_the_answer(rope_len):
+    """Positions behind the table would all be rotated as its last one."""
+    wl = TINY
+    ctx = mv.Context(wl.B, wl.S, wl.D, wl.H, wl.F, wl.nt,
+                     min_bytes=Answer.workspace_bytes(wl.B, wl.S, wl.D, wl.H, wl.F, 8))
+    layers = [mv.pack_layer(W.layer_weights(wl, l, device="cuda")) for l in range(2)]
+    plan = mv.PrefillPlan(ctx, layer_cfg(wl), layers, wl.B, wl.n2, wl.n3, wl.nt, wl.k_total, 1, rope_base=wl.rope_base,
+                          rope_len=rope_len)
+    with pytest.raises(ValueError, match="rope_len"):
+        Answer(plan, 8)
+    if rope_len:
+        Answer(plan, 7)                         # (its positions are there)
+    ctx.close()
