@@ -61,7 +61,8 @@ class Answer:
                 **options):
         """The plan's pruned prefill; returns the kept tokens' hidden states [B, S', D].  An action
         iteration's cold start prunes nothing and does not fit: smoothed steps count from 2."""
-        assert options.get("smooth_step", 0) != 1, "a cold start leaves every layer unpruned"
+        if options.get("smooth_step", 0) == 1:
+            raise ValueError("a cold start leaves every layer unpruned: its rows do not fit an answer's caches")
         y = self.plan.run(x, pos, key_bias, caches=self._cache_array, **options)
         self.length.copy_(self._start)
         self._bound = list(self.rows)

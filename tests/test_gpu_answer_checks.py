@@ -6,7 +6,7 @@ from paper_2604_09244_amd import binding as mv
 from paper_2604_09244_amd import workloads as W
 from paper_2604_09244_amd.answer import Answer
 from helpers import layer_cfg
-from test_gpu_answer import TINY
+from test_gpu_answer import TINY, _plan
 
 pytestmark = pytest.mark.gpu
 
@@ -25,3 +25,16 @@ def test_a_rotary_table_that_ends_before_the_answer(rope_len):
     if rope_len:
         Answer(plan, 7)                         # (its positions are there)
     ctx.close()
+
+
+def test_a_cold_start_is_refused_by_an_error():
+    """(not by an assertion, which an optimised interpreter leaves out)"""
+    plan, _ = _plan(TINY, 2, 1)
+    loop = Answer(plan, 4)
+    x, pos = W.hidden_states(TINY, device="cuda")
+    with pytest.raises(ValueError, match="cold start"):
+        loop.prefill(x, pos, None, smooth_step=1)
+    with pytest.raises(RuntimeError):           # nothing was filled
+        loop.step(x[:, :1].contiguous(), pos[:, :1].contiguous())
+    loop.prefill(x, pos, None, smooth_step=2)
+    plan.ctx.close()
