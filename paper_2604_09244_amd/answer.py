@@ -80,14 +80,19 @@ class Answer:
         B = plan.B
         assert mv._dev(x, torch.bfloat16).shape == (B, 1, plan.cfg.D)
         assert mv._dev(pos, torch.int32).shape == (B, 1)
-        self._taken += 1
-        self._bound = [b + 1 for b in self._bound]
+        bound = [b + 1 for b in self._bound]
         self.length += 1
         y = C.c_void_p()
-        mv._check(mv.load().mvla_decode_step(
-            ctx.handle, C.byref(plan.cfg), plan._layer_array, self._cache_array, plan.L,
-            x.data_ptr(), pos.data_ptr(), B, 1, None, self.length.data_ptr(), max(self._bound), 1,
-            self._h_array, C.byref(y)), "mvla_decode_step")
+        try:
+            mv._check(mv.load().mvla_decode_step(
+                ctx.handle, C.byref(plan.cfg), plan._layer_array, self._cache_array, plan.L,
+                x.data_ptr(), pos.data_ptr(), B, 1, None, self.length.data_ptr(), max(bound), 1,
+                self._h_array, C.byref(y)), "mvla_decode_step")
+        except mv.MvlaError:
+            self.length -= 1     # (refused before anything ran: the answer is where it was)
+            raise
+        self._taken += 1
+        self._bound = bound
         if self.budget is not None:
             if self.n_recent:
                 torch.sub(pos[:, 0], self.n_recent - 1, out=self._recent)

@@ -38,3 +38,28 @@ def test_a_cold_start_is_refused_by_an_error():
         loop.step(x[:, :1].contiguous(), pos[:, :1].contiguous())
     loop.prefill(x, pos, None, smooth_step=2)
     plan.ctx.close()
+
+
+def test_a_refused_step_leaves_the_answer_as_it_was():
+    """A step that the library refuses (its input lies in the buffer that a step writes) counts for nothing."""
+    outs, lengths = [], []
+    x, pos = W.hidden_states(TINY, device="cuda")
+    for refuse in (False, True):
+        plan, _ = _plan(TINY, 2, 1)
+        loop = Answer(plan, 3, 40)
+        last = loop.prefill(x, pos, None, on_the_fly=True)[:, -1:].contiguous()
+        at = torch.full((TINY.B, 1), TINY.S, dtype=torch.int32, device="cuda")
+        run = []
+        for t in range(3):
+            y = loop.step(last, at)
+            if refuse:
+                before = loop.length.clone()
+                with pytest.raises(mv.MvlaError if t < 2 else RuntimeError):
+                    loop.step(y, at)
+                assert torch.equal(loop.length, before)
+            last = y.clone()
+            run.append(last)
+            at += 1
+        outs.append(torch.stack(run)), lengths.append(loop.length.clone())
+        plan.ctx.close()
+    assert torch.equal(outs[0], outs[1]) and torch.equal(lengths[0], lengths[1])
