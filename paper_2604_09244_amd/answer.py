@@ -45,6 +45,9 @@ class Answer:
         self.rows = [plan.S if l < plan.p else plan.S_kept for l in range(L)]
         # a step adds its row before it evicts, so a budget needs one row more than it keeps
         most = [r + room if budget is None else max(r, min(budget, r + room)) + 1 for r in self.rows]
+        # (a step's rows are in the caches when its eviction asks for workspace: too late to refuse)
+        if plan.ctx.workspace.numel() < self.workspace_bytes(B, max(most), cfg.D, cfg.H, cfg.F, 0):
+            raise mv.MvlaError(-2, "Answer")
         self.caches = [mv.Cache4.empty(B, cfg.H, cfg.dh, m, dev) for m in most]
         self._cache_array = (mv.Cache4C * L)(*[c._c for c in self.caches])
         self.length, self._other = torch.zeros(L, B, **i32), torch.zeros(L, B, **i32)

@@ -63,3 +63,17 @@ def test_a_refused_step_leaves_the_answer_as_it_was():
         outs.append(torch.stack(run)), lengths.append(loop.length.clone())
         plan.ctx.close()
     assert torch.equal(outs[0], outs[1]) and torch.equal(lengths[0], lengths[1])
+
+
+def test_a_context_without_the_steps_workspace():
+    """Refused before an answer starts, not at a step of it."""
+    wl = TINY
+    ctx = mv.Context(wl.B, wl.S, wl.D, wl.H, wl.F, wl.nt)
+    layers = [mv.pack_layer(W.layer_weights(wl, l, device="cuda")) for l in range(2)]
+    plan = mv.PrefillPlan(ctx, layer_cfg(wl), layers, wl.B, wl.n2, wl.n3, wl.nt, wl.k_total, 1, rope_base=wl.rope_base,
+                          rope_len=wl.S + 60000)
+    assert ctx.workspace.numel() < Answer.workspace_bytes(wl.B, wl.S, wl.D, wl.H, wl.F, 60000)
+    with pytest.raises(mv.MvlaError, match="workspace"):
+        Answer(plan, 60000)
+    Answer(plan, 60000, 200)                    # (under a budget the caches stay short)
+    ctx.close()
