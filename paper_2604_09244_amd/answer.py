@@ -48,17 +48,22 @@ class Answer:
         # (a step's rows are in the caches when its eviction asks for workspace: too late to refuse)
         if plan.ctx.workspace.numel() < self.workspace_bytes(B, max(most), cfg.D, cfg.H, cfg.F, 0):
             raise mv.MvlaError(-2, "Answer")
-        self.caches = [mv.Cache4.empty(B, cfg.H, cfg.dh, m, dev) for m in most]
-        self._cache_array = (mv.Cache4C * L)(*[c._c for c in self.caches])
-        self.length, self._other = torch.zeros(L, B, **i32), torch.zeros(L, B, **i32)
-        self._start = torch.tensor(self.rows, **i32)[:, None].expand(L, B).contiguous()
-        self._recent = torch.zeros(B, **i32)
-        if budget is not None:
-            self._budgets = [min(budget, c.capacity) for c in self.caches]
-            self._kept = [torch.empty(B, cfg.H, b, **i32) for b in self._budgets]
-        self._h = [torch.empty(B, 1, cfg.D, dtype=torch.bfloat16, device=dev) for _ in range(2)]
+        with self._on_stream():
+            self.caches = [mv.Cache4.empty(B, cfg.H, cfg.dh, m, dev) for m in most]
+            self._cache_array = (mv.Cache4C * L)(*[c._c for c in self.caches])
+            self.length, self._other = torch.zeros(L, B, **i32), torch.zeros(L, B, **i32)
+            self._start = torch.tensor(self.rows, **i32)[:, None].expand(L, B).contiguous()
+            self._recent = torch.zeros(B, **i32)
+            if budget is not None:
+                self._budgets = [min(budget, c.capacity) for c in self.caches]
+                self._kept = [torch.empty(B, cfg.H, b, **i32) for b in self._budgets]
+            self._h = [torch.empty(B, 1, cfg.D, dtype=torch.bfloat16, device=dev) for _ in range(2)]
         self._h_array = (C.c_void_p * 2)(*[t.data_ptr() for t in self._h])
         self._bound = None       # by layer, what its length cannot exceed; None before the prefill
+
+    def _on_stream(self):
+        """The context's stream, for what torch does between the library's calls on it."""
+        return torch.cuda.stream(self.plan.ctx.stream)
 
     def prefill(self, x: torch.Tensor, pos: torch.Tensor, key_bias: Optional[torch.Tensor] = None,
                 **options):
@@ -67,7 +72,8 @@ class Answer:
         if options.get("smooth_step", 0) == 1:
             raise ValueError("a cold start leaves every layer unpruned: its rows do not fit an answer's caches")
         y = self.plan.run(x, pos, key_bias, caches=self._cache_array, **options)
-        self.length.copy_(self._start)
+        with self._on_stream():
+            self.length.copy_(self._start)
         self._bound = list(self.rows)
         self._taken = 0
         return y
@@ -84,7 +90,8 @@ class Answer:
         assert mv._dev(x, torch.bfloat16).shape == (B, 1, plan.cfg.D)
         assert mv._dev(pos, torch.int32).shape == (B, 1)
         bound = [b + 1 for b in self._bound]
-        self.length += 1
+        with self._on_stream():
+            self.length += 1
         y = C.c_void_p()
         try:
             mv._check(mv.load().mvla_decode_step(
@@ -92,13 +99,15 @@ class Answer:
                 x.data_ptr(), pos.data_ptr(), B, 1, None, self.length.data_ptr(), max(bound), 1,
                 self._h_array, C.byref(y)), "mvla_decode_step")
         except mv.MvlaError:
-            self.length -= 1     # (refused before anything ran: the answer is where it was)
+            with self._on_stream():
+                self.length -= 1     # (refused before anything ran: the answer is where it was)
             raise
         self._taken += 1
         self._bound = bound
         if self.budget is not None:
             if self.n_recent:
-                torch.sub(pos[:, 0], self.n_recent - 1, out=self._recent)
+                with self._on_stream():
+                    torch.sub(pos[:, 0], self.n_recent - 1, out=self._recent)
             for l, cache in enumerate(self.caches):
                 ctx.cache_evict(cache, cache, self.length[l], self._budgets[l], self.first_pos,
                                 self._recent if self.n_recent else None, self._bound[l],

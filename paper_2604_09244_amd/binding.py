@@ -301,8 +301,8 @@ class Context:
         lib = load()
         self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
         self._h = C.c_void_p()
-        stream = torch.cuda.current_stream(self.device).cuda_stream
-        _check(lib.mvla_create(C.byref(self._h), self.device.index or 0, stream,
+        self.stream = torch.cuda.current_stream(self.device)     # the one that the calls run on
+        _check(lib.mvla_create(C.byref(self._h), self.device.index or 0, self.stream.cuda_stream,
                                self.workspace.data_ptr(), nbytes), "mvla_create")
         self._rope = {}
 
@@ -323,6 +323,7 @@ class Context:
 
     def set_stream(self, stream: torch.cuda.Stream):
         _check(load().mvla_set_stream(self._h, stream.cuda_stream), "mvla_set_stream")
+        self.stream = stream
 
     # ---- timing ----------------------------------------------------------
     def profile_enable(self, kernel_ids: Optional[Sequence[int]], max_records: int = 4096):

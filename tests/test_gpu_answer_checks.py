@@ -77,3 +77,35 @@ def test_a_context_without_the_steps_workspace():
         Answer(plan, 60000)
     Answer(plan, 60000, 200)                    # (under a budget the caches stay short)
     ctx.close()
+
+
+def test_an_answer_whose_context_has_another_stream():
+    """Called under one stream, with a context bound to another that is busy: what a step does to its lengths waits for
+    the steps before it, as everything else of it does."""
+    x, pos = W.hidden_states(TINY, device="cuda")
+    tokens = torch.randn(4, TINY.B, 1, TINY.D, generator=torch.Generator().manual_seed(2)).to(torch.bfloat16).cuda()
+    at = [torch.full((TINY.B, 1), TINY.S + t, dtype=torch.int32, device="cuda") for t in range(4)]
+    a = torch.randn(8192, 8192, device="cuda")
+    runs = []
+    for busy in (False, True):
+        plan, _ = _plan(TINY, 2, 1)
+        loop = Answer(plan, 4, 40, n_recent=2)
+        side = torch.cuda.Stream()
+        torch.cuda.synchronize()
+        plan.ctx.set_stream(side)
+        outs = []
+        for turn in range(2):
+            if busy:
+                with torch.cuda.stream(side):
+                    for _ in range(4):
+                        b = a @ a               # (milliseconds of work before the prefill)
+            loop.prefill(x, pos, None, on_the_fly=True)
+            for t in range(4):
+                y = loop.step(tokens[t], at[t])
+                with torch.cuda.stream(side):
+                    outs.append(y.clone())
+        torch.cuda.synchronize()
+        runs.append((torch.stack(outs), loop.length.clone(), [c.pos[:, :, :40].clone() for c in loop.caches]))
+        plan.ctx.close()
+    for got, want in zip(runs[1], runs[0]):
+        assert all(torch.equal(g, w) for g, w in zip(got, want)) if isinstance(got, list) else torch.equal(got, want)
