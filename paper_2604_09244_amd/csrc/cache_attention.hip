@@ -603,6 +603,7 @@ __global__ __launch_bounds__(SOME_WAVES * 64) void some_rows_kernel(CacheView ca
 // Workgroup (x, key head, sample): the workgroups of a head share out its rows' outputs, and runs of 1024 slots whose
 // weights they add to the rows' own, from the logits that the pass over the cache left behind.
 constexpr int JOIN_THREADS = 256, JOIN_SLOTS = 1024, JOIN_ROWS = 16, MAX_SPLITS = 64;
+typedef float f32x4_any_t __attribute__((ext_vector_type(4), aligned(4)));   // weights start at any four bytes
 
 __global__ __launch_bounds__(JOIN_THREADS) void join_kernel(CacheView cache, CacheAttention a, int group, int splits,
                                                             const float* __restrict__ part_o, const float2* __restrict__ part_ml,
@@ -653,8 +654,8 @@ __global__ __launch_bounds__(JOIN_THREADS) void join_kernel(CacheView cache, Cac
     if (!logits) return;
     for (int slot = (blockIdx.x * JOIN_THREADS + tid) * 4; slot < span.len; slot += gridDim.x * JOIN_SLOTS) {
         float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-        float4* w = reinterpret_cast<float4*>(cache.weight + head * cache.capacity + slot);
-        float4 old = *w;
+        f32x4_any_t* w = reinterpret_cast<f32x4_any_t*>(cache.weight + head * cache.capacity + slot);
+        f32x4_any_t old = *w;
 #pragma unroll 4
         for (int r = 0; r < rows; ++r) {
             const int sees = seen_by(span, r / group);
