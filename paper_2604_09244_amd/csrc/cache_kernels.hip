@@ -181,9 +181,15 @@ int launch_cache_read(const CacheView& c, const int32_t* first, int n, bf16_t* k
 constexpr int EVICT_THREADS = 512, EVICT_WAVES = EVICT_THREADS / 64, EVICT_BINS = 2048, EVICT_FEW = 128;
 constexpr int EVICT_LDS = 16384;
 
-__device__ __forceinline__ uint32_t evict_key(float w, int pos, int first_pos, int recent_from) {
+// positions whose rows stay whatever their weight
+struct Staying {
+    int first_pos, recent_from;
+    bool recent;                                               // (else no position is)
+    __device__ __forceinline__ bool operator()(int pos) const { return pos < first_pos || (recent && pos >= recent_from); }
+};
+__device__ __forceinline__ uint32_t evict_key(float w, int pos, const Staying& stays) {
     const uint32_t bits = w > 0.f ? __float_as_uint(w) : 0u;   // (negative, NaN: as if nothing had looked at the row)
-    return bits | (pos < first_pos || pos >= recent_from ? 0x80000000u : 0u);
+    return bits | (stays(pos) ? 0x80000000u : 0u);
 }
 
 // 16 bytes of codes of a row, their scale byte, and its position or weight.  part: piece of the key row, then of the value
@@ -235,7 +241,7 @@ __global__ __launch_bounds__(EVICT_THREADS) void evict_select_kernel(CacheView c
     const int32_t* p = c.pos + row0;
     int32_t* out = kept + head * budget;
     int32_t* hole_mem = holes + head * min(budget, max_len);
-    const int recent = recent_from ? recent_from[b] : 0x7fffffff;
+    const Staying whatever = {first_pos, recent_from ? recent_from[b] : 0, recent_from != nullptr};
     if (h == 0 && tid == 0) len_out[b] = nb;
     auto move_rows = [&]() {
         if constexpr (MOVE_DH > 0) {
@@ -268,7 +274,7 @@ __global__ __launch_bounds__(EVICT_THREADS) void evict_select_kernel(CacheView c
     }
     auto key_of = [&](int i) __attribute__((always_inline)) {
         if constexpr (IN_LDS) return lds_rows[i];
-        else return evict_key(w[i], p[i], first_pos, recent);
+        else return evict_key(w[i], p[i], whatever);
     };
     // ---- key of the nb-th row
     uint32_t lo = 0xffffffffu, hi = 0;
@@ -280,13 +286,13 @@ __global__ __launch_bounds__(EVICT_THREADS) void evict_select_kernel(CacheView c
         for (int q = 0; q < 4; ++q) weight[q] = w[i1 + q * EVICT_THREADS], pos[q] = p[i1 + q * EVICT_THREADS];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            const uint32_t key = evict_key(weight[q], pos[q], first_pos, recent);
+            const uint32_t key = evict_key(weight[q], pos[q], whatever);
             if constexpr (IN_LDS) lds_rows[i1 + q * EVICT_THREADS] = key;
             lo = min(lo, key), hi = max(hi, key);
         }
     }
     for (; i1 < n; i1 += EVICT_THREADS) {
-        const uint32_t key = evict_key(w[i1], p[i1], first_pos, recent);
+        const uint32_t key = evict_key(w[i1], p[i1], whatever);
         if constexpr (IN_LDS) lds_rows[i1] = key;
         lo = min(lo, key), hi = max(hi, key);
     }
