@@ -38,3 +38,44 @@ def test_weights_at_any_four_bytes(B, H, H_kv, dh, n_q, T, shift):
     kept, new = ctx.cache_evict(cache, cache, ints(*(T,) * B), max(1, T // 2))
     assert (new == max(1, T // 2)).all() and (pos[:shift] == -7).all() and (pos[shift + before.numel():] == -7).all()
     ctx.close()
+
+
+def backwards(t, dims):
+    """The rows description of t [B, n, H, dh] with the axes `dims` walked from their ends."""
+    flipped = t.flip(dims).contiguous()
+    at, stride = flipped.data_ptr(), list(flipped.stride())
+    for d in dims:
+        at += 2 * (t.shape[d] - 1) * stride[d]
+        stride[d] = -stride[d]
+    return mv.Rows(at, *stride), flipped
+
+
+@pytest.mark.parametrize("dims", [(0,), (1,), (2,), (0, 1, 2)])
+@pytest.mark.parametrize("n_q,H,H_kv,dh", [(1, 4, 2, 128), (9, 2, 2, 64), (40, 2, 1, 128), (130, 2, 2, 64)])
+def test_rows_that_are_walked_backwards(n_q, H, H_kv, dh, dims):
+    rng = np.random.default_rng(n_q)
+    lib, B, T = mv.load(), 2, 200
+    ctx = context(B, H, H_kv, n_q, 224, dh)
+    k, v, q = bf16(rng, B, T, H_kv, dh), bf16(rng, B, T, H_kv, dh), bf16(rng, B, n_q, H, dh).cuda()
+    pos = torch.arange(T, dtype=torch.int32).repeat(B, 1).cuda()
+    length = ints(T, T - 30)
+    caches = [mv.Cache4.empty(B, H_kv, dh, 224) for _ in range(3)]
+    for c in caches:
+        for t in (c.k, c.v, c.k_scale, c.v_scale, c.weight):
+            t.zero_()
+    ctx.cache_append(caches[0], k.cuda(), v.cuda(), pos, ints(T, T))
+    for c, channels in ((caches[1], ()), (caches[2], (3,))):       # (channels backwards: the form that takes any)
+        (kr, k_held), (vr, v_held) = backwards(k.cuda(), dims + channels), backwards(v.cuda(), dims)
+        assert lib.mvla_cache_append(ctx.handle, c._ref, mv.C.byref(kr), mv.C.byref(vr), pos.data_ptr(), T, None,
+                                     ints(T, T).data_ptr()) == 0
+        torch.cuda.synchronize()
+        for name in ("k", "v", "k_scale", "v_scale"):
+            assert torch.equal(getattr(c, name), getattr(caches[0], name)), (name, channels)
+    want = ctx.cache_attention(caches[0], q, length, max_length=T, accumulate=True)
+    qr, q_held = backwards(q, dims)
+    out_r, out = backwards(torch.zeros_like(want), dims)
+    assert lib.mvla_cache_attention(ctx.handle, caches[1]._ref, mv.C.byref(qr), H, n_q, None, length.data_ptr(), T, dh ** -0.5, 1,
+                                    mv.C.byref(out_r)) == 0
+    torch.cuda.synchronize()
+    assert torch.equal(out.flip(dims), want) and torch.equal(caches[1].weight, caches[0].weight)
+    ctx.close()
