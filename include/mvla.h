@@ -482,7 +482,7 @@ int mvla_masked_prefill_step(mvla_ctx* ctx, const mvla_layer_cfg* cfg,
 typedef struct {
     int B, H_kv;       /* samples, key heads                                            */
     int dh;            /* head dim: 64 or 128                                           */
-    int capacity;      /* slots per sample, a multiple of 32                            */
+    int capacity;      /* slots per sample, a multiple of 32, at most 2^30              */
     void* k;           /* uint8 [B, H_kv, capacity, dh/2]  codes                        */
     void* v;           /* uint8 [B, H_kv, capacity, dh/2]                               */
     void* k_scale;     /* uint8 [B, H_kv, capacity, dh/32] powers                       */

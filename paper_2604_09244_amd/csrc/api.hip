@@ -416,13 +416,14 @@ int mvla_rope_table(mvla_ctx* ctx, double base, int rope_len, int dh, float* cos
 
 namespace {
 
-constexpr int kMaxGrid = 65535;   // of the second and third launch axes
+constexpr int kMaxGrid = 65535;     // of the second and third launch axes
+constexpr int kMaxSlots = 1 << 30;  // of a cache: the kernels step through slots in 32 bits, past the last one too
 
 int check_cache(const mvla_cache4* c) {
     if (!c || !c->k || !c->v || !c->k_scale || !c->v_scale || !c->pos || !c->weight) return MVLA_EINVAL;
     if (c->B <= 0 || c->H_kv <= 0 || c->capacity <= 0 || c->capacity % 32 != 0) return MVLA_EINVAL;
     if (c->dh != 64 && c->dh != 128) return MVLA_EUNSUPPORTED;
-    if (c->B > kMaxGrid || c->H_kv > kMaxGrid / 2) return MVLA_EUNSUPPORTED;
+    if (c->B > kMaxGrid || c->H_kv > kMaxGrid / 2 || c->capacity > kMaxSlots) return MVLA_EUNSUPPORTED;
     if (!aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->k_scale, 16) || !aligned(c->v_scale, 16) ||
         !aligned(c->pos, 4) || !aligned(c->weight, 4))
         return MVLA_EINVAL;
@@ -1130,6 +1131,7 @@ int mvla_score_only(mvla_ctx* ctx, const mvla_layer_cfg* cfg, const mvla_layer_w
 size_t mvla_cache_workspace_bytes(int B, int H, int H_kv, int dh, int n_q, int max_length) {
     if (B <= 0 || H <= 0 || H_kv <= 0 || H % H_kv != 0 || n_q <= 0 || max_length <= 0) return 0;
     if (dh != 64 && dh != 128) return 0;
+    if (B > kMaxGrid || H_kv > kMaxGrid / 2 || max_length > kMaxSlots || (int64_t)n_q * (H / H_kv) > 128 * (int64_t)kMaxGrid) return 0;
     const size_t attention = cache_attention_most_bytes(B, H, H_kv, dh, n_q, max_length);
     const size_t evict = (size_t)B * H_kv * max_length * 4;
     return kCounterBytes + gemm_partial_bytes() + align_up(attention > evict ? attention : evict, 256) + 256;
@@ -1191,6 +1193,7 @@ int mvla_cache_attention(mvla_ctx* ctx, const mvla_cache4* cache, const mvla_row
 size_t mvla_decode_workspace_bytes(int B, int n, int D, int H, int F, int max_length) {
     if (B <= 0 || n <= 0 || D <= 0 || H <= 0 || F <= 0 || D % H != 0 || max_length <= 0) return 0;
     if (D / H != 64 && D / H != 128) return 0;
+    if (B > kMaxGrid || H > kMaxGrid / 2 || max_length > kMaxSlots || n > 128 * kMaxGrid) return 0;
     const size_t over = align_up(layer_buffers(nullptr, B, n, D, F).bytes, 256) +
                         cache_attention_most_bytes(B, H, H, D / H, n, max_length);
     const size_t evict = (size_t)B * H * max_length * 4;

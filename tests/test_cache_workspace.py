@@ -59,3 +59,13 @@ def test_a_context_of_layers_holds_steps_of_fewer_tokens():
         have = lib.mvla_decode_workspace_bytes(B, n, D, H, F, length)
         for fewer in smaller_calls(n, 1):
             assert lib.mvla_decode_workspace_bytes(B, fewer, D, H, F, length) <= have, (B, n, fewer)
+
+
+def test_sizes_that_no_call_takes():
+    size, layers = mv.load().mvla_cache_workspace_bytes, mv.load().mvla_decode_workspace_bytes
+    assert size(1, 1, 1, 64, 1, 1 << 30) > 0 and layers(1, 1, 64, 1, 64, 1 << 30) > 0
+    for bad in ((1, 1, 1, 64, 1, (1 << 30) + 32), (1, 1, 1, 64, 1, 2 ** 31 - 1), (1, 1, 1, 64, 128 * 65535 + 1, 64),
+                (1, 64, 1, 64, 2 ** 31 - 1, 64), (65536, 1, 1, 64, 1, 64), (1, 40000, 40000, 64, 1, 64)):
+        assert size(*bad) == 0, bad
+    for bad in ((1, 1, 64, 1, 64, 2 ** 31 - 1), (65536, 1, 64, 1, 64, 64), (1, 128 * 65535 + 1, 64, 1, 64, 64)):
+        assert layers(*bad) == 0, bad
