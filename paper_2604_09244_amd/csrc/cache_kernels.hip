@@ -470,19 +470,23 @@ static int evict_select(const CacheView& c, const CacheView& d, const int32_t* l
     return MVLA_OK;
 }
 
-// Whether the workgroups copy the rows themselves.  Into another cache that pays with workgroups for the chip, and with few
-// rows, where a second launch costs the caller 3 us as well: 32 heads, 64 of 128 rows 6.9 us against 8.8 with the second
-// launch, 1344 of 2624 20.0 / 17.8, 8192 of 16384 102 / 61; 1344 of 2624, 128 heads 24.5 / 24.7, 256 31.0 / 32.0.  In place fewer
-// rows move: 32 heads, 512 of 1024 10.2 / 12.4, 1344 of 2624 17.7 / 17.7, 8192 of 16384 64 / 52; 1344 of 2624, 128 heads 17.8 /
-// 18.9, 512 22.3 / 26.5.
-static bool evict_moves(const CacheView& c, bool in_place, int budget, int max_len) {
-    const int rows = budget < max_len ? budget : max_len, heads = c.B * c.H_kv, cus = device_cu_count();
-    return in_place ? heads >= cus / 4 || rows <= 1024 : heads >= cus * 3 / 4 || rows <= 512;
+// Whether the workgroups of `heads` heads copy the (up to) `rows` rows that stay themselves: no second launch, which costs the
+// caller 3 us as well, but their copy waits for the selection, and few workgroups copy slowly.  Themselves / by the second
+// launch, us on the device, heads of 128.  Into another cache, every row that stays: 32 heads 64 of 128 rows 6.6 / 7.6, 512 of 1024
+// 11.2 / 10.5, 1344 of 2624 21.6 / 16.8; 128 heads 1344 25.9 / 25.7; 192 heads 1344 28.9 / 30.8, 2048 of 4096 40.7 / 41.6, 4096 of
+// 8192 86 / 79; 384 heads 2048 73 / 69; 512 heads 1344 57 / 60, 8192 of 16384 391 / 376.  In place, fewer rows: 32 heads 512 of
+// 1024 11.2 / 12.0, 1344 of 2624 17.6 / 17.0, 8192 of 16384 61 / 51; 64 heads 1344 17.9 / 17.8, 2048 21.6 / 20.7, 8192 62 / 53; 128
+// heads 1344 17.9 / 18.3, 2048 21.9 / 22.0, 4096 35 / 34, 8192 68 / 60; 192 heads 1344 18.1 / 19.3, 4096 36 / 37, 8192 69 / 65;
+// 256 heads 4096 36 / 39, 8192 70 / 70; one row a head of 64 heads, 8192 of 8193, 42 / 34.
+bool cache_evict_moves(int heads, int rows, bool in_place) {
+    const int cus = device_cu_count();
+    if (in_place) return heads >= cus * 3 / 4 || rows <= (heads >= cus / 2 ? 2048 : 1024);
+    return rows <= (heads >= cus * 3 / 4 ? 1536 : 512);
 }
 
 int launch_cache_evict(const CacheView& c, const CacheView& d, const int32_t* len, int max_len, int budget, int first_pos,
                        const int32_t* recent_from, int32_t* len_out, int32_t* kept, int32_t* holes, hipStream_t st) {
-    const bool move = evict_moves(c, c.k == d.k, budget, max_len);
+    const bool move = cache_evict_moves(c.B * c.H_kv, budget < max_len ? budget : max_len, c.k == d.k);
 #define MVLA_EVICT(LDS, DH) evict_select<LDS, DH>(c, d, len, max_len, budget, first_pos, recent_from, len_out, kept, holes, st)
     const int rc = max_len <= EVICT_LDS ? (!move ? MVLA_EVICT(true, 0) : c.dh == 128 ? MVLA_EVICT(true, 128) : MVLA_EVICT(true, 64))
                                         : (!move ? MVLA_EVICT(false, 0) : c.dh == 128 ? MVLA_EVICT(false, 128) : MVLA_EVICT(false, 64));

@@ -193,6 +193,7 @@ int launch_cache_read(const CacheView& c, const int32_t* first, int n, bf16_t* k
 // c into d (the same cache: in place); holes: int32 scratch [B, H_kv, min(budget, max_len)]
 int launch_cache_evict(const CacheView& c, const CacheView& d, const int32_t* len, int max_len, int budget, int first_pos,
                        const int32_t* recent_from, int32_t* len_out, int32_t* kept, int32_t* holes, hipStream_t st);
+bool cache_evict_moves(int heads, int rows, bool in_place);
 struct CacheAttention {
     CacheRows q, out;
     const int32_t *len, *n_new;
