@@ -181,11 +181,16 @@ int launch_cache_read(const CacheView& c, const int32_t* first, int n, bf16_t* k
 constexpr int EVICT_THREADS = 512, EVICT_WAVES = EVICT_THREADS / 64, EVICT_BINS = 2048, EVICT_FEW = 128;
 constexpr int EVICT_LDS = 16384;
 
-// positions whose rows stay whatever their weight
+// Positions whose rows stay whatever their weight: those outside [first, last], with the recent ones all beyond `last`.
 struct Staying {
-    int first_pos, recent_from;
-    bool recent;                                               // (else no position is)
-    __device__ __forceinline__ bool operator()(int pos) const { return pos < first_pos || (recent && pos >= recent_from); }
+    int first, last;
+    __device__ __forceinline__ Staying(int first_pos, const int32_t* recent_from, int b) : first(first_pos), last(0x7fffffff) {
+        if (!recent_from) return;
+        const int recent = recent_from[b];
+        if (recent > (int)0x80000000) last = recent - 1;
+        else first = 0x7fffffff, last = (int)0x80000000;       // (every position)
+    }
+    __device__ __forceinline__ bool operator()(int pos) const { return pos < first || pos > last; }
 };
 __device__ __forceinline__ uint32_t evict_key(float w, int pos, const Staying& stays) {
     const uint32_t bits = w > 0.f ? __float_as_uint(w) : 0u;   // (negative, NaN: as if nothing had looked at the row)
@@ -241,7 +246,7 @@ __global__ __launch_bounds__(EVICT_THREADS) void evict_select_kernel(CacheView c
     const int32_t* p = c.pos + row0;
     int32_t* out = kept + head * budget;
     int32_t* hole_mem = holes + head * min(budget, max_len);
-    const Staying whatever = {first_pos, recent_from ? recent_from[b] : 0, recent_from != nullptr};
+    const Staying whatever(first_pos, recent_from, b);
     if (h == 0 && tid == 0) len_out[b] = nb;
     auto move_rows = [&]() {
         if constexpr (MOVE_DH > 0) {
