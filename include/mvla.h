@@ -552,7 +552,8 @@ int mvla_cache_attention(mvla_ctx* ctx, const mvla_cache4* cache, const mvla_row
  * ascending order.  (So a step that evicts one row moves at most one.)
  * dst may be src itself (in place), or a cache of another capacity >= budget that shares
  * no memory with it (all kept rows are copied; src is only read).
- * length: device int32 [B]; recent_from: device int32 [B] or NULL (no recent rows).
+ * length: device int32 [B], clamped to [0, max_length] (rows beyond are lost);
+ * recent_from: device int32 [B] or NULL (no recent rows).
  * length_out: device int32 [B], new lengths; must not be `length`.
  * kept: device int32 [B, H_kv, budget]: slot of src that each slot of dst holds, -1
  *       beyond the new length. */

@@ -19,7 +19,8 @@ class Answer:
     to the pruning step, the kept rows behind it); ``step`` runs the layers on one new token a
     sample, adds the attention that the cached rows get to their weights and, with a ``budget``,
     evicts every layer down to that many rows a head (positions below ``first_pos`` and the last
-    ``n_recent`` ones stay).  Nothing is allocated and nothing waits on the device in a step.
+    ``n_recent`` ones stay).  Nothing is allocated and nothing waits on the device in a step.  A
+    prefill leaves no weights: the first eviction goes by the attention of the first token alone.
 
     The plan's rotary table has to cover the prompt's and the answer's positions (``rope_len`` of
     S + room at least) and its context the workspace (``Context(...,

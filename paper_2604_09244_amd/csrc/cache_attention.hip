@@ -4,6 +4,12 @@
 // and one of the query heads that share a key head (r = query * group + head of the group); it sees the slots below
 // its limit.  Both products are computed transposed (S^T = K Q^T, O^T = V^T P^T), so that a lane's column is a row r
 // and the logits that a lane holds are the operand that the second product takes from it.
+//
+// Logits, maxima, sums, outputs until they are stored and weights are 32-bit.  The second product's operand is not: its
+// matrix instruction takes bf16 as the values are, so each probability is rounded by up to 2^-9 of itself (of no matter
+// for the sum and for the weights, which take it unrounded).  The errors of a row's slots are independent, and outputs are bf16
+// anyway: off by 0.0018 to 0.0021 of their RMS against 64 bits, 0.0017 of it the rounding of the outputs alone (1 to 512
+// queries, 237 to 16384 slots).  Two bf16 parts a probability would take the rest away, for a second product twice as long.
 #include "common.h"
 #include "fp4.h"
 #include "wave.h"
@@ -62,7 +68,8 @@ __device__ __forceinline__ uint32_t column_or(uint32_t x) {
 // 16 samples of 2624 slots 42 us, 4.6 TB/s; one sample of 237 6.3 us, the latency of its loads and of the join.  64 x 8
 // heads of four rows, up to 16384 slots of ragged samples: 168 us here and 34 in join_kernel, 3.9 TB/s of the codes and
 // weights alone, 4.7 with the logits.  (Turns of a few samples, so that their logits stay in the last-level cache, were
-// never faster and up to twice as slow.)
+// never faster and up to twice as slow.)  Heads of 64, a query each, with weights: 64 x 32 heads of 2624 slots 103 us, 64 x 8 of
+// 16384 166 us, 4.0 and 3.8 TB/s of codes, powers and weights.
 constexpr int FEW_STEP = 32, FEW_ROWS = 16;
 
 template <int DH>
@@ -679,7 +686,8 @@ __global__ __launch_bounds__(JOIN_THREADS) void join_kernel(CacheView cache, Cac
 // 128 rows a workgroup, 32 a wave, 64 slots at a time: the codes become bf16 once per workgroup on their way into LDS
 // (keys row by row, values transposed), two stages deep, the next tile's codes on their way meanwhile.
 // Bound by the issue of vector operations (softmax, codes to bf16) beside the matrix products: 4 x 32 heads of 128, 512 rows
-// over 2624 slots 106 us, 0.75 PFLOP/s, a little above the attention over bf16 keys at these lengths.  (The second product's
+// over 2624 slots 106 us a call among others, 0.75 PFLOP/s, a little above the attention over bf16 keys at these lengths;
+// traced by a profiler, where launches lie apart, 119 to 137.  (The second product's
 // accumulators in turn rather than one after the other 109 / 105; two waves' priorities by phase, or exponentials
 // between the products by the scheduler's groups, no faster.)
 constexpr int MANY_THREADS = 256, MANY_ROWS = 128, MANY_KT = 64;

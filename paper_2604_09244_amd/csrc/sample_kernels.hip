@@ -21,9 +21,10 @@
 //
 // Long rows are dealt out over the chip, a slice a workgroup, in three launches: largest logits (and weights by bins),
 // list and tiles, choice.  Short ones take one workgroup and one launch, their tokens in registers.
-// Bound: chains of passes and barriers with few rows, 10 to 30 operations a token and look with many.  96 rows of 131073
-// bf16 tokens, settings that differ by row: 12.5 + 16 + 11 us, one read of them at the rate of a copy is 5; without a
-// filter 23 us, top-k 26, min-p 24, top-p 58.  One row of 32768 fp32 tokens with all filters 13 us, greedy 7.
+// Bound: chains of passes and barriers with few rows, 10 to 35 operations a token and look with many.  96 rows of 131073
+// bf16 tokens, settings that differ by row: 12 + 16.5 + 11 us, one read of them at the rate of a copy is 5; without a
+// filter 24 us, top-k 24, min-p 24, top-p 58, greedy 14.  One row of 32768 fp32 tokens: top-k and top-p 12 us, no filter 14,
+// top-p alone 28, greedy 4.5.
 #include "common.h"
 #include "mfma.h"
 #include "wave.h"
@@ -35,9 +36,9 @@ typedef unsigned long long u64;    // (as atomics take it)
 constexpr int SAMPLE_THREADS = 1024, SAMPLE_WAVES = SAMPLE_THREADS / 64;
 constexpr int SAMPLE_BINS = 1024;         // of octaves below the largest weight, and at most so many tiles
 constexpr int SAMPLE_LIST = 14336;        // tokens on the list: 112 of the 160 KiB of LDS
-// Tokens of a row that one workgroup takes by itself.  Rows of fp32, one workgroup a row against slices, us, without a filter /
-// with top-k and top-p / top-p alone: 96 of 32768 tokens 14 14 30 / 17 20 31, of 65536 22 19 47 / 23 25 46; one of 32768
-// 13 13 29 / 15 19 27, of 49152 18 16 37 / 15 19 27.
+// Tokens of a row that one workgroup takes by itself.  Rows of fp32, one workgroup a row against slices, us, without a filter,
+// with top-k and top-p, with top-p alone: 96 of 32768 tokens 15 13 30 / 17 19 32, of 65536 24 16 46 / 23 24 46; one of 32768
+// 14 12 28 / 15 17 26, of 49152 19 14 35 / 15 17 26.
 constexpr int ONE_WORKGROUP = 32768;
 constexpr int SLICE_THREADS = 256, SLICE_MAXIMA = 128;
 constexpr int SLICE_EACH = 12;            // tokens of a thread that come to its row's list together (24 KiB of LDS)
@@ -1173,7 +1174,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(const T* __restr
 namespace {
 
 // Tokens of a slice: 16384, and down to 8192 while two workgroups a compute unit are not there; a row has at most 32 slices.
-// (One row of 131072 fp32 tokens, 8 slices against 16: no filter 19.5 / 15.0 us, top-p 37.2 / 29.5, top-k 22.7 / 21.0.)
+// (One row of 131072 fp32 tokens, 8 slices against 16: no filter 19.6 / 15.3 us, top-p 35.7 / 28.2, top-k 21.1 / 19.7.)
 constexpr int SLICE_TOKENS = 16384, SLICE_LEAST = 8192;
 
 // bytes of scratch a row, and where its parts lie for `rows` rows
