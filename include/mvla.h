@@ -539,7 +539,8 @@ int mvla_cache_read(mvla_ctx* ctx, const mvla_cache4* cache, const int32_t* firs
  * max_length: the largest length that the call has to expect, at most the capacity (it
  *         sizes the launch).  scale: finite, > 0.
  * Products of bf16 queries with the cache's exact values, 32-bit sums; probabilities are
- * rounded to bf16 for the second product only. */
+ * rounded to bf16 for the second product only.  Sums over slots are divided by the row's
+ * total at the end: values beyond 2^128 / max_length may overflow in them. */
 int mvla_cache_attention(mvla_ctx* ctx, const mvla_cache4* cache, const mvla_rows* q, int H, int n_q,
                          const int32_t* n_new, const int32_t* length, int max_length, float scale,
                          int accumulate, const mvla_rows* out);
