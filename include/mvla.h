@@ -612,6 +612,141 @@ int mvla_sample(mvla_ctx* ctx, const void* logits, int half, int64_t row_stride,
                 const float* u, int32_t* token, float* prob);
 
 /* ------------------------------------------------------------------------ */
+/* Many prompts: rotation, a cache in pages, attention over it, log         */
+/* probabilities                                                            */
+/* ------------------------------------------------------------------------ */
+
+/* Frequencies of a rotation, for long contexts too.  Pair i of the first `rotated` values
+ * of a head turns by pos * f_i, f_i = base^(-2i / rotated), where factor = 1.  Otherwise f_i becomes
+ *     f_i * (s_i + (1 - s_i) / factor),   s_i = clamp((trained f_i / (2 pi) - low_turns) / (high_turns - low_turns), 0, 1):
+ * waves that turn high_turns times and more within the `trained` positions stay, those that
+ * turn low_turns times or less are `factor` times longer, those between are in between.
+ * (low_turns >= any: trained f_0 / (2 pi) with high_turns above it lengthens all of them.)
+ * gain multiplies cosines and sines. */
+typedef struct {
+    double base;       /* > 0, finite                                                   */
+    double factor;     /* >= 1, finite                                                  */
+    double low_turns, high_turns, trained;   /* read where factor > 1: 0 <= low < high, trained > 0, finite */
+    double gain;       /* > 0, finite                                                   */
+    int rotated;       /* values of a head that take part: even, 2 .. 256               */
+} mvla_rotation;
+
+/* Fill a rotary table of these angles: cos_out, sin_out: device fp32 [rope_len, rotated/2],
+ * row = position, evaluated in fp64 and rounded to fp32 once.  With factor 1 and gain 1 as
+ * mvla_rope_table for dh = rotated. */
+int mvla_rotation_table(mvla_ctx* ctx, const mvla_rotation* how, int rope_len, float* cos_out,
+                        float* sin_out);
+
+/* Turn the pairs of queries and keys by their positions (what a layer's projection does to
+ * whole heads in halves, for rows from anywhere):
+ *     y1 = x1 c - x2 s,  y2 = x2 c + x1 s,   c, s: entry (pos, i) of the tables,
+ * pair i being values i and i + rotated/2 of a head (interleaved = 0) or 2i and 2i + 1
+ * (interleaved != 0); values from `rotated` on are copied.  inverse != 0: s is taken negative,
+ * which turns back (and is the transposed map).  fp32, rounded once.
+ * q, q_out: bf16 [B, n, H, dh], k, k_out: bf16 [B, n, H_kv, dh] by their strides; an output
+ * is either its input (same address and strides) or shares no memory with any input.
+ * k, k_out NULL: queries alone.  pos: device int32 [B, n], clamped to [0, rope_len).
+ * dh: 2 .. 256; rotated <= dh.  channel == 1 with 16-byte aligned rows, dh, and rotated (halves:
+ * rotated/2) multiples of 8, is the fast form, any other is taken as well. */
+int mvla_rotate(mvla_ctx* ctx, const mvla_rows* q, int H, const mvla_rows* q_out, const mvla_rows* k,
+                int H_kv, const mvla_rows* k_out, const int32_t* pos, int B, int n, int dh, int rotated,
+                int interleaved, int inverse, const float* rope_cos, const float* rope_sin, int rope_len);
+
+/* A layer's key/value cache in pages that sequences share out among themselves: a pool of
+ * n_pages pages, each of `page` slots, a slot a key and a value row of dh values a key head.
+ * bits 16: values as bf16.  bits 8: in blocks of 32 values, a code of 8 bits a value (sign,
+ *   four exponent bits of bias 7, three mantissa bits: up to 448; 0x7f and 0xff NaN) and one power of two a
+ *   block, byte e: 2^(e - 127), 255: every value of the block is NaN.  A value that a call
+ *   writes is code * power, which bf16 holds exactly.
+ * All pointers are device pointers, caller-owned, 16-byte aligned.  Slots not in use may hold
+ * anything. */
+typedef struct {
+    int n_pages;       /* 1 .. 2^30                                                     */
+    int H_kv;          /* key heads                                                     */
+    int dh;            /* head dim: 64 or 128                                           */
+    int page;          /* slots a page: 16, 32, 64, 128 or 256                          */
+    int bits;          /* 16 or 8                                                       */
+    void* k;           /* [n_pages, H_kv, page, dh] bf16, or uint8 codes                */
+    void* v;           /* the same                                                      */
+    void* k_scale;     /* bits 8: uint8 [n_pages, H_kv, page, dh/32] powers; else NULL  */
+    void* v_scale;
+} mvla_pages;
+
+/* The sequences of a batch.  Their new tokens lie packed in the rows of a call's tensors,
+ * sequence b's in rows start[b] .. start[b+1] - 1 (both clamped to [0, n], n the rows of the
+ * call; rows before the first and behind the last sequence are nobody's: not read, outputs left as
+ * they were).  Slot t of sequence b is row t % page of page table[b, t / page].  A page
+ * number outside [0, n_pages) is no page: rows for it are not written, its slots read as zero
+ * and are seen by no query.  Pages may be shared for reading; of two rows that one call writes
+ * to one slot, either's values may remain, or parts of both.
+ * length counts the new rows already; it is clamped to [0, table_pitch * page]. */
+typedef struct {
+    int B;                     /* sequences                                             */
+    const int32_t* start;      /* device int32 [B + 1], ascending                       */
+    const int32_t* length;     /* device int32 [B]: slots in use                        */
+    const int32_t* table;      /* device int32 [B, table_pitch]: pages                  */
+    int table_pitch;           /* entries a sequence, table_pitch * page <= 2^30        */
+} mvla_page_batch;
+
+/* Bytes of a context's workspace with which mvla_pages_attention on up to B sequences, n
+ * rows, max_q queries a sequence and max_length slots is fastest (not less than mvla_create
+ * asks for).  The call runs with any workspace: it splits long sequences over as many
+ * workgroups as the workspace has room for.  0 for arguments that no call takes. */
+size_t mvla_pages_workspace_bytes(int B, int H, int H_kv, int dh, int n, int max_q, int max_length);
+
+/* Write new key and value rows: row i of sequence b's count c_b = start[b+1] - start[b] goes
+ * to slot length[b] - c_b + i; slots below 0 or beyond the table are not written.
+ * bits 16: as they are.  bits 8: magnitudes of finite values are limited to 247 * 2^120; a
+ * block's power is the smallest 2^(e-127), 0 <= e, under which its largest magnitude is below
+ * 464; each value is rounded to the nearest code, ties to the even one: finite values stay
+ * finite.  A block that holds an infinity or a NaN is written as NaN throughout.
+ * k, v: bf16 [n, H_kv, dh] by their strides (`sample` is not used).  channel == 1 with
+ * 16-byte aligned rows is the fast form, any other is taken as well. */
+int mvla_pages_append(mvla_ctx* ctx, const mvla_pages* pages, const mvla_page_batch* batch, const mvla_rows* k,
+                      const mvla_rows* v, int n);
+
+/* Read rows back: slots first[b] .. first[b] + n - 1 of every sequence and key head as bf16.
+ * Slots below 0, beyond the table or without a page read as zero.  (batch->start and ->length
+ * are not used and may be NULL.)
+ * first: device int32 [B] or NULL (0).  k_out, v_out: device bf16 [B, H_kv, n, dh], 16-byte
+ * aligned. */
+int mvla_pages_read(mvla_ctx* ctx, const mvla_pages* pages, const mvla_page_batch* batch, const int32_t* first,
+                    int n, void* k_out, void* v_out);
+
+/* Attention of the new tokens over their sequences,
+ *     out = sum_t p_t v_t,   p = softmax_t(scale * q . k_t),   lse = log sum_t exp(scale * q . k_t),
+ * query head h reading key head h / (H / H_kv).  Query i of sequence b's c_b sees the slots
+ * t < length[b] - c_b + i + 1 (the new rows are the last ones and see each other causally).
+ * Rows that see nothing, or only logits of -infinity, are written as zeros, their lse as
+ * -infinity.  A slot that a query does not see has no part in its result, whatever it holds.
+ * q, out: bf16 [n, H, dh] by their strides (`sample` is not used), channel == 1, 16-byte aligned
+ *         rows; must not overlap.  lse: device fp32 [n, H] or NULL.
+ * max_q, max_length: bounds on the c_b and on length that size the launch; rows from max_q on are
+ *         left as they were, lengths are clamped to max_length.  scale: finite, > 0.
+ * Products of bf16 queries with the cache's values, 32-bit sums; probabilities are rounded to
+ * bf16 for the second product only.  Every sum has a fixed order for one workspace size. */
+int mvla_pages_attention(mvla_ctx* ctx, const mvla_pages* pages, const mvla_page_batch* batch, const mvla_rows* q,
+                         int H, int n, int max_q, int max_length, float scale, const mvla_rows* out, float* lse);
+
+/* Log probabilities of given tokens in each row of logits, the row's entropy and its most
+ * likely tokens, y_v = (x_v - max) / temperature - log sum_w exp((x_w - max) / temperature):
+ *   logprob[b, j] = y of tokens[b, j] (-infinity for a token outside [0, V)),
+ *   entropy[b] = -sum_v exp(y_v) y_v, in nats,
+ *   top_token[b, r], top_logprob[b, r]: the r-th token in descending order of logits (equal
+ *   logits: lower index first) and its y; where fewer than `top` logits are above -infinity, -1 and
+ *   -infinity.
+ * NaN logits count as -infinity; +inf ones share everything; a row without any logit above
+ * -infinity has log probabilities of -infinity and entropy 0.  temperature not above 0 (or
+ * NaN): the first token of the order has y = 0, all others -infinity (as mvla_sample chooses).
+ * logits: device, bf16 (half != 0) or fp32 [B, V], rows row_stride elements apart; V <= 2^22.
+ * temperature: device fp32 [B] or NULL (1).  tokens: device int32 [B, n_tokens], n_tokens >= 0.
+ * logprob: device fp32 [B, n_tokens].  entropy: device fp32 [B] or NULL.
+ * top: 0 .. 32; top_token: device int32 [B, top], top_logprob: device fp32 [B, top]. */
+int mvla_logprobs(mvla_ctx* ctx, const void* logits, int half, int64_t row_stride, int B, int V,
+                  const float* temperature, const int32_t* tokens, int n_tokens, float* logprob, float* entropy,
+                  int top, int32_t* top_token, float* top_logprob);
+
+/* ------------------------------------------------------------------------ */
 /* Measurement (the paper's overhead study, Table 4, reports the pruning    */
 /* method's own cost apart from the step latency; these calls give the same */
 /* split per kernel)                                                        */
@@ -629,12 +764,13 @@ int mvla_profile_enable(mvla_ctx* ctx, uint32_t kernel_mask, int max_records);
  * Clears the record list. */
 int mvla_profile_read(mvla_ctx* ctx, int capacity, int32_t* ids, int32_t* tags, float* ms,
                       int32_t* n_out);
-/* Name of kernel id 0..23 ("rmsnorm", "gemm_qkv", "score_probs",
+/* Name of kernel id 0..28 ("rmsnorm", "gemm_qkv", "score_probs",
  * "attention", "gemm_o", "rmsnorm_mlp", "gemm_gateup", "gemm_down", "salience",
  * "budget", "select", "compact", "rope_table", "prune_fused", "smooth",
  * "decompose", "feature_share", "candidate_masks", "mask_indices",
- * "cache_append", "cache_read", "cache_attention", "cache_evict", "sample"; the last
- * five may hold several launches), "?" otherwise.  In mvla_prefill and mvla_masked_prefill_step a "compact" of up to
+ * "cache_append", "cache_read", "cache_attention", "cache_evict", "sample", "rotate",
+ * "pages_append", "pages_read", "pages_attention", "logprobs"; the last ten may hold several
+ * launches), "?" otherwise.  In mvla_prefill and mvla_masked_prefill_step a "compact" of up to
  * 4 Mi kept values writes the next layer's first norm too; no "rmsnorm" follows.
  * Rows of up to 384 values may be normalised by the gate/up projection itself (as the
  * choice by size has it): no "rmsnorm_mlp" then, its time is in "gemm_gateup". */

@@ -29,6 +29,8 @@ EXPORTS = [
     "mvla_set_gemm_choice", "mvla_prefill", "mvla_peak_probe", "mvla_salience_noalloc", "mvla_masked_prefill_step",
     "mvla_cache_workspace_bytes", "mvla_cache_append", "mvla_cache_read", "mvla_cache_attention",
     "mvla_cache_evict", "mvla_sample", "mvla_prefill_cached", "mvla_decode_workspace_bytes", "mvla_decode_step",
+    "mvla_rotation_table", "mvla_rotate", "mvla_pages_workspace_bytes", "mvla_pages_append", "mvla_pages_read",
+    "mvla_pages_attention", "mvla_logprobs",
 ]
 
 
@@ -110,6 +112,26 @@ class Rows(C.Structure):
                 ("head", C.c_int64), ("channel", C.c_int64)]
 
 
+class Rotation(C.Structure):
+    """mvla_rotation."""
+    _fields_ = [("base", C.c_double), ("factor", C.c_double), ("low_turns", C.c_double),
+                ("high_turns", C.c_double), ("trained", C.c_double), ("gain", C.c_double),
+                ("rotated", C.c_int)]
+
+
+class PagesC(C.Structure):
+    """mvla_pages."""
+    _fields_ = [("n_pages", C.c_int), ("H_kv", C.c_int), ("dh", C.c_int), ("page", C.c_int),
+                ("bits", C.c_int), ("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p),
+                ("v_scale", C.c_void_p)]
+
+
+class PageBatchC(C.Structure):
+    """mvla_page_batch."""
+    _fields_ = [("B", C.c_int), ("start", C.c_void_p), ("length", C.c_void_p), ("table", C.c_void_p),
+                ("table_pitch", C.c_int)]
+
+
 PROBE_READ, PROBE_COPY, PROBE_MFMA, PROBE_LAUNCH = 0, 1, 2, 3
 
 
@@ -182,6 +204,15 @@ def load() -> C.CDLL:
     lib.mvla_decode_step.argtypes = [vp, C.POINTER(LayerCfg), C.POINTER(LayerWeightsC), cache, i, vp,
                                      vp, i, i, vp, vp, i, i, C.POINTER(vp), C.POINTER(vp)]
     lib.mvla_sample.argtypes = [vp, vp, i, C.c_int64, i, i, vp, vp, vp, vp, vp, vp, vp]
+    pages, batch = C.POINTER(PagesC), C.POINTER(PageBatchC)
+    lib.mvla_rotation_table.argtypes = [vp, C.POINTER(Rotation), i, vp, vp]
+    lib.mvla_rotate.argtypes = [vp, rows, i, rows, rows, i, rows, vp, i, i, i, i, i, i, vp, vp, i]
+    lib.mvla_pages_workspace_bytes.restype = sz
+    lib.mvla_pages_workspace_bytes.argtypes = [i] * 7
+    lib.mvla_pages_append.argtypes = [vp, pages, batch, rows, rows, i]
+    lib.mvla_pages_read.argtypes = [vp, pages, batch, vp, i, vp, vp]
+    lib.mvla_pages_attention.argtypes = [vp, pages, batch, rows, i, i, i, i, f, rows, vp]
+    lib.mvla_logprobs.argtypes = [vp, vp, i, C.c_int64, i, i, vp, vp, i, vp, vp, i, vp, vp]
     lib.mvla_profile_enable.argtypes = [vp, C.c_uint32, i]
     lib.mvla_profile_read.argtypes = [vp, i, vp, vp, vp, vp]
     lib.mvla_kernel_name.restype = C.c_char_p
@@ -262,6 +293,56 @@ class Cache4:
                    new((dh // 32,), u8), new((), torch.int32), new((), torch.float32))
 
 
+def _packed_rows(t: torch.Tensor) -> Rows:
+    """Description of a bf16 tensor [tokens, heads, dh] of any strides."""
+    assert t.is_cuda and t.dtype == torch.bfloat16 and t.dim() == 3, (t.device, t.dtype, t.shape)
+    return Rows(t.data_ptr(), 0, *t.stride())
+
+
+class PagedCache:
+    """A layer's key/value cache in pages (mvla_pages) and the tensors that it lies in: k, v
+    [n_pages, H_kv, page, dh] as bf16, or as uint8 codes with the blocks' powers k_scale, v_scale
+    [n_pages, H_kv, page, dh/32].  ``PagedCache.empty`` allocates them."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
+                 v_scale: Optional[torch.Tensor] = None):
+        self.bits = 16 if k_scale is None else 8
+        dt = torch.bfloat16 if self.bits == 16 else torch.uint8
+        self.n_pages, self.H_kv, self.page, self.dh = _dev(k, dt).shape
+        assert _dev(v, dt).shape == k.shape and (k_scale is None) == (v_scale is None)
+        for s in (k_scale, v_scale):
+            assert s is None or _dev(s, torch.uint8).shape == (*k.shape[:3], self.dh // 32), s.shape
+        assert all(s is None or s.device == k.device for s in (v, k_scale, v_scale))
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.device = k.device
+        self._c = PagesC(self.n_pages, self.H_kv, self.dh, self.page, self.bits, k.data_ptr(), v.data_ptr(),
+                         _ptr(k_scale), _ptr(v_scale))
+        self._ref = C.byref(self._c)
+
+    @classmethod
+    def empty(cls, n_pages: int, H_kv: int, dh: int, page: int = 64, bits: int = 8, device=None) -> "PagedCache":
+        """A pool of ``n_pages`` pages of ``page`` slots (16, 32, 64, 128 or 256), of 16 or 8 bits a value."""
+        assert bits in (16, 8), bits
+        new = lambda n, dt: torch.empty(n_pages, H_kv, page, n, dtype=dt, device=device or "cuda")
+        if bits == 16:
+            return cls(new(dh, torch.bfloat16), new(dh, torch.bfloat16))
+        return cls(*(new(n, torch.uint8) for n in (dh, dh, dh // 32, dh // 32)))
+
+
+class PageBatch:
+    """The sequences of a batch (mvla_page_batch): start int32 [B + 1] (where each one's new rows
+    begin in the packed tensors), length int32 [B] (slots in use, new rows counted), table int32
+    [B, entries] (the pages of each).  The tensors' values may change from call to call."""
+
+    def __init__(self, start: torch.Tensor, length: torch.Tensor, table: torch.Tensor):
+        self.B, pitch = _dev(table, torch.int32).shape
+        assert _dev(length, torch.int32).shape == (self.B,) and _dev(start, torch.int32).shape == (self.B + 1,)
+        assert start.device == length.device == table.device
+        self.start, self.length, self.table, self.device = start, length, table, table.device
+        self._c = PageBatchC(self.B, start.data_ptr(), length.data_ptr(), table.data_ptr(), pitch)
+        self._ref = C.byref(self._c)
+
+
 class Context:
     """Owns a device workspace and a library context bound to the current stream.
     ``min_bytes``: at least so much workspace (the cache's calls: see ``cache_bytes``)."""
@@ -291,6 +372,27 @@ class Context:
         """A context for the calls on caches (and the token choice) alone: no layer runs in it."""
         self = cls.__new__(cls)
         nbytes = cls.cache_bytes(B, H, H_kv, n_q, max_length, dh)
+        if not torch.cuda.is_available():
+            raise RuntimeError("no GPU visible: the HIP path has no CPU fallback")
+        self.device = torch.device("cuda", torch.cuda.current_device()) if device is None else device
+        self._create(nbytes)
+        return self
+
+    @staticmethod
+    def pages_bytes(B: int, H: int, H_kv: int, n: int, max_q: int, max_length: int, dh: int) -> int:
+        """mvla_pages_workspace_bytes."""
+        nbytes = load().mvla_pages_workspace_bytes(B, H, H_kv, dh, n, max_q, max_length)
+        if nbytes == 0:
+            raise MvlaError(-1, "mvla_pages_workspace_bytes")
+        return nbytes
+
+    @classmethod
+    def for_pages(cls, B: int, H: int, H_kv: int, n: int, max_q: int, max_length: int, dh: int,
+                  device: Optional[torch.device] = None) -> "Context":
+        """A context for the calls on caches in pages, rotation and log probabilities alone: no layer
+        runs in it.  Up to B sequences, n rows in all, max_q a sequence, max_length slots."""
+        self = cls.__new__(cls)
+        nbytes = cls.pages_bytes(B, H, H_kv, n, max_q, max_length, dh)
         if not torch.cuda.is_available():
             raise RuntimeError("no GPU visible: the HIP path has no CPU fallback")
         self.device = torch.device("cuda", torch.cuda.current_device()) if device is None else device
@@ -664,6 +766,124 @@ class Context:
                                   _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p),
                                   u.data_ptr(), token.data_ptr(), _ptr(prob)), "mvla_sample")
         return token, prob
+
+    # ---- many prompts -----------------------------------------------------------
+    def _new(self, shape, dtype) -> torch.Tensor:
+        """An output: memory of the stream that the calls run on, also where another one is current."""
+        if torch.cuda.current_stream(self.device) == self.stream:
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        with torch.cuda.stream(self.stream):
+            return torch.empty(shape, dtype=dtype, device=self.device)
+
+    def rotary_table(self, rotated: int, rope_len: int, base: float = 10000.0, factor: float = 1.0,
+                     low_turns: float = 1.0, high_turns: float = 4.0, trained: float = 8192.0, gain: float = 1.0):
+        """(cos, sin) fp32 [rope_len, rotated/2] for ``rotate``.  ``factor`` > 1 lengthens the waves that
+        turn less than high_turns times within the trained positions, up to ``factor`` times those that
+        turn low_turns times or less; ``gain`` multiplies both tables."""
+        c, s = (self._new((rope_len, rotated // 2), torch.float32) for _ in range(2))
+        how = Rotation(base, factor, low_turns, high_turns, trained, gain, rotated)
+        _check(load().mvla_rotation_table(self._h, C.byref(how), rope_len, c.data_ptr(), s.data_ptr()),
+               "mvla_rotation_table")
+        return c, s
+
+    def rotate(self, q: torch.Tensor, k: Optional[torch.Tensor], pos: torch.Tensor, rope, interleaved: bool = False,
+               inverse: bool = False, out=None):
+        """Queries q [..., H, dh] and keys k [..., H_kv, dh] (bf16, any strides; [B, n, ...] or packed
+        [n, ...]; k may be None) turned by their positions pos (int32 [B, n] or [n]) with the tables
+        ``rope`` = (cos, sin).  ``out``: (q_out, k_out), also the inputs themselves.  Returns (q_out, k_out)."""
+        cos, sin = rope
+        rows = _packed_rows if q.dim() == 3 else _rows
+        B, n = (1, q.shape[0]) if q.dim() == 3 else q.shape[:2]
+        H, dh = q.shape[-2:]
+        assert _dev(pos, torch.int32).shape == q.shape[:-2] and q.device == pos.device == self.device
+        assert k is None or (k.shape[:-2] == q.shape[:-2] and k.shape[-1] == dh and k.device == q.device), k.shape
+        assert _dev(cos, torch.float32).shape == _dev(sin, torch.float32).shape and cos.device == q.device
+        if out is None:
+            out = (self._new(q.shape, torch.bfloat16), None if k is None else self._new(k.shape, torch.bfloat16))
+        q_out, k_out = out
+        assert q_out.shape == q.shape and q_out.device == q.device
+        assert (k is None) == (k_out is None) and (k is None or (k_out.shape == k.shape and k_out.device == k.device))
+        ref = lambda t: None if t is None else C.byref(rows(t))
+        _check(load().mvla_rotate(self._h, ref(q), H, ref(q_out), ref(k), 0 if k is None else k.shape[-2], ref(k_out),
+                                  pos.data_ptr(), B, n, dh, 2 * cos.shape[1], int(interleaved), int(inverse),
+                                  cos.data_ptr(), sin.data_ptr(), cos.shape[0]), "mvla_rotate")
+        return q_out, k_out
+
+    def pages_append(self, cache: PagedCache, batch: PageBatch, k: torch.Tensor, v: torch.Tensor):
+        """Write rows k, v [n, H_kv, dh] (bf16, any strides), packed as ``batch.start`` says, as the last
+        ones of each sequence's ``length`` (which counts them already)."""
+        n, H, dh = k.shape
+        assert k.shape == v.shape and (H, dh) == (cache.H_kv, cache.dh), (k.shape, v.shape)
+        assert k.device == v.device == cache.device == batch.device == self.device
+        _check(load().mvla_pages_append(self._h, cache._ref, batch._ref, C.byref(_packed_rows(k)),
+                                        C.byref(_packed_rows(v)), n), "mvla_pages_append")
+
+    def pages_read(self, cache: PagedCache, batch: PageBatch, first: Optional[torch.Tensor], n: int, out=None):
+        """Rows first[b] .. first[b] + n - 1 (first None: from 0) of each sequence as bf16 (k, v)
+        [B, H_kv, n, dh]."""
+        assert first is None or (_dev(first, torch.int32).shape == (batch.B,) and first.device == self.device)
+        assert cache.device == batch.device == self.device
+        shape = (batch.B, cache.H_kv, n, cache.dh)
+        k, v = (self._new(shape, torch.bfloat16) for _ in range(2)) if out is None else out
+        assert _dev(k, torch.bfloat16).shape == _dev(v, torch.bfloat16).shape == shape
+        assert k.device == v.device == self.device
+        _check(load().mvla_pages_read(self._h, cache._ref, batch._ref, _ptr(first), n, k.data_ptr(), v.data_ptr()),
+               "mvla_pages_read")
+        return k, v
+
+    def pages_attention(self, cache: PagedCache, batch: PageBatch, q: torch.Tensor, max_q: Optional[int] = None,
+                        max_length: Optional[int] = None, scale: Optional[float] = None, with_lse: bool = False,
+                        out=None):
+        """Attention of the new tokens q [n, H, dh] (bf16, packed as ``batch.start`` says) over their
+        sequences' cached rows.  ``max_q``, ``max_length``: bounds on a sequence's new rows and on
+        ``length`` (default: n, the table's).  Returns out [n, H, dh], or (out, lse fp32 [n, H]) with
+        ``with_lse``; ``out``: the tensor, or with ``with_lse`` the two."""
+        n, H, dh = q.shape
+        assert dh == cache.dh and q.device == cache.device == batch.device == self.device
+        lse = None
+        if out is None:
+            out = self._new(q.shape, torch.bfloat16)
+            if with_lse:
+                lse = self._new((n, H), torch.float32)
+        elif with_lse:
+            out, lse = out
+            assert _dev(lse, torch.float32).shape == (n, H) and lse.device == q.device
+        assert out.shape == q.shape and out.device == q.device
+        most = batch.table.shape[1] * cache.page
+        _check(load().mvla_pages_attention(self._h, cache._ref, batch._ref, C.byref(_packed_rows(q)), H, n,
+                                           max(n, 1) if max_q is None else max_q,
+                                           most if max_length is None else max_length,
+                                           dh ** -0.5 if scale is None else scale, C.byref(_packed_rows(out)),
+                                           _ptr(lse)), "mvla_pages_attention")
+        return (out, lse) if with_lse else out
+
+    def logprobs(self, logits: torch.Tensor, tokens: Optional[torch.Tensor], temperature: Optional[torch.Tensor] = None,
+                 top: int = 0, out=None):
+        """Log probabilities of the given tokens (int32 [B, m] or [B], None: of none) in each row of
+        logits [B, V] (bf16 or fp32, rows of any stride), the rows' entropies and the ``top`` (up to 32)
+        most likely tokens.  Returns (logprob, shaped as tokens, or None; entropy [B]; top_token int32
+        [B, top] and top_logprob [B, top], or None)."""
+        B, V = logits.shape
+        half = logits.dtype == torch.bfloat16
+        assert logits.device == self.device and (half or logits.dtype == torch.float32), (logits.device, logits.dtype)
+        assert logits.stride(1) == 1 or V == 1, logits.stride()
+        m = 0
+        if tokens is not None:
+            assert _dev(tokens, torch.int32).shape[0] == B and tokens.dim() in (1, 2) and tokens.device == self.device
+            m = 1 if tokens.dim() == 1 else tokens.shape[1]
+        assert temperature is None or (_dev(temperature, torch.float32).shape == (B,) and temperature.device == self.device)
+        if out is None:
+            f32 = torch.float32
+            out = (None if tokens is None else self._new(tokens.shape, f32), self._new((B,), f32),
+                   self._new((B, top), torch.int32) if top else None, self._new((B, top), f32) if top else None)
+        logprob, entropy, top_token, top_logprob = out
+        for t, shape, dt in ((logprob, tokens.shape if m else None, torch.float32), (entropy, (B,), torch.float32),
+                             (top_token, (B, top), torch.int32), (top_logprob, (B, top), torch.float32)):
+            assert t is None or (shape is None) or (_dev(t, dt).shape == shape and t.device == self.device)
+        _check(load().mvla_logprobs(self._h, logits.data_ptr(), int(half), logits.stride(0), B, V, _ptr(temperature),
+                                    _ptr(tokens), m, _ptr(logprob), _ptr(entropy), top, _ptr(top_token),
+                                    _ptr(top_logprob)), "mvla_logprobs")
+        return logprob, entropy, top_token, top_logprob
 
     def peak_probe(self, kind: int, buf: Optional[torch.Tensor], reps: int = 10) -> float:
         """Measured rate of a probe kernel (synchronises): GB/s for PROBE_READ / PROBE_COPY,

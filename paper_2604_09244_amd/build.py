@@ -10,7 +10,8 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libmvla.so")
 SOURCES = ["api.hip", "prune_kernels.hip", "mask_kernels.hip", "layer_kernels.hip", "gemm.hip", "attention.hip",
-           "cache_kernels.hip", "cache_attention.hip", "sample_kernels.hip", "probe_kernels.hip"]
+           "cache_kernels.hip", "cache_attention.hip", "sample_kernels.hip", "rotate_kernels.hip",
+           "pages_kernels.hip", "pages_attention.hip", "logprob_kernels.hip", "probe_kernels.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          # a wave starts with its first kernel arguments in scalar registers instead of loading them

@@ -110,7 +110,8 @@ const char* const kKernelNames[KID_COUNT] = {
     "rmsnorm", "gemm_qkv", "score_probs", "attention", "gemm_o", "rmsnorm_mlp",
     "gemm_gateup", "gemm_down", "salience", "budget", "select", "compact", "rope_table",
     "prune_fused", "smooth", "decompose", "feature_share", "candidate_masks", "mask_indices",
-    "cache_append", "cache_read", "cache_attention", "cache_evict", "sample"};
+    "cache_append", "cache_read", "cache_attention", "cache_evict", "sample", "rotate",
+    "pages_append", "pages_read", "pages_attention", "logprobs"};
 
 }  // namespace
 
@@ -1258,6 +1259,171 @@ int mvla_sample(mvla_ctx* ctx, const void* logits, int half, int64_t row_stride,
     TIMED(ctx, KID_SAMPLE, B, launch_sample(logits, half != 0, row_stride, B, V, temperature, top_k, top_p, min_p, u, token,
                                             prob, reinterpret_cast<char*>(ctx->gemm_partial), ctx->gemm_partial_bytes,
                                             ctx->stream));
+    return MVLA_OK;
+}
+
+// ---------------------------------------------------------------------------
+// Many prompts: rotation, the cache in pages, attention over it, log probabilities
+namespace {
+
+// The calls below may come from a thread whose current device is another one: launches go to the context's.
+struct OnDevice {
+    int before = -1;
+    explicit OnDevice(int device) {
+        int now = 0;
+        if (hipGetDevice(&now) == hipSuccess && now != device && hipSetDevice(device) == hipSuccess) before = now;
+    }
+    ~OnDevice() {
+        if (before >= 0) (void)hipSetDevice(before);
+    }
+};
+
+bool positive(double x) { return x > 0.0 && x <= 1e300; }
+
+int check_pages(const mvla_pages* c) {
+    if (!c || !c->k || !c->v || c->n_pages <= 0 || c->H_kv <= 0) return MVLA_EINVAL;
+    if (c->bits != 16 && c->bits != 8) return MVLA_EUNSUPPORTED;
+    if (c->dh != 64 && c->dh != 128) return MVLA_EUNSUPPORTED;
+    if (c->page < 16 || c->page > 256 || (c->page & (c->page - 1)) != 0) return MVLA_EUNSUPPORTED;
+    if (c->H_kv > kMaxGrid / 2 || c->n_pages > kMaxSlots) return MVLA_EUNSUPPORTED;
+    if (!aligned(c->k, 16) || !aligned(c->v, 16)) return MVLA_EINVAL;
+    if (c->bits == 8 && (!c->k_scale || !c->v_scale || !aligned(c->k_scale, 16) || !aligned(c->v_scale, 16))) return MVLA_EINVAL;
+    return MVLA_OK;
+}
+
+int check_page_batch(const mvla_page_batch* s, const mvla_pages& c, bool rows) {
+    if (!s || !s->table || (rows && (!s->start || !s->length))) return MVLA_EINVAL;
+    if (s->B <= 0 || s->table_pitch <= 0) return MVLA_EINVAL;
+    if (s->B > kMaxGrid || (int64_t)s->table_pitch * c.page > kMaxSlots) return MVLA_EUNSUPPORTED;
+    return MVLA_OK;
+}
+
+PagesView pages_view(const mvla_pages& c, const mvla_page_batch& s) {
+    auto u8 = [](void* p) { return static_cast<uint8_t*>(p); };
+    return {u8(c.k), u8(c.v), u8(c.k_scale), u8(c.v_scale), s.table, c.n_pages, c.H_kv, c.dh, __builtin_ctz((unsigned)c.page),
+            c.bits, s.B, s.table_pitch};
+}
+
+}  // namespace
+
+int mvla_rotation_table(mvla_ctx* ctx, const mvla_rotation* how, int rope_len, float* cos_out, float* sin_out) {
+    if (!ctx || !how || !cos_out || !sin_out || rope_len <= 0) return MVLA_EINVAL;
+    if (!aligned(cos_out, 4) || !aligned(sin_out, 4)) return MVLA_EINVAL;
+    if (how->rotated < 2 || how->rotated % 2 != 0 || !positive(how->base) || !positive(how->gain) || !positive(how->factor) ||
+        how->factor < 1.0)
+        return MVLA_EINVAL;
+    if (how->factor > 1.0 && (!positive(how->trained) || !(how->low_turns >= 0.0) || !(how->high_turns > how->low_turns) ||
+                              !positive(how->high_turns)))
+        return MVLA_EINVAL;
+    if (how->rotated > 256) return MVLA_EUNSUPPORTED;
+    const OnDevice on(ctx->device);
+    int rc;
+    TIMED(ctx, KID_ROPE_TABLE, rope_len, launch_rotation_table(*how, rope_len, cos_out, sin_out, ctx->stream));
+    return MVLA_OK;
+}
+
+int mvla_rotate(mvla_ctx* ctx, const mvla_rows* q, int H, const mvla_rows* q_out, const mvla_rows* k, int H_kv,
+                const mvla_rows* k_out, const int32_t* pos, int B, int n, int dh, int rotated, int interleaved, int inverse,
+                const float* rope_cos, const float* rope_sin, int rope_len) {
+    if (!ctx || !rope_cos || !rope_sin || rope_len <= 0 || B < 0 || n < 0 || H <= 0 || dh <= 0) return MVLA_EINVAL;
+    if (!aligned(rope_cos, 4) || !aligned(rope_sin, 4)) return MVLA_EINVAL;
+    if (rotated < 2 || rotated % 2 != 0 || rotated > dh || !k != !k_out || (k && H_kv <= 0)) return MVLA_EINVAL;
+    if (dh > 256 || H > kMaxGrid / 2 || (k && H_kv > kMaxGrid / 2 - H)) return MVLA_EUNSUPPORTED;
+    if (B == 0 || n == 0) return MVLA_OK;     // (an empty tensor has no address)
+    if (!q || !q_out || !pos || !aligned(pos, 4)) return MVLA_EINVAL;
+    for (const mvla_rows* r : {q, q_out, k, k_out})
+        if (r && (!r->data || !aligned(r->data, 2))) return MVLA_EINVAL;
+    if ((uint64_t)B * n >= (uint64_t)1 << 30 || (uint64_t)B * n * (H + (k ? H_kv : 0)) * dh >= (uint64_t)1 << 38) return MVLA_EUNSUPPORTED;
+    // in place is in place: the same rows at the same strides
+    for (int i = 0; i < 2; ++i) {
+        const mvla_rows *in = i ? k : q, *out = i ? k_out : q_out;
+        if (in && in->data == out->data &&
+            (in->token != out->token || in->head != out->head || in->channel != out->channel || (B > 1 && in->sample != out->sample)))
+            return MVLA_EINVAL;
+    }
+    RotateArgs a{};
+    a.in[0] = cache_rows(*q), a.out[0] = cache_rows(*q_out), a.heads[0] = H;
+    if (k) a.in[1] = cache_rows(*k), a.out[1] = cache_rows(*k_out), a.heads[1] = H_kv;
+    a.pos = pos, a.rc = rope_cos, a.rs = rope_sin;
+    a.B = B, a.n = n, a.dh = dh, a.rotated = rotated, a.rope_len = rope_len;
+    a.interleaved = interleaved != 0, a.inverse = inverse != 0;
+    const OnDevice on(ctx->device);
+    int rc;
+    TIMED(ctx, KID_ROTATE, B * n, launch_rotate(a, ctx->stream));
+    return MVLA_OK;
+}
+
+size_t mvla_pages_workspace_bytes(int B, int H, int H_kv, int dh, int n, int max_q, int max_length) {
+    if (B <= 0 || H <= 0 || H_kv <= 0 || H % H_kv != 0 || n <= 0 || max_q <= 0 || max_length <= 0) return 0;
+    if (dh != 64 && dh != 128) return 0;
+    if (B > kMaxGrid || H_kv > kMaxGrid / 2 || max_length > kMaxSlots || (int64_t)n * H >= (int64_t)1 << 31) return 0;
+    return kCounterBytes + gemm_partial_bytes() + align_up(pages_attention_bytes(B, H, H_kv, dh, n, max_q, max_length), 256) + 256;
+}
+
+int mvla_pages_append(mvla_ctx* ctx, const mvla_pages* pages, const mvla_page_batch* batch, const mvla_rows* k,
+                      const mvla_rows* v, int n) {
+    if (!ctx || n < 0) return MVLA_EINVAL;
+    if (int rc = check_pages(pages)) return rc;
+    if (int rc = check_page_batch(batch, *pages, true)) return rc;
+    if (n == 0) return MVLA_OK;
+    if (!k || !v || !k->data || !v->data || !aligned(k->data, 2) || !aligned(v->data, 2)) return MVLA_EINVAL;
+    if ((uint64_t)n * pages->H_kv * (pages->dh / 8) >= (uint64_t)1 << 31) return MVLA_EUNSUPPORTED;
+    const OnDevice on(ctx->device);
+    int rc;
+    TIMED(ctx, KID_PAGES_APPEND, n, launch_pages_append(pages_view(*pages, *batch), batch->start, batch->length, cache_rows(*k),
+                                                        cache_rows(*v), n, ctx->stream));
+    return MVLA_OK;
+}
+
+int mvla_pages_read(mvla_ctx* ctx, const mvla_pages* pages, const mvla_page_batch* batch, const int32_t* first, int n,
+                    void* k_out, void* v_out) {
+    if (!ctx || n < 0) return MVLA_EINVAL;
+    if (int rc = check_pages(pages)) return rc;
+    if (int rc = check_page_batch(batch, *pages, false)) return rc;
+    if (n == 0) return MVLA_OK;
+    if (!k_out || !v_out || !aligned(k_out, 16) || !aligned(v_out, 16)) return MVLA_EINVAL;
+    if ((uint64_t)n * pages->H_kv * (pages->dh / 8) >= (uint64_t)1 << 31) return MVLA_EUNSUPPORTED;
+    const OnDevice on(ctx->device);
+    int rc;
+    TIMED(ctx, KID_PAGES_READ, batch->B * n, launch_pages_read(pages_view(*pages, *batch), first, n, static_cast<bf16_t*>(k_out),
+                                                               static_cast<bf16_t*>(v_out), ctx->stream));
+    return MVLA_OK;
+}
+
+int mvla_pages_attention(mvla_ctx* ctx, const mvla_pages* pages, const mvla_page_batch* batch, const mvla_rows* q, int H,
+                         int n, int max_q, int max_length, float scale, const mvla_rows* out, float* lse) {
+    if (!ctx || n < 0) return MVLA_EINVAL;
+    if (int rc = check_pages(pages)) return rc;
+    if (int rc = check_page_batch(batch, *pages, true)) return rc;
+    if (H <= 0 || H % pages->H_kv != 0 || max_q <= 0 || max_length <= 0 || max_length > batch->table_pitch * pages->page)
+        return MVLA_EINVAL;
+    if (!(scale > 0.f) || !(scale <= 3.0e38f)) return MVLA_EINVAL;
+    if (n == 0) return MVLA_OK;
+    if (!q || !out || !q->data || !out->data || (lse && !aligned(lse, 4))) return MVLA_EINVAL;
+    CacheRows qr = cache_rows(*q), outr = cache_rows(*out);
+    qr.sample = outr.sample = 0;
+    if (!cache_rows_wide(qr) || !cache_rows_wide(outr)) return MVLA_EINVAL;
+    // (rows of a key head, and parts of rows, as the kernels count them)
+    if ((int64_t)n * H >= (int64_t)1 << 31) return MVLA_EUNSUPPORTED;
+    const OnDevice on(ctx->device);
+    int rc;
+    const PagesAttention a = {qr, outr, batch->start, batch->length, lse, H, n, max_q < n ? max_q : n, max_length, scale};
+    TIMED(ctx, KID_PAGES_ATTENTION, n, launch_pages_attention(pages_view(*pages, *batch), a, ctx->scratch, ctx->scratch_bytes,
+                                                              ctx->stream));
+    return MVLA_OK;
+}
+
+int mvla_logprobs(mvla_ctx* ctx, const void* logits, int half, int64_t row_stride, int B, int V, const float* temperature,
+                  const int32_t* tokens, int n_tokens, float* logprob, float* entropy, int top, int32_t* top_token,
+                  float* top_logprob) {
+    if (!ctx || !logits || B <= 0 || V <= 0 || n_tokens < 0 || top < 0) return MVLA_EINVAL;
+    if (!aligned(logits, half ? 2 : 4) || (n_tokens && (!tokens || !logprob)) || (top && (!top_token || !top_logprob))) return MVLA_EINVAL;
+    if (V > (1 << 22) || top > LOGPROBS_TOP || (int64_t)B * n_tokens >= (int64_t)1 << 31) return MVLA_EUNSUPPORTED;
+    const OnDevice on(ctx->device);
+    int rc;
+    TIMED(ctx, KID_LOGPROBS, B, launch_logprobs(logits, half != 0, row_stride, B, V, temperature, tokens, n_tokens, logprob, entropy,
+                                                top, top_token, top_logprob, reinterpret_cast<char*>(ctx->gemm_partial),
+                                                ctx->gemm_partial_bytes, ctx->stream));
     return MVLA_OK;
 }
 

@@ -16,7 +16,7 @@ enum KernelId {
     KID_RMSNORM_MLP, KID_GEMM_GATEUP, KID_GEMM_DOWN, KID_SALIENCE, KID_BUDGET, KID_SELECT,
     KID_COMPACT, KID_ROPE_TABLE, KID_PRUNE_FUSED, KID_SMOOTH, KID_DECOMPOSE, KID_FEATURE_SHARE,
     KID_CANDIDATE, KID_MASK_INDEX, KID_CACHE_APPEND, KID_CACHE_READ, KID_CACHE_ATTENTION, KID_CACHE_EVICT,
-    KID_SAMPLE, KID_COUNT
+    KID_SAMPLE, KID_ROTATE, KID_PAGES_APPEND, KID_PAGES_READ, KID_PAGES_ATTENTION, KID_LOGPROBS, KID_COUNT
 };
 
 struct ProfRecord {
@@ -208,5 +208,42 @@ int launch_cache_attention(const CacheView& c, const CacheAttention& a, char* sc
 int launch_sample(const void* logits, bool half, int64_t row_stride, int B, int V, const float* temperature,
                   const int32_t* top_k, const float* top_p, const float* min_p, const float* u, int32_t* token, float* prob,
                   char* scratch, size_t scratch_bytes, hipStream_t st);
+
+// rotate_kernels.hip
+int launch_rotation_table(const mvla_rotation& how, int rope_len, float* c, float* s, hipStream_t st);
+struct RotateArgs {
+    CacheRows in[2], out[2];   // queries, keys (heads 0: none)
+    int heads[2];
+    const int32_t* pos;
+    const float *rc, *rs;
+    int B, n, dh, rotated, rope_len;
+    bool interleaved, inverse;
+};
+int launch_rotate(const RotateArgs& a, hipStream_t st);
+
+// pages_kernels.hip, pages_attention.hip: the key/value cache in pages
+struct PagesView {
+    uint8_t *k, *v, *k_scale, *v_scale;
+    const int32_t* table;      // of a batch: [B, pitch]
+    int n_pages, H_kv, dh, log_page, bits, B, pitch;
+};
+int launch_pages_append(const PagesView& c, const int32_t* start, const int32_t* length, const CacheRows& k, const CacheRows& v,
+                        int n, hipStream_t st);
+int launch_pages_read(const PagesView& c, const int32_t* first, int n, bf16_t* k_out, bf16_t* v_out, hipStream_t st);
+struct PagesAttention {
+    CacheRows q, out;
+    const int32_t *start, *length;
+    float* lse;
+    int H, n, max_q, max_len;
+    float scale;
+};
+size_t pages_attention_bytes(int B, int H, int H_kv, int dh, int n, int max_q, int max_len);
+int launch_pages_attention(const PagesView& c, const PagesAttention& a, char* scratch, size_t scratch_bytes, hipStream_t st);
+
+// logprob_kernels.hip
+constexpr int LOGPROBS_TOP = 32;
+int launch_logprobs(const void* logits, bool half, int64_t row_stride, int B, int V, const float* temperature,
+                    const int32_t* tokens, int n_tokens, float* logprob, float* entropy, int top, int32_t* top_token,
+                    float* top_logprob, char* scratch, size_t scratch_bytes, hipStream_t st);
 
 }  // namespace mvla

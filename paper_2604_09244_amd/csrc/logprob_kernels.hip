@@ -1,0 +1,351 @@
+// Log probabilities of given tokens, entropy and the most likely tokens of rows of logits.
+//
+// With m the row's maximum and d = (x - m) / T <= 0: y = d - log S, S = sum exp(d), entropy = log S + sum exp(d) (-d) / S.
+// The tokens that reach the maximum are counted, the others summed: S = count + rest, so that where one token has nearly all
+// of the mass log S = log1p(rest) and the entropy keep their leading digits.
+//
+// A workgroup holds its part of a row in registers (the row, or a slice of it): the maximum first, then the sums, then
+// the most likely tokens, without a second look at memory.  For these, the threads' maxima form 64 groups; the n-th
+// largest group maximum is a bound that at least n logits reach, and in all but made-up rows few more.  Those go to a
+// list in LDS, where each one's place is the number of its betters.
+#include "common.h"
+#include "mfma.h"
+#include "wave.h"
+
+#include <algorithm>
+
+namespace mvla {
+
+constexpr int LP_THREADS = 256, LP_WAVES = LP_THREADS / 64, LP_LIST = 1024;
+constexpr float LP_LOWEST = -1.0e4f;       // an exponent whose power of two is zero
+
+// order of tokens: larger logit first, then lower index (never 0)
+__device__ __forceinline__ uint64_t lp_key(float x, uint32_t index) {
+    const uint32_t u = __float_as_uint(x + 0.f);                     // (-0 is 0)
+    return (uint64_t)(u & 0x80000000u ? ~u : u | 0x80000000u) << 32 | (0xffffffffu - index);
+}
+__device__ __forceinline__ float lp_logit(uint64_t key) {
+    const uint32_t u = (uint32_t)(key >> 32);
+    return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u);
+}
+__device__ __forceinline__ uint32_t lp_index(uint64_t key) { return 0xffffffffu - (uint32_t)key; }
+
+__device__ __forceinline__ float wave_max_f32(float x) {
+#pragma unroll
+    for (int o = 32; o; o >>= 1) x = fmaxf(x, __shfl_xor(x, o));
+    return x;
+}
+
+// What a slice of a row (or the row) amounts to.  rest, spread: sums over the logits below the maximum of exp(d) and of
+// exp(d) times -d / log 2.
+struct LpStats {
+    float m, rest, spread;
+    uint32_t count;
+};
+
+struct LpArgs {
+    const void* logits;
+    int64_t row_stride;
+    int V, n_tokens, top;
+    const float* temperature;
+    const int32_t* tokens;
+    float *logprob, *entropy;
+    int32_t* top_token;
+    float* top_logprob;
+};
+
+struct LpRow {
+    float T, k;           // k = 1 / (T log 2)
+    bool greedy;          // the first token of the order has everything
+    int n;                // best tokens that are needed
+};
+__device__ __forceinline__ LpRow lp_row(const LpArgs& a, int row) {
+    LpRow r;
+    r.T = a.temperature ? a.temperature[row] : 1.f;
+    r.greedy = !(r.T > 0.f);
+    if (r.greedy) r.T = 1.f;
+    r.k = (1.f / r.T) * 1.4426950408889634f;
+    r.n = r.greedy ? max(a.top, 1) : a.top;
+    return r;
+}
+
+template <bool HALF>
+__device__ __forceinline__ float lp_load(const void* logits, int64_t at) {
+    if constexpr (HALF) return bf16_to_f32(static_cast<const bf16_t*>(logits)[at]);
+    else return static_cast<const float*>(logits)[at];
+}
+
+// A row's results from its statistics and its best keys (in order, 0: none).
+template <bool HALF>
+__device__ __forceinline__ void lp_finish(const LpArgs& a, const LpRow& r, int row, const LpStats& s, const uint64_t* best, int tid) {
+    const bool none = s.m == -INFINITY;
+    const float log_s = s.count == 1 ? log1pf(s.rest) : logf((float)s.count + s.rest);
+    auto value = [&](float x, bool first) __attribute__((always_inline)) {
+        if (none || !(x > -INFINITY)) return -INFINITY;
+        if (r.greedy) return first ? 0.f : -INFINITY;
+        return x == s.m ? -log_s : (float)(((double)x - (double)s.m) / (double)r.T) - log_s;
+    };
+    const uint32_t first = r.greedy ? lp_index(best[0]) : 0u;
+    for (int j = tid; j < a.n_tokens; j += LP_THREADS) {
+        const int t = a.tokens[(size_t)row * a.n_tokens + j];
+        float y = -INFINITY;
+        if (t >= 0 && t < a.V) y = value(lp_load<HALF>(a.logits, row * a.row_stride + t), (uint32_t)t == first);
+        a.logprob[(size_t)row * a.n_tokens + j] = y;
+    }
+    if (tid < a.top) {
+        const uint64_t key = best[tid];
+        a.top_token[(size_t)row * a.top + tid] = key ? (int32_t)lp_index(key) : -1;
+        a.top_logprob[(size_t)row * a.top + tid] = key ? value(lp_logit(key), tid == 0) : -INFINITY;
+    }
+    if (tid == 0 && a.entropy)
+        a.entropy[row] = none || r.greedy ? 0.f : log_s + s.spread * 0.6931471805599453f / ((float)s.count + s.rest);
+}
+
+// Places of `count` different keys in a list in LDS: the best n to best[], zeros behind them.
+__device__ __forceinline__ void lp_rank(const uint64_t* list, int count, int n, uint64_t* best, int tid) {
+    for (int i = tid; i < count; i += LP_THREADS) {
+        const uint64_t key = list[i];
+        int place = 0;
+        for (int j = 0; j < count; ++j) place += list[j] > key;
+        if (place < n) best[place] = key;
+    }
+    if (tid >= count && tid < n) best[tid] = 0;
+}
+
+// VPT vectors of 16 bytes a thread.  Slices along blockIdx.y; whole rows (parts null) are finished here.
+template <bool HALF, int VPT>
+__global__ __launch_bounds__(LP_THREADS) void logprob_kernel(LpArgs a, int row0, LpStats* __restrict__ parts,
+                                                             uint64_t* __restrict__ part_keys, int key_pitch) {
+    constexpr int EPV = HALF ? 8 : 4, SIZE = HALF ? 2 : 4;
+    __shared__ float sh_max[LP_WAVES][64], sh_sum[LP_WAVES], sh_spread[LP_WAVES];
+    __shared__ uint32_t sh_count[LP_WAVES], sh_n;
+    __shared__ uint64_t list[LP_LIST], best[LOGPROBS_TOP], sh_key[LP_WAVES];
+    const int row = row0 + blockIdx.x, slice = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const LpRow r = lp_row(a, row);
+    const char* base = static_cast<const char*>(a.logits) + row * a.row_stride * SIZE;
+    // the row: up to EPV - 1 logits, whole vectors at 16-byte addresses, up to EPV - 1 logits
+    const int head = min((int)((16u - (uint32_t)(reinterpret_cast<uintptr_t>(base) & 15u)) % 16u) / SIZE, a.V);
+    const int nv = (a.V - head) / EPV, tail = a.V - head - nv * EPV;
+    const uint4* body = reinterpret_cast<const uint4*>(base + (size_t)head * SIZE);
+    const int v0 = slice * LP_THREADS * VPT;
+    const uint32_t no = HALF ? 0xff80ff80u : 0xff800000u;
+    uint4 raw[VPT];
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+        const int v = v0 + i * LP_THREADS + tid;
+        raw[i] = v < nv ? body[v] : make_uint4(no, no, no, no);
+    }
+    // (the first slice's first threads have one of the lone logits each)
+    const int lone = tid < head ? tid : a.V - tail + tid - head;
+    float x_lone = slice == 0 && tid < head + tail ? lp_load<HALF>(a.logits, row * a.row_stride + lone) : -INFINITY;
+    x_lone = fmaxf(x_lone, -INFINITY);
+    auto at = [&](int i, int e) __attribute__((always_inline)) {     // (NaN counts as -infinity)
+        const uint32_t w = HALF ? (e < 2 ? raw[i].x : e < 4 ? raw[i].y : e < 6 ? raw[i].z : raw[i].w)
+                                : (e == 0 ? raw[i].x : e == 1 ? raw[i].y : e == 2 ? raw[i].z : raw[i].w);
+        return fmaxf(HALF ? __uint_as_float(e & 1 ? w & 0xffff0000u : w << 16) : __uint_as_float(w), -INFINITY);
+    };
+    // ---- maximum
+    float mine = x_lone;
+#pragma unroll
+    for (int i = 0; i < VPT; ++i)
+#pragma unroll
+        for (int e = 0; e < EPV; ++e) mine = fmaxf(mine, at(i, e));
+    sh_max[wave][lane] = mine;
+    if (tid == 0) sh_n = 0;
+    __syncthreads();
+    float group = sh_max[0][lane];
+#pragma unroll
+    for (int w = 1; w < LP_WAVES; ++w) group = fmaxf(group, sh_max[w][lane]);
+    LpStats s;
+    s.m = wave_max_f32(group);
+    // ---- sums
+    s.rest = s.spread = 0.f;
+    s.count = 0;
+    auto add = [&](float x) __attribute__((always_inline)) {
+        const float d = fmaxf((x - s.m) * r.k, LP_LOWEST);
+        const bool most = x == s.m;
+        const float e = most ? 0.f : __builtin_amdgcn_exp2f(d);
+        s.rest += e;
+        s.spread = fmaf(e, -d, s.spread);
+        s.count += (uint32_t)__popcll(__ballot(most));
+    };
+    if (s.m > -INFINITY) {
+        add(x_lone);
+#pragma unroll
+        for (int i = 0; i < VPT; ++i)
+#pragma unroll
+            for (int e = 0; e < EPV; ++e) add(at(i, e));
+    }
+    s.rest = wave_sum_f32(s.rest);
+    s.spread = wave_sum_f32(s.spread);
+    if (lane == 0) sh_sum[wave] = s.rest, sh_spread[wave] = s.spread, sh_count[wave] = s.count;
+    // ---- the most likely tokens
+    if (r.n > 0) {
+        float bound = -INFINITY;
+        {
+            int place = 0;
+            for (int j = 0; j < 64; ++j) {
+                const float other = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(group), j));
+                place += other > group || (other == group && j < lane);
+            }
+            bound = __shfl(group, __ffsll((unsigned long long)__ballot(place == r.n - 1)) - 1);
+        }
+        if (mine >= bound) {
+            auto offer = [&](float x, uint32_t index) __attribute__((always_inline)) {
+                if (x >= bound && x > -INFINITY) {
+                    const uint32_t to = atomicAdd(&sh_n, 1u);
+                    if (to < LP_LIST) list[to] = lp_key(x, index);
+                }
+            };
+            offer(x_lone, (uint32_t)lone);
+#pragma unroll
+            for (int i = 0; i < VPT; ++i)
+#pragma unroll
+                for (int e = 0; e < EPV; ++e)
+                    offer(at(i, e), (uint32_t)(head + (v0 + i * LP_THREADS + tid) * EPV + e));
+        }
+        __syncthreads();
+        const int count = (int)sh_n;
+        if (count <= LP_LIST) {
+            lp_rank(list, count, r.n, best, tid);
+        } else {
+            // (rows of equal logits and the like) the best of what lies behind the last one, n times
+            uint64_t last = ~0ull;
+            for (int j = 0; j < r.n; ++j) {
+                uint64_t key = 0;
+                auto see = [&](float x, uint32_t index) __attribute__((always_inline)) {
+                    const uint64_t k = x > -INFINITY ? lp_key(x, index) : 0;
+                    if (k < last && k > key) key = k;
+                };
+                see(x_lone, (uint32_t)lone);
+#pragma unroll
+                for (int i = 0; i < VPT; ++i)
+#pragma unroll
+                    for (int e = 0; e < EPV; ++e)
+                        see(at(i, e), (uint32_t)(head + (v0 + i * LP_THREADS + tid) * EPV + e));
+#pragma unroll
+                for (int o = 32; o; o >>= 1) {
+                    const uint64_t other = (uint64_t)__shfl_xor((unsigned long long)key, o);
+                    key = other > key ? other : key;
+                }
+                if (lane == 0) sh_key[wave] = key;
+                __syncthreads();
+                key = sh_key[0];
+#pragma unroll
+                for (int w = 1; w < LP_WAVES; ++w) key = sh_key[w] > key ? sh_key[w] : key;
+                if (tid == 0) best[j] = key;
+                if (key) last = key;
+                else last = 0;
+                __syncthreads();
+            }
+        }
+    }
+    __syncthreads();
+    s.rest = s.spread = 0.f, s.count = 0;
+#pragma unroll
+    for (int w = 0; w < LP_WAVES; ++w) s.rest += sh_sum[w], s.spread += sh_spread[w], s.count += sh_count[w];
+    if (!parts) {
+        lp_finish<HALF>(a, r, row, s, best, tid);
+        return;
+    }
+    const size_t part = (size_t)blockIdx.x * gridDim.y + slice;
+    if (tid == 0) parts[part] = s;
+    if (tid < r.n) part_keys[part * key_pitch + tid] = best[tid];
+}
+
+// A row's slices joined.
+template <bool HALF>
+__global__ __launch_bounds__(LP_THREADS) void logprob_join_kernel(LpArgs a, int row0, int slices, const LpStats* __restrict__ parts,
+                                                                  const uint64_t* __restrict__ part_keys, int key_pitch) {
+    __shared__ LpStats sh[LP_WAVES];
+    __shared__ uint64_t list[LP_LIST], best[LOGPROBS_TOP], firsts[LP_THREADS];
+    __shared__ uint32_t sh_n;
+    __shared__ uint64_t sh_bound;
+    const int row = row0 + blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const LpRow r = lp_row(a, row);
+    const LpStats none = {-INFINITY, 0.f, 0.f, 0u};
+    LpStats s = tid < slices ? parts[(size_t)blockIdx.x * slices + tid] : none;
+    if (tid == 0) sh_n = 0, sh_bound = 1;
+    const float mine = wave_max_f32(s.m);
+    if (lane == 0) sh[wave].m = mine;
+    __syncthreads();
+    float m = sh[0].m;
+#pragma unroll
+    for (int w = 1; w < LP_WAVES; ++w) m = fmaxf(m, sh[w].m);
+    if (s.m == -INFINITY) {
+        s = none;
+    } else if (s.m != m) {        // moved to the row's maximum
+        const float apart = fminf((m - s.m) * r.k, -LP_LOWEST), f = __builtin_amdgcn_exp2f(-apart);
+        const float sum = s.rest + (float)s.count;
+        s.spread = f * (s.spread + apart * sum);
+        s.rest = f * sum;
+        s.count = 0;
+    }
+    s.rest = wave_sum_f32(s.rest);
+    s.spread = wave_sum_f32(s.spread);
+    s.count = wave_sum_u32(s.count);
+    if (lane == 0) sh[wave].rest = s.rest, sh[wave].spread = s.spread, sh[wave].count = s.count;
+    if (r.n > 0) {
+        const uint64_t* keys = part_keys + (size_t)blockIdx.x * slices * key_pitch;
+        if (slices > LP_LIST / LOGPROBS_TOP) {
+            // the n-th largest first key of a slice: at least n keys reach it, and those of n slices at most
+            const uint64_t key = tid < slices ? keys[(size_t)tid * key_pitch] : 0;
+            firsts[tid] = key;
+            __syncthreads();
+            int place = 0;
+            for (int j = 0; j < slices; ++j) place += firsts[j] > key;
+            if (key && place == r.n - 1) sh_bound = key;
+            __syncthreads();
+        }
+        const uint64_t bound = sh_bound;
+        for (int i = tid; i < slices * r.n; i += LP_THREADS) {
+            const uint64_t key = keys[(size_t)(i / r.n) * key_pitch + i % r.n];
+            if (key >= bound) {
+                const uint32_t to = atomicAdd(&sh_n, 1u);
+                if (to < LP_LIST) list[to] = key;
+            }
+        }
+        __syncthreads();
+        lp_rank(list, min((int)sh_n, LP_LIST), r.n, best, tid);
+    }
+    __syncthreads();
+    s = {m, 0.f, 0.f, 0u};
+#pragma unroll
+    for (int w = 0; w < LP_WAVES; ++w) s.rest += sh[w].rest, s.spread += sh[w].spread, s.count += sh[w].count;
+    lp_finish<HALF>(a, r, row, s, best, tid);
+}
+
+// ---- host --------------------------------------------------------------------------------------------------------
+template <bool HALF, int VPT>
+static int run_logprobs(const LpArgs& a, int B, char* scratch, size_t scratch_bytes, hipStream_t st) {
+    constexpr int EPV = HALF ? 8 : 4, PER = LP_THREADS * VPT;
+    const int slices = std::max(1, (a.V / EPV + PER - 1) / PER);
+    if (slices == 1) {
+        hipLaunchKernelGGL((logprob_kernel<HALF, VPT>), dim3(B, 1), dim3(LP_THREADS), 0, st, a, 0, nullptr, nullptr, 0);
+        MVLA_HIP_CHECK(hipGetLastError());
+        return MVLA_OK;
+    }
+    const int pitch = std::max(a.top, 1);
+    const size_t per_row = (size_t)slices * (sizeof(LpStats) + 8 * (size_t)pitch);
+    const int rows = (int)std::min<size_t>((size_t)B, (scratch_bytes - 256) / per_row);
+    LpStats* parts = reinterpret_cast<LpStats*>(scratch);
+    uint64_t* keys = reinterpret_cast<uint64_t*>(scratch + align_up((size_t)rows * slices * sizeof(LpStats), 256));
+    for (int row0 = 0; row0 < B; row0 += rows) {     // (more rows than the scratch holds: in turns)
+        const int n = std::min(rows, B - row0);
+        hipLaunchKernelGGL((logprob_kernel<HALF, VPT>), dim3(n, slices), dim3(LP_THREADS), 0, st, a, row0, parts, keys, pitch);
+        MVLA_HIP_CHECK(hipGetLastError());
+        hipLaunchKernelGGL((logprob_join_kernel<HALF>), dim3(n), dim3(LP_THREADS), 0, st, a, row0, slices, parts, keys, pitch);
+        MVLA_HIP_CHECK(hipGetLastError());
+    }
+    return MVLA_OK;
+}
+
+int launch_logprobs(const void* logits, bool half, int64_t row_stride, int B, int V, const float* temperature,
+                    const int32_t* tokens, int n_tokens, float* logprob, float* entropy, int top, int32_t* top_token,
+                    float* top_logprob, char* scratch, size_t scratch_bytes, hipStream_t st) {
+    const LpArgs a = {logits, row_stride, V, n_tokens, top, temperature, tokens, logprob, entropy, top_token, top_logprob};
+    if (half) return run_logprobs<true, 16>(a, B, scratch, scratch_bytes, st);
+    return run_logprobs<false, 16>(a, B, scratch, scratch_bytes, st);
+}
+
+}  // namespace mvla
