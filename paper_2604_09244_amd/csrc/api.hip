@@ -1404,7 +1404,8 @@ int mvla_pages_attention(mvla_ctx* ctx, const mvla_pages* pages, const mvla_page
     qr.sample = outr.sample = 0;
     if (!cache_rows_wide(qr) || !cache_rows_wide(outr)) return MVLA_EINVAL;
     // (rows of a key head, and parts of rows, as the kernels count them)
-    if ((int64_t)n * H >= (int64_t)1 << 31) return MVLA_EUNSUPPORTED;
+    if ((int64_t)n * H >= (int64_t)1 << 31 || (int64_t)(max_q < n ? max_q : n) * (H / pages->H_kv) > 128 * (int64_t)kMaxGrid)
+        return MVLA_EUNSUPPORTED;
     const OnDevice on(ctx->device);
     int rc;
     const PagesAttention a = {qr, outr, batch->start, batch->length, lse, H, n, max_q < n ? max_q : n, max_length, scale};

@@ -28,13 +28,39 @@ __device__ __forceinline__ float quad_sum(float x) {
     const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
-// whether one of a pair of bf16 values is no finite number
+// Values that are no finite numbers, where some rows see their slots and others do not: in a matrix product a weight of
+// zero would not keep them from the others.  They are taken out of the product; per dim, the first slot with a value of
+// +inf or NaN and the first with -inf or NaN say which rows' sums they belong to (a row sees the slots below its limit).
 __device__ __forceinline__ bool not_finite(uint32_t pair) {
     return (pair & 0x7f80u) == 0x7f80u || (pair & 0x7f800000u) == 0x7f800000u;
 }
+__device__ __forceinline__ bool not_finite(const uint4& x) {
+    return not_finite(x.x) || not_finite(x.y) || not_finite(x.z) || not_finite(x.w);
+}
+struct FirstBad {
+    int *up, *down;       // LDS, by dim
+};
+// the finite values of a pair (of dims `dim`, `dim` + 1), zeros for others
+__device__ __forceinline__ uint32_t cleaned(uint32_t pair, const FirstBad& first, int dim, int slot) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t x = pair >> (16 * i) & 0xffffu;
+        if ((x & 0x7f80u) != 0x7f80u) continue;
+        const bool nan = (x & 0x7fu) != 0, minus = x >> 15;
+        if (nan || !minus) atomicMin(first.up + dim + i, slot);
+        if (nan || minus) atomicMin(first.down + dim + i, slot);
+        pair &= i ? 0xffffu : 0xffff0000u;
+    }
+    return pair;
+}
+// what they add to a row's sum over the slots below `limit`
+__device__ __forceinline__ float bad_part(int up, int down, int limit) {
+    return (up < limit ? INFINITY : 0.f) + (down < limit ? -INFINITY : 0.f);
+}
+constexpr int NO_SLOT = 0x7fffffff;
 
 // ---- few rows ----------------------------------------------------------------------------------------------------
-// 16 rows a workgroup: a wave takes 32 slots at a time straight from memory to registers, nothing passes through LDS.
+// Up to 16 rows a key head: a wave takes 32 slots at a time straight from memory to registers, nothing passes through LDS.
 // The slots of a step are dealt to the operand rows so that no lane needs another's data:
 //   K: row r of tile j (of two) is slot 8 (r / 4) + 4 j + r % 4; the lanes of a row read neighbouring pieces of it
 //   S^T: a lane of group g then holds the logits of slots 8 g .. 8 g + 7 of its column, in order: its P^T operand
@@ -43,7 +69,7 @@ __device__ __forceinline__ bool not_finite(uint32_t pair) {
 //   O^T: tile d holds dims c CH + d, so a lane ends with CH consecutive dims per register index
 // A step lies in one page, or its halves in two: where they are comes from scalar loads, a round ahead.
 // Bound by memory: every cached row is read once.
-constexpr int FEW_STEP = 32, FEW_ROWS = 16, FEW_DEPTH_16 = 2, FEW_DEPTH_8 = 3;
+constexpr int FEW_STEP = 32, FEW_ROWS = 16;
 
 template <int DH, int BITS>
 struct PageRaw {
@@ -64,18 +90,18 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void few_pages_kern
                                                                                    float* __restrict__ part_o,
                                                                                    float2* __restrict__ part_ml) {
     constexpr int NB = DH / 32, CH = DH / 16, STEPS = DH / 32, KB = DH * BITS / 8;   // KB: bytes a row
-    constexpr int DEPTH = BITS == 16 ? FEW_DEPTH_16 : FEW_DEPTH_8;
     using Raw = PageRaw<DH, BITS>;
     extern __shared__ float4 sums[];          // [WAVES][rows][DH / 4] parts of O
     __shared__ float sh_m[WAVES][FEW_ROWS], sh_l[WAVES][FEW_ROWS];
+    __shared__ int sh_up[WAVES][DH], sh_down[WAVES][DH], sh_bad[WAVES];
 
-    const int part = blockIdx.x % parts, h = blockIdx.x / parts, b = blockIdx.y, r0 = blockIdx.z * FEW_ROWS;
+    const int part = blockIdx.x % parts, h = blockIdx.x / parts, b = blockIdx.y;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 15, g = lane >> 4;
     const PageSpan span = page_span(a.start, a.length, b, a.n, min(cache.pitch << cache.log_page, a.max_len));
-    const int rows = min(min(span.count, a.max_q) * group - r0, FEW_ROWS);
-    if (rows <= 0) return;
-    const int n_steps = (page_seen(span, (r0 + rows - 1) / group) + FEW_STEP - 1) / FEW_STEP;
+    const int rows = min(span.count, a.max_q) * group;
+    if (rows <= 0 || rows > FEW_ROWS) return;
+    const int n_steps = (page_seen(span, (rows - 1) / group) + FEW_STEP - 1) / FEW_STEP;
     const int used = max((n_steps + chunk - 1) / chunk, 1);
     if (part >= used) return;
     const int step0 = part * chunk, step1 = min(step0 + chunk, n_steps);
@@ -136,29 +162,24 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void few_pages_kern
             }
         }
     };
-    Raw raw[DEPTH];
-    StepRows next[DEPTH];
+    Raw x, ahead;
+    StepRows far;
     const int first = step0 + wave;
-#pragma unroll
-    for (int i = 0; i < DEPTH; ++i)
-        if (first + i * WAVES < step1) next[i] = find(first + i * WAVES);
-#pragma unroll
-    for (int i = 0; i < DEPTH; ++i)
-        if (first + i * WAVES < step1) load(raw[i], next[i]);
-#pragma unroll
-    for (int i = 0; i < DEPTH; ++i)
-        if (first + (i + DEPTH) * WAVES < step1) next[i] = find(first + (i + DEPTH) * WAVES);
+    if (first < step1) {
+        load(ahead, find(first));
+        if (first + WAVES < step1) far = find(first + WAVES);
+    }
 
-    // ---- this lane's column: row r0 + c (columns beyond the rows hold zeros and see everything; nobody reads them)
-    const int qi = (r0 + c) / group;
+    // ---- this lane's column: row c (columns beyond the rows hold zeros and see everything; nobody reads them)
+    const int qi = c / group;
     const bool real = c < rows;
     const int limit = real ? page_seen(span, qi) : span.len;
-    const int least = page_seen(span, r0 / group);        // no row sees fewer slots
+    const int least = page_seen(span, 0);                 // no row sees fewer slots
     uint4 qf[STEPS];
 #pragma unroll
     for (int st = 0; st < STEPS; ++st) qf[st] = make_uint4(0u, 0u, 0u, 0u);
     if (real) {
-        const bf16_t* src = a.q.p + (int64_t)(span.row0 + qi) * a.q.token + (int64_t)(h * group + (r0 + c) % group) * a.q.head;
+        const bf16_t* src = a.q.p + (int64_t)(span.row0 + qi) * a.q.token + (int64_t)(h * group + c % group) * a.q.head;
 #pragma unroll
         for (int st = 0; st < STEPS; ++st)
             qf[st] = *reinterpret_cast<const uint4*>(src + (BITS == 16 ? st * 32 + g * 8 : st / 2 * 64 + g * 16 + st % 2 * 8));
@@ -170,6 +191,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void few_pages_kern
 #pragma unroll
     for (int d = 0; d < CH; ++d) o[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     float run_m = -INFINITY, run_l = 0.f;     // run_l: this lane's share
+    bool bad = false;                         // (the wave's) values that are no finite numbers have been taken out
 
     auto take = [&](Raw& x, int step) __attribute__((always_inline)) {
         const int slot0 = step * FEW_STEP, my0 = slot0 + 8 * g;
@@ -204,7 +226,6 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void few_pages_kern
             }
         }
         // ---- slots that not every row sees, or that hold nothing yet
-        uint32_t lone = 0;                    // (the wave's) whether values that are no finite numbers have to be kept from some rows
         if (slot0 + FEW_STEP > least || x.missing) {
             const bool gone = x.missing >> (g >> 1) & 1u;
             bool any = false;
@@ -217,7 +238,16 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void few_pages_kern
                     any |= not_finite(w[i][e]);
                 }
             }
-            lone = __any(any);
+            if (__any(any)) {
+                if (!bad)                     // (of this wave alone: no other touches its part of LDS before the join)
+                    for (int d = lane; d < DH; d += 64) sh_up[wave][d] = sh_down[wave][d] = NO_SLOT;
+                bad = true;
+                const FirstBad first = {sh_up[wave], sh_down[wave]};
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+#pragma unroll
+                    for (int e = 0; e < CH / 2; ++e) w[i][e] = cleaned(w[i][e], first, c * CH + 2 * e, my0 + i);
+            }
         }
         // ---- softmax against the running maximum
         float top = s[0][0];
@@ -250,32 +280,17 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void few_pages_kern
                                         __builtin_amdgcn_perm(w[3][d / 2], w[2][d / 2], sel),
                                         __builtin_amdgcn_perm(w[5][d / 2], w[4][d / 2], sel),
                                         __builtin_amdgcn_perm(w[7][d / 2], w[6][d / 2], sel));
-            if (!lone) {
-                o[d] = mfma16(vf, pf, o[d]);
-                continue;
-            }
-            // a weight of zero times what is no finite number is none: slot by slot, and only into the rows that see it
-            for (int t = 0; t < FEW_STEP; ++t) {
-                const uint32_t half = (t & 1) ? 0xffff0000u : 0xffffu;
-                const bool mine = t >> 3 == g;
-                uint4 one;
-                one.x = mine && (t & 7) / 2 == 0 ? vf.x & half : 0u, one.y = mine && (t & 7) / 2 == 1 ? vf.y & half : 0u;
-                one.z = mine && (t & 7) / 2 == 2 ? vf.z & half : 0u, one.w = mine && (t & 7) / 2 == 3 ? vf.w & half : 0u;
-                const f32x4_t with = mfma16(one, pf, o[d]);
-                if (slot0 + t < limit)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) o[d][i] = with[i];
-            }
+            o[d] = mfma16(vf, pf, o[d]);
         }
     };
-    for (int step = first; step < step1; step += DEPTH * WAVES) {
-#pragma unroll
-        for (int i = 0; i < DEPTH; ++i)
-            if (step + i * WAVES < step1) {
-                take(raw[i], step + i * WAVES);
-                if (step + (i + DEPTH) * WAVES < step1) load(raw[i], next[i]);
-                if (step + (i + 2 * DEPTH) * WAVES < step1) next[i] = find(step + (i + 2 * DEPTH) * WAVES);
-            }
+#pragma unroll 1
+    for (int step = first; step < step1; step += WAVES) {
+        x = ahead;
+        if (step + WAVES < step1) {
+            load(ahead, far);
+            if (step + 2 * WAVES < step1) far = find(step + 2 * WAVES);
+        }
+        take(x, step);
     }
 
     // ---- the waves' parts of a row, joined
@@ -284,6 +299,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void few_pages_kern
         sh_m[wave][c] = run_m;
         sh_l[wave][c] = run_l;
     }
+    if (lane == 0) sh_bad[wave] = bad;
     float* sh_o = reinterpret_cast<float*>(sums);
     if (real)
 #pragma unroll
@@ -307,18 +323,398 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void few_pages_kern
             acc.x = fmaf(t.x, f, acc.x), acc.y = fmaf(t.y, f, acc.y);
             acc.z = fmaf(t.z, f, acc.z), acc.w = fmaf(t.w, f, acc.w);
         }
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w)
+            if (sh_bad[w]) {
+                const int sees = page_seen(span, r / group);
+                const int *up = &sh_up[w][ch], *down = &sh_down[w][ch];
+                acc.x += bad_part(up[0], down[0], sees), acc.y += bad_part(up[1], down[1], sees);
+                acc.z += bad_part(up[2], down[2], sees), acc.w += bad_part(up[3], down[3], sees);
+            }
         if (used == 1) {
-            const int row = span.row0 + (r0 + r) / group, head = h * group + (r0 + r) % group;
+            const int row = span.row0 + r / group, head = h * group + r % group;
             const float inv = l == 0.f ? 0.f : 1.f / l;      // (nothing seen, or nothing above -infinity: zeros)
             *reinterpret_cast<uint2*>(const_cast<bf16_t*>(a.out.p) + (int64_t)row * a.out.token + (int64_t)head * a.out.head + ch) =
                 make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
             if (a.lse && ch == 0) a.lse[(size_t)row * a.H + head] = l == 0.f ? -INFINITY : m * a.scale + logf(l);
         } else {
-            const size_t row = (((size_t)part * cache.B + b) * cache.H_kv + h) * pitch + r0 + r;
+            const size_t row = (((size_t)part * cache.B + b) * cache.H_kv + h) * pitch + r;
             *reinterpret_cast<float4*>(part_o + row * DH + ch) = acc;
             if (ch == 0) part_ml[row] = make_float2(m, l);
         }
     }
+}
+
+// ---- many rows -----------------------------------------------------------------------------------------------------
+// 32 rows a wave, 64 slots (a tile) at a time through LDS, where a workgroup's waves share them: 16-bit rows travel from
+// memory straight into LDS (16 bytes a lane), 8-bit ones through registers, where they become bf16.  Keys lie in LDS with
+// bits 2 and 3 of the slot swapped, so that a lane's eight probabilities of a 16-slot step are eight consecutive slots;
+// values lie row by row, and the reads that transpose 4 x 16 of them give a lane four slots of one dim.
+// In turn: the keys of the next tile are multiplied while this tile's logits become probabilities, this tile's values are
+// multiplied while the next tile's maxima are found.  So the matrix cores have work that waits for no vector
+// operation; two keys' and two values' tiles are in LDS, the next ones on their way.
+constexpr int MANY_KT = 64, MANY_WAVE_ROWS = 32;
+
+// straight from memory to LDS (16 bytes a lane from a wave-uniform base and a per-lane byte offset, to 1 KiB from lds_addr
+// on); untracked by the compiler: consumers come behind pages_wait and a barrier
+__device__ __forceinline__ void pages_dma16(const void* base, uint32_t off, uint32_t lds_addr) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_addr), "v"(off), "s"(base)
+                 : "memory", "m0");
+}
+__device__ __forceinline__ void pages_wait() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+__device__ __forceinline__ int many_slot(int r) { return (r & ~12) | ((r & 4) << 1) | ((r & 8) >> 1); }   // its own inverse
+// chunk (16 bytes) c of row r lies at chunk c ^ swizzle of the row: fragment reads touch every bank alike
+template <int DH>
+__device__ __forceinline__ int key_swizzle(int row) {
+    return DH == 128 ? row & 15 : (row >> 1) & 7;
+}
+template <int DH>
+__device__ __forceinline__ int value_swizzle(int row) {   // (the four rows of a transposing read in four quarters of the banks)
+    return DH == 128 ? ((row & 3) << 2) | ((row >> 2) & 3) : (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
+}
+
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
+
+// four slots of one dim: lane i of 16 gives the address of values 4 (i % 4) .. + 3 of row i / 4 of a 4 x 16 piece and gets
+// column i
+__device__ __forceinline__ uint2 read_transposed(uint32_t lds_addr) {
+    return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)lds_addr));
+}
+
+// The rows that a workgroup of `block` rows has to do with.
+struct ManyRows {
+    int rows, n_tiles;
+};
+__device__ __forceinline__ ManyRows many_rows(const PageSpan& span, int max_q, int group, int r0, int block) {
+    ManyRows m;
+    m.rows = min(span.count, max_q) * group;
+    m.n_tiles = r0 >= m.rows ? 0 : (page_seen(span, (min(r0 + block, m.rows) - 1) / group) + MANY_KT - 1) / MANY_KT;
+    return m;
+}
+
+template <int DH, int BITS, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, 2) void many_pages_kernel(PagesView cache, PagesAttention a, int group, int parts,
+                                                                   int chunk, float* __restrict__ part_o,
+                                                                   float2* __restrict__ part_ml) {
+    constexpr int NB = DH / 32, CPR = DH / 8, STEPS = DH / 16, DB = DH / 32, KB = DH * BITS / 8;
+    constexpr int TILE = MANY_KT * CPR;             // 16-byte chunks of a tile of keys, or of values
+    constexpr int THREADS = WAVES * 64, LD = TILE / THREADS, BLOCK = WAVES * MANY_WAVE_ROWS;
+    extern __shared__ uint4 lds[];                  // [2] keys, [2] values
+    __shared__ int sh_first[2 * DH], sh_bad;
+
+    const int h = blockIdx.x, b = blockIdx.z / parts, part = blockIdx.z % parts;
+    const int r0 = (gridDim.y - 1 - blockIdx.y) * BLOCK;    // (rows that see most first)
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int fr = lane & 31, fg = lane >> 5;
+    const PageSpan span = page_span(a.start, a.length, b, a.n, min(cache.pitch << cache.log_page, a.max_len));
+    const ManyRows work = many_rows(span, a.max_q, group, r0, BLOCK);
+    if (work.rows <= FEW_ROWS || r0 >= work.rows) return;
+    const int used = max((work.n_tiles + chunk - 1) / chunk, 1);
+    if (part >= used) return;
+    const int kt0 = part * chunk, kt1 = min(kt0 + chunk, work.n_tiles);
+
+    const int my_row = r0 + wave * MANY_WAVE_ROWS + fr, my_i = my_row / group;
+    const bool real = my_row < work.rows;
+    // (a row that is none takes part as if it saw everything and is not stored)
+    const int limit = real ? page_seen(span, my_i) : span.len;
+    const int least = page_seen(span, r0 / group);      // slots that all rows of the workgroup see
+    const int wave_row0 = r0 + wave * MANY_WAVE_ROWS;   // ... and that some row of the wave sees
+    const int wave_most = wave_row0 < work.rows ? page_seen(span, (min(wave_row0 + MANY_WAVE_ROWS, work.rows) - 1) / group) : 0;
+
+    uint4 qf[STEPS];
+#pragma unroll
+    for (int st = 0; st < STEPS; ++st) qf[st] = make_uint4(0u, 0u, 0u, 0u);
+    if (real) {
+        const bf16_t* src = a.q.p + (int64_t)(span.row0 + my_i) * a.q.token + (int64_t)(h * group + my_row % group) * a.q.head + fg * 8;
+#pragma unroll
+        for (int st = 0; st < STEPS; ++st) qf[st] = *reinterpret_cast<const uint4*>(src + st * 16);
+    }
+    // (in registers before any untracked load is in flight)
+#pragma unroll
+    for (int st = 0; st < STEPS; ++st) asm volatile("" : "+v"(qf[st].x), "+v"(qf[st].y), "+v"(qf[st].z), "+v"(qf[st].w));
+
+    // ---- where a tile's rows are: four groups of 16 slots, each in one page
+    struct TileRows {
+        size_t row[4];
+        uint32_t missing;
+    };
+    auto find = [&](int kt) __attribute__((always_inline)) {
+        TileRows s;
+        s.missing = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int slot = kt * MANY_KT + 16 * i;
+            int p = page_at(cache, b, slot >> cache.log_page);
+            if (p < 0) s.missing |= 1u << i, p = 0;
+            s.row[i] = page_row(cache, p, h, slot);
+        }
+        return s;
+    };
+    const uint32_t lds_base = (uint32_t)(uintptr_t)lds;
+    // ---- staging of 16-bit rows: chunk i * THREADS + tid of a tile is this lane's i-th
+    uint32_t k_off[LD], v_off[LD];
+    if constexpr (BITS == 16) {
+#pragma unroll
+        for (int i = 0; i < LD; ++i) {
+            const int at = i * THREADS + tid, row = at / CPR, ch = at % CPR;
+            k_off[i] = (uint32_t)((many_slot(row) & 15) * KB + (ch ^ key_swizzle<DH>(row)) * 16);
+            v_off[i] = (uint32_t)((row & 15) * KB + (ch ^ value_swizzle<DH>(row)) * 16);
+        }
+    }
+    auto group_of = [&](int i) __attribute__((always_inline)) {       // the 16-slot group of this wave's i-th KiB
+        return (i * THREADS + wave * 64) / CPR / 16;
+    };
+    auto dma = [&](const uint8_t* from, const TileRows& s, const uint32_t (&off)[LD], uint32_t to) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < LD; ++i) {
+            const int gi = group_of(i);
+            const size_t row = gi == 0 ? s.row[0] : gi == 1 ? s.row[1] : gi == 2 ? s.row[2] : s.row[3];
+            pages_dma16(from + row * KB, off[i], to + (uint32_t)(i * THREADS + wave * 64) * 16u);
+        }
+    };
+    // ---- staging of 8-bit rows: a thread has PER values of one row (a row's threads lie side by side)
+    constexpr int PER = MANY_KT * DH / THREADS, TPR = DH / PER;        // values a thread, threads a row
+    struct Codes {
+        uint4 w[PER / 16];
+        uint32_t e;
+    };
+    const int c_row = tid / TPR, c_part = tid % TPR;
+    auto load_codes = [&](Codes& x, const uint8_t* codes, const uint8_t* powers, const TileRows& s) __attribute__((always_inline)) {
+        const int gi = c_row / 16;
+        const size_t row = (gi == 0 ? s.row[0] : gi == 1 ? s.row[1] : gi == 2 ? s.row[2] : s.row[3]) + (c_row & 15);
+#pragma unroll
+        for (int i = 0; i < PER / 16; ++i) x.w[i] = *reinterpret_cast<const uint4*>(codes + row * KB + c_part * PER + i * 16);
+        if constexpr (PER <= 32) x.e = powers[row * NB + c_part * PER / 32];
+        else x.e = *reinterpret_cast<const uint16_t*>(powers + row * NB + c_part * 2);
+    };
+    auto put_codes = [&](const Codes& x, int lds_row, int swizzle, uint4* tile) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < PER / 8; ++i) {
+            const uint4& w = x.w[i / 2];
+            const float e = __uint_as_float(PER <= 32 ? x.e << 23 : (x.e >> (i / 4 * 8)) << 23);
+            tile[lds_row * CPR + ((c_part * (PER / 8) + i) ^ swizzle)] = fp8_values(i & 1 ? make_uint2(w.z, w.w) : make_uint2(w.x, w.y), e);
+        }
+    };
+
+    for (int d = tid; d < 2 * DH; d += THREADS) sh_first[d] = NO_SLOT;
+    if (tid == 0) sh_bad = 0;
+    f32x16_t o_acc[DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) o_acc[d][v] = 0.f;
+    float run_m = -INFINITY, run_l = 0.f;     // run_l: this lane's share of the row's sum
+    const float scale_log2e = a.scale * 1.4426950408889634f;
+
+    // fragments' places in a tile, in bytes.  Keys: row fr (32 rows on, the swizzle is the same), chunk 2 st + fg.  Values: row
+    // 8 fg + 4 half + i / 4 of a 16-slot step, chunk 4 d + 2 (lane / 16 % 2) + i % 4 / 2, half i % 2 of it, i = lane % 16.
+    // (st, d and half only turn bits within a row)
+    const uint32_t k_at = (uint32_t)(fr * CPR + (fg ^ key_swizzle<DH>(fr))) * 16u;
+    const int v_row = 8 * fg + ((lane & 15) >> 2), v_ch = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+    const uint32_t v_at = (uint32_t)((v_row * CPR + (v_ch ^ value_swizzle<DH>(v_row))) * 16 + (lane & 1) * 8);
+    auto key_products = [&](f32x16_t (&s)[2], uint32_t tile) __attribute__((always_inline)) {
+        const char* at = reinterpret_cast<const char*>(lds);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) s[t][v] = 0.f;
+#pragma unroll
+        for (int st = 0; st < STEPS; ++st)
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+                s[t] = mfma32(*reinterpret_cast<const uint4*>(at + ((tile + k_at) ^ (st << 5)) + t * 32 * CPR * 16), qf[st], s[t]);
+    };
+    // masks a tile's logits where not every row sees every slot; the tile's maximum of this lane's row
+    auto tile_max = [&](f32x16_t (&s)[2], int kt, uint32_t missing) __attribute__((always_inline)) {
+        const int key0 = kt * MANY_KT;
+        if (key0 + MANY_KT > least || missing) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    const int in = t * 32 + 16 * (v >> 3) + 8 * fg + (v & 7);
+                    if (key0 + in >= limit || (missing >> (in >> 4) & 1u)) s[t][v] = -INFINITY;
+                }
+        }
+        float m = fmaxf(s[0][0], s[1][0]);
+#pragma unroll
+        for (int v = 1; v < 16; ++v) m = fmaxf(m, fmaxf(s[0][v], s[1][v]));
+        const auto other = __builtin_amdgcn_permlane32_swap(__float_as_uint(m), __float_as_uint(m), false, false);
+        return fmaxf(__uint_as_float(other[0]), __uint_as_float(other[1]));
+    };
+    auto rescale = [&](float tile_m) __attribute__((always_inline)) {
+        const float new_m = fmaxf(run_m, tile_m);
+        if (__any(new_m != run_m)) {
+            const float corr = new_m == run_m ? 1.f : __builtin_amdgcn_exp2f((run_m - new_m) * scale_log2e);
+            run_l *= corr;
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) o_acc[d][v] *= corr;
+            run_m = new_m;
+        }
+    };
+    auto probabilities = [&](const f32x16_t (&s)[2], uint4 (&pf)[4]) __attribute__((always_inline)) {
+        const float neg_m = run_m == -INFINITY ? 0.f : -run_m * scale_log2e;
+        float sum[4] = {};
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int hh = 0; hh < 2; ++hh) {
+                float e[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    e[i] = __builtin_amdgcn_exp2f(fmaf(s[t][hh * 8 + i], scale_log2e, neg_m));
+                    sum[i & 3] += e[i];
+                }
+                pf[t * 2 + hh] = make_uint4(pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3]), pack_bf16x2(e[4], e[5]),
+                                            pack_bf16x2(e[6], e[7]));
+            }
+        run_l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    };
+    auto value_products = [&](const uint4 (&pf)[4], uint32_t tile) __attribute__((always_inline)) {
+        auto fragment = [&](int ks, int d) __attribute__((always_inline)) {
+            const uint2 lo = read_transposed(tile + (v_at ^ (d << 6)) + (uint32_t)(ks * 16 * CPR * 16));
+            const uint2 hi = read_transposed(tile + (v_at ^ (d << 6) ^ 16u) + (uint32_t)((ks * 16 + 4) * CPR * 16));
+            return make_uint4(lo.x, lo.y, hi.x, hi.y);
+        };
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+            for (int d = 0; d < DB; ++d) o_acc[d] = mfma32(fragment(ks, d), pf[ks], o_acc[d]);
+    };
+
+    // takes values that are no finite numbers, or that no row sees, out of a tile that not all rows see whole
+    const FirstBad first = {sh_first, sh_first + DH};
+    auto clean = [&](uint4* tile, int kt, uint32_t missing) __attribute__((always_inline)) {
+#pragma unroll 1
+        for (int at = tid; at < TILE; at += THREADS) {
+            const int row = at / CPR, slot = kt * MANY_KT + row;
+            uint4 x = tile[at];
+            if (slot >= span.len || (missing >> (row >> 4) & 1u)) {
+                x = make_uint4(0u, 0u, 0u, 0u);
+            } else {
+                if (!not_finite(x)) continue;
+                const int dim = (at % CPR ^ value_swizzle<DH>(row)) * 8;
+                x.x = cleaned(x.x, first, dim, slot), x.y = cleaned(x.y, first, dim + 2, slot);
+                x.z = cleaned(x.z, first, dim + 4, slot), x.w = cleaned(x.w, first, dim + 6, slot);
+                sh_bad = 1;
+            }
+            tile[at] = x;
+        }
+    };
+
+    // ---- the tiles.  In LDS at the head of turn kt: keys of kt + 1, values of kt; logits of kt in registers, masked, their
+    // maximum found.
+    const uint32_t K_BYTES = TILE * 16u;
+    auto k_tile = [&](int kt) __attribute__((always_inline)) { return (uint32_t)((kt - kt0) & 1) * K_BYTES; };
+    auto v_tile = [&](int kt) __attribute__((always_inline)) { return (uint32_t)(2 + ((kt - kt0) & 1)) * K_BYTES; };
+    auto tile_of = [&](uint32_t at) __attribute__((always_inline)) { return lds + at / 16; };
+    const int lds_key_row = many_slot(c_row);
+    if (kt0 < kt1) {
+        const int last = kt1 - 1;
+        TileRows here = find(kt0), ahead = find(min(kt0 + 1, last)), far = find(min(kt0 + 2, last));
+        uint32_t missing = here.missing;
+        Codes kc, vc;
+        if constexpr (BITS == 16) {
+            dma(cache.k, here, k_off, lds_base + k_tile(kt0));
+            dma(cache.k, ahead, k_off, lds_base + k_tile(kt0 + 1));
+            dma(cache.v, here, v_off, lds_base + v_tile(kt0));
+            pages_wait();
+        } else {
+            Codes k0, v0;
+            load_codes(k0, cache.k, cache.k_scale, here);
+            load_codes(kc, cache.k, cache.k_scale, ahead);
+            load_codes(v0, cache.v, cache.v_scale, here);
+            put_codes(k0, lds_key_row, key_swizzle<DH>(lds_key_row), tile_of(k_tile(kt0)));
+            put_codes(kc, lds_key_row, key_swizzle<DH>(lds_key_row), tile_of(k_tile(kt0 + 1)));
+            put_codes(v0, c_row, value_swizzle<DH>(c_row), tile_of(v_tile(kt0)));
+            load_codes(kc, cache.k, cache.k_scale, far);
+            load_codes(vc, cache.v, cache.v_scale, ahead);
+        }
+        __syncthreads();
+        f32x16_t s[2][2];
+        key_products(s[0], k_tile(kt0));
+        float m = tile_max(s[0], kt0, missing);
+        // (s_now: logits of kt, s_then: those of kt + 1)
+        auto turn = [&](f32x16_t (&s_now)[2], f32x16_t (&s_then)[2], int kt) __attribute__((always_inline)) {
+            // keys of kt + 1 and values of kt have landed for every wave; all have read keys of kt and values of kt - 1
+            if constexpr (BITS == 16) pages_wait();
+            __syncthreads();
+            const uint32_t next_missing = ahead.missing;
+            if (kt + 1 < kt1) {
+                if constexpr (BITS == 16) {
+                    dma(cache.v, ahead, v_off, lds_base + v_tile(kt + 1));
+                    if (kt + 2 < kt1) dma(cache.k, far, k_off, lds_base + k_tile(kt));
+                } else {
+                    put_codes(vc, c_row, value_swizzle<DH>(c_row), tile_of(v_tile(kt + 1)));
+                    if (kt + 2 < kt1) put_codes(kc, lds_key_row, key_swizzle<DH>(lds_key_row), tile_of(k_tile(kt)));
+                }
+                ahead = far;
+                far = find(min(kt + 3, last));
+                if constexpr (BITS == 8) {
+                    load_codes(vc, cache.v, cache.v_scale, ahead);
+                    load_codes(kc, cache.k, cache.k_scale, far);
+                }
+            }
+            if (kt * MANY_KT + MANY_KT > least || missing) {
+                clean(tile_of(v_tile(kt)), kt, missing);
+                __syncthreads();
+            }
+            if (kt * MANY_KT < wave_most) {
+                rescale(m);
+                uint4 pf[4];
+                key_products(s_then, k_tile(kt + 1));      // (behind the last tile: of what lies there, for nothing)
+                probabilities(s_now, pf);
+                value_products(pf, lds_base + v_tile(kt));
+                m = tile_max(s_then, kt + 1, next_missing);
+            }
+            missing = next_missing;
+        };
+        for (int kt = kt0; kt < kt1; kt += 2) {
+            turn(s[0], s[1], kt);
+            if (kt + 1 < kt1) turn(s[1], s[0], kt + 1);
+        }
+        if constexpr (BITS == 16) pages_wait();
+    }
+
+    // ---- this lane: row my_row, dims d 32 + 8 (v / 4) + 4 fg + v % 4
+    const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(run_l), __float_as_uint(run_l), false, false);
+    const float l = __uint_as_float(both[0]) + __uint_as_float(both[1]);
+    __syncthreads();
+    if (!real) return;
+    if (sh_bad)
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                const int dim = d * 32 + 8 * (v >> 2) + 4 * fg + (v & 3);
+                o_acc[d][v] += bad_part(sh_first[dim], sh_first[DH + dim], limit);
+            }
+    const int to = span.row0 + my_i, head = h * group + my_row % group;
+    if (used > 1) {
+        const size_t row = ((size_t)part * a.n + to) * a.H + head;
+        if (fg == 0) part_ml[row] = make_float2(run_m, l);
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int v4 = 0; v4 < 4; ++v4)
+                *reinterpret_cast<float4*>(part_o + row * DH + d * 32 + 8 * v4 + 4 * fg) =
+                    make_float4(o_acc[d][v4 * 4], o_acc[d][v4 * 4 + 1], o_acc[d][v4 * 4 + 2], o_acc[d][v4 * 4 + 3]);
+        return;
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    if (a.lse && fg == 0) a.lse[(size_t)to * a.H + head] = l == 0.f ? -INFINITY : run_m * a.scale + logf(l);
+    bf16_t* orow = const_cast<bf16_t*>(a.out.p) + (int64_t)to * a.out.token + (int64_t)head * a.out.head;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int v4 = 0; v4 < 4; ++v4)
+            *reinterpret_cast<uint2*>(orow + d * 32 + 8 * v4 + 4 * fg) =
+                make_uint2(pack_bf16x2(o_acc[d][v4 * 4] * inv, o_acc[d][v4 * 4 + 1] * inv),
+                           pack_bf16x2(o_acc[d][v4 * 4 + 2] * inv, o_acc[d][v4 * 4 + 3] * inv));
 }
 
 // ---- the parts of a row --------------------------------------------------------------------------------------------
@@ -326,22 +722,27 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void few_pages_kern
 // second part.
 constexpr int JOIN_WAVES = 4, MAX_PARTS = 64;
 
-template <int DH>
+// MANY: rows of many_pages_kernel, whose workgroups have `block` rows each and parts of `chunk` tiles; else of
+// few_pages_kernel.
+template <int DH, bool MANY>
 __global__ __launch_bounds__(JOIN_WAVES * 64) void join_pages_kernel(PagesView cache, PagesAttention a, int group, int chunk,
-                                                                     int pitch, const float* __restrict__ part_o,
+                                                                     int block, int pitch, const float* __restrict__ part_o,
                                                                      const float2* __restrict__ part_ml) {
     constexpr int QUADS = DH / 4, SHARES = 64 / QUADS;
     const int h = blockIdx.y, b = blockIdx.z, lane = threadIdx.x & 63;
     const int r = blockIdx.x * JOIN_WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const PageSpan span = page_span(a.start, a.length, b, a.n, min(cache.pitch << cache.log_page, a.max_len));
     const int rows = min(span.count, a.max_q) * group;
-    if (r >= rows) return;
-    const int last = min(r / FEW_ROWS * FEW_ROWS + FEW_ROWS, rows) - 1;      // (of the row's workgroup)
-    const int n_steps = (page_seen(span, last / group) + FEW_STEP - 1) / FEW_STEP;
+    if (r >= rows || (rows > FEW_ROWS) != MANY) return;
+    const int last = MANY ? min(r / block * block + block, rows) - 1 : rows - 1;      // (of the row's workgroup)
+    constexpr int STEP = MANY ? MANY_KT : FEW_STEP;
+    const int n_steps = (page_seen(span, last / group) + STEP - 1) / STEP;
     const int used = (n_steps + chunk - 1) / chunk;
     if (used <= 1) return;
     const float scale_log2e = a.scale * 1.4426950408889634f;
-    const size_t row = ((size_t)b * cache.H_kv + h) * pitch + r, apart = (size_t)cache.B * cache.H_kv * pitch;
+    const int to = span.row0 + r / group, head = h * group + r % group;
+    const size_t row = MANY ? (size_t)to * a.H + head : ((size_t)b * cache.H_kv + h) * pitch + r;
+    const size_t apart = MANY ? (size_t)a.n * a.H : (size_t)cache.B * cache.H_kv * pitch;
     const float2 ml = lane < used ? part_ml[lane * apart + row] : make_float2(-INFINITY, 0.f);
     float m = ml.x;
 #pragma unroll
@@ -362,7 +763,6 @@ __global__ __launch_bounds__(JOIN_WAVES * 64) void join_pages_kernel(PagesView c
     for (int o = QUADS; o < 64; o <<= 1)
         acc.x += __shfl_xor(acc.x, o), acc.y += __shfl_xor(acc.y, o), acc.z += __shfl_xor(acc.z, o), acc.w += __shfl_xor(acc.w, o);
     if (share) return;
-    const int to = span.row0 + r / group, head = h * group + r % group;
     const float inv = l == 0.f ? 0.f : 1.f / l;
     *reinterpret_cast<uint2*>(const_cast<bf16_t*>(a.out.p) + (int64_t)to * a.out.token + (int64_t)head * a.out.head + ch) =
         make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
@@ -372,7 +772,8 @@ __global__ __launch_bounds__(JOIN_WAVES * 64) void join_pages_kernel(PagesView c
 // ---- host --------------------------------------------------------------------------------------------------------
 namespace {
 
-constexpr size_t MOST_PART_ROWS = 65536;
+// rows of parts that there is memory for, of either kind
+constexpr size_t FEW_PART_ROWS = 65536, MANY_PART_ROWS = 131072;
 
 int allow_lds(const void* kernel, bool* set, size_t lds) {
     int dev = 0;
@@ -400,44 +801,93 @@ FewPlan few_plan(int64_t heads, int64_t rows, int max_len, int64_t room) {
 }
 
 template <int DH, int BITS, int WAVES>
-int launch_few(const PagesView& c, const PagesAttention& a, int group, const FewPlan& p, float* o, float2* ml, hipStream_t st) {
+int launch_few(const PagesView& c, const PagesAttention& a, int group, const FewPlan& p, int rows, float* o, float2* ml,
+               hipStream_t st) {
     static bool lds_set[kMaxDevices] = {};
     const size_t lds = (size_t)WAVES * FEW_ROWS * DH * 4;
     if (int rc = allow_lds(reinterpret_cast<const void*>(&few_pages_kernel<DH, BITS, WAVES>), lds_set, lds)) return rc;
-    const int rows = a.max_q * group, blocks = (rows + FEW_ROWS - 1) / FEW_ROWS;
-    hipLaunchKernelGGL((few_pages_kernel<DH, BITS, WAVES>), dim3(c.H_kv * p.parts, c.B, blocks), dim3(WAVES * 64), lds, st, c, a,
-                       group, p.parts, p.chunk, rows, o, ml);
+    hipLaunchKernelGGL((few_pages_kernel<DH, BITS, WAVES>), dim3(c.H_kv * p.parts, c.B), dim3(WAVES * 64), lds, st, c, a, group,
+                       p.parts, p.chunk, rows, o, ml);
     MVLA_HIP_CHECK(hipGetLastError());
     return MVLA_OK;
 }
 
+template <int DH, int BITS, int WAVES>
+int launch_many(const PagesView& c, const PagesAttention& a, int group, const FewPlan& p, float* o, float2* ml, hipStream_t st) {
+    static bool lds_set[kMaxDevices] = {};
+    const size_t lds = (size_t)4 * MANY_KT * DH * 2;
+    if (int rc = allow_lds(reinterpret_cast<const void*>(&many_pages_kernel<DH, BITS, WAVES>), lds_set, lds)) return rc;
+    const int blocks = (a.max_q * group + WAVES * MANY_WAVE_ROWS - 1) / (WAVES * MANY_WAVE_ROWS);
+    hipLaunchKernelGGL((many_pages_kernel<DH, BITS, WAVES>), dim3(c.H_kv, blocks, c.B * p.parts), dim3(WAVES * 64), lds, st, c, a,
+                       group, p.parts, p.chunk, o, ml);
+    MVLA_HIP_CHECK(hipGetLastError());
+    return MVLA_OK;
+}
+
+// parts of many rows: two workgroups a compute unit, eight tiles each at least
+FewPlan many_plan(int64_t wgs, int max_len, int64_t rows, int64_t B, int64_t room) {
+    FewPlan p;
+    p.waves = 4;
+    const int64_t cus = device_cu_count(), tiles = ((int64_t)max_len + MANY_KT - 1) / MANY_KT;
+    int64_t parts = std::min<int64_t>(2 * cus / wgs, (tiles + 7) / 8);
+    parts = std::max<int64_t>(1, std::min<int64_t>({parts, (int64_t)MAX_PARTS, room / rows, 65535 / B}));
+    p.chunk = (int)((tiles + parts - 1) / parts);
+    p.parts = (int)((tiles + p.chunk - 1) / p.chunk);
+    return p;
+}
+
 template <int DH>
 int run_pages(const PagesView& c, const PagesAttention& a, char* scratch, size_t scratch_bytes, hipStream_t st) {
-    const int group = a.H / c.H_kv, rows = a.max_q * group;
-    const int64_t heads = (int64_t)c.B * c.H_kv;
-    const int64_t room = std::min<int64_t>(MOST_PART_ROWS, (int64_t)((scratch_bytes - 256) / (DH * 4 + 8)));
-    const FewPlan p = few_plan(heads, rows, a.max_len, room);
+    const int group = a.H / c.H_kv;
+    const int64_t heads = (int64_t)c.B * c.H_kv, rows = (int64_t)a.max_q * group;
+    const int64_t room = (int64_t)((scratch_bytes - 256) / (DH * 4 + 8));
+    const int few_rows = (int)std::min<int64_t>(FEW_ROWS, rows);
+    // parts of many rows lie behind those of few
+    const int64_t few_room = std::min<int64_t>(FEW_PART_ROWS, room);
+    const int64_t many_room = std::min<int64_t>(MANY_PART_ROWS, room - few_room);
     float2* ml = reinterpret_cast<float2*>(scratch);
-    float* o = reinterpret_cast<float*>(scratch + align_up((size_t)room * 8, 256));
-    int rc;
-    if (c.bits == 16)
-        rc = p.waves == 8 ? launch_few<DH, 16, 8>(c, a, group, p, o, ml, st) : launch_few<DH, 16, 4>(c, a, group, p, o, ml, st);
-    else
-        rc = p.waves == 8 ? launch_few<DH, 8, 8>(c, a, group, p, o, ml, st) : launch_few<DH, 8, 4>(c, a, group, p, o, ml, st);
-    if (rc || p.parts == 1) return rc;
-    hipLaunchKernelGGL((join_pages_kernel<DH>), dim3((rows + JOIN_WAVES - 1) / JOIN_WAVES, c.H_kv, c.B), dim3(JOIN_WAVES * 64), 0, st,
-                       c, a, group, p.chunk, rows, o, ml);
-    MVLA_HIP_CHECK(hipGetLastError());
+    float* o = reinterpret_cast<float*>(scratch + align_up((size_t)(few_room + many_room) * 8, 256));
+    if (group <= FEW_ROWS) {
+        const FewPlan p = few_plan(heads, few_rows, a.max_len, few_room);
+        int rc;
+        if (c.bits == 16)
+            rc = p.waves == 8 ? launch_few<DH, 16, 8>(c, a, group, p, few_rows, o, ml, st) : launch_few<DH, 16, 4>(c, a, group, p, few_rows, o, ml, st);
+        else
+            rc = p.waves == 8 ? launch_few<DH, 8, 8>(c, a, group, p, few_rows, o, ml, st) : launch_few<DH, 8, 4>(c, a, group, p, few_rows, o, ml, st);
+        if (rc) return rc;
+        if (p.parts > 1) {
+            hipLaunchKernelGGL((join_pages_kernel<DH, false>), dim3((few_rows + JOIN_WAVES - 1) / JOIN_WAVES, c.H_kv, c.B),
+                               dim3(JOIN_WAVES * 64), 0, st, c, a, group, p.chunk, 0, few_rows, o, ml);
+            MVLA_HIP_CHECK(hipGetLastError());
+        }
+    }
+    if (rows <= FEW_ROWS) return MVLA_OK;
+    constexpr int WAVES = 4, BLOCK = WAVES * MANY_WAVE_ROWS;
+    // (workgroups that have rows: of all sequences' blocks no more than the packed rows fill)
+    const int64_t blocks = std::min<int64_t>(c.B * ((rows + BLOCK - 1) / BLOCK), (int64_t)a.n * group / BLOCK + c.B);
+    const FewPlan p = many_plan(c.H_kv * blocks, a.max_len, (int64_t)a.n * a.H, c.B, many_room);
+    float2* many_ml = ml + few_room;
+    float* many_o = o + few_room * DH;
+    if (int rc = c.bits == 16 ? launch_many<DH, 16, WAVES>(c, a, group, p, many_o, many_ml, st)
+                              : launch_many<DH, 8, WAVES>(c, a, group, p, many_o, many_ml, st))
+        return rc;
+    if (p.parts > 1) {
+        hipLaunchKernelGGL((join_pages_kernel<DH, true>), dim3((unsigned)((rows + JOIN_WAVES - 1) / JOIN_WAVES), c.H_kv, c.B),
+                           dim3(JOIN_WAVES * 64), 0, st, c, a, group, p.chunk, BLOCK, 0, many_o, many_ml);
+        MVLA_HIP_CHECK(hipGetLastError());
+    }
     return MVLA_OK;
 }
 
 }  // namespace
 
+// (grows with every argument: what either kind can use, not more than it takes)
 size_t pages_attention_bytes(int B, int H, int H_kv, int dh, int n, int max_q, int max_len) {
-    (void)max_len;
-    const size_t rows = std::min<size_t>((size_t)B * H_kv * max_q * (H / H_kv) * MAX_PARTS, MOST_PART_ROWS);
-    (void)n;
-    return rows * (dh * 4 + 8) + 256;
+    const size_t rows = (size_t)max_q * (H / H_kv), most = std::min<size_t>(MAX_PARTS, ((size_t)max_len + FEW_STEP - 1) / FEW_STEP);
+    size_t all = FEW_PART_ROWS;     // (whole: the parts of many rows lie behind them)
+    if (rows <= FEW_ROWS) all = std::min<size_t>((size_t)B * H_kv * rows * most, FEW_PART_ROWS);
+    else all += std::min<size_t>((size_t)n * H * most, MANY_PART_ROWS);
+    return all * (dh * 4 + 8) + 512;
 }
 
 int launch_pages_attention(const PagesView& c, const PagesAttention& a, char* scratch, size_t scratch_bytes, hipStream_t st) {
