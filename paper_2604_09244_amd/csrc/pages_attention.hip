@@ -28,6 +28,10 @@ __device__ __forceinline__ float quad_sum(float x) {
     const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
+// largest of three, in one operation (NaN if one is: its row's sum is NaN either way)
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
+}
 // Values that are no finite numbers, where some rows see their slots and others do not: in a matrix product a weight of
 // zero would not keep them from the others.  They are taken out of the product; per dim, the first slot with a value of
 // +inf or NaN and the first with -inf or NaN say which rows' sums they belong to (a row sees the slots below its limit).
@@ -250,9 +254,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void few_pages_kern
             }
         }
         // ---- softmax against the running maximum
-        float top = s[0][0];
-#pragma unroll
-        for (int i = 1; i < 8; ++i) top = fmaxf(top, s[i >> 2][i & 3]);
+        const float top = max3(max3(max3(s[0][0], s[0][1], s[0][2]), s[0][3], s[1][0]), s[1][1], max3(s[1][2], s[1][3], -INFINITY));
         if (__any(top > run_m)) {
             const float m = fmaxf(run_m, quad_max(top));
             const float f = m == run_m ? 1.f : __builtin_amdgcn_exp2f((run_m - m) * scale_log2e);
@@ -354,6 +356,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void few_pages_kern
 // multiplied while the next tile's maxima are found.  So the matrix cores have work that waits for no vector
 // operation; two keys' and two values' tiles are in LDS, the next ones on their way.
 constexpr int MANY_KT = 64, MANY_WAVE_ROWS = 32;
+constexpr float SLACK = 8.f;
 
 // straight from memory to LDS (16 bytes a lane from a wave-uniform base and a per-lane byte offset, to 1 KiB from lds_addr
 // on); untracked by the compiler: consumers come behind pages_wait and a barrier
@@ -376,11 +379,13 @@ __device__ __forceinline__ int value_swizzle(int row) {   // (the four rows of a
 
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
+typedef __attribute__((address_space(3))) char lds_char_t;
+typedef __attribute__((address_space(3))) f32x4_t lds_f32x4_t;
 
 // four slots of one dim: lane i of 16 gives the address of values 4 (i % 4) .. + 3 of row i / 4 of a 4 x 16 piece and gets
 // column i
-__device__ __forceinline__ uint2 read_transposed(uint32_t lds_addr) {
-    return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)lds_addr));
+__device__ __forceinline__ uint2 read_transposed(const lds_char_t* at) {
+    return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)at));
 }
 
 // The rows that a workgroup of `block` rows has to do with.
@@ -435,44 +440,52 @@ __global__ __launch_bounds__(WAVES * 64, 2) void many_pages_kernel(PagesView cac
 #pragma unroll
     for (int st = 0; st < STEPS; ++st) asm volatile("" : "+v"(qf[st].x), "+v"(qf[st].y), "+v"(qf[st].z), "+v"(qf[st].w));
 
-    // ---- where a tile's rows are: four groups of 16 slots, each in one page
-    struct TileRows {
-        size_t row[4];
-        uint32_t missing;
+    // ---- where a tile's rows are: four groups of 16 slots, each in one page.  64 entries of the sequence's table at a time
+    // in the lanes of a register, the next 64 on their way.
+    struct TilePages {
+        size_t at[4];                               // bytes from the pool's start to the groups' rows
+        uint32_t missing;                           // bit i: no page for group i
     };
+    const bool one_page = cache.log_page >= 6;      // a tile lies in one page
+    const size_t page_bytes = ((size_t)cache.H_kv << cache.log_page) * KB, head_at = ((size_t)h << cache.log_page) * KB;
+    auto entries = [&](int window) __attribute__((always_inline)) { return page_at(cache, b, window * 64 + lane); };
+    int window = (kt0 * MANY_KT >> cache.log_page) >> 6, pages = entries(window), pages_next = entries(window + 1);
     auto find = [&](int kt) __attribute__((always_inline)) {
-        TileRows s;
+        const int slot = kt * MANY_KT, entry = slot >> cache.log_page;
+        if (entry >> 6 != window) {
+            window = entry >> 6;
+            pages = pages_next;
+            pages_next = entries(window + 1);
+        }
+        TilePages s;
         s.missing = 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int slot = kt * MANY_KT + 16 * i;
-            int p = page_at(cache, b, slot >> cache.log_page);
-            if (p < 0) s.missing |= 1u << i, p = 0;
-            s.row[i] = page_row(cache, p, h, slot);
+            if (i == 0 || !one_page) {
+                const int p = __builtin_amdgcn_readlane(pages, ((slot + 16 * i) >> cache.log_page) & 63);
+                if (p < 0) s.missing |= one_page ? 15u : 1u << i;
+                s.at[i] = (size_t)max(p, 0) * page_bytes + head_at + (size_t)((slot + 16 * i) & ((1 << cache.log_page) - 1)) * KB;
+            } else {
+                s.at[i] = s.at[0] + (size_t)(16 * i) * KB;
+            }
         }
         return s;
     };
+    auto group_at = [&](const TilePages& s, int gi) __attribute__((always_inline)) {
+        return gi == 0 ? s.at[0] : gi == 1 ? s.at[1] : gi == 2 ? s.at[2] : s.at[3];
+    };
     const uint32_t lds_base = (uint32_t)(uintptr_t)lds;
-    // ---- staging of 16-bit rows: chunk i * THREADS + tid of a tile is this lane's i-th
-    uint32_t k_off[LD], v_off[LD];
-    if constexpr (BITS == 16) {
-#pragma unroll
-        for (int i = 0; i < LD; ++i) {
-            const int at = i * THREADS + tid, row = at / CPR, ch = at % CPR;
-            k_off[i] = (uint32_t)((many_slot(row) & 15) * KB + (ch ^ key_swizzle<DH>(row)) * 16);
-            v_off[i] = (uint32_t)((row & 15) * KB + (ch ^ value_swizzle<DH>(row)) * 16);
-        }
-    }
+    // ---- staging of 16-bit rows: chunk i * THREADS + tid of a tile is this lane's i-th, at the same place of its 16 rows each time
+    const int own_row = tid / CPR & 15, own_ch = tid % CPR;
+    const uint32_t k_off = (uint32_t)(many_slot(own_row) * KB + (own_ch ^ key_swizzle<DH>(own_row)) * 16);
+    const uint32_t v_off = (uint32_t)(own_row * KB + (own_ch ^ value_swizzle<DH>(own_row)) * 16);
     auto group_of = [&](int i) __attribute__((always_inline)) {       // the 16-slot group of this wave's i-th KiB
         return (i * THREADS + wave * 64) / CPR / 16;
     };
-    auto dma = [&](const uint8_t* from, const TileRows& s, const uint32_t (&off)[LD], uint32_t to) __attribute__((always_inline)) {
+    auto dma = [&](const uint8_t* from, const TilePages& s, uint32_t off, uint32_t to) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < LD; ++i) {
-            const int gi = group_of(i);
-            const size_t row = gi == 0 ? s.row[0] : gi == 1 ? s.row[1] : gi == 2 ? s.row[2] : s.row[3];
-            pages_dma16(from + row * KB, off[i], to + (uint32_t)(i * THREADS + wave * 64) * 16u);
-        }
+        for (int i = 0; i < LD; ++i)
+            pages_dma16(from + group_at(s, group_of(i)), off, to + (uint32_t)(i * THREADS + wave * 64) * 16u);
     };
     // ---- staging of 8-bit rows: a thread has PER values of one row (a row's threads lie side by side)
     constexpr int PER = MANY_KT * DH / THREADS, TPR = DH / PER;        // values a thread, threads a row
@@ -480,21 +493,28 @@ __global__ __launch_bounds__(WAVES * 64, 2) void many_pages_kernel(PagesView cac
         uint4 w[PER / 16];
         uint32_t e;
     };
-    const int c_row = tid / TPR, c_part = tid % TPR;
-    auto load_codes = [&](Codes& x, const uint8_t* codes, const uint8_t* powers, const TileRows& s) __attribute__((always_inline)) {
-        const int gi = c_row / 16;
-        const size_t row = (gi == 0 ? s.row[0] : gi == 1 ? s.row[1] : gi == 2 ? s.row[2] : s.row[3]) + (c_row & 15);
+    constexpr int CHUNKS = PER / 8;                                    // 16-byte chunks of bf16 that they become
+    static_assert(64 / TPR <= 16 && PER <= 32, "");
+    const int c_row = tid / TPR, c_part = tid % TPR, c_group = wave * 64 / TPR / 16;   // (a wave's rows lie in one group)
+    const uint32_t c_off = (uint32_t)((c_row & 15) * KB + c_part * PER), e_off = (uint32_t)((c_row & 15) * NB + c_part * PER / 32);
+    const int lds_key_row = many_slot(c_row);
+    const uint32_t k_put = (uint32_t)(lds_key_row * CPR + (c_part * CHUNKS ^ key_swizzle<DH>(lds_key_row))) * 16u;
+    const uint32_t v_put = (uint32_t)(c_row * CPR + (c_part * CHUNKS ^ value_swizzle<DH>(c_row))) * 16u;
+    auto load_codes = [&](Codes& x, const uint8_t* codes, const uint8_t* powers, const TilePages& s) __attribute__((always_inline)) {
+        const size_t at = group_at(s, c_group);
+        const uint8_t *c = codes + at, *e = powers + at / 32;
 #pragma unroll
-        for (int i = 0; i < PER / 16; ++i) x.w[i] = *reinterpret_cast<const uint4*>(codes + row * KB + c_part * PER + i * 16);
-        if constexpr (PER <= 32) x.e = powers[row * NB + c_part * PER / 32];
-        else x.e = *reinterpret_cast<const uint16_t*>(powers + row * NB + c_part * 2);
+        for (int i = 0; i < PER / 16; ++i) x.w[i] = *reinterpret_cast<const uint4*>(c + c_off + i * 16);
+        x.e = e[e_off];
     };
-    auto put_codes = [&](const Codes& x, int lds_row, int swizzle, uint4* tile) __attribute__((always_inline)) {
+    auto put_codes = [&](const Codes& x, uint32_t put, uint32_t tile) __attribute__((always_inline)) {
+        asm volatile("" : "+v"(put));
+        const float e = __uint_as_float(x.e << 23);
 #pragma unroll
-        for (int i = 0; i < PER / 8; ++i) {
+        for (int i = 0; i < CHUNKS; ++i) {
             const uint4& w = x.w[i / 2];
-            const float e = __uint_as_float(PER <= 32 ? x.e << 23 : (x.e >> (i / 4 * 8)) << 23);
-            tile[lds_row * CPR + ((c_part * (PER / 8) + i) ^ swizzle)] = fp8_values(i & 1 ? make_uint2(w.z, w.w) : make_uint2(w.x, w.y), e);
+            *reinterpret_cast<uint4*>(reinterpret_cast<char*>(lds) + (put ^ (i << 4)) + tile) =
+                fp8_values(i & 1 ? make_uint2(w.z, w.w) : make_uint2(w.x, w.y), e);
         }
     };
 
@@ -514,38 +534,47 @@ __global__ __launch_bounds__(WAVES * 64, 2) void many_pages_kernel(PagesView cac
     const uint32_t k_at = (uint32_t)(fr * CPR + (fg ^ key_swizzle<DH>(fr))) * 16u;
     const int v_row = 8 * fg + ((lane & 15) >> 2), v_ch = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
     const uint32_t v_at = (uint32_t)((v_row * CPR + (v_ch ^ value_swizzle<DH>(v_row))) * 16 + (lane & 1) * 8);
-    auto key_products = [&](f32x16_t (&s)[2], uint32_t tile) __attribute__((always_inline)) {
-        const char* at = reinterpret_cast<const char*>(lds);
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) s[t][v] = 0.f;
-#pragma unroll
-        for (int st = 0; st < STEPS; ++st)
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-                s[t] = mfma32(*reinterpret_cast<const uint4*>(at + ((tile + k_at) ^ (st << 5)) + t * 32 * CPR * 16), qf[st], s[t]);
+    const lds_char_t* lds_at = (const lds_char_t*)(lds_char_t*)lds;
+    auto key_fragment = [&](uint32_t at, uint32_t tile, int st, int t) __attribute__((always_inline)) {
+        const f32x4_t x = *(const lds_f32x4_t*)(lds_at + (at ^ (st << 5)) + (tile + t * 32 * CPR * 16));
+        return __builtin_bit_cast(uint4, x);
     };
-    // masks a tile's logits where not every row sees every slot; the tile's maximum of this lane's row
-    auto tile_max = [&](f32x16_t (&s)[2], int kt, uint32_t missing) __attribute__((always_inline)) {
-        const int key0 = kt * MANY_KT;
-        if (key0 + MANY_KT > least || missing) {
+    auto key_start = [&](uint4 (&kf)[4], uint32_t tile) __attribute__((always_inline)) {     // of the first two steps
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int v = 0; v < 16; ++v) {
-                    const int in = t * 32 + 16 * (v >> 3) + 8 * fg + (v & 7);
-                    if (key0 + in >= limit || (missing >> (in >> 4) & 1u)) s[t][v] = -INFINITY;
-                }
-        }
-        float m = fmaxf(s[0][0], s[1][0]);
-#pragma unroll
-        for (int v = 1; v < 16; ++v) m = fmaxf(m, fmaxf(s[0][v], s[1][v]));
+        for (int i = 0; i < 4; ++i) kf[i] = key_fragment(k_at, tile, i >> 1, i & 1);
+    };
+    // largest of the two lanes that share a row
+    auto both_max = [&](float m) __attribute__((always_inline)) {
         const auto other = __builtin_amdgcn_permlane32_swap(__float_as_uint(m), __float_as_uint(m), false, false);
         return fmaxf(__uint_as_float(other[0]), __uint_as_float(other[1]));
     };
+    auto max_of = [&](const f32x16_t (&s)[2]) __attribute__((always_inline)) {
+        float m = max3(s[0][0], s[1][0], s[0][1]), n = max3(s[1][1], s[0][2], s[1][2]);     // (two chains)
+#pragma unroll
+        for (int v = 3; v < 15; v += 2) m = max3(m, s[0][v], s[1][v]), n = max3(n, s[0][v + 1], s[1][v + 1]);
+        return both_max(max3(max3(m, n, s[0][15]), s[1][15], -INFINITY));
+    };
+    // where not every row sees all of a tile's slots: its logits masked, their maximum found again
+    auto mask = [&](f32x16_t (&s)[2], float& m, int kt, uint32_t missing) __attribute__((always_inline)) {
+        const int key0 = kt * MANY_KT;
+        if (key0 + MANY_KT <= least && !missing) return;
+        const int left = limit - key0 - 8 * fg;     // slots that the row sees from this lane's first on
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int hh = 0; hh < 2; ++hh) {
+                const int in = missing >> (2 * t + hh) & 1u ? 0 : left - (t * 32 + hh * 16);
+#pragma unroll
+                for (int v = 0; v < 8; ++v)
+                    if (v >= in) s[t][hh * 8 + v] = -INFINITY;
+            }
+        m = max_of(s);
+    };
+    // The sums' reference stays until a logit passes it by SLACK in powers of two: exponentials are at most 2^SLACK then,
+    // and the sums are hardly ever scaled again after the first tiles.
+    const float slack = SLACK / scale_log2e;
     auto rescale = [&](float tile_m) __attribute__((always_inline)) {
-        const float new_m = fmaxf(run_m, tile_m);
+        const float new_m = tile_m > run_m + slack ? tile_m : run_m;
         if (__any(new_m != run_m)) {
             const float corr = new_m == run_m ? 1.f : __builtin_amdgcn_exp2f((run_m - new_m) * scale_log2e);
             run_l *= corr;
@@ -556,41 +585,73 @@ __global__ __launch_bounds__(WAVES * 64, 2) void many_pages_kernel(PagesView cac
             run_m = new_m;
         }
     };
-    auto probabilities = [&](const f32x16_t (&s)[2], uint4 (&pf)[4]) __attribute__((always_inline)) {
+    // The products of a turn, step by step as they are to be issued (left to itself the compiler puts each step's reads right
+    // before its products, or lets registers spill): two products of the next tile's keys with the probabilities of a few of this
+    // tile's logits in their shadow, reads two steps ahead; then a 16-slot step of this tile's values with its share of
+    // the next tile's maxima.
+    auto products = [&](const f32x16_t (&now)[2], f32x16_t (&then)[2], uint4 (&kf)[4], uint32_t k_tile, uint32_t v_tile)
+        __attribute__((always_inline)) {
+        constexpr int PIECE = 32 / STEPS;     // logits a step
+        uint32_t k_here = k_at, v_here = v_at;
+        asm volatile("" : "+v"(k_here), "+v"(v_here));      // (places turned anew each time: kept, they would spill)
         const float neg_m = run_m == -INFINITY ? 0.f : -run_m * scale_log2e;
         float sum[4] = {};
+        uint32_t p[16];                       // probabilities, pairs of slots
+        uint2 vf[4][2];                       // values' fragments: of step n (of 4 DB) in vf[n % 4]
+        auto values = [&](int n) __attribute__((always_inline)) {
+            const int ks = n / DB, d = n % DB;
+            vf[n & 3][0] = read_transposed(lds_at + (v_here ^ (d << 6)) + (v_tile + ks * 16 * CPR * 16));
+            vf[n & 3][1] = read_transposed(lds_at + (v_here ^ (d << 6) ^ 16u) + (v_tile + (ks * 16 + 4) * CPR * 16));
+        };
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int hh = 0; hh < 2; ++hh) {
-                float e[8];
+            for (int v = 0; v < 16; ++v) then[t][v] = 0.f;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    e[i] = __builtin_amdgcn_exp2f(fmaf(s[t][hh * 8 + i], scale_log2e, neg_m));
-                    sum[i & 3] += e[i];
-                }
-                pf[t * 2 + hh] = make_uint4(pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3]), pack_bf16x2(e[4], e[5]),
-                                            pack_bf16x2(e[6], e[7]));
+        for (int st = 0; st < STEPS; ++st) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) then[t] = mfma32(kf[(st & 1) * 2 + t], qf[st], then[t]);
+            if (st + 2 < STEPS)
+#pragma unroll
+                for (int t = 0; t < 2; ++t) kf[(st & 1) * 2 + t] = key_fragment(k_here, k_tile, st + 2, t);
+            if (st >= STEPS - 2) values(2 * (st - STEPS + 2)), values(2 * (st - STEPS + 2) + 1);
+#pragma unroll
+            for (int i = 0; i < PIECE; i += 2) {
+                const int n = st * PIECE + i;
+                const float e0 = __builtin_amdgcn_exp2f(fmaf(now[n >> 4][n & 15], scale_log2e, neg_m));
+                const float e1 = __builtin_amdgcn_exp2f(fmaf(now[n >> 4][(n & 15) + 1], scale_log2e, neg_m));
+                sum[n & 2] += e0, sum[(n & 2) + 1] += e1;
+                p[n >> 1] = pack_bf16x2(e0, e1);
             }
+            __builtin_amdgcn_sched_barrier(0);
+        }
         run_l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-    };
-    auto value_products = [&](const uint4 (&pf)[4], uint32_t tile) __attribute__((always_inline)) {
-        auto fragment = [&](int ks, int d) __attribute__((always_inline)) {
-            const uint2 lo = read_transposed(tile + (v_at ^ (d << 6)) + (uint32_t)(ks * 16 * CPR * 16));
-            const uint2 hi = read_transposed(tile + (v_at ^ (d << 6) ^ 16u) + (uint32_t)((ks * 16 + 4) * CPR * 16));
-            return make_uint4(lo.x, lo.y, hi.x, hi.y);
-        };
+        float m = -INFINITY, other = -INFINITY;
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks)
+        for (int n = 0; n < 4 * DB; ++n) {
+            const int ks = n / DB, d = n % DB;
+            const uint2 lo = vf[n & 3][0], hi = vf[n & 3][1];
+            o_acc[d] = mfma32(make_uint4(lo.x, lo.y, hi.x, hi.y), make_uint4(p[4 * ks], p[4 * ks + 1], p[4 * ks + 2], p[4 * ks + 3]),
+                              o_acc[d]);
+            if (n + 4 < 4 * DB) values(n + 4);
 #pragma unroll
-            for (int d = 0; d < DB; ++d) o_acc[d] = mfma32(fragment(ks, d), pf[ks], o_acc[d]);
+            for (int v = 4 * n / DB; v < 4 * (n + 1) / DB; ++v) {
+                float& to = v & 1 ? other : m;
+                to = max3(to, then[0][v], then[1][v]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        m = max3(m, other, -INFINITY);
+        return both_max(m);
     };
 
     // takes values that are no finite numbers, or that no row sees, out of a tile that not all rows see whole
     const FirstBad first = {sh_first, sh_first + DH};
     auto clean = [&](uint4* tile, int kt, uint32_t missing) __attribute__((always_inline)) {
+        int from = tid;
+        asm volatile("" : "+v"(from));        // (nothing of this in registers between the tiles that need it)
 #pragma unroll 1
-        for (int at = tid; at < TILE; at += THREADS) {
+        for (int at = from; at < TILE; at += THREADS) {
             const int row = at / CPR, slot = kt * MANY_KT + row;
             uint4 x = tile[at];
             if (slot >= span.len || (missing >> (row >> 4) & 1u)) {
@@ -608,74 +669,89 @@ __global__ __launch_bounds__(WAVES * 64, 2) void many_pages_kernel(PagesView cac
 
     // ---- the tiles.  In LDS at the head of turn kt: keys of kt + 1, values of kt; logits of kt in registers, masked, their
     // maximum found.
-    const uint32_t K_BYTES = TILE * 16u;
-    auto k_tile = [&](int kt) __attribute__((always_inline)) { return (uint32_t)((kt - kt0) & 1) * K_BYTES; };
-    auto v_tile = [&](int kt) __attribute__((always_inline)) { return (uint32_t)(2 + ((kt - kt0) & 1)) * K_BYTES; };
+    // (parities are constants: places in LDS are the reads' own offsets)
+    constexpr uint32_t TILE_BYTES = TILE * 16u;
     auto tile_of = [&](uint32_t at) __attribute__((always_inline)) { return lds + at / 16; };
-    const int lds_key_row = many_slot(c_row);
     if (kt0 < kt1) {
         const int last = kt1 - 1;
-        TileRows here = find(kt0), ahead = find(min(kt0 + 1, last)), far = find(min(kt0 + 2, last));
-        uint32_t missing = here.missing;
+        TilePages ahead = find(kt0);
+        uint32_t missing = ahead.missing, next_missing, far_missing = 0;
         Codes kc, vc;
         if constexpr (BITS == 16) {
-            dma(cache.k, here, k_off, lds_base + k_tile(kt0));
-            dma(cache.k, ahead, k_off, lds_base + k_tile(kt0 + 1));
-            dma(cache.v, here, v_off, lds_base + v_tile(kt0));
+            dma(cache.k, ahead, k_off, lds_base);
+            dma(cache.v, ahead, v_off, lds_base + 2 * TILE_BYTES);
+            ahead = find(min(kt0 + 1, last));
+            next_missing = ahead.missing;
+            dma(cache.k, ahead, k_off, lds_base + TILE_BYTES);
             pages_wait();
         } else {
             Codes k0, v0;
-            load_codes(k0, cache.k, cache.k_scale, here);
+            load_codes(k0, cache.k, cache.k_scale, ahead);
+            load_codes(v0, cache.v, cache.v_scale, ahead);
+            ahead = find(min(kt0 + 1, last));
+            next_missing = ahead.missing;
             load_codes(kc, cache.k, cache.k_scale, ahead);
-            load_codes(v0, cache.v, cache.v_scale, here);
-            put_codes(k0, lds_key_row, key_swizzle<DH>(lds_key_row), tile_of(k_tile(kt0)));
-            put_codes(kc, lds_key_row, key_swizzle<DH>(lds_key_row), tile_of(k_tile(kt0 + 1)));
-            put_codes(v0, c_row, value_swizzle<DH>(c_row), tile_of(v_tile(kt0)));
-            load_codes(kc, cache.k, cache.k_scale, far);
             load_codes(vc, cache.v, cache.v_scale, ahead);
+            put_codes(k0, k_put, 0u);
+            put_codes(v0, v_put, 2 * TILE_BYTES);
+            put_codes(kc, k_put, TILE_BYTES);
+            ahead = find(min(kt0 + 2, last));
+            far_missing = ahead.missing;
+            load_codes(kc, cache.k, cache.k_scale, ahead);
         }
         __syncthreads();
         f32x16_t s[2][2];
-        key_products(s[0], k_tile(kt0));
-        float m = tile_max(s[0], kt0, missing);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+#pragma unroll
+            for (int v = 0; v < 16; ++v) s[0][t][v] = 0.f;
+#pragma unroll
+            for (int st = 0; st < STEPS; ++st) s[0][t] = mfma32(key_fragment(k_at, 0u, st, t), qf[st], s[0][t]);
+        }
+        float m = max_of(s[0]);
+        mask(s[0], m, kt0, missing);
         // (s_now: logits of kt, s_then: those of kt + 1)
-        auto turn = [&](f32x16_t (&s_now)[2], f32x16_t (&s_then)[2], int kt) __attribute__((always_inline)) {
+        auto turn = [&](f32x16_t (&s_now)[2], f32x16_t (&s_then)[2], int kt, auto odd) __attribute__((always_inline)) {
+            constexpr uint32_t O = decltype(odd)::value;
+            constexpr uint32_t K_NOW = O * TILE_BYTES, K_THEN = (1 - O) * TILE_BYTES, V_NOW = (2 + O) * TILE_BYTES, V_THEN = (3 - O) * TILE_BYTES;
             // keys of kt + 1 and values of kt have landed for every wave; all have read keys of kt and values of kt - 1
             if constexpr (BITS == 16) pages_wait();
             __syncthreads();
-            const uint32_t next_missing = ahead.missing;
+            uint4 kf[4];
+            key_start(kf, K_THEN);            // (on their way while the next tiles are asked for)
             if (kt + 1 < kt1) {
                 if constexpr (BITS == 16) {
-                    dma(cache.v, ahead, v_off, lds_base + v_tile(kt + 1));
-                    if (kt + 2 < kt1) dma(cache.k, far, k_off, lds_base + k_tile(kt));
+                    dma(cache.v, ahead, v_off, lds_base + V_THEN);
+                    if (kt + 2 < kt1) {
+                        ahead = find(kt + 2);
+                        far_missing = ahead.missing;
+                        dma(cache.k, ahead, k_off, lds_base + K_NOW);
+                    }
                 } else {
-                    put_codes(vc, c_row, value_swizzle<DH>(c_row), tile_of(v_tile(kt + 1)));
-                    if (kt + 2 < kt1) put_codes(kc, lds_key_row, key_swizzle<DH>(lds_key_row), tile_of(k_tile(kt)));
-                }
-                ahead = far;
-                far = find(min(kt + 3, last));
-                if constexpr (BITS == 8) {
-                    load_codes(vc, cache.v, cache.v_scale, ahead);
-                    load_codes(kc, cache.k, cache.k_scale, far);
+                    put_codes(vc, v_put, V_THEN);
+                    if (kt + 2 < kt1) {
+                        put_codes(kc, k_put, K_NOW);
+                        load_codes(vc, cache.v, cache.v_scale, ahead);
+                        ahead = find(min(kt + 3, last));
+                        load_codes(kc, cache.k, cache.k_scale, ahead);
+                    }
                 }
             }
             if (kt * MANY_KT + MANY_KT > least || missing) {
-                clean(tile_of(v_tile(kt)), kt, missing);
+                clean(tile_of(V_NOW), kt, missing);
                 __syncthreads();
             }
             if (kt * MANY_KT < wave_most) {
                 rescale(m);
-                uint4 pf[4];
-                key_products(s_then, k_tile(kt + 1));      // (behind the last tile: of what lies there, for nothing)
-                probabilities(s_now, pf);
-                value_products(pf, lds_base + v_tile(kt));
-                m = tile_max(s_then, kt + 1, next_missing);
+                m = products(s_now, s_then, kf, K_THEN, V_NOW);      // (behind the last tile: of the keys that lie there, for nothing)
+                mask(s_then, m, kt + 1, next_missing);
             }
-            missing = next_missing;
+            missing = next_missing, next_missing = far_missing;
+            if constexpr (BITS == 8) far_missing = ahead.missing;
         };
         for (int kt = kt0; kt < kt1; kt += 2) {
-            turn(s[0], s[1], kt);
-            if (kt + 1 < kt1) turn(s[1], s[0], kt + 1);
+            turn(s[0], s[1], kt, std::integral_constant<uint32_t, 0>{});
+            if (kt + 1 < kt1) turn(s[1], s[0], kt + 1, std::integral_constant<uint32_t, 1>{});
         }
         if constexpr (BITS == 16) pages_wait();
     }
