@@ -293,6 +293,11 @@ class Cache4:
                    new((dh // 32,), u8), new((), torch.int32), new((), torch.float32))
 
 
+def _current_stream(index: int) -> int:
+    """The handle of a device's current stream (torch.cuda.current_stream makes an object of it first)."""
+    return torch._C._cuda_getCurrentRawStream(index)
+
+
 def _packed_rows(t: torch.Tensor) -> Rows:
     """Description of a bf16 tensor [tokens, heads, dh] of any strides."""
     assert t.is_cuda and t.dtype == torch.bfloat16 and t.dim() == 3, (t.device, t.dtype, t.shape)
@@ -314,7 +319,7 @@ class PagedCache:
             assert s is None or _dev(s, torch.uint8).shape == (*k.shape[:3], self.dh // 32), s.shape
         assert all(s is None or s.device == k.device for s in (v, k_scale, v_scale))
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
-        self.device = k.device
+        self.device, self.index = k.device, k.get_device()
         self._c = PagesC(self.n_pages, self.H_kv, self.dh, self.page, self.bits, k.data_ptr(), v.data_ptr(),
                          _ptr(k_scale), _ptr(v_scale))
         self._ref = C.byref(self._c)
@@ -338,7 +343,8 @@ class PageBatch:
         self.B, pitch = _dev(table, torch.int32).shape
         assert _dev(length, torch.int32).shape == (self.B,) and _dev(start, torch.int32).shape == (self.B + 1,)
         assert start.device == length.device == table.device
-        self.start, self.length, self.table, self.device = start, length, table, table.device
+        self.start, self.length, self.table = start, length, table
+        self.device, self.index, self.entries = table.device, table.get_device(), pitch
         self._c = PageBatchC(self.B, start.data_ptr(), length.data_ptr(), table.data_ptr(), pitch)
         self._ref = C.byref(self._c)
 
@@ -403,7 +409,9 @@ class Context:
         lib = load()
         self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
         self._h = C.c_void_p()
+        self._index = self.device.index or 0
         self.stream = torch.cuda.current_stream(self.device)     # the one that the calls run on
+        self._raw_stream = self.stream.cuda_stream
         _check(lib.mvla_create(C.byref(self._h), self.device.index or 0, self.stream.cuda_stream,
                                self.workspace.data_ptr(), nbytes), "mvla_create")
         self._rope = {}
@@ -425,7 +433,7 @@ class Context:
 
     def set_stream(self, stream: torch.cuda.Stream):
         _check(load().mvla_set_stream(self._h, stream.cuda_stream), "mvla_set_stream")
-        self.stream = stream
+        self.stream, self._raw_stream = stream, stream.cuda_stream
 
     # ---- timing ----------------------------------------------------------
     def profile_enable(self, kernel_ids: Optional[Sequence[int]], max_records: int = 4096):
@@ -770,10 +778,21 @@ class Context:
     # ---- many prompts -----------------------------------------------------------
     def _new(self, shape, dtype) -> torch.Tensor:
         """An output: memory of the stream that the calls run on, also where another one is current."""
-        if torch.cuda.current_stream(self.device) == self.stream:
+        if _current_stream(self._index) == self._raw_stream:
             return torch.empty(shape, dtype=dtype, device=self.device)
         with torch.cuda.stream(self.stream):
             return torch.empty(shape, dtype=dtype, device=self.device)
+
+    def _like(self, t: torch.Tensor, dtype=None) -> torch.Tensor:
+        """As ``_new``, contiguous and shaped as ``t``."""
+        if _current_stream(self._index) == self._raw_stream:
+            return torch.empty_like(t, dtype=dtype, memory_format=torch.contiguous_format)
+        with torch.cuda.stream(self.stream):
+            return torch.empty_like(t, dtype=dtype, memory_format=torch.contiguous_format)
+
+    def _is(self, t: torch.Tensor, dtype, shape) -> bool:
+        """Whether a contiguous tensor of this type and shape lies on the context's device."""
+        return t.get_device() == self._index and t.dtype == dtype and t.shape == shape and t.is_contiguous()
 
     def rotary_table(self, rotated: int, rope_len: int, base: float = 10000.0, factor: float = 1.0,
                      low_turns: float = 1.0, high_turns: float = 4.0, trained: float = 8192.0, gain: float = 1.0):
@@ -792,41 +811,53 @@ class Context:
         [n, ...]; k may be None) turned by their positions pos (int32 [B, n] or [n]) with the tables
         ``rope`` = (cos, sin).  ``out``: (q_out, k_out), also the inputs themselves.  Returns (q_out, k_out)."""
         cos, sin = rope
-        rows = _packed_rows if q.dim() == 3 else _rows
-        B, n = (1, q.shape[0]) if q.dim() == 3 else q.shape[:2]
-        H, dh = q.shape[-2:]
-        assert _dev(pos, torch.int32).shape == q.shape[:-2] and q.device == pos.device == self.device
-        assert k is None or (k.shape[:-2] == q.shape[:-2] and k.shape[-1] == dh and k.device == q.device), k.shape
-        assert _dev(cos, torch.float32).shape == _dev(sin, torch.float32).shape and cos.device == q.device
+        if q.dim() == 3:
+            rows, B, (n, H, dh) = _packed_rows, 1, q.shape
+            tokens, H_kv = (n,), 0
+        else:
+            rows, (B, n, H, dh) = _rows, q.shape
+            tokens, H_kv = (B, n), 0
+        on = self._index
+        assert q.get_device() == on and self._is(pos, torch.int32, tokens), (q.device, pos.shape, pos.dtype)
+        rope_len, half = cos.shape
+        assert self._is(cos, torch.float32, cos.shape) and self._is(sin, torch.float32, cos.shape)
         if out is None:
-            out = (self._new(q.shape, torch.bfloat16), None if k is None else self._new(k.shape, torch.bfloat16))
-        q_out, k_out = out
-        assert q_out.shape == q.shape and q_out.device == q.device
-        assert (k is None) == (k_out is None) and (k is None or (k_out.shape == k.shape and k_out.device == k.device))
-        ref = lambda t: None if t is None else C.byref(rows(t))
-        _check(load().mvla_rotate(self._h, ref(q), H, ref(q_out), ref(k), 0 if k is None else k.shape[-2], ref(k_out),
-                                  pos.data_ptr(), B, n, dh, 2 * cos.shape[1], int(interleaved), int(inverse),
-                                  cos.data_ptr(), sin.data_ptr(), cos.shape[0]), "mvla_rotate")
+            q_out, k_out = self._like(q), None if k is None else self._like(k)
+        else:
+            q_out, k_out = out
+            assert q_out.shape == q.shape and q_out.get_device() == on and (k is None) == (k_out is None)
+        k_ref = k_out_ref = None
+        if k is not None:
+            H_kv = k.shape[-2]
+            assert k.shape == (*tokens, H_kv, dh) == k_out.shape and k.get_device() == k_out.get_device() == on, k.shape
+            k_ref, k_out_ref = C.byref(rows(k)), C.byref(rows(k_out))
+        _check(load().mvla_rotate(self._h, C.byref(rows(q)), H, C.byref(rows(q_out)), k_ref, H_kv, k_out_ref,
+                                  pos.data_ptr(), B, n, dh, 2 * half, interleaved, inverse, cos.data_ptr(),
+                                  sin.data_ptr(), rope_len), "mvla_rotate")
         return q_out, k_out
 
     def pages_append(self, cache: PagedCache, batch: PageBatch, k: torch.Tensor, v: torch.Tensor):
         """Write rows k, v [n, H_kv, dh] (bf16, any strides), packed as ``batch.start`` says, as the last
         ones of each sequence's ``length`` (which counts them already)."""
         n, H, dh = k.shape
-        assert k.shape == v.shape and (H, dh) == (cache.H_kv, cache.dh), (k.shape, v.shape)
-        assert k.device == v.device == cache.device == batch.device == self.device
+        on = self._index
+        assert k.shape == v.shape and H == cache.H_kv and dh == cache.dh, (k.shape, v.shape)
+        assert k.get_device() == v.get_device() == cache.index == batch.index == on
         _check(load().mvla_pages_append(self._h, cache._ref, batch._ref, C.byref(_packed_rows(k)),
                                         C.byref(_packed_rows(v)), n), "mvla_pages_append")
 
     def pages_read(self, cache: PagedCache, batch: PageBatch, first: Optional[torch.Tensor], n: int, out=None):
         """Rows first[b] .. first[b] + n - 1 (first None: from 0) of each sequence as bf16 (k, v)
         [B, H_kv, n, dh]."""
-        assert first is None or (_dev(first, torch.int32).shape == (batch.B,) and first.device == self.device)
-        assert cache.device == batch.device == self.device
+        assert first is None or self._is(first, torch.int32, (batch.B,))
+        assert cache.index == batch.index == self._index
         shape = (batch.B, cache.H_kv, n, cache.dh)
-        k, v = (self._new(shape, torch.bfloat16) for _ in range(2)) if out is None else out
-        assert _dev(k, torch.bfloat16).shape == _dev(v, torch.bfloat16).shape == shape
-        assert k.device == v.device == self.device
+        if out is None:
+            k = self._new(shape, torch.bfloat16)
+            v = self._like(k)
+        else:
+            k, v = out
+            assert self._is(k, torch.bfloat16, shape) and self._is(v, torch.bfloat16, shape)
         _check(load().mvla_pages_read(self._h, cache._ref, batch._ref, _ptr(first), n, k.data_ptr(), v.data_ptr()),
                "mvla_pages_read")
         return k, v
@@ -839,20 +870,21 @@ class Context:
         ``length`` (default: n, the table's).  Returns out [n, H, dh], or (out, lse fp32 [n, H]) with
         ``with_lse``; ``out``: the tensor, or with ``with_lse`` the two."""
         n, H, dh = q.shape
-        assert dh == cache.dh and q.device == cache.device == batch.device == self.device
+        on = self._index
+        assert dh == cache.dh and q.get_device() == cache.index == batch.index == on, (q.shape, q.device)
         lse = None
         if out is None:
-            out = self._new(q.shape, torch.bfloat16)
+            out = self._like(q)
             if with_lse:
                 lse = self._new((n, H), torch.float32)
-        elif with_lse:
-            out, lse = out
-            assert _dev(lse, torch.float32).shape == (n, H) and lse.device == q.device
-        assert out.shape == q.shape and out.device == q.device
-        most = batch.table.shape[1] * cache.page
+        else:
+            if with_lse:
+                out, lse = out
+                assert self._is(lse, torch.float32, (n, H))
+            assert out.shape == q.shape and out.get_device() == on
         _check(load().mvla_pages_attention(self._h, cache._ref, batch._ref, C.byref(_packed_rows(q)), H, n,
                                            max(n, 1) if max_q is None else max_q,
-                                           most if max_length is None else max_length,
+                                           batch.entries * cache.page if max_length is None else max_length,
                                            dh ** -0.5 if scale is None else scale, C.byref(_packed_rows(out)),
                                            _ptr(lse)), "mvla_pages_attention")
         return (out, lse) if with_lse else out
@@ -864,23 +896,27 @@ class Context:
         most likely tokens.  Returns (logprob, shaped as tokens, or None; entropy [B]; top_token int32
         [B, top] and top_logprob [B, top], or None)."""
         B, V = logits.shape
-        half = logits.dtype == torch.bfloat16
-        assert logits.device == self.device and (half or logits.dtype == torch.float32), (logits.device, logits.dtype)
+        half, f32 = logits.dtype == torch.bfloat16, torch.float32
+        assert logits.get_device() == self._index and (half or logits.dtype == f32), (logits.device, logits.dtype)
         assert logits.stride(1) == 1 or V == 1, logits.stride()
         m = 0
         if tokens is not None:
-            assert _dev(tokens, torch.int32).shape[0] == B and tokens.dim() in (1, 2) and tokens.device == self.device
             m = 1 if tokens.dim() == 1 else tokens.shape[1]
-        assert temperature is None or (_dev(temperature, torch.float32).shape == (B,) and temperature.device == self.device)
+            assert self._is(tokens, torch.int32, (B,) if tokens.dim() == 1 else (B, m)), (tokens.shape, tokens.dtype)
+        assert temperature is None or self._is(temperature, f32, (B,))
         if out is None:
-            f32 = torch.float32
-            out = (None if tokens is None else self._new(tokens.shape, f32), self._new((B,), f32),
-                   self._new((B, top), torch.int32) if top else None, self._new((B, top), f32) if top else None)
-        logprob, entropy, top_token, top_logprob = out
-        for t, shape, dt in ((logprob, tokens.shape if m else None, torch.float32), (entropy, (B,), torch.float32),
-                             (top_token, (B, top), torch.int32), (top_logprob, (B, top), torch.float32)):
-            assert t is None or (shape is None) or (_dev(t, dt).shape == shape and t.device == self.device)
-        _check(load().mvla_logprobs(self._h, logits.data_ptr(), int(half), logits.stride(0), B, V, _ptr(temperature),
+            logprob = None if tokens is None else self._like(tokens, f32)
+            entropy = self._new((B,), f32) if temperature is None else self._like(temperature)
+            top_token = top_logprob = None
+            if top:
+                top_token = self._new((B, top), torch.int32)
+                top_logprob = self._like(top_token, f32)
+        else:
+            logprob, entropy, top_token, top_logprob = out
+            assert tokens is None or self._is(logprob, f32, tokens.shape)
+            assert entropy is None or self._is(entropy, f32, (B,))
+            assert not top or (self._is(top_token, torch.int32, (B, top)) and self._is(top_logprob, f32, (B, top)))
+        _check(load().mvla_logprobs(self._h, logits.data_ptr(), half, logits.stride(0), B, V, _ptr(temperature),
                                     _ptr(tokens), m, _ptr(logprob), _ptr(entropy), top, _ptr(top_token),
                                     _ptr(top_logprob)), "mvla_logprobs")
         return logprob, entropy, top_token, top_logprob

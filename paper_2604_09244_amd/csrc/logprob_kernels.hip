@@ -13,6 +13,7 @@
 #include "wave.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace mvla {
 
@@ -30,10 +31,28 @@ __device__ __forceinline__ float lp_logit(uint64_t key) {
 }
 __device__ __forceinline__ uint32_t lp_index(uint64_t key) { return 0xffffffffu - (uint32_t)key; }
 
+// Largest of the 64 lanes, in all of them (no NaN among them; see wave_sum_f32).
 __device__ __forceinline__ float wave_max_f32(float x) {
-#pragma unroll
-    for (int o = 32; o; o >>= 1) x = fmaxf(x, __shfl_xor(x, o));
+    const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(h[0]), __uint_as_float(h[1]));
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    x = fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x128, 0xf, 0xf, false)));   // row_ror:8
+    x = fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x124, 0xf, 0xf, false)));
+    x = fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x122, 0xf, 0xf, false)));
+    x = fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x121, 0xf, 0xf, false)));
     return x;
+}
+__device__ __forceinline__ float lp_max3(float a, float b, float c) {      // (NaN if one is)
+    return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
+}
+// NaN to -infinity, in a word of logits
+template <bool HALF>
+__device__ __forceinline__ uint32_t lp_numbers(uint32_t w) {
+    if constexpr (!HALF) return (w & 0x7fffffffu) > 0x7f800000u ? 0xff800000u : w;
+    if ((w & 0x7fffu) > 0x7f80u) w = (w & 0xffff0000u) | 0xff80u;
+    if ((w & 0x7fff0000u) > 0x7f800000u) w = (w & 0xffffu) | 0xff800000u;
+    return w;
 }
 
 // What a slice of a row (or the row) amounts to.  rest, spread: sums over the logits below the maximum of exp(d) and of
@@ -75,6 +94,14 @@ __device__ __forceinline__ float lp_load(const void* logits, int64_t at) {
     else return static_cast<const float*>(logits)[at];
 }
 
+// adds n to a count in LDS and returns what it was (as one operation: the compiler's own form first adds up over the wave)
+__device__ __forceinline__ uint32_t lds_take(uint32_t* count, uint32_t n) {
+    uint32_t was;
+    const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint32_t*)count;
+    asm volatile("ds_add_rtn_u32 %0, %1, %2\n\ts_waitcnt lgkmcnt(0)" : "=v"(was) : "v"(at), "v"(n) : "memory");
+    return was;
+}
+
 // A row's results from its statistics and its best keys (in order, 0: none).
 template <bool HALF>
 __device__ __forceinline__ void lp_finish(const LpArgs& a, const LpRow& r, int row, const LpStats& s, const uint64_t* best, int tid) {
@@ -114,10 +141,10 @@ __device__ __forceinline__ void lp_rank(const uint64_t* list, int count, int n, 
 
 // VPT vectors of 16 bytes a thread.  Slices along blockIdx.y; whole rows (parts null) are finished here.
 template <bool HALF, int VPT>
-__global__ __launch_bounds__(LP_THREADS) void logprob_kernel(LpArgs a, int row0, LpStats* __restrict__ parts,
+__global__ __launch_bounds__(LP_THREADS, VPT == 16 ? 3 : 4) void logprob_kernel(LpArgs a, int row0, LpStats* __restrict__ parts,
                                                              uint64_t* __restrict__ part_keys, int key_pitch) {
     constexpr int EPV = HALF ? 8 : 4, SIZE = HALF ? 2 : 4;
-    __shared__ float sh_max[LP_WAVES][64], sh_sum[LP_WAVES], sh_spread[LP_WAVES];
+    __shared__ float sh_max[LP_WAVES][64], sh_group[64], sh_sum[LP_WAVES], sh_spread[LP_WAVES], sh_bound;
     __shared__ uint32_t sh_count[LP_WAVES], sh_n;
     __shared__ uint64_t list[LP_LIST], best[LOGPROBS_TOP], sh_key[LP_WAVES];
     const int row = row0 + blockIdx.x, slice = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -130,86 +157,154 @@ __global__ __launch_bounds__(LP_THREADS) void logprob_kernel(LpArgs a, int row0,
     const int v0 = slice * LP_THREADS * VPT;
     const uint32_t no = HALF ? 0xff80ff80u : 0xff800000u;
     uint4 raw[VPT];
+    if (v0 < nv) {                             // (loads in one go: the last vector again where there is none)
 #pragma unroll
-    for (int i = 0; i < VPT; ++i) {
-        const int v = v0 + i * LP_THREADS + tid;
-        raw[i] = v < nv ? body[v] : make_uint4(no, no, no, no);
+        for (int i = 0; i < VPT; ++i) raw[i] = body[min(v0 + i * LP_THREADS + tid, nv - 1)];
     }
+    if (v0 + VPT * LP_THREADS > nv)
+#pragma unroll
+        for (int i = 0; i < VPT; ++i)
+            if (v0 + i * LP_THREADS + tid >= nv) raw[i] = make_uint4(no, no, no, no);
     // (the first slice's first threads have one of the lone logits each)
     const int lone = tid < head ? tid : a.V - tail + tid - head;
     float x_lone = slice == 0 && tid < head + tail ? lp_load<HALF>(a.logits, row * a.row_stride + lone) : -INFINITY;
     x_lone = fmaxf(x_lone, -INFINITY);
-    auto at = [&](int i, int e) __attribute__((always_inline)) {     // (NaN counts as -infinity)
+    auto at = [&](int i, int e) __attribute__((always_inline)) {
         const uint32_t w = HALF ? (e < 2 ? raw[i].x : e < 4 ? raw[i].y : e < 6 ? raw[i].z : raw[i].w)
                                 : (e == 0 ? raw[i].x : e == 1 ? raw[i].y : e == 2 ? raw[i].z : raw[i].w);
-        return fmaxf(HALF ? __uint_as_float(e & 1 ? w & 0xffff0000u : w << 16) : __uint_as_float(w), -INFINITY);
+        return HALF ? __uint_as_float(e & 1 ? w & 0xffff0000u : w << 16) : __uint_as_float(w);
     };
-    // ---- maximum
-    float mine = x_lone;
+    // (the compiler would keep the unpacked logits of one pass for the next, in twice the registers)
+    auto packed = [&]() __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < VPT; ++i)
+        for (int i = 0; i < VPT; ++i) asm volatile("" : "+v"(raw[i].x), "+v"(raw[i].y), "+v"(raw[i].z), "+v"(raw[i].w));
+    };
+    // ---- maximum: of each vector, of the thread's, of the workgroup's
+    float top[VPT], mine = x_lone;
+    auto maxima = [&]() __attribute__((always_inline)) {
 #pragma unroll
-        for (int e = 0; e < EPV; ++e) mine = fmaxf(mine, at(i, e));
+        for (int i = 0; i < VPT; ++i) {
+            float m = lp_max3(at(i, 0), at(i, 1), at(i, 2));
+#pragma unroll
+            for (int e = 3; e + 1 < EPV; e += 2) m = lp_max3(m, at(i, e), at(i, e + 1));
+            top[i] = lp_max3(m, at(i, EPV - 1), -INFINITY);
+        }
+        mine = x_lone;
+#pragma unroll
+        for (int i = 0; i + 1 < VPT; i += 2) mine = lp_max3(mine, top[i], top[i + 1]);
+        if (VPT % 2) mine = lp_max3(mine, top[VPT - 1], -INFINITY);
+    };
+    maxima();
+    if (mine != mine) {                        // (rare) NaN counts as -infinity
+#pragma unroll
+        for (int i = 0; i < VPT; ++i)
+            raw[i] = make_uint4(lp_numbers<HALF>(raw[i].x), lp_numbers<HALF>(raw[i].y), lp_numbers<HALF>(raw[i].z), lp_numbers<HALF>(raw[i].w));
+        maxima();
+    }
+    packed();
     sh_max[wave][lane] = mine;
     if (tid == 0) sh_n = 0;
     __syncthreads();
     float group = sh_max[0][lane];
 #pragma unroll
     for (int w = 1; w < LP_WAVES; ++w) group = fmaxf(group, sh_max[w][lane]);
+    if (wave == 0) sh_group[lane] = group;
     LpStats s;
     s.m = wave_max_f32(group);
     // ---- sums
+    // d = x k - m k with one rounding of its own; what m k was rounded by is made good behind the sums.  (m k beyond the
+    // largest number: no other logit lies near enough to count)
+    float k = r.k, mk = s.m * k;
+    if (!(fabsf(mk) < INFINITY)) k = 0.f, mk = INFINITY;
+    const float off = k > 0.f ? fmaf(s.m, k, -mk) : 0.f;
     s.rest = s.spread = 0.f;
     s.count = 0;
-    auto add = [&](float x) __attribute__((always_inline)) {
-        const float d = fmaxf((x - s.m) * r.k, LP_LOWEST);
-        const bool most = x == s.m;
-        const float e = most ? 0.f : __builtin_amdgcn_exp2f(d);
-        s.rest += e;
-        s.spread = fmaf(e, -d, s.spread);
-        s.count += (uint32_t)__popcll(__ballot(most));
-    };
-    if (s.m > -INFINITY) {
+    auto sums = [&](auto with_most) __attribute__((always_inline)) {
+        auto add = [&](float x) __attribute__((always_inline)) {
+            const float d = fmaxf(fmaf(x, k, -mk), LP_LOWEST);       // (-infinity, and what is no number, to a power of zero)
+            float e = __builtin_amdgcn_exp2f(d);
+            if constexpr (decltype(with_most)::value) {
+                const bool most = x == s.m;
+                e = most ? 0.f : e;
+                s.count += (uint32_t)__popcll(__ballot(most));
+            }
+            s.rest += e;
+            s.spread = fmaf(e, -d, s.spread);
+        };
         add(x_lone);
 #pragma unroll
         for (int i = 0; i < VPT; ++i)
 #pragma unroll
             for (int e = 0; e < EPV; ++e) add(at(i, e));
+    };
+    if (s.m > -INFINITY) {
+        if (__any(mine == s.m)) sums(std::true_type{});
+        else sums(std::false_type{});
     }
+    packed();
+    s.spread = fmaf(off, s.rest, s.spread) * __builtin_amdgcn_exp2f(-off);
+    s.rest *= __builtin_amdgcn_exp2f(-off);
     s.rest = wave_sum_f32(s.rest);
     s.spread = wave_sum_f32(s.spread);
     if (lane == 0) sh_sum[wave] = s.rest, sh_spread[wave] = s.spread, sh_count[wave] = s.count;
     // ---- the most likely tokens
     if (r.n > 0) {
-        float bound = -INFINITY;
-        {
+        __syncthreads();
+        {   // four lanes a group maximum, a quarter of the others each
+            const int own = wave * 16 + (lane >> 2), part = (lane & 3) * 16;
+            const float v = sh_group[own];
             int place = 0;
-            for (int j = 0; j < 64; ++j) {
-                const float other = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(group), j));
-                place += other > group || (other == group && j < lane);
-            }
-            bound = __shfl(group, __ffsll((unsigned long long)__ballot(place == r.n - 1)) - 1);
-        }
-        if (mine >= bound) {
-            auto offer = [&](float x, uint32_t index) __attribute__((always_inline)) {
-                if (x >= bound && x > -INFINITY) {
-                    const uint32_t to = atomicAdd(&sh_n, 1u);
-                    if (to < LP_LIST) list[to] = lp_key(x, index);
-                }
-            };
-            offer(x_lone, (uint32_t)lone);
 #pragma unroll
-            for (int i = 0; i < VPT; ++i)
+            for (int j = 0; j < 16; ++j) {
+                const float other = sh_group[part + j];
+                place += other > v || (other == v && part + j < own);
+            }
+            place += __builtin_amdgcn_update_dpp(0, place, 0xb1, 0xf, 0xf, false);   // quad_perm [1,0,3,2]
+            place += __builtin_amdgcn_update_dpp(0, place, 0x4e, 0xf, 0xf, false);   // quad_perm [2,3,0,1]
+            if (place == r.n - 1) sh_bound = v;
+        }
+        __syncthreads();
+        const float bound = sh_bound;
+        if (mine >= bound) {
+            auto offer = [&](const float (&x)[EPV], uint32_t first) __attribute__((always_inline)) {
+                uint32_t which = 0;
+#pragma unroll
+                for (int e = 0; e < EPV; ++e) which |= x[e] >= bound && x[e] > -INFINITY ? 1u << e : 0u;
+                uint32_t to = lds_take(&sh_n, (uint32_t)__popc(which));
 #pragma unroll
                 for (int e = 0; e < EPV; ++e)
-                    offer(at(i, e), (uint32_t)(head + (v0 + i * LP_THREADS + tid) * EPV + e));
+                    if (which >> e & 1u) {
+                        if (to < LP_LIST) list[to] = lp_key(x[e], first + e);
+                        ++to;
+                    }
+            };
+            // (few threads have any, and hardly one more than one vector: read again rather than looked for in registers)
+            uint32_t have = 0;
+#pragma unroll
+            for (int i = 0; i < VPT; ++i) have |= top[i] >= bound && v0 + i * LP_THREADS + tid < nv ? 1u << i : 0u;
+            while (have) {
+                const int v = v0 + (__ffs(have) - 1) * LP_THREADS + tid;
+                have &= have - 1;
+                float x[EPV];
+#pragma unroll
+                for (int e = 0; e < EPV; ++e) x[e] = lp_load<HALF>(body, (int64_t)v * EPV + e);
+                offer(x, (uint32_t)(head + v * EPV));
+            }
+            if (x_lone >= bound) {
+                float x[EPV];
+                x[0] = x_lone;
+#pragma unroll
+                for (int e = 1; e < EPV; ++e) x[e] = -INFINITY;
+                offer(x, (uint32_t)lone);
+            }
         }
         __syncthreads();
         const int count = (int)sh_n;
         if (count <= LP_LIST) {
             lp_rank(list, count, r.n, best, tid);
         } else {
-            // (rows of equal logits and the like) the best of what lies behind the last one, n times
+            // (rows of equal logits and the like) the best of what lies behind the last one, n times, from memory: registers
+            // read in a loop would be more than there are
             uint64_t last = ~0ull;
             for (int j = 0; j < r.n; ++j) {
                 uint64_t key = 0;
@@ -218,11 +313,10 @@ __global__ __launch_bounds__(LP_THREADS) void logprob_kernel(LpArgs a, int row0,
                     if (k < last && k > key) key = k;
                 };
                 see(x_lone, (uint32_t)lone);
-#pragma unroll
-                for (int i = 0; i < VPT; ++i)
-#pragma unroll
-                    for (int e = 0; e < EPV; ++e)
-                        see(at(i, e), (uint32_t)(head + (v0 + i * LP_THREADS + tid) * EPV + e));
+                const int end = head + min(v0 + LP_THREADS * VPT, nv) * EPV;
+#pragma unroll 1
+                for (int k = head + v0 * EPV + tid; k < end; k += LP_THREADS)
+                    see(lp_load<HALF>(a.logits, row * a.row_stride + k), (uint32_t)k);
 #pragma unroll
                 for (int o = 32; o; o >>= 1) {
                     const uint64_t other = (uint64_t)__shfl_xor((unsigned long long)key, o);
@@ -344,8 +438,16 @@ int launch_logprobs(const void* logits, bool half, int64_t row_stride, int B, in
                     const int32_t* tokens, int n_tokens, float* logprob, float* entropy, int top, int32_t* top_token,
                     float* top_logprob, char* scratch, size_t scratch_bytes, hipStream_t st) {
     const LpArgs a = {logits, row_stride, V, n_tokens, top, temperature, tokens, logprob, entropy, top_token, top_logprob};
-    if (half) return run_logprobs<true, 16>(a, B, scratch, scratch_bytes, st);
-    return run_logprobs<false, 16>(a, B, scratch, scratch_bytes, st);
+    // As few slices as leave a workgroup for every compute unit.
+    const int64_t want = device_cu_count(), vectors = V / (half ? 8 : 4);
+    auto fills = [&](int vpt) { return B * ((vectors + LP_THREADS * vpt - 1) / (LP_THREADS * vpt)) >= want; };
+    const int64_t most = (int64_t)LP_THREADS * LP_THREADS;      // (vectors that a slice for each of the joining threads takes)
+    const int vpt = fills(16) || vectors > 4 * most ? 16 : fills(4) || vectors > most ? 4 : 1;
+    if (half)
+        return vpt == 16 ? run_logprobs<true, 16>(a, B, scratch, scratch_bytes, st)
+               : vpt == 4 ? run_logprobs<true, 4>(a, B, scratch, scratch_bytes, st) : run_logprobs<true, 1>(a, B, scratch, scratch_bytes, st);
+    return vpt == 16 ? run_logprobs<false, 16>(a, B, scratch, scratch_bytes, st)
+           : vpt == 4 ? run_logprobs<false, 4>(a, B, scratch, scratch_bytes, st) : run_logprobs<false, 1>(a, B, scratch, scratch_bytes, st);
 }
 
 }  // namespace mvla
