@@ -17,6 +17,17 @@ __device__ __forceinline__ PageSpan page_span(const int32_t* start, const int32_
 // slots that query i sees
 __device__ __forceinline__ int page_seen(const PageSpan& s, int i) { return min(max(s.len - s.count + i + 1, 0), s.len); }
 
+// The sequence whose rows hold packed row i, as far as the starts are ascending (in [0, B) whatever they are).  `first`:
+// the same row for all lanes of a wave, not behind i.
+__device__ __forceinline__ int sequence_of(const int32_t* start, int B, int first, int i) {
+    const int lane = threadIdx.x & 63;
+    int b = 0;
+    for (int at = 0; at < B; at += 64)      // the loads of a wave do not wait for each other, as a binary search's would
+        b += __popcll(__ballot(at + lane < B && start[at + lane + 1] <= first));
+    while (b < B - 1 && start[b + 1] <= i) ++b;
+    return min(b, B - 1);
+}
+
 // The page of slots `entry * page` on of sequence b; -1: none.
 __device__ __forceinline__ int page_at(const PagesView& c, int b, int entry) {
     if ((unsigned)entry >= (unsigned)c.pitch) return -1;

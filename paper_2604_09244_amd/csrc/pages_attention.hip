@@ -88,18 +88,15 @@ struct StepRows {
     uint32_t missing;
 };
 
+// Part `part` of sequence b's rows of key head h: steps part * chunk .. + chunk - 1.
 template <int DH, int BITS, int WAVES>
-__global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void few_pages_kernel(PagesView cache, PagesAttention a, int group,
-                                                                                   int parts, int chunk, int pitch,
-                                                                                   float* __restrict__ part_o,
-                                                                                   float2* __restrict__ part_ml) {
+__device__ __forceinline__ void few_rows(const PagesView& cache, const PagesAttention& a, int group, int chunk, int pitch,
+                                         float* __restrict__ part_o, float2* __restrict__ part_ml, int part, int h, int b, float4* sums) {
     constexpr int NB = DH / 32, CH = DH / 16, STEPS = DH / 32, KB = DH * BITS / 8;   // KB: bytes a row
     using Raw = PageRaw<DH, BITS>;
-    extern __shared__ float4 sums[];          // [WAVES][rows][DH / 4] parts of O
-    __shared__ float sh_m[WAVES][FEW_ROWS], sh_l[WAVES][FEW_ROWS];
+    __shared__ float sh_m[WAVES][FEW_ROWS], sh_l[WAVES][FEW_ROWS];     // (sums: [WAVES][rows][DH / 4] parts of O)
     __shared__ int sh_up[WAVES][DH], sh_down[WAVES][DH], sh_bad[WAVES];
 
-    const int part = blockIdx.x % parts, h = blockIdx.x / parts, b = blockIdx.y;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 15, g = lane >> 4;
     const PageSpan span = page_span(a.start, a.length, b, a.n, min(cache.pitch << cache.log_page, a.max_len));
@@ -347,6 +344,15 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void few_pages_kern
     }
 }
 
+template <int DH, int BITS, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void few_pages_kernel(PagesView cache, PagesAttention a, int group,
+                                                                                   int chunk, int pitch, float* __restrict__ part_o,
+                                                                                   float2* __restrict__ part_ml) {
+    extern __shared__ float4 sums[];
+    // (workgroups are dealt to the eight XCDs in turn: parts outermost, or those that only long sequences have would meet on one)
+    few_rows<DH, BITS, WAVES>(cache, a, group, chunk, pitch, part_o, part_ml, blockIdx.z, blockIdx.x, blockIdx.y, sums);
+}
+
 // ---- many rows -----------------------------------------------------------------------------------------------------
 // 32 rows a wave, 64 slots (a tile) at a time through LDS, where a workgroup's waves share them: 16-bit rows travel from
 // memory straight into LDS (16 bytes a lane), 8-bit ones through registers, where they become bf16.  Keys lie in LDS with
@@ -388,45 +394,119 @@ __device__ __forceinline__ uint2 read_transposed(const lds_char_t* at) {
     return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)at));
 }
 
-// The rows that a workgroup of `block` rows has to do with.
-struct ManyRows {
-    int rows, n_tiles;
+// What a launch of both kinds takes.
+struct PageParts {
+    float *few_o, *many_o;
+    float2 *few_ml, *many_ml;
+    int* many_chunk;      // what the workgroups found, for the join: tiles a part, whether any row is in parts (null: no such ones)
+    int few_chunk, few_parts, few_pitch, many_most;
 };
-__device__ __forceinline__ ManyRows many_rows(const PageSpan& span, int max_q, int group, int r0, int block) {
-    ManyRows m;
-    m.rows = min(span.count, max_q) * group;
-    m.n_tiles = r0 >= m.rows ? 0 : (page_seen(span, (min(r0 + block, m.rows) - 1) / group) + MANY_KT - 1) / MANY_KT;
-    return m;
+struct MixedArgs {
+    PagesView cache;
+    PagesAttention a;
+    PageParts parts;
+    int group, workgroups, wanted;
+};
+// The arguments read anew (they are the kernel's only ones): kept in registers through the loop over tiles, which has none to
+// spare, they would make it spill.
+__device__ __forceinline__ MixedArgs late_args() {
+    auto p = __builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return *reinterpret_cast<const MixedArgs*>((const void*)p);
 }
 
-template <int DH, int BITS, int WAVES>
-__global__ __launch_bounds__(WAVES * 64, 2) void many_pages_kernel(PagesView cache, PagesAttention a, int group, int parts,
-                                                                   int chunk, float* __restrict__ part_o,
-                                                                   float2* __restrict__ part_ml) {
-    constexpr int NB = DH / 32, CPR = DH / 8, STEPS = DH / 16, DB = DH / 32, KB = DH * BITS / 8;
-    constexpr int TILE = MANY_KT * CPR;             // 16-byte chunks of a tile of keys, or of values
-    constexpr int THREADS = WAVES * 64, LD = TILE / THREADS, BLOCK = WAVES * MANY_WAVE_ROWS;
-    extern __shared__ uint4 lds[];                  // [2] keys, [2] values
+constexpr int MANY_WAVES = 4, MANY_BLOCK = MANY_WAVES * MANY_WAVE_ROWS, MANY_LEAST = 8;   // rows a workgroup; tiles a part at least
+
+// What the workgroups of a key head share out: the blocks of 128 rows of every sequence that has more rows than
+// few_rows takes, each in parts of `chunk` tiles.  Only the device knows how many there are, so every workgroup counts them.
+struct ManyItem {
+    int b, r0, part, chunk, total;
+    bool parted;          // whether any row is in parts
+};
+struct ManySize {
+    int blocks, tiles;    // of a sequence: blocks of rows, tiles that its last row sees
+    bool few;             // it has few rows
+};
+__device__ __forceinline__ ManySize many_size(const PagesView& cache, const PagesAttention& a, int group, int b) {
+    if (b >= cache.B) return {0, 0, false};
+    const PageSpan span = page_span(a.start, a.length, b, a.n, min(cache.pitch << cache.log_page, a.max_len));
+    const int rows = min(span.count, a.max_q) * group;
+    if (rows <= FEW_ROWS) return {0, 0, rows > 0};
+    return {(rows + MANY_BLOCK - 1) / MANY_BLOCK, (page_seen(span, (rows - 1) / group) + MANY_KT - 1) / MANY_KT, false};
+}
+// item: which of them; wanted: how many there should be (parts are made until there are); most: parts of a block at most
+__device__ __forceinline__ ManyItem many_item(const PagesView& cache, const PagesAttention& a, int group, int item, int wanted, int most,
+                                              int few_parts) {
+    const int lane = threadIdx.x & 63;
+    ManyItem it = {-1, 0, 0, 0, 0, false};
+    const ManySize own = many_size(cache, a, group, lane);
+    double tiles = 0.0;
+    int blocks = 0, longest = 0;
+    for (int b0 = 0; b0 < cache.B; b0 += 64) {
+        const ManySize s = b0 ? many_size(cache, a, group, b0 + lane) : own;
+        tiles += wave_sum_f64((double)s.blocks * s.tiles);
+        blocks += (int)wave_sum_u32((uint32_t)s.blocks);
+        it.parted |= few_parts > 1 && __any(s.few);
+        int m = s.tiles;
+#pragma unroll
+        for (int o = 32; o; o >>= 1) m = max(m, __shfl_xor(m, o));
+        longest = max(longest, m);
+    }
+    const double share = wanted > blocks ? ceil(tiles / (wanted - blocks)) : (double)longest;
+    it.chunk = max(max((int)min(share, (double)longest), MANY_LEAST), (longest + most - 1) / most);
+    for (int b0 = 0; b0 < cache.B; b0 += 64) {
+        const ManySize s = b0 ? many_size(cache, a, group, b0 + lane) : own;
+        const int parts = max((s.tiles + it.chunk - 1) / it.chunk, 1);
+        int end = s.blocks * parts;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int before = __shfl_up(end, o);
+            if (lane >= o) end += before;
+        }
+        const int at = item - it.total;               // (counted from this run of sequences on)
+        const unsigned long long behind = __ballot(end > at);
+        if (it.b < 0 && at >= 0 && behind) {
+            const int l = __ffsll(behind) - 1;
+            it.b = b0 + l;
+            const int p = __builtin_amdgcn_readlane(parts, l), n = __builtin_amdgcn_readlane(s.blocks, l);
+            const int in = at - (__builtin_amdgcn_readlane(end, l) - n * p);
+            it.r0 = (n - 1 - in / p) * MANY_BLOCK;    // (rows that see most first)
+            it.part = in % p;
+        }
+        it.total += __builtin_amdgcn_readlane(end, 63);
+    }
+    it.parted |= longest > it.chunk;
+    it.chunk = __builtin_amdgcn_readfirstlane(it.chunk);
+    it.b = __builtin_amdgcn_readfirstlane(it.b), it.r0 = __builtin_amdgcn_readfirstlane(it.r0), it.part = __builtin_amdgcn_readfirstlane(it.part);
+    it.total = __builtin_amdgcn_readfirstlane(it.total);
+    return it;
+}
+
+template <int DH, int BITS>
+__device__ __forceinline__ void many_rows(const PagesView& cache, const PagesAttention& a, int group, int h, int b, int r0, int part,
+                                          int chunk, uint4* lds) {
+    constexpr int WAVES = MANY_WAVES, CPR = DH / 8, STEPS = DH / 16, DB = DH / 32, KB = DH * BITS / 8;
+    constexpr int TILE = MANY_KT * CPR;             // 16-byte chunks of a tile of keys, or of values; LDS: [2] keys, [2] values
+    constexpr int THREADS = WAVES * 64, LD = TILE / THREADS;
     __shared__ int sh_first[2 * DH], sh_bad;
 
-    const int h = blockIdx.x, b = blockIdx.z / parts, part = blockIdx.z % parts;
-    const int r0 = (gridDim.y - 1 - blockIdx.y) * BLOCK;    // (rows that see most first)
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int fr = lane & 31, fg = lane >> 5;
     const PageSpan span = page_span(a.start, a.length, b, a.n, min(cache.pitch << cache.log_page, a.max_len));
-    const ManyRows work = many_rows(span, a.max_q, group, r0, BLOCK);
-    if (work.rows <= FEW_ROWS || r0 >= work.rows) return;
-    const int used = max((work.n_tiles + chunk - 1) / chunk, 1);
+    const int rows = min(span.count, a.max_q) * group;
+    const int n_tiles = (page_seen(span, (min(r0 + MANY_BLOCK, rows) - 1) / group) + MANY_KT - 1) / MANY_KT;
+    const int used = max((n_tiles + chunk - 1) / chunk, 1);
     if (part >= used) return;
-    const int kt0 = part * chunk, kt1 = min(kt0 + chunk, work.n_tiles);
+    const int kt0 = part * chunk, kt1 = min(kt0 + chunk, n_tiles);
 
     const int my_row = r0 + wave * MANY_WAVE_ROWS + fr, my_i = my_row / group;
-    const bool real = my_row < work.rows;
+    const bool real = my_row < rows;
     // (a row that is none takes part as if it saw everything and is not stored)
     const int limit = real ? page_seen(span, my_i) : span.len;
+    const int own_limit = limit - 8 * fg;
     const int least = page_seen(span, r0 / group);      // slots that all rows of the workgroup see
     const int wave_row0 = r0 + wave * MANY_WAVE_ROWS;   // ... and that some row of the wave sees
-    const int wave_most = wave_row0 < work.rows ? page_seen(span, (min(wave_row0 + MANY_WAVE_ROWS, work.rows) - 1) / group) : 0;
+    const int wave_most = wave_row0 < rows ? page_seen(span, (min(wave_row0 + MANY_WAVE_ROWS, rows) - 1) / group) : 0;
 
     uint4 qf[STEPS];
 #pragma unroll
@@ -496,16 +576,18 @@ __global__ __launch_bounds__(WAVES * 64, 2) void many_pages_kernel(PagesView cac
     constexpr int CHUNKS = PER / 8;                                    // 16-byte chunks of bf16 that they become
     static_assert(64 / TPR <= 16 && PER <= 32, "");
     const int c_row = tid / TPR, c_part = tid % TPR, c_group = wave * 64 / TPR / 16;   // (a wave's rows lie in one group)
-    const uint32_t c_off = (uint32_t)((c_row & 15) * KB + c_part * PER), e_off = (uint32_t)((c_row & 15) * NB + c_part * PER / 32);
+    const uint32_t c_off = (uint32_t)((c_row & 15) * KB + c_part * PER);               // (in bytes of codes; of powers a 32nd)
     const int lds_key_row = many_slot(c_row);
     const uint32_t k_put = (uint32_t)(lds_key_row * CPR + (c_part * CHUNKS ^ key_swizzle<DH>(lds_key_row))) * 16u;
     const uint32_t v_put = (uint32_t)(c_row * CPR + (c_part * CHUNKS ^ value_swizzle<DH>(c_row))) * 16u;
     auto load_codes = [&](Codes& x, const uint8_t* codes, const uint8_t* powers, const TilePages& s) __attribute__((always_inline)) {
         const size_t at = group_at(s, c_group);
         const uint8_t *c = codes + at, *e = powers + at / 32;
+        uint32_t off = c_off;
+        asm volatile("" : "+v"(off));         // (a 32-bit place from the wave's base: sums with the bases would be kept, and spill)
 #pragma unroll
-        for (int i = 0; i < PER / 16; ++i) x.w[i] = *reinterpret_cast<const uint4*>(c + c_off + i * 16);
-        x.e = e[e_off];
+        for (int i = 0; i < PER / 16; ++i) x.w[i] = *reinterpret_cast<const uint4*>(c + off + i * 16);
+        x.e = e[off >> 5];
     };
     auto put_codes = [&](const Codes& x, uint32_t put, uint32_t tile) __attribute__((always_inline)) {
         asm volatile("" : "+v"(put));
@@ -558,7 +640,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void many_pages_kernel(PagesView cac
     auto mask = [&](f32x16_t (&s)[2], float& m, int kt, uint32_t missing) __attribute__((always_inline)) {
         const int key0 = kt * MANY_KT;
         if (key0 + MANY_KT <= least && !missing) return;
-        const int left = limit - key0 - 8 * fg;     // slots that the row sees from this lane's first on
+        const int left = own_limit - key0;          // slots that the row sees from this lane's first on
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -572,9 +654,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void many_pages_kernel(PagesView cac
     };
     // The sums' reference stays until a logit passes it by SLACK in powers of two: exponentials are at most 2^SLACK then,
     // and the sums are hardly ever scaled again after the first tiles.
-    const float slack = SLACK / scale_log2e;
     auto rescale = [&](float tile_m) __attribute__((always_inline)) {
-        const float new_m = tile_m > run_m + slack ? tile_m : run_m;
+        const float new_m = (tile_m - run_m) * scale_log2e > SLACK ? tile_m : run_m;
         if (__any(new_m != run_m)) {
             const float corr = new_m == run_m ? 1.f : __builtin_amdgcn_exp2f((run_m - new_m) * scale_log2e);
             run_l *= corr;
@@ -648,7 +729,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void many_pages_kernel(PagesView cac
     // takes values that are no finite numbers, or that no row sees, out of a tile that not all rows see whole
     const FirstBad first = {sh_first, sh_first + DH};
     auto clean = [&](uint4* tile, int kt, uint32_t missing) __attribute__((always_inline)) {
-        int from = tid;
+        int from = wave * 64 + (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
         asm volatile("" : "+v"(from));        // (nothing of this in registers between the tiles that need it)
 #pragma unroll 1
         for (int at = from; at < TILE; at += THREADS) {
@@ -769,21 +850,22 @@ __global__ __launch_bounds__(WAVES * 64, 2) void many_pages_kernel(PagesView cac
                 const int dim = d * 32 + 8 * (v >> 2) + 4 * fg + (v & 3);
                 o_acc[d][v] += bad_part(sh_first[dim], sh_first[DH + dim], limit);
             }
+    const MixedArgs n = late_args();
     const int to = span.row0 + my_i, head = h * group + my_row % group;
     if (used > 1) {
-        const size_t row = ((size_t)part * a.n + to) * a.H + head;
-        if (fg == 0) part_ml[row] = make_float2(run_m, l);
+        const size_t row = ((size_t)part * n.a.n + to) * n.a.H + head;
+        if (fg == 0) n.parts.many_ml[row] = make_float2(run_m, l);
 #pragma unroll
         for (int d = 0; d < DB; ++d)
 #pragma unroll
             for (int v4 = 0; v4 < 4; ++v4)
-                *reinterpret_cast<float4*>(part_o + row * DH + d * 32 + 8 * v4 + 4 * fg) =
+                *reinterpret_cast<float4*>(n.parts.many_o + row * DH + d * 32 + 8 * v4 + 4 * fg) =
                     make_float4(o_acc[d][v4 * 4], o_acc[d][v4 * 4 + 1], o_acc[d][v4 * 4 + 2], o_acc[d][v4 * 4 + 3]);
         return;
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
-    if (a.lse && fg == 0) a.lse[(size_t)to * a.H + head] = l == 0.f ? -INFINITY : run_m * a.scale + logf(l);
-    bf16_t* orow = const_cast<bf16_t*>(a.out.p) + (int64_t)to * a.out.token + (int64_t)head * a.out.head;
+    if (n.a.lse && fg == 0) n.a.lse[(size_t)to * n.a.H + head] = l == 0.f ? -INFINITY : run_m * n.a.scale + logf(l);
+    bf16_t* orow = const_cast<bf16_t*>(n.a.out.p) + (int64_t)to * n.a.out.token + (int64_t)head * n.a.out.head;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -793,56 +875,106 @@ __global__ __launch_bounds__(WAVES * 64, 2) void many_pages_kernel(PagesView cac
                            pack_bf16x2(o_acc[d][v4 * 4 + 2] * inv, o_acc[d][v4 * 4 + 3] * inv));
 }
 
-// ---- the parts of a row --------------------------------------------------------------------------------------------
-// A wave a row, four rows a workgroup; lane p knows part p's maximum and sum, half a wave (of 128 dims) adds every
-// second part.
-constexpr int JOIN_WAVES = 4, MAX_PARTS = 64;
+// One launch for both: the first workgroups have many rows (`wanted` of them a key head, or as many as there are blocks),
+// the others few, so that a prompt's products go beside the memory reads of answers' next tokens.
+template <int DH, int BITS>
+__global__ __launch_bounds__(MANY_WAVES * 64, 2) void mixed_pages_kernel(MixedArgs m) {
+    extern __shared__ uint4 lds[];
+    const int x = blockIdx.x;
+    if (x >= m.workgroups * m.cache.H_kv) {
+        const int f = x - m.workgroups * m.cache.H_kv, h = f % m.cache.H_kv, b = f / m.cache.H_kv % m.cache.B;
+        few_rows<DH, BITS, MANY_WAVES>(m.cache, m.a, m.group, m.parts.few_chunk, m.parts.few_pitch, m.parts.few_o, m.parts.few_ml,
+                                       f / m.cache.H_kv / m.cache.B, h, b, reinterpret_cast<float4*>(lds));
+        return;
+    }
+    for (int turn = 0;; ++turn) {              // (once, unless starts overlap)
+        const MixedArgs n = late_args();
+        const int h = x % n.cache.H_kv, item = x / n.cache.H_kv + turn * n.workgroups;
+        const ManyItem it = many_item(n.cache, n.a, n.group, item, n.wanted, n.parts.many_most, n.parts.few_parts);
+        if (x == 0 && turn == 0 && threadIdx.x == 0) n.parts.many_chunk[0] = it.chunk, n.parts.many_chunk[1] = it.parted;
+        if (it.b < 0) return;
+        many_rows<DH, BITS>(n.cache, n.a, n.group, h, it.b, it.r0, it.part, it.chunk, lds);
+        if (item + n.workgroups >= it.total) return;
+        __syncthreads();
+    }
+}
 
-// MANY: rows of many_pages_kernel, whose workgroups have `block` rows each and parts of `chunk` tiles; else of
-// few_pages_kernel.
-template <int DH, bool MANY>
-__global__ __launch_bounds__(JOIN_WAVES * 64) void join_pages_kernel(PagesView cache, PagesAttention a, int group, int chunk,
-                                                                     int block, int pitch, const float* __restrict__ part_o,
-                                                                     const float2* __restrict__ part_ml) {
+// ---- the parts of a row --------------------------------------------------------------------------------------------
+// A wave takes a token's rows of JOIN_HEADS heads, whose loads do not wait for each other; lane p knows part p's maximum and
+// sum, half a wave (of 128 dims) adds every second part.
+constexpr int JOIN_WAVES = 4, JOIN_HEADS = 4, MAX_PARTS = 64;
+
+template <int DH>
+__global__ __launch_bounds__(JOIN_WAVES * 64) void join_pages_kernel(PagesView cache, PagesAttention a, int group, PageParts parts) {
     constexpr int QUADS = DH / 4, SHARES = 64 / QUADS;
-    const int h = blockIdx.y, b = blockIdx.z, lane = threadIdx.x & 63;
-    const int r = blockIdx.x * JOIN_WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, runs = (a.H + JOIN_HEADS - 1) / JOIN_HEADS;
+    // (behind workgroups of many rows: whether there are parts at all)
+    if (parts.many_chunk && !parts.many_chunk[1]) return;
+    const uint32_t id = blockIdx.x * JOIN_WAVES + (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (id >= (uint32_t)a.n * (uint32_t)runs) return;
+    const int to = (int)(id / (uint32_t)runs), head0 = (int)(id % (uint32_t)runs) * JOIN_HEADS;
+    const int b = sequence_of(a.start, cache.B, to, to);
     const PageSpan span = page_span(a.start, a.length, b, a.n, min(cache.pitch << cache.log_page, a.max_len));
-    const int rows = min(span.count, a.max_q) * group;
-    if (r >= rows || (rows > FEW_ROWS) != MANY) return;
-    const int last = MANY ? min(r / block * block + block, rows) - 1 : rows - 1;      // (of the row's workgroup)
-    constexpr int STEP = MANY ? MANY_KT : FEW_STEP;
-    const int n_steps = (page_seen(span, last / group) + STEP - 1) / STEP;
-    const int used = (n_steps + chunk - 1) / chunk;
-    if (used <= 1) return;
+    const int i = to - span.row0, rows = min(span.count, a.max_q) * group;
+    if (i < 0 || i >= min(span.count, a.max_q)) return;
+    const bool many = rows > FEW_ROWS;
+    const int step = many ? MANY_KT : FEW_STEP, chunk = many ? parts.many_chunk[0] : parts.few_chunk;
     const float scale_log2e = a.scale * 1.4426950408889634f;
-    const int to = span.row0 + r / group, head = h * group + r % group;
-    const size_t row = MANY ? (size_t)to * a.H + head : ((size_t)b * cache.H_kv + h) * pitch + r;
-    const size_t apart = MANY ? (size_t)a.n * a.H : (size_t)cache.B * cache.H_kv * pitch;
-    const float2 ml = lane < used ? part_ml[lane * apart + row] : make_float2(-INFINITY, 0.f);
-    float m = ml.x;
+    const size_t apart = many ? (size_t)a.n * a.H : (size_t)cache.B * cache.H_kv * parts.few_pitch;
+    const float* part_o = many ? parts.many_o : parts.few_o;
+    const float2* part_ml = many ? parts.many_ml : parts.few_ml;
+    int used[JOIN_HEADS], most = 0;
+    size_t row[JOIN_HEADS];
+    float2 ml[JOIN_HEADS];
 #pragma unroll
-    for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-    const float f = ml.x == m ? 1.f : __builtin_amdgcn_exp2f((ml.x - m) * scale_log2e);
-    const float l = wave_sum_f32(ml.y * f);
+    for (int k = 0; k < JOIN_HEADS; ++k) {
+        const int head = min(head0 + k, a.H - 1), h = head / group, r = i * group + head % group;
+        const int last = many ? min(r / MANY_BLOCK * MANY_BLOCK + MANY_BLOCK, rows) - 1 : rows - 1;   // (of the row's workgroup)
+        used[k] = head0 + k < a.H ? ((page_seen(span, last / group) + step - 1) / step + chunk - 1) / chunk : 0;
+        row[k] = many ? (size_t)to * a.H + head : ((size_t)b * cache.H_kv + h) * parts.few_pitch + r;
+        ml[k] = used[k] > 1 && lane < used[k] ? part_ml[lane * apart + row[k]] : make_float2(-INFINITY, 0.f);
+        most = max(most, used[k]);
+    }
+    if (most <= 1) return;
     const int share = lane / QUADS, ch = lane % QUADS * 4;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int p0 = 0; p0 < used; p0 += SHARES) {
+    float m[JOIN_HEADS], f[JOIN_HEADS], l[JOIN_HEADS];
+    float4 acc[JOIN_HEADS];
+#pragma unroll
+    for (int k = 0; k < JOIN_HEADS; ++k) {
+        m[k] = ml[k].x;
+#pragma unroll
+        for (int o = 32; o; o >>= 1) m[k] = fmaxf(m[k], __shfl_xor(m[k], o));
+        f[k] = ml[k].x == m[k] ? 1.f : __builtin_amdgcn_exp2f((ml[k].x - m[k]) * scale_log2e);
+        l[k] = wave_sum_f32(ml[k].y * f[k]);
+        acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    for (int p0 = 0; p0 < most; p0 += SHARES) {
         const int p = p0 + share;
-        const float fp = __shfl(f, min(p, 63));
-        if (p < used) {
-            const float4 t = *reinterpret_cast<const float4*>(part_o + (p * apart + row) * DH + ch);
-            acc.x = fmaf(t.x, fp, acc.x), acc.y = fmaf(t.y, fp, acc.y), acc.z = fmaf(t.z, fp, acc.z), acc.w = fmaf(t.w, fp, acc.w);
+        float4 t[JOIN_HEADS];
+#pragma unroll
+        for (int k = 0; k < JOIN_HEADS; ++k)
+            t[k] = used[k] > 1 && p < used[k] ? *reinterpret_cast<const float4*>(part_o + (p * apart + row[k]) * DH + ch)
+                                              : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int k = 0; k < JOIN_HEADS; ++k) {
+            const float fp = __shfl(f[k], min(p, 63));
+            acc[k].x = fmaf(t[k].x, fp, acc[k].x), acc[k].y = fmaf(t[k].y, fp, acc[k].y);
+            acc[k].z = fmaf(t[k].z, fp, acc[k].z), acc[k].w = fmaf(t[k].w, fp, acc[k].w);
         }
     }
 #pragma unroll
-    for (int o = QUADS; o < 64; o <<= 1)
-        acc.x += __shfl_xor(acc.x, o), acc.y += __shfl_xor(acc.y, o), acc.z += __shfl_xor(acc.z, o), acc.w += __shfl_xor(acc.w, o);
-    if (share) return;
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    *reinterpret_cast<uint2*>(const_cast<bf16_t*>(a.out.p) + (int64_t)to * a.out.token + (int64_t)head * a.out.head + ch) =
-        make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
-    if (a.lse && ch == 0) a.lse[(size_t)to * a.H + head] = l == 0.f ? -INFINITY : m * a.scale + logf(l);
+    for (int k = 0; k < JOIN_HEADS; ++k) {
+#pragma unroll
+        for (int o = QUADS; o < 64; o <<= 1)
+            acc[k].x += __shfl_xor(acc[k].x, o), acc[k].y += __shfl_xor(acc[k].y, o), acc[k].z += __shfl_xor(acc[k].z, o),
+                acc[k].w += __shfl_xor(acc[k].w, o);
+        if (share || used[k] <= 1) continue;
+        const float inv = l[k] == 0.f ? 0.f : 1.f / l[k];
+        const int head = head0 + k;
+        *reinterpret_cast<uint2*>(const_cast<bf16_t*>(a.out.p) + (int64_t)to * a.out.token + (int64_t)head * a.out.head + ch) =
+            make_uint2(pack_bf16x2(acc[k].x * inv, acc[k].y * inv), pack_bf16x2(acc[k].z * inv, acc[k].w * inv));
+        if (a.lse && ch == 0) a.lse[(size_t)to * a.H + head] = l[k] == 0.f ? -INFINITY : m[k] * a.scale + logf(l[k]);
+    }
 }
 
 // ---- host --------------------------------------------------------------------------------------------------------
@@ -865,11 +997,15 @@ struct FewPlan {
     int waves, parts, chunk;
 };
 // room: rows of parts that there is memory for
-FewPlan few_plan(int64_t heads, int64_t rows, int max_len, int64_t room) {
+FewPlan few_plan(int64_t heads, int64_t rows, int max_len, int64_t room, bool mixed) {
     FewPlan p;
     const int64_t cus = device_cu_count(), steps = ((int64_t)max_len + FEW_STEP - 1) / FEW_STEP;
-    p.waves = heads <= cus ? 8 : 4;
-    int64_t parts = std::min<int64_t>((4 * cus + heads - 1) / heads, (steps + p.waves - 1) / p.waves);
+    p.waves = heads <= cus && !mixed ? 8 : 4;
+    // enough workgroups to fill the chip, and where they would still be long (eight steps a wave) so many that sequences of
+    // different lengths even out
+    const int64_t fill = std::min((4 * cus + heads - 1) / heads, (steps + p.waves - 1) / p.waves);
+    const int64_t even = std::min(steps / (8 * p.waves), (16 * cus + heads - 1) / heads);
+    int64_t parts = std::max(fill, even);
     parts = std::max<int64_t>(1, std::min<int64_t>({parts, (int64_t)MAX_PARTS, room / (heads * rows)}));
     p.chunk = (int)((steps + parts - 1) / parts);
     p.parts = (int)((steps + p.chunk - 1) / p.chunk);
@@ -877,81 +1013,70 @@ FewPlan few_plan(int64_t heads, int64_t rows, int max_len, int64_t room) {
 }
 
 template <int DH, int BITS, int WAVES>
-int launch_few(const PagesView& c, const PagesAttention& a, int group, const FewPlan& p, int rows, float* o, float2* ml,
-               hipStream_t st) {
+int launch_few(const PagesView& c, const PagesAttention& a, int group, const FewPlan& p, const PageParts& parts, hipStream_t st) {
     static bool lds_set[kMaxDevices] = {};
     const size_t lds = (size_t)WAVES * FEW_ROWS * DH * 4;
     if (int rc = allow_lds(reinterpret_cast<const void*>(&few_pages_kernel<DH, BITS, WAVES>), lds_set, lds)) return rc;
-    hipLaunchKernelGGL((few_pages_kernel<DH, BITS, WAVES>), dim3(c.H_kv * p.parts, c.B), dim3(WAVES * 64), lds, st, c, a, group,
-                       p.parts, p.chunk, rows, o, ml);
+    hipLaunchKernelGGL((few_pages_kernel<DH, BITS, WAVES>), dim3(c.H_kv, c.B, p.parts), dim3(WAVES * 64), lds, st, c, a, group,
+                       p.chunk, parts.few_pitch, parts.few_o, parts.few_ml);
     MVLA_HIP_CHECK(hipGetLastError());
     return MVLA_OK;
 }
 
-template <int DH, int BITS, int WAVES>
-int launch_many(const PagesView& c, const PagesAttention& a, int group, const FewPlan& p, float* o, float2* ml, hipStream_t st) {
+template <int DH, int BITS>
+int launch_mixed(const PagesView& c, const PagesAttention& a, int group, int workgroups, int wanted, const PageParts& parts,
+                 hipStream_t st) {
     static bool lds_set[kMaxDevices] = {};
-    const size_t lds = (size_t)4 * MANY_KT * DH * 2;
-    if (int rc = allow_lds(reinterpret_cast<const void*>(&many_pages_kernel<DH, BITS, WAVES>), lds_set, lds)) return rc;
-    const int blocks = (a.max_q * group + WAVES * MANY_WAVE_ROWS - 1) / (WAVES * MANY_WAVE_ROWS);
-    hipLaunchKernelGGL((many_pages_kernel<DH, BITS, WAVES>), dim3(c.H_kv, blocks, c.B * p.parts), dim3(WAVES * 64), lds, st, c, a,
-                       group, p.parts, p.chunk, o, ml);
+    const size_t lds = std::max<size_t>((size_t)4 * MANY_KT * DH * 2, (size_t)MANY_WAVES * FEW_ROWS * DH * 4);
+    if (int rc = allow_lds(reinterpret_cast<const void*>(&mixed_pages_kernel<DH, BITS>), lds_set, lds)) return rc;
+    const unsigned grid = (unsigned)c.H_kv * ((unsigned)workgroups + (unsigned)parts.few_parts * (unsigned)c.B);
+    const MixedArgs m = {c, a, parts, group, workgroups, wanted};
+    hipLaunchKernelGGL((mixed_pages_kernel<DH, BITS>), dim3(grid), dim3(MANY_WAVES * 64), lds, st, m);
     MVLA_HIP_CHECK(hipGetLastError());
     return MVLA_OK;
-}
-
-// parts of many rows: two workgroups a compute unit, eight tiles each at least
-FewPlan many_plan(int64_t wgs, int max_len, int64_t rows, int64_t B, int64_t room) {
-    FewPlan p;
-    p.waves = 4;
-    const int64_t cus = device_cu_count(), tiles = ((int64_t)max_len + MANY_KT - 1) / MANY_KT;
-    int64_t parts = std::min<int64_t>(2 * cus / wgs, (tiles + 7) / 8);
-    parts = std::max<int64_t>(1, std::min<int64_t>({parts, (int64_t)MAX_PARTS, room / rows, 65535 / B}));
-    p.chunk = (int)((tiles + parts - 1) / parts);
-    p.parts = (int)((tiles + p.chunk - 1) / p.chunk);
-    return p;
 }
 
 template <int DH>
 int run_pages(const PagesView& c, const PagesAttention& a, char* scratch, size_t scratch_bytes, hipStream_t st) {
     const int group = a.H / c.H_kv;
     const int64_t heads = (int64_t)c.B * c.H_kv, rows = (int64_t)a.max_q * group;
-    const int64_t room = (int64_t)((scratch_bytes - 256) / (DH * 4 + 8));
-    const int few_rows = (int)std::min<int64_t>(FEW_ROWS, rows);
-    // parts of many rows lie behind those of few
-    const int64_t few_room = std::min<int64_t>(FEW_PART_ROWS, room);
-    const int64_t many_room = std::min<int64_t>(MANY_PART_ROWS, room - few_room);
-    float2* ml = reinterpret_cast<float2*>(scratch);
-    float* o = reinterpret_cast<float*>(scratch + align_up((size_t)(few_room + many_room) * 8, 256));
-    if (group <= FEW_ROWS) {
-        const FewPlan p = few_plan(heads, few_rows, a.max_len, few_room);
-        int rc;
+    // scratch: 256 bytes, maxima and sums, outputs; parts of many rows behind those of few
+    const int64_t room = (int64_t)((scratch_bytes - std::min<size_t>(scratch_bytes, 512)) / (DH * 4 + 8));
+    const int64_t few_room = std::min<int64_t>(FEW_PART_ROWS, room), many_room = std::min<int64_t>(MANY_PART_ROWS, room - few_room);
+    PageParts parts;
+    parts.many_chunk = reinterpret_cast<int*>(scratch);
+    parts.few_ml = reinterpret_cast<float2*>(scratch + 256);
+    parts.many_ml = parts.few_ml + few_room;
+    parts.few_o = reinterpret_cast<float*>(scratch + 256 + align_up((size_t)(few_room + many_room) * 8, 256));
+    parts.many_o = parts.few_o + few_room * DH;
+    parts.few_pitch = (int)std::min<int64_t>(FEW_ROWS, rows);
+    const bool mixed = rows > FEW_ROWS;
+    const FewPlan p = few_plan(heads, parts.few_pitch, a.max_len, few_room, mixed);
+    parts.few_chunk = p.chunk;
+    parts.few_parts = group > FEW_ROWS ? 0 : p.parts;
+    parts.many_most = (int)std::max<int64_t>(1, std::min<int64_t>(MAX_PARTS, many_room / ((int64_t)a.n * a.H)));
+    bool join = parts.few_parts > 1;
+    int rc;
+    if (!mixed) {
+        parts.many_chunk = nullptr;
         if (c.bits == 16)
-            rc = p.waves == 8 ? launch_few<DH, 16, 8>(c, a, group, p, few_rows, o, ml, st) : launch_few<DH, 16, 4>(c, a, group, p, few_rows, o, ml, st);
+            rc = p.waves == 8 ? launch_few<DH, 16, 8>(c, a, group, p, parts, st) : launch_few<DH, 16, 4>(c, a, group, p, parts, st);
         else
-            rc = p.waves == 8 ? launch_few<DH, 8, 8>(c, a, group, p, few_rows, o, ml, st) : launch_few<DH, 8, 4>(c, a, group, p, few_rows, o, ml, st);
-        if (rc) return rc;
-        if (p.parts > 1) {
-            hipLaunchKernelGGL((join_pages_kernel<DH, false>), dim3((few_rows + JOIN_WAVES - 1) / JOIN_WAVES, c.H_kv, c.B),
-                               dim3(JOIN_WAVES * 64), 0, st, c, a, group, p.chunk, 0, few_rows, o, ml);
-            MVLA_HIP_CHECK(hipGetLastError());
-        }
+            rc = p.waves == 8 ? launch_few<DH, 8, 8>(c, a, group, p, parts, st) : launch_few<DH, 8, 4>(c, a, group, p, parts, st);
+    } else {
+        // (blocks: as many as there can be; sequences' rows together are no more than the call's)
+        const int64_t blocks = std::min<int64_t>(c.B * ((rows + MANY_BLOCK - 1) / MANY_BLOCK), (int64_t)a.n * group / MANY_BLOCK + c.B);
+        const int wanted = (int)std::max<int64_t>(1, 2 * (int64_t)device_cu_count() / c.H_kv);
+        const int workgroups = (int)std::max<int64_t>(wanted, blocks);
+        join |= parts.many_most > 1 && a.max_len > MANY_LEAST * MANY_KT;
+        rc = c.bits == 16 ? launch_mixed<DH, 16>(c, a, group, workgroups, wanted, parts, st)
+                          : launch_mixed<DH, 8>(c, a, group, workgroups, wanted, parts, st);
     }
-    if (rows <= FEW_ROWS) return MVLA_OK;
-    constexpr int WAVES = 4, BLOCK = WAVES * MANY_WAVE_ROWS;
-    // (workgroups that have rows: of all sequences' blocks no more than the packed rows fill)
-    const int64_t blocks = std::min<int64_t>(c.B * ((rows + BLOCK - 1) / BLOCK), (int64_t)a.n * group / BLOCK + c.B);
-    const FewPlan p = many_plan(c.H_kv * blocks, a.max_len, (int64_t)a.n * a.H, c.B, many_room);
-    float2* many_ml = ml + few_room;
-    float* many_o = o + few_room * DH;
-    if (int rc = c.bits == 16 ? launch_many<DH, 16, WAVES>(c, a, group, p, many_o, many_ml, st)
-                              : launch_many<DH, 8, WAVES>(c, a, group, p, many_o, many_ml, st))
-        return rc;
-    if (p.parts > 1) {
-        hipLaunchKernelGGL((join_pages_kernel<DH, true>), dim3((unsigned)((rows + JOIN_WAVES - 1) / JOIN_WAVES), c.H_kv, c.B),
-                           dim3(JOIN_WAVES * 64), 0, st, c, a, group, p.chunk, BLOCK, 0, many_o, many_ml);
-        MVLA_HIP_CHECK(hipGetLastError());
-    }
+    if (rc || !join) return rc;
+    const uint32_t waves = (uint32_t)a.n * (uint32_t)((a.H + JOIN_HEADS - 1) / JOIN_HEADS);
+    hipLaunchKernelGGL((join_pages_kernel<DH>), dim3((waves + JOIN_WAVES - 1) / JOIN_WAVES), dim3(JOIN_WAVES * 64), 0, st, c, a, group,
+                       parts);
+    MVLA_HIP_CHECK(hipGetLastError());
     return MVLA_OK;
 }
 
@@ -963,7 +1088,7 @@ size_t pages_attention_bytes(int B, int H, int H_kv, int dh, int n, int max_q, i
     size_t all = FEW_PART_ROWS;     // (whole: the parts of many rows lie behind them)
     if (rows <= FEW_ROWS) all = std::min<size_t>((size_t)B * H_kv * rows * most, FEW_PART_ROWS);
     else all += std::min<size_t>((size_t)n * H * most, MANY_PART_ROWS);
-    return all * (dh * 4 + 8) + 512;
+    return all * (dh * 4 + 8) + 1024;
 }
 
 int launch_pages_attention(const PagesView& c, const PagesAttention& a, char* scratch, size_t scratch_bytes, hipStream_t st) {

@@ -16,17 +16,6 @@ __device__ __forceinline__ uint32_t limited(uint32_t pair) {
     return (pair & 0x80008000u) | m;
 }
 
-// The sequence whose rows hold packed row i, as far as the starts are ascending (in [0, B) whatever they are).  `first`:
-// the same row for all lanes of a wave, not behind i.
-__device__ __forceinline__ int sequence_of(const int32_t* start, int B, int first, int i) {
-    const int lane = threadIdx.x & 63;
-    int b = 0;
-    for (int at = 0; at < B; at += 64)      // the loads of a wave do not wait for each other, as a binary search's would
-        b += __popcll(__ballot(at + lane < B && start[at + lane + 1] <= first));
-    while (b < B - 1 && start[b + 1] <= i) ++b;
-    return min(b, B - 1);
-}
-
 // ---- rows into pages ---------------------------------------------------------------------------------------------
 // A lane takes eight values of a token's row (16 bytes, whole lines per wave); four lanes are a block of 32 and agree
 // on its largest magnitude by two quad permutes.  blockIdx.y: keys or values.
