@@ -1278,6 +1278,8 @@ struct OnDevice {
     }
 };
 
+constexpr int64_t kMaxPageHeads = 1 << 22, kMaxPageRows = 1 << 28;   // key heads of all sequences, query rows of all heads
+
 bool positive(double x) { return x > 0.0 && x <= 1e300; }
 
 int check_pages(const mvla_pages* c) {
@@ -1294,7 +1296,7 @@ int check_pages(const mvla_pages* c) {
 int check_page_batch(const mvla_page_batch* s, const mvla_pages& c, bool rows) {
     if (!s || !s->table || (rows && (!s->start || !s->length))) return MVLA_EINVAL;
     if (s->B <= 0 || s->table_pitch <= 0) return MVLA_EINVAL;
-    if (s->B > kMaxGrid || (int64_t)s->table_pitch * c.page > kMaxSlots) return MVLA_EUNSUPPORTED;
+    if (s->B > kMaxGrid || (int64_t)s->B * c.H_kv > kMaxPageHeads || (int64_t)s->table_pitch * c.page > kMaxSlots) return MVLA_EUNSUPPORTED;
     return MVLA_OK;
 }
 
@@ -1315,7 +1317,7 @@ int mvla_rotation_table(mvla_ctx* ctx, const mvla_rotation* how, int rope_len, f
     if (how->factor > 1.0 && (!positive(how->trained) || !(how->low_turns >= 0.0) || !(how->high_turns > how->low_turns) ||
                               !positive(how->high_turns)))
         return MVLA_EINVAL;
-    if (how->rotated > 256) return MVLA_EUNSUPPORTED;
+    if (how->rotated > 256 || (int64_t)rope_len * (how->rotated / 2) >= (int64_t)1 << 31) return MVLA_EUNSUPPORTED;
     const OnDevice on(ctx->device);
     int rc;
     TIMED(ctx, KID_ROPE_TABLE, rope_len, launch_rotation_table(*how, rope_len, cos_out, sin_out, ctx->stream));
@@ -1333,7 +1335,7 @@ int mvla_rotate(mvla_ctx* ctx, const mvla_rows* q, int H, const mvla_rows* q_out
     if (!q || !q_out || !pos || !aligned(pos, 4)) return MVLA_EINVAL;
     for (const mvla_rows* r : {q, q_out, k, k_out})
         if (r && (!r->data || !aligned(r->data, 2))) return MVLA_EINVAL;
-    if ((uint64_t)B * n >= (uint64_t)1 << 30 || (uint64_t)B * n * (H + (k ? H_kv : 0)) * dh >= (uint64_t)1 << 38) return MVLA_EUNSUPPORTED;
+    if ((uint64_t)B * n >= (uint64_t)1 << 30 || (uint64_t)B * n * (H + (k ? H_kv : 0)) * dh >= (uint64_t)1 << 31) return MVLA_EUNSUPPORTED;
     // in place is in place: the same rows at the same strides
     for (int i = 0; i < 2; ++i) {
         const mvla_rows *in = i ? k : q, *out = i ? k_out : q_out;
@@ -1356,7 +1358,9 @@ int mvla_rotate(mvla_ctx* ctx, const mvla_rows* q, int H, const mvla_rows* q_out
 size_t mvla_pages_workspace_bytes(int B, int H, int H_kv, int dh, int n, int max_q, int max_length) {
     if (B <= 0 || H <= 0 || H_kv <= 0 || H % H_kv != 0 || n <= 0 || max_q <= 0 || max_length <= 0) return 0;
     if (dh != 64 && dh != 128) return 0;
-    if (B > kMaxGrid || H_kv > kMaxGrid / 2 || max_length > kMaxSlots || (int64_t)n * H >= (int64_t)1 << 31) return 0;
+    if (B > kMaxGrid || H_kv > kMaxGrid / 2 || (int64_t)B * H_kv > kMaxPageHeads || max_length > kMaxSlots ||
+        (int64_t)n * H >= kMaxPageRows)
+        return 0;
     return kCounterBytes + gemm_partial_bytes() + align_up(pages_attention_bytes(B, H, H_kv, dh, n, max_q, max_length), 256) + 256;
 }
 
@@ -1403,9 +1407,7 @@ int mvla_pages_attention(mvla_ctx* ctx, const mvla_pages* pages, const mvla_page
     CacheRows qr = cache_rows(*q), outr = cache_rows(*out);
     qr.sample = outr.sample = 0;
     if (!cache_rows_wide(qr) || !cache_rows_wide(outr)) return MVLA_EINVAL;
-    // (rows of a key head, and parts of rows, as the kernels count them)
-    if ((int64_t)n * H >= (int64_t)1 << 31 || (int64_t)(max_q < n ? max_q : n) * (H / pages->H_kv) > 128 * (int64_t)kMaxGrid)
-        return MVLA_EUNSUPPORTED;
+    if ((int64_t)n * H >= kMaxPageRows) return MVLA_EUNSUPPORTED;
     const OnDevice on(ctx->device);
     int rc;
     const PagesAttention a = {qr, outr, batch->start, batch->length, lse, H, n, max_q < n ? max_q : n, max_length, scale};

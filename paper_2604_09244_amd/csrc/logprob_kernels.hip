@@ -18,6 +18,7 @@
 namespace mvla {
 
 constexpr int LP_THREADS = 256, LP_WAVES = LP_THREADS / 64, LP_LIST = 1024;
+constexpr int LP_ROWS = 1 << 22;           // of a launch
 constexpr float LP_LOWEST = -1.0e4f;       // an exponent whose power of two is zero
 
 // order of tokens: larger logit first, then lower index (never 0)
@@ -212,16 +213,18 @@ __global__ __launch_bounds__(LP_THREADS, VPT == 16 ? 3 : 4) void logprob_kernel(
     LpStats s;
     s.m = wave_max_f32(group);
     // ---- sums
-    // d = x k - m k with one rounding of its own; what m k was rounded by is made good behind the sums.  (m k beyond the
-    // largest number: no other logit lies near enough to count)
+    // d = x k - m k with one rounding of its own; what m k was rounded by (a quarter at most below 2^22) is made good behind the
+    // sums.  Beyond that: fp32 logits are subtracted first, and where no other logit than the largest lies near enough to
+    // count (bf16 ones are 2^-8 of the largest apart) every power is zero.
     float k = r.k, mk = s.m * k;
-    if (!(fabsf(mk) < INFINITY)) k = 0.f, mk = INFINITY;
-    const float off = k > 0.f ? fmaf(s.m, k, -mk) : 0.f;
+    const bool far = !HALF && fabsf(mk) >= 0x1p22f && fabsf(mk) < 0x1p40f;
+    if (!far && !(fabsf(mk) < 0x1p22f)) k = 0.f, mk = INFINITY;
+    const float off = k > 0.f && !far ? fmaf(s.m, k, -mk) : 0.f;
     s.rest = s.spread = 0.f;
     s.count = 0;
-    auto sums = [&](auto with_most) __attribute__((always_inline)) {
+    auto sums = [&](auto with_most, auto subtract) __attribute__((always_inline)) {
         auto add = [&](float x) __attribute__((always_inline)) {
-            const float d = fmaxf(fmaf(x, k, -mk), LP_LOWEST);       // (-infinity, and what is no number, to a power of zero)
+            const float d = fmaxf(decltype(subtract)::value ? (x - s.m) * k : fmaf(x, k, -mk), LP_LOWEST);       // (-infinity, and what is no number, to a power of zero)
             float e = __builtin_amdgcn_exp2f(d);
             if constexpr (decltype(with_most)::value) {
                 const bool most = x == s.m;
@@ -238,8 +241,9 @@ __global__ __launch_bounds__(LP_THREADS, VPT == 16 ? 3 : 4) void logprob_kernel(
             for (int e = 0; e < EPV; ++e) add(at(i, e));
     };
     if (s.m > -INFINITY) {
-        if (__any(mine == s.m)) sums(std::true_type{});
-        else sums(std::false_type{});
+        if (!HALF && far) sums(std::true_type{}, std::bool_constant<!HALF>{});
+        else if (__any(mine == s.m)) sums(std::true_type{}, std::false_type{});
+        else sums(std::false_type{}, std::false_type{});
     }
     packed();
     s.spread = fmaf(off, s.rest, s.spread) * __builtin_amdgcn_exp2f(-off);
@@ -415,13 +419,17 @@ static int run_logprobs(const LpArgs& a, int B, char* scratch, size_t scratch_by
     constexpr int EPV = HALF ? 8 : 4, PER = LP_THREADS * VPT;
     const int slices = std::max(1, (a.V / EPV + PER - 1) / PER);
     if (slices == 1) {
-        hipLaunchKernelGGL((logprob_kernel<HALF, VPT>), dim3(B, 1), dim3(LP_THREADS), 0, st, a, 0, nullptr, nullptr, 0);
-        MVLA_HIP_CHECK(hipGetLastError());
+        for (int row0 = 0; row0 < B; row0 += LP_ROWS) {
+            hipLaunchKernelGGL((logprob_kernel<HALF, VPT>), dim3(std::min(B - row0, LP_ROWS), 1), dim3(LP_THREADS), 0, st, a, row0,
+                               nullptr, nullptr, 0);
+            MVLA_HIP_CHECK(hipGetLastError());
+            if (B - row0 <= LP_ROWS) break;
+        }
         return MVLA_OK;
     }
     const int pitch = std::max(a.top, 1);
     const size_t per_row = (size_t)slices * (sizeof(LpStats) + 8 * (size_t)pitch);
-    const int rows = (int)std::min<size_t>((size_t)B, (scratch_bytes - 256) / per_row);
+    const int rows = (int)std::min<size_t>(std::min<size_t>((size_t)B, LP_ROWS), (scratch_bytes - 256) / per_row);
     LpStats* parts = reinterpret_cast<LpStats*>(scratch);
     uint64_t* keys = reinterpret_cast<uint64_t*>(scratch + align_up((size_t)rows * slices * sizeof(LpStats), 256));
     for (int row0 = 0; row0 < B; row0 += rows) {     // (more rows than the scratch holds: in turns)
@@ -430,6 +438,7 @@ static int run_logprobs(const LpArgs& a, int B, char* scratch, size_t scratch_by
         MVLA_HIP_CHECK(hipGetLastError());
         hipLaunchKernelGGL((logprob_join_kernel<HALF>), dim3(n), dim3(LP_THREADS), 0, st, a, row0, slices, parts, keys, pitch);
         MVLA_HIP_CHECK(hipGetLastError());
+        if (B - row0 <= rows) break;
     }
     return MVLA_OK;
 }
