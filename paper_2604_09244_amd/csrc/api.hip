@@ -1426,7 +1426,7 @@ int mvla_logprobs(mvla_ctx* ctx, const void* logits, int half, int64_t row_strid
     int rc;
     TIMED(ctx, KID_LOGPROBS, B, launch_logprobs(logits, half != 0, row_stride, B, V, temperature, tokens, n_tokens, logprob, entropy,
                                                 top, top_token, top_logprob, reinterpret_cast<char*>(ctx->gemm_partial),
-                                                ctx->gemm_partial_bytes, ctx->stream));
+                                                ctx->gemm_partial_bytes, ctx->counters, kCounterWords / 2, ctx->stream));
     return MVLA_OK;
 }
 

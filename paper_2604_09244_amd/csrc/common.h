@@ -244,6 +244,6 @@ int launch_pages_attention(const PagesView& c, const PagesAttention& a, char* sc
 constexpr int LOGPROBS_TOP = 32;
 int launch_logprobs(const void* logits, bool half, int64_t row_stride, int B, int V, const float* temperature,
                     const int32_t* tokens, int n_tokens, float* logprob, float* entropy, int top, int32_t* top_token,
-                    float* top_logprob, char* scratch, size_t scratch_bytes, hipStream_t st);
+                    float* top_logprob, char* scratch, size_t scratch_bytes, uint32_t* counters, int n_counters, hipStream_t st);
 
 }  // namespace mvla

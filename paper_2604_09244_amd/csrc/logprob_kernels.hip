@@ -140,15 +140,102 @@ __device__ __forceinline__ void lp_rank(const uint64_t* list, int count, int n, 
     if (tid >= count && tid < n) best[tid] = 0;
 }
 
-// VPT vectors of 16 bytes a thread.  Slices along blockIdx.y; whole rows (parts null) are finished here.
+// What the slices of a launch's rows leave for the one that ends last: their statistics and best keys, read and written past
+// the caches that the eight XCDs do not share (no fences: they would write back all that lies in them).
+struct LpParts {
+    uint32_t* stats;      // [rows][slices][4], null: whole rows
+    uint64_t* keys;       // [rows][slices][pitch]
+    uint32_t* arrived;    // [rows], zero between launches
+    int pitch;
+};
+template <class T>
+__device__ __forceinline__ void lp_put(T* to, T v) {
+    __hip_atomic_store(to, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+template <class T>
+__device__ __forceinline__ T lp_get(const T* from) {
+    return __hip_atomic_load(from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+struct LpShared {
+    float sum[LP_WAVES], spread[LP_WAVES];
+    uint32_t count[LP_WAVES], n;
+    uint64_t first;
+};
+// The slices of a row joined, a thread each.
+template <bool HALF>
+__device__ __forceinline__ void lp_join(const LpArgs& a, const LpRow& r, int row, const LpParts& parts, int in_launch, int slices, LpShared& sh,
+                                        uint64_t* list, uint64_t* best, int tid) {
+    const int lane = tid & 63, wave = tid >> 6;
+    const size_t first = (size_t)in_launch * slices;
+    const uint32_t* stats = parts.stats + first * 4;
+    const uint64_t* keys = parts.keys + first * parts.pitch;
+    LpStats s = {-INFINITY, 0.f, 0.f, 0u};
+    uint64_t key = 0;
+    if (tid < slices) {
+        s.m = __uint_as_float(lp_get(&stats[tid * 4])), s.rest = __uint_as_float(lp_get(&stats[tid * 4 + 1]));
+        s.spread = __uint_as_float(lp_get(&stats[tid * 4 + 2])), s.count = lp_get(&stats[tid * 4 + 3]);
+        if (r.n > 0) key = lp_get(&keys[(size_t)tid * parts.pitch]);
+    }
+    const float wave_m = wave_max_f32(s.m);
+    if (lane == 0) sh.sum[wave] = wave_m;
+    if (tid == 0) sh.n = 0, sh.first = 1;
+    list[tid] = key;                           // (each slice's best)
+    __syncthreads();
+    float m = sh.sum[0];
+#pragma unroll
+    for (int w = 1; w < LP_WAVES; ++w) m = fmaxf(m, sh.sum[w]);
+    if (s.m == -INFINITY) {
+        s = {-INFINITY, 0.f, 0.f, 0u};
+    } else if (s.m != m) {                     // moved to the row's maximum
+        const float apart = fminf((m - s.m) * r.k, -LP_LOWEST), f = __builtin_amdgcn_exp2f(-apart);
+        const float sum = s.rest + (float)s.count;
+        s.spread = f * (s.spread + apart * sum);
+        s.rest = f * sum;
+        s.count = 0;
+    }
+    s.rest = wave_sum_f32(s.rest);
+    s.spread = wave_sum_f32(s.spread);
+    s.count = wave_sum_u32(s.count);
+    if (r.n > 0 && slices > LP_LIST / LOGPROBS_TOP) {
+        // the n-th largest best key of a slice: at least n keys reach it, and those of n slices at most
+        int place = 0;
+        for (int j = 0; j < slices; ++j) place += list[j] > key;
+        if (key && place == r.n - 1) sh.first = key;
+    }
+    __syncthreads();
+    if (lane == 0) sh.sum[wave] = s.rest, sh.spread[wave] = s.spread, sh.count[wave] = s.count;
+    if (r.n > 0) {
+        const uint64_t least = sh.first;
+        for (int i = tid; i < slices * r.n; i += LP_THREADS) {
+            const uint64_t k = lp_get(&keys[(size_t)(i / r.n) * parts.pitch + i % r.n]);
+            if (k >= least) {
+                const uint32_t to = lds_take(&sh.n, 1u);
+                if (to < LP_LIST) list[to] = k;
+            }
+        }
+        __syncthreads();
+        lp_rank(list, min((int)sh.n, LP_LIST), r.n, best, tid);
+    }
+    __syncthreads();
+    s = {m, 0.f, 0.f, 0u};
+#pragma unroll
+    for (int w = 0; w < LP_WAVES; ++w) s.rest += sh.sum[w], s.spread += sh.spread[w], s.count += sh.count[w];
+    lp_finish<HALF>(a, r, row, s, best, tid);
+}
+
+// VPT vectors of 16 bytes a thread.  Slices along blockIdx.y.  With 1 or 4 vectors all of a launch's workgroups run at once and
+// the last one of a row to end joins its slices (1 x 32768: 14.0 us, and 16.8 with a second launch).  With 16 they take turns,
+// and each would hold its registers until its count has come back: joined by a second launch (2624 x 131073: 174 us, not 220).
 template <bool HALF, int VPT>
-__global__ __launch_bounds__(LP_THREADS, VPT == 16 ? 3 : 4) void logprob_kernel(LpArgs a, int row0, LpStats* __restrict__ parts,
-                                                             uint64_t* __restrict__ part_keys, int key_pitch) {
+__global__ __launch_bounds__(LP_THREADS, VPT == 16 ? 3 : 4) void logprob_kernel(LpArgs a, int row0, LpParts parts) {
     constexpr int EPV = HALF ? 8 : 4, SIZE = HALF ? 2 : 4;
-    __shared__ float sh_max[LP_WAVES][64], sh_group[64], sh_sum[LP_WAVES], sh_spread[LP_WAVES], sh_bound;
-    __shared__ uint32_t sh_count[LP_WAVES], sh_n;
+    __shared__ float sh_max[LP_WAVES][64], sh_group[64], sh_bound;
+    __shared__ bool sh_last;
+    __shared__ LpShared sh;
     __shared__ uint64_t list[LP_LIST], best[LOGPROBS_TOP], sh_key[LP_WAVES];
-    const int row = row0 + blockIdx.x, slice = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int in_launch = blockIdx.x, row = row0 + in_launch, slice = blockIdx.y;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const LpRow r = lp_row(a, row);
     const char* base = static_cast<const char*>(a.logits) + row * a.row_stride * SIZE;
     // the row: up to EPV - 1 logits, whole vectors at 16-byte addresses, up to EPV - 1 logits
@@ -204,7 +291,7 @@ __global__ __launch_bounds__(LP_THREADS, VPT == 16 ? 3 : 4) void logprob_kernel(
     }
     packed();
     sh_max[wave][lane] = mine;
-    if (tid == 0) sh_n = 0;
+    if (tid == 0) sh.n = 0;
     __syncthreads();
     float group = sh_max[0][lane];
 #pragma unroll
@@ -250,7 +337,7 @@ __global__ __launch_bounds__(LP_THREADS, VPT == 16 ? 3 : 4) void logprob_kernel(
     s.rest *= __builtin_amdgcn_exp2f(-off);
     s.rest = wave_sum_f32(s.rest);
     s.spread = wave_sum_f32(s.spread);
-    if (lane == 0) sh_sum[wave] = s.rest, sh_spread[wave] = s.spread, sh_count[wave] = s.count;
+    if (lane == 0) sh.sum[wave] = s.rest, sh.spread[wave] = s.spread, sh.count[wave] = s.count;
     // ---- the most likely tokens
     if (r.n > 0) {
         __syncthreads();
@@ -274,7 +361,7 @@ __global__ __launch_bounds__(LP_THREADS, VPT == 16 ? 3 : 4) void logprob_kernel(
                 uint32_t which = 0;
 #pragma unroll
                 for (int e = 0; e < EPV; ++e) which |= x[e] >= bound && x[e] > -INFINITY ? 1u << e : 0u;
-                uint32_t to = lds_take(&sh_n, (uint32_t)__popc(which));
+                uint32_t to = lds_take(&sh.n, (uint32_t)__popc(which));
 #pragma unroll
                 for (int e = 0; e < EPV; ++e)
                     if (which >> e & 1u) {
@@ -303,7 +390,7 @@ __global__ __launch_bounds__(LP_THREADS, VPT == 16 ? 3 : 4) void logprob_kernel(
             }
         }
         __syncthreads();
-        const int count = (int)sh_n;
+        const int count = (int)sh.n;
         if (count <= LP_LIST) {
             lp_rank(list, count, r.n, best, tid);
         } else {
@@ -341,111 +428,66 @@ __global__ __launch_bounds__(LP_THREADS, VPT == 16 ? 3 : 4) void logprob_kernel(
     __syncthreads();
     s.rest = s.spread = 0.f, s.count = 0;
 #pragma unroll
-    for (int w = 0; w < LP_WAVES; ++w) s.rest += sh_sum[w], s.spread += sh_spread[w], s.count += sh_count[w];
-    if (!parts) {
+    for (int w = 0; w < LP_WAVES; ++w) s.rest += sh.sum[w], s.spread += sh.spread[w], s.count += sh.count[w];
+    if (!parts.stats) {
         lp_finish<HALF>(a, r, row, s, best, tid);
         return;
     }
-    const size_t part = (size_t)blockIdx.x * gridDim.y + slice;
-    if (tid == 0) parts[part] = s;
-    if (tid < r.n) part_keys[part * key_pitch + tid] = best[tid];
+    const int slices = gridDim.y;
+    const size_t first = (size_t)in_launch * slices;
+    if (tid < 4) {
+        const uint32_t w = tid == 0 ? __float_as_uint(s.m) : tid == 1 ? __float_as_uint(s.rest) : tid == 2 ? __float_as_uint(s.spread) : s.count;
+        lp_put(&parts.stats[(first + slice) * 4 + tid], w);
+    }
+    if (tid < r.n) lp_put(&parts.keys[(first + slice) * parts.pitch + tid], best[tid]);
+    if (VPT == 16) return;                     // (joined by a launch)
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (tid == 0) {
+        const uint32_t before = __hip_atomic_fetch_add(&parts.arrived[in_launch], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        sh_last = before == (uint32_t)slices - 1u;
+        if (sh_last) lp_put(&parts.arrived[in_launch], 0u);
+    }
+    __syncthreads();
+    if (!sh_last) return;
+    lp_join<HALF>(a, r, row, parts, in_launch, slices, sh, list, best, tid);
 }
 
-// A row's slices joined.
+// The join of long launches, in a launch of its own.
 template <bool HALF>
-__global__ __launch_bounds__(LP_THREADS) void logprob_join_kernel(LpArgs a, int row0, int slices, const LpStats* __restrict__ parts,
-                                                                  const uint64_t* __restrict__ part_keys, int key_pitch) {
-    __shared__ LpStats sh[LP_WAVES];
-    __shared__ uint64_t list[LP_LIST], best[LOGPROBS_TOP], firsts[LP_THREADS];
-    __shared__ uint32_t sh_n;
-    __shared__ uint64_t sh_bound;
-    const int row = row0 + blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const LpRow r = lp_row(a, row);
-    const LpStats none = {-INFINITY, 0.f, 0.f, 0u};
-    LpStats s = tid < slices ? parts[(size_t)blockIdx.x * slices + tid] : none;
-    if (tid == 0) sh_n = 0, sh_bound = 1;
-    const float mine = wave_max_f32(s.m);
-    if (lane == 0) sh[wave].m = mine;
-    __syncthreads();
-    float m = sh[0].m;
-#pragma unroll
-    for (int w = 1; w < LP_WAVES; ++w) m = fmaxf(m, sh[w].m);
-    if (s.m == -INFINITY) {
-        s = none;
-    } else if (s.m != m) {        // moved to the row's maximum
-        const float apart = fminf((m - s.m) * r.k, -LP_LOWEST), f = __builtin_amdgcn_exp2f(-apart);
-        const float sum = s.rest + (float)s.count;
-        s.spread = f * (s.spread + apart * sum);
-        s.rest = f * sum;
-        s.count = 0;
-    }
-    s.rest = wave_sum_f32(s.rest);
-    s.spread = wave_sum_f32(s.spread);
-    s.count = wave_sum_u32(s.count);
-    if (lane == 0) sh[wave].rest = s.rest, sh[wave].spread = s.spread, sh[wave].count = s.count;
-    if (r.n > 0) {
-        const uint64_t* keys = part_keys + (size_t)blockIdx.x * slices * key_pitch;
-        if (slices > LP_LIST / LOGPROBS_TOP) {
-            // the n-th largest first key of a slice: at least n keys reach it, and those of n slices at most
-            const uint64_t key = tid < slices ? keys[(size_t)tid * key_pitch] : 0;
-            firsts[tid] = key;
-            __syncthreads();
-            int place = 0;
-            for (int j = 0; j < slices; ++j) place += firsts[j] > key;
-            if (key && place == r.n - 1) sh_bound = key;
-            __syncthreads();
-        }
-        const uint64_t bound = sh_bound;
-        for (int i = tid; i < slices * r.n; i += LP_THREADS) {
-            const uint64_t key = keys[(size_t)(i / r.n) * key_pitch + i % r.n];
-            if (key >= bound) {
-                const uint32_t to = atomicAdd(&sh_n, 1u);
-                if (to < LP_LIST) list[to] = key;
-            }
-        }
-        __syncthreads();
-        lp_rank(list, min((int)sh_n, LP_LIST), r.n, best, tid);
-    }
-    __syncthreads();
-    s = {m, 0.f, 0.f, 0u};
-#pragma unroll
-    for (int w = 0; w < LP_WAVES; ++w) s.rest += sh[w].rest, s.spread += sh[w].spread, s.count += sh[w].count;
-    lp_finish<HALF>(a, r, row, s, best, tid);
+__global__ __launch_bounds__(LP_THREADS) void logprob_join_kernel(LpArgs a, int row0, int slices, LpParts parts) {
+    __shared__ LpShared sh;
+    __shared__ uint64_t list[LP_LIST], best[LOGPROBS_TOP];
+    const int row = row0 + blockIdx.x, tid = threadIdx.x;
+    lp_join<HALF>(a, lp_row(a, row), row, parts, blockIdx.x, slices, sh, list, best, tid);
 }
 
 // ---- host --------------------------------------------------------------------------------------------------------
 template <bool HALF, int VPT>
-static int run_logprobs(const LpArgs& a, int B, char* scratch, size_t scratch_bytes, hipStream_t st) {
+static int run_logprobs(const LpArgs& a, int B, char* scratch, size_t scratch_bytes, uint32_t* counters, int n_counters, hipStream_t st) {
     constexpr int EPV = HALF ? 8 : 4, PER = LP_THREADS * VPT;
     const int slices = std::max(1, (a.V / EPV + PER - 1) / PER);
-    if (slices == 1) {
-        for (int row0 = 0; row0 < B; row0 += LP_ROWS) {
-            hipLaunchKernelGGL((logprob_kernel<HALF, VPT>), dim3(std::min(B - row0, LP_ROWS), 1), dim3(LP_THREADS), 0, st, a, row0,
-                               nullptr, nullptr, 0);
-            MVLA_HIP_CHECK(hipGetLastError());
-            if (B - row0 <= LP_ROWS) break;
-        }
-        return MVLA_OK;
-    }
     const int pitch = std::max(a.top, 1);
-    const size_t per_row = (size_t)slices * (sizeof(LpStats) + 8 * (size_t)pitch);
-    const int rows = (int)std::min<size_t>(std::min<size_t>((size_t)B, LP_ROWS), (scratch_bytes - 256) / per_row);
-    LpStats* parts = reinterpret_cast<LpStats*>(scratch);
-    uint64_t* keys = reinterpret_cast<uint64_t*>(scratch + align_up((size_t)rows * slices * sizeof(LpStats), 256));
-    for (int row0 = 0; row0 < B; row0 += rows) {     // (more rows than the scratch holds: in turns)
-        const int n = std::min(rows, B - row0);
-        hipLaunchKernelGGL((logprob_kernel<HALF, VPT>), dim3(n, slices), dim3(LP_THREADS), 0, st, a, row0, parts, keys, pitch);
-        MVLA_HIP_CHECK(hipGetLastError());
-        hipLaunchKernelGGL((logprob_join_kernel<HALF>), dim3(n), dim3(LP_THREADS), 0, st, a, row0, slices, parts, keys, pitch);
-        MVLA_HIP_CHECK(hipGetLastError());
-        if (B - row0 <= rows) break;
+    const size_t per_row = (size_t)slices * (16 + 8 * (size_t)pitch);
+    // (rows in turns: of a launch, and what scratch and counters hold)
+    const int rows = slices == 1 ? LP_ROWS : (int)std::min<size_t>((size_t)n_counters, (scratch_bytes - 256) / per_row);
+    LpParts parts = {nullptr, nullptr, counters, pitch};
+    if (slices > 1) {
+        parts.stats = reinterpret_cast<uint32_t*>(scratch);
+        parts.keys = reinterpret_cast<uint64_t*>(scratch + align_up((size_t)rows * slices * 16, 256));
     }
-    return MVLA_OK;
+    for (int row0 = 0;; row0 += rows) {
+        const int n = std::min(rows, B - row0);
+        hipLaunchKernelGGL((logprob_kernel<HALF, VPT>), dim3(n, slices), dim3(LP_THREADS), 0, st, a, row0, parts);
+        if (VPT == 16 && slices > 1) hipLaunchKernelGGL((logprob_join_kernel<HALF>), dim3(n), dim3(LP_THREADS), 0, st, a, row0, slices, parts);
+        MVLA_HIP_CHECK(hipGetLastError());
+        if (B - row0 <= rows) return MVLA_OK;
+    }
 }
 
 int launch_logprobs(const void* logits, bool half, int64_t row_stride, int B, int V, const float* temperature,
                     const int32_t* tokens, int n_tokens, float* logprob, float* entropy, int top, int32_t* top_token,
-                    float* top_logprob, char* scratch, size_t scratch_bytes, hipStream_t st) {
+                    float* top_logprob, char* scratch, size_t scratch_bytes, uint32_t* counters, int n_counters, hipStream_t st) {
     const LpArgs a = {logits, row_stride, V, n_tokens, top, temperature, tokens, logprob, entropy, top_token, top_logprob};
     // As few slices as leave a workgroup for every compute unit.
     const int64_t want = device_cu_count(), vectors = V / (half ? 8 : 4);
@@ -453,10 +495,10 @@ int launch_logprobs(const void* logits, bool half, int64_t row_stride, int B, in
     const int64_t most = (int64_t)LP_THREADS * LP_THREADS;      // (vectors that a slice for each of the joining threads takes)
     const int vpt = fills(16) || vectors > 4 * most ? 16 : fills(4) || vectors > most ? 4 : 1;
     if (half)
-        return vpt == 16 ? run_logprobs<true, 16>(a, B, scratch, scratch_bytes, st)
-               : vpt == 4 ? run_logprobs<true, 4>(a, B, scratch, scratch_bytes, st) : run_logprobs<true, 1>(a, B, scratch, scratch_bytes, st);
-    return vpt == 16 ? run_logprobs<false, 16>(a, B, scratch, scratch_bytes, st)
-           : vpt == 4 ? run_logprobs<false, 4>(a, B, scratch, scratch_bytes, st) : run_logprobs<false, 1>(a, B, scratch, scratch_bytes, st);
+        return vpt == 16 ? run_logprobs<true, 16>(a, B, scratch, scratch_bytes, counters, n_counters, st)
+               : vpt == 4 ? run_logprobs<true, 4>(a, B, scratch, scratch_bytes, counters, n_counters, st) : run_logprobs<true, 1>(a, B, scratch, scratch_bytes, counters, n_counters, st);
+    return vpt == 16 ? run_logprobs<false, 16>(a, B, scratch, scratch_bytes, counters, n_counters, st)
+           : vpt == 4 ? run_logprobs<false, 4>(a, B, scratch, scratch_bytes, counters, n_counters, st) : run_logprobs<false, 1>(a, B, scratch, scratch_bytes, counters, n_counters, st);
 }
 
 }  // namespace mvla

@@ -99,14 +99,6 @@ __device__ __forceinline__ void few_rows(const PagesView& cache, const PagesAtte
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 15, g = lane >> 4;
-    const PageSpan span = page_span(a.start, a.length, b, a.n, min(cache.pitch << cache.log_page, a.max_len));
-    const int rows = min(span.count, a.max_q) * group;
-    if (rows <= 0 || rows > FEW_ROWS) return;
-    const int n_steps = (page_seen(span, (rows - 1) / group) + FEW_STEP - 1) / FEW_STEP;
-    const int used = max((n_steps + chunk - 1) / chunk, 1);
-    if (part >= used) return;
-    const int step0 = part * chunk, step1 = min(step0 + chunk, n_steps);
-
     // ---- where a step's rows are
     auto find = [&](int step) __attribute__((always_inline)) {
         StepRows s;
@@ -163,13 +155,21 @@ __device__ __forceinline__ void few_rows(const PagesView& cache, const PagesAtte
             }
         }
     };
+    // A sequence's first step is asked for before its rows and length are known: what it does not have is not looked at.
     Raw x, ahead;
     StepRows far;
-    const int first = step0 + wave;
-    if (first < step1) {
-        load(ahead, find(first));
-        if (first + WAVES < step1) far = find(first + WAVES);
-    }
+    const int first = part * chunk + wave;
+    if (part == 0) load(ahead, find(first));
+    const PageSpan span = page_span(a.start, a.length, b, a.n, min(cache.pitch << cache.log_page, a.max_len));
+    const int rows = min(span.count, a.max_q) * group;
+    if (rows <= 0 || rows > FEW_ROWS) return;
+    const int n_steps = (page_seen(span, (rows - 1) / group) + FEW_STEP - 1) / FEW_STEP;
+    const int used = max((n_steps + chunk - 1) / chunk, 1);
+    if (part >= used) return;
+    const int step0 = part * chunk, step1 = min(step0 + chunk, n_steps);
+
+    if (part && first < step1) load(ahead, find(first));
+    if (first + WAVES < step1) far = find(first + WAVES);
 
     // ---- this lane's column: row c (columns beyond the rows hold zeros and see everything; nobody reads them)
     const int qi = c / group;
