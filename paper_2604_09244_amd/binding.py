@@ -304,6 +304,19 @@ def _packed_rows(t: torch.Tensor) -> Rows:
     return Rows(t.data_ptr(), 0, *t.stride())
 
 
+class RotaryTable(tuple):
+    """(cos, sin) of ``Context.rotate``, fp32 [rope_len, rotated/2], looked at once: a pair of such
+    tensors serves as well, but is looked at in every call."""
+
+    def __new__(cls, cos: torch.Tensor, sin: torch.Tensor):
+        self = super().__new__(cls, (cos, sin))
+        self.rope_len, half = _dev(cos, torch.float32).shape
+        assert _dev(sin, torch.float32).shape == cos.shape and sin.device == cos.device, (sin.shape, sin.device)
+        self.rotated, self.index = 2 * half, cos.get_device()
+        self._cos, self._sin = cos.data_ptr(), sin.data_ptr()
+        return self
+
+
 class PagedCache:
     """A layer's key/value cache in pages (mvla_pages) and the tensors that it lies in: k, v
     [n_pages, H_kv, page, dh] as bf16, or as uint8 codes with the blocks' powers k_scale, v_scale
@@ -796,21 +809,22 @@ class Context:
 
     def rotary_table(self, rotated: int, rope_len: int, base: float = 10000.0, factor: float = 1.0,
                      low_turns: float = 1.0, high_turns: float = 4.0, trained: float = 8192.0, gain: float = 1.0):
-        """(cos, sin) fp32 [rope_len, rotated/2] for ``rotate``.  ``factor`` > 1 lengthens the waves that
+        """A ``RotaryTable`` (cos, sin) for ``rotate``.  ``factor`` > 1 lengthens the waves that
         turn less than high_turns times within the trained positions, up to ``factor`` times those that
         turn low_turns times or less; ``gain`` multiplies both tables."""
         c, s = (self._new((rope_len, rotated // 2), torch.float32) for _ in range(2))
         how = Rotation(base, factor, low_turns, high_turns, trained, gain, rotated)
         _check(load().mvla_rotation_table(self._h, C.byref(how), rope_len, c.data_ptr(), s.data_ptr()),
                "mvla_rotation_table")
-        return c, s
+        return RotaryTable(c, s)
 
     def rotate(self, q: torch.Tensor, k: Optional[torch.Tensor], pos: torch.Tensor, rope, interleaved: bool = False,
                inverse: bool = False, out=None):
         """Queries q [..., H, dh] and keys k [..., H_kv, dh] (bf16, any strides; [B, n, ...] or packed
         [n, ...]; k may be None) turned by their positions pos (int32 [B, n] or [n]) with the tables
         ``rope`` = (cos, sin).  ``out``: (q_out, k_out), also the inputs themselves.  Returns (q_out, k_out)."""
-        cos, sin = rope
+        if type(rope) is not RotaryTable:
+            rope = RotaryTable(*rope)
         if q.dim() == 3:
             rows, B, (n, H, dh) = _packed_rows, 1, q.shape
             tokens, H_kv = (n,), 0
@@ -818,9 +832,7 @@ class Context:
             rows, (B, n, H, dh) = _rows, q.shape
             tokens, H_kv = (B, n), 0
         on = self._index
-        assert q.get_device() == on and self._is(pos, torch.int32, tokens), (q.device, pos.shape, pos.dtype)
-        rope_len, half = cos.shape
-        assert self._is(cos, torch.float32, cos.shape) and self._is(sin, torch.float32, cos.shape)
+        assert q.get_device() == on == rope.index and self._is(pos, torch.int32, tokens), (q.device, pos.shape, pos.dtype)
         if out is None:
             q_out, k_out = self._like(q), None if k is None else self._like(k)
         else:
@@ -832,8 +844,8 @@ class Context:
             assert k.shape == (*tokens, H_kv, dh) == k_out.shape and k.get_device() == k_out.get_device() == on, k.shape
             k_ref, k_out_ref = C.byref(rows(k)), C.byref(rows(k_out))
         _check(load().mvla_rotate(self._h, C.byref(rows(q)), H, C.byref(rows(q_out)), k_ref, H_kv, k_out_ref,
-                                  pos.data_ptr(), B, n, dh, 2 * half, interleaved, inverse, cos.data_ptr(),
-                                  sin.data_ptr(), rope_len), "mvla_rotate")
+                                  pos.data_ptr(), B, n, dh, rope.rotated, interleaved, inverse, rope._cos,
+                                  rope._sin, rope.rope_len), "mvla_rotate")
         return q_out, k_out
 
     def pages_append(self, cache: PagedCache, batch: PageBatch, k: torch.Tensor, v: torch.Tensor):

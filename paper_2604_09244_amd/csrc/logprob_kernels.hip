@@ -440,7 +440,7 @@ __global__ __launch_bounds__(LP_THREADS, VPT == 16 ? 3 : 4) void logprob_kernel(
         lp_put(&parts.stats[(first + slice) * 4 + tid], w);
     }
     if (tid < r.n) lp_put(&parts.keys[(first + slice) * parts.pitch + tid], best[tid]);
-    if (VPT == 16) return;                     // (joined by a launch)
+    if (VPT >= 8) return;                      // (joined by a launch)
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     if (tid == 0) {
@@ -479,7 +479,7 @@ static int run_logprobs(const LpArgs& a, int B, char* scratch, size_t scratch_by
     for (int row0 = 0;; row0 += rows) {
         const int n = std::min(rows, B - row0);
         hipLaunchKernelGGL((logprob_kernel<HALF, VPT>), dim3(n, slices), dim3(LP_THREADS), 0, st, a, row0, parts);
-        if (VPT == 16 && slices > 1) hipLaunchKernelGGL((logprob_join_kernel<HALF>), dim3(n), dim3(LP_THREADS), 0, st, a, row0, slices, parts);
+        if (VPT >= 8 && slices > 1) hipLaunchKernelGGL((logprob_join_kernel<HALF>), dim3(n), dim3(LP_THREADS), 0, st, a, row0, slices, parts);
         MVLA_HIP_CHECK(hipGetLastError());
         if (B - row0 <= rows) return MVLA_OK;
     }
@@ -489,16 +489,24 @@ int launch_logprobs(const void* logits, bool half, int64_t row_stride, int B, in
                     const int32_t* tokens, int n_tokens, float* logprob, float* entropy, int top, int32_t* top_token,
                     float* top_logprob, char* scratch, size_t scratch_bytes, uint32_t* counters, int n_counters, hipStream_t st) {
     const LpArgs a = {logits, row_stride, V, n_tokens, top, temperature, tokens, logprob, entropy, top_token, top_logprob};
-    // As few slices as leave a workgroup for every compute unit.
+    // A row that 2048 vectors hold is one workgroup's, of as few as hold it: empty places cost what full ones do, and their
+    // registers room (us; 4096 rows of 2048 bf16: 17.9 with 1 vector a thread, 57.9 with 16; of 8192: 26.8 with 4, 58.9 with 16;
+    // of 16384: 37.8 with 8, 59.9 with 16).  Longer rows: as few slices as leave a workgroup for every compute unit (4096 rows of
+    // 50000: 123 with 16, 138 with 4; 64 rows of 50000: 13.4 with 4, 16.0 with 16).
     const int64_t want = device_cu_count(), vectors = V / (half ? 8 : 4);
     auto fills = [&](int vpt) { return B * ((vectors + LP_THREADS * vpt - 1) / (LP_THREADS * vpt)) >= want; };
     const int64_t most = (int64_t)LP_THREADS * LP_THREADS;      // (vectors that a slice for each of the joining threads takes)
-    const int vpt = fills(16) || vectors > 4 * most ? 16 : fills(4) || vectors > most ? 4 : 1;
-    if (half)
-        return vpt == 16 ? run_logprobs<true, 16>(a, B, scratch, scratch_bytes, counters, n_counters, st)
-               : vpt == 4 ? run_logprobs<true, 4>(a, B, scratch, scratch_bytes, counters, n_counters, st) : run_logprobs<true, 1>(a, B, scratch, scratch_bytes, counters, n_counters, st);
-    return vpt == 16 ? run_logprobs<false, 16>(a, B, scratch, scratch_bytes, counters, n_counters, st)
-           : vpt == 4 ? run_logprobs<false, 4>(a, B, scratch, scratch_bytes, counters, n_counters, st) : run_logprobs<false, 1>(a, B, scratch, scratch_bytes, counters, n_counters, st);
+    int vpt;
+    if (vectors <= 8 * LP_THREADS) vpt = vectors <= LP_THREADS ? 1 : vectors <= 4 * LP_THREADS ? 4 : 8;
+    else vpt = fills(16) || vectors > 4 * most ? 16 : fills(4) || vectors > most ? 4 : 1;
+    auto run = [&](auto of_16_bits) {
+        constexpr bool HALF = decltype(of_16_bits)::value;
+        return vpt == 16  ? run_logprobs<HALF, 16>(a, B, scratch, scratch_bytes, counters, n_counters, st)
+               : vpt == 8 ? run_logprobs<HALF, 8>(a, B, scratch, scratch_bytes, counters, n_counters, st)
+               : vpt == 4 ? run_logprobs<HALF, 4>(a, B, scratch, scratch_bytes, counters, n_counters, st)
+                          : run_logprobs<HALF, 1>(a, B, scratch, scratch_bytes, counters, n_counters, st);
+    };
+    return half ? run(std::true_type{}) : run(std::false_type{});
 }
 
 }  // namespace mvla

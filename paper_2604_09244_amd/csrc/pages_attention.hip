@@ -1000,12 +1000,21 @@ struct FewPlan {
 FewPlan few_plan(int64_t heads, int64_t rows, int max_len, int64_t room, bool mixed) {
     FewPlan p;
     const int64_t cus = device_cu_count(), steps = ((int64_t)max_len + FEW_STEP - 1) / FEW_STEP;
-    p.waves = heads <= cus && !mixed ? 8 : 4;
-    // enough workgroups to fill the chip, and where they would still be long (eight steps a wave) so many that sequences of
-    // different lengths even out
-    const int64_t fill = std::min((4 * cus + heads - 1) / heads, (steps + p.waves - 1) / p.waves);
-    const int64_t even = std::min(steps / (8 * p.waves), (16 * cus + heads - 1) / heads);
-    int64_t parts = std::max(fill, even);
+    // Three steps a wave are quicker than a join: a short sequence is one workgroup's, of eight waves where there are few of
+    // them (us; 8 heads x 600 slots: 10.5, and 12.9 in four parts; 512 x 600: 21.9, and 28.2 in two).
+    p.waves = !mixed && heads <= cus && steps <= 3 * 8 ? 8 : 4;
+    int64_t parts = 1;
+    if (steps > 3 * p.waves) {
+        // a workgroup for every compute unit, of two steps a wave at least (8 heads x 4096 slots: 15.8 in 16 parts, 18.7 in 32;
+        // 8 x 32768: 36.9 in 32, 43.3 in 64; 128 x 2624: 34.3 in 2, 36.3 in 8); beside many rows, whose workgroups are long, four
+        // (512 tokens beside 31 sequences of up to 2624 slots, 256 heads: 75.5 in 4 parts, 96.4 in one)
+        const int64_t fill = mixed ? std::min((4 * cus + heads - 1) / heads, (steps + p.waves - 1) / p.waves)
+                                   : std::min((cus + heads - 1) / heads, (steps + 2 * p.waves - 1) / (2 * p.waves));
+        // and where they would still be long so many that sequences of different lengths even out (512 heads of up to 16384
+        // slots: 283 in 8 parts, 354 in one; of up to 2048: 43.1 in one, 47.5 in two)
+        const int64_t even = std::min(steps / ((mixed ? 8 : 16) * p.waves), (16 * cus + heads - 1) / heads);
+        parts = std::max(fill, even);
+    }
     parts = std::max<int64_t>(1, std::min<int64_t>({parts, (int64_t)MAX_PARTS, room / (heads * rows)}));
     p.chunk = (int)((steps + parts - 1) / parts);
     p.parts = (int)((steps + p.chunk - 1) / p.chunk);

@@ -32,7 +32,7 @@ int launch_rotation_table(const mvla_rotation& how, int rope_len, float* c, floa
 
 // ---- rows by 16 bytes --------------------------------------------------------------------------------------------
 // A lane takes 16 values of a head: pairs i .. i + 7 of either half, or 16 neighbours; behind the rotated values it
-// copies 16.  Its cosines and sines serve HEADS heads.
+// copies 16.
 constexpr int ROTATE_THREADS = 256;
 
 struct Rotor {
@@ -45,71 +45,59 @@ __device__ __forceinline__ float value_of(const uint4& x, int i) {
     return __uint_as_float(i & 1 ? w & 0xffff0000u : w << 16);
 }
 
-template <bool SIDES, int HEADS>
-__global__ __launch_bounds__(ROTATE_THREADS) void rotate_wide_kernel(RotateArgs a, int units, int groups0, int tokens) {
-    // unit u of a token: 16 values of HEADS heads of the queries (first groups0 groups) or of the keys
+template <bool SIDES>
+__global__ __launch_bounds__(ROTATE_THREADS) void rotate_wide_kernel(RotateArgs a, int units, int tokens) {
+    // unit u of a token: 16 values of a head of the queries (first heads[0] heads) or of the keys
     const int chunks = (a.dh + 15) / 16;
     const int per = units < ROTATE_THREADS ? ROTATE_THREADS / units : 1;     // tokens a workgroup
     const int mine = threadIdx.x / units;
     const int t = (int)(blockIdx.x * per) + (per > 1 ? mine : 0);
     const int u = per > 1 ? (int)threadIdx.x - mine * units : (int)(blockIdx.y * ROTATE_THREADS + threadIdx.x);
     if ((per > 1 && mine >= per) || t >= tokens || u >= units) return;
-    const int ch = u % chunks, group = u / chunks;
-    const int which = group >= groups0, h0 = (group - (which ? groups0 : 0)) * HEADS;
+    int h = u / chunks;
+    const int ch = u - h * chunks, which = h >= a.heads[0];
+    if (which) h -= a.heads[0];
     const int b = t / a.n, i = t - b * a.n;
     const CacheRows &in = a.in[which], &out = a.out[which];
-    const bf16_t* src = in.p + b * in.sample + i * in.token + h0 * in.head;
-    bf16_t* dst = const_cast<bf16_t*>(out.p) + b * out.sample + i * out.token + h0 * out.head;
-    const int heads = min(HEADS, a.heads[which] - h0);
+    const bf16_t* src = in.p + b * in.sample + i * in.token + h * in.head;
+    bf16_t* dst = const_cast<bf16_t*>(out.p) + b * out.sample + i * out.token + h * out.head;
     const int half = a.rotated / 2, turned = a.rotated / 16;
     // (first and second 8 values of this lane)
     const bool turns = ch < turned;
     const int d0 = turns && !SIDES ? ch * 8 : ch * 16, d1 = turns && !SIDES ? half + ch * 8 : ch * 16 + 8;
     const bool two = turns || d1 < a.dh;
-    uint4 x[HEADS], y[HEADS];
-#pragma unroll
-    for (int j = 0; j < HEADS; ++j)
-        if (j < heads) {
-            x[j] = *reinterpret_cast<const uint4*>(src + j * in.head + d0);
-            if (two) y[j] = *reinterpret_cast<const uint4*>(src + j * in.head + d1);
-        }
+    const uint4 x = *reinterpret_cast<const uint4*>(src + d0);
+    uint4 y;
+    if (two) y = *reinterpret_cast<const uint4*>(src + d1);
     if (!turns) {
-#pragma unroll
-        for (int j = 0; j < HEADS; ++j)
-            if (j < heads) {
-                *reinterpret_cast<uint4*>(dst + j * out.head + d0) = x[j];
-                if (two) *reinterpret_cast<uint4*>(dst + j * out.head + d1) = y[j];
-            }
+        *reinterpret_cast<uint4*>(dst + d0) = x;
+        if (two) *reinterpret_cast<uint4*>(dst + d1) = y;
         return;
     }
     const size_t at = (size_t)min(max(a.pos[t], 0), a.rope_len - 1) * half + ch * 8;
     float c[8], s[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) c[e] = a.rc[at + e], s[e] = a.inverse ? -a.rs[at + e] : a.rs[at + e];
+    float p[8], q[8];
+    if constexpr (SIDES) {
 #pragma unroll
-    for (int j = 0; j < HEADS; ++j)
-        if (j < heads) {
-            float p[8], q[8];
-            if constexpr (SIDES) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float x1 = value_of(x[j], 2 * e), x2 = value_of(x[j], 2 * e + 1);
-                    const float y1 = value_of(y[j], 2 * e), y2 = value_of(y[j], 2 * e + 1);
-                    p[2 * e] = x1 * c[e] - x2 * s[e], p[2 * e + 1] = x2 * c[e] + x1 * s[e];
-                    q[2 * e] = y1 * c[4 + e] - y2 * s[4 + e], q[2 * e + 1] = y2 * c[4 + e] + y1 * s[4 + e];
-                }
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float x1 = value_of(x[j], e), x2 = value_of(y[j], e);
-                    p[e] = x1 * c[e] - x2 * s[e], q[e] = x2 * c[e] + x1 * s[e];
-                }
-            }
-            *reinterpret_cast<uint4*>(dst + j * out.head + d0) = make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]),
-                                                                            pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7]));
-            *reinterpret_cast<uint4*>(dst + j * out.head + d1) = make_uint4(pack_bf16x2(q[0], q[1]), pack_bf16x2(q[2], q[3]),
-                                                                            pack_bf16x2(q[4], q[5]), pack_bf16x2(q[6], q[7]));
+        for (int e = 0; e < 4; ++e) {
+            const float x1 = value_of(x, 2 * e), x2 = value_of(x, 2 * e + 1);
+            const float y1 = value_of(y, 2 * e), y2 = value_of(y, 2 * e + 1);
+            p[2 * e] = x1 * c[e] - x2 * s[e], p[2 * e + 1] = x2 * c[e] + x1 * s[e];
+            q[2 * e] = y1 * c[4 + e] - y2 * s[4 + e], q[2 * e + 1] = y2 * c[4 + e] + y1 * s[4 + e];
         }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float x1 = value_of(x, e), x2 = value_of(y, e);
+            p[e] = x1 * c[e] - x2 * s[e], q[e] = x2 * c[e] + x1 * s[e];
+        }
+    }
+    *reinterpret_cast<uint4*>(dst + d0) = make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]),
+                                                     pack_bf16x2(p[6], p[7]));
+    *reinterpret_cast<uint4*>(dst + d1) = make_uint4(pack_bf16x2(q[0], q[1]), pack_bf16x2(q[2], q[3]), pack_bf16x2(q[4], q[5]),
+                                                     pack_bf16x2(q[6], q[7]));
 }
 
 // ---- rows of any strides and sizes: a lane a pair, or a value behind the pairs ---------------------------------------
@@ -140,14 +128,13 @@ __global__ __launch_bounds__(ROTATE_THREADS) void rotate_any_kernel(RotateArgs a
     dst[d2 * out.channel] = f32_to_bf16(x2 * c + x1 * s);
 }
 
-template <bool SIDES, int HEADS>
+template <bool SIDES>
 static int launch_wide(const RotateArgs& a, hipStream_t st) {
-    const int tokens = a.B * a.n, chunks = (a.dh + 15) / 16;
-    const int g0 = (a.heads[0] + HEADS - 1) / HEADS, g1 = (a.heads[1] + HEADS - 1) / HEADS;
-    const int units = (g0 + g1) * chunks, per = units < ROTATE_THREADS ? ROTATE_THREADS / units : 1;
+    const int tokens = a.B * a.n, units = (a.heads[0] + a.heads[1]) * ((a.dh + 15) / 16);
+    const int per = units < ROTATE_THREADS ? ROTATE_THREADS / units : 1;
     const unsigned y = per > 1 ? 1u : (unsigned)((units + ROTATE_THREADS - 1) / ROTATE_THREADS);
-    hipLaunchKernelGGL((rotate_wide_kernel<SIDES, HEADS>), dim3((unsigned)((tokens + per - 1) / per), y), dim3(ROTATE_THREADS), 0, st,
-                       a, units, g0, tokens);
+    hipLaunchKernelGGL((rotate_wide_kernel<SIDES>), dim3((unsigned)((tokens + per - 1) / per), y), dim3(ROTATE_THREADS), 0, st, a,
+                       units, tokens);
     MVLA_HIP_CHECK(hipGetLastError());
     return MVLA_OK;
 }
@@ -165,7 +152,7 @@ int launch_rotate(const RotateArgs& a, hipStream_t st) {
         MVLA_HIP_CHECK(hipGetLastError());
         return MVLA_OK;
     }
-    return a.interleaved ? launch_wide<true, 1>(a, st) : launch_wide<false, 1>(a, st);
+    return a.interleaved ? launch_wide<true>(a, st) : launch_wide<false>(a, st);
 }
 
 }  // namespace mvla

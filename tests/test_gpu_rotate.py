@@ -139,3 +139,16 @@ def test_empty_calls_and_refusals(ctx):
         ctx.rotate(q, q[:3], pos, rope)
     with pytest.raises(AssertionError):
         ctx.rotate(q, None, pos.long(), rope)
+
+
+def test_a_pair_of_tables_serves_like_a_rotary_table(ctx):
+    g = torch.Generator(device="cuda").manual_seed(9)
+    q = torch.randn(5, 2, 64, generator=g, device="cuda").bfloat16()
+    pos, rope = torch.arange(5, dtype=torch.int32, device="cuda"), ctx.rotary_table(64, 10)
+    cos, sin = rope
+    assert type(rope) is mv.RotaryTable and rope.rope_len == 10 and rope.rotated == 64 and cos is rope[0] and sin is rope[1]
+    want = ctx.rotate(q, None, pos, rope)[0]
+    assert torch.equal(ctx.rotate(q, None, pos, (cos, sin))[0], want)
+    for bad in [(cos.t().contiguous().t(), sin), (cos, sin[:9]), (cos.half(), sin), (cos, sin.cpu())]:
+        with pytest.raises(AssertionError):
+            ctx.rotate(q, None, pos, bad)
