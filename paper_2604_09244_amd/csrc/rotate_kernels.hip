@@ -31,9 +31,14 @@ int launch_rotation_table(const mvla_rotation& how, int rope_len, float* c, floa
 }
 
 // ---- rows by 16 bytes --------------------------------------------------------------------------------------------
-// A lane takes 16 values of a head: pairs i .. i + 7 of either half, or 16 neighbours; behind the rotated values it
-// copies 16.
-constexpr int ROTATE_THREADS = 256;
+// A lane takes two runs of 8 values of a head, the same places of either half of the rotated ones (eight pairs of halves, or
+// four pairs of neighbours each) or of those behind them, so that a wave's accesses are whole stretches; of ROTATE_TURNS tokens, whose
+// loads do not wait for each other.
+// Bound by memory: 2 bytes in and 2 out a value, and the tokens' cosines and sines once.  41984 tokens of 32 + 8 heads of 128
+// (us, all of the head rotated / half of it): 153 / 168, which is 5.6 / 5.1 TB/s; with stores through the caches 162 / 172;
+// one token a lane 173 / 173; four 155 / 165.
+constexpr int ROTATE_THREADS = 256, ROTATE_TURNS = 2;
+
 
 struct Rotor {
     const float *c, *s;   // the row's
@@ -49,55 +54,67 @@ template <bool SIDES>
 __global__ __launch_bounds__(ROTATE_THREADS) void rotate_wide_kernel(RotateArgs a, int units, int tokens) {
     // unit u of a token: 16 values of a head of the queries (first heads[0] heads) or of the keys
     const int chunks = (a.dh + 15) / 16;
-    const int per = units < ROTATE_THREADS ? ROTATE_THREADS / units : 1;     // tokens a workgroup
+    const int per = units < ROTATE_THREADS ? ROTATE_THREADS / units : 1;     // tokens a workgroup and turn
     const int mine = threadIdx.x / units;
-    const int t = (int)(blockIdx.x * per) + (per > 1 ? mine : 0);
+    const int t0 = (int)(blockIdx.x * (per * ROTATE_TURNS)) + (per > 1 ? mine : 0);
     const int u = per > 1 ? (int)threadIdx.x - mine * units : (int)(blockIdx.y * ROTATE_THREADS + threadIdx.x);
-    if ((per > 1 && mine >= per) || t >= tokens || u >= units) return;
+    if ((per > 1 && mine >= per) || t0 >= tokens || u >= units) return;
     int h = u / chunks;
     const int ch = u - h * chunks, which = h >= a.heads[0];
     if (which) h -= a.heads[0];
-    const int b = t / a.n, i = t - b * a.n;
     const CacheRows &in = a.in[which], &out = a.out[which];
-    const bf16_t* src = in.p + b * in.sample + i * in.token + h * in.head;
-    bf16_t* dst = const_cast<bf16_t*>(out.p) + b * out.sample + i * out.token + h * out.head;
     const int half = a.rotated / 2, turned = a.rotated / 16;
     // (first and second 8 values of this lane)
     const bool turns = ch < turned;
-    const int d0 = turns && !SIDES ? ch * 8 : ch * 16, d1 = turns && !SIDES ? half + ch * 8 : ch * 16 + 8;
+    const int d0 = turns ? ch * 8 : a.rotated + (ch - turned) * 8, d1 = d0 + (turns ? half : (chunks - turned) * 8);
     const bool two = turns || d1 < a.dh;
-    const uint4 x = *reinterpret_cast<const uint4*>(src + d0);
-    uint4 y;
-    if (two) y = *reinterpret_cast<const uint4*>(src + d1);
-    if (!turns) {
-        *reinterpret_cast<uint4*>(dst + d0) = x;
-        if (two) *reinterpret_cast<uint4*>(dst + d1) = y;
-        return;
-    }
-    const size_t at = (size_t)min(max(a.pos[t], 0), a.rope_len - 1) * half + ch * 8;
-    float c[8], s[8];
+    const int e0 = SIDES ? ch * 4 : ch * 8, e1 = SIDES ? half / 2 + ch * 4 : e0 + 4;     // their first and second 4 pairs
+    uint4 x[ROTATE_TURNS], y[ROTATE_TURNS];
+    bf16_t* dst[ROTATE_TURNS];
+    const float *rc[ROTATE_TURNS], *rs[ROTATE_TURNS];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) c[e] = a.rc[at + e], s[e] = a.inverse ? -a.rs[at + e] : a.rs[at + e];
-    float p[8], q[8];
-    if constexpr (SIDES) {
+    for (int j = 0; j < ROTATE_TURNS; ++j) {
+        const int t = min(t0 + j * per, tokens - 1), b = t / a.n, i = t - b * a.n;
+        const bf16_t* src = in.p + b * in.sample + i * in.token + h * in.head;
+        dst[j] = const_cast<bf16_t*>(out.p) + b * out.sample + i * out.token + h * out.head;
+        const size_t at = (size_t)min(max(a.pos[t], 0), a.rope_len - 1) * half;
+        rc[j] = a.rc + at, rs[j] = a.rs + at;
+        x[j] = *reinterpret_cast<const uint4*>(src + d0);
+        if (two) y[j] = *reinterpret_cast<const uint4*>(src + d1);
+    }
+#pragma unroll
+    for (int j = 0; j < ROTATE_TURNS; ++j) {
+        if (t0 + j * per >= tokens) return;
+        if (!turns) {
+            store_past_caches(dst[j] + d0, x[j]);
+            if (two) store_past_caches(dst[j] + d1, y[j]);
+            continue;
+        }
+        float c[8], s[8];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const float x1 = value_of(x, 2 * e), x2 = value_of(x, 2 * e + 1);
-            const float y1 = value_of(y, 2 * e), y2 = value_of(y, 2 * e + 1);
-            p[2 * e] = x1 * c[e] - x2 * s[e], p[2 * e + 1] = x2 * c[e] + x1 * s[e];
-            q[2 * e] = y1 * c[4 + e] - y2 * s[4 + e], q[2 * e + 1] = y2 * c[4 + e] + y1 * s[4 + e];
+            c[e] = rc[j][e0 + e], c[4 + e] = rc[j][e1 + e];
+            s[e] = a.inverse ? -rs[j][e0 + e] : rs[j][e0 + e], s[4 + e] = a.inverse ? -rs[j][e1 + e] : rs[j][e1 + e];
         }
-    } else {
+        float p[8], q[8];
+        if constexpr (SIDES) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float x1 = value_of(x, e), x2 = value_of(y, e);
-            p[e] = x1 * c[e] - x2 * s[e], q[e] = x2 * c[e] + x1 * s[e];
+            for (int e = 0; e < 4; ++e) {
+                const float x1 = value_of(x[j], 2 * e), x2 = value_of(x[j], 2 * e + 1);
+                const float y1 = value_of(y[j], 2 * e), y2 = value_of(y[j], 2 * e + 1);
+                p[2 * e] = x1 * c[e] - x2 * s[e], p[2 * e + 1] = x2 * c[e] + x1 * s[e];
+                q[2 * e] = y1 * c[4 + e] - y2 * s[4 + e], q[2 * e + 1] = y2 * c[4 + e] + y1 * s[4 + e];
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float x1 = value_of(x[j], e), x2 = value_of(y[j], e);
+                p[e] = x1 * c[e] - x2 * s[e], q[e] = x2 * c[e] + x1 * s[e];
+            }
         }
+        store_past_caches(dst[j] + d0, make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7])));
+        store_past_caches(dst[j] + d1, make_uint4(pack_bf16x2(q[0], q[1]), pack_bf16x2(q[2], q[3]), pack_bf16x2(q[4], q[5]), pack_bf16x2(q[6], q[7])));
     }
-    *reinterpret_cast<uint4*>(dst + d0) = make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]),
-                                                     pack_bf16x2(p[6], p[7]));
-    *reinterpret_cast<uint4*>(dst + d1) = make_uint4(pack_bf16x2(q[0], q[1]), pack_bf16x2(q[2], q[3]), pack_bf16x2(q[4], q[5]),
-                                                     pack_bf16x2(q[6], q[7]));
 }
 
 // ---- rows of any strides and sizes: a lane a pair, or a value behind the pairs ---------------------------------------
@@ -133,8 +150,8 @@ static int launch_wide(const RotateArgs& a, hipStream_t st) {
     const int tokens = a.B * a.n, units = (a.heads[0] + a.heads[1]) * ((a.dh + 15) / 16);
     const int per = units < ROTATE_THREADS ? ROTATE_THREADS / units : 1;
     const unsigned y = per > 1 ? 1u : (unsigned)((units + ROTATE_THREADS - 1) / ROTATE_THREADS);
-    hipLaunchKernelGGL((rotate_wide_kernel<SIDES>), dim3((unsigned)((tokens + per - 1) / per), y), dim3(ROTATE_THREADS), 0, st, a,
-                       units, tokens);
+    hipLaunchKernelGGL((rotate_wide_kernel<SIDES>), dim3((unsigned)((tokens + per * ROTATE_TURNS - 1) / (per * ROTATE_TURNS)), y),
+                       dim3(ROTATE_THREADS), 0, st, a, units, tokens);
     MVLA_HIP_CHECK(hipGetLastError());
     return MVLA_OK;
 }
