@@ -45,6 +45,12 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
 __device__ __forceinline__ uint16_t f32_to_bf16(float f) { return (uint16_t)pack_bf16x2(f, 0.f); }
 
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+// bytes that nobody reads again: of whole lines that a wave reads at once (half lines would be fetched twice)
+template <class T>
+__device__ __forceinline__ T load_past_caches(const void* from) {
+    return __builtin_nontemporal_load(static_cast<const T*>(from));
+}
 // 16 bytes that are not worth a place in the caches: of whole stretches that a wave writes once
 __device__ __forceinline__ void store_past_caches(void* to, uint4 v) {
     __builtin_nontemporal_store(u32x4_t{v.x, v.y, v.z, v.w}, static_cast<u32x4_t*>(to));
