@@ -646,8 +646,8 @@ int mvla_rotation_table(mvla_ctx* ctx, const mvla_rotation* how, int rope_len, f
  * q, q_out: bf16 [B, n, H, dh], k, k_out: bf16 [B, n, H_kv, dh] by their strides; an output
  * is either its input (same address and strides) or shares no memory with any input.
  * k, k_out NULL: queries alone.  pos: device int32 [B, n], clamped to [0, rope_len).
- * dh: 2 .. 256; rotated <= dh.  channel == 1 with 16-byte aligned rows, dh, and rotated (halves:
- * rotated/2) multiples of 8, is the fast form, any other is taken as well. */
+ * dh: 2 .. 256; rotated <= dh.  channel == 1 with 16-byte aligned rows and dh a multiple of 8
+ * is the fast form, any other is taken as well. */
 int mvla_rotate(mvla_ctx* ctx, const mvla_rows* q, int H, const mvla_rows* q_out, const mvla_rows* k,
                 int H_kv, const mvla_rows* k_out, const int32_t* pos, int B, int n, int dh, int rotated,
                 int interleaved, int inverse, const float* rope_cos, const float* rope_sin, int rope_len);

@@ -363,6 +363,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void few_pages_kern
 // In turn: the keys of the next tile are multiplied while this tile's logits become probabilities, this tile's values are
 // multiplied while the next tile's maxima are found.  So the matrix cores have work that waits for no vector
 // operation; two keys' and two values' tiles are in LDS, the next ones on their way.
+// Bound by the matrix products and the exponentials beside them.  2048 tokens behind 14336, 32 heads of 128: 537 us, 0.96 PFLOP/s.
 constexpr int MANY_KT = 64, MANY_WAVE_ROWS = 32;
 constexpr float SLACK = 8.f;
 
@@ -655,7 +656,8 @@ __device__ __forceinline__ void many_rows(const PagesView& cache, const PagesAtt
         m = max_of(s);
     };
     // The sums' reference stays until a logit passes it by SLACK in powers of two: exponentials are at most 2^SLACK then,
-    // and the sums are hardly ever scaled again after the first tiles.
+    // and the sums are hardly ever scaled again after the first tiles.  (With SLACK 0 a pass of 595 us took 621; outputs
+    // are 0.0023 of their RMS off instead of 0.0020, 0.0017 of which is their own rounding.)
     auto rescale = [&](float tile_m) __attribute__((always_inline)) {
         const float new_m = (tile_m - run_m) * scale_log2e > SLACK ? tile_m : run_m;
         if (__any(new_m != run_m)) {
@@ -904,6 +906,8 @@ __global__ __launch_bounds__(MANY_WAVES * 64, 2) void mixed_pages_kernel(MixedAr
 // ---- the parts of a row --------------------------------------------------------------------------------------------
 // A wave takes a token's rows of JOIN_HEADS heads, whose loads do not wait for each other; lane p knows part p's maximum and
 // sum, half a wave (of 128 dims) adds every second part.
+// Bound by memory where there is much (543 tokens of 32 heads in up to four parts: 11.7 us), by its launch where
+// there is little (64 rows of 32 heads in up to 8 parts: 8.5).
 constexpr int JOIN_WAVES = 4, JOIN_HEADS = 4, MAX_PARTS = 64;
 
 template <int DH>

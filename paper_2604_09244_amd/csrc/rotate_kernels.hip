@@ -1,7 +1,8 @@
 // Rotation of queries and keys by position, and its tables.
 //
 // A pair (x1, x2) turns by the angle pos * f_i: y1 = x1 c - x2 s, y2 = x2 c + x1 s.  Cosines and sines come from a table,
-// whose angles are formed in 64 bits: far positions have angles of thousands of turns.
+// whose angles are formed in 64 bits: far positions have angles of thousands of turns.  (The table of 131072
+// positions of 32 pairs takes 60 us, once: bound by the 64-bit sines.)
 #include "common.h"
 #include "mfma.h"
 
@@ -30,27 +31,18 @@ int launch_rotation_table(const mvla_rotation& how, int rope_len, float* c, floa
     return MVLA_OK;
 }
 
-// ---- rows by 16 bytes --------------------------------------------------------------------------------------------
-// A lane takes two runs of 8 values of a head, the same places of either half of the rotated ones (eight pairs of halves, or
-// four pairs of neighbours each) or of those behind them, so that a wave's accesses are whole stretches; of ROTATE_TURNS tokens, whose
-// loads do not wait for each other.
-// Bound by memory: 2 bytes in and 2 out a value, and the tokens' cosines and sines once.  41984 tokens of 32 + 8 heads of 128
-// (us, all of the head rotated / half of it): 153 / 168, which is 5.6 / 5.1 TB/s; with stores through the caches 162 / 172;
-// one token a lane 173 / 173; four 155 / 165.
+// ---- halves of 16 bytes ------------------------------------------------------------------------------------------
+// A lane takes two runs of 8 values of a head, the same places of either half of the rotated ones or of those behind them, so that
+// a wave's accesses are whole stretches; of ROTATE_TURNS tokens, whose loads do not wait for each other.
+// Bound by memory: 2 bytes in and 2 out a value, and the tokens' cosines and sines once.  41984 tokens of 32 + 8 heads of 128,
+// all rotated: 153 us, 5.6 TB/s; with stores through the caches 162, one token a lane 173, four 155; in the form below 184.
 constexpr int ROTATE_THREADS = 256, ROTATE_TURNS = 2;
-
-
-struct Rotor {
-    const float *c, *s;   // the row's
-    float sign;
-};
 
 __device__ __forceinline__ float value_of(const uint4& x, int i) {
     const uint32_t w = i < 2 ? x.x : i < 4 ? x.y : i < 6 ? x.z : x.w;
     return __uint_as_float(i & 1 ? w & 0xffff0000u : w << 16);
 }
 
-template <bool SIDES>
 __global__ __launch_bounds__(ROTATE_THREADS) void rotate_wide_kernel(RotateArgs a, int units, int tokens) {
     // unit u of a token: 16 values of a head of the queries (first heads[0] heads) or of the keys
     const int chunks = (a.dh + 15) / 16;
@@ -68,7 +60,6 @@ __global__ __launch_bounds__(ROTATE_THREADS) void rotate_wide_kernel(RotateArgs 
     const bool turns = ch < turned;
     const int d0 = turns ? ch * 8 : a.rotated + (ch - turned) * 8, d1 = d0 + (turns ? half : (chunks - turned) * 8);
     const bool two = turns || d1 < a.dh;
-    const int e0 = SIDES ? ch * 4 : ch * 8, e1 = SIDES ? half / 2 + ch * 4 : e0 + 4;     // their first and second 4 pairs
     uint4 x[ROTATE_TURNS], y[ROTATE_TURNS];
     bf16_t* dst[ROTATE_TURNS];
     const float *rc[ROTATE_TURNS], *rs[ROTATE_TURNS];
@@ -77,7 +68,7 @@ __global__ __launch_bounds__(ROTATE_THREADS) void rotate_wide_kernel(RotateArgs 
         const int t = min(t0 + j * per, tokens - 1), b = t / a.n, i = t - b * a.n;
         const bf16_t* src = in.p + b * in.sample + i * in.token + h * in.head;
         dst[j] = const_cast<bf16_t*>(out.p) + b * out.sample + i * out.token + h * out.head;
-        const size_t at = (size_t)min(max(a.pos[t], 0), a.rope_len - 1) * half;
+        const size_t at = (size_t)min(max(a.pos[t], 0), a.rope_len - 1) * half + (turns ? ch * 8 : 0);
         rc[j] = a.rc + at, rs[j] = a.rs + at;
         x[j] = *reinterpret_cast<const uint4*>(src + d0);
         if (two) y[j] = *reinterpret_cast<const uint4*>(src + d1);
@@ -92,32 +83,81 @@ __global__ __launch_bounds__(ROTATE_THREADS) void rotate_wide_kernel(RotateArgs 
         }
         float c[8], s[8];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            c[e] = rc[j][e0 + e], c[4 + e] = rc[j][e1 + e];
-            s[e] = a.inverse ? -rs[j][e0 + e] : rs[j][e0 + e], s[4 + e] = a.inverse ? -rs[j][e1 + e] : rs[j][e1 + e];
-        }
+        for (int e = 0; e < 8; ++e) c[e] = rc[j][e], s[e] = a.inverse ? -rs[j][e] : rs[j][e];
         float p[8], q[8];
-        if constexpr (SIDES) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float x1 = value_of(x[j], 2 * e), x2 = value_of(x[j], 2 * e + 1);
-                const float y1 = value_of(y[j], 2 * e), y2 = value_of(y[j], 2 * e + 1);
-                p[2 * e] = x1 * c[e] - x2 * s[e], p[2 * e + 1] = x2 * c[e] + x1 * s[e];
-                q[2 * e] = y1 * c[4 + e] - y2 * s[4 + e], q[2 * e + 1] = y2 * c[4 + e] + y1 * s[4 + e];
-            }
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float x1 = value_of(x[j], e), x2 = value_of(y[j], e);
-                p[e] = x1 * c[e] - x2 * s[e], q[e] = x2 * c[e] + x1 * s[e];
-            }
+        for (int e = 0; e < 8; ++e) {
+            const float x1 = value_of(x[j], e), x2 = value_of(y[j], e);
+            p[e] = x1 * c[e] - x2 * s[e], q[e] = x2 * c[e] + x1 * s[e];
         }
         store_past_caches(dst[j] + d0, make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7])));
         store_past_caches(dst[j] + d1, make_uint4(pack_bf16x2(q[0], q[1]), pack_bf16x2(q[2], q[3]), pack_bf16x2(q[4], q[5]), pack_bf16x2(q[6], q[7])));
     }
 }
 
+// ---- rows by 16 bytes, any even number of rotated values -------------------------------------------------------------
+// A lane takes 8 values of ROTATE_HEADS heads of a token, whose cosines and sines it loads once.  Neighbours are at home in a
+// lane; the other half's values come through LDS.  Bound by memory; 41984 tokens of 32 + 8 heads of 128 (us): neighbours, all
+// rotated 151, 64 of them 146 (5.9 TB/s); halves, 120 rotated 173, 64 of them 163.
+constexpr int ROTATE_HEADS = 4;
+
+template <bool SIDES>
+__global__ __launch_bounds__(ROTATE_THREADS) void rotate_rows_kernel(RotateArgs a, int groups0, int groups, int tokens) {
+    __shared__ uint4 held[SIDES ? 1 : ROTATE_HEADS][SIDES ? 1 : ROTATE_THREADS];
+    const int tid = threadIdx.x, chunks = a.dh / 8, per = ROTATE_THREADS / chunks;
+    const int mine = tid / chunks, ch = tid - mine * chunks;
+    const int id = (int)blockIdx.x * per + mine, t = min(id / groups, tokens - 1), group = id % groups;
+    const int which = group >= groups0, h0 = (group - (which ? groups0 : 0)) * ROTATE_HEADS;
+    const int heads = mine < per && id / groups < tokens ? min(ROTATE_HEADS, a.heads[which] - h0) : 0;
+    const int b = t / a.n, i = t - b * a.n, half = a.rotated / 2;
+    const CacheRows &in = a.in[which], &out = a.out[which];
+    const bf16_t* src = in.p + b * in.sample + i * in.token + h0 * in.head + ch * 8;
+    bf16_t* dst = const_cast<bf16_t*>(out.p) + b * out.sample + i * out.token + h0 * out.head + ch * 8;
+    uint4 x[ROTATE_HEADS];
+#pragma unroll
+    for (int j = 0; j < ROTATE_HEADS; ++j)
+        if (j < heads) x[j] = *reinterpret_cast<const uint4*>(src + j * in.head);
+    const size_t at = (size_t)min(max(a.pos[t], 0), a.rope_len - 1) * half;
+    float c[8], s[8];                          // of the pairs in order, or of each value
+#pragma unroll
+    for (int e = 0; e < (SIDES ? 4 : 8); ++e) {
+        const int d = ch * 8 + e, pair = SIDES ? ch * 4 + e : d < half ? d : d - half;
+        c[e] = a.rc[at + min(pair, half - 1)], s[e] = a.rs[at + min(pair, half - 1)];
+        if (a.inverse) s[e] = -s[e];
+    }
+    if constexpr (!SIDES) {
+#pragma unroll
+        for (int j = 0; j < ROTATE_HEADS; ++j)
+            if (j < heads) held[j][tid] = x[j];
+        __syncthreads();
+    }
+#pragma unroll
+    for (int j = 0; j < ROTATE_HEADS; ++j) {
+        if (j >= heads) return;
+        float y[8];
+        if constexpr (SIDES) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float x1 = value_of(x[j], 2 * e), x2 = value_of(x[j], 2 * e + 1);
+                const bool turns = ch * 4 + e < half;
+                y[2 * e] = turns ? x1 * c[e] - x2 * s[e] : x1, y[2 * e + 1] = turns ? x2 * c[e] + x1 * s[e] : x2;
+            }
+        } else {
+            const bf16_t* row = reinterpret_cast<const bf16_t*>(&held[j][mine * chunks]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int d = ch * 8 + e;
+                const float own = value_of(x[j], e), other = bf16_to_f32(row[d < half ? d + half : d < a.rotated ? d - half : d]);
+                y[e] = d < half ? own * c[e] - other * s[e] : d < a.rotated ? own * c[e] + other * s[e] : own;
+            }
+        }
+        store_past_caches(dst + j * out.head, make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]),
+                                                         pack_bf16x2(y[6], y[7])));
+    }
+}
+
 // ---- rows of any strides and sizes: a lane a pair, or a value behind the pairs ---------------------------------------
+// Two bytes at a time: 41984 tokens of 32 + 8 heads of 128 at odd addresses take 555 us, with 120 values rotated 771.
 __global__ __launch_bounds__(ROTATE_THREADS) void rotate_any_kernel(RotateArgs a, int units, int tokens) {
     const int half = a.rotated / 2, per_head = half + a.dh - a.rotated;
     const int per = units < ROTATE_THREADS ? ROTATE_THREADS / units : 1;
@@ -146,21 +186,30 @@ __global__ __launch_bounds__(ROTATE_THREADS) void rotate_any_kernel(RotateArgs a
 }
 
 template <bool SIDES>
+static int launch_rows(const RotateArgs& a, hipStream_t st) {
+    const int per = ROTATE_THREADS / (a.dh / 8), g0 = (a.heads[0] + ROTATE_HEADS - 1) / ROTATE_HEADS;
+    const int groups = g0 + (a.heads[1] + ROTATE_HEADS - 1) / ROTATE_HEADS;
+    const unsigned grid = (unsigned)(((int64_t)a.B * a.n * groups + per - 1) / per);
+    hipLaunchKernelGGL((rotate_rows_kernel<SIDES>), dim3(grid), dim3(ROTATE_THREADS), 0, st, a, g0, groups, a.B * a.n);
+    MVLA_HIP_CHECK(hipGetLastError());
+    return MVLA_OK;
+}
+
 static int launch_wide(const RotateArgs& a, hipStream_t st) {
     const int tokens = a.B * a.n, units = (a.heads[0] + a.heads[1]) * ((a.dh + 15) / 16);
     const int per = units < ROTATE_THREADS ? ROTATE_THREADS / units : 1;
     const unsigned y = per > 1 ? 1u : (unsigned)((units + ROTATE_THREADS - 1) / ROTATE_THREADS);
-    hipLaunchKernelGGL((rotate_wide_kernel<SIDES>), dim3((unsigned)((tokens + per * ROTATE_TURNS - 1) / (per * ROTATE_TURNS)), y),
+    hipLaunchKernelGGL(rotate_wide_kernel, dim3((unsigned)((tokens + per * ROTATE_TURNS - 1) / (per * ROTATE_TURNS)), y),
                        dim3(ROTATE_THREADS), 0, st, a, units, tokens);
     MVLA_HIP_CHECK(hipGetLastError());
     return MVLA_OK;
 }
 
 int launch_rotate(const RotateArgs& a, hipStream_t st) {
-    bool wide = a.dh % 8 == 0 && a.rotated % 16 == 0;
+    bool rows = a.dh % 8 == 0;
     for (int i = 0; i < 2; ++i)
-        if (a.heads[i]) wide = wide && cache_rows_wide(a.in[i]) && cache_rows_wide(a.out[i]);
-    if (!wide) {
+        if (a.heads[i]) rows = rows && cache_rows_wide(a.in[i]) && cache_rows_wide(a.out[i]);
+    if (!rows) {
         const int tokens = a.B * a.n, units = (a.heads[0] + a.heads[1]) * (a.rotated / 2 + a.dh - a.rotated);
         const int per = units < ROTATE_THREADS ? ROTATE_THREADS / units : 1;
         const unsigned y = per > 1 ? 1u : (unsigned)((units + ROTATE_THREADS - 1) / ROTATE_THREADS);
@@ -169,7 +218,8 @@ int launch_rotate(const RotateArgs& a, hipStream_t st) {
         MVLA_HIP_CHECK(hipGetLastError());
         return MVLA_OK;
     }
-    return a.interleaved ? launch_wide<true>(a, st) : launch_wide<false>(a, st);
+    if (a.interleaved) return launch_rows<true>(a, st);
+    return a.rotated % 16 == 0 ? launch_wide(a, st) : launch_rows<false>(a, st);
 }
 
 }  // namespace mvla

@@ -10,7 +10,7 @@ LIMITS = {
                             ("mixed_pages_kernelILi128ELi16E", 2, 96), ("mixed_pages_kernelILi128ELi8E", 2, 192),
                             ("mixed_pages_kernelILi64E", 2, 0), ("join_pages_kernel", 4, 0)],
     "pages_kernels.hip": [("pages_append_kernel", 8, 0), ("pages_read_kernel", 8, 0)],
-    "rotate_kernels.hip": [("rotation_table_kernel", 4, 0), ("rotate_wide_kernel", 6, 0), ("rotate_any_kernel", 8, 0)],
+    "rotate_kernels.hip": [("rotation_table_kernel", 4, 0), ("rotate_wide_kernel", 6, 0), ("rotate_rows_kernel", 5, 0), ("rotate_any_kernel", 8, 0)],
     "logprob_kernels.hip": [("logprob_kernelILb1ELi16E", 3, 0), ("logprob_kernelILb0ELi16E", 3, 0),
                             ("logprob_kernelILb1ELi8E", 4, 0), ("logprob_kernelILb0ELi8E", 4, 0), ("logprob_kernelILb1ELi4E", 8, 0),
                             ("logprob_kernelILb0ELi4E", 8, 0), ("logprob_kernelILb1ELi1E", 8, 0), ("logprob_kernelILb0ELi1E", 8, 0),
