@@ -363,7 +363,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void few_pages_kern
 // In turn: the keys of the next tile are multiplied while this tile's logits become probabilities, this tile's values are
 // multiplied while the next tile's maxima are found.  So the matrix cores have work that waits for no vector
 // operation; two keys' and two values' tiles are in LDS, the next ones on their way.
-// Bound by the matrix products and the exponentials beside them.  2048 tokens behind 14336, 32 heads of 128: 537 us, 0.96 PFLOP/s.
+// Bound by the matrix products and the exponentials beside them.  2048 tokens behind 14336, 32 heads of 128: 537 to 569 us, 0.91 to 0.96 PFLOP/s.
 constexpr int MANY_KT = 64, MANY_WAVE_ROWS = 32;
 constexpr float SLACK = 8.f;
 
