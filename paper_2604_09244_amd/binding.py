@@ -316,6 +316,9 @@ class RotaryTable(tuple):
         self._cos, self._sin = cos.data_ptr(), sin.data_ptr()
         return self
 
+    def __reduce__(self):          # (a copy looks at its own tensors)
+        return RotaryTable, tuple(self)
+
 
 class PagedCache:
     """A layer's key/value cache in pages (mvla_pages) and the tensors that it lies in: k, v

@@ -473,7 +473,8 @@ static int run_logprobs(const LpArgs& a, int B, char* scratch, size_t scratch_by
     const int pitch = std::max(a.top, 1);
     const size_t per_row = (size_t)slices * (16 + 8 * (size_t)pitch);
     // (rows in turns: of a launch, and what scratch and counters hold)
-    const int rows = slices == 1 ? LP_ROWS : (int)std::min<size_t>((size_t)n_counters, (scratch_bytes - 256) / per_row);
+    const size_t most = VPT >= 8 ? LP_ROWS : n_counters;
+    const int rows = slices == 1 ? LP_ROWS : (int)std::min(most, (scratch_bytes - 256) / per_row);
     LpParts parts = {nullptr, nullptr, counters, pitch};
     if (slices > 1) {
         parts.stats = reinterpret_cast<uint32_t*>(scratch);

@@ -153,6 +153,48 @@ def test_long_rows_of_many(ctx):
     assert torch.equal(tt[-300:].long(), order)
 
 
+@pytest.mark.parametrize("half", [True, False])
+@pytest.mark.parametrize("vectors", [256, 1024, 2048, 4096])
+def test_rows_at_the_ends_of_a_workgroup(ctx, half, vectors):
+    """One logit more or less than a thread's vectors hold, at every address; few rows and many."""
+    rng = np.random.default_rng(vectors)
+    whole = vectors * (8 if half else 4)
+    for B, V, shift in ((2, whole - 1, 0), (2, whole, 1), (3, whole + 1, 3), (2, whole + 9, 0), (300, whole + 1, 1)):
+        x = torch.from_numpy(rng.standard_normal((B, V + 3)) * 3).to(torch.bfloat16 if half else torch.float32).cuda()
+        tokens = rng.integers(0, V, (B, 2))
+        tokens[:, 1] = V - 1
+        check(ctx, x[:, shift:shift + V], tokens, None, 20, [0, B - 1])
+
+
+def test_slices_joined_in_replays(ctx):
+    """Slices joined by the last one to end: replays over other logits, calls of other sizes in between, the same bits."""
+    g = torch.Generator("cuda").manual_seed(3)
+    cases = [(1, 262145, torch.bfloat16), (40, 50021, torch.float32), (3, 40000, torch.float32)]
+    logits = [torch.randn(B, V, device="cuda", generator=g).to(t) for B, V, t in cases]
+    tokens = [torch.randint(0, V, (B, 1), device="cuda", dtype=torch.int32) for B, V, _ in cases]
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        own = mv.Context.for_pages(1, 1, 1, 1, 1, 1, 64)
+        own.logprobs(logits[0], tokens[0], top=32)
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            got = [own.logprobs(x, t, top=32) for x, t in zip(logits, tokens)]
+        for turn in range(4):
+            for x in logits:
+                x.copy_(torch.randn(x.shape, device="cuda", generator=g) * (turn + 1))
+            graph.replay()
+            stream.synchronize()
+            for x, t, outs in zip(logits, tokens, got):
+                want = own.logprobs(x, t, top=32)
+                stream.synchronize()
+                assert all(torch.equal(a, b) for a, b in zip(outs, want))
+                order = torch.sort(x.float(), dim=1, descending=True, stable=True).indices[:, :32]
+                assert torch.equal(outs[2].long(), order)
+    torch.cuda.current_stream().wait_stream(stream)
+
+
 def test_refusals(ctx):
     x, tok = torch.zeros(2, 10, device="cuda"), ints([1, 2])
     for kw, code in ((dict(top=33), EUNSUPPORTED), (dict(top=-1), EINVAL)):

@@ -2,6 +2,9 @@
 
 Bar: a product's two terms are each off by their own rounding, the table's and the sum's, 2^-22 of |x1| + |x2| together,
 times the gain; the result by half a step of bf16, 2^-8 of itself."""
+import copy
+import pickle
+
 import numpy as np
 import pytest
 import torch
@@ -152,3 +155,9 @@ def test_a_pair_of_tables_serves_like_a_rotary_table(ctx):
     for bad in [(cos.t().contiguous().t(), sin), (cos, sin[:9]), (cos.half(), sin), (cos, sin.cpu())]:
         with pytest.raises(AssertionError):
             ctx.rotate(q, None, pos, bad)
+
+
+def test_a_copied_rotary_table_is_its_own(ctx):
+    rope = ctx.rotary_table(64, 10)
+    for twin in (copy.deepcopy(rope), pickle.loads(pickle.dumps(rope))):
+        assert type(twin) is mv.RotaryTable and twin._cos == twin[0].data_ptr() != rope._cos and torch.equal(twin[1], rope[1])
