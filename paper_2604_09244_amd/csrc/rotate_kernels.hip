@@ -35,7 +35,7 @@ int launch_rotation_table(const mvla_rotation& how, int rope_len, float* c, floa
 // A lane takes two runs of 8 values of a head, the same places of either half of the rotated ones or of those behind them, so that
 // a wave's accesses are whole stretches; of ROTATE_TURNS tokens, whose loads do not wait for each other.
 // Bound by memory: 2 bytes in and 2 out a value, and the tokens' cosines and sines once.  41984 tokens of 32 + 8 heads of 128,
-// all rotated: 153 us, 5.6 TB/s; with stores through the caches 162, one token a lane 173, four 155; in the form below 184.
+// all rotated: 153 us, 5.6 TB/s; with stores through the caches 162, one token a lane 173, four 155; in the form below 194.
 constexpr int ROTATE_THREADS = 256, ROTATE_TURNS = 2;
 
 __device__ __forceinline__ float value_of(const uint4& x, int i) {
@@ -98,12 +98,12 @@ __global__ __launch_bounds__(ROTATE_THREADS) void rotate_wide_kernel(RotateArgs 
 // ---- rows by 16 bytes, any even number of rotated values -------------------------------------------------------------
 // A lane takes 8 values of ROTATE_HEADS heads of a token, whose cosines and sines it loads once.  Neighbours are at home in a
 // lane; the other half's values come through LDS.  Bound by memory; 41984 tokens of 32 + 8 heads of 128 (us): neighbours, all
-// rotated 151, 64 of them 146 (5.9 TB/s); halves, 120 rotated 173, 64 of them 163.
+// rotated 151, 64 of them 146 (5.9 TB/s); halves, 120 rotated 181, 74 of them 169.
 constexpr int ROTATE_HEADS = 4;
 
 template <bool SIDES>
 __global__ __launch_bounds__(ROTATE_THREADS) void rotate_rows_kernel(RotateArgs a, int groups0, int groups, int tokens) {
-    __shared__ uint4 held[SIDES ? 1 : ROTATE_HEADS][SIDES ? 1 : ROTATE_THREADS];
+    __shared__ uint32_t held[SIDES ? 1 : ROTATE_HEADS][4][SIDES ? 1 : ROTATE_THREADS];     // (word i of every lane's 16 bytes)
     const int tid = threadIdx.x, chunks = a.dh / 8, per = ROTATE_THREADS / chunks;
     const int mine = tid / chunks, ch = tid - mine * chunks;
     const int id = (int)blockIdx.x * per + mine, t = min(id / groups, tokens - 1), group = id % groups;
@@ -128,7 +128,7 @@ __global__ __launch_bounds__(ROTATE_THREADS) void rotate_rows_kernel(RotateArgs 
     if constexpr (!SIDES) {
 #pragma unroll
         for (int j = 0; j < ROTATE_HEADS; ++j)
-            if (j < heads) held[j][tid] = x[j];
+            if (j < heads) held[j][0][tid] = x[j].x, held[j][1][tid] = x[j].y, held[j][2][tid] = x[j].z, held[j][3][tid] = x[j].w;
         __syncthreads();
     }
 #pragma unroll
@@ -143,11 +143,12 @@ __global__ __launch_bounds__(ROTATE_THREADS) void rotate_rows_kernel(RotateArgs 
                 y[2 * e] = turns ? x1 * c[e] - x2 * s[e] : x1, y[2 * e + 1] = turns ? x2 * c[e] + x1 * s[e] : x2;
             }
         } else {
-            const bf16_t* row = reinterpret_cast<const bf16_t*>(&held[j][mine * chunks]);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const int d = ch * 8 + e;
-                const float own = value_of(x[j], e), other = bf16_to_f32(row[d < half ? d + half : d < a.rotated ? d - half : d]);
+                const int from = d < half ? d + half : d < a.rotated ? d - half : d;
+                const uint32_t word = held[j][from / 2 % 4][mine * chunks + from / 8];
+                const float own = value_of(x[j], e), other = __uint_as_float(from % 2 ? word & 0xffff0000u : word << 16);
                 y[e] = d < half ? own * c[e] - other * s[e] : d < a.rotated ? own * c[e] + other * s[e] : own;
             }
         }
