@@ -139,8 +139,7 @@ __global__ __launch_bounds__(ROTATE_THREADS) void rotate_rows_kernel(RotateArgs 
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const float x1 = value_of(x[j], 2 * e), x2 = value_of(x[j], 2 * e + 1);
-                const bool turns = ch * 4 + e < half;
-                y[2 * e] = turns ? x1 * c[e] - x2 * s[e] : x1, y[2 * e + 1] = turns ? x2 * c[e] + x1 * s[e] : x2;
+                y[2 * e] = x1 * c[e] - x2 * s[e], y[2 * e + 1] = x2 * c[e] + x1 * s[e];
             }
         } else {
 #pragma unroll
@@ -149,11 +148,12 @@ __global__ __launch_bounds__(ROTATE_THREADS) void rotate_rows_kernel(RotateArgs 
                 const int from = d < half ? d + half : d < a.rotated ? d - half : d;
                 const uint32_t word = held[j][from / 2 % 4][mine * chunks + from / 8];
                 const float own = value_of(x[j], e), other = __uint_as_float(from % 2 ? word & 0xffff0000u : word << 16);
-                y[e] = d < half ? own * c[e] - other * s[e] : d < a.rotated ? own * c[e] + other * s[e] : own;
+                y[e] = d < half ? own * c[e] - other * s[e] : own * c[e] + other * s[e];
             }
         }
-        store_past_caches(dst + j * out.head, make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]),
-                                                         pack_bf16x2(y[6], y[7])));
+        const int end = a.rotated - ch * 8;    // (words behind it are copied bit by bit)
+        store_past_caches(dst + j * out.head, make_uint4(0 < end ? pack_bf16x2(y[0], y[1]) : x[j].x, 2 < end ? pack_bf16x2(y[2], y[3]) : x[j].y,
+                                                         4 < end ? pack_bf16x2(y[4], y[5]) : x[j].z, 6 < end ? pack_bf16x2(y[6], y[7]) : x[j].w));
     }
 }
 

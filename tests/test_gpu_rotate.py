@@ -161,3 +161,13 @@ def test_a_copied_rotary_table_is_its_own(ctx):
     rope = ctx.rotary_table(64, 10)
     for twin in (copy.deepcopy(rope), pickle.loads(pickle.dumps(rope))):
         assert type(twin) is mv.RotaryTable and twin._cos == twin[0].data_ptr() != rope._cos and torch.equal(twin[1], rope[1])
+
+
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("dh,rot", [(64, 32), (64, 30), (128, 74), (72, 2), (50, 20)])
+def test_values_behind_the_rotated_ones_keep_their_bits(ctx, dh, rot, inter):
+    rng = np.random.default_rng(rot)
+    q = torch.from_numpy(rng.integers(-32768, 32768, (70, 5, dh)).astype(np.int16)).cuda()      # NaN of every kind among them
+    pos, rope = torch.arange(70, dtype=torch.int32, device="cuda"), ctx.rotary_table(rot, 70)
+    got = ctx.rotate(q.view(torch.bfloat16), None, pos, rope, interleaved=inter)[0].view(torch.int16)
+    assert torch.equal(got[..., rot:], q[..., rot:])
