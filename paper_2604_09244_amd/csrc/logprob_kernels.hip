@@ -10,7 +10,7 @@
 // list in LDS, where each one's place is the number of its betters.
 //
 // Bound by vector operations, 12 to 15 a logit (unpacking, maximum, difference, power, two sums): 2624 rows of 131073 bf16 with
-// 20 best tokens take 170 us, 4.0 TB/s, of which the join is 11; one row of 32768 fp32 a chain of 10 us.
+// 20 best tokens take 170 us, 4.0 TB/s, of which the join is 11; one row of 32768 fp32 a chain of 9.4 us.
 #include "common.h"
 #include "mfma.h"
 #include "wave.h"
@@ -227,7 +227,7 @@ __device__ __forceinline__ void lp_join(const LpArgs& a, const LpRow& r, int row
     lp_finish<HALF>(a, r, row, s, best, tid);
 }
 
-// VPT vectors of 16 bytes a thread.  Slices along blockIdx.y.  With 1 or 4 vectors all of a launch's workgroups run at once and
+// VPT vectors of 16 bytes a thread.  Slices along blockIdx.y.  With 4 vectors all of a launch's workgroups run at once and
 // the last one of a row to end joins its slices (a call on 1 x 32768: 14 us, and 17 with a second launch).  With 16 they take turns,
 // and each would hold its registers until its count has come back: joined by a second launch (2624 x 131073: 174 us, not 220).
 template <bool HALF, int VPT>
@@ -495,14 +495,13 @@ int launch_logprobs(const void* logits, bool half, int64_t row_stride, int B, in
     const LpArgs a = {logits, row_stride, V, n_tokens, top, temperature, tokens, logprob, entropy, top_token, top_logprob};
     // A row that 2048 vectors hold is one workgroup's, of as few as hold it: empty places cost what full ones do, and their
     // registers room (us; 4096 rows of 2048 bf16: 17.9 with 1 vector a thread, 57.9 with 16; of 8192: 26.8 with 4, 58.9 with 16;
-    // of 16384: 37.8 with 8, 59.9 with 16).  Longer rows: as few slices as leave a workgroup for every compute unit (4096 rows of
-    // 50000: 123 with 16, 138 with 4; 64 rows of 50000: 13.4 with 4, 16.0 with 16).
-    const int64_t want = device_cu_count(), vectors = V / (half ? 8 : 4);
-    auto fills = [&](int vpt) { return B * ((vectors + LP_THREADS * vpt - 1) / (LP_THREADS * vpt)) >= want; };
-    const int64_t most = (int64_t)LP_THREADS * LP_THREADS;      // (vectors that a slice for each of the joining threads takes)
-    int vpt;
-    if (vectors <= 8 * LP_THREADS) vpt = vectors <= LP_THREADS ? 1 : vectors <= 4 * LP_THREADS ? 4 : 8;
-    else vpt = fills(16) || vectors > 4 * most ? 16 : fills(4) || vectors > most ? 4 : 1;
+    // of 16384: 37.8 with 8, 59.9 with 16).  Longer rows: 16 where that leaves a workgroup for every compute unit, else 4 (4096 rows
+    // of 50000: 123 with 16, 138 with 4; 64 rows of 50000: 13.4 with 4, 16.0 with 16; one of 32768 fp32, on the device: 9.4 with
+    // 4, 10.3 with 1).
+    const int64_t vectors = V / (half ? 8 : 4);
+    const bool fills = B * ((vectors + 16 * LP_THREADS - 1) / (16 * LP_THREADS)) >= device_cu_count();
+    const int64_t most = 4 * LP_THREADS * LP_THREADS;          // (vectors that a slice of 4 for each of the joining threads takes)
+    const int vpt = vectors <= LP_THREADS ? 1 : vectors <= 4 * LP_THREADS ? 4 : vectors <= 8 * LP_THREADS ? 8 : fills || vectors > most ? 16 : 4;
     auto run = [&](auto of_16_bits) {
         constexpr bool HALF = decltype(of_16_bits)::value;
         return vpt == 16  ? run_logprobs<HALF, 16>(a, B, scratch, scratch_bytes, counters, n_counters, st)
