@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Dict, List, Optional, Sequence
 
 import torch
@@ -206,12 +207,12 @@ def load() -> C.CDLL:
     lib.mvla_sample.argtypes = [vp, vp, i, C.c_int64, i, i, vp, vp, vp, vp, vp, vp, vp]
     pages, batch = C.POINTER(PagesC), C.POINTER(PageBatchC)
     lib.mvla_rotation_table.argtypes = [vp, C.POINTER(Rotation), i, vp, vp]
-    lib.mvla_rotate.argtypes = [vp, rows, i, rows, rows, i, rows, vp, i, i, i, i, i, i, vp, vp, i]
+    lib.mvla_rotate.argtypes = [vp, vp, i, vp, vp, i, vp, vp, i, i, i, i, i, i, vp, vp, i]
     lib.mvla_pages_workspace_bytes.restype = sz
     lib.mvla_pages_workspace_bytes.argtypes = [i] * 7
-    lib.mvla_pages_append.argtypes = [vp, pages, batch, rows, rows, i]
+    lib.mvla_pages_append.argtypes = [vp, pages, batch, vp, vp, i]
     lib.mvla_pages_read.argtypes = [vp, pages, batch, vp, i, vp, vp]
-    lib.mvla_pages_attention.argtypes = [vp, pages, batch, rows, i, i, i, i, f, rows, vp]
+    lib.mvla_pages_attention.argtypes = [vp, pages, batch, vp, i, i, i, i, f, vp, vp]
     lib.mvla_logprobs.argtypes = [vp, vp, i, C.c_int64, i, i, vp, vp, i, vp, vp, i, vp, vp]
     lib.mvla_profile_enable.argtypes = [vp, C.c_uint32, i]
     lib.mvla_profile_read.argtypes = [vp, i, vp, vp, vp, vp]
@@ -298,10 +299,15 @@ def _current_stream(index: int) -> int:
     return torch._C._cuda_getCurrentRawStream(index)
 
 
-def _packed_rows(t: torch.Tensor) -> Rows:
-    """Description of a bf16 tensor [tokens, heads, dh] of any strides."""
-    assert t.is_cuda and t.dtype == torch.bfloat16 and t.dim() == 3, (t.device, t.dtype, t.shape)
-    return Rows(t.data_ptr(), 0, *t.stride())
+_pack_rows = struct.Struct("@P4q").pack
+
+
+def _rows_of(t: torch.Tensor) -> bytes:
+    """Description (the bytes of a Rows) of a bf16 tensor [B, tokens, heads, dh] or [tokens, heads, dh] of any
+    strides, whose device and shape the caller has looked at."""
+    assert t.dtype == torch.bfloat16, t.dtype
+    strides = t.stride()
+    return _pack_rows(t.data_ptr(), *strides) if len(strides) == 4 else _pack_rows(t.data_ptr(), 0, *strides)
 
 
 class RotaryTable(tuple):
@@ -431,6 +437,8 @@ class Context:
         _check(lib.mvla_create(C.byref(self._h), self.device.index or 0, self.stream.cuda_stream,
                                self.workspace.data_ptr(), nbytes), "mvla_create")
         self._rope = {}
+        self._none = {t: torch.empty(0, dtype=t, device=self.device)        # (what new tensors are quickest made from)
+                      for t in (torch.bfloat16, torch.float32, torch.int32)}
 
     def close(self):
         if getattr(self, "_h", None) is not None and self._h.value:
@@ -795,9 +803,9 @@ class Context:
     def _new(self, shape, dtype) -> torch.Tensor:
         """An output: memory of the stream that the calls run on, also where another one is current."""
         if _current_stream(self._index) == self._raw_stream:
-            return torch.empty(shape, dtype=dtype, device=self.device)
+            return self._none[dtype].new_empty(shape)
         with torch.cuda.stream(self.stream):
-            return torch.empty(shape, dtype=dtype, device=self.device)
+            return self._none[dtype].new_empty(shape)
 
     def _like(self, t: torch.Tensor, dtype=None) -> torch.Tensor:
         """As ``_new``, contiguous and shaped as ``t``."""
@@ -829,10 +837,10 @@ class Context:
         if type(rope) is not RotaryTable:
             rope = RotaryTable(*rope)
         if q.dim() == 3:
-            rows, B, (n, H, dh) = _packed_rows, 1, q.shape
+            B, (n, H, dh) = 1, q.shape
             tokens, H_kv = (n,), 0
         else:
-            rows, (B, n, H, dh) = _rows, q.shape
+            B, n, H, dh = q.shape
             tokens, H_kv = (B, n), 0
         on = self._index
         assert q.get_device() == on == rope.index and self._is(pos, torch.int32, tokens), (q.device, pos.shape, pos.dtype)
@@ -845,8 +853,8 @@ class Context:
         if k is not None:
             H_kv = k.shape[-2]
             assert k.shape == (*tokens, H_kv, dh) == k_out.shape and k.get_device() == k_out.get_device() == on, k.shape
-            k_ref, k_out_ref = C.byref(rows(k)), C.byref(rows(k_out))
-        _check(load().mvla_rotate(self._h, C.byref(rows(q)), H, C.byref(rows(q_out)), k_ref, H_kv, k_out_ref,
+            k_ref, k_out_ref = _rows_of(k), _rows_of(k_out)
+        _check(load().mvla_rotate(self._h, _rows_of(q), H, _rows_of(q_out), k_ref, H_kv, k_out_ref,
                                   pos.data_ptr(), B, n, dh, rope.rotated, interleaved, inverse, rope._cos,
                                   rope._sin, rope.rope_len), "mvla_rotate")
         return q_out, k_out
@@ -858,8 +866,7 @@ class Context:
         on = self._index
         assert k.shape == v.shape and H == cache.H_kv and dh == cache.dh, (k.shape, v.shape)
         assert k.get_device() == v.get_device() == cache.index == batch.index == on
-        _check(load().mvla_pages_append(self._h, cache._ref, batch._ref, C.byref(_packed_rows(k)),
-                                        C.byref(_packed_rows(v)), n), "mvla_pages_append")
+        _check(load().mvla_pages_append(self._h, cache._ref, batch._ref, _rows_of(k), _rows_of(v), n), "mvla_pages_append")
 
     def pages_read(self, cache: PagedCache, batch: PageBatch, first: Optional[torch.Tensor], n: int, out=None):
         """Rows first[b] .. first[b] + n - 1 (first None: from 0) of each sequence as bf16 (k, v)
@@ -897,10 +904,10 @@ class Context:
                 out, lse = out
                 assert self._is(lse, torch.float32, (n, H))
             assert out.shape == q.shape and out.get_device() == on
-        _check(load().mvla_pages_attention(self._h, cache._ref, batch._ref, C.byref(_packed_rows(q)), H, n,
+        _check(load().mvla_pages_attention(self._h, cache._ref, batch._ref, _rows_of(q), H, n,
                                            max(n, 1) if max_q is None else max_q,
                                            batch.entries * cache.page if max_length is None else max_length,
-                                           dh ** -0.5 if scale is None else scale, C.byref(_packed_rows(out)),
+                                           dh ** -0.5 if scale is None else scale, _rows_of(out),
                                            _ptr(lse)), "mvla_pages_attention")
         return (out, lse) if with_lse else out
 

@@ -150,8 +150,8 @@ def test_empty_calls_and_refusals():
         bad = garbage_pool(2, 2, 64, 16, 8)
         setattr(bad._c, field, value)
         with pytest.raises(mv.MvlaError) as e:
-            mv._check(mv.load().mvla_pages_append(ctx.handle, bad._ref, batch._ref, mv.C.byref(mv._packed_rows(x)),
-                                                  mv.C.byref(mv._packed_rows(x)), 8), "append")
+            mv._check(mv.load().mvla_pages_append(ctx.handle, bad._ref, batch._ref, mv._rows_of(x),
+                                                  mv._rows_of(x), 8), "append")
         assert e.value.code == code, field
         with pytest.raises(mv.MvlaError) as e:
             mv._check(mv.load().mvla_pages_read(ctx.handle, bad._ref, batch._ref, None, 8, k.data_ptr(), v.data_ptr()), "read")
