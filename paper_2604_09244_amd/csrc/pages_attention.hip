@@ -66,7 +66,9 @@ constexpr int NO_SLOT = 0x7fffffff;
 // ---- few rows ----------------------------------------------------------------------------------------------------
 // Up to 16 rows a key head: a wave takes 32 slots at a time straight from memory to registers, nothing passes through LDS.
 // The slots of a step are dealt to the operand rows so that no lane needs another's data:
-//   K: row r of tile j (of two) is slot 8 (r / 4) + 4 j + r % 4; the lanes of a row read neighbouring pieces of it
+//   K: row r of tile j (of two) is slot 8 (r / 4) + 4 j + r % 4; the lanes of a row read neighbouring pieces of it (of 8
+//      bits 32 bytes in a row, which have one power: with two a lane, and a register too many for three waves a SIMD, the
+//      257 us below were 295)
 //   S^T: a lane of group g then holds the logits of slots 8 g .. 8 g + 7 of its column, in order: its P^T operand
 //   V: lane c of a group takes dims c CH .. c CH + CH - 1 of the group's eight slots; two permutes turn two slots' pairs of
 //      dims into pairs of slots of one dim
@@ -74,7 +76,7 @@ constexpr int NO_SLOT = 0x7fffffff;
 // A step lies in one page, or its halves in two: where they are comes from scalar loads, a round ahead.
 // Bound by memory: every cached row is read once.  16 sequences of 2624 slots, 32 heads of 16 bits: 112 us, 6.1 TB/s (values kept
 // in caches: 121; keys past them too, whose reads are of half lines: 118).  64 of up to 16384 slots, 8 key heads of 8 bits with
-// four query heads each: 294 us, 4.9 TB/s.
+// four query heads each: 257 us, 5.6 TB/s.
 constexpr int FEW_STEP = 32, FEW_ROWS = 16;
 
 template <int DH, int BITS>
@@ -120,10 +122,10 @@ __device__ __forceinline__ void few_rows(const PagesView& cache, const PagesAtte
         const size_t kr = (c < 8 ? s.row[0] : s.row[1]) + k_row, vr = (g < 2 ? s.row[0] : s.row[1]) + 8 * g;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            const uint8_t* p = cache.k + (kr + 4 * j) * KB + g * 16;
+            const uint8_t* p = cache.k + (kr + 4 * j) * KB + g * (BITS == 8 ? KB / 4 : 16);
 #pragma unroll
             for (int i = 0; i < Raw::KW / 4; ++i) {
-                const uint4 w = *reinterpret_cast<const uint4*>(p + i * 64);
+                const uint4 w = *reinterpret_cast<const uint4*>(p + i * (BITS == 8 ? 16 : 64));
                 x.k[j][4 * i] = w.x, x.k[j][4 * i + 1] = w.y, x.k[j][4 * i + 2] = w.z, x.k[j][4 * i + 3] = w.w;
             }
             if constexpr (BITS == 8) {
@@ -185,7 +187,7 @@ __device__ __forceinline__ void few_rows(const PagesView& cache, const PagesAtte
         const bf16_t* src = a.q.p + (int64_t)(span.row0 + qi) * a.q.token + (int64_t)(h * group + c % group) * a.q.head;
 #pragma unroll
         for (int st = 0; st < STEPS; ++st)
-            qf[st] = *reinterpret_cast<const uint4*>(src + (BITS == 16 ? st * 32 + g * 8 : st / 2 * 64 + g * 16 + st % 2 * 8));
+            qf[st] = *reinterpret_cast<const uint4*>(src + (BITS == 16 ? st * 32 + g * 8 : g * (DH / 4) + st * 8));
     }
     const float scale_log2e = a.scale * 1.4426950408889634f;
     const int v_blk = DH == 128 ? c >> 2 : c >> 3;
@@ -208,8 +210,8 @@ __device__ __forceinline__ void few_rows(const PagesView& cache, const PagesAtte
                 uint4 kf;
                 if constexpr (BITS == 16) {
                     kf = make_uint4(x.k[j][4 * st], x.k[j][4 * st + 1], x.k[j][4 * st + 2], x.k[j][4 * st + 3]);
-                } else {   // (the byte of block st / 2 * 2 + g / 2 turned to the exponent's place)
-                    const float e = __uint_as_float(__builtin_amdgcn_alignbit(x.ks[j], x.ks[j], 9 + 8 * (st / 2 * 2 + (g >> 1))));
+                } else {   // (the byte of the lane's block turned to the exponent's place)
+                    const float e = __uint_as_float(__builtin_amdgcn_alignbit(x.ks[j], x.ks[j], 9 + 8 * (DH == 128 ? g : g >> 1)));
                     kf = fp8_values(make_uint2(x.k[j][2 * st], x.k[j][2 * st + 1]), e);
                 }
                 s[j] = mfma16(kf, qf[st], s[j]);

@@ -6,7 +6,8 @@ from test_kernel_resources import _resource_usage
 # kernel, waves a SIMD at least, bytes of scratch a lane at most (many rows of 128 spill outside their loop over tiles where rows
 # are 16-bit, and a few registers within it where they become bf16 on the way)
 LIMITS = {
-    "pages_attention.hip": [("few_pages_kernelILi128E", 2, 0), ("few_pages_kernelILi64E", 4, 0),
+    "pages_attention.hip": [("few_pages_kernelILi128ELi16E", 2, 0), ("few_pages_kernelILi128ELi8E", 3, 0),
+                            ("few_pages_kernelILi64E", 4, 0),
                             ("mixed_pages_kernelILi128ELi16E", 2, 96), ("mixed_pages_kernelILi128ELi8E", 2, 192),
                             ("mixed_pages_kernelILi64E", 2, 0), ("join_pages_kernel", 4, 0)],
     "pages_kernels.hip": [("pages_append_kernel", 8, 0), ("pages_read_kernel", 8, 0)],
