@@ -52,6 +52,44 @@ def test_rows_come_back(dh, bits, page):
         assert torch.equal(torch.where(touched, 0, x.view(torch.uint8)), torch.where(touched, 0, y.view(torch.uint8)))
 
 
+@pytest.mark.parametrize("wide", [True, False])
+@pytest.mark.parametrize("dh,bits", [(128, 8), (64, 8), (128, 16)])
+def test_many_rows_come_back(dh, bits, wide):
+    """So many rows that a lane takes several: of sequences that begin and end anywhere, with bad pages among them."""
+    rng = np.random.default_rng(dh + bits + wide)
+    lengths, new = [700, 1, 0, 1203, 33, 900], [511, 1, 0, 1203, 2, 17]
+    H, page = 11, 32
+    n_pages, table = deal(rng, lengths, page, entries=40)
+    table[3, 7], table[0, 20] = -5, n_pages                   # (no pages: not written, zeros)
+    cache = garbage_pool(n_pages, H, dh, page, bits)
+    before = all_bytes(cache)
+    at = np.concatenate([[3], 3 + np.cumsum(new)])
+    n = int(at[-1]) + 5
+    k, v = (bf16(rng, n, H, dh, scale=3.0) for _ in range(2))
+    kc, vc = ((x.cuda() if wide else torch.stack([x, x], -1).cuda()[..., 1]) for x in (k, v))
+    batch = mv.PageBatch(ints(at.tolist()), ints(lengths), torch.from_numpy(table).cuda())
+    ctx = mv.Context.for_pages(len(lengths), H, H, n, n, 40 * page, dh)
+    ctx.pages_append(cache, batch, kc, vc)
+    first = [t - c for t, c in zip(lengths, new)]
+    kr, vr = ctx.pages_read(cache, batch, ints(first), 1204)
+    touched = np.zeros((n_pages, page), bool)
+    for x, got in ((k, kr), (v, vr)):
+        for b, c in enumerate(new):
+            rows = x[at[b]:at[b + 1]].double().numpy().transpose(1, 0, 2)
+            want = rows if bits == 16 or c == 0 else M.fp8_decode(*M.fp8_encode(rows))
+            want = want.copy()
+            for s in range(c):
+                p = table[b, (first[b] + s) // page]
+                if 0 <= p < n_pages:
+                    touched[p, (first[b] + s) % page] = True
+                else:
+                    want[:, s] = 0.0
+            assert np.array_equal(f64(got[b, :, :c]), want), b
+    touched = torch.from_numpy(touched).cuda()[:, None, :, None]
+    for x, y in zip(before, all_bytes(cache)):
+        assert torch.equal(torch.where(touched, 0, x.view(torch.uint8)), torch.where(touched, 0, y.view(torch.uint8)))
+
+
 @pytest.mark.parametrize("dh", [64, 128])
 def test_codes_and_powers(dh):
     """Every exponent, ties, the ends of the range, blocks with no number: codes and powers as the definition has them."""
