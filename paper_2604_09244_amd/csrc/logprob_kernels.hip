@@ -10,7 +10,7 @@
 // list in LDS, where each one's place is the number of its betters.
 //
 // Bound by vector operations, 12 to 15 a logit (unpacking, maximum, difference, power, two sums): 2624 rows of 131073 bf16 with
-// 20 best tokens take 170 us, 4.0 TB/s, of which the join is 11; one row of 32768 fp32 a chain of 9.4 us.
+// 20 best tokens take 167 us, 4.1 TB/s, of which the join is 11; one row of 32768 fp32 a chain of 9.4 us.
 #include "common.h"
 #include "mfma.h"
 #include "wave.h"
@@ -227,11 +227,13 @@ __device__ __forceinline__ void lp_join(const LpArgs& a, const LpRow& r, int row
     lp_finish<HALF>(a, r, row, s, best, tid);
 }
 
-// VPT vectors of 16 bytes a thread.  Slices along blockIdx.y.  With 4 vectors all of a launch's workgroups run at once and
-// the last one of a row to end joins its slices (a call on 1 x 32768: 14 us, and 17 with a second launch).  With 16 they take turns,
-// and each would hold its registers until its count has come back: joined by a second launch (2624 x 131073: 174 us, not 220).
+// VPT vectors of 16 bytes a thread; four waves a SIMD, for which 16 vectors leave no register over (4 are kept in memory; with
+// three waves 4096 rows of 32768 bf16 take 63 us instead of 60).  Slices along blockIdx.y.  With 4 vectors all of a launch's
+// workgroups run at once and the last one of a row to end joins its slices (a call on 1 x 32768: 14 us, and 17 with a second
+// launch).  With 16 they take turns, and each would hold its registers until its count has come back: joined by a second launch
+// (2624 x 131073, with three waves: 174 us, not 220).
 template <bool HALF, int VPT>
-__global__ __launch_bounds__(LP_THREADS, VPT == 16 ? 3 : 4) void logprob_kernel(LpArgs a, int row0, LpParts parts) {
+__global__ __launch_bounds__(LP_THREADS, 4) void logprob_kernel(LpArgs a, int row0, LpParts parts) {
     constexpr int EPV = HALF ? 8 : 4, SIZE = HALF ? 2 : 4;
     __shared__ float sh_max[LP_WAVES][64], sh_group[64], sh_bound;
     __shared__ bool sh_last;
@@ -271,8 +273,10 @@ __global__ __launch_bounds__(LP_THREADS, VPT == 16 ? 3 : 4) void logprob_kernel(
         for (int i = 0; i < VPT; ++i) asm volatile("" : "+v"(raw[i].x), "+v"(raw[i].y), "+v"(raw[i].z), "+v"(raw[i].w));
     };
     // ---- maximum: of each vector, of the thread's, of the workgroup's
-    float top[VPT], mine = x_lone;
+    float mine = x_lone;
+    uint32_t tops[HALF ? (VPT + 1) / 2 : VPT];  // of each vector; of 16 bits two a word
     auto maxima = [&]() __attribute__((always_inline)) {
+        float top[VPT];
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             float m = lp_max3(at(i, 0), at(i, 1), at(i, 2));
@@ -284,6 +288,12 @@ __global__ __launch_bounds__(LP_THREADS, VPT == 16 ? 3 : 4) void logprob_kernel(
 #pragma unroll
         for (int i = 0; i + 1 < VPT; i += 2) mine = lp_max3(mine, top[i], top[i + 1]);
         if (VPT % 2) mine = lp_max3(mine, top[VPT - 1], -INFINITY);
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) {
+            if (!HALF) tops[i] = __float_as_uint(top[i]);
+            else if (i % 2) tops[i / 2] = __builtin_amdgcn_perm(__float_as_uint(top[i]), __float_as_uint(top[i - 1]), 0x07060302u);
+            else if (i + 1 == VPT) tops[i / 2] = __float_as_uint(top[i]) >> 16;
+        }
     };
     maxima();
     if (mine != mine) {                        // (rare) NaN counts as -infinity
@@ -293,6 +303,8 @@ __global__ __launch_bounds__(LP_THREADS, VPT == 16 ? 3 : 4) void logprob_kernel(
         maxima();
     }
     packed();
+#pragma unroll
+    for (auto& w : tops) asm volatile("" : "+v"(w));
     sh_max[wave][lane] = mine;
     if (tid == 0) sh.n = 0;
     __syncthreads();
@@ -375,7 +387,10 @@ __global__ __launch_bounds__(LP_THREADS, VPT == 16 ? 3 : 4) void logprob_kernel(
             // (few threads have any, and hardly one more than one vector: read again rather than looked for in registers)
             uint32_t have = 0;
 #pragma unroll
-            for (int i = 0; i < VPT; ++i) have |= top[i] >= bound && v0 + i * LP_THREADS + tid < nv ? 1u << i : 0u;
+            for (int i = 0; i < VPT; ++i) {
+                const float top = __uint_as_float(!HALF ? tops[i] : i % 2 ? tops[i / 2] & 0xffff0000u : tops[i / 2] << 16);
+                have |= top >= bound && v0 + i * LP_THREADS + tid < nv ? 1u << i : 0u;
+            }
             while (have) {
                 const int v = v0 + (__ffs(have) - 1) * LP_THREADS + tid;
                 have &= have - 1;
