@@ -32,6 +32,12 @@ __device__ __forceinline__ float quad_sum(float x) {
 __device__ __forceinline__ float max3(float a, float b, float c) {
     return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
 }
+// An exponential is 2^(x c - m c), c = scale log2 e, by one rounding behind the exact x c: what m c itself was rounded by (half
+// a step) stays in the exponent, that of the largest logit too.  Below this bound it is 2^-9 at most, as much as rounding to bf16
+// takes of a probability.  From it on (logits of ten thousands) a wave subtracts m first: left there, the rounding would weigh a
+// row's parts by different factors, and from 2^31 on make its sum zero or infinite.  The look at it costs 0 to 2 % of a pass.
+constexpr float FAR_REFERENCE = 0x1p16f;
+
 // Values that are no finite numbers, where some rows see their slots and others do not: in a matrix product a weight of
 // zero would not keep them from the others.  They are taken out of the product; per dim, the first slot with a value of
 // +inf or NaN and the first with -inf or NaN say which rows' sums they belong to (a row sees the slots below its limit).
@@ -266,7 +272,13 @@ __device__ __forceinline__ void few_rows(const PagesView& cache, const PagesAtte
                 for (int i = 0; i < 4; ++i) o[d][i] *= f;
             run_m = m;
         }
-        const float neg_m = run_m == -INFINITY ? 0.f : -run_m * scale_log2e;   // (a row that has seen nothing yet)
+        float neg_m = run_m == -INFINITY ? 0.f : -run_m * scale_log2e;         // (a row that has seen nothing yet)
+        if (__any(!(fabsf(neg_m) < FAR_REFERENCE))) {
+            const float from = run_m == -INFINITY ? 0.f : run_m;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s[i >> 2][i & 3] -= from;
+            neg_m = 0.f;
+        }
         float e[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -676,12 +688,20 @@ __device__ __forceinline__ void many_rows(const PagesView& cache, const PagesAtt
     // before its products, or lets registers spill): two products of the next tile's keys with the probabilities of a few of this
     // tile's logits in their shadow, reads two steps ahead; then a 16-slot step of this tile's values with its share of
     // the next tile's maxima.
-    auto products = [&](const f32x16_t (&now)[2], f32x16_t (&then)[2], uint4 (&kf)[4], uint32_t k_tile, uint32_t v_tile)
+    auto products = [&](f32x16_t (&now)[2], f32x16_t (&then)[2], uint4 (&kf)[4], uint32_t k_tile, uint32_t v_tile)
         __attribute__((always_inline)) {
         constexpr int PIECE = 32 / STEPS;     // logits a step
         uint32_t k_here = k_at, v_here = v_at;
         asm volatile("" : "+v"(k_here), "+v"(v_here));      // (places turned anew each time: kept, they would spill)
-        const float neg_m = run_m == -INFINITY ? 0.f : -run_m * scale_log2e;
+        float neg_m = run_m == -INFINITY ? 0.f : -run_m * scale_log2e;
+        if (__any(!(fabsf(neg_m) < FAR_REFERENCE))) {
+            const float from = run_m == -INFINITY ? 0.f : run_m;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) now[t][v] -= from;
+            neg_m = 0.f;
+        }
         float sum[4] = {};
         uint32_t p[16];                       // probabilities, pairs of slots
         uint2 vf[4][2];                       // values' fragments: of step n (of 4 DB) in vf[n % 4]
