@@ -348,7 +348,8 @@ __device__ __forceinline__ void few_rows(const PagesView& cache, const PagesAtte
             }
         if (used == 1) {
             const int row = span.row0 + r / group, head = h * group + r % group;
-            const float inv = l == 0.f ? 0.f : 1.f / l;      // (nothing seen, or nothing above -infinity: zeros)
+            if (l == 0.f) acc = make_float4(0.f, 0.f, 0.f, 0.f);     // (nothing seen, or nothing above -infinity: whatever the values are)
+            const float inv = l == 0.f ? 0.f : 1.f / l;
             *reinterpret_cast<uint2*>(const_cast<bf16_t*>(a.out.p) + (int64_t)row * a.out.token + (int64_t)head * a.out.head + ch) =
                 make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
             if (a.lse && ch == 0) a.lse[(size_t)row * a.H + head] = l == 0.f ? -INFINITY : m * a.scale + logf(l);
@@ -889,6 +890,11 @@ __device__ __forceinline__ void many_rows(const PagesView& cache, const PagesAtt
                     make_float4(o_acc[d][v4 * 4], o_acc[d][v4 * 4 + 1], o_acc[d][v4 * 4 + 2], o_acc[d][v4 * 4 + 3]);
         return;
     }
+    if (l == 0.f)                              // (zeros, whatever the values are)
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) o_acc[d][v] = 0.f;
     const float inv = l == 0.f ? 0.f : 1.f / l;
     if (n.a.lse && fg == 0) n.a.lse[(size_t)to * n.a.H + head] = l == 0.f ? -INFINITY : run_m * n.a.scale + logf(l);
     bf16_t* orow = const_cast<bf16_t*>(n.a.out.p) + (int64_t)to * n.a.out.token + (int64_t)head * n.a.out.head;
@@ -997,6 +1003,7 @@ __global__ __launch_bounds__(JOIN_WAVES * 64) void join_pages_kernel(PagesView c
             acc[k].x += __shfl_xor(acc[k].x, o), acc[k].y += __shfl_xor(acc[k].y, o), acc[k].z += __shfl_xor(acc[k].z, o),
                 acc[k].w += __shfl_xor(acc[k].w, o);
         if (share || used[k] <= 1) continue;
+        if (l[k] == 0.f) acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
         const float inv = l[k] == 0.f ? 0.f : 1.f / l[k];
         const int head = head0 + k;
         *reinterpret_cast<uint2*>(const_cast<bf16_t*>(a.out.p) + (int64_t)to * a.out.token + (int64_t)head * a.out.head + ch) =
