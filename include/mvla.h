@@ -722,7 +722,7 @@ int mvla_pages_read(mvla_ctx* ctx, const mvla_pages* pages, const mvla_page_batc
  * q, out: bf16 [n, H, dh] by their strides (`sample` is not used), channel == 1, 16-byte aligned
  *         rows; must not overlap.  lse: device fp32 [n, H] or NULL.
  * max_q, max_length: bounds on the c_b and on length that size the launch; rows from max_q on are
- *         left as they were, lengths are clamped to max_length.  scale: finite, > 0.
+ *         left as they were, lengths are clamped to max_length.  scale: > 0, below 2.35e38 (times log2 e finite).
  * Products of bf16 queries with the cache's values, 32-bit sums; probabilities are rounded to
  * bf16 for the second product only.  Every sum has a fixed order for one workspace size. */
 int mvla_pages_attention(mvla_ctx* ctx, const mvla_pages* pages, const mvla_page_batch* batch, const mvla_rows* q,

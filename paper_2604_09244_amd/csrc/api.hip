@@ -1401,7 +1401,7 @@ int mvla_pages_attention(mvla_ctx* ctx, const mvla_pages* pages, const mvla_page
     if (int rc = check_page_batch(batch, *pages, true)) return rc;
     if (H <= 0 || H % pages->H_kv != 0 || max_q <= 0 || max_length <= 0 || max_length > batch->table_pitch * pages->page)
         return MVLA_EINVAL;
-    if (!(scale > 0.f) || !(scale <= 3.0e38f)) return MVLA_EINVAL;
+    if (!(scale > 0.f) || !(scale * 1.4426950408889634f < INFINITY)) return MVLA_EINVAL;     // (the kernels take it times log2 e)
     if (n == 0) return MVLA_OK;
     if (!q || !out || !q->data || !out->data || (lse && !aligned(lse, 4))) return MVLA_EINVAL;
     CacheRows qr = cache_rows(*q), outr = cache_rows(*out);
