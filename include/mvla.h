@@ -735,8 +735,8 @@ int mvla_pages_attention(mvla_ctx* ctx, const mvla_pages* pages, const mvla_page
  *   top_token[b, r], top_logprob[b, r]: the r-th token in descending order of logits (equal
  *   logits: lower index first) and its y; where fewer than `top` logits are above -infinity, -1 and
  *   -infinity.
- * NaN logits count as -infinity; +inf ones share everything; a row without any logit above
- * -infinity has log probabilities of -infinity and entropy 0.  temperature not above 0 (or
+ * NaN logits count as -infinity; +inf ones share everything, at any temperature; a row without any logit
+ * above -infinity has log probabilities of -infinity and entropy 0.  temperature not above 0 (or
  * NaN): the first token of the order has y = 0, all others -infinity (as mvla_sample chooses).
  * logits: device, bf16 (half != 0) or fp32 [B, V], rows row_stride elements apart; V <= 2^22.
  * temperature: device fp32 [B] or NULL (1).  tokens: device int32 [B, n_tokens], n_tokens >= 0.

@@ -114,7 +114,9 @@ __device__ __forceinline__ void lp_finish(const LpArgs& a, const LpRow& r, int r
     auto value = [&](float x, bool first) __attribute__((always_inline)) {
         if (none || !(x > -INFINITY)) return -INFINITY;
         if (r.greedy) return first ? 0.f : -INFINITY;
-        return x == s.m ? -log_s : (float)(((double)x - (double)s.m) / (double)r.T) - log_s;
+        if (x == s.m) return -log_s;
+        // (beside a logit of +infinity the others have nothing, at any temperature)
+        return s.m == INFINITY ? -INFINITY : (float)(((double)x - (double)s.m) / (double)r.T) - log_s;
     };
     const uint32_t first = r.greedy ? lp_index(best[0]) : 0u;
     for (int j = tid; j < a.n_tokens; j += LP_THREADS) {
