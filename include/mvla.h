@@ -738,7 +738,7 @@ int mvla_pages_attention(mvla_ctx* ctx, const mvla_pages* pages, const mvla_page
  * NaN logits count as -infinity; +inf ones share everything, at any temperature; a row without any logit
  * above -infinity has log probabilities of -infinity and entropy 0.  temperature not above 0 (or
  * NaN): the first token of the order has y = 0, all others -infinity (as mvla_sample chooses).
- * logits: device, bf16 (half != 0) or fp32 [B, V], rows row_stride elements apart; V <= 2^22.
+ * logits: device, bf16 (half != 0) or fp32 [B, V], rows row_stride elements apart; B >= 1, V: 1 .. 2^22.
  * temperature: device fp32 [B] or NULL (1).  tokens: device int32 [B, n_tokens], n_tokens >= 0.
  * logprob: device fp32 [B, n_tokens].  entropy: device fp32 [B] or NULL.
  * top: 0 .. 32; top_token: device int32 [B, top], top_logprob: device fp32 [B, top]. */

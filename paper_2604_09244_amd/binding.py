@@ -916,7 +916,7 @@ class Context:
         """Log probabilities of the given tokens (int32 [B, m] or [B], None: of none) in each row of
         logits [B, V] (bf16 or fp32, rows of any stride), the rows' entropies and the ``top`` (up to 32)
         most likely tokens.  Returns (logprob, shaped as tokens, or None; entropy [B]; top_token int32
-        [B, top] and top_logprob [B, top], or None)."""
+        [B, top] and top_logprob [B, top], or None); B may be 0."""
         B, V = logits.shape
         half, f32 = logits.dtype == torch.bfloat16, torch.float32
         assert logits.get_device() == self._index and (half or logits.dtype == f32), (logits.device, logits.dtype)
@@ -938,6 +938,8 @@ class Context:
             assert tokens is None or self._is(logprob, f32, tokens.shape)
             assert entropy is None or self._is(entropy, f32, (B,))
             assert not top or (self._is(top_token, torch.int32, (B, top)) and self._is(top_logprob, f32, (B, top)))
+        if B == 0 and V and top <= 32:     # (no rows, which the library's call refuses)
+            return logprob, entropy, top_token, top_logprob
         _check(load().mvla_logprobs(self._h, logits.data_ptr(), half, logits.stride(0), B, V, _ptr(temperature),
                                     _ptr(tokens), m, _ptr(logprob), _ptr(entropy), top, _ptr(top_token),
                                     _ptr(top_logprob)), "mvla_logprobs")
