@@ -679,7 +679,9 @@ typedef struct {
  * number outside [0, n_pages) is no page: rows for it are not written, its slots read as zero
  * and are seen by no query.  Pages may be shared for reading; of two rows that one call writes
  * to one slot, either's values may remain, or parts of both.
- * length counts the new rows already; it is clamped to [0, table_pitch * page]. */
+ * length counts the new rows already; it is clamped to [0, table_pitch * page]: a sequence that has
+ * outgrown its table is taken as one that fills it, whose new rows are the table's last slots (what
+ * lay there is overwritten by an append; a caller that wants to keep it hands out another page first). */
 typedef struct {
     int B;                     /* sequences                                             */
     const int32_t* start;      /* device int32 [B + 1], ascending                       */
@@ -695,7 +697,8 @@ typedef struct {
 size_t mvla_pages_workspace_bytes(int B, int H, int H_kv, int dh, int n, int max_q, int max_length);
 
 /* Write new key and value rows: row i of sequence b's count c_b = start[b+1] - start[b] goes
- * to slot length[b] - c_b + i; slots below 0 or beyond the table are not written.
+ * to slot length[b] - c_b + i of the clamped length (so never beyond the table); slots below 0 are
+ * not written.
  * bits 16: as they are.  bits 8: magnitudes of finite values are limited to 247 * 2^120; a
  * block's power is the smallest 2^(e-127), 0 <= e, under which its largest magnitude is below
  * 464; each value is rounded to the nearest code, ties to the even one: finite values stay

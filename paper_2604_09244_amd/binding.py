@@ -861,7 +861,8 @@ class Context:
 
     def pages_append(self, cache: PagedCache, batch: PageBatch, k: torch.Tensor, v: torch.Tensor):
         """Write rows k, v [n, H_kv, dh] (bf16, any strides), packed as ``batch.start`` says, as the last
-        ones of each sequence's ``length`` (which counts them already)."""
+        ones of each sequence's ``length`` (which counts them already; one beyond the table counts as the
+        table's, so that its last slots are overwritten)."""
         n, H, dh = k.shape
         on = self._index
         assert k.shape == v.shape and H == cache.H_kv and dh == cache.dh, (k.shape, v.shape)
