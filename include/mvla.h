@@ -646,8 +646,8 @@ int mvla_rotation_table(mvla_ctx* ctx, const mvla_rotation* how, int rope_len, f
  * q, q_out: bf16 [B, n, H, dh], k, k_out: bf16 [B, n, H_kv, dh] by their strides; an output
  * is either its input (same address and strides) or shares no memory with any input.
  * k, k_out NULL: queries alone.  pos: device int32 [B, n], clamped to [0, rope_len).
- * dh: 2 .. 256; rotated <= dh.  channel == 1 with 16-byte aligned rows and dh a multiple of 8
- * is the fast form, any other is taken as well. */
+ * dh: 2 .. 256; rotated <= dh; H + H_kv < 2^15, B * n < 2^30, B * n * (H + H_kv) * dh < 2^31.
+ * channel == 1 with 16-byte aligned rows and dh a multiple of 8 is the fast form, any other is taken as well. */
 int mvla_rotate(mvla_ctx* ctx, const mvla_rows* q, int H, const mvla_rows* q_out, const mvla_rows* k,
                 int H_kv, const mvla_rows* k_out, const int32_t* pos, int B, int n, int dh, int rotated,
                 int interleaved, int inverse, const float* rope_cos, const float* rope_sin, int rope_len);
@@ -662,7 +662,7 @@ int mvla_rotate(mvla_ctx* ctx, const mvla_rows* q, int H, const mvla_rows* q_out
  * anything. */
 typedef struct {
     int n_pages;       /* 1 .. 2^30                                                     */
-    int H_kv;          /* key heads                                                     */
+    int H_kv;          /* key heads: 1 .. 2^15 - 1                                      */
     int dh;            /* head dim: 64 or 128                                           */
     int page;          /* slots a page: 16, 32, 64, 128 or 256                          */
     int bits;          /* 16 or 8                                                       */
@@ -683,7 +683,7 @@ typedef struct {
  * outgrown its table is taken as one that fills it, whose new rows are the table's last slots (what
  * lay there is overwritten by an append; a caller that wants to keep it hands out another page first). */
 typedef struct {
-    int B;                     /* sequences                                             */
+    int B;                     /* sequences: 1 .. 2^16 - 1, B * H_kv <= 2^22             */
     const int32_t* start;      /* device int32 [B + 1], ascending                       */
     const int32_t* length;     /* device int32 [B]: slots in use                        */
     const int32_t* table;      /* device int32 [B, table_pitch]: pages                  */
@@ -698,7 +698,7 @@ size_t mvla_pages_workspace_bytes(int B, int H, int H_kv, int dh, int n, int max
 
 /* Write new key and value rows: row i of sequence b's count c_b = start[b+1] - start[b] goes
  * to slot length[b] - c_b + i of the clamped length (so never beyond the table); slots below 0 are
- * not written.
+ * not written.  n * H_kv * dh < 2^34.
  * bits 16: as they are.  bits 8: magnitudes of finite values are limited to 247 * 2^120; a
  * block's power is the smallest 2^(e-127), 0 <= e, under which its largest magnitude is below
  * 464; each value is rounded to the nearest code, ties to the even one: finite values stay
@@ -712,7 +712,7 @@ int mvla_pages_append(mvla_ctx* ctx, const mvla_pages* pages, const mvla_page_ba
  * Slots below 0, beyond the table or without a page read as zero.  (batch->start and ->length
  * are not used and may be NULL.)
  * first: device int32 [B] or NULL (0).  k_out, v_out: device bf16 [B, H_kv, n, dh], 16-byte
- * aligned. */
+ * aligned.  n * H_kv * dh < 2^34. */
 int mvla_pages_read(mvla_ctx* ctx, const mvla_pages* pages, const mvla_page_batch* batch, const int32_t* first,
                     int n, void* k_out, void* v_out);
 
@@ -726,6 +726,7 @@ int mvla_pages_read(mvla_ctx* ctx, const mvla_pages* pages, const mvla_page_batc
  *         rows; must not overlap.  lse: device fp32 [n, H] or NULL.
  * max_q, max_length: bounds on the c_b and on length that size the launch; rows from max_q on are
  *         left as they were, lengths are clamped to max_length.  scale: > 0, below 2.35e38 (times log2 e finite).
+ * n * H < 2^28.
  * Products of bf16 queries with the cache's values, 32-bit sums; probabilities are rounded to
  * bf16 for the second product only.  Every sum has a fixed order for one workspace size. */
 int mvla_pages_attention(mvla_ctx* ctx, const mvla_pages* pages, const mvla_page_batch* batch, const mvla_rows* q,
@@ -743,7 +744,7 @@ int mvla_pages_attention(mvla_ctx* ctx, const mvla_pages* pages, const mvla_page
  * NaN): the first token of the order has y = 0, all others -infinity (as mvla_sample chooses).
  * logits: device, bf16 (half != 0) or fp32 [B, V], rows row_stride elements apart; B >= 1, V: 1 .. 2^22.
  * temperature: device fp32 [B] or NULL (1).  tokens: device int32 [B, n_tokens], n_tokens >= 0.
- * logprob: device fp32 [B, n_tokens].  entropy: device fp32 [B] or NULL.
+ * logprob: device fp32 [B, n_tokens], B * n_tokens < 2^31.  entropy: device fp32 [B] or NULL.
  * top: 0 .. 32; top_token: device int32 [B, top], top_logprob: device fp32 [B, top]. */
 int mvla_logprobs(mvla_ctx* ctx, const void* logits, int half, int64_t row_stride, int B, int V,
                   const float* temperature, const int32_t* tokens, int n_tokens, float* logprob, float* entropy,
