@@ -80,7 +80,7 @@ constexpr int NO_SLOT = 0x7fffffff;
 //      dims into pairs of slots of one dim
 //   O^T: tile d holds dims c CH + d, so a lane ends with CH consecutive dims per register index
 // A step lies in one page, or its halves in two: where they are comes from scalar loads, a round ahead.
-// Bound by memory: every cached row is read once.  16 sequences of 2624 slots, 32 heads of 16 bits: 112 us, 6.1 TB/s (values kept
+// Bound by memory: every cached row is read once.  16 sequences of 2624 slots, 32 heads of 16 bits: 110 us, 6.2 TB/s (values kept
 // in caches: 121; keys past them too, whose reads are of half lines: 118).  64 of up to 16384 slots, 8 key heads of 8 bits with
 // four query heads each: 257 us, 5.6 TB/s.
 constexpr int FEW_STEP = 32, FEW_ROWS = 16;
@@ -376,9 +376,11 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void few_pages_kern
 // bits 2 and 3 of the slot swapped, so that a lane's eight probabilities of a 16-slot step are eight consecutive slots;
 // values lie row by row, and the reads that transpose 4 x 16 of them give a lane four slots of one dim.
 // In turn: the keys of the next tile are multiplied while this tile's logits become probabilities, this tile's values are
-// multiplied while the next tile's maxima are found.  So the matrix cores have work that waits for no vector
-// operation; two keys' and two values' tiles are in LDS, the next ones on their way.
-// Bound by the matrix products and the exponentials beside them.  2048 tokens behind 14336, 32 heads of 128: 537 to 569 us, 0.91 to 0.96 PFLOP/s.
+// multiplied while the next tile's maxima are found.  So there are products that wait for no vector operation; two
+// keys' and two values' tiles are in LDS, the next ones on their way.
+// Bound by matrix and vector operations, which still mostly take turns: products are under way 44 % of the time, vector operations
+// issue 38 %.  (All of a tile's exponentials lie beside the keys' products, whose pairs are issued before them.)  2048 tokens behind
+// 14336, 32 heads of 128: 546 to 571 us, 0.90 to 0.94 PFLOP/s.
 constexpr int MANY_KT = 64, MANY_WAVE_ROWS = 32;
 constexpr float SLACK = 8.f;
 
@@ -671,8 +673,8 @@ __device__ __forceinline__ void many_rows(const PagesView& cache, const PagesAtt
         m = max_of(s);
     };
     // The sums' reference stays until a logit passes it by SLACK in powers of two: exponentials are at most 2^SLACK then,
-    // and the sums are hardly ever scaled again after the first tiles.  (With SLACK 0 a pass of 595 us took 621; outputs
-    // are 0.0023 of their RMS off instead of 0.0020, 0.0017 of which is their own rounding.)
+    // and the sums are hardly ever scaled again after the first tiles.  (With SLACK 0 a pass of 564 us took 584; outputs
+    // are 0.0022 to 0.0023 of their RMS off instead of 0.0019 to 0.0022, 0.0017 of which is their own rounding.)
     auto rescale = [&](float tile_m) __attribute__((always_inline)) {
         const float new_m = (tile_m - run_m) * scale_log2e > SLACK ? tile_m : run_m;
         if (__any(new_m != run_m)) {
@@ -934,7 +936,7 @@ __global__ __launch_bounds__(MANY_WAVES * 64, 2) void mixed_pages_kernel(MixedAr
 // ---- the parts of a row --------------------------------------------------------------------------------------------
 // A wave takes a token's rows of JOIN_HEADS heads, whose loads do not wait for each other; lane p knows part p's maximum and
 // sum, half a wave (of 128 dims) adds every second part.
-// Bound by memory where there is much (543 tokens of 32 heads in up to four parts: 11.7 us), by its launch where
+// Bound by memory where there is much (543 tokens of 32 heads in up to four parts: 12 us), by its launch where
 // there is little (64 rows of 32 heads in up to 8 parts: 8.5).
 constexpr int JOIN_WAVES = 4, JOIN_HEADS = 4, MAX_PARTS = 64;
 

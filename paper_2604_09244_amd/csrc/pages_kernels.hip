@@ -19,8 +19,8 @@ __device__ __forceinline__ uint32_t limited(uint32_t pair) {
 // ---- rows into pages ---------------------------------------------------------------------------------------------
 // A lane takes eight values of a token's row (16 bytes, whole lines per wave), of STORE_TURNS rows, whose loads do not wait for
 // each other; four lanes are a block of 32 and agree on its largest magnitude by two quad permutes.  blockIdx.y: keys or values.
-// Bound by memory: 2 bytes in, 1 + 1/32 (or 2) out a value.  16 sequences of 1344 tokens to 8 bits: 73 us, 5.5 TB/s (with one
-// row a lane 6 more).
+// Bound by memory: 2 bytes in, 1 + 1/32 (or 2) out a value.  16 sequences of up to 1344 new tokens to 8 bits (335 MB): 71
+// to 80 us, 4.2 to 4.7 TB/s (with one row a lane 6 more).
 constexpr int STORE_THREADS = 256, STORE_TURNS = 4;
 
 template <int DH, int BITS, int TURNS>
@@ -106,7 +106,7 @@ int launch_pages_append(const PagesView& c, const int32_t* start, const int32_t*
 
 // ---- rows out of pages -------------------------------------------------------------------------------------------
 // A lane writes 16 bytes of bf16 of each of STORE_TURNS rows: whole lines out per wave.
-// Bound by memory: 1 + 1/32 (or 2) bytes in, 2 out a value.  16 sequences of 1344 rows from 8 bits: 67 us, 6.0 TB/s (with
+// Bound by memory: 1 + 1/32 (or 2) bytes in, 2 out a value.  16 sequences of 1344 rows from 8 bits (471 MB): 65 us, 7.2 TB/s (with
 // stores through the caches 20 more, with one row a lane another 30).
 template <int DH, int BITS>
 __global__ __launch_bounds__(STORE_THREADS) void pages_read_kernel(PagesView c, const int32_t* __restrict__ first, int n,
