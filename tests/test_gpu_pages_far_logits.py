@@ -1,6 +1,6 @@
 """Attention over pages where logits are finite and far from zero.
 
-Inputs whose logits fp32 holds exactly.  Near ones: a constant from dim 0 (2^10 times 2^7 to 3 2^10, either sign), and from dim 32
+Inputs whose logits fp32 holds exactly.  Near ones: a constant from dim 0 (2^10 times 2^7 to 2560, either sign), and from dim 32
 (another block of the cache in 8 bits) 1 times a number of at most four bits between -7 and 7; the sum is a multiple of a
 quarter below 2^24 of them.  Apart ones: one dim alone, a product of two bf16 numbers.
 
@@ -40,7 +40,7 @@ FEW = np.array([0, 0.25, 0.5, 0.75, 1, 1.25, 1.5, 1.75, 2, 2.5, 3, 3.5, 4, 5, 6,
 @pytest.mark.parametrize("bits", [16, 8])
 @pytest.mark.parametrize("dh", [64, 128])
 @pytest.mark.parametrize("counts,lengths", [((3, 1), (90, 700)), ((40, 33), (300, 64)), ((1, 1), (5000, 40)), ((60, 1), (5000, 2049))])
-@pytest.mark.parametrize("far", [2.0 ** 7, -2.0 ** 11, 3 * 2.0 ** 10])
+@pytest.mark.parametrize("far", [2.0 ** 7, -2.0 ** 11, 2560.0])
 def test_near_each_other(far, counts, lengths, dh, bits):
     rng = np.random.default_rng(dh + bits + counts[0])
     H, T = 2, max(lengths)
